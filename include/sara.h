@@ -330,6 +330,122 @@ SARA_API int sara_attention_decode(const uint16_t *q, const uint16_t *kv, int64_
 SARA_API int sara_sample(const float *logits, int32_t R, int32_t V, uint64_t sample_seed,
                          const int64_t *uid, const int32_t *t, int32_t *token, void *stream);
 
+/* ---------------------------------------------------------------------------------------
+ * An 8-bit paged KV cache: writing tokens into it, reading them back, and decode attention over it.
+ * Device pointers, work is issued on `stream` and not waited for, nothing is allocated: the calls may be
+ * captured into a CUDA graph.  Device arrays that hold lengths, positions and block ids are checked by the
+ * kernels: what they say never makes a kernel leave its buffers, and a sequence that they describe wrongly
+ * (below) sets *status to SARA_EINVAL (one int32 on the device, or NULL; never cleared by the library).
+ * ------------------------------------------------------------------------------------- */
+
+/* 16- and 32-bit types of operands. */
+#define SARA_BF16 0
+#define SARA_FP16 1
+#define SARA_FP32 2
+
+/* Formats of the cache's codes. */
+#define SARA_KV8_E4M3 0    /* 8-bit floating point, 3 bits of fraction, largest value 448 */
+#define SARA_KV8_INT8 1    /* whole numbers -127 .. 127 */
+
+#define SARA_KV8_PAGE 128  /* positions of a block of the paged cache */
+#define SARA_KV8_SCALE 32  /* consecutive positions (of one KV head, K or V) that share a scale */
+
+/*
+ * value = code * scale.  A scale is a power of two 2^e, e the smallest integer >= -100 for which the largest
+ * magnitude of its 32 positions is at most 448 * 2^e (E4M3) or 127 * 2^e (INT8), so that raising it later (a
+ * larger token joins the block) changes the codes already there by no more than the bits that fall off their
+ * lower end: what is read back is off by at most half a step of the format at that value (E4M3: 2^-4 of the
+ * value), or one step of the smallest codes (2^-9 scale; INT8: scale) where the scale was raised.
+ * A NaN or an infinity makes its block's scale NaN: the whole block then reads as NaN, until it is written again
+ * from its first position on.
+ */
+typedef struct {
+    uint8_t *codes;          /* [n_blocks][2 (K, V)][n_kv_heads][128][head_dim], 16-byte aligned */
+    float *scales;           /* [n_blocks][2 (K, V)][n_kv_heads][4] */
+    const int32_t *table;    /* [n_seq][table_stride]: sequence i's position p is in block
+                                table[i * table_stride + p / 128] */
+    int64_t table_stride;    /* >= max_blocks */
+    int32_t n_blocks;
+    int32_t max_blocks;      /* entries of a table row: positions are < 128 * max_blocks */
+    int32_t n_kv_heads;
+    int32_t head_dim;        /* 32, 64 or 128 */
+    int32_t format;          /* SARA_KV8_* */
+} sara_kv8_cache;
+
+/*
+ * Quantise new tokens into the cache.  Sequence i's tokens are rows seq_start[i] .. seq_start[i + 1] of k and v
+ * (seq_start [n_seq + 1], non-decreasing, at most total; rows behind the last sequence are not read) and take its positions
+ * pos0[i], pos0[i] + 1, ...  One token each is a decode step's append, whole prompts a prefill.  Positions
+ * before pos0[i] keep their values (their codes are rescaled where a new token raises the block's scale); a block written from its
+ * first position on takes a new scale; codes at positions behind the new tokens are left as they are and no longer mean
+ * anything in a block that was written to.  A scale only rises until its block is written from its first position on.
+ * k, v: [total] rows of [n_kv_heads][head_dim] (type SARA_BF16 or SARA_FP16), k_stride and v_stride elements apart (multiples of 8),
+ * 16-byte aligned.  The blocks that a call writes to belong to one sequence each (shared blocks are for reading).
+ * A sequence with a wrong range (seq_start, pos0, past max_blocks) is not written, nor is a block whose id is not in
+ * [0, n_blocks); both set *status.
+ */
+SARA_API int sara_kv8_write(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *pos0, const int32_t *seq_start,
+                            int32_t total, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t type,
+                            int32_t *status, void *stream);
+
+/*
+ * Read tokens back: row seq_start[i] + j of k and v receives position pos0[i] + j of sequence i, rounded once to `type`
+ * (any SARA_* type).  Layout as sara_kv8_write.  Rows that belong to no sequence are left as they are.
+ * Positions outside the table or in a block whose id is wrong read as NaN and set *status.
+ */
+SARA_API int sara_kv8_read(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *pos0, const int32_t *seq_start,
+                           int32_t total, void *k, int64_t k_stride, void *v, int64_t v_stride, int32_t type, int32_t *status,
+                           void *stream);
+
+/*
+ * Decode attention over the cache: out[i][h] = softmax(q[i][h] . K / sqrt(head_dim)) V over the positions
+ * first[i] <= p < ctx[i] of sequence i (first NULL: 0), one query row per sequence, n_heads / n_kv_heads in 1..8
+ * query heads to a KV head.  A row without a position (ctx[i] <= first[i]) gives 0.
+ * q, out: [n_seq][n_heads][head_dim] of `type` (SARA_BF16 or SARA_FP16), rows of q q_stride elements apart (a multiple of 8),
+ * both 16-byte aligned.  lse: [n_seq][n_heads] fp32 or NULL, the natural logarithm of the sum of the exponentiated scores
+ * (-inf for a row without a position).  Masked positions and positions behind ctx are not read.
+ * A row with ctx outside [0, 128 * max_blocks], first < 0 or a block id outside [0, n_blocks) gives NaN and sets *status.
+ * workspace: sara_attention_kv8_workspace_bytes(...) bytes of device scratch, 16-byte aligned, all zero on first use and left
+ * zero where it has to be; calls that share one must not overlap.
+ */
+SARA_API size_t sara_attention_kv8_workspace_bytes(int32_t n_seq, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim);
+SARA_API int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_t n_heads, const void *q,
+                                       int64_t q_stride, const int32_t *ctx, const int32_t *first, void *out, float *lse,
+                                       int32_t type, int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Scoring of sampled tokens, next to sara_sample: log-probabilities of given tokens under softmax(logits), with each row's
+ * entropy and top alternatives, and the gradient of both.  Device pointers, not waited for, nothing allocated.
+ * ------------------------------------------------------------------------------------- */
+
+/*
+ * logits [R] rows of V values (`type`: any SARA_* type), row_stride >= V elements apart, aligned to their type.  With m = max_v z_v and
+ * S = sum_v exp(z_v - m), all in fp32:
+ *   logprob[r] = z[token] - m - log S                        entropy[r] = log S - sum_v exp(z_v - m) (z_v - m) / S
+ *   stats[r] = {m, log S}                                    (what sara_logprobs_backward wants)
+ *   top_token[r][0..top), top_logprob[r][0..top): the `top` (0..32) most probable tokens in falling order, ties to the lowest id.
+ *     Tokens of logit -inf or NaN are not listed; unused places hold -1 and -inf.
+ * tokens [R] int32: a negative one marks a row of padding, which is not read (logprob 0, entropy 0, stats {0, 0}, no alternatives); one
+ * >= V gives the logprob NaN.  A row whose logits are all -inf has logprob -inf, entropy 0, stats {-inf, 0}; a NaN or +inf
+ * among the logits makes logprob, entropy, log S and every top_logprob of the row NaN.
+ * Each output may be NULL, and tokens too where logprob is (every row is then live); top_token and top_logprob go together with top > 0.
+ */
+SARA_API int sara_logprobs(const void *logits, int64_t row_stride, int32_t type, int32_t R, int32_t V, const int32_t *tokens,
+                           int32_t top, float *logprob, float *entropy, float *stats, int32_t *top_token, float *top_logprob,
+                           void *stream);
+
+/*
+ * The gradient with respect to the logits, p = softmax(z) of the row:
+ *   grad_logits[r][v] = grad_logprob[r] (1[v = token[r]] - p_v) - grad_entropy[r] p_v (log p_v + entropy[r])
+ * rounded once to the logits' type.  stats and entropy as sara_logprobs gave them for the same logits and tokens.
+ * grad_logprob and grad_entropy [R] fp32, each may be NULL (0); entropy is wanted with grad_entropy, tokens with grad_logprob.  grad_logits:
+ * rows grad_stride >= V elements apart; it may be `logits` itself (same stride).  Rows of padding and rows whose logits are all
+ * -inf get 0; a token >= V, a NaN or +inf among the logits makes the row NaN.
+ */
+SARA_API int sara_logprobs_backward(const void *logits, int64_t row_stride, int32_t type, int32_t R, int32_t V,
+                                    const int32_t *tokens, const float *stats, const float *entropy, const float *grad_logprob,
+                                    const float *grad_entropy, void *grad_logits, int64_t grad_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -24,6 +24,26 @@ inline void check_cuda(cudaError_t e, const char *what, const char *file, int li
 }
 #define CK(x) ::sara::check_cuda((x), #x, __FILE__, __LINE__)
 
+inline int sm_count() {
+    int dev = 0, sms = 0;
+    CK(cudaGetDevice(&dev));
+    CK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    return sms;
+}
+
+// Runs an entry point's body: the code it returns, no exception past the C boundary.
+template <typename F>
+inline int op_guard(F fn) {
+    try {
+        fn();
+        return SARA_OK;
+    } catch (const SaraError &e) {
+        return e.code;
+    } catch (...) {
+        return SARA_EDEVICE;
+    }
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *,
                                   const cuuint64_t *, const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave,
                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);

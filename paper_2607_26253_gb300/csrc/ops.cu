@@ -35,13 +35,6 @@ int gemm_rows_sms() {
 
 namespace {
 
-int sm_count() {
-    int dev = 0, sms = 0;
-    CK(cudaGetDevice(&dev));
-    CK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    return sms;
-}
-
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // The workspace of the GEMM's contract (the kernel no longer uses it; sizes unchanged).
@@ -63,18 +56,6 @@ void launch_g(dim3 grid, int G, cudaStream_t s, const AttnParams &a) {
         case 4: attn_rows_kernel<HD, 4><<<grid, kAttnThreads, 0, s>>>(a); break;
         case 6: attn_rows_kernel<HD, 6><<<grid, kAttnThreads, 0, s>>>(a); break;
         default: attn_rows_kernel<HD, 8><<<grid, kAttnThreads, 0, s>>>(a); break;
-    }
-}
-
-template <typename F>
-int op_guard(F fn) {
-    try {
-        fn();
-        return SARA_OK;
-    } catch (const SaraError &e) {
-        return e.code;
-    } catch (...) {
-        return SARA_EDEVICE;
     }
 }
 
