@@ -2,6 +2,8 @@
 //   m = max z, S = sum e^(z - m), T = sum e^(z - m) (z - m)
 //   logprob = z[token] - m - log S,   entropy = log S - T / S
 //   dz_v = g (1[v = token] - p_v) - g' p_v (log p_v + entropy)
+// Both are bound by reading (and for the gradient writing) the logits once: 16 bytes a lane, a step's loads in flight during the
+// one before, sums in fp32 against the thread's own running maximum.
 #pragma once
 #include "device_common.cuh"
 #include "host_util.h"
@@ -9,12 +11,79 @@
 namespace sara {
 
 constexpr int kScoreMaxTop = 32;
+constexpr float kLog2e = 1.44269504f;
 
+// exp of a difference d <= 0 (or NaN): 2^-22 relative, 0 below 2^-126
+__device__ __forceinline__ float exp_neg(float d) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(d * kLog2e));
+    return y;
+}
+
+// The same down to the subnormal range, where a gradient's factors may still bring it back into the normal one
+__device__ __forceinline__ float exp_neg_full(float d) {
+    float y;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(d * kLog2e));
+    return y;
+}
+
+// A row's elements as the aligned 16-byte vectors that hold them: vector k has elements k E - off .. + E - 1, of
+// which those in [0, V) are the row's.
+template <int TYPE>
+struct RowVectors {
+    static constexpr int kSize = TYPE == SARA_FP32 ? 4 : 2, E = 16 / kSize;
+    static constexpr uint32_t kNone = TYPE == SARA_FP32 ? 0xff800000u : TYPE == SARA_BF16 ? 0xff80ff80u : 0xfc00fc00u;  // -inf
+    const uint8_t *base;  // of vector 0
+    uint32_t off, V;
+    __device__ __forceinline__ RowVectors(const void *z, int64_t row, int64_t stride, int V_) {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(z) + (uintptr_t)(row * stride * kSize);
+        off = (uint32_t)(a & 15) / kSize;
+        base = reinterpret_cast<const uint8_t *>(a & ~(uintptr_t)15);
+        V = (uint32_t)V_;
+    }
+    __device__ __forceinline__ int vectors() const { return (int)((off + V + (E - 1)) / E); }
+    __device__ __forceinline__ uint32_t first(int k) const { return (uint32_t)k * E - off; }  // (wraps below 0 for k = 0)
+    __device__ __forceinline__ bool whole(int k) const { return first(k) < V && V - first(k) >= (uint32_t)E; }
+    // The row's elements of vector k, -inf in the place of others.  (Plain loads: the gradient may take the logits' place.)
+    __device__ __forceinline__ uint4 load(int k) const {
+        const uint8_t *p = base + (int64_t)k * 16;
+        if (whole(k)) return *reinterpret_cast<const uint4 *>(p);
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = kNone;
+            if constexpr (TYPE == SARA_FP32) {
+                if (first(k) + i < V) w[i] = reinterpret_cast<const uint32_t *>(p)[i];
+            } else {
+                if (first(k) + 2 * i < V) w[i] = (w[i] & 0xffff0000u) | reinterpret_cast<const uint16_t *>(p)[2 * i];
+                if (first(k) + 2 * i + 1 < V) w[i] = (w[i] & 0xffffu) | (uint32_t)reinterpret_cast<const uint16_t *>(p)[2 * i + 1] << 16;
+            }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+template <int TYPE>
+__device__ __forceinline__ void unpack_vector(const uint4 &x, float (&z)[16 / (TYPE == SARA_FP32 ? 4 : 2)]) {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (TYPE == SARA_FP32) {
+            z[i] = __uint_as_float(w[i]);
+        } else if constexpr (TYPE == SARA_BF16) {
+            z[2 * i] = __uint_as_float(w[i] << 16);
+            z[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        } else {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[i]));
+            z[2 * i] = f.x;
+            z[2 * i + 1] = f.y;
+        }
+    }
+}
 template <int TYPE>
 __device__ __forceinline__ float load_logit(const void *z, int64_t i) {
-    if constexpr (TYPE == SARA_FP32) return __ldg(static_cast<const float *>(z) + i);
-    else if constexpr (TYPE == SARA_BF16) return bf16_to_f32(__ldg(static_cast<const uint16_t *>(z) + i));
-    else return f16_to_f32(__ldg(static_cast<const uint16_t *>(z) + i));
+    if constexpr (TYPE == SARA_FP32) return static_cast<const float *>(z)[i];
+    else if constexpr (TYPE == SARA_BF16) return bf16_to_f32(static_cast<const uint16_t *>(z)[i]);
+    else return f16_to_f32(static_cast<const uint16_t *>(z)[i]);
 }
 
 struct ScoreParams {
@@ -25,92 +94,245 @@ struct ScoreParams {
     float *logprob, *entropy, *stats;
     int32_t *top_token;
     float *top_logprob;
+    int ctas;  // a row
 };
 
-// A logit's place in the order of the alternatives: by value, then the lower token; 0 for one that is not listed.
-__device__ __forceinline__ uint64_t score_key(float z, int v) {
+// ------------------------------------------------------------------------------- alternatives
+// A logit's place in their order: by value, then the lower token; 0 for one that is not listed.
+__device__ __forceinline__ uint64_t score_key(float z, uint32_t v) {
     if (!(z > -INFINITY)) return 0;
     const uint32_t b = __float_as_uint(z + 0.f);  // (-0 as 0)
-    return ((uint64_t)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32) | (uint32_t)(0x7fffffff - v);
+    return ((uint64_t)(b & 0x80000000u ? ~b : b | 0x80000000u) << 32) | (0x7fffffffu - v);
 }
 __device__ __forceinline__ float score_key_value(uint64_t k) {
     const uint32_t b = (uint32_t)(k >> 32);
-    return __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
+    return k == 0 ? -INFINITY : __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
 }
-__device__ __forceinline__ int score_key_token(uint64_t k) { return 0x7fffffff - (int)(uint32_t)k; }
+__device__ __forceinline__ int score_key_token(uint64_t k) { return k == 0 ? -1 : 0x7fffffff - (int)(uint32_t)k; }
 
-template <typename T, typename F>
-__device__ __forceinline__ T block_reduce256(T x, T *room, F f) {
+// A warp's 32 best keys so far, lane i the i-th
+struct ScoreList {
+    uint64_t key = 0;
+    __device__ __forceinline__ void insert(uint64_t k) {  // (the same k in every lane)
+        const int lane = threadIdx.x & 31;
+        const int rank = __popc(__ballot_sync(0xffffffffu, key > k));
+        const uint64_t up = __shfl_up_sync(0xffffffffu, key, 1);
+        key = lane < rank ? key : lane == rank ? k : up;
+    }
+    // another list, given in reverse order: the element-wise larger keys are the best 32 of both and a bitonic
+    // sequence, which five exchanges sort
+    __device__ __forceinline__ void merge_reversed(uint64_t other) {
+        key = key > other ? key : other;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) x = f(x, __shfl_xor_sync(0xffffffffu, x, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = x;
-    __syncthreads();
-    x = room[0];
-    for (int w = 1; w < 8; ++w) x = f(x, room[w]);
-    return x;
+        for (int d = 16; d > 0; d >>= 1) {
+            const uint64_t o = __shfl_xor_sync(0xffffffffu, key, d);
+            key = ((threadIdx.x & d) == 0) == (key > o) ? key : o;
+        }
+    }
+};
+// The `top`-th largest of the lanes' values
+__device__ __forceinline__ float warp_nth_largest(float v, int top) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+        for (int d = size / 2; d > 0; d >>= 1) {
+            const float o = __shfl_xor_sync(0xffffffffu, v, d);
+            const bool larger_here = ((lane & d) == 0) == ((lane & size) == 0 || size == 32);
+            v = larger_here ? fmaxf(v, o) : fminf(v, o);
+        }
+    return __shfl_sync(0xffffffffu, v, top - 1);
 }
 
-// One CTA per row: the maximum, the sums against it, and one pass for each alternative.
-template <int TYPE>
+// ------------------------------------------------------------------------------- sums
+struct ScoreSums {
+    float m = -3.4028235e38f, s = 0.f, t = 0.f;  // maximum, sum e^(z - m), sum e^(z - m) (z - m)
+    // to a maximum n >= m.  (The bound keeps 0 times infinity out where the maxima are that far apart.)
+    __device__ __forceinline__ void rebase(float n) {
+        const float d = fmaxf(m - n, -1e4f), f = exp_neg(d);
+        t = (t + s * d) * f;
+        s *= f;
+        m = n;
+    }
+    __device__ __forceinline__ void join(float om, float os, float ot) {
+        ScoreSums o;
+        o.m = om;
+        o.s = os;
+        o.t = ot;
+        const float n = fmaxf(m, om);
+        rebase(n);
+        o.rebase(n);
+        s += o.s;
+        t += o.t;
+    }
+};
+
+// One row per group of WARPS warps (8: a CTA; 1: eight rows to a CTA), or, where p.ctas > 1, per cluster of that many
+// CTAs, each a contiguous share of its vectors.
+template <int TYPE, bool TOP, int WARPS>
 __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
-    __shared__ float room[8];
-    __shared__ uint64_t kroom[8];
-    const int r = blockIdx.x, tok = p.tokens ? p.tokens[r] : 0;
-    const int64_t row = r * p.stride;
+    using Row = RowVectors<TYPE>;
+    constexpr int E = Row::E, U = TYPE == SARA_FP32 ? 4 : 2, STEP = 32 * WARPS;
+    __shared__ float s_sums[3][8];
+    __shared__ uint64_t s_key[TOP ? 8 : 1][32];
+    __shared__ volatile float s_floor[8];
+    __shared__ uint32_t c_sums[3][8], c_key[TOP ? 8 : 1][32][2];  // (rank 0) the cluster's
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = threadIdx.x % STEP;
+    const bool cluster = WARPS > 1 && p.ctas > 1;
+    if (cluster) cluster_arrive();  // (waited for before the stores into rank 0's shared memory)
+    const int64_t r64 = WARPS > 1 ? (int64_t)(blockIdx.x / (unsigned)p.ctas) : (int64_t)blockIdx.x * 8 + warp;
+    const int rank = WARPS > 1 ? (int)(blockIdx.x % (unsigned)p.ctas) : 0;
+    if (r64 >= p.R) return;
+    const int r = (int)r64, tok = p.tokens ? p.tokens[r] : 0;
+    const bool pad = tok < 0;
+    const Row row(p.z, r, p.stride, p.V);
     const float nan = __int_as_float(0x7fc00000);
-    if (tok < 0) {
-        if (threadIdx.x == 0) {
-            if (p.logprob) p.logprob[r] = 0.f;
-            if (p.entropy) p.entropy[r] = 0.f;
-            if (p.stats) p.stats[2 * (int64_t)r] = p.stats[2 * (int64_t)r + 1] = 0.f;
-        }
-        for (int j = threadIdx.x; j < p.top; j += 256) {
-            p.top_token[(int64_t)r * p.top + j] = -1;
-            p.top_logprob[(int64_t)r * p.top + j] = -INFINITY;
-        }
-        return;
+    const float ztok = part == 0 && rank == 0 && !pad && tok < p.V ? load_logit<TYPE>(p.z, r * p.stride + tok) : nan;
+
+    ScoreSums a;
+    ScoreList list;
+    uint64_t kth = 0;                           // the list's entry `top`
+    float kth_v = -INFINITY, floor = -INFINITY;  // its value; no alternative is below this
+    const int nv = pad ? 0 : row.vectors(), per = (nv + p.ctas - 1) / p.ctas, v1 = min(nv, (rank + 1) * per);
+    uint4 next[U];
+    auto load = [&](int k, uint4 (&x)[U]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = k + u * STEP < v1 ? row.load(k + u * STEP) : make_uint4(Row::kNone, Row::kNone, Row::kNone, Row::kNone);
+    };
+    if (TOP) {
+        if (lane == 0) s_floor[warp] = -INFINITY;
+        if (WARPS > 1) __syncthreads();
     }
-    float m = -INFINITY;
-    for (int64_t v = threadIdx.x; v < p.V; v += 256) m = fmaxf(m, load_logit<TYPE>(p.z, row + v));
-    m = block_reduce256(m, room, [](float a, float b) { return fmaxf(a, b); });
-    float S = 0.f, T = 0.f;
-    for (int64_t v = threadIdx.x; v < p.V; v += 256) {
-        const float z = load_logit<TYPE>(p.z, row + v);
-        if (z == -INFINITY) continue;
-        const float d = z - m, e = expf(d);
-        S += e;
-        T += e > 0.f ? e * d : e;
+    const int v0 = min(rank * per, v1);
+    load(v0 + part, next);
+    bool begun = false;
+#pragma unroll 1
+    for (int b = v0; b < v1; b += U * STEP) {  // (every lane of a warp the same steps)
+        const int k = b + part;
+        float z[U][E];
+#pragma unroll
+        for (int u = 0; u < U; ++u) unpack_vector<TYPE>(next[u], z[u]);
+        if (v1 - b > U * STEP) load(k + U * STEP, next);
+        float best = -INFINITY;  // (a NaN is not the maximum; it reaches the sums)
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < E; ++e) best = fmaxf(best, z[u][e]);
+        if (best > a.m) a.rebase(best);
+        float s2 = 0.f, t2 = 0.f;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float d = z[u][e] - a.m, w = exp_neg(d);
+                (e & 1 ? s2 : a.s) += w;
+                float &t = e & 1 ? t2 : a.t;
+                t = fmaf(w, fmaxf(d, -1000.f), t);  // (a logit of -inf has w = 0)
+            }
+        a.s += s2;
+        a.t += t2;
+        if constexpr (TOP) {
+            if (!begun) {  // the list is empty: nothing below the top-th of the lanes' maxima can matter
+                begun = true;
+                floor = warp_nth_largest(best, p.top);
+            }
+            if (WARPS > 1) {
+#pragma unroll
+                for (int w = 0; w < 8; ++w) floor = fmaxf(floor, s_floor[w]);  // (another warp's top-th; one that is late reads an older one)
+            }
+            // earlier steps had the lower tokens, so equal to the own top-th is too late, equal to another warp's is not
+            if (__any_sync(0xffffffffu, best > kth_v && best >= floor)) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < E; ++e) {
+                        const uint64_t key = z[u][e] >= floor ? score_key(z[u][e], row.first(k + u * STEP) + e) : 0;
+                        uint32_t cand = __ballot_sync(0xffffffffu, key > kth);
+                        while (cand) {
+                            const int src = __ffs(cand) - 1;
+                            cand &= cand - 1;
+                            const uint64_t c = __shfl_sync(0xffffffffu, key, src);
+                            if (c > kth) {
+                                list.insert(c);
+                                kth = __shfl_sync(0xffffffffu, list.key, p.top - 1);
+                            }
+                        }
+                    }
+                kth_v = score_key_value(kth);
+                if (WARPS > 1 && lane == 0) s_floor[warp] = fmaxf(s_floor[warp], kth_v);
+                __syncwarp();
+            }
+        }
     }
-    S = block_reduce256(S, room, [](float a, float b) { return a + b; });
-    T = block_reduce256(T, room, [](float a, float b) { return a + b; });
-    const bool none = S == 0.f;  // every logit is -inf
-    const float ls = none ? 0.f : logf(S);
-    if (threadIdx.x == 0) {
-        const float z = tok < p.V ? load_logit<TYPE>(p.z, row + tok) : nan;
-        if (p.logprob) p.logprob[r] = none && tok < p.V ? -INFINITY : z - m - ls;
-        if (p.entropy) p.entropy[r] = none ? 0.f : ls - T / S;
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1)
+        a.join(__shfl_xor_sync(0xffffffffu, a.m, d), __shfl_xor_sync(0xffffffffu, a.s, d), __shfl_xor_sync(0xffffffffu, a.t, d));
+    if constexpr (WARPS > 1) {
+        if (lane == 0) {
+            s_sums[0][warp] = a.m;
+            s_sums[1][warp] = a.s;
+            s_sums[2][warp] = a.t;
+        }
+        if (TOP) s_key[warp][lane] = list.key;
+        if (cluster) cluster_wait();  // every CTA of the cluster has started
+        __syncthreads();
+        if (warp == 0) {
+#pragma unroll
+            for (int w = 1; w < 8; ++w) {
+                a.join(s_sums[0][w], s_sums[1][w], s_sums[2][w]);
+                if (TOP) list.merge_reversed(s_key[w][31 - lane]);
+            }
+        }
+        if (cluster) {
+            if (warp == 0) {
+                if (lane < 3) st_cluster_u32(cluster_addr(&c_sums[lane][rank], 0), __float_as_uint(lane == 0 ? a.m : lane == 1 ? a.s : a.t));
+                if (TOP) {
+                    st_cluster_u32(cluster_addr(&c_key[rank][lane][0], 0), (uint32_t)list.key);
+                    st_cluster_u32(cluster_addr(&c_key[rank][lane][1], 0), (uint32_t)(list.key >> 32));
+                }
+            }
+            cluster_sync();
+            if (rank != 0) return;
+            if (warp == 0) {
+                for (int c = 1; c < p.ctas; ++c) {
+                    a.join(__uint_as_float(c_sums[0][c]), __uint_as_float(c_sums[1][c]), __uint_as_float(c_sums[2][c]));
+                    if (TOP) list.merge_reversed((uint64_t)c_key[c][31 - lane][1] << 32 | c_key[c][31 - lane][0]);
+                }
+            }
+        }
+        if (warp != 0) return;
+    }
+    const bool none = a.s == 0.f;  // every logit is -inf
+    const float m = pad ? 0.f : none ? -INFINITY : a.m, ls = none ? 0.f : logf(a.s);
+    if (lane == 0) {
+        if (p.logprob) p.logprob[r] = pad ? 0.f : none && tok < p.V ? -INFINITY : ztok - m - ls;
+        if (p.entropy) p.entropy[r] = none ? 0.f : ls - a.t / a.s;
         if (p.stats) {
             p.stats[2 * (int64_t)r] = m;
             p.stats[2 * (int64_t)r + 1] = ls;
         }
     }
-    uint64_t last = ~0ull;
-    for (int j = 0; j < p.top; ++j) {
-        uint64_t best = 0;
-        for (int64_t v = threadIdx.x; v < p.V; v += 256) {
-            const uint64_t k = score_key(load_logit<TYPE>(p.z, row + v), (int)v);
-            if (k < last && k > best) best = k;
-        }
-        best = block_reduce256(best, kroom, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
-        last = best;
-        if (threadIdx.x == 0) {
-            p.top_token[(int64_t)r * p.top + j] = best ? score_key_token(best) : -1;
-            p.top_logprob[(int64_t)r * p.top + j] = best ? score_key_value(best) - m - ls : -INFINITY;
-        }
+    if (TOP && lane < p.top) {
+        p.top_token[(int64_t)r * p.top + lane] = score_key_token(list.key);
+        p.top_logprob[(int64_t)r * p.top + lane] = list.key ? score_key_value(list.key) - m - ls : -INFINITY;
     }
 }
 
+constexpr int kScoreMaxCtas = 8;
+template <int TYPE, bool TOP>
+inline void launch_score(cudaStream_t s, int sms, ScoreParams p) {
+    const int vectors = p.V / (TYPE == SARA_FP32 ? 4 : 8);
+    p.ctas = 1;
+    if (vectors <= 512) {
+        score_kernel<TYPE, TOP, 1><<<(unsigned)((p.R + 7) / 8), 256, 0, s>>>(p);
+        CK(cudaGetLastError());
+        return;
+    }
+    while (p.ctas < kScoreMaxCtas && vectors > 512 * p.ctas && (int64_t)p.R * 2 * p.ctas <= (int64_t)8 * sms) p.ctas *= 2;
+    launch_cluster(s, false, dim3((unsigned)p.R * p.ctas), dim3(256), 0, (unsigned)p.ctas, score_kernel<TYPE, TOP, 8>, p);
+}
+
+// ------------------------------------------------------------------------------- gradient
 struct ScoreGradParams {
     const void *z;
     int64_t stride;
@@ -119,32 +341,90 @@ struct ScoreGradParams {
     const float *stats, *entropy, *glp, *gent;
     void *out;
     int64_t out_stride;
+    int segs;       // of a row
+    int64_t warps;  // R * segs
 };
+constexpr int kGradVectors = 4;  // a lane
 
-// One CTA per row.  (Not __ldg: the gradient may take the logits' place.)
+template <int TYPE>
+__device__ __forceinline__ uint32_t pack_grad(float a, float b) {
+    if constexpr (TYPE == SARA_BF16) return (uint32_t)f32_to_bf16(a) | ((uint32_t)f32_to_bf16(b) << 16);
+    else return (uint32_t)__half_as_ushort(__float2half_rn(a)) | ((uint32_t)__half_as_ushort(__float2half_rn(b)) << 16);
+}
+
+// One warp per segment of 32 x 4 vectors of a row.  A thread reads what it writes before it writes it, so the gradient
+// may take the logits' place.
 template <int TYPE>
 __global__ void __launch_bounds__(256) score_grad_kernel(ScoreGradParams p) {
-    const int r = blockIdx.x, tok = p.tokens ? p.tokens[r] : 0;
-    const int64_t row = r * p.stride, orow = r * p.out_stride;
+    using Row = RowVectors<TYPE>;
+    constexpr int E = Row::E;
+    const int64_t w = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    if (w >= p.warps) return;
+    const int r = (int)(w / p.segs), seg = (int)(w - (int64_t)r * p.segs), lane = threadIdx.x & 31;
+    const Row row(p.z, r, p.stride, p.V);
+    const int nv = row.vectors(), k0 = seg * (32 * kGradVectors) + lane;
+    const int tok = p.tokens ? p.tokens[r] : 0;
+    uint4 x[kGradVectors];
+    if (tok >= 0) {
+#pragma unroll
+        for (int u = 0; u < kGradVectors; ++u)
+            if (k0 + 32 * u < nv) x[u] = row.load(k0 + 32 * u);
+    }
     const float m = p.stats[2 * (int64_t)r], ls = p.stats[2 * (int64_t)r + 1];
     const float g = p.glp ? p.glp[r] : 0.f, gh = p.gent ? p.gent[r] : 0.f, H = p.gent ? p.entropy[r] : 0.f;
-    const bool zero = tok < 0 || (m == -INFINITY && ls == 0.f), wrong = tok >= p.V;
-    for (int64_t v = threadIdx.x; v < p.V; v += 256) {
-        float y = 0.f;
-        if (wrong) {
-            y = __int_as_float(0x7fc00000);
-        } else if (!zero) {
-            float z;
-            if constexpr (TYPE == SARA_FP32) z = static_cast<const float *>(p.z)[row + v];
-            else if constexpr (TYPE == SARA_BF16) z = bf16_to_f32(static_cast<const uint16_t *>(p.z)[row + v]);
-            else z = f16_to_f32(static_cast<const uint16_t *>(p.z)[row + v]);
-            const float lp = z - m - ls, q = expf(lp);
-            y = g * ((v == tok ? 1.f : 0.f) - q) - (q == 0.f ? 0.f : gh * q * (lp + H));
+    const bool zero = tok < 0 || (m == -INFINITY && ls == 0.f && tok < p.V), wrong = tok >= p.V;
+    uint8_t *out = static_cast<uint8_t *>(p.out) + ((int64_t)r * p.out_stride - row.off) * Row::kSize;  // of vector 0
+    const bool vec = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
+#pragma unroll
+    for (int u = 0; u < kGradVectors; ++u) {
+        const int k = k0 + 32 * u;
+        if (k >= nv) continue;
+        float y[E];
+        if (zero || wrong) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) y[e] = zero ? 0.f : __int_as_float(0x7fc00000);
+        } else {
+            unpack_vector<TYPE>(x[u], y);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const float lp = (y[e] - m) - ls, q = exp_neg_full(lp);
+                y[e] = -q * fmaf(gh, fmaxf(lp, -1000.f) + H, g);  // (a logit of -inf has q = 0)
+            }
+            const uint32_t at = (uint32_t)tok - row.first(k);
+            if (at < (uint32_t)E) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (at == (uint32_t)e) y[e] += g;
+            }
         }
-        if constexpr (TYPE == SARA_FP32) static_cast<float *>(p.out)[orow + v] = y;
-        else if constexpr (TYPE == SARA_BF16) static_cast<uint16_t *>(p.out)[orow + v] = f32_to_bf16(y);
-        else static_cast<uint16_t *>(p.out)[orow + v] = __half_as_ushort(__float2half_rn(y));
+        uint8_t *o = out + (int64_t)k * 16;
+        if (vec && row.whole(k)) {
+            if constexpr (TYPE == SARA_FP32)
+                *reinterpret_cast<float4 *>(o) = make_float4(y[0], y[1], y[2], y[3]);
+            else
+                *reinterpret_cast<uint4 *>(o) = make_uint4(pack_grad<TYPE>(y[0], y[1]), pack_grad<TYPE>(y[2], y[3]),
+                                                          pack_grad<TYPE>(y[4], y[5]), pack_grad<TYPE>(y[6], y[7]));
+        } else {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                if (row.first(k) + e >= row.V) continue;
+                if constexpr (TYPE == SARA_FP32) reinterpret_cast<float *>(o)[e] = y[e];
+                else reinterpret_cast<uint16_t *>(o)[e] = (uint16_t)pack_grad<TYPE>(y[e], 0.f);
+            }
+        }
     }
+}
+
+template <int TYPE>
+inline void launch_score_grad(cudaStream_t s, ScoreGradParams p) {
+    constexpr int E = RowVectors<TYPE>::E, kSeg = 32 * kGradVectors;
+    const int64_t vectors = ((int64_t)p.V + 2 * E - 2) / E;  // the most that a row's place can make of it
+    p.segs = (int)((vectors + kSeg - 1) / kSeg);
+    p.warps = (int64_t)p.R * p.segs;
+    const int64_t ctas = (p.warps + 7) / 8;
+    if (ctas > INT32_MAX) throw SaraError(SARA_EINVAL, "too many logits");
+    score_grad_kernel<TYPE><<<(unsigned)ctas, 256, 0, s>>>(p);
+    CK(cudaGetLastError());
 }
 
 }  // namespace sara

@@ -2,6 +2,8 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "../../include/sara.h"
 #include "host_util.h"
 #include "logprob.cuh"
@@ -26,12 +28,16 @@ int sara_logprobs(const void *logits, int64_t row_stride, int32_t type, int32_t 
     if (R == 0) return SARA_OK;
     if (!logits_ok(logits, row_stride, type, R, V)) return SARA_EINVAL;
     return op_guard([&] {
-        const ScoreParams p{logits, row_stride, R, V, top, tokens, logprob, entropy, stats, top_token, top_logprob};
+        const ScoreParams p{logits, row_stride, R, V, top, tokens, logprob, entropy, stats, top_token, top_logprob, 1};
         cudaStream_t s = static_cast<cudaStream_t>(stream);
-        if (type == SARA_FP32) score_kernel<SARA_FP32><<<R, 256, 0, s>>>(p);
-        else if (type == SARA_BF16) score_kernel<SARA_BF16><<<R, 256, 0, s>>>(p);
-        else score_kernel<SARA_FP16><<<R, 256, 0, s>>>(p);
-        CK(cudaGetLastError());
+        const int sms = sm_count();
+        auto launch = [&](auto t) {
+            if (top > 0) launch_score<t.value, true>(s, sms, p);
+            else launch_score<t.value, false>(s, sms, p);
+        };
+        if (type == SARA_FP32) launch(std::integral_constant<int, SARA_FP32>());
+        else if (type == SARA_BF16) launch(std::integral_constant<int, SARA_BF16>());
+        else launch(std::integral_constant<int, SARA_FP16>());
     });
 }
 
@@ -44,12 +50,12 @@ int sara_logprobs_backward(const void *logits, int64_t row_stride, int32_t type,
     if (!logits_ok(logits, row_stride, type, R, V) || !logits_ok(grad_logits, grad_stride, type, R, V) || !stats) return SARA_EINVAL;
     if (logits == grad_logits && R > 1 && row_stride != grad_stride) return SARA_EINVAL;
     return op_guard([&] {
-        const ScoreGradParams p{logits, row_stride, R, V, tokens, stats, entropy, grad_logprob, grad_entropy, grad_logits, grad_stride};
+        const ScoreGradParams p{logits, row_stride, R, V, tokens, stats, entropy, grad_logprob, grad_entropy, grad_logits, grad_stride,
+                                0, 0};
         cudaStream_t s = static_cast<cudaStream_t>(stream);
-        if (type == SARA_FP32) score_grad_kernel<SARA_FP32><<<R, 256, 0, s>>>(p);
-        else if (type == SARA_BF16) score_grad_kernel<SARA_BF16><<<R, 256, 0, s>>>(p);
-        else score_grad_kernel<SARA_FP16><<<R, 256, 0, s>>>(p);
-        CK(cudaGetLastError());
+        if (type == SARA_FP32) launch_score_grad<SARA_FP32>(s, p);
+        else if (type == SARA_BF16) launch_score_grad<SARA_BF16>(s, p);
+        else launch_score_grad<SARA_FP16>(s, p);
     });
 }
 
