@@ -400,7 +400,7 @@ SARA_API int sara_kv8_read(const sara_kv8_cache *cache, int32_t n_seq, const int
 /*
  * Decode attention over the cache: out[i][h] = softmax(q[i][h] . K / sqrt(head_dim)) V over the positions
  * first[i] <= p < ctx[i] of sequence i (first NULL: 0), one query row per sequence, n_heads / n_kv_heads in 1..8
- * query heads to a KV head.  A row without a position (ctx[i] <= first[i]) gives 0.
+ * query heads to a KV head, n_seq * n_kv_heads * max_blocks < 2^30.  A row without a position (ctx[i] <= first[i]) gives 0.
  * q, out: [n_seq][n_heads][head_dim] of `type` (SARA_BF16 or SARA_FP16), rows of q q_stride elements apart (a multiple of 8),
  * both 16-byte aligned.  lse: [n_seq][n_heads] fp32 or NULL, the natural logarithm of the sum of the exponentiated scores
  * (-inf for a row without a position).  Masked positions and positions behind ctx are not read.

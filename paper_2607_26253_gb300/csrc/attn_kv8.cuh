@@ -11,17 +11,23 @@
 //     multiples of 2^-31 of the maximum (probabilities are scaled by 2^7).
 //   - A scale covers both of a warp's rows of 8 positions: K's is a factor of the scores, V's of P, relative to the largest so far
 //     (vref), so that neither costs a multiplication per code.
-// Online softmax in fp32 per warp; the maximum is re-based only when a probability would pass 2^8, so most pages
-// skip the column maximum and the rescale.  Work: the (row, KV head, page) triples in one list, cut into equal
-// shares, one per CTA; a (row, KV head) that several CTAs share is joined by the last of them to finish, in the list's order.
+// Online softmax in fp32 per warp; the maximum is re-based only when a probability would pass 2^8, so most steps
+// skip the column maximum and the rescale.  Work: the (row, KV head, 64 positions) triples in one list, cut into
+// equal shares, one per CTA of 4 warps; a (row, KV head) that several CTAs share is joined by the last of them to
+// finish, in the list's order, in two levels where there are many.
 #pragma once
 #include "kv8.cuh"
 
 namespace sara {
 
-constexpr int kAttnKv8Warps = 8;
+constexpr int kAttnKv8Warps = 4;
 constexpr int kAttnKv8Threads = 32 * kAttnKv8Warps;
-constexpr int kAttnKv8MaxCtas = 512;
+constexpr int kAttnKv8Step = 16 * kAttnKv8Warps;                // positions of an entry of the list
+constexpr int kAttnKv8PageSteps = kKv8Page / kAttnKv8Step;
+constexpr int kAttnKv8SmCtas = 16 / kAttnKv8Warps;
+constexpr int kAttnKv8MaxCtas = 160 * kAttnKv8SmCtas;
+constexpr int kAttnKv8Group = 16;                               // states joined at a time
+constexpr int kAttnKv8Groups = kAttnKv8MaxCtas / kAttnKv8Group + 1;
 
 struct AttnKv8Params {
     Kv8Cache c;
@@ -31,8 +37,8 @@ struct AttnKv8Params {
     uint16_t *out;
     float *lse;
     int32_t *status;
-    int *count;   // [n][KVH] finished shares of a (row, KV head) that several CTAs work on; left zero
-    float *part;  // [CTA][2][8 (hd + 2)] their states: max and sum of 8 heads, then their outputs
+    int *count;   // [CTA][2][2] arrivals at the two levels of a join, kept at its first state; left zero
+    float *part;  // [CTA][2][8 (hd + 2)] states: max and sum of 8 heads, then their outputs
     int n, H, type;
     float scale_log2;  // log2(e) / sqrt(hd)
 };
@@ -68,33 +74,36 @@ __device__ __forceinline__ void load_codes(const uint8_t *p, uint32_t *r) {
         asm("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(r[0]) : "l"(p));
 }
 
-// A row's positions, and the pages that hold them
+// A row's positions, and the steps of the list that hold them
 struct AttnKv8Row {
-    int first, ctx, page0, pages;
+    int first, ctx, step0, steps;
     bool bad;
 };
-__device__ __forceinline__ AttnKv8Row attn_kv8_row(const AttnKv8Params &p, int i) {
+__device__ __forceinline__ AttnKv8Row attn_kv8_row(int ctx, int first, int max_blocks) {
     AttnKv8Row r;
-    r.ctx = __ldg(p.ctx + i);
-    r.first = p.first ? min(__ldg(p.first + i), r.ctx) : 0;  // (past the end: no position)
-    r.bad = r.ctx < 0 || r.first < 0 || r.ctx > (int64_t)p.c.max_blocks * kKv8Page;
-    r.page0 = r.first / kKv8Page;
-    r.pages = r.bad || r.ctx <= r.first ? 0 : (r.ctx - 1) / kKv8Page - r.page0 + 1;
+    r.ctx = ctx;
+    r.first = min(first, ctx);  // (past the end: no position)
+    r.bad = r.ctx < 0 || r.first < 0 || r.ctx > (int64_t)max_blocks * kKv8Page;
+    r.step0 = r.first / kAttnKv8Step;
+    r.steps = r.bad || r.ctx <= r.first ? 0 : (r.ctx - 1) / kAttnKv8Step - r.step0 + 1;
     return r;
+}
+__device__ __forceinline__ AttnKv8Row attn_kv8_row(const AttnKv8Params &p, int i) {
+    return attn_kv8_row(__ldg(p.ctx + i), p.first ? __ldg(p.first + i) : 0, p.c.max_blocks);
 }
 
 // Inclusive prefix of v over the CTA's threads, and the total
-__device__ __forceinline__ int64_t attn_kv8_scan(int64_t v, int64_t &total, int64_t *room) {
+__device__ __forceinline__ int attn_kv8_scan(int v, int &total, int *room) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(0xffffffffu, v, o);
+        const int y = __shfl_up_sync(0xffffffffu, v, o);
         if (lane >= o) v += y;
     }
     __syncthreads();
     if (lane == 31) room[warp] = v;
     __syncthreads();
-    int64_t before = 0;
+    int before = 0;
     total = 0;
 #pragma unroll
     for (int w = 0; w < kAttnKv8Warps; ++w) {
@@ -105,63 +114,130 @@ __device__ __forceinline__ int64_t attn_kv8_scan(int64_t v, int64_t &total, int6
 }
 
 template <int HD, int FMT>
-__global__ void __launch_bounds__(kAttnKv8Threads, 2) attn_kv8_kernel(AttnKv8Params p) {
+__global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kernel(AttnKv8Params p) {
     constexpr int KW = HD / 16, VW = HD / 32, NT = HD / 16;  // words a lane of a key row, of a value row; output tiles
     constexpr int KL = KW < 4 ? KW : 4;                      // words a load
     constexpr int PITCH = HD + 4;                            // (conflict-free 8-byte stores)
+    constexpr int STATE = 8 * (HD + 2);
     constexpr float kShift = 7.f;
     __shared__ __align__(16) float s_o[kAttnKv8Warps][8][PITCH];
-    __shared__ float s_m[kAttnKv8Warps][8], s_l[kAttnKv8Warps][8], s_M[8], s_L[8];
-    __shared__ int64_t s_room[kAttnKv8Warps], s_base;
-    __shared__ int s_row, s_last;
+    __shared__ float s_m[kAttnKv8Warps][8], s_l[kAttnKv8Warps][8], s_M[8], s_L[8], s_f[8][kAttnKv8Groups];
+    __shared__ int s_room[kAttnKv8Warps], s_row, s_base, s_last;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int KVH = p.c.KVH, G = p.H / KVH;
     const float nan = __int_as_float(0x7fc00000);
 
-    // rows without a position, and wrong ones
-    for (int i = blockIdx.x; i < p.n; i += gridDim.x) {
-        const AttnKv8Row r = attn_kv8_row(p, i);
-        if (r.pages) continue;
-        const float y = r.bad ? nan : 0.f;
-        const uint32_t y2 = p.type == SARA_BF16 ? pack2<SARA_BF16>(y, y) : pack2<SARA_FP16>(y, y);
-        uint32_t *o = reinterpret_cast<uint32_t *>(p.out + (int64_t)i * p.H * HD);
-        for (int e = tid; e < p.H * HD / 2; e += kAttnKv8Threads) o[e] = y2;
-        if (p.lse)
-            for (int e = tid; e < p.H; e += kAttnKv8Threads) p.lse[(int64_t)i * p.H + e] = r.bad ? nan : -INFINITY;
-        if (r.bad && tid == 0) kv8_report(p.status);
-    }
-
-    // this CTA's share of the list, and the row in which it begins
-    int64_t total = 0;
+    // this CTA's share lo .. hi of the list, and the row in which it begins
+    int steps = 0, end = 0, total = 0;
+    bool idle = false;  // a row without a position (or a wrong one) that is this CTA's to write
     for (int b = 0; b < p.n; b += kAttnKv8Threads) {
-        int64_t sum;
-        attn_kv8_scan(b + tid < p.n ? attn_kv8_row(p, b + tid).pages : 0, sum, s_room);
+        int sum;
+        steps = b + tid < p.n ? attn_kv8_row(p, b + tid).steps : 0;
+        idle = idle || (b + tid < p.n && steps == 0 && (unsigned)(b + tid) % gridDim.x == blockIdx.x);
+        end = total + attn_kv8_scan(steps, sum, s_room);
         total += sum;
     }
     total *= KVH;
-    const int64_t ctas = min((int64_t)gridDim.x, total);
-    if (blockIdx.x >= ctas) return;
-    const int64_t lo = blockIdx.x * total / ctas, hi = (blockIdx.x + 1) * total / ctas;
-    for (int64_t b = 0, before = 0; b < p.n; b += kAttnKv8Threads) {
-        int64_t sum;
-        const int pages = b + tid < p.n ? attn_kv8_row(p, (int)b + tid).pages : 0;
-        const int64_t end = (before + attn_kv8_scan(pages, sum, s_room)) * KVH;
-        if (lo < end && lo >= end - (int64_t)pages * KVH) {
-            s_row = (int)b + tid;
-            s_base = end - (int64_t)pages * KVH;
+    const int ctas = min((int)gridDim.x, total), c = blockIdx.x;
+    const int share = ctas ? total / ctas : 0, more = total - share * ctas;  // the first `more` CTAs have one entry more
+    const int lo = c * share + min(c, more), hi = c < ctas ? lo + share + (c < more) : lo;
+    if (p.n <= kAttnKv8Threads) {
+        if (lo < hi && lo < end * KVH && lo >= (end - steps) * KVH) {
+            s_row = tid;
+            s_base = (end - steps) * KVH;
         }
-        before += sum;
-        if (before * KVH > lo) break;
+    } else if (lo < hi) {
+        for (int b = 0, before = 0; b < p.n && before * KVH <= lo; b += kAttnKv8Threads) {
+            int sum;
+            steps = b + tid < p.n ? attn_kv8_row(p, b + tid).steps : 0;
+            end = before + attn_kv8_scan(steps, sum, s_room);
+            if (lo < end * KVH && lo >= (end - steps) * KVH) {
+                s_row = b + tid;
+                s_base = (end - steps) * KVH;
+            }
+            before += sum;
+        }
     }
-    __syncthreads();
-    int row = s_row;
-    int64_t base = s_base;
+    if (__syncthreads_or(idle)) {
+        for (int i = c; i < p.n; i += gridDim.x) {
+            const AttnKv8Row r = attn_kv8_row(p, i);
+            if (r.steps) continue;
+            const float y = r.bad ? nan : 0.f;
+            const uint32_t y2 = p.type == SARA_BF16 ? pack2<SARA_BF16>(y, y) : pack2<SARA_FP16>(y, y);
+            uint32_t *o = reinterpret_cast<uint32_t *>(p.out + (int64_t)i * p.H * HD);
+            for (int e = tid; e < p.H * HD / 2; e += kAttnKv8Threads) o[e] = y2;
+            if (p.lse)
+                for (int e = tid; e < p.H; e += kAttnKv8Threads) p.lse[(int64_t)i * p.H + e] = r.bad ? nan : -INFINITY;
+            if (r.bad && tid == 0) kv8_report(p.status);
+        }
+    }
+    if (lo >= hi) return;
+    auto cta_of = [&](int x) {  // whose share entry x is
+        const int big = more * (share + 1);
+        return x < big ? x / (share + 1) : more + (x - big) / share;
+    };
+    auto put = [&](int row, int head, int i, float y0, float y1) {  // two neighbouring outputs, at place i of a state
+        const int dim = HD / 8 * (i % 16 / 2) + i / 16 * 2;
+        *reinterpret_cast<uint32_t *>(p.out + ((int64_t)row * p.H + head) * HD + dim) =
+            p.type == SARA_BF16 ? pack2<SARA_BF16>(y0, y1) : pack2<SARA_FP16>(y0, y1);
+    };
+    int row = s_row, base = s_base;
     AttnKv8Row r = attn_kv8_row(p, row);
 
-    for (int64_t at = lo; at < hi;) {
-        const int h = (int)((at - base) / r.pages), a = (int)((at - base) % r.pages);
-        const int64_t unit = base + (int64_t)h * r.pages;
-        const int b = (int)min((int64_t)r.pages, hi - unit);  // pages a .. b of the row's, for KV head h
+    for (int at = lo; at < hi;) {
+        const int h = (at - base) / r.steps, a = at - base - h * r.steps, unit = base + h * r.steps;
+        const int b = min(r.steps, hi - unit);  // entries a .. b of the row's, for KV head h
+        // this warp's positions of step x: 64 x + 16 warp .. + 15; the row's first and last step may have none
+        int xa = r.step0 + a, xb = r.step0 + b;
+        if (xa * kAttnKv8Step + 16 * warp + 16 <= r.first) ++xa;
+        if ((xb - 1) * kAttnKv8Step + 16 * warp >= r.ctx) --xb;
+        const int32_t *tab = p.c.table + row * p.c.table_stride;
+        int ids = 0, idbase = 0;  // this lane's entry of the 32 table entries from idbase on
+        bool wrong = false;
+        auto block_of = [&](int x, bool begin) {
+            const int page = x / kAttnKv8PageSteps;
+            if (begin || page - idbase >= 32) {
+                idbase = page;
+                ids = (page + lane) * kAttnKv8PageSteps < xb ? __ldg(tab + page + lane) : 0;
+                const bool out = ids < 0 || ids >= p.c.n_blocks;
+                wrong = wrong || out;
+                ids = out ? -1 : ids;
+            }
+            return __shfl_sync(0xffffffffu, ids, page - idbase);
+        };
+        const int lane_k = (KW == 8 ? 16 : HD / 4) * t, lane_v = HD / 8 * g;
+        auto edge = [&](int x) {  // whether some of the 16 positions are masked
+            const int p0 = x * kAttnKv8Step + 16 * warp;
+            return p0 < r.first || p0 + 16 > r.ctx;
+        };
+        auto slot_of = [&](int x, int e) {  // (masked positions stand for the nearest that is not: their probability is 0)
+            return min(max(x * kAttnKv8Step + 16 * warp + e, r.first), r.ctx - 1) & (kKv8Page - 1);
+        };
+        auto block_in_page = [&](int x) { return (x % kAttnKv8PageSteps * kAttnKv8Step + 16 * warp) / kKv8Block; };
+        uint32_t kr[2][KW];
+        float ks = 0.f;
+        int blk = 0;
+        auto load_k = [&](int x) {
+            const int64_t tile = kv8_tile(p.c, max(blk, 0), 0, h);
+            ks = blk < 0 ? nan : __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
+            const uint8_t *k = p.c.codes + tile * (kKv8Page * HD) + lane_k;
+            if (!edge(x)) {
+                k += (x % kAttnKv8PageSteps * kAttnKv8Step + 16 * warp + g) * HD;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + 8 * e * HD + 64 * i, &kr[e][4 * i]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+#pragma unroll
+                    for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + slot_of(x, g + 8 * e) * HD + 64 * i, &kr[e][4 * i]);
+            }
+        };
+        if (xa < xb) {
+            blk = block_of(xa, true);
+            load_k(xa);
+        }
 
         // queries: head g of the group, the dims of this lane's key words
         uint32_t qb[KW][2];
@@ -184,9 +260,9 @@ __global__ void __launch_bounds__(kAttnKv8Threads, 2) attn_kv8_kernel(AttnKv8Par
                 top = max(top & 0xffff, top >> 16);
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                // 2^e: the largest magnitude's power of two becomes 2^14
-                const int e = min(14 - ((int)(top >> 7) - 127), 126);
-                const float f = pow2f(max(e, -113));
+                // 2^e brings the largest magnitude's power of two to 2^14
+                const int e = max(min(14 - ((int)(top >> 7) - 127), 126), -113);
+                const float f = pow2f(e);
 #pragma unroll
                 for (int s = 0; s < KW; ++s)
 #pragma unroll
@@ -194,7 +270,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, 2) attn_kv8_kernel(AttnKv8Par
                         const float2 x = unpack2<SARA_BF16>(qb[s][i]);
                         qb[s][i] = pack_half2(x.x * f, x.y * f);
                     }
-                mul *= pow2f(-max(e, -113));
+                mul *= pow2f(-e);
             }
             mul0 = __shfl_sync(0xffffffffu, mul, 8 * t);
             mul1 = __shfl_sync(0xffffffffu, mul, 8 * t + 4);
@@ -205,82 +281,44 @@ __global__ void __launch_bounds__(kAttnKv8Threads, 2) attn_kv8_kernel(AttnKv8Par
         for (int j = 0; j < NT; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
-
-        // this warp's positions of page x: 128 x + 16 warp .. + 15; the row's first and last page may have none
-        int pa = r.page0 + a, pb = r.page0 + b;
-        if (pa * kKv8Page + 16 * warp + 16 <= r.first) ++pa;
-        if ((pb - 1) * kKv8Page + 16 * warp >= r.ctx) --pb;
-        const int32_t *tab = p.c.table + row * p.c.table_stride;
-        int ids = 0;     // this lane's entry of the 32 table entries from idbase on
-        int idbase = 0;
-        bool wrong = false;
-        auto block_of = [&](int x, int begin) -> int64_t {
-            if (((x - begin) & 31) == 0) {
-                idbase = x;
-                ids = x + lane < pb ? __ldg(tab + x + lane) : 0;
-                const bool out = ids < 0 || ids >= p.c.n_blocks;
-                wrong = wrong || out;
-                ids = out ? -1 : ids;
-            }
-            return __shfl_sync(0xffffffffu, ids, x - idbase);
-        };
-        auto slot_of = [&](int x, int e) {  // (masked positions stand for the nearest that is not: their probability is 0)
-            const int pos = x * kKv8Page + 16 * warp + e;
-            return min(max(pos, r.first), r.ctx - 1) & (kKv8Page - 1);
-        };
-        uint32_t kr[2][KW];
-        float ks = 0.f;
-        int64_t blk = 0;
-        auto load_k = [&](int x, int64_t id) {
-            const int64_t tile = kv8_tile(p.c, (int)max(id, (int64_t)0), 0, h);
-            ks = id < 0 ? nan : __ldg(p.c.scales + tile * kKv8PageBlocks + (warp >> 1));
-            const uint8_t *k = p.c.codes + tile * (kKv8Page * HD) + (KW == 8 ? 16 : HD / 4) * t;
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + slot_of(x, g + 8 * e) * HD + 64 * i, &kr[e][4 * i]);
-        };
-        if (pa < pb) {
-            blk = block_of(pa, pa);
-            load_k(pa, blk);
-        }
 #pragma unroll 1
-        for (int x = pa; x < pb; ++x) {
-            // values of this page, keys of the next
+        for (int x = xa; x < xb; ++x) {
+            // this step's values come while its scores are taken, the next one's keys after that
             uint32_t vr[4][VW];
-            const int64_t vtile = kv8_tile(p.c, (int)max(blk, (int64_t)0), 1, h);
-            const float vs = __ldg(p.c.scales + vtile * kKv8PageBlocks + (warp >> 1));
-            const uint8_t *v = p.c.codes + vtile * (kKv8Page * HD) + HD / 8 * g;
+            const int64_t tile = kv8_tile(p.c, max(blk, 0), 1, h);
+            const float vs = __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
+            const uint8_t *v = p.c.codes + tile * (kKv8Page * HD) + lane_v;
+            const bool cut = edge(x);
+            if (!cut) {
+                v += (x % kAttnKv8PageSteps * kAttnKv8Step + 16 * warp + 2 * t) * HD;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) load_codes<VW>(v + slot_of(x, 2 * t + (e & 1) + 8 * (e >> 1)) * HD, vr[e]);
-            uint32_t kc[2][KW];
+                for (int e = 0; e < 4; ++e) load_codes<VW>(v + ((e & 1) + 8 * (e >> 1)) * HD, vr[e]);
+            } else {
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-#pragma unroll
-                for (int s = 0; s < KW; ++s) kc[e][s] = kr[e][s];
-            const float kscale = ks;
-            if (x + 1 < pb) {
-                blk = block_of(x + 1, pa);
-                load_k(x + 1, blk);
+                for (int e = 0; e < 4; ++e) load_codes<VW>(v + slot_of(x, 2 * t + (e & 1) + 8 * (e >> 1)) * HD, vr[e]);
             }
             float s[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < KW; ++i) {
                 uint32_t f[4];
-                decode4_half<FMT>(kc[0][i], f[0], f[2]);
-                decode4_half<FMT>(kc[1][i], f[1], f[3]);
+                decode4_half<FMT>(kr[0][i], f[0], f[2]);
+                decode4_half<FMT>(kr[1][i], f[1], f[3]);
                 mma_f16_16816(i & 1 ? s2 : s, f, qb[i][0], qb[i][1]);
             }
+            const float f0 = ks * mul0, f1 = ks * mul1;
+            if (x + 1 < xb) {
+                blk = block_of(x + 1, false);
+                load_k(x + 1);
+            }
             // s[0], s[1]: position g, heads 2 t and 2 t + 1; s[2], s[3]: position g + 8
-            const float f0 = kscale * mul0, f1 = kscale * mul1;
             s[0] = (s[0] + s2[0]) * f0;
             s[1] = (s[1] + s2[1]) * f1;
             s[2] = (s[2] + s2[2]) * f0;
             s[3] = (s[3] + s2[3]) * f1;
-            const int p0 = x * kKv8Page + 16 * warp;
-            if (p0 < r.first || p0 + 16 > r.ctx) {
-                if (p0 + g < r.first || p0 + g >= r.ctx) s[0] = s[1] = -INFINITY;
-                if (p0 + g + 8 < r.first || p0 + g + 8 >= r.ctx) s[2] = s[3] = -INFINITY;
+            if (cut) {
+                const int p0 = x * kAttnKv8Step + 16 * warp + g;
+                if (p0 < r.first || p0 >= r.ctx) s[0] = s[1] = -INFINITY;
+                if (p0 + 8 < r.first || p0 + 8 >= r.ctx) s[2] = s[3] = -INFINITY;
             }
             if (__any_sync(0xffffffffu, fmaxf(s[0], s[2]) > m0 + 8.f || fmaxf(s[1], s[3]) > m1 + 8.f)) {
                 float n0 = fmaxf(m0, fmaxf(s[0], s[2])), n1 = fmaxf(m1, fmaxf(s[1], s[3]));
@@ -329,15 +367,15 @@ __global__ void __launch_bounds__(kAttnKv8Threads, 2) attn_kv8_kernel(AttnKv8Par
             ph[1] = movmatrix_trans(ph[1]);
 #pragma unroll
             for (int i = 0; i < VW; ++i) {
-                uint32_t f0[4], f1[4];  // dims 4 i, 4 i + 1 and 4 i + 2, 4 i + 3 of the lane's
-                decode4_half<FMT>(__byte_perm(vr[0][i], vr[1][i], 0x5140), f0[0], f0[1]);
-                decode4_half<FMT>(__byte_perm(vr[2][i], vr[3][i], 0x5140), f0[2], f0[3]);
-                decode4_half<FMT>(__byte_perm(vr[0][i], vr[1][i], 0x7362), f1[0], f1[1]);
-                decode4_half<FMT>(__byte_perm(vr[2][i], vr[3][i], 0x7362), f1[2], f1[3]);
-                mma_f16_16816(o[2 * i], f0, ph[0], ph[1]);
-                mma_f16_16816(o[2 * i + 1], f1, ph[0], ph[1]);
-                mma_f16_16816(o[2 * i], f0, pl[0], pl[1]);
-                mma_f16_16816(o[2 * i + 1], f1, pl[0], pl[1]);
+                uint32_t v0[4], v1[4];  // dims 4 i, 4 i + 1 and 4 i + 2, 4 i + 3 of the lane's
+                decode4_half<FMT>(__byte_perm(vr[0][i], vr[1][i], 0x5140), v0[0], v0[1]);
+                decode4_half<FMT>(__byte_perm(vr[2][i], vr[3][i], 0x5140), v0[2], v0[3]);
+                decode4_half<FMT>(__byte_perm(vr[0][i], vr[1][i], 0x7362), v1[0], v1[1]);
+                decode4_half<FMT>(__byte_perm(vr[2][i], vr[3][i], 0x7362), v1[2], v1[3]);
+                mma_f16_16816(o[2 * i], v0, ph[0], ph[1]);
+                mma_f16_16816(o[2 * i + 1], v1, ph[0], ph[1]);
+                mma_f16_16816(o[2 * i], v0, pl[0], pl[1]);
+                mma_f16_16816(o[2 * i + 1], v1, pl[0], pl[1]);
             }
         }
         if (wrong) kv8_report(p.status);
@@ -374,27 +412,20 @@ __global__ void __launch_bounds__(kAttnKv8Threads, 2) attn_kv8_kernel(AttnKv8Par
             s_L[tid] = L;
         }
         __syncthreads();
-        const bool whole = a == 0 && b == r.pages;
-        float *mine = p.part + ((int64_t)blockIdx.x * 2 + (a == 0)) * (8 * (HD + 2));
+        const bool whole = a == 0 && b == r.steps;
+        float *mine = p.part + (c * 2 + (a == 0)) * STATE;  // (a share begins in at most one unit that it does not begin)
         for (int e = tid; e < G * HD / 2; e += kAttnKv8Threads) {
             const int hh = e / (HD / 2), i = e % (HD / 2) * 2;
             float y0 = 0.f, y1 = 0.f;
 #pragma unroll
             for (int w = 0; w < kAttnKv8Warps; ++w) {
-                const float2 x = *reinterpret_cast<const float2 *>(&s_o[w][hh][i]);
+                const float2 y = *reinterpret_cast<const float2 *>(&s_o[w][hh][i]);
                 const float f = s_m[w][hh];
-                y0 += f * x.x;
-                y1 += f * x.y;
+                y0 += f * y.x;
+                y1 += f * y.y;
             }
-            if (whole) {
-                const int dim = HD / 8 * (i % 16 / 2) + i / 16 * 2;
-                y0 /= s_L[hh];
-                y1 /= s_L[hh];
-                *reinterpret_cast<uint32_t *>(p.out + ((int64_t)row * p.H + h * G + hh) * HD + dim) =
-                    p.type == SARA_BF16 ? pack2<SARA_BF16>(y0, y1) : pack2<SARA_FP16>(y0, y1);
-            } else {
-                *reinterpret_cast<float2 *>(mine + 16 + hh * HD + i) = make_float2(y0, y1);
-            }
+            if (whole) put(row, h * G + hh, i, y0 / s_L[hh], y1 / s_L[hh]);
+            else *reinterpret_cast<float2 *>(mine + 16 + hh * HD + i) = make_float2(y0, y1);
         }
         if (tid < G) {
             if (!whole) {
@@ -405,55 +436,96 @@ __global__ void __launch_bounds__(kAttnKv8Threads, 2) attn_kv8_kernel(AttnKv8Par
             }
         }
         if (!whole) {
-            // CTA of entry x: the largest c with c total / ctas <= x
-            const int64_t c0 = ((unit + 1) * ctas - 1) / total, c1 = ((unit + r.pages) * ctas - 1) / total;
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                int *n = p.count + (int64_t)row * KVH + h;
-                s_last = atomicAdd(n, 1) == (int)(c1 - c0);
-                if (s_last) *n = 0;
+            // the unit's states are those of CTAs c0 .. c1; more than a group's are joined group by group first, each group's
+            // result in the place of its first state
+            const int c0 = cta_of(unit), c1 = cta_of(unit + r.steps - 1);
+            const bool two = c1 - c0 >= kAttnKv8Group;
+            int from = c0, n = c1 - c0 + 1, pace = 1;
+            if (two) {
+                from = max(c0, c & ~(kAttnKv8Group - 1));
+                n = min(c1, c | (kAttnKv8Group - 1)) - from + 1;
             }
-            __syncthreads();
-            if (s_last) {
+            auto member = [&](int k) { return pace == 1 ? from + k : k == 0 ? c0 : (c0 & ~(kAttnKv8Group - 1)) + k * kAttnKv8Group; };
+            auto state = [&](int x) { return p.part + (x * 2 + (x == c0)) * STATE; };
+            for (int level = 0;; ++level) {
                 __threadfence();
-                auto state = [&](int64_t c) { return p.part + (c * 2 + (c == c0)) * (8 * (HD + 2)); };
-                for (int e = tid; e < G * HD / 2; e += kAttnKv8Threads) {
-                    const int hh = e / (HD / 2), i = e % (HD / 2) * 2;
-                    float M = -3.4028235e38f, L = 0.f, y0 = 0.f, y1 = 0.f;
-#pragma unroll 4
-                    for (int64_t c = c0; c <= c1; ++c) {
-                        const float *x = state(c);
-                        const float mc = __ldcg(x + hh), lc = __ldcg(x + 8 + hh);
-                        const float2 yc = __ldcg(reinterpret_cast<const float2 *>(x + 16 + hh * HD + i));
-                        const float N = fmaxf(M, mc), fa = ex2(M - N), fb = ex2(mc - N);
-                        M = N;
-                        L = L * fa + lc * fb;
-                        y0 = y0 * fa + yc.x * fb;
-                        y1 = y1 * fa + yc.y * fb;
-                    }
-                    const int dim = HD / 8 * (i % 16 / 2) + i / 16 * 2;
-                    y0 /= L;
-                    y1 /= L;
-                    *reinterpret_cast<uint32_t *>(p.out + ((int64_t)row * p.H + h * G + hh) * HD + dim) =
-                        p.type == SARA_BF16 ? pack2<SARA_BF16>(y0, y1) : pack2<SARA_FP16>(y0, y1);
-                    if (p.lse && i == 0) p.lse[(int64_t)row * p.H + h * G + hh] = (M - kShift + log2f(L)) * 0.69314718f;
+                __syncthreads();
+                if (tid == 0) {
+                    int *arrived = p.count + (from * 2 + (from == c0)) * 2 + level;
+                    s_last = atomicAdd(arrived, 1) == n - 1;
+                    if (s_last) *arrived = 0;
                 }
+                __syncthreads();
+                if (!s_last) break;
+                __threadfence();
+                const bool final = level == 1 || !two;
+                // factors of the states, 16 lanes a head
+                {
+                    const int hh = tid / 16, k0 = tid % 16;
+                    float M = -3.4028235e38f, L = 0.f;
+                    for (int k = k0; k < n; k += 16) M = fmaxf(M, __ldcg(state(member(k)) + hh));
+#pragma unroll
+                    for (int d = 8; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
+                    for (int k = k0; k < n; k += 16) {
+                        const float *y = state(member(k));
+                        const float f = ex2(__ldcg(y + hh) - M);
+                        s_f[hh][k] = f;
+                        L += f * __ldcg(y + 8 + hh);
+                    }
+#pragma unroll
+                    for (int d = 8; d > 0; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
+                    if (k0 == 0) {
+                        s_M[hh] = M;
+                        s_L[hh] = L;
+                    }
+                }
+                __syncthreads();
+                float *to = state(from);
+                for (int e = tid; e < G * HD / 4; e += kAttnKv8Threads) {
+                    const int hh = e / (HD / 4), i = e % (HD / 4) * 4;
+                    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+                    for (int k = 0; k < n; ++k) {
+                        const float4 z = __ldcg(reinterpret_cast<const float4 *>(state(member(k)) + 16 + hh * HD + i));
+                        const float f = s_f[hh][k];
+                        y.x += f * z.x;
+                        y.y += f * z.y;
+                        y.z += f * z.z;
+                        y.w += f * z.w;
+                    }
+                    if (final) {
+                        const float L = s_L[hh];
+                        put(row, h * G + hh, i, y.x / L, y.y / L);
+                        put(row, h * G + hh, i + 2, y.z / L, y.w / L);
+                    } else {
+                        *reinterpret_cast<float4 *>(to + 16 + hh * HD + i) = y;
+                    }
+                }
+                if (tid < G) {
+                    if (!final) {
+                        to[tid] = s_M[tid];
+                        to[8 + tid] = s_L[tid];
+                    } else if (p.lse) {
+                        p.lse[(int64_t)row * p.H + h * G + tid] = (s_M[tid] - kShift + log2f(s_L[tid])) * 0.69314718f;
+                    }
+                }
+                if (final) break;
+                from = c0;
+                n = c1 / kAttnKv8Group - c0 / kAttnKv8Group + 1;
+                pace = kAttnKv8Group;
             }
         }
-        __syncthreads();  // (shared memory is the next share's)
+        __syncthreads();  // (shared memory is the next unit's)
         at = unit + b;
         if (at < hi && h == KVH - 1) {
-            base += (int64_t)KVH * r.pages;
+            base += KVH * r.steps;
             do r = attn_kv8_row(p, ++row);
-            while (r.pages == 0);
+            while (r.steps == 0);
         }
     }
 }
 
-inline size_t attn_kv8_count_bytes(int n, int KVH) { return ((size_t)n * KVH * sizeof(int) + 255) / 256 * 256; }
-inline size_t attn_kv8_workspace(int n, int KVH, int hd) {
-    return attn_kv8_count_bytes(n, KVH) + (size_t)kAttnKv8MaxCtas * 2 * 8 * (hd + 2) * sizeof(float);
-}
+inline size_t attn_kv8_count_bytes() { return kAttnKv8MaxCtas * 4 * sizeof(int); }
+inline size_t attn_kv8_workspace(int hd) { return attn_kv8_count_bytes() + (size_t)kAttnKv8MaxCtas * 2 * 8 * (hd + 2) * sizeof(float); }
 
 }  // namespace sara

@@ -96,7 +96,7 @@ int sara_kv8_read(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *pos
 
 size_t sara_attention_kv8_workspace_bytes(int32_t n_seq, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
     if (n_seq < 1 || n_heads < 1 || n_kv_heads < 1 || head_dim < 1) return 0;
-    return attn_kv8_workspace(n_seq, n_kv_heads, head_dim);
+    return attn_kv8_workspace(head_dim);
 }
 
 int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_t n_heads, const void *q, int64_t q_stride,
@@ -109,7 +109,7 @@ int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
     if (q_stride % 8 || (n_seq > 1 && q_stride < (int64_t)n_heads * cache->head_dim)) return SARA_EINVAL;
     if ((int64_t)n_seq * n_heads > INT32_MAX) return SARA_EINVAL;
     return op_guard([&] {
-        if (workspace_bytes < attn_kv8_workspace(n_seq, cache->n_kv_heads, cache->head_dim)) throw SaraError(SARA_EINVAL, "workspace too small");
+        if (workspace_bytes < attn_kv8_workspace(cache->head_dim)) throw SaraError(SARA_EINVAL, "workspace too small");
         AttnKv8Params p{};
         p.c = device_cache(cache);
         p.q = static_cast<const uint16_t *>(q);
@@ -123,12 +123,13 @@ int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
         p.H = n_heads;
         p.type = type;
         p.count = static_cast<int *>(workspace);
-        p.part = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + attn_kv8_count_bytes(n_seq, cache->n_kv_heads));
+        p.part = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + attn_kv8_count_bytes());
         p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)cache->head_dim));
         cudaStream_t s = static_cast<cudaStream_t>(stream);
-        // two CTAs an SM, fewer where there are not as many pages
-        const int64_t pages = (int64_t)n_seq * cache->n_kv_heads * cache->max_blocks;
-        const unsigned ctas = (unsigned)std::min<int64_t>(std::min(2 * sm_count(), kAttnKv8MaxCtas), pages);
+        // as many CTAs as fit, fewer where there are not as many entries
+        const int64_t entries = (int64_t)n_seq * cache->n_kv_heads * cache->max_blocks * kAttnKv8PageSteps;
+        if (entries > INT32_MAX) throw SaraError(SARA_EINVAL, "too many blocks");
+        const unsigned ctas = (unsigned)std::min<int64_t>(std::min(kAttnKv8SmCtas * sm_count(), kAttnKv8MaxCtas), entries);
         by_shape(cache, [&](auto hd, auto fmt) {
             attn_kv8_kernel<hd.value, fmt.value><<<ctas, kAttnKv8Threads, 0, s>>>(p);
         });

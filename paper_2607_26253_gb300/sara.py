@@ -373,213 +373,3 @@ def sample(logits, uid, t, sample_seed: int):
     _check(load().sara_sample(logits.data_ptr(), R, V, sample_seed, uid.data_ptr(), t.data_ptr(), tok.data_ptr(),
                               torch.cuda.current_stream().cuda_stream))
     return tok
-
-
-KV8_PAGE, KV8_SCALE = 128, 32   # positions of a cache block, and of a scale
-
-
-def _type_code(dtype, what, fp32=True):
-    """SARA_BF16 / SARA_FP16 / SARA_FP32 of a torch dtype."""
-    import torch
-    code = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}.get(dtype, 3)
-    if code > (2 if fp32 else 1):
-        raise SaraError(SARA_EINVAL, f"{what} is {dtype}")
-    return code
-
-
-def _refuse_unless(ok, msg):
-    if not ok:
-        raise SaraError(SARA_EINVAL, msg)
-
-
-def _int32_arg(x, shape, device, what):
-    import torch
-    _refuse_unless(x.dtype == torch.int32 and tuple(x.shape) == shape and x.device == device and x.is_contiguous(),
-                   f"{what} must be a contiguous int32 tensor of shape {shape} on {device}")
-
-
-def _f32_arg(x, shape, device, what):
-    import torch
-    _refuse_unless(x.dtype == torch.float32 and tuple(x.shape) == shape and x.device == device and x.is_contiguous(),
-                   f"{what} must be a contiguous fp32 tensor of shape {shape} on {device}")
-
-
-def _launch(device, fn, *args):
-    """fn(*args, stream) on the device's current stream."""
-    import torch
-    _refuse_unless(device.type == "cuda", f"operands must be CUDA tensors, not on {device}")
-    if device.index == torch.cuda.current_device():
-        _check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
-    else:
-        with torch.cuda.device(device):
-            _check(fn(*args, torch.cuda.current_stream(device).cuda_stream))
-
-
-def _kv8(codes, scales, table):
-    """The Kv8Cache of a cache's tensors, checked."""
-    import torch
-    fmt = {torch.float8_e4m3fn: 0, torch.int8: 1}.get(codes.dtype)
-    _refuse_unless(fmt is not None, f"codes must be float8_e4m3fn or int8, not {codes.dtype}")
-    _refuse_unless(codes.dim() == 5 and codes.shape[1] == 2 and codes.shape[3] == KV8_PAGE and codes.is_contiguous(),
-                   "codes must be contiguous, [n_blocks, 2, n_kv_heads, 128, head_dim]")
-    nb, _, kvh, _, hd = codes.shape
-    _f32_arg(scales, (nb, 2, kvh, KV8_PAGE // KV8_SCALE), codes.device, "scales")
-    _refuse_unless(table.dtype == torch.int32 and table.dim() == 2 and table.device == codes.device
-                   and (table.stride(1) == 1 or table.shape[1] == 1)
-                   and (table.shape[0] <= 1 or table.stride(0) >= table.shape[1]),
-                   "table must be an int32 tensor [n_seq, max_blocks] with rows of consecutive elements")
-    stride = max(table.stride(0), table.shape[1])
-    return Kv8Cache(codes.data_ptr(), scales.data_ptr(), table.data_ptr(), stride, nb, table.shape[1], kvh, hd, fmt)
-
-
-def _kv8_tokens(x, c, what):
-    """Row stride of a tensor of tokens [T, n_kv_heads, head_dim] whose heads lie side by side."""
-    _refuse_unless(x.dim() == 3 and x.shape[1] == c.n_kv_heads and x.shape[2] == c.head_dim and x.stride(2) == 1
-                   and (x.shape[1] == 1 or x.stride(1) == c.head_dim),
-                   f"{what} must be [tokens, {c.n_kv_heads}, {c.head_dim}], each token's heads side by side")
-    return x.stride(0)
-
-
-def _status_arg(status, device):
-    if status is not None:
-        _int32_arg(status, (1,), device, "status")
-    return _ptr(status)
-
-
-def kv8_cache(n_blocks: int, n_kv_heads: int, head_dim: int, dtype=None, device="cuda"):
-    """An empty 8-bit paged KV cache: codes [n_blocks, 2, n_kv_heads, 128, head_dim] (torch.float8_e4m3fn, the default, or
-    torch.int8) and scales [n_blocks, 2, n_kv_heads, 4]."""
-    import torch
-    codes = torch.zeros((n_blocks, 2, n_kv_heads, KV8_PAGE, head_dim), dtype=torch.uint8, device=device)
-    scales = torch.ones((n_blocks, 2, n_kv_heads, KV8_PAGE // KV8_SCALE), dtype=torch.float32, device=device)
-    return codes.view(dtype or torch.float8_e4m3fn), scales
-
-
-def kv8_write(codes, scales, table, k, v, pos0, seq_start, status=None):
-    """Quantise new tokens into the cache (see sara_kv8_write): rows seq_start[i] .. seq_start[i + 1] of k and v
-    [T, n_kv_heads, head_dim] (bf16 or fp16) become positions pos0[i], pos0[i] + 1, ... of sequence i, whose blocks stand
-    in table[i].  pos0 [n_seq] and seq_start [n_seq + 1] int32; status: int32 [1], set to SARA_EINVAL by a wrong range or
-    block id.  Everything on one GPU."""
-    c = _kv8(codes, scales, table)
-    n, dev = table.shape[0], codes.device
-    _refuse_unless(k.dtype == v.dtype and k.shape[0] == v.shape[0] and k.device == dev and v.device == dev,
-                   "k and v must have one type and length, on the cache's device")
-    ks, vs = _kv8_tokens(k, c, "k"), _kv8_tokens(v, c, "v")
-    _int32_arg(pos0, (n,), dev, "pos0")
-    _int32_arg(seq_start, (n + 1,), dev, "seq_start")
-    _launch(dev, load().sara_kv8_write, ctypes.byref(c), n, pos0.data_ptr(), seq_start.data_ptr(), k.shape[0], k.data_ptr(),
-            ks, v.data_ptr(), vs, _type_code(k.dtype, "k", fp32=False), _status_arg(status, dev))
-
-
-def kv8_read(codes, scales, table, pos0, seq_start, total: int, dtype=None, status=None, out=None):
-    """Read positions back (see sara_kv8_read): (k, v), each [total, n_kv_heads, head_dim] of `dtype` (bf16, the default, fp16 or
-    fp32), row seq_start[i] + j holding position pos0[i] + j of sequence i.  `out`: (k, v) to write into instead; rows
-    of no sequence are left as they are there, and are not defined otherwise."""
-    import torch
-    c = _kv8(codes, scales, table)
-    n, dev = table.shape[0], codes.device
-    if out is None:
-        shape = (total, c.n_kv_heads, c.head_dim)
-        out = tuple(torch.empty(shape, dtype=dtype or torch.bfloat16, device=dev) for _ in range(2))
-    k, v = out
-    _refuse_unless(k.dtype == v.dtype and k.shape[0] == v.shape[0] == total and k.device == dev and v.device == dev,
-                   "out must be two tensors of one type and length, on the cache's device")
-    ks, vs = _kv8_tokens(k, c, "out[0]"), _kv8_tokens(v, c, "out[1]")
-    _int32_arg(pos0, (n,), dev, "pos0")
-    _int32_arg(seq_start, (n + 1,), dev, "seq_start")
-    _launch(dev, load().sara_kv8_read, ctypes.byref(c), n, pos0.data_ptr(), seq_start.data_ptr(), total, k.data_ptr(), ks,
-            v.data_ptr(), vs, _type_code(k.dtype, "out"), _status_arg(status, dev))
-    return k, v
-
-
-def attention_kv8_workspace(n_seq: int, n_heads: int, n_kv_heads: int, head_dim: int, device="cuda"):
-    """The scratch of attention_decode_kv8 for up to these sizes, to be kept from call to call (zeroed; calls that
-    share it must not overlap)."""
-    import torch
-    return torch.zeros(load().sara_attention_kv8_workspace_bytes(n_seq, n_heads, n_kv_heads, head_dim), dtype=torch.uint8,
-                       device=device)
-
-
-def attention_decode_kv8(q, codes, scales, table, ctx, first=None, workspace=None, out=None, lse=None, status=None):
-    """Decode attention over the 8-bit cache (see sara_attention_decode_kv8): q [n_seq, n_heads, head_dim] bf16 or fp16, row i over
-    positions first[i] (None: 0) <= p < ctx[i] of sequence i; returns `out`, like q.  lse: fp32 [n_seq, n_heads] that receives the
-    logarithm of each row's sum."""
-    import torch
-    c = _kv8(codes, scales, table)
-    n, dev = table.shape[0], codes.device
-    _refuse_unless(q.dim() == 3 and q.shape[0] == n and q.shape[2] == c.head_dim and q.device == dev and q.stride(2) == 1
-                   and (q.shape[1] == 1 or q.stride(1) == c.head_dim),
-                   f"q must be [{n}, heads, {c.head_dim}] on {dev}, each row's heads side by side")
-    H = q.shape[1]
-    if out is None:
-        out = torch.empty((n, H, c.head_dim), dtype=q.dtype, device=dev)
-    _refuse_unless(out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous() and out.device == dev,
-                   "out must be contiguous and like q")
-    _int32_arg(ctx, (n,), dev, "ctx")
-    if first is not None:
-        _int32_arg(first, (n,), dev, "first")
-    if lse is not None:
-        _f32_arg(lse, (n, H), dev, "lse")
-    if workspace is None:
-        workspace = attention_kv8_workspace(n, H, c.n_kv_heads, c.head_dim, dev)
-    _refuse_unless(workspace.device == dev and workspace.is_contiguous(), "workspace must be contiguous, on the cache's device")
-    _launch(dev, load().sara_attention_decode_kv8, ctypes.byref(c), n, H, q.data_ptr(), q.stride(0), ctx.data_ptr(), _ptr(first),
-            out.data_ptr(), _ptr(lse), _type_code(q.dtype, "q", fp32=False), _status_arg(status, dev), workspace.data_ptr(),
-            workspace.numel() * workspace.element_size())
-    return out
-
-
-@dataclass
-class LogProbs:
-    logprob: object            # [R] fp32, of the given tokens (None without tokens)
-    entropy: object            # [R] fp32
-    stats: object              # [R, 2] fp32: each row's maximum and the logarithm of its sum, for logprobs_backward
-    top_token: object = None   # [R, top] int32, -1 behind the last alternative
-    top_logprob: object = None  # [R, top] fp32
-
-
-def _logits_arg(z, what="logits"):
-    _refuse_unless(z.dim() == 2 and (z.shape[1] == 1 or z.stride(1) == 1), f"{what} must be [rows, vocabulary], rows of consecutive elements")
-    return _type_code(z.dtype, what)
-
-
-def logprobs(logits, tokens, top: int = 0) -> LogProbs:
-    """Log-probabilities of one token per row of logits [R, V] (bf16, fp16 or fp32; rows may be strided), each row's
-    entropy and its `top` (at most 32) most probable tokens (see sara_logprobs).  tokens [R] int32, negative for rows
-    of padding; None: entropy and alternatives alone."""
-    import torch
-    code = _logits_arg(logits)
-    R, V = logits.shape
-    dev = logits.device
-    if tokens is not None:
-        _int32_arg(tokens, (R,), dev, "tokens")
-    _refuse_unless(0 <= top <= 32, "top must be 0 .. 32")
-    o = LogProbs(torch.empty(R, dtype=torch.float32, device=dev) if tokens is not None else None,
-                 torch.empty(R, dtype=torch.float32, device=dev), torch.empty((R, 2), dtype=torch.float32, device=dev))
-    if top:
-        o.top_token = torch.empty((R, top), dtype=torch.int32, device=dev)
-        o.top_logprob = torch.empty((R, top), dtype=torch.float32, device=dev)
-    _launch(dev, load().sara_logprobs, logits.data_ptr(), logits.stride(0), code, R, V, _ptr(tokens), top, _ptr(o.logprob),
-            o.entropy.data_ptr(), o.stats.data_ptr(), _ptr(o.top_token), _ptr(o.top_logprob))
-    return o
-
-
-def logprobs_backward(logits, tokens, stats, entropy, grad_logprob=None, grad_entropy=None, out=None):
-    """Gradient of logprobs with respect to the logits (see sara_logprobs_backward), in the logits' type: grad_logprob and
-    grad_entropy [R] fp32 weigh the rows' log-probabilities and entropies.  `out` may be `logits` itself."""
-    import torch
-    code = _logits_arg(logits)
-    R, V = logits.shape
-    dev = logits.device
-    if tokens is not None:
-        _int32_arg(tokens, (R,), dev, "tokens")
-    _f32_arg(stats, (R, 2), dev, "stats")
-    for x, what in ((entropy, "entropy"), (grad_logprob, "grad_logprob"), (grad_entropy, "grad_entropy")):
-        if x is not None:
-            _f32_arg(x, (R,), dev, what)
-    if out is None:
-        out = torch.empty((R, V), dtype=logits.dtype, device=dev)
-    _refuse_unless(_logits_arg(out, "out") == code and out.shape == logits.shape and out.device == dev, "out must be like logits")
-    _launch(dev, load().sara_logprobs_backward, logits.data_ptr(), logits.stride(0), code, R, V, _ptr(tokens), stats.data_ptr(),
-            _ptr(entropy), _ptr(grad_logprob), _ptr(grad_entropy), out.data_ptr(), out.stride(0))
-    return out
