@@ -22,12 +22,17 @@ namespace sara {
 
 constexpr int kAttnKv8Warps = 4;
 constexpr int kAttnKv8Threads = 32 * kAttnKv8Warps;
-constexpr int kAttnKv8Step = 16 * kAttnKv8Warps;                // positions of an entry of the list
-constexpr int kAttnKv8PageSteps = kKv8Page / kAttnKv8Step;
+// Positions that a warp takes at a time: as many bytes in flight at 64 dims as at 128; 32 is a scale's block
+__host__ __device__ constexpr int attn_kv8_positions(int hd) { return hd == 128 ? 16 : 32; }
+__host__ __device__ constexpr int attn_kv8_step(int hd) { return attn_kv8_positions(hd) * kAttnKv8Warps; }  // positions of an entry of the list
 constexpr int kAttnKv8SmCtas = 16 / kAttnKv8Warps;
 constexpr int kAttnKv8MaxCtas = 160 * kAttnKv8SmCtas;
 constexpr int kAttnKv8Group = 16;                               // states joined at a time
 constexpr int kAttnKv8Groups = kAttnKv8MaxCtas / kAttnKv8Group + 1;
+constexpr float kAttnKv8Shift = 7.f;                            // log2 of the probabilities' scale
+
+// Floats of a state: max and sum of 8 heads, then their outputs
+__host__ __device__ constexpr int attn_kv8_state(int hd) { return 8 * (hd + 2); }
 
 struct AttnKv8Params {
     Kv8Cache c;
@@ -38,7 +43,7 @@ struct AttnKv8Params {
     float *lse;
     int32_t *status;
     int *count;   // [CTA][2][2] arrivals at the two levels of a join, kept at its first state; left zero
-    float *part;  // [CTA][2][8 (hd + 2)] states: max and sum of 8 heads, then their outputs
+    float *part;  // [CTA][2] states
     int n, H, type;
     float scale_log2;  // log2(e) / sqrt(hd)
 };
@@ -79,17 +84,15 @@ struct AttnKv8Row {
     int first, ctx, step0, steps;
     bool bad;
 };
-__device__ __forceinline__ AttnKv8Row attn_kv8_row(int ctx, int first, int max_blocks) {
-    AttnKv8Row r;
-    r.ctx = ctx;
-    r.first = min(first, ctx);  // (past the end: no position)
-    r.bad = r.ctx < 0 || r.first < 0 || r.ctx > (int64_t)max_blocks * kKv8Page;
-    r.step0 = r.first / kAttnKv8Step;
-    r.steps = r.bad || r.ctx <= r.first ? 0 : (r.ctx - 1) / kAttnKv8Step - r.step0 + 1;
-    return r;
-}
+template <int STEP>
 __device__ __forceinline__ AttnKv8Row attn_kv8_row(const AttnKv8Params &p, int i) {
-    return attn_kv8_row(__ldg(p.ctx + i), p.first ? __ldg(p.first + i) : 0, p.c.max_blocks);
+    AttnKv8Row r;
+    r.ctx = __ldg(p.ctx + i);
+    r.first = p.first ? min(__ldg(p.first + i), r.ctx) : 0;  // (past the end: no position)
+    r.bad = r.ctx < 0 || r.first < 0 || r.ctx > (int64_t)p.c.max_blocks * kKv8Page;
+    r.step0 = r.first / STEP;
+    r.steps = r.bad || r.ctx <= r.first ? 0 : (r.ctx - 1) / STEP - r.step0 + 1;
+    return r;
 }
 
 // Inclusive prefix of v over the CTA's threads, and the total
@@ -113,16 +116,110 @@ __device__ __forceinline__ int attn_kv8_scan(int v, int &total, int *room) {
     return before + v;
 }
 
+// Two neighbouring outputs, at place i of a state
+template <int HD>
+__device__ __forceinline__ void attn_kv8_put(const AttnKv8Params &p, int row, int head, int i, float y0, float y1) {
+    const int dim = HD / 8 * (i % 16 / 2) + i / 16 * 2;
+    *reinterpret_cast<uint32_t *>(p.out + ((int64_t)row * p.H + head) * HD + dim) =
+        p.type == SARA_BF16 ? pack2<SARA_BF16>(y0, y1) : pack2<SARA_FP16>(y0, y1);
+}
+
+// CTA c has written its state of a (row, KV head) that CTAs c0 .. c1 share; the last of them joins the states.  More than a
+// group's are joined group by group first, each group's result in the place of its first state.
+template <int HD>
+__device__ __forceinline__ void attn_kv8_join(const AttnKv8Params &p, int row, int h, int c, int c0, int c1) {
+    __shared__ float s_M[8], s_L[8], s_f[8][kAttnKv8Groups];
+    __shared__ int s_last;
+    const int tid = threadIdx.x, G = p.H / p.c.KVH;
+    const bool two = c1 - c0 >= kAttnKv8Group;
+    int from = c0, n = c1 - c0 + 1, pace = 1;
+    if (two) {
+        from = max(c0, c & ~(kAttnKv8Group - 1));
+        n = min(c1, c | (kAttnKv8Group - 1)) - from + 1;
+    }
+    auto state = [&](int k) {  // of the group's member k
+        const int x = pace == 1 ? from + k : k == 0 ? c0 : (c0 & ~(kAttnKv8Group - 1)) + k * kAttnKv8Group;
+        return p.part + (x * 2 + (x == c0)) * attn_kv8_state(HD);
+    };
+#pragma unroll 1
+    for (int level = 0;; ++level) {
+        __syncthreads();
+        if (tid == 0) {
+            int *arrived = p.count + (from * 2 + (from == c0)) * 2 + level;
+            s_last = atom_add_acq_rel_gpu(arrived, 1) == n - 1;  // (orders the CTA's stores before it, its loads behind)
+            if (s_last) *arrived = 0;
+        }
+        __syncthreads();
+        if (!s_last) return;
+        const bool final = level == 1 || !two;
+        {  // the states' factors, 16 lanes a head
+            const int hh = tid / 16;
+            float M = -3.4028235e38f, L = 0.f;
+#pragma unroll 1
+            for (int k = tid % 16; k < n; k += 16) {
+                const float m = __ldcg(state(k) + hh), l = __ldcg(state(k) + 8 + hh), N = fmaxf(M, m);
+                L = L * ex2(M - N) + l * ex2(m - N);
+                M = N;
+                s_f[hh][k] = m;
+            }
+            float N = M;
+#pragma unroll
+            for (int d = 8; d > 0; d >>= 1) N = fmaxf(N, __shfl_xor_sync(0xffffffffu, N, d));
+            L *= ex2(M - N);
+#pragma unroll
+            for (int d = 8; d > 0; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
+            for (int k = tid % 16; k < n; k += 16) s_f[hh][k] = ex2(s_f[hh][k] - N);
+            if (tid % 16 == 0) {
+                s_M[hh] = N;
+                s_L[hh] = L;
+            }
+        }
+        __syncthreads();
+        for (int e = tid; e < G * HD / 4; e += kAttnKv8Threads) {
+            const int hh = e / (HD / 4), i = e % (HD / 4) * 4;
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+            for (int k = 0; k < n; ++k) {
+                const float4 z = __ldcg(reinterpret_cast<const float4 *>(state(k) + 16 + 4 * e));
+                const float f = s_f[hh][k];
+                y.x += f * z.x;
+                y.y += f * z.y;
+                y.z += f * z.z;
+                y.w += f * z.w;
+            }
+            if (final) {
+                const float L = s_L[hh];
+                attn_kv8_put<HD>(p, row, h * G + hh, i, y.x / L, y.y / L);
+                attn_kv8_put<HD>(p, row, h * G + hh, i + 2, y.z / L, y.w / L);
+            } else {
+                *reinterpret_cast<float4 *>(state(0) + 16 + 4 * e) = y;
+            }
+        }
+        if (tid < G) {
+            if (!final) {
+                state(0)[tid] = s_M[tid];
+                state(0)[8 + tid] = s_L[tid];
+            } else if (p.lse) {
+                p.lse[(int64_t)row * p.H + h * G + tid] = (s_M[tid] - kAttnKv8Shift + log2f(s_L[tid])) * 0.69314718f;
+            }
+        }
+        if (final) return;
+        from = c0;
+        n = c1 / kAttnKv8Group - c0 / kAttnKv8Group + 1;
+        pace = kAttnKv8Group;
+    }
+}
+
 template <int HD, int FMT>
 __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kernel(AttnKv8Params p) {
     constexpr int KW = HD / 16, VW = HD / 32, NT = HD / 16;  // words a lane of a key row, of a value row; output tiles
     constexpr int KL = KW < 4 ? KW : 4;                      // words a load
+    constexpr int POS = attn_kv8_positions(HD), NG = POS / 16, STEP = attn_kv8_step(HD), PS = kKv8Page / STEP;
     constexpr int PITCH = HD + 4;                            // (conflict-free 8-byte stores)
-    constexpr int STATE = 8 * (HD + 2);
-    constexpr float kShift = 7.f;
+    constexpr int STATE = attn_kv8_state(HD);
     __shared__ __align__(16) float s_o[kAttnKv8Warps][8][PITCH];
-    __shared__ float s_m[kAttnKv8Warps][8], s_l[kAttnKv8Warps][8], s_M[8], s_L[8], s_f[8][kAttnKv8Groups];
-    __shared__ int s_room[kAttnKv8Warps], s_row, s_base, s_last;
+    __shared__ float s_m[kAttnKv8Warps][8], s_l[kAttnKv8Warps][8], s_M[8], s_L[8];
+    __shared__ int s_room[kAttnKv8Warps], s_row, s_base;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int KVH = p.c.KVH, G = p.H / KVH;
     const float nan = __int_as_float(0x7fc00000);
@@ -132,7 +229,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
     bool idle = false;  // a row without a position (or a wrong one) that is this CTA's to write
     for (int b = 0; b < p.n; b += kAttnKv8Threads) {
         int sum;
-        steps = b + tid < p.n ? attn_kv8_row(p, b + tid).steps : 0;
+        steps = b + tid < p.n ? attn_kv8_row<STEP>(p, b + tid).steps : 0;
         idle = idle || (b + tid < p.n && steps == 0 && (unsigned)(b + tid) % gridDim.x == blockIdx.x);
         end = total + attn_kv8_scan(steps, sum, s_room);
         total += sum;
@@ -149,7 +246,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
     } else if (lo < hi) {
         for (int b = 0, before = 0; b < p.n && before * KVH <= lo; b += kAttnKv8Threads) {
             int sum;
-            steps = b + tid < p.n ? attn_kv8_row(p, b + tid).steps : 0;
+            steps = b + tid < p.n ? attn_kv8_row<STEP>(p, b + tid).steps : 0;
             end = before + attn_kv8_scan(steps, sum, s_room);
             if (lo < end * KVH && lo >= (end - steps) * KVH) {
                 s_row = b + tid;
@@ -160,7 +257,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
     }
     if (__syncthreads_or(idle)) {
         for (int i = c; i < p.n; i += gridDim.x) {
-            const AttnKv8Row r = attn_kv8_row(p, i);
+            const AttnKv8Row r = attn_kv8_row<STEP>(p, i);
             if (r.steps) continue;
             const float y = r.bad ? nan : 0.f;
             const uint32_t y2 = p.type == SARA_BF16 ? pack2<SARA_BF16>(y, y) : pack2<SARA_FP16>(y, y);
@@ -176,29 +273,24 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
         const int big = more * (share + 1);
         return x < big ? x / (share + 1) : more + (x - big) / share;
     };
-    auto put = [&](int row, int head, int i, float y0, float y1) {  // two neighbouring outputs, at place i of a state
-        const int dim = HD / 8 * (i % 16 / 2) + i / 16 * 2;
-        *reinterpret_cast<uint32_t *>(p.out + ((int64_t)row * p.H + head) * HD + dim) =
-            p.type == SARA_BF16 ? pack2<SARA_BF16>(y0, y1) : pack2<SARA_FP16>(y0, y1);
-    };
     int row = s_row, base = s_base;
-    AttnKv8Row r = attn_kv8_row(p, row);
+    AttnKv8Row r = attn_kv8_row<STEP>(p, row);
 
     for (int at = lo; at < hi;) {
         const int h = (at - base) / r.steps, a = at - base - h * r.steps, unit = base + h * r.steps;
         const int b = min(r.steps, hi - unit);  // entries a .. b of the row's, for KV head h
-        // this warp's positions of step x: 64 x + 16 warp .. + 15; the row's first and last step may have none
+        // this warp's positions of step x: STEP x + POS warp .. + POS - 1; the row's first and last step may have none
         int xa = r.step0 + a, xb = r.step0 + b;
-        if (xa * kAttnKv8Step + 16 * warp + 16 <= r.first) ++xa;
-        if ((xb - 1) * kAttnKv8Step + 16 * warp >= r.ctx) --xb;
+        if (xa * STEP + POS * (warp + 1) <= r.first) ++xa;
+        if ((xb - 1) * STEP + POS * warp >= r.ctx) --xb;
         const int32_t *tab = p.c.table + row * p.c.table_stride;
         int ids = 0, idbase = 0;  // this lane's entry of the 32 table entries from idbase on
         bool wrong = false;
         auto block_of = [&](int x, bool begin) {
-            const int page = x / kAttnKv8PageSteps;
+            const int page = x / PS;
             if (begin || page - idbase >= 32) {
                 idbase = page;
-                ids = (page + lane) * kAttnKv8PageSteps < xb ? __ldg(tab + page + lane) : 0;
+                ids = (page + lane) * PS < xb ? __ldg(tab + page + lane) : 0;
                 const bool out = ids < 0 || ids >= p.c.n_blocks;
                 wrong = wrong || out;
                 ids = out ? -1 : ids;
@@ -206,32 +298,45 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             return __shfl_sync(0xffffffffu, ids, page - idbase);
         };
         const int lane_k = (KW == 8 ? 16 : HD / 4) * t, lane_v = HD / 8 * g;
-        auto edge = [&](int x) {  // whether some of the 16 positions are masked
-            const int p0 = x * kAttnKv8Step + 16 * warp;
-            return p0 < r.first || p0 + 16 > r.ctx;
+        auto edge = [&](int x) {  // whether some of its positions are masked
+            const int p0 = x * STEP + POS * warp;
+            return p0 < r.first || p0 + POS > r.ctx;
         };
         auto slot_of = [&](int x, int e) {  // (masked positions stand for the nearest that is not: their probability is 0)
-            return min(max(x * kAttnKv8Step + 16 * warp + e, r.first), r.ctx - 1) & (kKv8Page - 1);
+            return min(max(x * STEP + POS * warp + e, r.first), r.ctx - 1) & (kKv8Page - 1);
         };
-        auto block_in_page = [&](int x) { return (x % kAttnKv8PageSteps * kAttnKv8Step + 16 * warp) / kKv8Block; };
-        uint32_t kr[2][KW];
-        float ks = 0.f;
+        auto block_in_page = [&](int x) { return (x % PS * STEP + POS * warp) / kKv8Block; };
+        uint32_t kr[2 * NG][KW], vr[4 * NG][VW];  // positions g + 8 e; 2 t + (e & 1) + 8 (e >> 1)
+        float ks = 0.f, vs = 0.f;
         int blk = 0;
         auto load_k = [&](int x) {
             const int64_t tile = kv8_tile(p.c, max(blk, 0), 0, h);
             ks = blk < 0 ? nan : __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
             const uint8_t *k = p.c.codes + tile * (kKv8Page * HD) + lane_k;
             if (!edge(x)) {
-                k += (x % kAttnKv8PageSteps * kAttnKv8Step + 16 * warp + g) * HD;
+                k += (x % PS * STEP + POS * warp + g) * HD;
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
+                for (int e = 0; e < 2 * NG; ++e)
 #pragma unroll
                     for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + 8 * e * HD + 64 * i, &kr[e][4 * i]);
             } else {
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
+                for (int e = 0; e < 2 * NG; ++e)
 #pragma unroll
                     for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + slot_of(x, g + 8 * e) * HD + 64 * i, &kr[e][4 * i]);
+            }
+        };
+        auto load_v = [&](int x) {
+            const int64_t tile = kv8_tile(p.c, max(blk, 0), 1, h);
+            vs = __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
+            const uint8_t *v = p.c.codes + tile * (kKv8Page * HD) + lane_v;
+            if (!edge(x)) {
+                v += (x % PS * STEP + POS * warp + 2 * t) * HD;
+#pragma unroll
+                for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(v + ((e & 1) + 8 * (e >> 1)) * HD, vr[e]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(v + slot_of(x, 2 * t + (e & 1) + 8 * (e >> 1)) * HD, vr[e]);
             }
         };
         if (xa < xb) {
@@ -283,45 +388,45 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
 #pragma unroll 1
         for (int x = xa; x < xb; ++x) {
-            // this step's values come while its scores are taken, the next one's keys after that
-            uint32_t vr[4][VW];
-            const int64_t tile = kv8_tile(p.c, max(blk, 0), 1, h);
-            const float vs = __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
-            const uint8_t *v = p.c.codes + tile * (kKv8Page * HD) + lane_v;
-            const bool cut = edge(x);
-            if (!cut) {
-                v += (x % kAttnKv8PageSteps * kAttnKv8Step + 16 * warp + 2 * t) * HD;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) load_codes<VW>(v + ((e & 1) + 8 * (e >> 1)) * HD, vr[e]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) load_codes<VW>(v + slot_of(x, 2 * t + (e & 1) + 8 * (e >> 1)) * HD, vr[e]);
-            }
-            float s[4] = {0.f, 0.f, 0.f, 0.f}, s2[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < KW; ++i) {
-                uint32_t f[4];
-                decode4_half<FMT>(kr[0][i], f[0], f[2]);
-                decode4_half<FMT>(kr[1][i], f[1], f[3]);
-                mma_f16_16816(i & 1 ? s2 : s, f, qb[i][0], qb[i][1]);
-            }
+            // the next step's keys load over this one's as soon as the scores are taken, its values once they are used
+            load_v(x);
+            float s[NG][4];
             const float f0 = ks * mul0, f1 = ks * mul1;
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+                float s2[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+#pragma unroll
+                for (int i = 0; i < KW; ++i) {
+                    uint32_t f[4];
+                    decode4_half<FMT>(kr[2 * n][i], f[0], f[2]);
+                    decode4_half<FMT>(kr[2 * n + 1][i], f[1], f[3]);
+                    mma_f16_16816(i & 1 ? s2 : s[n], f, qb[i][0], qb[i][1]);
+                }
+                // s[n][0], s[n][1]: position 16 n + g, heads 2 t and 2 t + 1; s[n][2], s[n][3]: position 16 n + g + 8
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] = (s[n][e] + s2[e]) * (e & 1 ? f1 : f0);
+            }
+            const bool cut = edge(x);
+            const float vsc = vs;
             if (x + 1 < xb) {
                 blk = block_of(x + 1, false);
                 load_k(x + 1);
             }
-            // s[0], s[1]: position g, heads 2 t and 2 t + 1; s[2], s[3]: position g + 8
-            s[0] = (s[0] + s2[0]) * f0;
-            s[1] = (s[1] + s2[1]) * f1;
-            s[2] = (s[2] + s2[2]) * f0;
-            s[3] = (s[3] + s2[3]) * f1;
-            if (cut) {
-                const int p0 = x * kAttnKv8Step + 16 * warp + g;
-                if (p0 < r.first || p0 >= r.ctx) s[0] = s[1] = -INFINITY;
-                if (p0 + 8 < r.first || p0 + 8 >= r.ctx) s[2] = s[3] = -INFINITY;
+            float t0 = -INFINITY, t1 = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+                if (cut) {
+                    const int p0 = x * STEP + POS * warp + 16 * n + g;
+                    if (p0 < r.first || p0 >= r.ctx) s[n][0] = s[n][1] = -INFINITY;
+                    if (p0 + 8 < r.first || p0 + 8 >= r.ctx) s[n][2] = s[n][3] = -INFINITY;
+                }
+                t0 = fmaxf(t0, fmaxf(s[n][0], s[n][2]));
+                t1 = fmaxf(t1, fmaxf(s[n][1], s[n][3]));
             }
-            if (__any_sync(0xffffffffu, fmaxf(s[0], s[2]) > m0 + 8.f || fmaxf(s[1], s[3]) > m1 + 8.f)) {
-                float n0 = fmaxf(m0, fmaxf(s[0], s[2])), n1 = fmaxf(m1, fmaxf(s[1], s[3]));
+            if (__any_sync(0xffffffffu, t0 > m0 + 8.f || t1 > m1 + 8.f)) {
+                float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) {
                     n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, d));
@@ -340,42 +445,45 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                     o[j][3] *= a1;
                 }
             }
-            const float c0 = m0 - kShift, c1 = m1 - kShift;
-            float w0 = ex2(s[0] - c0), w1 = ex2(s[1] - c1), w2 = ex2(s[2] - c0), w3 = ex2(s[3] - c1);
-            l0 += w0 + w2;
-            l1 += w1 + w3;
-            if (!(vs <= vref)) {  // the largest scale so far (or NaN)
-                const float inv = 1.f / vs, f = vref * inv;
-                vref = vs;
+            if (!(vsc <= vref)) {  // the largest scale so far (or NaN)
+                const float inv = 1.f / vsc, f = vref * inv;
+                vref = vsc;
                 vinv = inv;
 #pragma unroll
                 for (int j = 0; j < NT; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[j][e] *= f;
             }
-            const float vf = vs * vinv;
-            w0 *= vf;
-            w1 *= vf;
-            w2 *= vf;
-            w3 *= vf;
-            uint32_t ph[2] = {pack_half2(w0, w1), pack_half2(w2, w3)}, pl[2];
-            const float2 h0 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[0]));
-            const float2 h1 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[1]));
-            pl[0] = movmatrix_trans(pack_half2(w0 - h0.x, w1 - h0.y));
-            pl[1] = movmatrix_trans(pack_half2(w2 - h1.x, w3 - h1.y));
-            ph[0] = movmatrix_trans(ph[0]);
-            ph[1] = movmatrix_trans(ph[1]);
+            const float c0 = m0 - kAttnKv8Shift, c1 = m1 - kAttnKv8Shift, vf = vsc * vinv;
 #pragma unroll
-            for (int i = 0; i < VW; ++i) {
-                uint32_t v0[4], v1[4];  // dims 4 i, 4 i + 1 and 4 i + 2, 4 i + 3 of the lane's
-                decode4_half<FMT>(__byte_perm(vr[0][i], vr[1][i], 0x5140), v0[0], v0[1]);
-                decode4_half<FMT>(__byte_perm(vr[2][i], vr[3][i], 0x5140), v0[2], v0[3]);
-                decode4_half<FMT>(__byte_perm(vr[0][i], vr[1][i], 0x7362), v1[0], v1[1]);
-                decode4_half<FMT>(__byte_perm(vr[2][i], vr[3][i], 0x7362), v1[2], v1[3]);
-                mma_f16_16816(o[2 * i], v0, ph[0], ph[1]);
-                mma_f16_16816(o[2 * i + 1], v1, ph[0], ph[1]);
-                mma_f16_16816(o[2 * i], v0, pl[0], pl[1]);
-                mma_f16_16816(o[2 * i + 1], v1, pl[0], pl[1]);
+            for (int n = 0; n < NG; ++n) {
+                float w0 = ex2(s[n][0] - c0), w1 = ex2(s[n][1] - c1), w2 = ex2(s[n][2] - c0), w3 = ex2(s[n][3] - c1);
+                l0 += w0 + w2;
+                l1 += w1 + w3;
+                w0 *= vf;
+                w1 *= vf;
+                w2 *= vf;
+                w3 *= vf;
+                uint32_t ph[2] = {pack_half2(w0, w1), pack_half2(w2, w3)}, pl[2];
+                const float2 h0 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[0]));
+                const float2 h1 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[1]));
+                pl[0] = movmatrix_trans(pack_half2(w0 - h0.x, w1 - h0.y));
+                pl[1] = movmatrix_trans(pack_half2(w2 - h1.x, w3 - h1.y));
+                ph[0] = movmatrix_trans(ph[0]);
+                ph[1] = movmatrix_trans(ph[1]);
+#pragma unroll
+                for (int i = 0; i < VW; ++i) {
+                    uint32_t v0[4], v1[4];  // dims 4 i, 4 i + 1 and 4 i + 2, 4 i + 3 of the lane's
+                    const uint32_t a = vr[4 * n][i], b = vr[4 * n + 1][i], c = vr[4 * n + 2][i], d = vr[4 * n + 3][i];
+                    decode4_half<FMT>(__byte_perm(a, b, 0x5140), v0[0], v0[1]);
+                    decode4_half<FMT>(__byte_perm(c, d, 0x5140), v0[2], v0[3]);
+                    decode4_half<FMT>(__byte_perm(a, b, 0x7362), v1[0], v1[1]);
+                    decode4_half<FMT>(__byte_perm(c, d, 0x7362), v1[2], v1[3]);
+                    mma_f16_16816(o[2 * i], v0, ph[0], ph[1]);
+                    mma_f16_16816(o[2 * i + 1], v1, ph[0], ph[1]);
+                    mma_f16_16816(o[2 * i], v0, pl[0], pl[1]);
+                    mma_f16_16816(o[2 * i + 1], v1, pl[0], pl[1]);
+                }
             }
         }
         if (wrong) kv8_report(p.status);
@@ -424,7 +532,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                 y0 += f * y.x;
                 y1 += f * y.y;
             }
-            if (whole) put(row, h * G + hh, i, y0 / s_L[hh], y1 / s_L[hh]);
+            if (whole) attn_kv8_put<HD>(p, row, h * G + hh, i, y0 / s_L[hh], y1 / s_L[hh]);
             else *reinterpret_cast<float2 *>(mine + 16 + hh * HD + i) = make_float2(y0, y1);
         }
         if (tid < G) {
@@ -432,100 +540,23 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                 mine[tid] = s_M[tid];
                 mine[8 + tid] = s_L[tid];
             } else if (p.lse) {
-                p.lse[(int64_t)row * p.H + h * G + tid] = (s_M[tid] - kShift + log2f(s_L[tid])) * 0.69314718f;
+                p.lse[(int64_t)row * p.H + h * G + tid] = (s_M[tid] - kAttnKv8Shift + log2f(s_L[tid])) * 0.69314718f;
             }
         }
         if (!whole) {
-            // the unit's states are those of CTAs c0 .. c1; more than a group's are joined group by group first, each group's
-            // result in the place of its first state
-            const int c0 = cta_of(unit), c1 = cta_of(unit + r.steps - 1);
-            const bool two = c1 - c0 >= kAttnKv8Group;
-            int from = c0, n = c1 - c0 + 1, pace = 1;
-            if (two) {
-                from = max(c0, c & ~(kAttnKv8Group - 1));
-                n = min(c1, c | (kAttnKv8Group - 1)) - from + 1;
-            }
-            auto member = [&](int k) { return pace == 1 ? from + k : k == 0 ? c0 : (c0 & ~(kAttnKv8Group - 1)) + k * kAttnKv8Group; };
-            auto state = [&](int x) { return p.part + (x * 2 + (x == c0)) * STATE; };
-            for (int level = 0;; ++level) {
-                __threadfence();
-                __syncthreads();
-                if (tid == 0) {
-                    int *arrived = p.count + (from * 2 + (from == c0)) * 2 + level;
-                    s_last = atomicAdd(arrived, 1) == n - 1;
-                    if (s_last) *arrived = 0;
-                }
-                __syncthreads();
-                if (!s_last) break;
-                __threadfence();
-                const bool final = level == 1 || !two;
-                // factors of the states, 16 lanes a head
-                {
-                    const int hh = tid / 16, k0 = tid % 16;
-                    float M = -3.4028235e38f, L = 0.f;
-                    for (int k = k0; k < n; k += 16) M = fmaxf(M, __ldcg(state(member(k)) + hh));
-#pragma unroll
-                    for (int d = 8; d > 0; d >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, d));
-                    for (int k = k0; k < n; k += 16) {
-                        const float *y = state(member(k));
-                        const float f = ex2(__ldcg(y + hh) - M);
-                        s_f[hh][k] = f;
-                        L += f * __ldcg(y + 8 + hh);
-                    }
-#pragma unroll
-                    for (int d = 8; d > 0; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
-                    if (k0 == 0) {
-                        s_M[hh] = M;
-                        s_L[hh] = L;
-                    }
-                }
-                __syncthreads();
-                float *to = state(from);
-                for (int e = tid; e < G * HD / 4; e += kAttnKv8Threads) {
-                    const int hh = e / (HD / 4), i = e % (HD / 4) * 4;
-                    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-                    for (int k = 0; k < n; ++k) {
-                        const float4 z = __ldcg(reinterpret_cast<const float4 *>(state(member(k)) + 16 + hh * HD + i));
-                        const float f = s_f[hh][k];
-                        y.x += f * z.x;
-                        y.y += f * z.y;
-                        y.z += f * z.z;
-                        y.w += f * z.w;
-                    }
-                    if (final) {
-                        const float L = s_L[hh];
-                        put(row, h * G + hh, i, y.x / L, y.y / L);
-                        put(row, h * G + hh, i + 2, y.z / L, y.w / L);
-                    } else {
-                        *reinterpret_cast<float4 *>(to + 16 + hh * HD + i) = y;
-                    }
-                }
-                if (tid < G) {
-                    if (!final) {
-                        to[tid] = s_M[tid];
-                        to[8 + tid] = s_L[tid];
-                    } else if (p.lse) {
-                        p.lse[(int64_t)row * p.H + h * G + tid] = (s_M[tid] - kShift + log2f(s_L[tid])) * 0.69314718f;
-                    }
-                }
-                if (final) break;
-                from = c0;
-                n = c1 / kAttnKv8Group - c0 / kAttnKv8Group + 1;
-                pace = kAttnKv8Group;
-            }
+            attn_kv8_join<HD>(p, row, h, c, cta_of(unit), cta_of(unit + r.steps - 1));
         }
         __syncthreads();  // (shared memory is the next unit's)
         at = unit + b;
         if (at < hi && h == KVH - 1) {
             base += KVH * r.steps;
-            do r = attn_kv8_row(p, ++row);
+            do r = attn_kv8_row<STEP>(p, ++row);
             while (r.steps == 0);
         }
     }
 }
 
 inline size_t attn_kv8_count_bytes() { return kAttnKv8MaxCtas * 4 * sizeof(int); }
-inline size_t attn_kv8_workspace(int hd) { return attn_kv8_count_bytes() + (size_t)kAttnKv8MaxCtas * 2 * 8 * (hd + 2) * sizeof(float); }
+inline size_t attn_kv8_workspace(int hd) { return attn_kv8_count_bytes() + (size_t)kAttnKv8MaxCtas * 2 * attn_kv8_state(hd) * sizeof(float); }
 
 }  // namespace sara

@@ -127,7 +127,7 @@ int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
         p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)cache->head_dim));
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         // as many CTAs as fit, fewer where there are not as many entries
-        const int64_t entries = (int64_t)n_seq * cache->n_kv_heads * cache->max_blocks * kAttnKv8PageSteps;
+        const int64_t entries = (int64_t)n_seq * cache->n_kv_heads * cache->max_blocks * (kKv8Page / attn_kv8_step(cache->head_dim));
         if (entries > INT32_MAX) throw SaraError(SARA_EINVAL, "too many blocks");
         const unsigned ctas = (unsigned)std::min<int64_t>(std::min(kAttnKv8SmCtas * sm_count(), kAttnKv8MaxCtas), entries);
         by_shape(cache, [&](auto hd, auto fmt) {
