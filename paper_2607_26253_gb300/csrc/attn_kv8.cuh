@@ -124,40 +124,64 @@ __device__ __forceinline__ void attn_kv8_put(const AttnKv8Params &p, int row, in
         p.type == SARA_BF16 ? pack2<SARA_BF16>(y0, y1) : pack2<SARA_FP16>(y0, y1);
 }
 
-// CTA c has written its state of a (row, KV head) that CTAs c0 .. c1 share; the last of them joins the states.  More than a
-// group's are joined group by group first, each group's result in the place of its first state.
+// A (row, KV head) that CTAs c0 .. c1 share, as CTA c sees it: its states, or where there are more than a group's those
+// of its group, whose result takes the place of the first; then the groups' results.
+struct AttnKv8Join {
+    int row, h, c0, c1;  // row < 0: nothing
+};
 template <int HD>
-__device__ __forceinline__ void attn_kv8_join(const AttnKv8Params &p, int row, int h, int c, int c0, int c1) {
-    __shared__ float s_M[8], s_L[8], s_f[8][kAttnKv8Groups];
-    __shared__ int s_last;
-    const int tid = threadIdx.x, G = p.H / p.c.KVH;
-    const bool two = c1 - c0 >= kAttnKv8Group;
-    int from = c0, n = c1 - c0 + 1, pace = 1;
-    if (two) {
-        from = max(c0, c & ~(kAttnKv8Group - 1));
-        n = min(c1, c | (kAttnKv8Group - 1)) - from + 1;
-    }
-    auto state = [&](int k) {  // of the group's member k
-        const int x = pace == 1 ? from + k : k == 0 ? c0 : (c0 & ~(kAttnKv8Group - 1)) + k * kAttnKv8Group;
-        return p.part + (x * 2 + (x == c0)) * attn_kv8_state(HD);
-    };
-#pragma unroll 1
-    for (int level = 0;; ++level) {
-        __syncthreads();
-        if (tid == 0) {
-            int *arrived = p.count + (from * 2 + (from == c0)) * 2 + level;
-            s_last = atom_add_acq_rel_gpu(arrived, 1) == n - 1;  // (orders the CTA's stores before it, its loads behind)
-            if (s_last) *arrived = 0;
+struct AttnKv8Group {
+    const AttnKv8Params &p;
+    const AttnKv8Join j;
+    int from, n, pace;
+    __device__ __forceinline__ AttnKv8Group(const AttnKv8Params &p_, const AttnKv8Join &j_, int c) : p(p_), j(j_), from(j_.c0), n(j_.c1 - j_.c0 + 1), pace(1) {
+        if (two()) {
+            from = max(j.c0, c & ~(kAttnKv8Group - 1));
+            n = min(j.c1, c | (kAttnKv8Group - 1)) - from + 1;
         }
-        __syncthreads();
-        if (!s_last) return;
-        const bool final = level == 1 || !two;
-        {  // the states' factors, 16 lanes a head
+    }
+    __device__ __forceinline__ bool two() const { return j.c1 - j.c0 >= kAttnKv8Group; }
+    __device__ __forceinline__ void groups() {
+        from = j.c0;
+        n = j.c1 / kAttnKv8Group - j.c0 / kAttnKv8Group + 1;
+        pace = kAttnKv8Group;
+    }
+    __device__ __forceinline__ float *state(int k) const {
+        const int x = pace == 1 ? from + k : k == 0 ? j.c0 : (j.c0 & ~(kAttnKv8Group - 1)) + k * kAttnKv8Group;
+        return p.part + (x * 2 + (x == j.c0)) * attn_kv8_state(HD);
+    }
+    // One thread, after a barrier: whether the CTA is the last of the group to come
+    __device__ __forceinline__ bool arrive() const {
+        int *arrived = p.count + (from * 2 + (from == j.c0)) * 2 + (pace > 1);
+        const bool last = atom_add_acq_rel_gpu(arrived, 1) == n - 1;  // (orders the CTA's stores before it, its loads behind)
+        if (last) *arrived = 0;
+        return last;
+    }
+};
+
+// The last CTA of a group joins its states, and so on up.  Whole CTAs; s_f, s_ml: room for factors and results of 8 heads.
+template <int HD>
+__device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD> u, float (*s_f)[kAttnKv8Groups], float (*s_ml)[8], int *s_last) {
+    constexpr int B = 8;  // states at a time
+    const AttnKv8Params &p = u.p;
+    const int tid = threadIdx.x, G = p.H / p.c.KVH;
+#pragma unroll 1
+    for (;;) {
+        const bool final = !u.two() || u.pace > 1;
+        // the first states' outputs are on their way while the factors are made, 16 lanes a head
+        float4 z[B];
+        auto load = [&](int e, int k0) {
+#pragma unroll
+            for (int k = 0; k < B; ++k)
+                if (k0 + k < u.n && e < G * HD / 4) z[k] = __ldcg(reinterpret_cast<const float4 *>(u.state(k0 + k) + 16 + 4 * e));
+        };
+        load(tid, 0);
+        {
             const int hh = tid / 16;
             float M = -3.4028235e38f, L = 0.f;
 #pragma unroll 1
-            for (int k = tid % 16; k < n; k += 16) {
-                const float m = __ldcg(state(k) + hh), l = __ldcg(state(k) + 8 + hh), N = fmaxf(M, m);
+            for (int k = tid % 16; k < u.n; k += 16) {
+                const float m = __ldcg(u.state(k) + hh), l = __ldcg(u.state(k) + 8 + hh), N = fmaxf(M, m);
                 L = L * ex2(M - N) + l * ex2(m - N);
                 M = N;
                 s_f[hh][k] = m;
@@ -168,45 +192,53 @@ __device__ __forceinline__ void attn_kv8_join(const AttnKv8Params &p, int row, i
             L *= ex2(M - N);
 #pragma unroll
             for (int d = 8; d > 0; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
-            for (int k = tid % 16; k < n; k += 16) s_f[hh][k] = ex2(s_f[hh][k] - N);
+            for (int k = tid % 16; k < u.n; k += 16) s_f[hh][k] = ex2(s_f[hh][k] - N);
             if (tid % 16 == 0) {
-                s_M[hh] = N;
-                s_L[hh] = L;
+                s_ml[0][hh] = N;
+                s_ml[1][hh] = L;
             }
         }
         __syncthreads();
+#pragma unroll 1
         for (int e = tid; e < G * HD / 4; e += kAttnKv8Threads) {
             const int hh = e / (HD / 4), i = e % (HD / 4) * 4;
             float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-            for (int k = 0; k < n; ++k) {
-                const float4 z = __ldcg(reinterpret_cast<const float4 *>(state(k) + 16 + 4 * e));
-                const float f = s_f[hh][k];
-                y.x += f * z.x;
-                y.y += f * z.y;
-                y.z += f * z.z;
-                y.w += f * z.w;
+#pragma unroll 1
+            for (int k0 = 0; k0 < u.n; k0 += B) {
+                if (e != tid || k0 > 0) load(e, k0);
+#pragma unroll
+                for (int k = 0; k < B; ++k)
+                    if (k0 + k < u.n) {
+                        const float f = s_f[hh][k0 + k];
+                        y.x += f * z[k].x;
+                        y.y += f * z[k].y;
+                        y.z += f * z[k].z;
+                        y.w += f * z[k].w;
+                    }
             }
             if (final) {
-                const float L = s_L[hh];
-                attn_kv8_put<HD>(p, row, h * G + hh, i, y.x / L, y.y / L);
-                attn_kv8_put<HD>(p, row, h * G + hh, i + 2, y.z / L, y.w / L);
+                const float L = 1.f / s_ml[1][hh];
+                attn_kv8_put<HD>(p, u.j.row, u.j.h * G + hh, i, y.x * L, y.y * L);
+                attn_kv8_put<HD>(p, u.j.row, u.j.h * G + hh, i + 2, y.z * L, y.w * L);
             } else {
-                *reinterpret_cast<float4 *>(state(0) + 16 + 4 * e) = y;
+                *reinterpret_cast<float4 *>(u.state(0) + 16 + 4 * e) = y;
             }
         }
         if (tid < G) {
+            const float M = s_ml[0][tid], L = s_ml[1][tid];
             if (!final) {
-                state(0)[tid] = s_M[tid];
-                state(0)[8 + tid] = s_L[tid];
+                u.state(0)[tid] = M;
+                u.state(0)[8 + tid] = L;
             } else if (p.lse) {
-                p.lse[(int64_t)row * p.H + h * G + tid] = (s_M[tid] - kAttnKv8Shift + log2f(s_L[tid])) * 0.69314718f;
+                p.lse[(int64_t)u.j.row * p.H + u.j.h * G + tid] = (M - kAttnKv8Shift + log2f(L)) * 0.69314718f;
             }
         }
+        __syncthreads();
         if (final) return;
-        from = c0;
-        n = c1 / kAttnKv8Group - c0 / kAttnKv8Group + 1;
-        pace = kAttnKv8Group;
+        u.groups();
+        if (tid == 0) *s_last = u.arrive();
+        __syncthreads();
+        if (!*s_last) return;
     }
 }
 
@@ -218,8 +250,9 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
     constexpr int PITCH = HD + 4;                            // (conflict-free 8-byte stores)
     constexpr int STATE = attn_kv8_state(HD);
     __shared__ __align__(16) float s_o[kAttnKv8Warps][8][PITCH];
-    __shared__ float s_m[kAttnKv8Warps][8], s_l[kAttnKv8Warps][8], s_M[8], s_L[8];
-    __shared__ int s_room[kAttnKv8Warps], s_row, s_base;
+    __shared__ float s_m[kAttnKv8Warps][8], s_l[kAttnKv8Warps][8], s_ml[2][8], s_f[8][kAttnKv8Groups];
+    __shared__ AttnKv8Join s_join[2];
+    __shared__ int s_room[kAttnKv8Warps], s_row, s_base, s_last[2];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int KVH = p.c.KVH, G = p.H / KVH;
     const float nan = __int_as_float(0x7fc00000);
@@ -269,6 +302,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
         }
     }
     if (lo >= hi) return;
+    if (tid < 2) s_join[tid].row = -1;
     auto cta_of = [&](int x) {  // whose share entry x is
         const int big = more * (share + 1);
         return x < big ? x / (share + 1) : more + (x - big) / share;
@@ -506,46 +540,34 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             *reinterpret_cast<float2 *>(&s_o[warp][2 * t + 1][16 * j + 2 * g]) = make_float2(o[j][1] * vref, o[j][3] * vref);
         }
         __syncthreads();
-        if (tid < 8) {
-            float M = s_m[0][tid], L = 0.f;
-#pragma unroll
-            for (int w = 1; w < kAttnKv8Warps; ++w) M = fmaxf(M, s_m[w][tid]);
-#pragma unroll
-            for (int w = 0; w < kAttnKv8Warps; ++w) {
-                const float f = ex2(s_m[w][tid] - M);
-                L += f * s_l[w][tid];
-                s_m[w][tid] = f;
-            }
-            s_M[tid] = M;
-            s_L[tid] = L;
-        }
-        __syncthreads();
         const bool whole = a == 0 && b == r.steps;
         float *mine = p.part + (c * 2 + (a == 0)) * STATE;  // (a share begins in at most one unit that it does not begin)
         for (int e = tid; e < G * HD / 2; e += kAttnKv8Threads) {
             const int hh = e / (HD / 2), i = e % (HD / 2) * 2;
-            float y0 = 0.f, y1 = 0.f;
+            float M = s_m[0][hh], L = 0.f, y0 = 0.f, y1 = 0.f;
+#pragma unroll
+            for (int w = 1; w < kAttnKv8Warps; ++w) M = fmaxf(M, s_m[w][hh]);
 #pragma unroll
             for (int w = 0; w < kAttnKv8Warps; ++w) {
                 const float2 y = *reinterpret_cast<const float2 *>(&s_o[w][hh][i]);
-                const float f = s_m[w][hh];
+                const float f = ex2(s_m[w][hh] - M);
+                L += f * s_l[w][hh];
                 y0 += f * y.x;
                 y1 += f * y.y;
             }
-            if (whole) attn_kv8_put<HD>(p, row, h * G + hh, i, y0 / s_L[hh], y1 / s_L[hh]);
-            else *reinterpret_cast<float2 *>(mine + 16 + hh * HD + i) = make_float2(y0, y1);
-        }
-        if (tid < G) {
-            if (!whole) {
-                mine[tid] = s_M[tid];
-                mine[8 + tid] = s_L[tid];
-            } else if (p.lse) {
-                p.lse[(int64_t)row * p.H + h * G + tid] = (s_M[tid] - kAttnKv8Shift + log2f(s_L[tid])) * 0.69314718f;
+            if (whole) {
+                const float inv = 1.f / L;
+                attn_kv8_put<HD>(p, row, h * G + hh, i, y0 * inv, y1 * inv);
+                if (p.lse && i == 0) p.lse[(int64_t)row * p.H + h * G + hh] = (M - kAttnKv8Shift + log2f(L)) * 0.69314718f;
+            } else {
+                *reinterpret_cast<float2 *>(mine + 16 + hh * HD + i) = make_float2(y0, y1);
+                if (i == 0) {
+                    mine[hh] = M;
+                    mine[8 + hh] = L;
+                }
             }
         }
-        if (!whole) {
-            attn_kv8_join<HD>(p, row, h, c, cta_of(unit), cta_of(unit + r.steps - 1));
-        }
+        if (!whole && tid == 0) s_join[a == 0] = {row, h, cta_of(unit), cta_of(unit + r.steps - 1)};
         __syncthreads();  // (shared memory is the next unit's)
         at = unit + b;
         if (at < hi && h == KVH - 1) {
@@ -554,6 +576,13 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             while (r.steps == 0);
         }
     }
+
+    // the units that other CTAs share: at most the one in which the share begins and the one in which it ends
+    if ((tid == 0 || tid == 32) && s_join[tid / 32].row >= 0) s_last[tid / 32] = AttnKv8Group<HD>(p, s_join[tid / 32], c).arrive();
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < 2; ++i)
+        if (s_join[i].row >= 0 && s_last[i]) attn_kv8_join<HD>({p, s_join[i], c}, s_f, s_ml, &s_last[i]);
 }
 
 inline size_t attn_kv8_count_bytes() { return kAttnKv8MaxCtas * 4 * sizeof(int); }
