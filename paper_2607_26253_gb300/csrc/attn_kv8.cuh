@@ -169,13 +169,19 @@ __device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD> u, float (*s_f)[k
     for (;;) {
         const bool final = !u.two() || u.pace > 1;
         // the first states' outputs are on their way while the factors are made, 16 lanes a head
-        float4 z[B];
-        auto load = [&](int e, int k0) {
+        constexpr int PER = 8 * HD / 4 / kAttnKv8Threads > 0 ? 8 * HD / 4 / kAttnKv8Threads : 1;  // quads of outputs a thread
+        float4 z[PER][B], y[PER];
+        auto load = [&](int k0) {
 #pragma unroll
             for (int k = 0; k < B; ++k)
-                if (k0 + k < u.n && e < G * HD / 4) z[k] = __ldcg(reinterpret_cast<const float4 *>(u.state(k0 + k) + 16 + 4 * e));
+                if (k0 + k < u.n) {
+                    const float4 *src = reinterpret_cast<const float4 *>(u.state(k0 + k) + 16) + tid;
+#pragma unroll
+                    for (int j = 0; j < PER; ++j)
+                        if (tid + j * kAttnKv8Threads < G * HD / 4) z[j][k] = __ldcg(src + j * kAttnKv8Threads);
+                }
         };
-        load(tid, 0);
+        load(0);
         {
             const int hh = tid / 16;
             float M = -3.4028235e38f, L = 0.f;
@@ -199,29 +205,35 @@ __device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD> u, float (*s_f)[k
             }
         }
         __syncthreads();
+#pragma unroll
+        for (int j = 0; j < PER; ++j) y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
-        for (int e = tid; e < G * HD / 4; e += kAttnKv8Threads) {
-            const int hh = e / (HD / 4), i = e % (HD / 4) * 4;
-            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-            for (int k0 = 0; k0 < u.n; k0 += B) {
-                if (e != tid || k0 > 0) load(e, k0);
+        for (int k0 = 0; k0 < u.n; k0 += B) {
+            if (k0 > 0) load(k0);
+#pragma unroll
+            for (int j = 0; j < PER; ++j) {
+                const int hh = min((tid + j * kAttnKv8Threads) / (HD / 4), 7);
 #pragma unroll
                 for (int k = 0; k < B; ++k)
                     if (k0 + k < u.n) {
                         const float f = s_f[hh][k0 + k];
-                        y.x += f * z[k].x;
-                        y.y += f * z[k].y;
-                        y.z += f * z[k].z;
-                        y.w += f * z[k].w;
+                        y[j].x += f * z[j][k].x;
+                        y[j].y += f * z[j][k].y;
+                        y[j].z += f * z[j][k].z;
+                        y[j].w += f * z[j][k].w;
                     }
             }
+        }
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const int e = tid + j * kAttnKv8Threads, hh = e / (HD / 4), i = e % (HD / 4) * 4;
+            if (e >= G * HD / 4) continue;
             if (final) {
                 const float L = 1.f / s_ml[1][hh];
-                attn_kv8_put<HD>(p, u.j.row, u.j.h * G + hh, i, y.x * L, y.y * L);
-                attn_kv8_put<HD>(p, u.j.row, u.j.h * G + hh, i + 2, y.z * L, y.w * L);
+                attn_kv8_put<HD>(p, u.j.row, u.j.h * G + hh, i, y[j].x * L, y[j].y * L);
+                attn_kv8_put<HD>(p, u.j.row, u.j.h * G + hh, i + 2, y[j].z * L, y[j].w * L);
             } else {
-                *reinterpret_cast<float4 *>(u.state(0) + 16 + 4 * e) = y;
+                *reinterpret_cast<float4 *>(u.state(0) + 16 + 4 * e) = y[j];
             }
         }
         if (tid < G) {
