@@ -28,7 +28,7 @@ __host__ __device__ constexpr int attn_kv8_step(int hd) { return attn_kv8_positi
 constexpr int kAttnKv8SmCtas = 16 / kAttnKv8Warps;
 constexpr int kAttnKv8MaxCtas = 160 * kAttnKv8SmCtas;
 constexpr int kAttnKv8Group = 16;                               // states joined at a time
-constexpr int kAttnKv8Groups = kAttnKv8MaxCtas / kAttnKv8Group + 1;
+constexpr int kAttnKv8Batch = 8;                                // of them in shared memory
 constexpr float kAttnKv8Shift = 7.f;                            // log2 of the probabilities' scale
 
 // Floats of a state: max and sum of 8 heads, then their outputs
@@ -95,27 +95,6 @@ __device__ __forceinline__ AttnKv8Row attn_kv8_row(const AttnKv8Params &p, int i
     return r;
 }
 
-// Inclusive prefix of v over the CTA's threads, and the total
-__device__ __forceinline__ int attn_kv8_scan(int v, int &total, int *room) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, v, o);
-        if (lane >= o) v += y;
-    }
-    __syncthreads();
-    if (lane == 31) room[warp] = v;
-    __syncthreads();
-    int before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kAttnKv8Warps; ++w) {
-        if (w < warp) before += room[w];
-        total += room[w];
-    }
-    return before + v;
-}
-
 // Two neighbouring outputs, at place i of a state
 template <int HD>
 __device__ __forceinline__ void attn_kv8_put(const AttnKv8Params &p, int row, int head, int i, float y0, float y1) {
@@ -159,95 +138,76 @@ struct AttnKv8Group {
     }
 };
 
-// The last CTA of a group joins its states, and so on up.  Whole CTAs; s_f, s_ml: room for factors and results of 8 heads.
+// The last CTA of a group joins its states, and so on up, 8 states at a time by way of shared memory (whose copies leave the
+// main loop its registers): 16 threads a head.  Whole CTAs; room: of 8 states.
 template <int HD>
-__device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD> u, float (*s_f)[kAttnKv8Groups], float (*s_ml)[8], int *s_last) {
-    constexpr int B = 8;  // states at a time
+__device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD> u, float *room, int *s_last) {
+    constexpr int B = kAttnKv8Batch, STATE = attn_kv8_state(HD), NF = HD / 16, W = NF < 4 ? NF : 4;
     const AttnKv8Params &p = u.p;
-    const int tid = threadIdx.x, G = p.H / p.c.KVH;
+    const int tid = threadIdx.x, G = p.H / p.c.KVH, hh = tid / 16, i0 = tid % 16 * W;
+    const uint32_t to = smem_u32(room);
 #pragma unroll 1
     for (;;) {
-        const bool final = !u.two() || u.pace > 1;
-        // the first states' outputs are on their way while the factors are made, 16 lanes a head
-        constexpr int PER = 8 * HD / 4 / kAttnKv8Threads > 0 ? 8 * HD / 4 / kAttnKv8Threads : 1;  // quads of outputs a thread
-        float4 z[PER][B], y[PER];
-        auto load = [&](int k0) {
+        float M = -3.4028235e38f, L = 0.f, y[NF];
 #pragma unroll
-            for (int k = 0; k < B; ++k)
-                if (k0 + k < u.n) {
-                    const float4 *src = reinterpret_cast<const float4 *>(u.state(k0 + k) + 16) + tid;
-#pragma unroll
-                    for (int j = 0; j < PER; ++j)
-                        if (tid + j * kAttnKv8Threads < G * HD / 4) z[j][k] = __ldcg(src + j * kAttnKv8Threads);
-                }
-        };
-        load(0);
-        {
-            const int hh = tid / 16;
-            float M = -3.4028235e38f, L = 0.f;
-#pragma unroll 1
-            for (int k = tid % 16; k < u.n; k += 16) {
-                const float m = __ldcg(u.state(k) + hh), l = __ldcg(u.state(k) + 8 + hh), N = fmaxf(M, m);
-                L = L * ex2(M - N) + l * ex2(m - N);
-                M = N;
-                s_f[hh][k] = m;
-            }
-            float N = M;
-#pragma unroll
-            for (int d = 8; d > 0; d >>= 1) N = fmaxf(N, __shfl_xor_sync(0xffffffffu, N, d));
-            L *= ex2(M - N);
-#pragma unroll
-            for (int d = 8; d > 0; d >>= 1) L += __shfl_xor_sync(0xffffffffu, L, d);
-            for (int k = tid % 16; k < u.n; k += 16) s_f[hh][k] = ex2(s_f[hh][k] - N);
-            if (tid % 16 == 0) {
-                s_ml[0][hh] = N;
-                s_ml[1][hh] = L;
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < PER; ++j) y[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int i = 0; i < NF; ++i) y[i] = 0.f;
 #pragma unroll 1
         for (int k0 = 0; k0 < u.n; k0 += B) {
-            if (k0 > 0) load(k0);
 #pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                const int hh = min((tid + j * kAttnKv8Threads) / (HD / 4), 7);
+            for (int k = 0; k < B; ++k) {
+                if (k >= u.n - k0) continue;
+                const float *src = u.state(k0 + k);
 #pragma unroll
-                for (int k = 0; k < B; ++k)
-                    if (k0 + k < u.n) {
-                        const float f = s_f[hh][k0 + k];
-                        y[j].x += f * z[j][k].x;
-                        y[j].y += f * z[j][k].y;
-                        y[j].z += f * z[j][k].z;
-                        y[j].w += f * z[j][k].w;
-                    }
+                for (int e = 0; e < STATE / 4; e += kAttnKv8Threads)
+                    if (e + tid < STATE / 4) cp_async16(to + (k * STATE + 4 * (e + tid)) * 4, src + 4 * (e + tid));
+            }
+            cp_async_commit();
+            cp_async_wait<0>();
+            __syncthreads();
+            float N = M, m[B];
+#pragma unroll
+            for (int k = 0; k < B; ++k) {  // (behind the last state: nothing)
+                m[k] = k < u.n - k0 ? room[k * STATE + hh] : -INFINITY;
+                N = fmaxf(N, m[k]);
+            }
+            const float old = ex2(M - N);
+            M = N;
+            L *= old;
+#pragma unroll
+            for (int i = 0; i < NF; ++i) y[i] *= old;
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+                if (k >= u.n - k0) continue;
+                const float *x = room + k * STATE;
+                const float f = ex2(m[k] - N);
+                L += f * x[8 + hh];
+#pragma unroll
+                for (int i = 0; i < NF; ++i) y[i] += f * x[16 + hh * HD + i0 + i / W * 64 + i % W];
+            }
+            __syncthreads();
+        }
+        const bool final = !u.two() || u.pace > 1;
+        if (hh < G) {
+            const float inv = 1.f / L;
+            float *x = u.state(0);
+#pragma unroll
+            for (int i = 0; i < NF; i += 2) {
+                const int at = i0 + i / W * 64 + i % W;
+                if (final) attn_kv8_put<HD>(p, u.j.row, u.j.h * G + hh, at, y[i] * inv, y[i + 1] * inv);
+                else *reinterpret_cast<float2 *>(x + 16 + hh * HD + at) = make_float2(y[i], y[i + 1]);
+            }
+            if (tid % 16 == 0) {
+                if (!final) {
+                    x[hh] = M;
+                    x[8 + hh] = L;
+                } else if (p.lse) {
+                    p.lse[(int64_t)u.j.row * p.H + u.j.h * G + hh] = (M - kAttnKv8Shift + log2f(L)) * 0.69314718f;
+                }
             }
         }
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int e = tid + j * kAttnKv8Threads, hh = e / (HD / 4), i = e % (HD / 4) * 4;
-            if (e >= G * HD / 4) continue;
-            if (final) {
-                const float L = 1.f / s_ml[1][hh];
-                attn_kv8_put<HD>(p, u.j.row, u.j.h * G + hh, i, y[j].x * L, y[j].y * L);
-                attn_kv8_put<HD>(p, u.j.row, u.j.h * G + hh, i + 2, y[j].z * L, y[j].w * L);
-            } else {
-                *reinterpret_cast<float4 *>(u.state(0) + 16 + 4 * e) = y[j];
-            }
-        }
-        if (tid < G) {
-            const float M = s_ml[0][tid], L = s_ml[1][tid];
-            if (!final) {
-                u.state(0)[tid] = M;
-                u.state(0)[8 + tid] = L;
-            } else if (p.lse) {
-                p.lse[(int64_t)u.j.row * p.H + u.j.h * G + tid] = (M - kAttnKv8Shift + log2f(L)) * 0.69314718f;
-            }
-        }
-        __syncthreads();
         if (final) return;
         u.groups();
+        __syncthreads();
         if (tid == 0) *s_last = u.arrive();
         __syncthreads();
         if (!*s_last) return;
@@ -261,47 +221,29 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
     constexpr int POS = attn_kv8_positions(HD), NG = POS / 16, STEP = attn_kv8_step(HD), PS = kKv8Page / STEP;
     constexpr int PITCH = HD + 4;                            // (conflict-free 8-byte stores)
     constexpr int STATE = attn_kv8_state(HD);
-    __shared__ __align__(16) float s_o[kAttnKv8Warps][8][PITCH];
-    __shared__ float s_m[kAttnKv8Warps][8], s_l[kAttnKv8Warps][8], s_ml[2][8], s_f[8][kAttnKv8Groups];
+    __shared__ __align__(16) union {
+        float o[kAttnKv8Warps][8][PITCH];     // the warps' outputs
+        float room[kAttnKv8Batch * STATE];  // states that are joined
+    } sm;
+    auto &s_o = sm.o;
+    __shared__ float s_m[kAttnKv8Warps][8], s_l[kAttnKv8Warps][8];
     __shared__ AttnKv8Join s_join[2];
-    __shared__ int s_room[kAttnKv8Warps], s_row, s_base, s_last[2];
+    __shared__ int s_last[2];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int KVH = p.c.KVH, G = p.H / KVH;
     const float nan = __int_as_float(0x7fc00000);
 
-    // this CTA's share lo .. hi of the list, and the row in which it begins
-    int steps = 0, end = 0, total = 0;
+    // this CTA's share lo .. hi of the list, and the row in which it begins: every warp for itself, 32 rows at a time
+    int steps = 0, total = 0;
     bool idle = false;  // a row without a position (or a wrong one) that is this CTA's to write
-    for (int b = 0; b < p.n; b += kAttnKv8Threads) {
-        int sum;
-        steps = b + tid < p.n ? attn_kv8_row<STEP>(p, b + tid).steps : 0;
-        idle = idle || (b + tid < p.n && steps == 0 && (unsigned)(b + tid) % gridDim.x == blockIdx.x);
-        end = total + attn_kv8_scan(steps, sum, s_room);
-        total += sum;
+#pragma unroll 4
+    for (int i = lane; i - lane < p.n; i += 32) {
+        steps = i < p.n ? attn_kv8_row<STEP>(p, i).steps : 0;
+        if (i < p.n && steps == 0) idle = idle || (unsigned)i % gridDim.x == blockIdx.x;
+        total += __reduce_add_sync(0xffffffffu, steps);
     }
-    total *= KVH;
-    const int ctas = min((int)gridDim.x, total), c = blockIdx.x;
-    const int share = ctas ? total / ctas : 0, more = total - share * ctas;  // the first `more` CTAs have one entry more
-    const int lo = c * share + min(c, more), hi = c < ctas ? lo + share + (c < more) : lo;
-    if (p.n <= kAttnKv8Threads) {
-        if (lo < hi && lo < end * KVH && lo >= (end - steps) * KVH) {
-            s_row = tid;
-            s_base = (end - steps) * KVH;
-        }
-    } else if (lo < hi) {
-        for (int b = 0, before = 0; b < p.n && before * KVH <= lo; b += kAttnKv8Threads) {
-            int sum;
-            steps = b + tid < p.n ? attn_kv8_row<STEP>(p, b + tid).steps : 0;
-            end = before + attn_kv8_scan(steps, sum, s_room);
-            if (lo < end * KVH && lo >= (end - steps) * KVH) {
-                s_row = b + tid;
-                s_base = (end - steps) * KVH;
-            }
-            before += sum;
-        }
-    }
-    if (__syncthreads_or(idle)) {
-        for (int i = c; i < p.n; i += gridDim.x) {
+    if (__any_sync(0xffffffffu, idle)) {
+        for (int i = blockIdx.x; i < p.n; i += gridDim.x) {
             const AttnKv8Row r = attn_kv8_row<STEP>(p, i);
             if (r.steps) continue;
             const float y = r.bad ? nan : 0.f;
@@ -313,95 +255,125 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             if (r.bad && tid == 0) kv8_report(p.status);
         }
     }
-    if (lo >= hi) return;
+    total *= KVH;
+    const int ctas = min((int)gridDim.x, total), c = blockIdx.x;
+    if (c >= ctas) return;
+    const int share = total / ctas, more = total - share * ctas;  // the first `more` CTAs have one entry more
+    const int lo = c * share + min(c, more), hi = lo + share + (c < more);
+    int row = 0, base = 0;  // base: of the row's first entry
+    for (int i = lane, before = 0;; i += 32) {
+        if (p.n > 32) steps = i < p.n ? attn_kv8_row<STEP>(p, i).steps : 0;
+        int end = steps;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, end, d);
+            if (lane >= d) end += y;
+        }
+        const uint32_t behind = __ballot_sync(0xffffffffu, (before + end) * KVH > lo);
+        if (behind) {  // (lo < total: some row holds it)
+            row = i - lane + __ffs(behind) - 1;
+            base = (before + __shfl_sync(0xffffffffu, end - steps, __ffs(behind) - 1)) * KVH;
+            break;
+        }
+        before += __shfl_sync(0xffffffffu, end, 31);
+    }
     if (tid < 2) s_join[tid].row = -1;
     auto cta_of = [&](int x) {  // whose share entry x is
         const int big = more * (share + 1);
         return x < big ? x / (share + 1) : more + (x - big) / share;
     };
-    int row = s_row, base = s_base;
-    AttnKv8Row r = attn_kv8_row<STEP>(p, row);
 
-    for (int at = lo; at < hi;) {
-        const int h = (at - base) / r.steps, a = at - base - h * r.steps, unit = base + h * r.steps;
-        const int b = min(r.steps, hi - unit);  // entries a .. b of the row's, for KV head h
+    AttnKv8Row r = attn_kv8_row<STEP>(p, row);
+    int h = 0, a = 0, b = 0, unit = 0, xa = 0, xb = 0;  // entries unit + a .. unit + b: of the row, for KV head h
+    const int32_t *tab = nullptr;
+    int ids = 0, idbase = 0;  // this lane's entry of the 32 table entries from idbase on
+    bool wrong = false;
+    auto block_of = [&](int x, bool begin) {
+        const int page = x / PS;
+        if (begin || page - idbase >= 32) {
+            idbase = page;
+            ids = (page + lane) * PS < xb ? __ldg(tab + page + lane) : 0;
+            const bool out = ids < 0 || ids >= p.c.n_blocks;
+            wrong = wrong || out;
+            ids = out ? -1 : ids;
+        }
+        return __shfl_sync(0xffffffffu, ids, page - idbase);
+    };
+    const int lane_k = (KW == 8 ? 16 : HD / 4) * t, lane_v = HD / 8 * g;
+    auto edge = [&](int x) {  // whether some of its positions are masked
+        const int p0 = x * STEP + POS * warp;
+        return p0 < r.first || p0 + POS > r.ctx;
+    };
+    auto slot_of = [&](int x, int e) {  // (masked positions stand for the nearest that is not: their probability is 0)
+        return min(max(x * STEP + POS * warp + e, r.first), r.ctx - 1) & (kKv8Page - 1);
+    };
+    auto block_in_page = [&](int x) { return (x % PS * STEP + POS * warp) / kKv8Block; };
+    uint32_t kr[2 * NG][KW], vr[4 * NG][VW];  // positions g + 8 e; 2 t + (e & 1) + 8 (e >> 1)
+    float ks = 0.f, vs = 0.f;
+    int blk = 0;
+    auto load_k = [&](int x) {
+        const int64_t tile = kv8_tile(p.c, max(blk, 0), 0, h);
+        ks = blk < 0 ? nan : __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
+        const uint8_t *k = p.c.codes + tile * (kKv8Page * HD) + lane_k;
+        if (!edge(x)) {
+            k += (x % PS * STEP + POS * warp + g) * HD;
+#pragma unroll
+            for (int e = 0; e < 2 * NG; ++e)
+#pragma unroll
+                for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + 8 * e * HD + 64 * i, &kr[e][4 * i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 2 * NG; ++e)
+#pragma unroll
+                for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + slot_of(x, g + 8 * e) * HD + 64 * i, &kr[e][4 * i]);
+        }
+    };
+    auto load_v = [&](int x) {
+        const int64_t tile = kv8_tile(p.c, max(blk, 0), 1, h);
+        vs = __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
+        const uint8_t *v = p.c.codes + tile * (kKv8Page * HD) + lane_v;
+        if (!edge(x)) {
+            v += (x % PS * STEP + POS * warp + 2 * t) * HD;
+#pragma unroll
+            for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(v + ((e & 1) + 8 * (e >> 1)) * HD, vr[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(v + slot_of(x, 2 * t + (e & 1) + 8 * (e >> 1)) * HD, vr[e]);
+        }
+    };
+    // queries: head g of the group, the dims of this lane's key words
+    uint32_t qb[KW][2];
+    auto begin = [&](int at) {  // the unit of entry `at`; its first keys and its queries are on their way
+        h = (at - base) / r.steps;
+        unit = base + h * r.steps;
+        a = at - unit;
+        b = min(r.steps, hi - unit);
         // this warp's positions of step x: STEP x + POS warp .. + POS - 1; the row's first and last step may have none
-        int xa = r.step0 + a, xb = r.step0 + b;
+        xa = r.step0 + a;
+        xb = r.step0 + b;
         if (xa * STEP + POS * (warp + 1) <= r.first) ++xa;
         if ((xb - 1) * STEP + POS * warp >= r.ctx) --xb;
-        const int32_t *tab = p.c.table + row * p.c.table_stride;
-        int ids = 0, idbase = 0;  // this lane's entry of the 32 table entries from idbase on
-        bool wrong = false;
-        auto block_of = [&](int x, bool begin) {
-            const int page = x / PS;
-            if (begin || page - idbase >= 32) {
-                idbase = page;
-                ids = (page + lane) * PS < xb ? __ldg(tab + page + lane) : 0;
-                const bool out = ids < 0 || ids >= p.c.n_blocks;
-                wrong = wrong || out;
-                ids = out ? -1 : ids;
-            }
-            return __shfl_sync(0xffffffffu, ids, page - idbase);
-        };
-        const int lane_k = (KW == 8 ? 16 : HD / 4) * t, lane_v = HD / 8 * g;
-        auto edge = [&](int x) {  // whether some of its positions are masked
-            const int p0 = x * STEP + POS * warp;
-            return p0 < r.first || p0 + POS > r.ctx;
-        };
-        auto slot_of = [&](int x, int e) {  // (masked positions stand for the nearest that is not: their probability is 0)
-            return min(max(x * STEP + POS * warp + e, r.first), r.ctx - 1) & (kKv8Page - 1);
-        };
-        auto block_in_page = [&](int x) { return (x % PS * STEP + POS * warp) / kKv8Block; };
-        uint32_t kr[2 * NG][KW], vr[4 * NG][VW];  // positions g + 8 e; 2 t + (e & 1) + 8 (e >> 1)
-        float ks = 0.f, vs = 0.f;
-        int blk = 0;
-        auto load_k = [&](int x) {
-            const int64_t tile = kv8_tile(p.c, max(blk, 0), 0, h);
-            ks = blk < 0 ? nan : __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
-            const uint8_t *k = p.c.codes + tile * (kKv8Page * HD) + lane_k;
-            if (!edge(x)) {
-                k += (x % PS * STEP + POS * warp + g) * HD;
-#pragma unroll
-                for (int e = 0; e < 2 * NG; ++e)
-#pragma unroll
-                    for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + 8 * e * HD + 64 * i, &kr[e][4 * i]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 2 * NG; ++e)
-#pragma unroll
-                    for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + slot_of(x, g + 8 * e) * HD + 64 * i, &kr[e][4 * i]);
-            }
-        };
-        auto load_v = [&](int x) {
-            const int64_t tile = kv8_tile(p.c, max(blk, 0), 1, h);
-            vs = __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
-            const uint8_t *v = p.c.codes + tile * (kKv8Page * HD) + lane_v;
-            if (!edge(x)) {
-                v += (x % PS * STEP + POS * warp + 2 * t) * HD;
-#pragma unroll
-                for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(v + ((e & 1) + 8 * (e >> 1)) * HD, vr[e]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(v + slot_of(x, 2 * t + (e & 1) + 8 * (e >> 1)) * HD, vr[e]);
-            }
-        };
+        tab = p.c.table + row * p.c.table_stride;
         if (xa < xb) {
             blk = block_of(xa, true);
             load_k(xa);
         }
+        const uint16_t *qp = p.q + row * p.q_stride + (int64_t)(h * G + min(g, G - 1)) * HD;
+#pragma unroll
+        for (int s = 0; s < KW; ++s) {
+            const int d = KW == 8 ? 64 * (s / 4) + 16 * t + 4 * (s % 4) : HD / 4 * t + 4 * s;
+            const uint2 x = __ldg(reinterpret_cast<const uint2 *>(qp + d));
+            qb[s][0] = x.x;
+            qb[s][1] = x.y;
+        }
+    };
 
-        // queries: head g of the group, the dims of this lane's key words
-        uint32_t qb[KW][2];
+    begin(lo);
+    for (int at = lo;;) {
         float mul0, mul1;  // from MMA sums to base-2 exponents, heads 2 t and 2 t + 1
         {
-            const uint16_t *qp = p.q + row * p.q_stride + (int64_t)(h * G + min(g, G - 1)) * HD;
 #pragma unroll
-            for (int s = 0; s < KW; ++s) {
-                const int d = KW == 8 ? 64 * (s / 4) + 16 * t + 4 * (s % 4) : HD / 4 * t + 4 * s;
-                const uint2 x = __ldg(reinterpret_cast<const uint2 *>(qp + d));
-                qb[s][0] = g < G ? x.x : 0;
-                qb[s][1] = g < G ? x.y : 0;
-            }
+            for (int s = 0; s < KW; ++s) qb[s][0] = g < G ? qb[s][0] : 0, qb[s][1] = g < G ? qb[s][1] : 0;
             float mul = p.scale_log2;
             if (p.type == SARA_BF16) {
                 uint32_t top = 0;
@@ -434,7 +406,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
 #pragma unroll 1
         for (int x = xa; x < xb; ++x) {
-            // the next step's keys load over this one's as soon as the scores are taken, its values once they are used
+            // this step's values come while its scores are taken, the next one's keys after that
             load_v(x);
             float s[NG][4];
             const float f0 = ks * mul0, f1 = ks * mul1;
@@ -532,7 +504,6 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                 }
             }
         }
-        if (wrong) kv8_report(p.status);
 
         // the warps' states: o[j][e], o[j][2 + e]: head 2 t + e, dims hd / 8 g + 2 j and + 1, at place 16 j + 2 g
 #pragma unroll
@@ -551,9 +522,19 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             *reinterpret_cast<float2 *>(&s_o[warp][2 * t][16 * j + 2 * g]) = make_float2(o[j][0] * vref, o[j][2] * vref);
             *reinterpret_cast<float2 *>(&s_o[warp][2 * t + 1][16 * j + 2 * g]) = make_float2(o[j][1] * vref, o[j][3] * vref);
         }
+        const AttnKv8Join me = {row, h, unit, unit + r.steps - 1};
+        const bool begins = a == 0, whole = begins && b == r.steps;
+        at = unit + b;
+        if (at < hi) {  // the next unit's loads, while this one is put together
+            if (h == KVH - 1) {
+                base += KVH * r.steps;
+                do r = attn_kv8_row<STEP>(p, ++row);
+                while (r.steps == 0);
+            }
+            begin(at);
+        }
         __syncthreads();
-        const bool whole = a == 0 && b == r.steps;
-        float *mine = p.part + (c * 2 + (a == 0)) * STATE;  // (a share begins in at most one unit that it does not begin)
+        float *mine = p.part + (c * 2 + begins) * STATE;  // (a share begins in at most one unit that it does not begin)
         for (int e = tid; e < G * HD / 2; e += kAttnKv8Threads) {
             const int hh = e / (HD / 2), i = e % (HD / 2) * 2;
             float M = s_m[0][hh], L = 0.f, y0 = 0.f, y1 = 0.f;
@@ -569,8 +550,8 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             }
             if (whole) {
                 const float inv = 1.f / L;
-                attn_kv8_put<HD>(p, row, h * G + hh, i, y0 * inv, y1 * inv);
-                if (p.lse && i == 0) p.lse[(int64_t)row * p.H + h * G + hh] = (M - kAttnKv8Shift + log2f(L)) * 0.69314718f;
+                attn_kv8_put<HD>(p, me.row, me.h * G + hh, i, y0 * inv, y1 * inv);
+                if (p.lse && i == 0) p.lse[(int64_t)me.row * p.H + me.h * G + hh] = (M - kAttnKv8Shift + log2f(L)) * 0.69314718f;
             } else {
                 *reinterpret_cast<float2 *>(mine + 16 + hh * HD + i) = make_float2(y0, y1);
                 if (i == 0) {
@@ -579,22 +560,18 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                 }
             }
         }
-        if (!whole && tid == 0) s_join[a == 0] = {row, h, cta_of(unit), cta_of(unit + r.steps - 1)};
+        if (!whole && tid == 0) s_join[begins] = {me.row, me.h, cta_of(me.c0), cta_of(me.c1)};
         __syncthreads();  // (shared memory is the next unit's)
-        at = unit + b;
-        if (at < hi && h == KVH - 1) {
-            base += KVH * r.steps;
-            do r = attn_kv8_row<STEP>(p, ++row);
-            while (r.steps == 0);
-        }
+        if (at >= hi) break;
     }
+    if (wrong) kv8_report(p.status);
 
     // the units that other CTAs share: at most the one in which the share begins and the one in which it ends
     if ((tid == 0 || tid == 32) && s_join[tid / 32].row >= 0) s_last[tid / 32] = AttnKv8Group<HD>(p, s_join[tid / 32], c).arrive();
     __syncthreads();
 #pragma unroll 1
     for (int i = 0; i < 2; ++i)
-        if (s_join[i].row >= 0 && s_last[i]) attn_kv8_join<HD>({p, s_join[i], c}, s_f, s_ml, &s_last[i]);
+        if (s_join[i].row >= 0 && s_last[i]) attn_kv8_join<HD>({p, s_join[i], c}, sm.room, &s_last[i]);
 }
 
 inline size_t attn_kv8_count_bytes() { return kAttnKv8MaxCtas * 4 * sizeof(int); }
