@@ -2,8 +2,11 @@
 //   m = max z, S = sum e^(z - m), T = sum e^(z - m) (z - m)
 //   logprob = z[token] - m - log S,   entropy = log S - T / S
 //   dz_v = g (1[v = token] - p_v) - g' p_v (log p_v + entropy)
-// Both are bound by reading (and for the gradient writing) the logits once: 16 bytes a lane, a step's loads in flight during the
-// one before, sums in fp32 against the thread's own running maximum.
+// The gradient is bound by reading and writing the logits once (2,048 x 151,936 in fp32: 334 us, 7.1 TB/s).  The scores read
+// them once, 16 bytes a lane, a step's loads in flight during the one before; 16-bit logits come so fast that the
+// instructions per logit count, so they are taken two at a time and in base 2:
+//   e^(z - m) = 2^(z log2(e) - r) 2^-c,  r = m log2(e) as rounded, c what the rounding took: one fused operation a logit,
+// and c, the same for all, is put right once, in log S.  Sums in fp32 against the thread's own running maximum.
 #pragma once
 #include "device_common.cuh"
 #include "host_util.h"
@@ -11,16 +14,14 @@
 namespace sara {
 
 constexpr int kScoreMaxTop = 32;
-constexpr float kLog2e = 1.44269504f;
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 
-// exp of a difference d <= 0 (or NaN): 2^-22 relative, 0 below 2^-126
-__device__ __forceinline__ float exp_neg(float d) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(d * kLog2e));
-    return y;
+__device__ __forceinline__ float exp2_approx(float y) {  // 2^-22 relative, 0 below 2^-126
+    float e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(y));
+    return e;
 }
-
-// The same down to the subnormal range, where a gradient's factors may still bring it back into the normal one
+// e^d down to the subnormal range, where a gradient's factors may still bring it back into the normal one
 __device__ __forceinline__ float exp_neg_full(float d) {
     float y;
     asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(d * kLog2e));
@@ -79,6 +80,33 @@ __device__ __forceinline__ void unpack_vector(const uint4 &x, float (&z)[16 / (T
         }
     }
 }
+// The larger of two words' logits (of 16-bit types: pairs); a NaN gives way
+template <int TYPE>
+__device__ __forceinline__ uint32_t max_word(uint32_t a, uint32_t b) {
+    if constexpr (TYPE == SARA_FP32) {
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    } else {
+        uint32_t r;
+        if constexpr (TYPE == SARA_BF16) asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+}
+__device__ __forceinline__ uint64_t pack_f32x2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 unpack_f32x2(uint64_t x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
 template <int TYPE>
 __device__ __forceinline__ float load_logit(const void *z, int64_t i) {
     if constexpr (TYPE == SARA_FP32) return static_cast<const float *>(z)[i];
@@ -110,26 +138,36 @@ __device__ __forceinline__ float score_key_value(uint64_t k) {
 }
 __device__ __forceinline__ int score_key_token(uint64_t k) { return k == 0 ? -1 : 0x7fffffff - (int)(uint32_t)k; }
 
-// A warp's 32 best keys so far, lane i the i-th
+__device__ __forceinline__ uint64_t exchange_key(uint64_t key, int d, bool larger) {
+    const uint64_t o = __shfl_xor_sync(0xffffffffu, key, d);
+    return larger == (key > o) ? key : o;
+}
+// A warp's 32 best keys so far, lane i the i-th.  Candidates are collected in shared memory and joined 32 at a
+// time: sorted the other way round, the element-wise larger keys are the best 32 of both and a bitonic sequence, which five
+// exchanges sort.
 struct ScoreList {
     uint64_t key = 0;
-    __device__ __forceinline__ void insert(uint64_t k) {  // (the same k in every lane)
+    __device__ __forceinline__ void join(uint64_t other) {
         const int lane = threadIdx.x & 31;
-        const int rank = __popc(__ballot_sync(0xffffffffu, key > k));
-        const uint64_t up = __shfl_up_sync(0xffffffffu, key, 1);
-        key = lane < rank ? key : lane == rank ? k : up;
-    }
-    // another list, given in reverse order: the element-wise larger keys are the best 32 of both and a bitonic
-    // sequence, which five exchanges sort
-    __device__ __forceinline__ void merge_reversed(uint64_t other) {
+#pragma unroll
+        for (int size = 2; size <= 32; size <<= 1)
+#pragma unroll
+            for (int d = size / 2; d > 0; d >>= 1) other = exchange_key(other, d, ((lane & d) == 0) == ((lane & size) != 0 && size < 32));
         key = key > other ? key : other;
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) {
-            const uint64_t o = __shfl_xor_sync(0xffffffffu, key, d);
-            key = ((threadIdx.x & d) == 0) == (key > o) ? key : o;
-        }
+        for (int d = 16; d > 0; d >>= 1) key = exchange_key(key, d, (lane & d) == 0);
     }
 };
+// The `top` best of n <= 256 keys, thread i's place being the number of larger ones.  out: zeroed before.
+__device__ __forceinline__ void rank_keys(const uint64_t *keys, int n, int top, uint64_t *out) {
+    const int i = threadIdx.x;
+    if (i >= n) return;
+    const uint64_t k = keys[i];
+    int rank = 0;
+#pragma unroll 4
+    for (int j = 0; j < n; ++j) rank += keys[j] > k;
+    if (rank < top && k) out[rank] = k;
+}
 // The `top`-th largest of the lanes' values
 __device__ __forceinline__ float warp_nth_largest(float v, int top) {
     const int lane = threadIdx.x & 31;
@@ -145,38 +183,95 @@ __device__ __forceinline__ float warp_nth_largest(float v, int top) {
 }
 
 // ------------------------------------------------------------------------------- sums
+// Maximum m, s = sum 2^(z log2(e) - r), t = sum 2^y y with y that exponent.  Where m log2(e) has no room in fp32, r is exact.
 struct ScoreSums {
-    float m = -3.4028235e38f, s = 0.f, t = 0.f;  // maximum, sum e^(z - m), sum e^(z - m) (z - m)
+    float m = -3.4028235e38f, s = 0.f, t = 0.f;
+    static __device__ __forceinline__ bool plain(float m) { return fabsf(m) < 1e37f; }
+    static __device__ __forceinline__ float carry(float m) { return plain(m) ? fmaf(m, kLog2e, -(m * kLog2e)) : 0.f; }  // c
     // to a maximum n >= m.  (The bound keeps 0 times infinity out where the maxima are that far apart.)
     __device__ __forceinline__ void rebase(float n) {
-        const float d = fmaxf(m - n, -1e4f), f = exp_neg(d);
+        const float d = fmaxf(fmaf(m - n, kLog2e, carry(n) - carry(m)), -1e4f), f = exp2_approx(d);
         t = (t + s * d) * f;
         s *= f;
         m = n;
     }
-    __device__ __forceinline__ void join(float om, float os, float ot) {
-        ScoreSums o;
-        o.m = om;
-        o.s = os;
-        o.t = ot;
-        const float n = fmaxf(m, om);
+    // of LANES neighbouring lanes, the first lane's among them
+    template <int LANES>
+    __device__ __forceinline__ void join_lanes() {
+        float n = m;
+#pragma unroll
+        for (int d = LANES / 2; d > 0; d >>= 1) n = fmaxf(n, __shfl_xor_sync(0xffffffffu, n, d));
         rebase(n);
-        o.rebase(n);
-        s += o.s;
-        t += o.t;
+#pragma unroll
+        for (int d = LANES / 2; d > 0; d >>= 1) {
+            s += __shfl_xor_sync(0xffffffffu, s, d);
+            t += __shfl_xor_sync(0xffffffffu, t, d);
+        }
+    }
+    // of the first n <= 8 columns of a table, in every lane of a warp
+    __device__ __forceinline__ void join_table(const float (*x)[8], int n) {
+        const int lane = threadIdx.x & 7;
+        m = lane < n ? x[0][lane] : -3.4028235e38f;
+        s = lane < n ? x[1][lane] : 0.f;
+        t = lane < n ? x[2][lane] : 0.f;
+        join_lanes<8>();
+    }
+    // a vector's logits, none above m (a logit of -inf adds nothing, a NaN stays)
+    template <int E>
+    __device__ __forceinline__ void add(const float (&z)[E], uint64_t &s2, uint64_t &t2) {
+        const float r = -(m * kLog2e);
+        const uint64_t r2 = pack_f32x2(r, r), l2 = pack_f32x2(kLog2e, kLog2e);
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+            const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(z[e], z[e + 1]), l2, r2));
+            const uint64_t w = pack_f32x2(exp2_approx(y.x), exp2_approx(y.y));
+            s2 = add_f32x2(s2, w);
+            t2 = fma_f32x2(w, pack_f32x2(fmaxf(y.x, -1000.f), fmaxf(y.y, -1000.f)), t2);
+        }
+    }
+    template <int E>
+    __device__ __forceinline__ void add_far(const float (&z)[E]) {  // where !plain(m)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float y = (z[e] - m) * kLog2e, w = exp2_approx(y);
+            s += w;
+            t = fmaf(w, fmaxf(y, -1000.f), t);
+        }
     }
 };
+
+// The `top`-th largest (top <= 32) of 64 values, by every lane of a warp: the one that has fewer than `top` above and, with its
+// equals, at least `top`
+__device__ __forceinline__ float nth_of_64(const float *x, int top) {
+    const int lane = threadIdx.x & 31;
+    const float a = x[lane], b = x[32 + lane];
+    int above_a = 0, above_b = 0, least_a = 0, least_b = 0;
+#pragma unroll 4
+    for (int j = 0; j < 64; j += 4) {
+        const float4 y = *reinterpret_cast<const float4 *>(x + j);
+        above_a += (y.x > a) + (y.y > a) + (y.z > a) + (y.w > a);
+        above_b += (y.x > b) + (y.y > b) + (y.z > b) + (y.w > b);
+        least_a += (y.x >= a) + (y.y >= a) + (y.z >= a) + (y.w >= a);
+        least_b += (y.x >= b) + (y.y >= b) + (y.z >= b) + (y.w >= b);
+    }
+    const bool is_a = above_a < top && least_a >= top, is_b = above_b < top && least_b >= top;
+    const uint32_t who = __ballot_sync(0xffffffffu, is_a || is_b);
+    return __shfl_sync(0xffffffffu, is_a ? a : b, __ffs(who) - 1);
+}
 
 // One row per group of WARPS warps (8: a CTA; 1: eight rows to a CTA), or, where p.ctas > 1, per cluster of that many
 // CTAs, each a contiguous share of its vectors.
 template <int TYPE, bool TOP, int WARPS>
 __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
     using Row = RowVectors<TYPE>;
-    constexpr int E = Row::E, U = TYPE == SARA_FP32 ? 4 : 2, STEP = 32 * WARPS;
+    constexpr int E = Row::E, U = WARPS > 1 ? 4 : 2, STEP = 32 * WARPS;
     __shared__ float s_sums[3][8];
-    __shared__ uint64_t s_key[TOP ? 8 : 1][32];
+    __shared__ uint64_t s_cand[TOP ? 8 : 1][64];              // candidates that a warp has not joined yet
+    __shared__ uint64_t s_key[TOP ? 8 * 32 : 1], s_best[32];  // the warps' candidates; the CTA's alternatives
+    __shared__ __align__(16) float s_group[64];
     __shared__ volatile float s_floor[8];
-    __shared__ uint32_t c_sums[3][8], c_key[TOP ? 8 : 1][32][2];  // (rank 0) the cluster's
+    __shared__ int s_held[8];
+    __shared__ __align__(8) uint32_t c_sums[3][8], c_key[TOP ? 8 * 32 : 1][2];  // (rank 0) the cluster's
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = threadIdx.x % STEP;
     const bool cluster = WARPS > 1 && p.ctas > 1;
     if (cluster) cluster_arrive();  // (waited for before the stores into rank 0's shared memory)
@@ -191,6 +286,7 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
 
     ScoreSums a;
     ScoreList list;
+    int held = 0;                               // candidates in s_cand
     uint64_t kth = 0;                           // the list's entry `top`
     float kth_v = -INFINITY, floor = -INFINITY;  // its value; no alternative is below this
     const int nv = pad ? 0 : row.vectors(), per = (nv + p.ctas - 1) / p.ctas, v1 = min(nv, (rank + 1) * per);
@@ -199,114 +295,149 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
 #pragma unroll
         for (int u = 0; u < U; ++u) x[u] = k + u * STEP < v1 ? row.load(k + u * STEP) : make_uint4(Row::kNone, Row::kNone, Row::kNone, Row::kNone);
     };
+    auto join = [&](int least) {  // candidates into the list, 32 at a time
+        while (held >= least) {
+            __syncwarp();
+            const int at = max(held - 32, 0);
+            list.join(at + lane < held ? s_cand[warp][at + lane] : 0);
+            held = at;
+        }
+        kth = __shfl_sync(0xffffffffu, list.key, p.top - 1);
+        kth_v = score_key_value(kth);
+        floor = fmaxf(floor, kth_v);
+        if (WARPS > 1 && lane == 0) s_floor[warp] = floor;
+        __syncwarp();
+    };
     if (TOP) {
         if (lane == 0) s_floor[warp] = -INFINITY;
         if (WARPS > 1) __syncthreads();
     }
     const int v0 = min(rank * per, v1);
     load(v0 + part, next);
-    bool begun = false;
 #pragma unroll 1
     for (int b = v0; b < v1; b += U * STEP) {  // (every lane of a warp the same steps)
         const int k = b + part;
-        float z[U][E];
+        uint4 cur[U];
+        uint32_t most = Row::kNone;
 #pragma unroll
-        for (int u = 0; u < U; ++u) unpack_vector<TYPE>(next[u], z[u]);
+        for (int u = 0; u < U; ++u) {
+            cur[u] = next[u];
+            most = max_word<TYPE>(most, max_word<TYPE>(max_word<TYPE>(cur[u].x, cur[u].y), max_word<TYPE>(cur[u].z, cur[u].w)));
+        }
         if (v1 - b > U * STEP) load(k + U * STEP, next);
-        float best = -INFINITY;  // (a NaN is not the maximum; it reaches the sums)
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < E; ++e) best = fmaxf(best, z[u][e]);
+        const float best = TYPE == SARA_FP32 ? __uint_as_float(most) : TYPE == SARA_BF16 ? fmaxf(__uint_as_float(most << 16), __uint_as_float(most & 0xffff0000u))
+                                                                                          : fmaxf(f16_to_f32((uint16_t)most), f16_to_f32((uint16_t)(most >> 16)));
         if (best > a.m) a.rebase(best);
-        float s2 = 0.f, t2 = 0.f;
+        float z[E];
+        if (ScoreSums::plain(a.m)) {
+            uint64_t s2 = pack_f32x2(a.s, 0.f), t2 = pack_f32x2(a.t, 0.f);
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float d = z[u][e] - a.m, w = exp_neg(d);
-                (e & 1 ? s2 : a.s) += w;
-                float &t = e & 1 ? t2 : a.t;
-                t = fmaf(w, fmaxf(d, -1000.f), t);  // (a logit of -inf has w = 0)
+            for (int u = 0; u < U; ++u) {
+                unpack_vector<TYPE>(cur[u], z);
+                a.add(z, s2, t2);
             }
-        a.s += s2;
-        a.t += t2;
+            a.s = unpack_f32x2(s2).x + unpack_f32x2(s2).y;
+            a.t = unpack_f32x2(t2).x + unpack_f32x2(t2).y;
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                unpack_vector<TYPE>(cur[u], z);
+                a.add_far(z);
+            }
+        }
         if constexpr (TOP) {
-            if (!begun) {  // the list is empty: nothing below the top-th of the lanes' maxima can matter
-                begun = true;
-                floor = warp_nth_largest(best, p.top);
+            if (b == v0) {  // nothing below the top-th of some parts' maxima can matter: the lanes, or all of the CTA by fours
+                if constexpr (WARPS > 1) {
+                    float four = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
+                    four = fmaxf(four, __shfl_xor_sync(0xffffffffu, four, 2));
+                    if (lane % 4 == 0) s_group[threadIdx.x / 4] = four;
+                    __syncthreads();
+                    floor = nth_of_64(s_group, p.top);
+                } else {
+                    floor = warp_nth_largest(best, p.top);
+                }
             }
             if (WARPS > 1) {
 #pragma unroll
-                for (int w = 0; w < 8; ++w) floor = fmaxf(floor, s_floor[w]);  // (another warp's top-th; one that is late reads an older one)
+                for (int w = 0; w < 8; ++w) floor = fmaxf(floor, s_floor[w]);  // (another warp's; one that is late reads an older one)
             }
             // earlier steps had the lower tokens, so equal to the own top-th is too late, equal to another warp's is not
             if (__any_sync(0xffffffffu, best > kth_v && best >= floor)) {
+                uint32_t mask = 0;  // this lane's logits that may count
+                const float least = fmaxf(floor, -3.4028235e38f);
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+                for (int u = 0; u < U; ++u) {
+                    unpack_vector<TYPE>(cur[u], z);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const uint64_t key = z[u][e] >= floor ? score_key(z[u][e], row.first(k + u * STEP) + e) : 0;
-                        uint32_t cand = __ballot_sync(0xffffffffu, key > kth);
-                        while (cand) {
-                            const int src = __ffs(cand) - 1;
-                            cand &= cand - 1;
-                            const uint64_t c = __shfl_sync(0xffffffffu, key, src);
-                            if (c > kth) {
-                                list.insert(c);
-                                kth = __shfl_sync(0xffffffffu, list.key, p.top - 1);
-                            }
-                        }
-                    }
-                kth_v = score_key_value(kth);
-                if (WARPS > 1 && lane == 0) s_floor[warp] = fmaxf(s_floor[warp], kth_v);
-                __syncwarp();
+                    for (int e = 0; e < E; ++e) mask |= (uint32_t)(z[e] >= least) << (u * E + e);
+                }
+#pragma unroll 1
+                while (__any_sync(0xffffffffu, mask != 0)) {  // (few: read again, from the cache)
+                    const int i = mask ? __ffs(mask) - 1 : 0;
+                    const uint32_t v = row.first(k + i / E * STEP) + i % E;
+                    const uint64_t key = mask ? score_key(load_logit<TYPE>(p.z, r * p.stride + v), v) : 0;
+                    mask &= mask - 1;
+                    const uint32_t cand = __ballot_sync(0xffffffffu, key > kth);
+                    if (key > kth) s_cand[warp][held + __popc(cand & ((1u << lane) - 1))] = key;
+                    held += __popc(cand);
+                    if (held >= 32) join(32);
+                }
             }
         }
     }
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1)
-        a.join(__shfl_xor_sync(0xffffffffu, a.m, d), __shfl_xor_sync(0xffffffffu, a.s, d), __shfl_xor_sync(0xffffffffu, a.t, d));
+    const bool sorted = WARPS == 1 || kth != 0;  // (only then the list holds something)
+    if (TOP && sorted && held > 0) join(1);
+    a.template join_lanes<32>();
     if constexpr (WARPS > 1) {
         if (lane == 0) {
             s_sums[0][warp] = a.m;
             s_sums[1][warp] = a.s;
             s_sums[2][warp] = a.t;
+            if (TOP) s_held[warp] = sorted ? p.top : held;
         }
-        if (TOP) s_key[warp][lane] = list.key;
+        if (TOP && warp == 0) s_best[lane] = 0;
         if (cluster) cluster_wait();  // every CTA of the cluster has started
         __syncthreads();
-        if (warp == 0) {
+        if (warp == 0) a.join_table(s_sums, 8);
+        if (TOP) {
+            int from = 0, n = 0;
 #pragma unroll
-            for (int w = 1; w < 8; ++w) {
-                a.join(s_sums[0][w], s_sums[1][w], s_sums[2][w]);
-                if (TOP) list.merge_reversed(s_key[w][31 - lane]);
+            for (int w = 0; w < 8; ++w) {
+                if (w < warp) from += s_held[w];
+                n += s_held[w];
             }
+            if (lane < s_held[warp]) s_key[from + lane] = sorted ? list.key : s_cand[warp][lane];
+            __syncthreads();
+            rank_keys(s_key, n, p.top, s_best);
+            __syncthreads();
+            list.key = s_best[lane];
         }
         if (cluster) {
             if (warp == 0) {
                 if (lane < 3) st_cluster_u32(cluster_addr(&c_sums[lane][rank], 0), __float_as_uint(lane == 0 ? a.m : lane == 1 ? a.s : a.t));
-                if (TOP) {
-                    st_cluster_u32(cluster_addr(&c_key[rank][lane][0], 0), (uint32_t)list.key);
-                    st_cluster_u32(cluster_addr(&c_key[rank][lane][1], 0), (uint32_t)(list.key >> 32));
+                if (TOP && lane < p.top) {
+                    st_cluster_u32(cluster_addr(&c_key[rank * p.top + lane][0], 0), (uint32_t)list.key);
+                    st_cluster_u32(cluster_addr(&c_key[rank * p.top + lane][1], 0), (uint32_t)(list.key >> 32));
                 }
             }
             cluster_sync();
             if (rank != 0) return;
-            if (warp == 0) {
-                for (int c = 1; c < p.ctas; ++c) {
-                    a.join(__uint_as_float(c_sums[0][c]), __uint_as_float(c_sums[1][c]), __uint_as_float(c_sums[2][c]));
-                    if (TOP) list.merge_reversed((uint64_t)c_key[c][31 - lane][1] << 32 | c_key[c][31 - lane][0]);
-                }
+            if (warp == 0) a.join_table(reinterpret_cast<const float (*)[8]>(c_sums), p.ctas);
+            if (TOP) {
+                if (warp == 0) s_best[lane] = 0;
+                __syncthreads();
+                rank_keys(reinterpret_cast<const uint64_t *>(c_key), p.ctas * p.top, p.top, s_best);
+                __syncthreads();
+                list.key = s_best[lane];
             }
         }
         if (warp != 0) return;
     }
     const bool none = a.s == 0.f;  // every logit is -inf
-    const float m = pad ? 0.f : none ? -INFINITY : a.m, ls = none ? 0.f : logf(a.s);
+    const float m = pad ? 0.f : none ? -INFINITY : a.m, ls = none ? 0.f : fmaf(-kLn2, ScoreSums::carry(a.m), logf(a.s));
     if (lane == 0) {
         if (p.logprob) p.logprob[r] = pad ? 0.f : none && tok < p.V ? -INFINITY : ztok - m - ls;
-        if (p.entropy) p.entropy[r] = none ? 0.f : ls - a.t / a.s;
+        if (p.entropy) p.entropy[r] = none ? 0.f : fmaf(-kLn2, a.t / a.s, logf(a.s));  // (c cancels)
         if (p.stats) {
             p.stats[2 * (int64_t)r] = m;
             p.stats[2 * (int64_t)r + 1] = ls;
