@@ -13,7 +13,7 @@
 
 namespace sara {
 
-constexpr int kScoreMaxTop = 32;
+constexpr int kScoreMaxTop = 32, kScoreMaxCtas = 8;
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 
 __device__ __forceinline__ float exp2_approx(float y) {  // 2^-22 relative, 0 below 2^-126
@@ -158,15 +158,20 @@ struct ScoreList {
         for (int d = 16; d > 0; d >>= 1) key = exchange_key(key, d, (lane & d) == 0);
     }
 };
-// The `top` best of n <= 256 keys, thread i's place being the number of larger ones.  out: zeroed before.
+// The `top` best of n keys to their places in `out` (zeroed before), a key's place being the number of larger ones: four threads a
+// key.  Whole CTAs.
 __device__ __forceinline__ void rank_keys(const uint64_t *keys, int n, int top, uint64_t *out) {
-    const int i = threadIdx.x;
-    if (i >= n) return;
-    const uint64_t k = keys[i];
-    int rank = 0;
+    const int part = threadIdx.x & 3;
+    for (int i0 = 0; i0 < n; i0 += blockDim.x / 4) {
+        const int i = i0 + (int)threadIdx.x / 4;
+        const uint64_t k = i < n ? keys[i] : 0;
+        int rank = 0;
 #pragma unroll 4
-    for (int j = 0; j < n; ++j) rank += keys[j] > k;
-    if (rank < top && k) out[rank] = k;
+        for (int j = part; j < n; j += 4) rank += keys[j] > k;
+        rank += __shfl_xor_sync(0xffffffffu, rank, 1);
+        rank += __shfl_xor_sync(0xffffffffu, rank, 2);
+        if (part == 0 && rank < top && k) out[rank] = k;
+    }
 }
 // The `top`-th largest of the lanes' values
 __device__ __forceinline__ float warp_nth_largest(float v, int top) {
@@ -208,13 +213,14 @@ struct ScoreSums {
             t += __shfl_xor_sync(0xffffffffu, t, d);
         }
     }
-    // of the first n <= 8 columns of a table, in every lane of a warp
-    __device__ __forceinline__ void join_table(const float (*x)[8], int n) {
-        const int lane = threadIdx.x & 7;
+    // of the first n <= COLUMNS columns of a table, in every lane of a warp
+    template <int COLUMNS>
+    __device__ __forceinline__ void join_table(const float (*x)[COLUMNS], int n) {
+        const int lane = threadIdx.x & (COLUMNS - 1);
         m = lane < n ? x[0][lane] : -3.4028235e38f;
         s = lane < n ? x[1][lane] : 0.f;
         t = lane < n ? x[2][lane] : 0.f;
-        join_lanes<8>();
+        join_lanes<COLUMNS>();
     }
     // a vector's logits, none above m (a logit of -inf adds nothing, a NaN stays)
     template <int E>
@@ -240,38 +246,44 @@ struct ScoreSums {
     }
 };
 
-// The `top`-th largest (top <= 32) of 64 values, by every lane of a warp: the one that has fewer than `top` above and, with its
-// equals, at least `top`
-__device__ __forceinline__ float nth_of_64(const float *x, int top) {
-    const int lane = threadIdx.x & 31;
-    const float a = x[lane], b = x[32 + lane];
-    int above_a = 0, above_b = 0, least_a = 0, least_b = 0;
-#pragma unroll 4
-    for (int j = 0; j < 64; j += 4) {
-        const float4 y = *reinterpret_cast<const float4 *>(x + j);
-        above_a += (y.x > a) + (y.y > a) + (y.z > a) + (y.w > a);
-        above_b += (y.x > b) + (y.y > b) + (y.z > b) + (y.w > b);
-        least_a += (y.x >= a) + (y.y >= a) + (y.z >= a) + (y.w >= a);
-        least_b += (y.x >= b) + (y.y >= b) + (y.z >= b) + (y.w >= b);
+// Whether a value, of 64 in x, is the `top`-th largest (top <= 32): fewer than `top` are above it and, with its equals, at least
+// `top` not below.  Four threads a value (256 in all).
+__device__ __forceinline__ bool is_nth_of_64(const float *x, int top, float &v) {
+    const int part = threadIdx.x & 3;
+    v = x[threadIdx.x / 4];
+    int above = 0, least = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const float4 y = *reinterpret_cast<const float4 *>(x + 16 * j + 4 * part);
+        above += (y.x > v) + (y.y > v) + (y.z > v) + (y.w > v);
+        least += (y.x >= v) + (y.y >= v) + (y.z >= v) + (y.w >= v);
     }
-    const bool is_a = above_a < top && least_a >= top, is_b = above_b < top && least_b >= top;
-    const uint32_t who = __ballot_sync(0xffffffffu, is_a || is_b);
-    return __shfl_sync(0xffffffffu, is_a ? a : b, __ffs(who) - 1);
+    int n = above << 16 | least;
+    n += __shfl_xor_sync(0xffffffffu, n, 1);
+    n += __shfl_xor_sync(0xffffffffu, n, 2);
+    return (n >> 16) < top && (n & 0xffff) >= top;
 }
+// Floats as integers of the same order
+__device__ __forceinline__ int ordered(float f) {
+    const int b = __float_as_int(f);
+    return b < 0 ? b ^ 0x7fffffff : b;
+}
+__device__ __forceinline__ float from_ordered(int i) { return __int_as_float(i < 0 ? i ^ 0x7fffffff : i); }
 
-// One row per group of WARPS warps (8: a CTA; 1: eight rows to a CTA), or, where p.ctas > 1, per cluster of that many
+// One row per group of WARPS warps (1: eight rows to a CTA; else a CTA), or, where p.ctas > 1, per cluster of that many
 // CTAs, each a contiguous share of its vectors.
 template <int TYPE, bool TOP, int WARPS>
 __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
+    constexpr int CW = 8;  // the CTA's warps
     using Row = RowVectors<TYPE>;
     constexpr int E = Row::E, U = WARPS > 1 ? 4 : 2, STEP = 32 * WARPS;
-    __shared__ float s_sums[3][8];
-    __shared__ uint64_t s_cand[TOP ? 8 : 1][64];              // candidates that a warp has not joined yet
-    __shared__ uint64_t s_key[TOP ? 8 * 32 : 1], s_best[32];  // the warps' candidates; the CTA's alternatives
+    __shared__ float s_sums[3][CW];
+    __shared__ uint64_t s_cand[TOP ? CW : 1][64];             // candidates that a warp has not joined yet
+    __shared__ uint64_t s_key[TOP ? CW * 32 : 1], s_best[32];  // the warps' candidates; the CTA's alternatives
     __shared__ __align__(16) float s_group[64];
-    __shared__ volatile float s_floor[8];
-    __shared__ int s_held[8];
-    __shared__ __align__(8) uint32_t c_sums[3][8], c_key[TOP ? 8 * 32 : 1][2];  // (rank 0) the cluster's
+    __shared__ int s_floor;  // no alternative is below this (ordered)
+    __shared__ int s_held[CW];
+    __shared__ __align__(8) uint32_t c_sums[3][kScoreMaxCtas], c_key[TOP ? kScoreMaxCtas * 32 : 1][2];  // (rank 0) the cluster's
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = threadIdx.x % STEP;
     const bool cluster = WARPS > 1 && p.ctas > 1;
     if (cluster) cluster_arrive();  // (waited for before the stores into rank 0's shared memory)
@@ -305,13 +317,10 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
         kth = __shfl_sync(0xffffffffu, list.key, p.top - 1);
         kth_v = score_key_value(kth);
         floor = fmaxf(floor, kth_v);
-        if (WARPS > 1 && lane == 0) s_floor[warp] = floor;
+        if (WARPS > 1 && lane == 0) atomicMax(&s_floor, ordered(floor));
         __syncwarp();
     };
-    if (TOP) {
-        if (lane == 0) s_floor[warp] = -INFINITY;
-        if (WARPS > 1) __syncthreads();
-    }
+    if (TOP && WARPS > 1 && threadIdx.x == 0) s_floor = ordered(-INFINITY);
     const int v0 = min(rank * per, v1);
     load(v0 + part, next);
 #pragma unroll 1
@@ -346,21 +355,19 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
             }
         }
         if constexpr (TOP) {
-            if (b == v0) {  // nothing below the top-th of some parts' maxima can matter: the lanes, or all of the CTA by fours
+            if (b == v0) {  // nothing below the top-th of some parts' maxima can matter: of the lanes, or of a 64th of the CTA each
                 if constexpr (WARPS > 1) {
-                    float four = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1));
+                    float four = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1)), v;
                     four = fmaxf(four, __shfl_xor_sync(0xffffffffu, four, 2));
                     if (lane % 4 == 0) s_group[threadIdx.x / 4] = four;
                     __syncthreads();
-                    floor = nth_of_64(s_group, p.top);
+                    if (is_nth_of_64(s_group, p.top, v)) s_floor = ordered(v);  // (all that are have the same value)
+                    __syncthreads();
                 } else {
                     floor = warp_nth_largest(best, p.top);
                 }
             }
-            if (WARPS > 1) {
-#pragma unroll
-                for (int w = 0; w < 8; ++w) floor = fmaxf(floor, s_floor[w]);  // (another warp's; one that is late reads an older one)
-            }
+            if (WARPS > 1) floor = fmaxf(floor, from_ordered(*(volatile int *)&s_floor));  // (a late one is a lower bound all the same)
             // earlier steps had the lower tokens, so equal to the own top-th is too late, equal to another warp's is not
             if (__any_sync(0xffffffffu, best > kth_v && best >= floor)) {
                 uint32_t mask = 0;  // this lane's logits that may count
@@ -398,11 +405,11 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
         if (TOP && warp == 0) s_best[lane] = 0;
         if (cluster) cluster_wait();  // every CTA of the cluster has started
         __syncthreads();
-        if (warp == 0) a.join_table(s_sums, 8);
+        if (warp == 0) a.join_table(s_sums, WARPS);
         if (TOP) {
             int from = 0, n = 0;
 #pragma unroll
-            for (int w = 0; w < 8; ++w) {
+            for (int w = 0; w < WARPS; ++w) {
                 if (w < warp) from += s_held[w];
                 n += s_held[w];
             }
@@ -422,7 +429,7 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
             }
             cluster_sync();
             if (rank != 0) return;
-            if (warp == 0) a.join_table(reinterpret_cast<const float (*)[8]>(c_sums), p.ctas);
+            if (warp == 0) a.join_table(reinterpret_cast<const float (*)[kScoreMaxCtas]>(c_sums), p.ctas);
             if (TOP) {
                 if (warp == 0) s_best[lane] = 0;
                 __syncthreads();
@@ -449,7 +456,6 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
     }
 }
 
-constexpr int kScoreMaxCtas = 8;
 template <int TYPE, bool TOP>
 inline void launch_score(cudaStream_t s, int sms, ScoreParams p) {
     const int vectors = p.V / (TYPE == SARA_FP32 ? 4 : 8);
