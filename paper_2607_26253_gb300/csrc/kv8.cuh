@@ -43,15 +43,20 @@ __device__ __forceinline__ int exponent_for(float amax) {
     return max(e, kKv8LowestExp);
 }
 
-// Two codes of two fp32 values (|x| at most the format's top), to the nearest, ties to even: low byte first.
+// Codes of four fp32 values times f (|x f| at most the format's top; the product is exact), to the nearest, ties to even: first
+// value in the low byte.
 template <int FMT>
-__device__ __forceinline__ uint32_t encode2(float a, float b) {
+__device__ __forceinline__ uint32_t encode4(float2 a, float2 b, float f) {
     if constexpr (FMT == SARA_KV8_E4M3) {
-        uint16_t r;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
-        return r;
+        uint16_t lo, hi;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(a.y * f), "f"(a.x * f));
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(b.y * f), "f"(b.x * f));
+        return (uint32_t)lo | (uint32_t)hi << 16;
     } else {
-        return ((uint32_t)__float2int_rn(a) & 0xff) | (((uint32_t)__float2int_rn(b) & 0xff) << 8);
+        constexpr float kUnits = 12582912.f;  // 1.5 * 2^23: the sum's last bits are the rounded whole number
+        const uint32_t x = __float_as_uint(fmaf(a.x, f, kUnits)), y = __float_as_uint(fmaf(a.y, f, kUnits));
+        const uint32_t z = __float_as_uint(fmaf(b.x, f, kUnits)), w = __float_as_uint(fmaf(b.y, f, kUnits));
+        return __byte_perm(__byte_perm(x, y, 0x0040), __byte_perm(z, w, 0x0040), 0x5410);
     }
 }
 // Two codes (low 16 bits of w) as an fp16 pair: exact in both formats (e4m3 is a subset of fp16).
@@ -84,6 +89,17 @@ template <int TYPE>
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     if constexpr (TYPE == SARA_BF16) return (uint32_t)f32_to_bf16(a) | ((uint32_t)f32_to_bf16(b) << 16);
     else return (uint32_t)__half_as_ushort(__float2half_rn(a)) | ((uint32_t)__half_as_ushort(__float2half_rn(b)) << 16);
+}
+
+// The larger magnitudes of two pairs; a NaN stays
+template <int TYPE>
+__device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    if constexpr (TYPE == SARA_BF16)
+        asm("{\n\t.reg .b32 x, y;\n\tabs.bf16x2 x, %1;\n\tabs.bf16x2 y, %2;\n\tmax.NaN.bf16x2 %0, x, y;\n\t}" : "=r"(r) : "r"(a), "r"(b));
+    else
+        asm("{\n\t.reg .b32 x, y;\n\tabs.f16x2 x, %1;\n\tabs.f16x2 y, %2;\n\tmax.NaN.f16x2 %0, x, y;\n\t}" : "=r"(r) : "r"(a), "r"(b));
+    return r;
 }
 
 // The packed tokens of n sequences in units of one scale block: sequence i's units begin at start[i] / 32 + 2 i, which
@@ -162,14 +178,22 @@ __global__ void __launch_bounds__(128) kv8_write_kernel(Kv8Cache c, Kv8Range r, 
     const uint16_t *src = (kv ? v : k) + h * HD + dim;
     const int64_t stride = kv ? v_stride : k_stride;
     uint4 e[IT];
-    uint32_t top = 0;  // the largest magnitude's bits, which order as the magnitudes do, NaN above infinity
+    uint32_t top = 0;
+    const bool full = x.hi - x.lo == kKv8Block;
+    src += (x.row + (base - x.lo) + lane / LT) * stride;  // (of the block's first position: the loads stay behind x.lo)
+    if (full) {
 #pragma unroll
-    for (int i = 0; i < IT; ++i) {
-        const int p = base + i * TW + lane / LT;
-        e[i] = p >= x.lo && p < x.hi ? __ldg(reinterpret_cast<const uint4 *>(src + (x.row + (p - x.lo)) * stride)) : make_uint4(0, 0, 0, 0);
-        top = __vmaxu2(top, __vmaxu2(__vmaxu2(e[i].x & 0x7fff7fffu, e[i].y & 0x7fff7fffu),
-                                     __vmaxu2(e[i].z & 0x7fff7fffu, e[i].w & 0x7fff7fffu)));
+        for (int i = 0; i < IT; ++i) e[i] = __ldg(reinterpret_cast<const uint4 *>(src + i * (TW * stride)));
+    } else {
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+            const int p = base + i * TW + lane / LT;
+            e[i] = p >= x.lo && p < x.hi ? __ldg(reinterpret_cast<const uint4 *>(src + i * (TW * stride))) : make_uint4(0, 0, 0, 0);
+        }
     }
+#pragma unroll
+    for (int i = 0; i < IT; ++i) top = max_abs2<TYPE>(top, max_abs2<TYPE>(max_abs2<TYPE>(e[i].x, e[i].y), max_abs2<TYPE>(e[i].z, e[i].w)));
+    // magnitudes order as their bits do, NaN above infinity
     top = __reduce_max_sync(0xffffffffu, max(top & 0xffff, top >> 16));
     const float amax = unpack2<TYPE>(top).x;
     const float was = x.held ? *scale : 0.f;
@@ -193,35 +217,45 @@ __global__ void __launch_bounds__(128) kv8_write_kernel(Kv8Cache c, Kv8Range r, 
                     uint2 o = *at;
                     uint32_t n[2] = {o.x, o.y};
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const float2 a = decode2<FMT>(n[j] & 0xffff), b = decode2<FMT>(n[j] >> 16);
-                        n[j] = encode2<FMT>(a.x * f, a.y * f) | encode2<FMT>(b.x * f, b.y * f) << 16;
-                    }
+                    for (int j = 0; j < 2; ++j) n[j] = encode4<FMT>(decode2<FMT>(n[j] & 0xffff), decode2<FMT>(n[j] >> 16), f);
                     *at = make_uint2(n[0], n[1]);
                 }
             }
         }
     }
     const float f = pow2f(-ex);
+    codes += lane / LT * HD;
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
         const int p = base + i * TW + lane / LT;
-        if (p >= x.lo && p < x.hi) {
-            const float2 a = unpack2<TYPE>(e[i].x), b = unpack2<TYPE>(e[i].y), d = unpack2<TYPE>(e[i].z), g = unpack2<TYPE>(e[i].w);
-            *reinterpret_cast<uint2 *>(codes + (p - base) * HD) =
-                make_uint2(encode2<FMT>(a.x * f, a.y * f) | encode2<FMT>(b.x * f, b.y * f) << 16,
-                           encode2<FMT>(d.x * f, d.y * f) | encode2<FMT>(g.x * f, g.y * f) << 16);
-        }
+        if (full || (p >= x.lo && p < x.hi))
+            *reinterpret_cast<uint2 *>(codes + i * TW * HD) =
+                make_uint2(encode4<FMT>(unpack2<TYPE>(e[i].x), unpack2<TYPE>(e[i].y), f),
+                           encode4<FMT>(unpack2<TYPE>(e[i].z), unpack2<TYPE>(e[i].w), f));
     }
     __syncwarp();
     if (lane == 0) *scale = pow2f(ex);
 }
 
-// One warp per scale block, KV head and K or V, 8 dims a lane.
-template <int HD, int FMT>
+// Sixteen values to 16 `type` elements at p (16-byte aligned)
+template <int TYPE>
+__device__ __forceinline__ void store16(uint8_t *p, const float2 (&y)[8]) {
+    if constexpr (TYPE == SARA_FP32) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) reinterpret_cast<float4 *>(p)[j] = make_float4(y[2 * j].x, y[2 * j].y, y[2 * j + 1].x, y[2 * j + 1].y);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            reinterpret_cast<uint4 *>(p)[j] = make_uint4(pack2<TYPE>(y[4 * j].x, y[4 * j].y), pack2<TYPE>(y[4 * j + 1].x, y[4 * j + 1].y),
+                                                        pack2<TYPE>(y[4 * j + 2].x, y[4 * j + 2].y), pack2<TYPE>(y[4 * j + 3].x, y[4 * j + 3].y));
+    }
+}
+
+// One warp per scale block, KV head and K or V, 16 dims a lane, the block's codes in flight together.
+template <int HD, int FMT, int TYPE>
 __global__ void __launch_bounds__(128) kv8_read_kernel(Kv8Cache c, Kv8Range r, uint8_t *k, int64_t k_stride, uint8_t *v,
-                                                       int64_t v_stride, int type, int64_t warps, int32_t *status) {
-    constexpr int LT = HD / 8, TW = 32 / LT, IT = kKv8Block / TW;
+                                                       int64_t v_stride, int64_t warps, int32_t *status) {
+    constexpr int LT = HD / 16, TW = 32 / LT, IT = kKv8Block / TW, SIZE = TYPE == SARA_FP32 ? 4 : 2;
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     if (w >= warps) return;
     const int lane = threadIdx.x & 31, h = (int)(w % c.KVH), kv = (int)(w / c.KVH % 2);
@@ -235,34 +269,36 @@ __global__ void __launch_bounds__(128) kv8_read_kernel(Kv8Cache c, Kv8Range r, u
     }
     if (bad) kv8_report(status);
     const int64_t tile = kv8_tile(c, bad ? 0 : block, kv, h);
-    const int base = x.lo / kKv8Block * kKv8Block, dim = lane % LT * 8;
-    const uint8_t *codes = c.codes + (tile * kKv8Page + base % kKv8Page) * HD + dim;
+    const int base = x.lo / kKv8Block * kKv8Block, dim = lane % LT * 16;
+    const uint8_t *codes = c.codes + (tile * kKv8Page + base % kKv8Page + lane / LT) * HD + dim;
     const float s = bad ? __int_as_float(0x7fc00000) : __ldg(c.scales + tile * kKv8PageBlocks + base % kKv8Page / kKv8Block);
-    const int64_t stride = kv ? v_stride : k_stride;
-    uint8_t *dst = kv ? v : k;
-#pragma unroll 4
+    const int64_t stride = (kv ? v_stride : k_stride) * SIZE;
+    uint8_t *dst = (kv ? v : k) + (x.row + (base - x.lo) + lane / LT) * stride + (h * HD + dim) * SIZE;
+    const bool full = x.hi - x.lo == kKv8Block;
+    uint4 o[IT];
+#pragma unroll
     for (int i = 0; i < IT; ++i) {
         const int p = base + i * TW + lane / LT;
-        if (p < x.lo || p >= x.hi) continue;
-        const uint2 o = bad ? make_uint2(0, 0) : __ldg(reinterpret_cast<const uint2 *>(codes + (p - base) * HD));
-        float2 y[4] = {decode2<FMT>(o.x & 0xffff), decode2<FMT>(o.x >> 16), decode2<FMT>(o.y & 0xffff), decode2<FMT>(o.y >> 16)};
+        o[i] = make_uint4(0, 0, 0, 0);
+        if (!bad && (full || (p >= x.lo && p < x.hi))) o[i] = __ldg(reinterpret_cast<const uint4 *>(codes + i * TW * HD));
+    }
+#pragma unroll
+    for (int i = 0; i < IT; ++i) {
+        const int p = base + i * TW + lane / LT;
+        if (!full && (p < x.lo || p >= x.hi)) continue;
+        const uint32_t n[4] = {o[i].x, o[i].y, o[i].z, o[i].w};
+        float2 y[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
+            y[2 * j] = decode2<FMT>(n[j] & 0xffff);
+            y[2 * j + 1] = decode2<FMT>(n[j] >> 16);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
             y[j].x *= s;
             y[j].y *= s;
         }
-        const int64_t at = (x.row + (p - x.lo)) * stride + h * HD + dim;
-        if (type == SARA_FP32) {
-            float4 *d = reinterpret_cast<float4 *>(dst + at * 4);
-            d[0] = make_float4(y[0].x, y[0].y, y[1].x, y[1].y);
-            d[1] = make_float4(y[2].x, y[2].y, y[3].x, y[3].y);
-        } else {
-            uint32_t o4[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                o4[j] = type == SARA_BF16 ? pack2<SARA_BF16>(y[j].x, y[j].y) : pack2<SARA_FP16>(y[j].x, y[j].y);
-            *reinterpret_cast<uint4 *>(dst + at * 2) = make_uint4(o4[0], o4[1], o4[2], o4[3]);
-        }
+        store16<TYPE>(dst + i * TW * stride, y);
     }
 }
 

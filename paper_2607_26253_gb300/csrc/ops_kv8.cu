@@ -87,8 +87,11 @@ int sara_kv8_read(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *pos
         const Kv8Range r{pos0, seq_start, n_seq, total};
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         by_shape(cache, [&](auto hd, auto fmt) {
-            kv8_read_kernel<hd.value, fmt.value><<<ctas, 128, 0, s>>>(device_cache(cache), r, static_cast<uint8_t *>(k), k_stride,
-                                                                     static_cast<uint8_t *>(v), v_stride, type, warps, status);
+            const auto kern = type == SARA_BF16   ? kv8_read_kernel<hd.value, fmt.value, SARA_BF16>
+                              : type == SARA_FP16 ? kv8_read_kernel<hd.value, fmt.value, SARA_FP16>
+                                                  : kv8_read_kernel<hd.value, fmt.value, SARA_FP32>;
+            kern<<<ctas, 128, 0, s>>>(device_cache(cache), r, static_cast<uint8_t *>(k), k_stride, static_cast<uint8_t *>(v), v_stride,
+                                      warps, status);
         });
         CK(cudaGetLastError());
     });
