@@ -237,21 +237,26 @@ __global__ void __launch_bounds__(128) kv8_write_kernel(Kv8Cache c, Kv8Range r, 
     if (lane == 0) *scale = pow2f(ex);
 }
 
-// Sixteen values to 16 `type` elements at p (16-byte aligned)
-template <int TYPE>
-__device__ __forceinline__ void store16(uint8_t *p, const float2 (&y)[8]) {
+// Eight codes times s to 8 `type` elements at p (16-byte aligned)
+template <int FMT, int TYPE>
+__device__ __forceinline__ void store8(uint8_t *p, uint2 o, float s) {
+    float2 y[4] = {decode2<FMT>(o.x & 0xffff), decode2<FMT>(o.x >> 16), decode2<FMT>(o.y & 0xffff), decode2<FMT>(o.y >> 16)};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        y[j].x *= s;
+        y[j].y *= s;
+    }
     if constexpr (TYPE == SARA_FP32) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) reinterpret_cast<float4 *>(p)[j] = make_float4(y[2 * j].x, y[2 * j].y, y[2 * j + 1].x, y[2 * j + 1].y);
+        for (int j = 0; j < 2; ++j) reinterpret_cast<float4 *>(p)[j] = make_float4(y[2 * j].x, y[2 * j].y, y[2 * j + 1].x, y[2 * j + 1].y);
     } else {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-            reinterpret_cast<uint4 *>(p)[j] = make_uint4(pack2<TYPE>(y[4 * j].x, y[4 * j].y), pack2<TYPE>(y[4 * j + 1].x, y[4 * j + 1].y),
-                                                        pack2<TYPE>(y[4 * j + 2].x, y[4 * j + 2].y), pack2<TYPE>(y[4 * j + 3].x, y[4 * j + 3].y));
+        *reinterpret_cast<uint4 *>(p) = make_uint4(pack2<TYPE>(y[0].x, y[0].y), pack2<TYPE>(y[1].x, y[1].y), pack2<TYPE>(y[2].x, y[2].y),
+                                                   pack2<TYPE>(y[3].x, y[3].y));
     }
 }
 
-// One warp per scale block, KV head and K or V, 16 dims a lane, the block's codes in flight together.
+// One warp per scale block, KV head and K or V, 16 codes a lane, the block's in flight together.  Two neighbouring lanes
+// exchange halves, so that each of their stores fills a 32-byte sector.
 template <int HD, int FMT, int TYPE>
 __global__ void __launch_bounds__(128) kv8_read_kernel(Kv8Cache c, Kv8Range r, uint8_t *k, int64_t k_stride, uint8_t *v,
                                                        int64_t v_stride, int64_t warps, int32_t *status) {
@@ -269,8 +274,8 @@ __global__ void __launch_bounds__(128) kv8_read_kernel(Kv8Cache c, Kv8Range r, u
     }
     if (bad) kv8_report(status);
     const int64_t tile = kv8_tile(c, bad ? 0 : block, kv, h);
-    const int base = x.lo / kKv8Block * kKv8Block, dim = lane % LT * 16;
-    const uint8_t *codes = c.codes + (tile * kKv8Page + base % kKv8Page + lane / LT) * HD + dim;
+    const int base = x.lo / kKv8Block * kKv8Block, dim = lane % LT / 2 * 32 + 8 * (lane & 1);
+    const uint8_t *codes = c.codes + (tile * kKv8Page + base % kKv8Page + lane / LT) * HD + lane % LT * 16;
     const float s = bad ? __int_as_float(0x7fc00000) : __ldg(c.scales + tile * kKv8PageBlocks + base % kKv8Page / kKv8Block);
     const int64_t stride = (kv ? v_stride : k_stride) * SIZE;
     uint8_t *dst = (kv ? v : k) + (x.row + (base - x.lo) + lane / LT) * stride + (h * HD + dim) * SIZE;
@@ -285,20 +290,13 @@ __global__ void __launch_bounds__(128) kv8_read_kernel(Kv8Cache c, Kv8Range r, u
 #pragma unroll
     for (int i = 0; i < IT; ++i) {
         const int p = base + i * TW + lane / LT;
+        const bool odd = lane & 1;
+        const uint2 give = odd ? make_uint2(o[i].x, o[i].y) : make_uint2(o[i].z, o[i].w);
+        const uint2 got = make_uint2(__shfl_xor_sync(0xffffffffu, give.x, 1), __shfl_xor_sync(0xffffffffu, give.y, 1));
         if (!full && (p < x.lo || p >= x.hi)) continue;
-        const uint32_t n[4] = {o[i].x, o[i].y, o[i].z, o[i].w};
-        float2 y[8];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            y[2 * j] = decode2<FMT>(n[j] & 0xffff);
-            y[2 * j + 1] = decode2<FMT>(n[j] >> 16);
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            y[j].x *= s;
-            y[j].y *= s;
-        }
-        store16<TYPE>(dst + i * TW * stride, y);
+        uint8_t *at = dst + i * TW * stride;
+        store8<FMT, TYPE>(at, odd ? got : make_uint2(o[i].x, o[i].y), s);
+        store8<FMT, TYPE>(at + 16 * SIZE, odd ? make_uint2(o[i].z, o[i].w) : got, s);
     }
 }
 
