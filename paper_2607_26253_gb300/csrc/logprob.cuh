@@ -13,7 +13,7 @@
 
 namespace sara {
 
-constexpr int kScoreMaxTop = 32, kScoreMaxCtas = 8;
+constexpr int kScoreMaxTop = 32, kScoreMaxCtas = 8, kScoreWarpVectors = 512, kScoreTopWarpVectors = 1024;
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.69314718f;
 
 __device__ __forceinline__ float exp2_approx(float y) {  // 2^-22 relative, 0 below 2^-126
@@ -272,9 +272,14 @@ __device__ __forceinline__ float from_ordered(int i) { return __int_as_float(i <
 
 // One row per group of WARPS warps (1: eight rows to a CTA; else a CTA), or, where p.ctas > 1, per cluster of that many
 // CTAs, each a contiguous share of its vectors.
+// CTAs an SM that the registers have to leave room for.  (The alternatives of 16-bit logits would spill at four: 2,048 x 151,936, top 8:
+// 132 us, 148 with four.)
+constexpr int score_sm_ctas(int type, bool top, int warps) {
+    return warps == 4 ? 8 : warps == 1 && !top ? 6 : warps == 8 && top && type != SARA_FP32 ? 3 : 4;
+}
 template <int TYPE, bool TOP, int WARPS>
-__global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
-    constexpr int CW = 8;  // the CTA's warps
+__global__ void __launch_bounds__(WARPS > 1 ? 32 * WARPS : 256, score_sm_ctas(TYPE, TOP, WARPS)) score_kernel(ScoreParams p) {
+    constexpr int CW = WARPS > 1 ? WARPS : 8;  // the CTA's warps
     using Row = RowVectors<TYPE>;
     constexpr int E = Row::E, U = WARPS > 1 ? 4 : 2, STEP = 32 * WARPS;
     __shared__ float s_sums[3][CW];
@@ -298,7 +303,7 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
 
     ScoreSums a;
     ScoreList list;
-    int held = 0;                               // candidates in s_cand
+    int nb = 0, held = 0;                       // steps; candidates in s_cand
     uint64_t kth = 0;                           // the list's entry `top`
     float kth_v = -INFINITY, floor = -INFINITY;  // its value; no alternative is below this
     const int nv = pad ? 0 : row.vectors(), per = (nv + p.ctas - 1) / p.ctas, v1 = min(nv, (rank + 1) * per);
@@ -355,16 +360,18 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
             }
         }
         if constexpr (TOP) {
-            if (b == v0) {  // nothing below the top-th of some parts' maxima can matter: of the lanes, or of a 64th of the CTA each
+            // nothing below the top-th of some parts' maxima so far can matter (of the lanes, or of a 64th of the CTA each): taken
+            // again whenever the steps have doubled, so that a long row's later steps hold few candidates
+            if (++nb, (nb & (nb - 1)) == 0) {
                 if constexpr (WARPS > 1) {
-                    float four = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, 1)), v;
+                    float four = fmaxf(a.m, __shfl_xor_sync(0xffffffffu, a.m, 1)), v;
                     four = fmaxf(four, __shfl_xor_sync(0xffffffffu, four, 2));
                     if (lane % 4 == 0) s_group[threadIdx.x / 4] = four;
                     __syncthreads();
-                    if (is_nth_of_64(s_group, p.top, v)) s_floor = ordered(v);  // (all that are have the same value)
+                    if (is_nth_of_64(s_group, p.top, v)) atomicMax(&s_floor, ordered(v));
                     __syncthreads();
                 } else {
-                    floor = warp_nth_largest(best, p.top);
+                    floor = fmaxf(floor, warp_nth_largest(a.m, p.top));
                 }
             }
             if (WARPS > 1) floor = fmaxf(floor, from_ordered(*(volatile int *)&s_floor));  // (a late one is a lower bound all the same)
@@ -456,16 +463,27 @@ __global__ void __launch_bounds__(256) score_kernel(ScoreParams p) {
     }
 }
 
+// Few rows are split over a cluster while a CTA would still hold more than 512 vectors and the CTAs fit the SMs at once (8 an SM; rows
+// that fill the SMs lose by it: 2,048 x 151,936 96 us in one CTA each, 102 in two, 163 in eight).  Many rows take a warp each up to
+// 512 vectors, 4 warps up to 8,192 (8,192 x 8,192: 31 us, 43 with 8 warps; 4,096 x 50,304: 66, 72), 8 warps beyond
+// (3,000 x 151,936: 131 us, 140 with 4).  The alternatives' bound wants the 256 threads.
 template <int TYPE, bool TOP>
 inline void launch_score(cudaStream_t s, int sms, ScoreParams p) {
     const int vectors = p.V / (TYPE == SARA_FP32 ? 4 : 8);
     p.ctas = 1;
-    if (vectors <= 512) {
+    while (p.ctas < kScoreMaxCtas && vectors > 512 * p.ctas && (int64_t)p.R * 2 * p.ctas <= (int64_t)8 * sms) p.ctas *= 2;
+    if (p.ctas == 1 && vectors <= (TOP ? kScoreTopWarpVectors : kScoreWarpVectors)) {
         score_kernel<TYPE, TOP, 1><<<(unsigned)((p.R + 7) / 8), 256, 0, s>>>(p);
         CK(cudaGetLastError());
         return;
     }
-    while (p.ctas < kScoreMaxCtas && vectors > 512 * p.ctas && (int64_t)p.R * 2 * p.ctas <= (int64_t)8 * sms) p.ctas *= 2;
+    if constexpr (!TOP) {
+        if (p.ctas == 1 && vectors <= 8192) {
+            score_kernel<TYPE, false, 4><<<(unsigned)p.R, 128, 0, s>>>(p);
+            CK(cudaGetLastError());
+            return;
+        }
+    }
     launch_cluster(s, false, dim3((unsigned)p.R * p.ctas), dim3(256), 0, (unsigned)p.ctas, score_kernel<TYPE, TOP, 8>, p);
 }
 
