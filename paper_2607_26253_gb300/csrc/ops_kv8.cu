@@ -17,8 +17,9 @@ namespace {
 
 bool misaligned(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
 
-bool cache_ok(const sara_kv8_cache *c) {
-    return c && c->codes && c->scales && c->table && c->n_blocks >= 1 && c->max_blocks >= 1 &&
+// (a batch of no sequences has no table)
+bool cache_ok(const sara_kv8_cache *c, int n_seq) {
+    return c && c->codes && c->scales && (c->table || n_seq == 0) && c->n_blocks >= 1 && c->max_blocks >= 1 &&
            c->max_blocks <= INT32_MAX / SARA_KV8_PAGE && c->table_stride >= c->max_blocks && c->n_kv_heads >= 1 &&
            c->n_kv_heads <= 65536 && (c->head_dim == 32 || c->head_dim == 64 || c->head_dim == 128) &&
            (c->format == SARA_KV8_E4M3 || c->format == SARA_KV8_INT8) && !misaligned(c->codes, 16) && !misaligned(c->scales, 4);
@@ -58,7 +59,7 @@ extern "C" {
 int sara_kv8_write(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *pos0, const int32_t *seq_start, int32_t total,
                    const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t type, int32_t *status,
                    void *stream) {
-    if (!cache_ok(cache) || n_seq < 0 || total < 0 || (type != SARA_BF16 && type != SARA_FP16)) return SARA_EINVAL;
+    if (!cache_ok(cache, n_seq) || n_seq < 0 || total < 0 || (type != SARA_BF16 && type != SARA_FP16)) return SARA_EINVAL;
     if (n_seq == 0 || total == 0) return SARA_OK;
     if (!pos0 || !seq_start || !rows_ok(cache, k, k_stride, total) || !rows_ok(cache, v, v_stride, total)) return SARA_EINVAL;
     return op_guard([&] {
@@ -78,7 +79,7 @@ int sara_kv8_write(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *po
 
 int sara_kv8_read(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *pos0, const int32_t *seq_start, int32_t total,
                   void *k, int64_t k_stride, void *v, int64_t v_stride, int32_t type, int32_t *status, void *stream) {
-    if (!cache_ok(cache) || n_seq < 0 || total < 0 || type < SARA_BF16 || type > SARA_FP32) return SARA_EINVAL;
+    if (!cache_ok(cache, n_seq) || n_seq < 0 || total < 0 || type < SARA_BF16 || type > SARA_FP32) return SARA_EINVAL;
     if (n_seq == 0 || total == 0) return SARA_OK;
     if (!pos0 || !seq_start || !rows_ok(cache, k, k_stride, total) || !rows_ok(cache, v, v_stride, total)) return SARA_EINVAL;
     return op_guard([&] {
@@ -105,7 +106,7 @@ size_t sara_attention_kv8_workspace_bytes(int32_t n_seq, int32_t n_heads, int32_
 int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_t n_heads, const void *q, int64_t q_stride,
                               const int32_t *ctx, const int32_t *first, void *out, float *lse, int32_t type, int32_t *status,
                               void *workspace, size_t workspace_bytes, void *stream) {
-    if (!cache_ok(cache) || n_seq < 0 || n_heads < 1 || (type != SARA_BF16 && type != SARA_FP16)) return SARA_EINVAL;
+    if (!cache_ok(cache, n_seq) || n_seq < 0 || n_heads < 1 || (type != SARA_BF16 && type != SARA_FP16)) return SARA_EINVAL;
     if (n_heads % cache->n_kv_heads || n_heads / cache->n_kv_heads > 8) return SARA_EINVAL;
     if (n_seq == 0) return SARA_OK;
     if (!q || !ctx || !out || !workspace || misaligned(q, 16) || misaligned(out, 16) || misaligned(workspace, 16)) return SARA_EINVAL;

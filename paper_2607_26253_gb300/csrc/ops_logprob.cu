@@ -24,8 +24,8 @@ extern "C" {
 int sara_logprobs(const void *logits, int64_t row_stride, int32_t type, int32_t R, int32_t V, const int32_t *tokens, int32_t top,
                   float *logprob, float *entropy, float *stats, int32_t *top_token, float *top_logprob, void *stream) {
     if (type < SARA_BF16 || type > SARA_FP32 || R < 0 || V < 1 || top < 0 || top > kScoreMaxTop) return SARA_EINVAL;
-    if ((logprob && !tokens) || (top > 0 && (!top_token || !top_logprob))) return SARA_EINVAL;
     if (R == 0) return SARA_OK;
+    if ((logprob && !tokens) || (top > 0 && (!top_token || !top_logprob))) return SARA_EINVAL;
     if (!logits_ok(logits, row_stride, type, R, V)) return SARA_EINVAL;
     return op_guard([&] {
         const ScoreParams p{logits, row_stride, R, V, top, tokens, logprob, entropy, stats, top_token, top_logprob, 1};
@@ -45,8 +45,8 @@ int sara_logprobs_backward(const void *logits, int64_t row_stride, int32_t type,
                            const float *stats, const float *entropy, const float *grad_logprob, const float *grad_entropy,
                            void *grad_logits, int64_t grad_stride, void *stream) {
     if (type < SARA_BF16 || type > SARA_FP32 || R < 0 || V < 1) return SARA_EINVAL;
-    if ((grad_logprob && !tokens) || (grad_entropy && !entropy)) return SARA_EINVAL;
     if (R == 0) return SARA_OK;
+    if ((grad_logprob && !tokens) || (grad_entropy && !entropy)) return SARA_EINVAL;
     if (!logits_ok(logits, row_stride, type, R, V) || !logits_ok(grad_logits, grad_stride, type, R, V) || !stats) return SARA_EINVAL;
     if (logits == grad_logits && R > 1 && row_stride != grad_stride) return SARA_EINVAL;
     return op_guard([&] {

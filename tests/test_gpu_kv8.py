@@ -429,6 +429,98 @@ def test_long_row(pkg):
     _check_attention(c, q, [150000], pkg.attention_decode_kv8(q, c.codes, c.scales, c.tab, _i32([150000])), "fp16")
 
 
+def test_wider_tables_rows_before_the_first_sequence_and_strided_queries(pkg):
+    # the table is a part of a wider one; the first sequence's tokens do not begin at row 0; q is a part of a projection's rows
+    import torch
+    rng = np.random.default_rng(20)
+    n, kvh, hd, H = 3, 2, 64, 8
+    c = Cache(pkg, rng, n, 2, kvh, hd, "e4m3")
+    wide = torch.full((n, 7), -5, dtype=torch.int32, device="cuda")
+    wide[:, 2:4] = c.tab
+    c.tab = wide[:, 2:4]
+    k, v = _tokens(rng, 200, kvh, hd, "bf16")
+    k[:9], v[:9] = float("nan"), float("nan")
+    c.write(k, v, [0, 0, 0], [9, 110, 110, 200])
+    c.check()
+    qkv = _q(rng, n, 2 * H, hd, "bf16")
+    q = qkv[:, H // 2:H // 2 + H]
+    ctx = [101, 0, 90]
+    _check_attention(c, q, ctx, pkg.attention_decode_kv8(q, c.codes, c.scales, c.tab, _i32(ctx)), "bf16")
+    out = tuple(torch.full((200, kvh, hd), 7.0, device="cuda") for _ in range(2))
+    pkg.kv8_read(c.codes, c.scales, c.tab, _i32([0, 0, 0]), _i32([9, 110, 110, 200]), 200, out=out)
+    assert (out[0][:9] == 7).all() and torch.isfinite(out[0]).all()
+    want, _ = oracle.read(c.want_codes, c.want_scales, c.table[2], 0, 90)
+    assert np.array_equal(out[0][110:].double().cpu().numpy(), want)
+
+
+def test_rollouts_share_their_prompts_pages(pkg):
+    # the same full pages at the head of several rows, a page of its own behind them for each
+    rng = np.random.default_rng(21)
+    n, kvh, hd = 6, 2, 128
+    c = Cache(pkg, rng, n, 3, kvh, hd, "int8")
+    c.table[1:, :2] = c.table[0, :2]
+    c.tab = _i32(c.table)
+    k, v = _tokens(rng, 256, kvh, hd, "bf16")
+    one = c.tab
+    c.tab = _i32(c.table[:1])
+    c.write(k, v, [0], [0, 256])
+    c.tab = one
+    for t in range(3):
+        k, v = _tokens(rng, n, kvh, hd, "bf16")
+        c.write(k, v, [256 + t] * n, np.arange(n + 1))
+    c.check()
+    q = _q(rng, n, 12, hd, "bf16")
+    _check_attention(c, q, [259] * n, pkg.attention_decode_kv8(q, c.codes, c.scales, c.tab, _i32([259] * n)), "bf16")
+
+
+@pytest.mark.parametrize("n", [1, 5, 700])
+def test_batches_without_a_position(pkg, n):
+    import torch
+    codes, scales = pkg.kv8_cache(4, 2, 64)
+    table, zero = _i32(np.zeros((n, 2))), _i32(np.zeros(n))
+    q, lse = torch.ones((n, 4, 64), dtype=torch.float16, device="cuda"), torch.zeros((n, 4), device="cuda")
+    out = pkg.attention_decode_kv8(q, codes, scales, table, zero, lse=lse)
+    assert (out == 0).all() and (lse == -np.inf).all()
+    none = torch.empty((0, 2, 64), dtype=torch.float16, device="cuda")
+    pkg.kv8_write(codes, scales, table, none, none, zero, _i32(np.zeros(n + 1)))
+    k, v = pkg.kv8_read(codes, scales, table, zero, _i32(np.zeros(n + 1)), 0)
+    assert k.shape == v.shape == (0, 2, 64)
+
+
+def test_batches_of_no_sequence(pkg):
+    import torch
+    codes, scales = pkg.kv8_cache(4, 2, 64)
+    table, none = torch.empty((0, 2), dtype=torch.int32, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    x = torch.empty((0, 2, 64), dtype=torch.float16, device="cuda")
+    pkg.kv8_write(codes, scales, table, x, x, none, _i32([0]))
+    pkg.kv8_read(codes, scales, table, none, _i32([0]), 0)
+    assert pkg.attention_decode_kv8(torch.empty((0, 4, 64), dtype=torch.float16, device="cuda"), codes, scales, table, none).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("typ", ["bf16", "fp16"])
+def test_queries_of_every_size(pkg, typ):
+    # a NaN or an infinity in one head leaves the others; queries of zero, near the type's ends, far apart within a row
+    import torch
+    rng = np.random.default_rng(22)
+    c = Cache(pkg, rng, 5, 4, 2, 128, "e4m3")
+    q = _q(rng, 5, 8, 128, typ)
+    top = float(torch.finfo(q.dtype).max)
+    ctx = [500] * 5
+    q[0, 1, 3], q[1, 6, 100] = float("nan"), float("inf")
+    q[2] = 0
+    q[3, 0] *= 2.0 ** -20 if typ == "fp16" else 2.0 ** -120
+    q[3, 1, 5] = 0.01 * top if typ == "fp16" else 300.0
+    q[4, :, 1:] *= 2.0 ** -10
+    out = pkg.attention_decode_kv8(q, c.codes, c.scales, c.tab, _i32(ctx))
+    bad = out.isnan().any(-1).cpu().numpy()
+    assert bad[0].tolist() == [i == 1 for i in range(8)] and bad[1].tolist() == [i == 6 for i in range(8)] and not bad[2:].any()
+    q[0, 1, 3], q[1, 6, 100] = 0.5, 0.25
+    good = pkg.attention_decode_kv8(q, c.codes, c.scales, c.tab, _i32(ctx))
+    keep = torch.from_numpy(~bad).cuda()
+    assert torch.equal(out[keep], good[keep])
+    _check_attention(c, q, ctx, good, typ)
+
+
 # ------------------------------------------------------------------------------------------------ together
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 def test_prompts_then_decode_steps(pkg, fmt):

@@ -94,6 +94,29 @@ def test_rows(pkg, R, V):
     _check(pkg.logprobs(z, _i32(tok), top=5), z, tok, 5)
 
 
+# on either side of the lines between a warp, 4 warps, 8 warps and a cluster a row, with and without alternatives
+@pytest.mark.parametrize("R,V,typ,top", [(609, 4099, "bf16", 0), (609, 65600, "bf16", 0), (609, 70001, "bf16", 0), (700, 5003, "fp32", 0),
+                                        (609, 8190, "bf16", 7), (609, 8300, "fp16", 7), (304, 33000, "fp32", 0), (305, 33000, "fp32", 3),
+                                        (1300, 2051, "fp32", 32), (40, 300, "fp32", 1)])
+def test_kernels_by_size(pkg, R, V, typ, top):
+    rng = np.random.default_rng(R + V)
+    z = _logits(rng, R, V, typ, 3.0)
+    tok = rng.integers(0, V, R)
+    tok[::9] = -1
+    keep = rng.permutation(R)[:60]  # (a part of the rows against the oracle)
+    o = pkg.logprobs(z, _i32(tok), top=top)
+    pick = lambda x: x[_i32(keep).long()] if x is not None else None  # noqa: E731
+    _check(pkg.LogProbs(*[pick(x) for x in (o.logprob, o.entropy, o.stats, o.top_token, o.top_logprob)]), pick(z), tok[keep], top)
+
+
+def test_no_rows(pkg):
+    import torch
+    z, none = torch.empty((0, 50), device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
+    o = pkg.logprobs(z, none, top=3)
+    assert o.logprob.shape == (0,) and o.top_token.shape == (0, 3)
+    assert pkg.logprobs_backward(z, none, o.stats, o.entropy, o.logprob).shape == (0, 50)
+
+
 @pytest.mark.parametrize("typ", ["fp32", "bf16", "fp16"])
 @pytest.mark.parametrize("off", [0, 1, 3])
 def test_strided_rows_off_every_alignment(pkg, off, typ):

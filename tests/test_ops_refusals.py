@@ -47,6 +47,7 @@ def test_write_and_read_refusals(lib):
             assert call(fn, **bad) == -1, bad
         for t in types:  # nothing to do: no device is touched
             assert call(fn, n=0, typ=t) == 0 and call(fn, total=0, typ=t) == 0
+            assert call(fn, cache=_cache(table=0), n=0, typ=t, pos0=None, start=None) == 0
 
 
 def test_attention_refusals(lib):
@@ -61,7 +62,7 @@ def test_attention_refusals(lib):
     for bad in (dict(n=-1), dict(H=0), dict(H=7), dict(H=18), dict(q=None), dict(q=A + 8), dict(qs=511), dict(qs=256), dict(ctx=None),
                 dict(out=None), dict(out=A + 8), dict(typ=2), dict(typ=-1), dict(ws=None), dict(ws=A + 8), dict(nbytes=0), dict(n=1 << 28, H=16)):
         assert call(**bad) == -1, bad
-    assert call(n=0) == 0
+    assert call(n=0) == 0 and call(n=0, cache=_cache(table=0)) == 0
 
 
 def test_scoring_refusals(lib):
@@ -150,5 +151,6 @@ def test_binding_refuses_tensors_that_do_not_fit(pkg):
     _refused(pkg, pkg.logprobs_backward, z, i32(4), st[:, :1], h, h, h)
     _refused(pkg, pkg.logprobs_backward, z, i32(4), st, h[:3], h, h)
     _refused(pkg, pkg.logprobs_backward, z, i32(4), st, h, h.double(), h)
+    _refused(pkg, pkg.logprobs_backward, z, i32(4), st, h, h[:1].expand(4), h)  # (not broadcast)
     _refused(pkg, pkg.logprobs_backward, z, i32(4), st, h, h, h, out=z.half())
     _refused(pkg, pkg.logprobs_backward, z, i32(4), st, h, h, h, out=z[:3])
