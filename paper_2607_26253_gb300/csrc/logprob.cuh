@@ -21,11 +21,10 @@ __device__ __forceinline__ float exp2_approx(float y) {  // 2^-22 relative, 0 be
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(y));
     return e;
 }
-// e^d down to the subnormal range, where a gradient's factors may still bring it back into the normal one
-__device__ __forceinline__ float exp_neg_full(float d) {
-    float y;
-    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(d * kLog2e));
-    return y;
+__device__ __forceinline__ float exp2_full(float y) {  // the same down to the subnormal range
+    float e;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(e) : "f"(y));
+    return e;
 }
 
 // A row's elements as the aligned 16-byte vectors that hold them: vector k has elements k E - off .. + E - 1, of
@@ -45,6 +44,9 @@ struct RowVectors {
     __device__ __forceinline__ int vectors() const { return (int)((off + V + (E - 1)) / E); }
     __device__ __forceinline__ uint32_t first(int k) const { return (uint32_t)k * E - off; }  // (wraps below 0 for k = 0)
     __device__ __forceinline__ bool whole(int k) const { return first(k) < V && V - first(k) >= (uint32_t)E; }
+    // The vectors whose elements are all the row's are [whole_from, whole_to).
+    __device__ __forceinline__ int whole_from() const { return off ? 1 : 0; }
+    __device__ __forceinline__ int whole_to() const { return (int)((off + V) / E); }
     // The row's elements of vector k, -inf in the place of others.  (Plain loads: the gradient may take the logits' place.)
     __device__ __forceinline__ uint4 load(int k) const {
         const uint8_t *p = base + (int64_t)k * 16;
@@ -91,6 +93,19 @@ __device__ __forceinline__ uint32_t max_word(uint32_t a, uint32_t b) {
         else asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
         return r;
     }
+}
+// Logits (of 16-bit types: pairs) raised to at least `least` (a word of the same type); a NaN stays
+template <int TYPE>
+__device__ __forceinline__ uint32_t raise_word(uint32_t a, uint32_t least) {
+    uint32_t r;
+    if constexpr (TYPE == SARA_FP32) asm("max.NaN.f32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(least));
+    else if constexpr (TYPE == SARA_BF16) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(least));
+    else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(least));
+    return r;
+}
+template <int TYPE>
+__device__ __forceinline__ uint4 raise_vector(const uint4 &x, uint32_t least) {
+    return make_uint4(raise_word<TYPE>(x.x, least), raise_word<TYPE>(x.y, least), raise_word<TYPE>(x.z, least), raise_word<TYPE>(x.w, least));
 }
 __device__ __forceinline__ uint64_t pack_f32x2(float a, float b) {
     uint64_t r;
@@ -188,10 +203,13 @@ __device__ __forceinline__ float warp_nth_largest(float v, int top) {
 }
 
 // ------------------------------------------------------------------------------- sums
-// Maximum m, s = sum 2^(z log2(e) - r), t = sum 2^y y with y that exponent.  Where m log2(e) has no room in fp32, r is exact.
+// Maximum m, s = sum 2^(z log2(e) - r), t = sum 2^y y with y that exponent.  Where m log2(e) has no room in fp32 (or logits below m
+// none in their type), r is exact and logits are taken one by one.
+template <int TYPE>
 struct ScoreSums {
+    static constexpr uint32_t kLeast = TYPE == SARA_FP32 ? 0xfe967699u : TYPE == SARA_BF16 ? 0xfe96fe96u : 0xfbfffbffu;  // -1e38; fp16: its lowest
     float m = -3.4028235e38f, s = 0.f, t = 0.f;
-    static __device__ __forceinline__ bool plain(float m) { return fabsf(m) < 1e37f; }
+    static __device__ __forceinline__ bool plain(float m) { return fabsf(m) < 1e37f && (TYPE != SARA_FP16 || m > -6e4f); }
     static __device__ __forceinline__ float carry(float m) { return plain(m) ? fmaf(m, kLog2e, -(m * kLog2e)) : 0.f; }  // c
     // to a maximum n >= m.  (The bound keeps 0 times infinity out where the maxima are that far apart.)
     __device__ __forceinline__ void rebase(float n) {
@@ -222,21 +240,26 @@ struct ScoreSums {
         t = lane < n ? x[2][lane] : 0.f;
         join_lanes<COLUMNS>();
     }
-    // a vector's logits, none above m (a logit of -inf adds nothing, a NaN stays)
-    template <int E>
-    __device__ __forceinline__ void add(const float (&z)[E], uint64_t &s2, uint64_t &t2) {
+    // a vector's logits, none above m: one of -inf, raised to a finite one, still adds nothing to either sum; a NaN stays
+    __device__ __forceinline__ void add(const uint4 &x, uint64_t &s2, uint64_t &t2) const {
+        constexpr int E = RowVectors<TYPE>::E;
         const float r = -(m * kLog2e);
         const uint64_t r2 = pack_f32x2(r, r), l2 = pack_f32x2(kLog2e, kLog2e);
+        float z[E];
+        unpack_vector<TYPE>(raise_vector<TYPE>(x, kLeast), z);
 #pragma unroll
         for (int e = 0; e < E; e += 2) {
-            const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(z[e], z[e + 1]), l2, r2));
-            const uint64_t w = pack_f32x2(exp2_approx(y.x), exp2_approx(y.y));
-            s2 = add_f32x2(s2, w);
-            t2 = fma_f32x2(w, pack_f32x2(fmaxf(y.x, -1000.f), fmaxf(y.y, -1000.f)), t2);
+            const uint64_t y2 = fma_f32x2(pack_f32x2(z[e], z[e + 1]), l2, r2);
+            const float2 y = unpack_f32x2(y2);
+            const uint64_t w2 = pack_f32x2(exp2_approx(y.x), exp2_approx(y.y));
+            s2 = add_f32x2(s2, w2);
+            t2 = fma_f32x2(w2, y2, t2);
         }
     }
-    template <int E>
-    __device__ __forceinline__ void add_far(const float (&z)[E]) {  // where !plain(m)
+    __device__ __forceinline__ void add_far(const uint4 &x) {  // where !plain(m)
+        constexpr int E = RowVectors<TYPE>::E;
+        float z[E];
+        unpack_vector<TYPE>(x, z);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float y = (z[e] - m) * kLog2e, w = exp2_approx(y);
@@ -301,16 +324,26 @@ __global__ void __launch_bounds__(WARPS > 1 ? 32 * WARPS : 256, score_sm_ctas(TY
     const float nan = __int_as_float(0x7fc00000);
     const float ztok = part == 0 && rank == 0 && !pad && tok < p.V ? load_logit<TYPE>(p.z, r * p.stride + tok) : nan;
 
-    ScoreSums a;
+    ScoreSums<TYPE> a;
     ScoreList list;
     int nb = 0, held = 0;                       // steps; candidates in s_cand
     uint64_t kth = 0;                           // the list's entry `top`
     float kth_v = -INFINITY, floor = -INFINITY;  // its value; no alternative is below this
     const int nv = pad ? 0 : row.vectors(), per = (nv + p.ctas - 1) / p.ctas, v1 = min(nv, (rank + 1) * per);
     uint4 next[U];
-    auto load = [&](int k, uint4 (&x)[U]) {
+    const int w0 = row.whole_from(), w1 = min(v1, row.whole_to());
+    auto load = [&](int b, uint4 (&x)[U]) {  // the step of vectors from b on
+        if (b >= w0 && b + U * STEP <= w1) {
+            const uint4 *q = reinterpret_cast<const uint4 *>(row.base) + b + part;
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = k + u * STEP < v1 ? row.load(k + u * STEP) : make_uint4(Row::kNone, Row::kNone, Row::kNone, Row::kNone);
+            for (int u = 0; u < U; ++u) x[u] = q[u * STEP];
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int k = b + part + u * STEP;
+                x[u] = k < v1 ? row.load(k) : make_uint4(Row::kNone, Row::kNone, Row::kNone, Row::kNone);
+            }
+        }
     };
     auto join = [&](int least) {  // candidates into the list, 32 at a time
         while (held >= least) {
@@ -327,7 +360,7 @@ __global__ void __launch_bounds__(WARPS > 1 ? 32 * WARPS : 256, score_sm_ctas(TY
     };
     if (TOP && WARPS > 1 && threadIdx.x == 0) s_floor = ordered(-INFINITY);
     const int v0 = min(rank * per, v1);
-    load(v0 + part, next);
+    load(v0, next);
 #pragma unroll 1
     for (int b = v0; b < v1; b += U * STEP) {  // (every lane of a warp the same steps)
         const int k = b + part;
@@ -338,26 +371,19 @@ __global__ void __launch_bounds__(WARPS > 1 ? 32 * WARPS : 256, score_sm_ctas(TY
             cur[u] = next[u];
             most = max_word<TYPE>(most, max_word<TYPE>(max_word<TYPE>(cur[u].x, cur[u].y), max_word<TYPE>(cur[u].z, cur[u].w)));
         }
-        if (v1 - b > U * STEP) load(k + U * STEP, next);
+        if (v1 - b > U * STEP) load(b + U * STEP, next);
         const float best = TYPE == SARA_FP32 ? __uint_as_float(most) : TYPE == SARA_BF16 ? fmaxf(__uint_as_float(most << 16), __uint_as_float(most & 0xffff0000u))
                                                                                           : fmaxf(f16_to_f32((uint16_t)most), f16_to_f32((uint16_t)(most >> 16)));
         if (best > a.m) a.rebase(best);
-        float z[E];
-        if (ScoreSums::plain(a.m)) {
+        if (a.plain(a.m)) {
             uint64_t s2 = pack_f32x2(a.s, 0.f), t2 = pack_f32x2(a.t, 0.f);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                unpack_vector<TYPE>(cur[u], z);
-                a.add(z, s2, t2);
-            }
+            for (int u = 0; u < U; ++u) a.add(cur[u], s2, t2);
             a.s = unpack_f32x2(s2).x + unpack_f32x2(s2).y;
             a.t = unpack_f32x2(t2).x + unpack_f32x2(t2).y;
         } else {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                unpack_vector<TYPE>(cur[u], z);
-                a.add_far(z);
-            }
+            for (int u = 0; u < U; ++u) a.add_far(cur[u]);
         }
         if constexpr (TOP) {
             // nothing below the top-th of some parts' maxima so far can matter (of the lanes, or of a 64th of the CTA each): taken
@@ -381,6 +407,7 @@ __global__ void __launch_bounds__(WARPS > 1 ? 32 * WARPS : 256, score_sm_ctas(TY
                 const float least = fmaxf(floor, -3.4028235e38f);
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
+                    float z[E];
                     unpack_vector<TYPE>(cur[u], z);
 #pragma unroll
                     for (int e = 0; e < E; ++e) mask |= (uint32_t)(z[e] >= least) << (u * E + e);
@@ -448,7 +475,7 @@ __global__ void __launch_bounds__(WARPS > 1 ? 32 * WARPS : 256, score_sm_ctas(TY
         if (warp != 0) return;
     }
     const bool none = a.s == 0.f;  // every logit is -inf
-    const float m = pad ? 0.f : none ? -INFINITY : a.m, ls = none ? 0.f : fmaf(-kLn2, ScoreSums::carry(a.m), logf(a.s));
+    const float m = pad ? 0.f : none ? -INFINITY : a.m, ls = none ? 0.f : fmaf(-kLn2, ScoreSums<TYPE>::carry(a.m), logf(a.s));
     if (lane == 0) {
         if (p.logprob) p.logprob[r] = pad ? 0.f : none && tok < p.V ? -INFINITY : ztok - m - ls;
         if (p.entropy) p.entropy[r] = none ? 0.f : fmaf(-kLn2, a.t / a.s, logf(a.s));  // (c cancels)
@@ -502,10 +529,33 @@ struct ScoreGradParams {
 constexpr int kGradVectors = 4;  // a lane
 
 template <int TYPE>
-__device__ __forceinline__ uint32_t pack_grad(float a, float b) {
-    if constexpr (TYPE == SARA_BF16) return (uint32_t)f32_to_bf16(a) | ((uint32_t)f32_to_bf16(b) << 16);
-    else return (uint32_t)__half_as_ushort(__float2half_rn(a)) | ((uint32_t)__half_as_ushort(__float2half_rn(b)) << 16);
+__device__ __forceinline__ uint32_t pack_grad(float a, float b) {  // both to the nearest, one conversion
+    uint32_t r;
+    if constexpr (TYPE == SARA_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(b), "f"(a));
+    return r;
 }
+
+// What a row's gradients share: with R = (max + log S) log2(e) as rounded and c what the rounding added,
+//   y = z log2(e) - R,  p = 2^y 2^c,  dz = -2^y (a y + b) with a = 2^c g' ln 2 and b = 2^c (g + g' (entropy + c ln 2))
+template <int TYPE>
+struct GradRow {
+    float r, a, b;
+    uint32_t least;  // a logit below every one that counts: those of -inf are raised to it
+    bool plain;      // else the logits are taken one by one
+    __device__ __forceinline__ GradRow(float m, float ls, float g, float gh, float H) {
+        plain = fabsf(m) < 1e6f && (TYPE != SARA_FP16 || m > -6e4f);
+        const float p1 = m * kLog2e, p2 = ls * kLog2e;
+        r = p1 + p2;
+        const float v = r - p1;  // (the sum's own rounding, and the products')
+        const float c = -(((p1 - (r - v)) + (p2 - v)) + (fmaf(m, kLog2e, -p1) + fmaf(ls, kLog2e, -p2)));
+        const float k = exp2_approx(c);
+        a = k * gh * kLn2;
+        b = k * fmaf(gh, fmaf(c, kLn2, H), g);
+        const float low = m - 1000.f - fabsf(m) * 0.015625f;
+        least = TYPE == SARA_FP32 ? __float_as_uint(low) : TYPE == SARA_BF16 ? f32_to_bf16(low) * 0x10001u : f32_to_f16_sat(low) * 0x10001u;
+    }
+};
 
 // One warp per segment of 32 x 4 vectors of a row.  A thread reads what it writes before it writes it, so the gradient
 // may take the logits' place.
@@ -517,33 +567,54 @@ __global__ void __launch_bounds__(256) score_grad_kernel(ScoreGradParams p) {
     if (w >= p.warps) return;
     const int r = (int)(w / p.segs), seg = (int)(w - (int64_t)r * p.segs), lane = threadIdx.x & 31;
     const Row row(p.z, r, p.stride, p.V);
-    const int nv = row.vectors(), k0 = seg * (32 * kGradVectors) + lane;
+    const int nv = row.vectors(), from = seg * (32 * kGradVectors), k0 = from + lane;
     const int tok = p.tokens ? p.tokens[r] : 0;
+    uint8_t *out = static_cast<uint8_t *>(p.out) + ((int64_t)r * p.out_stride - row.off) * Row::kSize;  // of vector 0
+    const bool vec = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
+    const bool inside = from >= row.whole_from() && from + 32 * kGradVectors <= row.whole_to();  // whole vectors alone
     uint4 x[kGradVectors];
     if (tok >= 0) {
+        if (inside) {
+            const uint4 *q = reinterpret_cast<const uint4 *>(row.base) + k0;
 #pragma unroll
-        for (int u = 0; u < kGradVectors; ++u)
-            if (k0 + 32 * u < nv) x[u] = row.load(k0 + 32 * u);
+            for (int u = 0; u < kGradVectors; ++u) x[u] = q[32 * u];
+        } else {
+#pragma unroll
+            for (int u = 0; u < kGradVectors; ++u)
+                if (k0 + 32 * u < nv) x[u] = row.load(k0 + 32 * u);
+        }
     }
     const float m = p.stats[2 * (int64_t)r], ls = p.stats[2 * (int64_t)r + 1];
     const float g = p.glp ? p.glp[r] : 0.f, gh = p.gent ? p.gent[r] : 0.f, H = p.gent ? p.entropy[r] : 0.f;
     const bool zero = tok < 0 || (m == -INFINITY && ls == 0.f && tok < p.V), wrong = tok >= p.V;
-    uint8_t *out = static_cast<uint8_t *>(p.out) + ((int64_t)r * p.out_stride - row.off) * Row::kSize;  // of vector 0
-    const bool vec = (reinterpret_cast<uintptr_t>(out) & 15) == 0;
+    const GradRow<TYPE> c(m, ls, g, gh, H);
+    const uint64_t l2 = pack_f32x2(kLog2e, kLog2e), r2 = pack_f32x2(-c.r, -c.r), a2 = pack_f32x2(-c.a, -c.a), b2 = pack_f32x2(-c.b, -c.b);
 #pragma unroll
     for (int u = 0; u < kGradVectors; ++u) {
         const int k = k0 + 32 * u;
-        if (k >= nv) continue;
+        if (!inside && k >= nv) continue;
         float y[E];
         if (zero || wrong) {
 #pragma unroll
             for (int e = 0; e < E; ++e) y[e] = zero ? 0.f : __int_as_float(0x7fc00000);
         } else {
-            unpack_vector<TYPE>(x[u], y);
+            if (c.plain) {
+                unpack_vector<TYPE>(raise_vector<TYPE>(x[u], c.least), y);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float lp = (y[e] - m) - ls, q = exp_neg_full(lp);
-                y[e] = -q * fmaf(gh, fmaxf(lp, -1000.f) + H, g);  // (a logit of -inf has q = 0)
+                for (int e = 0; e < E; e += 2) {
+                    const uint64_t y2 = fma_f32x2(pack_f32x2(y[e], y[e + 1]), l2, r2);
+                    const float2 t = unpack_f32x2(y2), f = unpack_f32x2(fma_f32x2(y2, a2, b2));
+                    // (a product with a subnormal power may be normal again; fp16 has no room for either)
+                    y[e] = (TYPE == SARA_FP16 ? exp2_approx(t.x) : exp2_full(t.x)) * f.x;
+                    y[e + 1] = (TYPE == SARA_FP16 ? exp2_approx(t.y) : exp2_full(t.y)) * f.y;
+                }
+            } else {
+                unpack_vector<TYPE>(x[u], y);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float lp = (y[e] - m) - ls, q = exp2_full(lp * kLog2e);
+                    y[e] = -q * fmaf(gh, fmaxf(lp, -1000.f) + H, g);  // (a logit of -inf has q = 0)
+                }
             }
             const uint32_t at = (uint32_t)tok - row.first(k);
             if (at < (uint32_t)E) {
@@ -553,7 +624,7 @@ __global__ void __launch_bounds__(256) score_grad_kernel(ScoreGradParams p) {
             }
         }
         uint8_t *o = out + (int64_t)k * 16;
-        if (vec && row.whole(k)) {
+        if (vec && (inside || row.whole(k))) {
             if constexpr (TYPE == SARA_FP32)
                 *reinterpret_cast<float4 *>(o) = make_float4(y[0], y[1], y[2], y[3]);
             else
