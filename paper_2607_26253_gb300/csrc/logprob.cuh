@@ -538,8 +538,11 @@ __device__ __forceinline__ uint32_t pack_grad(float a, float b) {  // both to th
 
 // What a row's gradients share: with R = (max + log S) log2(e) as rounded and c what the rounding added,
 //   y = z log2(e) - R,  p = 2^y 2^c,  dz = -2^y (a y + b) with a = 2^c g' ln 2 and b = 2^c (g + g' (entropy + c ln 2))
+// A subnormal p may meet a factor that makes a normal product.  fp32 takes the full exponential for it; bf16, whose 8 bits can spare
+// the last of y's, has y 32 higher and the factor 2^-32 lower; fp16 has no room for such products.
 template <int TYPE>
 struct GradRow {
+    static constexpr float kLift = TYPE == SARA_BF16 ? 32.f : 0.f;
     float r, a, b;
     uint32_t least;  // a logit below every one that counts: those of -inf are raised to it
     bool plain;      // else the logits are taken one by one
@@ -552,6 +555,11 @@ struct GradRow {
         const float k = exp2_approx(c);
         a = k * gh * kLn2;
         b = k * fmaf(gh, fmaf(c, kLn2, H), g);
+        if constexpr (kLift > 0.f) {
+            r -= kLift;
+            b = fmaf(-kLift, a, b) * 2.3283064e-10f;  // 2^-32
+            a *= 2.3283064e-10f;
+        }
         const float low = m - 1000.f - fabsf(m) * 0.015625f;
         least = TYPE == SARA_FP32 ? __float_as_uint(low) : TYPE == SARA_BF16 ? f32_to_bf16(low) * 0x10001u : f32_to_f16_sat(low) * 0x10001u;
     }
@@ -604,9 +612,8 @@ __global__ void __launch_bounds__(256) score_grad_kernel(ScoreGradParams p) {
                 for (int e = 0; e < E; e += 2) {
                     const uint64_t y2 = fma_f32x2(pack_f32x2(y[e], y[e + 1]), l2, r2);
                     const float2 t = unpack_f32x2(y2), f = unpack_f32x2(fma_f32x2(y2, a2, b2));
-                    // (a product with a subnormal power may be normal again; fp16 has no room for either)
-                    y[e] = (TYPE == SARA_FP16 ? exp2_approx(t.x) : exp2_full(t.x)) * f.x;
-                    y[e + 1] = (TYPE == SARA_FP16 ? exp2_approx(t.y) : exp2_full(t.y)) * f.y;
+                    y[e] = (TYPE == SARA_FP32 ? exp2_full(t.x) : exp2_approx(t.x)) * f.x;
+                    y[e + 1] = (TYPE == SARA_FP32 ? exp2_full(t.y) : exp2_approx(t.y)) * f.y;
                 }
             } else {
                 unpack_vector<TYPE>(x[u], y);
