@@ -28,7 +28,7 @@ __host__ __device__ constexpr int attn_kv8_step(int hd) { return attn_kv8_positi
 constexpr int kAttnKv8SmCtas = 16 / kAttnKv8Warps;
 constexpr int kAttnKv8MaxCtas = 160 * kAttnKv8SmCtas;
 constexpr int kAttnKv8Group = 16;                               // states joined at a time
-constexpr int kAttnKv8Batch = 8;                                // of them in shared memory
+constexpr int kAttnKv8Batch = 4;                                // of them to a copy, two copies in shared memory
 constexpr float kAttnKv8Shift = 7.f;                            // log2 of the probabilities' scale
 
 // Floats of a state: max and sum of 8 heads, then their outputs
@@ -138,36 +138,41 @@ struct AttnKv8Group {
     }
 };
 
-// The last CTA of a group joins its states, and so on up, 8 states at a time by way of shared memory (whose copies leave the
-// main loop its registers): 16 threads a head.  Whole CTAs; room: of 8 states.
+// The last CTA of a group joins its states, and so on up, by way of shared memory (whose copies leave the main loop its
+// registers): 16 threads a head, two batches of states on their way at a time.  Whole CTAs; room: of both batches.
 template <int HD>
 __device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD> u, float *room, int *s_last) {
     constexpr int B = kAttnKv8Batch, STATE = attn_kv8_state(HD), NF = HD / 16, W = NF < 4 ? NF : 4;
     const AttnKv8Params &p = u.p;
     const int tid = threadIdx.x, G = p.H / p.c.KVH, hh = tid / 16, i0 = tid % 16 * W;
-    const uint32_t to = smem_u32(room);
+    auto fetch = [&](int k0) {  // the batch from state k0 on, if there is one
+        const uint32_t to = smem_u32(room + (k0 / B & 1) * (B * STATE));
+#pragma unroll
+        for (int k = 0; k < B; ++k) {
+            if (k >= u.n - k0) continue;
+            const float *src = u.state(k0 + k);
+#pragma unroll
+            for (int e = 0; e < STATE / 4; e += kAttnKv8Threads)
+                if (e + tid < STATE / 4) cp_async16(to + (k * STATE + 4 * (e + tid)) * 4, src + 4 * (e + tid));
+        }
+        cp_async_commit();
+    };
 #pragma unroll 1
     for (;;) {
         float M = -3.4028235e38f, L = 0.f, y[NF];
 #pragma unroll
         for (int i = 0; i < NF; ++i) y[i] = 0.f;
+        fetch(0);
+        fetch(B);
 #pragma unroll 1
         for (int k0 = 0; k0 < u.n; k0 += B) {
-#pragma unroll
-            for (int k = 0; k < B; ++k) {
-                if (k >= u.n - k0) continue;
-                const float *src = u.state(k0 + k);
-#pragma unroll
-                for (int e = 0; e < STATE / 4; e += kAttnKv8Threads)
-                    if (e + tid < STATE / 4) cp_async16(to + (k * STATE + 4 * (e + tid)) * 4, src + 4 * (e + tid));
-            }
-            cp_async_commit();
-            cp_async_wait<0>();
+            cp_async_wait<1>();
             __syncthreads();
+            const float *batch = room + (k0 / B & 1) * (B * STATE);
             float N = M, m[B];
 #pragma unroll
             for (int k = 0; k < B; ++k) {  // (behind the last state: nothing)
-                m[k] = k < u.n - k0 ? room[k * STATE + hh] : -INFINITY;
+                m[k] = k < u.n - k0 ? batch[k * STATE + hh] : -INFINITY;
                 N = fmaxf(N, m[k]);
             }
             const float old = ex2(M - N);
@@ -178,13 +183,14 @@ __device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD> u, float *room, i
 #pragma unroll
             for (int k = 0; k < B; ++k) {
                 if (k >= u.n - k0) continue;
-                const float *x = room + k * STATE;
+                const float *x = batch + k * STATE;
                 const float f = ex2(m[k] - N);
                 L += f * x[8 + hh];
 #pragma unroll
                 for (int i = 0; i < NF; ++i) y[i] += f * x[16 + hh * HD + i0 + i / W * 64 + i % W];
             }
             __syncthreads();
+            fetch(k0 + 2 * B);
         }
         const bool final = !u.two() || u.pace > 1;
         if (hh < G) {
@@ -223,7 +229,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
     constexpr int STATE = attn_kv8_state(HD);
     __shared__ __align__(16) union {
         float o[kAttnKv8Warps][8][PITCH];     // the warps' outputs
-        float room[kAttnKv8Batch * STATE];  // states that are joined
+        float room[2 * kAttnKv8Batch * STATE];  // states that are joined
     } sm;
     auto &s_o = sm.o;
     __shared__ float s_m[kAttnKv8Warps][8], s_l[kAttnKv8Warps][8];

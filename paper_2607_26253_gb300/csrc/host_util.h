@@ -3,6 +3,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <stdexcept>
 #include <string>
 
@@ -24,10 +25,15 @@ inline void check_cuda(cudaError_t e, const char *what, const char *file, int li
 }
 #define CK(x) ::sara::check_cuda((x), #x, __FILE__, __LINE__)
 
+// SMs of the current device, asked for once a device
 inline int sm_count() {
+    constexpr int kMaxDevices = 64;
+    static std::atomic<int> known[kMaxDevices];
     int dev = 0, sms = 0;
     CK(cudaGetDevice(&dev));
+    if (dev >= 0 && dev < kMaxDevices && (sms = known[dev].load(std::memory_order_relaxed)) > 0) return sms;
     CK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    if (dev >= 0 && dev < kMaxDevices) known[dev].store(sms, std::memory_order_relaxed);
     return sms;
 }
 
