@@ -2,19 +2,25 @@
 //     out[i, h] = softmax(q[i, h] . K[first_i .. ctx_i)^T / sqrt(hd)) V[first_i .. ctx_i)
 // Bound by reading the codes once (2 hd bytes a position and KV head), so every byte goes from memory to registers in
 // the order in which the warp-level MMAs want it, 16 bytes a lane, and becomes fp16 there, which both
-// formats fit exactly; a warp takes 16 positions of each page of 128.
+// formats fit exactly; a warp takes 16 positions at a time (32 below 128 dims).
 //   - Scores: A = K (rows: positions), B = q^T (columns: the group's query heads, at most 8).  Lane (g, t) loads
 //     16 consecutive dims of positions g and g + 8; which dims meet in a k-step does not matter as long as q is laid out
 //     alike.  bf16 queries enter as fp16 after a power of two has brought the row's largest to 2^14.
 //   - Output: A = V^T (rows: dims, lane (g, t) holds hd / 8 dims of 4 positions, byte permutes pair the positions),
 //     B = P^T, the scores' own registers transposed by movmatrix.  P enters as an fp16 pair, hi + lo: 22 bits, and
 //     multiples of 2^-31 of the maximum (probabilities are scaled by 2^7).
-//   - A scale covers both of a warp's rows of 8 positions: K's is a factor of the scores, V's of P, relative to the largest so far
+//   - A scale covers all of a warp's positions: K's is a factor of the scores, V's of P, relative to the largest so far
 //     (vref), so that neither costs a multiplication per code.
 // Online softmax in fp32 per warp; the maximum is re-based only when a probability would pass 2^8, so most steps
-// skip the column maximum and the rescale.  Work: the (row, KV head, 64 positions) triples in one list, cut into
-// equal shares, one per CTA of 4 warps; a (row, KV head) that several CTAs share is joined by the last of them to
-// finish, in the list's order, in two levels where there are many.
+// skip the column maximum and the rescale.  A step's values are asked for before its scores are taken, the next step's keys
+// over the used ones right after: 64 KB an SM are on their way (both ahead of a whole step: 179 us for 174 below).
+// Work: the (row, KV head, 64 or 128 positions) triples in one list, cut into equal shares, one per CTA of 4 warps (4 an SM:
+// 8-warp CTAs on whole pages took 212 us for 174, since fewer units overlap where one ends); a unit's first loads are
+// under way while the one before is put together.  A (row, KV head) that several CTAs share is joined by the last of them
+// to finish, in the list's order (so results repeat bit for bit), in two levels where there are many.
+// Measured (kernel in a graph): 64 rows x 8,192 positions, 32 / 8 heads of 128: 171 us, 6.3 TB/s; 2 x 200,000, 16 / 2 heads: 48 us
+// (the steps end after 33 to 37, the two levels of joins take 10); 26 ragged rows of mean 758, 12 / 2 heads: 12 us and one row 7.6,
+// chains of latencies: share 0.7 us, first keys 1.1, step 0.5, state 0.9, arrival 0.7, join 2.5.
 #pragma once
 #include "kv8.cuh"
 

@@ -3,6 +3,8 @@
 // A power of two costs e4m3 nothing (its steps are relative) and int8 half a bit on average, and it makes raising a scale
 // exact but for the bits that fall off the lower end: the errors of any number of raises add up to at most
 // 1/2 + 1/4 + ... of one smallest step, where a free scale would round every code again each time.
+// Both directions are bound by memory: 64 x 1,024 tokens of 8 heads of 128 are written in 61 us (403 MB, 6.6 TB/s), 48 x 4,096 read back
+// in 178 (1,208 MB, 6.8 TB/s); one token each of 26 rows 3.5 us, a chain of three dependent loads.
 #pragma once
 #include "device_common.cuh"
 #include "host_util.h"
@@ -152,7 +154,8 @@ __device__ __forceinline__ bool kv8_find(const Kv8Range &r, int max_blocks, int6
 }
 
 // One warp per scale block, KV head and K or V: the block's new tokens wait in registers for their largest
-// magnitude, so k and v are read once.
+// magnitude, so k and v are read once.  (64 registers a lane at 128 dims: 20 warps an SM hold 160 KB, more than the
+// bandwidth times the latency.)
 template <int HD, int FMT, int TYPE>
 __global__ void __launch_bounds__(128) kv8_write_kernel(Kv8Cache c, Kv8Range r, const uint16_t *k, int64_t k_stride,
                                                         const uint16_t *v, int64_t v_stride, int64_t warps, int32_t *status) {

@@ -124,14 +124,16 @@ def kv8_read(codes, scales, table, pos0, seq_start, total: int, dtype=None, stat
     if out is None:
         shape, dtype = (total, c.n_kv_heads, c.head_dim), dtype or torch.bfloat16
         k, v = scales.new_empty(shape, dtype=dtype), scales.new_empty(shape, dtype=dtype)
+        ks = vs = c.n_kv_heads * c.head_dim
     else:
         k, v = out
+        ks, vs = _kv8_tokens(k, c, total, dev, "out[0]"), _kv8_tokens(v, c, total, dev, "out[1]")
     typ = _types.get(k.dtype)
     if typ is None or v.dtype != k.dtype:
         _refuse("what is read must be bf16, fp16 or fp32")
     _launch(dev, load().sara_kv8_read, ctypes.byref(c), n, _vector(pos0, _int32, n, dev, "pos0"),
-            _vector(seq_start, _int32, n + 1, dev, "seq_start"), total, k.data_ptr(), _kv8_tokens(k, c, total, dev, "out[0]"),
-            v.data_ptr(), _kv8_tokens(v, c, total, dev, "out[1]"), typ, _vector(status, _int32, 1, dev, "status"))
+            _vector(seq_start, _int32, n + 1, dev, "seq_start"), total, k.data_ptr(), ks, v.data_ptr(), vs, typ,
+            _vector(status, _int32, 1, dev, "status"))
     return k, v
 
 
@@ -158,14 +160,16 @@ def attention_decode_kv8(q, codes, scales, table, ctx, first=None, workspace=Non
         _refuse("q must have each row's heads side by side")
     if out is None:
         out = q.new_empty(shape)
+        at = out.data_ptr()
+    else:
+        at = _matrix(out, q.dtype, shape, dev, "out")
     if workspace is None:
         workspace = attention_kv8_workspace(n, H, c.n_kv_heads, hd, q.device)
     elif workspace.get_device() != dev or not workspace.is_contiguous():
         _refuse("workspace must be contiguous, on the cache's device")
     _launch(dev, load().sara_attention_decode_kv8, ctypes.byref(c), n, H, q.data_ptr(), row, _vector(ctx, _int32, n, dev, "ctx"),
-            _vector(first, _int32, n, dev, "first"), _matrix(out, q.dtype, shape, dev, "out"),
-            _matrix(lse, _fp32, (n, H), dev, "lse"), typ, _vector(status, _int32, 1, dev, "status"), workspace.data_ptr(),
-            workspace.nbytes)
+            _vector(first, _int32, n, dev, "first"), at, _matrix(lse, _fp32, (n, H), dev, "lse"), typ,
+            _vector(status, _int32, 1, dev, "status"), workspace.data_ptr(), workspace.nbytes)
     return out
 
 
@@ -218,10 +222,11 @@ def logprobs_backward(logits, tokens, stats, entropy, grad_logprob=None, grad_en
     shape = logits.shape
     R, V = shape
     if out is None:
-        out = logits.new_empty(shape)
-    otyp, orow, odev = _logits(out, "out")
-    if otyp != typ or odev != dev or out.shape != shape:
-        _refuse("out must be like logits")
+        out, orow = logits.new_empty(shape), V
+    else:
+        otyp, orow, odev = _logits(out, "out")
+        if otyp != typ or odev != dev or out.shape != shape:
+            _refuse("out must be like logits")
     _launch(dev, load().sara_logprobs_backward, logits.data_ptr(), row, typ, R, V, _vector(tokens, _int32, R, dev, "tokens"),
             _matrix(stats, _fp32, (R, 2), dev, "stats"), _vector(entropy, _fp32, R, dev, "entropy"),
             _vector(grad_logprob, _fp32, R, dev, "grad_logprob"), _vector(grad_entropy, _fp32, R, dev, "grad_entropy"),
