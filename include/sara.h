@@ -391,7 +391,8 @@ SARA_API int sara_kv8_write(const sara_kv8_cache *cache, int32_t n_seq, const in
 /*
  * Read tokens back: row seq_start[i] + j of k and v receives position pos0[i] + j of sequence i, rounded once to `type`
  * (any SARA_* type).  Layout as sara_kv8_write.  Rows that belong to no sequence are left as they are.
- * Positions outside the table or in a block whose id is wrong read as NaN and set *status.
+ * Positions outside the table or in a block whose id is wrong read as NaN and set *status; a wrong seq_start sets it too, and its rows
+ * are left as they are.
  */
 SARA_API int sara_kv8_read(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *pos0, const int32_t *seq_start,
                            int32_t total, void *k, int64_t k_stride, void *v, int64_t v_stride, int32_t type, int32_t *status,

@@ -45,7 +45,7 @@ def write(codes, scales, fmt, table_row, pos0, k, v):
                     continue
                 e = exponent(np.abs(new).max(), fmt)
                 if a > base:
-                    eo = int(np.rint(np.log2(old)))
+                    eo = int(np.frexp(old)[1]) - 1
                     if eo < e:
                         codes[page, kv, h, base:a] = to_grid(codes[page, kv, h, base:a] * 2.0 ** (eo - e), fmt)
                     e = max(e, eo)

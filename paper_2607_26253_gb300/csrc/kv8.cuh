@@ -118,8 +118,14 @@ struct Kv8Unit {
     int seq, lo, hi;  // positions lo .. hi of the sequence, within one scale block
     int row;          // packed row of position lo
     bool held;        // the block holds earlier tokens
-    bool bad;         // the sequence's range is wrong
+    bool bad;         // the sequence's positions are wrong
 };
+// Warp w < n looks at sequence w's range, whichever unit is its own: starts that fall may leave a sequence without one.
+__device__ __forceinline__ void kv8_check(const Kv8Range &r, int max_blocks, int64_t w, int32_t *status) {
+    if (w >= r.n || (threadIdx.x & 31) != 0 || !status) return;
+    const int a = __ldg(r.start + w), b = __ldg(r.start + w + 1), p0 = __ldg(r.pos0 + w);
+    if (a < 0 || b < a || b > r.total || (b > a && (p0 < 0 || (int64_t)p0 + (b - a) > (int64_t)max_blocks * kKv8Page))) kv8_report(status);
+}
 // Whole warps call this with the same u.  False: nothing to do.
 __device__ __forceinline__ bool kv8_find(const Kv8Range &r, int max_blocks, int64_t u, Kv8Unit &x) {
     const int lane = threadIdx.x & 31;
@@ -133,11 +139,7 @@ __device__ __forceinline__ bool kv8_find(const Kv8Range &r, int max_blocks, int6
         hi = min(hi, lo + step);
     }
     const int a = __ldg(r.start + lo), b = __ldg(r.start + lo + 1), p0 = __ldg(r.pos0 + lo);
-    if (a < 0 || b < a || b > r.total) {
-        x.bad = true;
-        x.lo = x.hi = 0;
-        return true;
-    }
+    if (a < 0 || b < a || b > r.total) return false;
     const int64_t local = u - kv8_first_unit(a, lo);
     if (local < 0 || b == a) return false;
     const int64_t end = (int64_t)p0 + (b - a);
@@ -163,12 +165,10 @@ __global__ void __launch_bounds__(128) kv8_write_kernel(Kv8Cache c, Kv8Range r, 
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     if (w >= warps) return;
     const int lane = threadIdx.x & 31, h = (int)(w % c.KVH), kv = (int)(w / c.KVH % 2);
+    kv8_check(r, c.max_blocks, w, status);
     Kv8Unit x;
     if (!kv8_find(r, c.max_blocks, w / (2 * c.KVH), x)) return;
-    if (x.bad) {
-        kv8_report(status);
-        return;
-    }
+    if (x.bad) return;  // (reported above)
     const int block = __ldg(c.table + x.seq * c.table_stride + x.lo / kKv8Page);
     if (block < 0 || block >= c.n_blocks) {
         kv8_report(status);
@@ -267,6 +267,7 @@ __global__ void __launch_bounds__(128) kv8_read_kernel(Kv8Cache c, Kv8Range r, u
     const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
     if (w >= warps) return;
     const int lane = threadIdx.x & 31, h = (int)(w % c.KVH), kv = (int)(w / c.KVH % 2);
+    kv8_check(r, c.max_blocks, w, status);
     Kv8Unit x;
     if (!kv8_find(r, c.max_blocks, w / (2 * c.KVH), x)) return;
     bool bad = x.bad;

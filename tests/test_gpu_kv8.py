@@ -199,7 +199,8 @@ def test_wrong_ranges_and_blocks_are_skipped_and_reported(pkg):
         assert (w, r) == (pkg.SARA_EINVAL, pkg.SARA_EINVAL)
         assert np.isnan(x[20:30]).all() and np.isfinite(np.delete(x, slice(20, 30))).all()
     # starts that leave the tokens or fall: nothing outside them is touched
-    for bad in ([0, 10, 20, 30, 40, 50, 61], [0, 10, 20, 30, 40, 50, 2 ** 31 - 1], [-5, 10, 20, 30, 40, 50, 60], [0, 30, 20, 30, 40, 50, 60]):
+    for bad in ([0, 10, 20, 30, 40, 50, 61], [0, 10, 20, 30, 40, 50, 2 ** 31 - 1], [-5, 10, 20, 30, 40, 50, 60], [0, 30, 20, 30, 40, 50, 60],
+                [0, 60, 0, 60, 0, 60, 0], [60, 50, 40, 30, 20, 10, 0], [0, 2 ** 31 - 1, -2 ** 31, 3, 4, 5, 6], [0, 10, 20, 30, 40, 61, 60]):
         w, r, x = call(np.zeros(6), bad)
         assert (w, r) == (pkg.SARA_EINVAL, pkg.SARA_EINVAL)
     spare = np.setdiff1d(np.arange(c.codes.shape[0]), good[:, 0])
