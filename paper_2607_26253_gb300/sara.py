@@ -125,7 +125,7 @@ def load(path: str = LIB_PATH):
     lib.sara_gemm_bf16_static.restype = ctypes.c_int
     lib.sara_set_limits.argtypes = [c_p, ctypes.POINTER(Limits)]
     lib.sara_set_limits.restype = ctypes.c_int
-    i32, i64, cache_p = ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(Kv8Cache)
+    i32, i64, cache_p = ctypes.c_int32, ctypes.c_int64, c_p  # (a Kv8Cache by reference, or its bytes)
     lib.sara_kv8_write.argtypes = [cache_p, i32, c_p, c_p, i32, c_p, i64, c_p, i64, i32, c_p, c_p]
     lib.sara_kv8_write.restype = ctypes.c_int
     lib.sara_kv8_read.argtypes = lib.sara_kv8_write.argtypes
