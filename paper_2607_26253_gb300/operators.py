@@ -1,8 +1,8 @@
 """Operators on torch CUDA tensors over an 8-bit paged KV cache and over the logits of sampled tokens (include/sara.h).
 
-Results are not recorded by autograd: logprobs has its gradient as a call of its own.  These are a decode step's calls, and most of them cost more on the host than on the GPU: checks are written out where they are
-made, messages put together only for a refusal, and the cache's description is packed as bytes instead of a ctypes structure
-(~2 us of 14 a call).
+Results are not recorded by autograd: logprobs has its gradient as a call of its own.  These are a decode step's calls, and
+most of them cost more on the host than on the GPU: checks are written out where they are made, messages put together only for a
+refusal, and the cache's description is packed as bytes instead of a ctypes structure (~2 us of 14 a call).
 """
 from __future__ import annotations
 
