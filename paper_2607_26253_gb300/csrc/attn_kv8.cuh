@@ -33,7 +33,7 @@ __host__ __device__ constexpr int attn_kv8_positions(int hd) { return hd == 128 
 __host__ __device__ constexpr int attn_kv8_step(int hd) { return attn_kv8_positions(hd) * kAttnKv8Warps; }  // positions of an entry of the list
 constexpr int kAttnKv8SmCtas = 16 / kAttnKv8Warps;
 constexpr int kAttnKv8MaxCtas = 160 * kAttnKv8SmCtas;
-constexpr int kAttnKv8Group = 16;                               // states joined at a time
+constexpr int kAttnKv8Group = 16;                               // states joined at a time (2 x 200,000: 48.0 us; 8 49.0, 32 49.5, 64 53.2)
 constexpr int kAttnKv8Batch = 4;                                // of them to a copy, two copies in shared memory
 constexpr float kAttnKv8Shift = 7.f;                            // log2 of the probabilities' scale
 
@@ -230,6 +230,8 @@ template <int HD, int FMT>
 __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kernel(AttnKv8Params p) {
     constexpr int KW = HD / 16, VW = HD / 32, NT = HD / 16;  // words a lane of a key row, of a value row; output tiles
     constexpr int KL = KW < 4 ? KW : 4;                      // words a load
+    // Steps at a time: 32 dims leave registers for two (64 rows x 16,384: 121 -> 105 us, int8 131 -> 115; 512 positions 12.3 -> 12.7)
+    constexpr int SUB = HD == 32 ? 2 : 1;
     constexpr int POS = attn_kv8_positions(HD), NG = POS / 16, STEP = attn_kv8_step(HD), PS = kKv8Page / STEP;
     constexpr int PITCH = HD + 4;                            // (conflict-free 8-byte stores)
     constexpr int STATE = attn_kv8_state(HD);
@@ -312,45 +314,46 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
         return __shfl_sync(0xffffffffu, ids, page - idbase);
     };
     const int lane_k = (KW == 8 ? 16 : HD / 4) * t, lane_v = HD / 8 * g;
+    auto step_of = [&](int x, int u) { return u == 0 ? x : min(x + u, xb - 1); };  // (behind the last step that step again, masked)
     auto edge = [&](int x) {  // whether some of its positions are masked
         const int p0 = x * STEP + POS * warp;
-        return p0 < r.first || p0 + POS > r.ctx;
+        return p0 < r.first || p0 > r.ctx - POS;
     };
     auto slot_of = [&](int x, int e) {  // (masked positions stand for the nearest that is not: their probability is 0)
         return min(max(x * STEP + POS * warp + e, r.first), r.ctx - 1) & (kKv8Page - 1);
     };
     auto block_in_page = [&](int x) { return (x % PS * STEP + POS * warp) / kKv8Block; };
-    uint32_t kr[2 * NG][KW], vr[4 * NG][VW];  // positions g + 8 e; 2 t + (e & 1) + 8 (e >> 1)
-    float ks = 0.f, vs = 0.f;
-    int blk = 0;
-    auto load_k = [&](int x) {
-        const int64_t tile = kv8_tile(p.c, max(blk, 0), 0, h);
-        ks = blk < 0 ? nan : __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
+    uint32_t kr[SUB][2 * NG][KW], vr[SUB][4 * NG][VW];  // positions g + 8 e; 2 t + (e & 1) + 8 (e >> 1)
+    float ks[SUB], vs[SUB];
+    int blk[SUB] = {};
+    auto load_k = [&](int x, int u) {
+        const int64_t tile = kv8_tile(p.c, max(blk[u], 0), 0, h);
+        ks[u] = blk[u] < 0 ? nan : __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
         const uint8_t *k = p.c.codes + tile * (kKv8Page * HD) + lane_k;
         if (!edge(x)) {
             k += (x % PS * STEP + POS * warp + g) * HD;
 #pragma unroll
             for (int e = 0; e < 2 * NG; ++e)
 #pragma unroll
-                for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + 8 * e * HD + 64 * i, &kr[e][4 * i]);
+                for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + 8 * e * HD + 64 * i, &kr[u][e][4 * i]);
         } else {
 #pragma unroll
             for (int e = 0; e < 2 * NG; ++e)
 #pragma unroll
-                for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + slot_of(x, g + 8 * e) * HD + 64 * i, &kr[e][4 * i]);
+                for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + slot_of(x, g + 8 * e) * HD + 64 * i, &kr[u][e][4 * i]);
         }
     };
-    auto load_v = [&](int x) {
-        const int64_t tile = kv8_tile(p.c, max(blk, 0), 1, h);
-        vs = __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
+    auto load_v = [&](int x, int u) {
+        const int64_t tile = kv8_tile(p.c, max(blk[u], 0), 1, h);
+        vs[u] = __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
         const uint8_t *v = p.c.codes + tile * (kKv8Page * HD) + lane_v;
         if (!edge(x)) {
             v += (x % PS * STEP + POS * warp + 2 * t) * HD;
 #pragma unroll
-            for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(v + ((e & 1) + 8 * (e >> 1)) * HD, vr[e]);
+            for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(v + ((e & 1) + 8 * (e >> 1)) * HD, vr[u][e]);
         } else {
 #pragma unroll
-            for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(v + slot_of(x, 2 * t + (e & 1) + 8 * (e >> 1)) * HD, vr[e]);
+            for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(v + slot_of(x, 2 * t + (e & 1) + 8 * (e >> 1)) * HD, vr[u][e]);
         }
     };
     // queries: head g of the group, the dims of this lane's key words
@@ -367,8 +370,11 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
         if ((xb - 1) * STEP + POS * warp >= r.ctx) --xb;
         tab = p.c.table + row * p.c.table_stride;
         if (xa < xb) {
-            blk = block_of(xa, true);
-            load_k(xa);
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                blk[u] = block_of(step_of(xa, u), u == 0);
+                load_k(step_of(xa, u), u);
+            }
         }
         const uint16_t *qp = p.q + row * p.q_stride + (int64_t)(h * G + min(g, G - 1)) * HD;
 #pragma unroll
@@ -417,43 +423,62 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
 #pragma unroll 1
-        for (int x = xa; x < xb; ++x) {
-            // this step's values come while its scores are taken, the next one's keys after that
-            load_v(x);
-            float s[NG][4];
-            const float f0 = ks * mul0, f1 = ks * mul1;
+        for (int x = xa; x < xb; x += SUB) {
+            // these steps' values come while their scores are taken, the next ones' keys after that
 #pragma unroll
-            for (int n = 0; n < NG; ++n) {
-                float s2[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int u = 0; u < SUB; ++u) load_v(step_of(x, u), u);
+            float s[SUB][NG][4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
+            for (int u = 0; u < SUB; ++u) {
+                const float f0 = ks[u] * mul0, f1 = ks[u] * mul1;
 #pragma unroll
-                for (int i = 0; i < KW; ++i) {
-                    uint32_t f[4];
-                    decode4_half<FMT>(kr[2 * n][i], f[0], f[2]);
-                    decode4_half<FMT>(kr[2 * n + 1][i], f[1], f[3]);
-                    mma_f16_16816(i & 1 ? s2 : s[n], f, qb[i][0], qb[i][1]);
+                for (int n = 0; n < NG; ++n) {
+                    float s2[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[u][n][e] = 0.f;
+#pragma unroll
+                    for (int i = 0; i < KW; ++i) {
+                        uint32_t f[4];
+                        decode4_half<FMT>(kr[u][2 * n][i], f[0], f[2]);
+                        decode4_half<FMT>(kr[u][2 * n + 1][i], f[1], f[3]);
+                        mma_f16_16816(i & 1 ? s2 : s[u][n], f, qb[i][0], qb[i][1]);
+                    }
+                    // s[u][n][0], [1]: position 16 n + g, heads 2 t and 2 t + 1; [2], [3]: position 16 n + g + 8
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[u][n][e] = (s[u][n][e] + s2[e]) * (e & 1 ? f1 : f0);
                 }
-                // s[n][0], s[n][1]: position 16 n + g, heads 2 t and 2 t + 1; s[n][2], s[n][3]: position 16 n + g + 8
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[n][e] = (s[n][e] + s2[e]) * (e & 1 ? f1 : f0);
             }
-            const bool cut = edge(x);
-            const float vsc = vs;
-            if (x + 1 < xb) {
-                blk = block_of(x + 1, false);
-                load_k(x + 1);
+            float vsc[SUB];
+            bool cut[SUB];
+#pragma unroll
+            for (int u = 0; u < SUB; ++u) {
+                vsc[u] = vs[u];
+                cut[u] = edge(x + u);
+            }
+            if (x + SUB < xb) {
+#pragma unroll
+                for (int u = 0; u < SUB; ++u) {
+                    blk[u] = block_of(step_of(x + SUB, u), false);
+                    load_k(step_of(x + SUB, u), u);
+                }
             }
             float t0 = -INFINITY, t1 = -INFINITY;
 #pragma unroll
-            for (int n = 0; n < NG; ++n) {
-                if (cut) {
-                    const int p0 = x * STEP + POS * warp + 16 * n + g;
-                    if (p0 < r.first || p0 >= r.ctx) s[n][0] = s[n][1] = -INFINITY;
-                    if (p0 + 8 < r.first || p0 + 8 >= r.ctx) s[n][2] = s[n][3] = -INFINITY;
+            for (int u = 0; u < SUB; ++u) {
+                const bool none = u > 0 && x + u >= xb;
+                if (none || cut[u]) {
+#pragma unroll
+                    for (int n = 0; n < NG; ++n) {
+                        const int p0 = (x + u) * STEP + POS * warp + 16 * n + g;
+                        if (none || p0 < r.first || p0 >= r.ctx) s[u][n][0] = s[u][n][1] = -INFINITY;
+                        if (none || p0 + 8 < r.first || p0 + 8 >= r.ctx) s[u][n][2] = s[u][n][3] = -INFINITY;
+                    }
                 }
-                t0 = fmaxf(t0, fmaxf(s[n][0], s[n][2]));
-                t1 = fmaxf(t1, fmaxf(s[n][1], s[n][3]));
+#pragma unroll
+                for (int n = 0; n < NG; ++n) {
+                    t0 = fmaxf(t0, fmaxf(s[u][n][0], s[u][n][2]));
+                    t1 = fmaxf(t1, fmaxf(s[u][n][1], s[u][n][3]));
+                }
             }
             if (__any_sync(0xffffffffu, t0 > m0 + 8.f || t1 > m1 + 8.f)) {
                 float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
@@ -475,44 +500,48 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                     o[j][3] *= a1;
                 }
             }
-            if (!(vsc <= vref)) {  // the largest scale so far (or NaN)
-                const float inv = 1.f / vsc, f = vref * inv;
-                vref = vsc;
-                vinv = inv;
+            const float c0 = m0 - kAttnKv8Shift, c1 = m1 - kAttnKv8Shift;
 #pragma unroll
-                for (int j = 0; j < NT; ++j)
+            for (int u = 0; u < SUB; ++u) {
+                if (!(vsc[u] <= vref)) {  // the largest scale so far (or NaN)
+                    const float inv = 1.f / vsc[u], f = vref * inv;
+                    vref = vsc[u];
+                    vinv = inv;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) o[j][e] *= f;
-            }
-            const float c0 = m0 - kAttnKv8Shift, c1 = m1 - kAttnKv8Shift, vf = vsc * vinv;
+                    for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int n = 0; n < NG; ++n) {
-                float w0 = ex2(s[n][0] - c0), w1 = ex2(s[n][1] - c1), w2 = ex2(s[n][2] - c0), w3 = ex2(s[n][3] - c1);
-                l0 += w0 + w2;
-                l1 += w1 + w3;
-                w0 *= vf;
-                w1 *= vf;
-                w2 *= vf;
-                w3 *= vf;
-                uint32_t ph[2] = {pack_half2(w0, w1), pack_half2(w2, w3)}, pl[2];
-                const float2 h0 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[0]));
-                const float2 h1 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[1]));
-                pl[0] = movmatrix_trans(pack_half2(w0 - h0.x, w1 - h0.y));
-                pl[1] = movmatrix_trans(pack_half2(w2 - h1.x, w3 - h1.y));
-                ph[0] = movmatrix_trans(ph[0]);
-                ph[1] = movmatrix_trans(ph[1]);
+                        for (int e = 0; e < 4; ++e) o[j][e] *= f;
+                }
+                const float vf = vsc[u] * vinv;
 #pragma unroll
-                for (int i = 0; i < VW; ++i) {
-                    uint32_t v0[4], v1[4];  // dims 4 i, 4 i + 1 and 4 i + 2, 4 i + 3 of the lane's
-                    const uint32_t a = vr[4 * n][i], b = vr[4 * n + 1][i], c = vr[4 * n + 2][i], d = vr[4 * n + 3][i];
-                    decode4_half<FMT>(__byte_perm(a, b, 0x5140), v0[0], v0[1]);
-                    decode4_half<FMT>(__byte_perm(c, d, 0x5140), v0[2], v0[3]);
-                    decode4_half<FMT>(__byte_perm(a, b, 0x7362), v1[0], v1[1]);
-                    decode4_half<FMT>(__byte_perm(c, d, 0x7362), v1[2], v1[3]);
-                    mma_f16_16816(o[2 * i], v0, ph[0], ph[1]);
-                    mma_f16_16816(o[2 * i + 1], v1, ph[0], ph[1]);
-                    mma_f16_16816(o[2 * i], v0, pl[0], pl[1]);
-                    mma_f16_16816(o[2 * i + 1], v1, pl[0], pl[1]);
+                for (int n = 0; n < NG; ++n) {
+                    float w0 = ex2(s[u][n][0] - c0), w1 = ex2(s[u][n][1] - c1), w2 = ex2(s[u][n][2] - c0), w3 = ex2(s[u][n][3] - c1);
+                    l0 += w0 + w2;
+                    l1 += w1 + w3;
+                    w0 *= vf;
+                    w1 *= vf;
+                    w2 *= vf;
+                    w3 *= vf;
+                    uint32_t ph[2] = {pack_half2(w0, w1), pack_half2(w2, w3)}, pl[2];
+                    const float2 h0 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[0]));
+                    const float2 h1 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[1]));
+                    pl[0] = movmatrix_trans(pack_half2(w0 - h0.x, w1 - h0.y));
+                    pl[1] = movmatrix_trans(pack_half2(w2 - h1.x, w3 - h1.y));
+                    ph[0] = movmatrix_trans(ph[0]);
+                    ph[1] = movmatrix_trans(ph[1]);
+#pragma unroll
+                    for (int i = 0; i < VW; ++i) {
+                        uint32_t v0[4], v1[4];  // dims 4 i, 4 i + 1 and 4 i + 2, 4 i + 3 of the lane's
+                        const uint32_t a = vr[u][4 * n][i], b = vr[u][4 * n + 1][i], c = vr[u][4 * n + 2][i], d = vr[u][4 * n + 3][i];
+                        decode4_half<FMT>(__byte_perm(a, b, 0x5140), v0[0], v0[1]);
+                        decode4_half<FMT>(__byte_perm(c, d, 0x5140), v0[2], v0[3]);
+                        decode4_half<FMT>(__byte_perm(a, b, 0x7362), v1[0], v1[1]);
+                        decode4_half<FMT>(__byte_perm(c, d, 0x7362), v1[2], v1[3]);
+                        mma_f16_16816(o[2 * i], v0, ph[0], ph[1]);
+                        mma_f16_16816(o[2 * i + 1], v1, ph[0], ph[1]);
+                        mma_f16_16816(o[2 * i], v0, pl[0], pl[1]);
+                        mma_f16_16816(o[2 * i + 1], v1, pl[0], pl[1]);
+                    }
                 }
             }
         }
