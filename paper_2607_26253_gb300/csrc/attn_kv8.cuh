@@ -14,13 +14,15 @@
 // Online softmax in fp32 per warp; the maximum is re-based only when a probability would pass 2^8, so most steps
 // skip the column maximum and the rescale.  A step's values are asked for before its scores are taken, the next step's keys
 // over the used ones right after: 64 KB an SM are on their way (both ahead of a whole step: 179 us for 174 below).
-// Work: the (row, KV head, 64 or 128 positions) triples in one list, cut into equal shares, one per CTA of 4 warps (4 an SM:
-// 8-warp CTAs on whole pages took 212 us for 174, since fewer units overlap where one ends); a unit's first loads are
-// under way while the one before is put together.  A (row, KV head) that several CTAs share is joined by the last of them
-// to finish, in the list's order (so results repeat bit for bit), in two levels where there are many.
+// Work: the (row, KV head, positions) triples in one list, cut into equal shares, one per CTA of 4 warps (4 an SM:
+// 8-warp CTAs on whole pages took 212 us for 174, since fewer units overlap where one ends), or per warp where there are many
+// rows (kAttnKv8Units); a unit's first loads are under way while the one before is put together.  A (row, KV head) that several
+// shares hold is joined by the last of them to finish, in the list's order (so results repeat bit for bit), by levels where there
+// are many.
 // Measured (kernel in a graph): 64 rows x 8,192 positions, 32 / 8 heads of 128: 171 us, 6.3 TB/s; 2 x 200,000, 16 / 2 heads: 48 us
 // (the steps end after 33 to 37, the two levels of joins take 10); 26 ragged rows of mean 758, 12 / 2 heads: 12 us and one row 7.6,
-// chains of latencies: share 0.7 us, first keys 1.1, step 0.5, state 0.9, arrival 0.7, join 2.5.
+// chains of latencies: share 0.7 us, first keys 1.1, step 0.5, state 0.9, arrival 0.7, join 2.5.  700 ragged rows of mean 200,
+// 32 / 8 heads: 71 us (44 at the copy's rate: the units are 13 steps of a warp, each begins with two exposed latencies).
 #pragma once
 #include "kv8.cuh"
 
@@ -30,9 +32,16 @@ constexpr int kAttnKv8Warps = 4;
 constexpr int kAttnKv8Threads = 32 * kAttnKv8Warps;
 // Positions that a warp takes at a time: as many bytes in flight at 64 dims as at 128; 32 is a scale's block
 __host__ __device__ constexpr int attn_kv8_positions(int hd) { return hd == 128 ? 16 : 32; }
-__host__ __device__ constexpr int attn_kv8_step(int hd) { return attn_kv8_positions(hd) * kAttnKv8Warps; }  // positions of an entry of the list
+__host__ __device__ constexpr int attn_kv8_step(int hd, int warps) { return attn_kv8_positions(hd) * warps; }  // positions of an entry of the list
 constexpr int kAttnKv8SmCtas = 16 / kAttnKv8Warps;
 constexpr int kAttnKv8MaxCtas = 160 * kAttnKv8SmCtas;
+constexpr int kAttnKv8MaxShares = kAttnKv8MaxCtas * kAttnKv8Warps;
+// (row, KV head) pairs from which each warp has a share of its own: nothing is put together between warps, but there are
+// four times the states to join.  8 KV heads of 128, us with a CTA's shares and a warp's: 600 pairs of 200 positions 16.3, 23.0;
+// 1,400: 28.2, 26.8 (of 4,000: 235, 239); 2,800: 49.5, 40.9 (464, 465); 5,600: 88.4, 70.7 (903, 918); of 64 and 32 dims from 1,400 on
+// 6 to 50 % in favour of the warps'
+constexpr int kAttnKv8Units = 1600;
+constexpr int kAttnKv8Levels = 3;                               // of joins
 constexpr int kAttnKv8Group = 16;                               // states joined at a time (2 x 200,000: 48.0 us; 8 49.0, 32 49.5, 64 53.2)
 constexpr int kAttnKv8Batch = 4;                                // of them to a copy, two copies in shared memory
 constexpr float kAttnKv8Shift = 7.f;                            // log2 of the probabilities' scale
@@ -48,8 +57,8 @@ struct AttnKv8Params {
     uint16_t *out;
     float *lse;
     int32_t *status;
-    int *count;   // [CTA][2][2] arrivals at the two levels of a join, kept at its first state; left zero
-    float *part;  // [CTA][2] states
+    int *count;   // [share][2][levels] arrivals at a join, kept at its first state; left zero
+    float *part;  // [share][2] states
     int n, H, type;
     float scale_log2;  // log2(e) / sqrt(hd)
 };
@@ -109,48 +118,57 @@ __device__ __forceinline__ void attn_kv8_put(const AttnKv8Params &p, int row, in
         p.type == SARA_BF16 ? pack2<SARA_BF16>(y0, y1) : pack2<SARA_FP16>(y0, y1);
 }
 
-// A (row, KV head) that CTAs c0 .. c1 share, as CTA c sees it: its states, or where there are more than a group's those
-// of its group, whose result takes the place of the first; then the groups' results.
+// A (row, KV head) that shares c0 .. c1 hold together, as share c sees it: its states, or where there are more than a
+// group's those of its group, whose result takes the place of the first; then the groups' results, and so on up (for the
+// shares of CTAs, whose number is smaller, two levels at most: a level costs them more than a longer group).
 struct AttnKv8Join {
     int row, h, c0, c1;  // row < 0: nothing
 };
-template <int HD>
+template <int HD, int W>
 struct AttnKv8Group {
     const AttnKv8Params &p;
     const AttnKv8Join j;
-    int from, n, pace;
-    __device__ __forceinline__ AttnKv8Group(const AttnKv8Params &p_, const AttnKv8Join &j_, int c) : p(p_), j(j_), from(j_.c0), n(j_.c1 - j_.c0 + 1), pace(1) {
-        if (two()) {
-            from = max(j.c0, c & ~(kAttnKv8Group - 1));
-            n = min(j.c1, c | (kAttnKv8Group - 1)) - from + 1;
-        }
+    const int c;
+    int level, pace, from, n;
+    bool whole;
+    __device__ __forceinline__ AttnKv8Group(const AttnKv8Params &p_, const AttnKv8Join &j_, int c_) : p(p_), j(j_), c(c_), level(0), pace(1) { set(); }
+    __device__ __forceinline__ void set() {
+        const int wide = pace * kAttnKv8Group, of = j.c1 / pace - j.c0 / pace + 1;
+        whole = of <= kAttnKv8Group || level == (W == 1 ? kAttnKv8Levels : 2) - 1;
+        from = whole ? j.c0 : max(j.c0, c & ~(wide - 1));
+        n = whole ? of : min(j.c1, c | (wide - 1)) / pace - from / pace + 1;
     }
-    __device__ __forceinline__ bool two() const { return j.c1 - j.c0 >= kAttnKv8Group; }
-    __device__ __forceinline__ void groups() {
-        from = j.c0;
-        n = j.c1 / kAttnKv8Group - j.c0 / kAttnKv8Group + 1;
-        pace = kAttnKv8Group;
+    __device__ __forceinline__ void up() {
+        ++level;
+        pace *= kAttnKv8Group;
+        set();
     }
     __device__ __forceinline__ float *state(int k) const {
-        const int x = pace == 1 ? from + k : k == 0 ? j.c0 : (j.c0 & ~(kAttnKv8Group - 1)) + k * kAttnKv8Group;
+        const int x = k == 0 ? from : (from & ~(pace - 1)) + k * pace;
         return p.part + (x * 2 + (x == j.c0)) * attn_kv8_state(HD);
     }
-    // One thread, after a barrier: whether the CTA is the last of the group to come
+    // One thread, after a barrier: whether the share is the last of the group to come
     __device__ __forceinline__ bool arrive() const {
-        int *arrived = p.count + (from * 2 + (from == j.c0)) * 2 + (pace > 1);
-        const bool last = atom_add_acq_rel_gpu(arrived, 1) == n - 1;  // (orders the CTA's stores before it, its loads behind)
+        int *arrived = p.count + (from * 2 + (from == j.c0)) * kAttnKv8Levels + level;
+        const bool last = atom_add_acq_rel_gpu(arrived, 1) == n - 1;  // (orders the share's stores before it, its loads behind)
         if (last) *arrived = 0;
         return last;
     }
 };
+template <int W>
+__device__ __forceinline__ void attn_kv8_sync() {  // of a share's threads
+    if constexpr (W == 1) __syncwarp();
+    else __syncthreads();
+}
 
-// The last CTA of a group joins its states, and so on up, by way of shared memory (whose copies leave the main loop its
-// registers): 16 threads a head, two batches of states on their way at a time.  Whole CTAs; room: of both batches.
-template <int HD>
-__device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD> u, float *room, int *s_last) {
-    constexpr int B = kAttnKv8Batch, STATE = attn_kv8_state(HD), NF = HD / 16, W = NF < 4 ? NF : 4;
+// The last share of a group joins its states, and so on up, by way of shared memory (whose copies leave the main loop its
+// registers): 4 threads a head and warp, two batches of states on their way at a time.  tid: of the share's W warps; room: of both
+// batches.
+template <int HD, int W>
+__device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD, W> u, float *room, int *s_last, int tid) {
+    constexpr int T = 4 * W, B = kAttnKv8Batch * W / kAttnKv8Warps, STATE = attn_kv8_state(HD), NF = HD / T, V = NF < 4 ? NF : 4;
     const AttnKv8Params &p = u.p;
-    const int tid = threadIdx.x, G = p.H / p.c.KVH, hh = tid / 16, i0 = tid % 16 * W;
+    const int G = p.H / p.c.KVH, hh = tid / T, i0 = tid % T * V;
     auto fetch = [&](int k0) {  // the batch from state k0 on, if there is one
         const uint32_t to = smem_u32(room + (k0 / B & 1) * (B * STATE));
 #pragma unroll
@@ -158,7 +176,7 @@ __device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD> u, float *room, i
             if (k >= u.n - k0) continue;
             const float *src = u.state(k0 + k);
 #pragma unroll
-            for (int e = 0; e < STATE / 4; e += kAttnKv8Threads)
+            for (int e = 0; e < STATE / 4; e += 32 * W)
                 if (e + tid < STATE / 4) cp_async16(to + (k * STATE + 4 * (e + tid)) * 4, src + 4 * (e + tid));
         }
         cp_async_commit();
@@ -173,7 +191,7 @@ __device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD> u, float *room, i
 #pragma unroll 1
         for (int k0 = 0; k0 < u.n; k0 += B) {
             cp_async_wait<1>();
-            __syncthreads();
+            attn_kv8_sync<W>();
             const float *batch = room + (k0 / B & 1) * (B * STATE);
             float N = M, m[B];
 #pragma unroll
@@ -193,23 +211,22 @@ __device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD> u, float *room, i
                 const float f = ex2(m[k] - N);
                 L += f * x[8 + hh];
 #pragma unroll
-                for (int i = 0; i < NF; ++i) y[i] += f * x[16 + hh * HD + i0 + i / W * 64 + i % W];
+                for (int i = 0; i < NF; ++i) y[i] += f * x[16 + hh * HD + i0 + i / V * (T * V) + i % V];
             }
-            __syncthreads();
+            attn_kv8_sync<W>();
             fetch(k0 + 2 * B);
         }
-        const bool final = !u.two() || u.pace > 1;
         if (hh < G) {
             const float inv = 1.f / L;
             float *x = u.state(0);
 #pragma unroll
             for (int i = 0; i < NF; i += 2) {
-                const int at = i0 + i / W * 64 + i % W;
-                if (final) attn_kv8_put<HD>(p, u.j.row, u.j.h * G + hh, at, y[i] * inv, y[i + 1] * inv);
+                const int at = i0 + i / V * (T * V) + i % V;
+                if (u.whole) attn_kv8_put<HD>(p, u.j.row, u.j.h * G + hh, at, y[i] * inv, y[i + 1] * inv);
                 else *reinterpret_cast<float2 *>(x + 16 + hh * HD + at) = make_float2(y[i], y[i + 1]);
             }
-            if (tid % 16 == 0) {
-                if (!final) {
+            if (tid % T == 0) {
+                if (!u.whole) {
                     x[hh] = M;
                     x[8 + hh] = L;
                 } else if (p.lse) {
@@ -217,22 +234,23 @@ __device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD> u, float *room, i
                 }
             }
         }
-        if (final) return;
-        u.groups();
-        __syncthreads();
+        if (u.whole) return;
+        u.up();
+        attn_kv8_sync<W>();
         if (tid == 0) *s_last = u.arrive();
-        __syncthreads();
+        attn_kv8_sync<W>();
         if (!*s_last) return;
     }
 }
 
-template <int HD, int FMT>
+// W: warps of a share
+template <int HD, int FMT, int W>
 __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kernel(AttnKv8Params p) {
     constexpr int KW = HD / 16, VW = HD / 32, NT = HD / 16;  // words a lane of a key row, of a value row; output tiles
     constexpr int KL = KW < 4 ? KW : 4;                      // words a load
     // Steps at a time: 32 dims leave registers for two (64 rows x 16,384: 121 -> 105 us, int8 131 -> 115; 512 positions 12.3 -> 12.7)
     constexpr int SUB = HD == 32 ? 2 : 1;
-    constexpr int POS = attn_kv8_positions(HD), NG = POS / 16, STEP = attn_kv8_step(HD), PS = kKv8Page / STEP;
+    constexpr int POS = attn_kv8_positions(HD), NG = POS / 16, STEP = attn_kv8_step(HD, W), PS = kKv8Page / STEP;
     constexpr int PITCH = HD + 4;                            // (conflict-free 8-byte stores)
     constexpr int STATE = attn_kv8_state(HD);
     __shared__ __align__(16) union {
@@ -241,22 +259,47 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
     } sm;
     auto &s_o = sm.o;
     __shared__ float s_m[kAttnKv8Warps][8], s_l[kAttnKv8Warps][8];
-    __shared__ AttnKv8Join s_join[2];
-    __shared__ int s_last[2];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    constexpr int SHARES = kAttnKv8Warps / W;                // of a CTA
+    __shared__ AttnKv8Join s_joins[SHARES][2];
+    __shared__ int s_lasts[SHARES][2];
+    const int tid = threadIdx.x, warp = (tid >> 5) % W, mine = (tid >> 5) / W, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    auto &s_join = s_joins[mine];
+    auto &s_last = s_lasts[mine];
     const int KVH = p.c.KVH, G = p.H / KVH;
     const float nan = __int_as_float(0x7fc00000);
 
-    // this CTA's share lo .. hi of the list, and the row in which it begins: every warp for itself, 32 rows at a time
+    // this share lo .. hi of the list, and the row in which it begins: up to 32 rows by every warp for itself, more in 32 parts,
+    // 8 a warp (every warp all by itself took 94 us for 88 at 700 rows)
+    const bool many = p.n > 32;
+    const int deep = (p.n + 1023) / 1024;  // rows of a part / 32
+    __shared__ int s_part[32];
     int steps = 0, total = 0;
     bool idle = false;  // a row without a position (or a wrong one) that is this CTA's to write
-#pragma unroll 4
-    for (int i = lane; i - lane < p.n; i += 32) {
-        steps = i < p.n ? attn_kv8_row<STEP>(p, i).steps : 0;
-        if (i < p.n && steps == 0) idle = idle || (unsigned)i % gridDim.x == blockIdx.x;
-        total += __reduce_add_sync(0xffffffffu, steps);
+    auto steps_of = [&](int i) {
+        const int y = i < p.n ? attn_kv8_row<STEP>(p, i).steps : 0;
+        idle = idle || (i < p.n && y == 0 && (unsigned)i % gridDim.x == blockIdx.x);
+        return y;
+    };
+    if (many) {
+        int sums[8] = {};
+        const int at = (tid >> 5) * 8;
+        for (int d = 0; d < deep; ++d)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sums[k] += steps_of(((at + k) * deep + d) * 32 + lane);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            sums[k] = __reduce_add_sync(0xffffffffu, sums[k]);
+            if (lane == 0) s_part[at + k] = sums[k];
+        }
+        idle = __syncthreads_or(idle);
+        total = s_part[lane];
+    } else {
+        total = steps = steps_of(lane);
+        idle = __any_sync(0xffffffffu, idle);
     }
-    if (__any_sync(0xffffffffu, idle)) {
+    const int part = total;
+    total = __reduce_add_sync(0xffffffffu, total);
+    if (idle) {
         for (int i = blockIdx.x; i < p.n; i += gridDim.x) {
             const AttnKv8Row r = attn_kv8_row<STEP>(p, i);
             if (r.steps) continue;
@@ -270,29 +313,32 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
         }
     }
     total *= KVH;
-    const int ctas = min((int)gridDim.x, total), c = blockIdx.x;
-    if (c >= ctas) return;
-    const int share = total / ctas, more = total - share * ctas;  // the first `more` CTAs have one entry more
+    const int shares = min((int)gridDim.x * SHARES, total), c = blockIdx.x * SHARES + mine;
+    if (c >= shares) return;
+    const int share = total / shares, more = total - share * shares;  // the first `more` shares have one entry more
     const int lo = c * share + min(c, more), hi = lo + share + (c < more);
     int row = 0, base = 0;  // base: of the row's first entry
-    for (int i = lane, before = 0;; i += 32) {
-        if (p.n > 32) steps = i < p.n ? attn_kv8_row<STEP>(p, i).steps : 0;
-        int end = steps;
+    auto find = [&](int y) {  // the first lane whose end is behind lo (there is one); base: entries before it
+        int end = y;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, end, d);
-            if (lane >= d) end += y;
+            const int z = __shfl_up_sync(0xffffffffu, end, d);
+            if (lane >= d) end += z;
         }
-        const uint32_t behind = __ballot_sync(0xffffffffu, (before + end) * KVH > lo);
-        if (behind) {  // (lo < total: some row holds it)
-            row = i - lane + __ffs(behind) - 1;
-            base = (before + __shfl_sync(0xffffffffu, end - steps, __ffs(behind) - 1)) * KVH;
-            break;
-        }
-        before += __shfl_sync(0xffffffffu, end, 31);
+        const uint32_t behind = __ballot_sync(0xffffffffu, (base + end) * KVH > lo);
+        const int k = behind ? __ffs(behind) - 1 : 32;
+        base += __shfl_sync(0xffffffffu, behind ? end - y : end, behind ? k : 31);
+        return k;
+    };
+    if (many) {
+        row = find(part) * deep * 32;
+        for (int k = 32; k == 32; row += k) k = find(row + lane < p.n ? attn_kv8_row<STEP>(p, row + lane).steps : 0);
+    } else {
+        row = find(steps);
     }
-    if (tid < 2) s_join[tid].row = -1;
-    auto cta_of = [&](int x) {  // whose share entry x is
+    base *= KVH;
+    if (warp == 0 && lane == 0) s_join[0].row = s_join[1].row = -1;
+    auto share_of = [&](int x) {  // whose share entry x is
         const int big = more * (share + 1);
         return x < big ? x / (share + 1) : more + (x - big) / share;
     };
@@ -375,6 +421,10 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                 blk[u] = block_of(step_of(xa, u), u == 0);
                 load_k(step_of(xa, u), u);
             }
+            if constexpr (W == 1) {
+#pragma unroll
+                for (int u = 0; u < SUB; ++u) load_v(step_of(xa, u), u);
+            }
         }
         const uint16_t *qp = p.q + row * p.q_stride + (int64_t)(h * G + min(g, G - 1)) * HD;
 #pragma unroll
@@ -424,9 +474,12 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
 #pragma unroll 1
         for (int x = xa; x < xb; x += SUB) {
-            // these steps' values come while their scores are taken, the next ones' keys after that
+            // these steps' values come while their scores are taken, the next ones' keys after that (a warp's share has the first
+            // values come with the first keys, 700 rows: 78 -> 71 us with the parts above; a CTA's loses 2 % of a long row by it)
+            if constexpr (W > 1) {
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) load_v(step_of(x, u), u);
+                for (int u = 0; u < SUB; ++u) load_v(step_of(x, u), u);
+            }
             float s[SUB][NG][4];
 #pragma unroll
             for (int u = 0; u < SUB; ++u) {
@@ -544,24 +597,30 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                     }
                 }
             }
+            if (W == 1 && x + SUB < xb) {
+#pragma unroll
+                for (int u = 0; u < SUB; ++u) load_v(step_of(x + SUB, u), u);
+            }
         }
 
-        // the warps' states: o[j][e], o[j][2 + e]: head 2 t + e, dims hd / 8 g + 2 j and + 1, at place 16 j + 2 g
+        // this warp's state: o[j][e], o[j][2 + e]: head 2 t + e, dims hd / 8 g + 2 j and + 1, at place 16 j + 2 g
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) {
             l0 += __shfl_xor_sync(0xffffffffu, l0, d);
             l1 += __shfl_xor_sync(0xffffffffu, l1, d);
         }
-        if (g == 0) {
-            s_m[warp][2 * t] = m0;
-            s_m[warp][2 * t + 1] = m1;
-            s_l[warp][2 * t] = l0;
-            s_l[warp][2 * t + 1] = l1;
-        }
+        if constexpr (W > 1) {
+            if (g == 0) {
+                s_m[warp][2 * t] = m0;
+                s_m[warp][2 * t + 1] = m1;
+                s_l[warp][2 * t] = l0;
+                s_l[warp][2 * t + 1] = l1;
+            }
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-            *reinterpret_cast<float2 *>(&s_o[warp][2 * t][16 * j + 2 * g]) = make_float2(o[j][0] * vref, o[j][2] * vref);
-            *reinterpret_cast<float2 *>(&s_o[warp][2 * t + 1][16 * j + 2 * g]) = make_float2(o[j][1] * vref, o[j][3] * vref);
+            for (int j = 0; j < NT; ++j) {
+                *reinterpret_cast<float2 *>(&s_o[warp][2 * t][16 * j + 2 * g]) = make_float2(o[j][0] * vref, o[j][2] * vref);
+                *reinterpret_cast<float2 *>(&s_o[warp][2 * t + 1][16 * j + 2 * g]) = make_float2(o[j][1] * vref, o[j][3] * vref);
+            }
         }
         const AttnKv8Join me = {row, h, unit, unit + r.steps - 1};
         const bool begins = a == 0, whole = begins && b == r.steps;
@@ -574,48 +633,84 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             }
             begin(at);
         }
-        __syncthreads();
-        float *mine = p.part + (c * 2 + begins) * STATE;  // (a share begins in at most one unit that it does not begin)
-        for (int e = tid; e < G * HD / 2; e += kAttnKv8Threads) {
-            const int hh = e / (HD / 2), i = e % (HD / 2) * 2;
-            float M = s_m[0][hh], L = 0.f, y0 = 0.f, y1 = 0.f;
+        float *state = p.part + (c * 2 + begins) * STATE;  // (a share begins in at most one unit that it does not begin)
+        if constexpr (W == 1) {
 #pragma unroll
-            for (int w = 1; w < kAttnKv8Warps; ++w) M = fmaxf(M, s_m[w][hh]);
+            for (int e = 0; e < 2; ++e) {
+                const int hh = 2 * t + e;
+                const float M = e ? m1 : m0, L = e ? l1 : l0, inv = 1.f / L;
+                if (hh >= G) continue;
+                if (whole) {
+                    uint32_t y[NT];
 #pragma unroll
-            for (int w = 0; w < kAttnKv8Warps; ++w) {
-                const float2 y = *reinterpret_cast<const float2 *>(&s_o[w][hh][i]);
-                const float f = ex2(s_m[w][hh] - M);
-                L += f * s_l[w][hh];
-                y0 += f * y.x;
-                y1 += f * y.y;
+                    for (int j = 0; j < NT; ++j)
+                        y[j] = p.type == SARA_BF16 ? pack2<SARA_BF16>(o[j][e] * vref * inv, o[j][2 + e] * vref * inv)
+                                                   : pack2<SARA_FP16>(o[j][e] * vref * inv, o[j][2 + e] * vref * inv);
+                    uint32_t *out = reinterpret_cast<uint32_t *>(p.out + ((int64_t)me.row * p.H + me.h * G + hh) * HD + HD / 8 * g);
+#pragma unroll
+                    for (int j = 0; j < NT; j += 2) *reinterpret_cast<uint2 *>(out + j) = make_uint2(y[j], y[j + 1]);
+                    if (p.lse && g == 0) p.lse[(int64_t)me.row * p.H + me.h * G + hh] = (M - kAttnKv8Shift + log2f(L)) * 0.69314718f;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < NT; ++j)
+                        *reinterpret_cast<float2 *>(state + 16 + hh * HD + 16 * j + 2 * g) = make_float2(o[j][e] * vref, o[j][2 + e] * vref);
+                    if (g == 0) {
+                        state[hh] = M;
+                        state[8 + hh] = L;
+                    }
+                }
             }
-            if (whole) {
-                const float inv = 1.f / L;
-                attn_kv8_put<HD>(p, me.row, me.h * G + hh, i, y0 * inv, y1 * inv);
-                if (p.lse && i == 0) p.lse[(int64_t)me.row * p.H + me.h * G + hh] = (M - kAttnKv8Shift + log2f(L)) * 0.69314718f;
-            } else {
-                *reinterpret_cast<float2 *>(mine + 16 + hh * HD + i) = make_float2(y0, y1);
-                if (i == 0) {
-                    mine[hh] = M;
-                    mine[8 + hh] = L;
+        } else {
+            __syncthreads();
+            for (int e = tid; e < G * HD / 2; e += kAttnKv8Threads) {
+                const int hh = e / (HD / 2), i = e % (HD / 2) * 2;
+                float M = s_m[0][hh], L = 0.f, y0 = 0.f, y1 = 0.f;
+#pragma unroll
+                for (int w = 1; w < kAttnKv8Warps; ++w) M = fmaxf(M, s_m[w][hh]);
+#pragma unroll
+                for (int w = 0; w < kAttnKv8Warps; ++w) {
+                    const float2 y = *reinterpret_cast<const float2 *>(&s_o[w][hh][i]);
+                    const float f = ex2(s_m[w][hh] - M);
+                    L += f * s_l[w][hh];
+                    y0 += f * y.x;
+                    y1 += f * y.y;
+                }
+                if (whole) {
+                    const float inv = 1.f / L;
+                    attn_kv8_put<HD>(p, me.row, me.h * G + hh, i, y0 * inv, y1 * inv);
+                    if (p.lse && i == 0) p.lse[(int64_t)me.row * p.H + me.h * G + hh] = (M - kAttnKv8Shift + log2f(L)) * 0.69314718f;
+                } else {
+                    *reinterpret_cast<float2 *>(state + 16 + hh * HD + i) = make_float2(y0, y1);
+                    if (i == 0) {
+                        state[hh] = M;
+                        state[8 + hh] = L;
+                    }
                 }
             }
         }
-        if (!whole && tid == 0) s_join[begins] = {me.row, me.h, cta_of(me.c0), cta_of(me.c1)};
-        __syncthreads();  // (shared memory is the next unit's)
+        if (!whole && lane == 0 && warp == 0) s_join[begins] = {me.row, me.h, share_of(me.c0), share_of(me.c1)};
+        attn_kv8_sync<W>();  // (shared memory is the next unit's)
         if (at >= hi) break;
     }
     if (wrong) kv8_report(p.status);
 
-    // the units that other CTAs share: at most the one in which the share begins and the one in which it ends
-    if ((tid == 0 || tid == 32) && s_join[tid / 32].row >= 0) s_last[tid / 32] = AttnKv8Group<HD>(p, s_join[tid / 32], c).arrive();
-    __syncthreads();
+    // the units that other shares hold too: at most the one in which the share begins and the one in which it ends
+    const int who = W == 1 ? lane : lane == 0 ? warp : 2;
+    if (who < 2 && s_join[who].row >= 0) s_last[who] = AttnKv8Group<HD, W>(p, s_join[who], c).arrive();
+    attn_kv8_sync<W>();
 #pragma unroll 1
     for (int i = 0; i < 2; ++i)
-        if (s_join[i].row >= 0 && s_last[i]) attn_kv8_join<HD>({p, s_join[i], c}, sm.room, &s_last[i]);
+        if (s_join[i].row >= 0 && s_last[i])
+            attn_kv8_join<HD, W>({p, s_join[i], c}, sm.room + mine * (2 * kAttnKv8Batch * STATE / SHARES), &s_last[i], 32 * warp + lane);
 }
 
-inline size_t attn_kv8_count_bytes() { return kAttnKv8MaxCtas * 4 * sizeof(int); }
-inline size_t attn_kv8_workspace(int hd) { return attn_kv8_count_bytes() + (size_t)kAttnKv8MaxCtas * 2 * attn_kv8_state(hd) * sizeof(float); }
+inline int64_t attn_kv8_entries(int n, int kvh, int max_blocks, int step) { return (int64_t)n * kvh * max_blocks * (kKv8Page / step); }
+inline int attn_kv8_warps(int n, int kvh, int hd, int max_blocks) {
+    return (int64_t)n * kvh >= kAttnKv8Units && attn_kv8_entries(n, kvh, max_blocks, attn_kv8_step(hd, 1)) <= INT32_MAX ? 1 : kAttnKv8Warps;
+}
+inline size_t attn_kv8_count_bytes() { return kAttnKv8MaxShares * 2 * kAttnKv8Levels * sizeof(int); }
+inline size_t attn_kv8_workspace(int hd, int warps) {
+    return attn_kv8_count_bytes() + (size_t)kAttnKv8MaxShares / warps * 2 * attn_kv8_state(hd) * sizeof(float);
+}
 
 }  // namespace sara

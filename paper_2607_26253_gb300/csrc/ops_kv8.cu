@@ -100,7 +100,7 @@ int sara_kv8_read(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *pos
 
 size_t sara_attention_kv8_workspace_bytes(int32_t n_seq, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim) {
     if (n_seq < 1 || n_heads < 1 || n_kv_heads < 1 || head_dim < 1) return 0;
-    return attn_kv8_workspace(head_dim);
+    return attn_kv8_workspace(head_dim, attn_kv8_warps(n_seq, n_kv_heads, head_dim, 1));
 }
 
 int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_t n_heads, const void *q, int64_t q_stride,
@@ -113,7 +113,8 @@ int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
     if (q_stride % 8 || (n_seq > 1 && q_stride < (int64_t)n_heads * cache->head_dim)) return SARA_EINVAL;
     if ((int64_t)n_seq * n_heads > INT32_MAX) return SARA_EINVAL;
     return op_guard([&] {
-        if (workspace_bytes < attn_kv8_workspace(cache->head_dim)) throw SaraError(SARA_EINVAL, "workspace too small");
+        const int hd = cache->head_dim, warps = attn_kv8_warps(n_seq, cache->n_kv_heads, hd, cache->max_blocks);
+        if (workspace_bytes < attn_kv8_workspace(hd, warps)) throw SaraError(SARA_EINVAL, "workspace too small");
         AttnKv8Params p{};
         p.c = device_cache(cache);
         p.q = static_cast<const uint16_t *>(q);
@@ -131,11 +132,12 @@ int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
         p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)cache->head_dim));
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         // as many CTAs as fit, fewer where there are not as many entries
-        const int64_t entries = (int64_t)n_seq * cache->n_kv_heads * cache->max_blocks * (kKv8Page / attn_kv8_step(cache->head_dim));
+        const int64_t entries = attn_kv8_entries(n_seq, cache->n_kv_heads, cache->max_blocks, attn_kv8_step(hd, warps));
         if (entries > INT32_MAX) throw SaraError(SARA_EINVAL, "too many blocks");
-        const unsigned ctas = (unsigned)std::min<int64_t>(std::min(kAttnKv8SmCtas * sm_count(), kAttnKv8MaxCtas), entries);
+        const unsigned ctas = (unsigned)std::min<int64_t>(std::min(kAttnKv8SmCtas * sm_count(), kAttnKv8MaxCtas), (entries + kAttnKv8Warps / warps - 1) / (kAttnKv8Warps / warps));
         by_shape(cache, [&](auto hd, auto fmt) {
-            attn_kv8_kernel<hd.value, fmt.value><<<ctas, kAttnKv8Threads, 0, s>>>(p);
+            if (warps == 1) attn_kv8_kernel<hd.value, fmt.value, 1><<<ctas, kAttnKv8Threads, 0, s>>>(p);
+            else attn_kv8_kernel<hd.value, fmt.value, kAttnKv8Warps><<<ctas, kAttnKv8Threads, 0, s>>>(p);
         });
         CK(cudaGetLastError());
     });

@@ -231,9 +231,9 @@ def test_read(pkg, hd, kvh, fmt, typ):
 
 
 # ------------------------------------------------------------------------------------------------ attention
-def _check_attention(c, q, ctx, out, typ, first=None, lse=None):
+def _check_attention(c, q, ctx, out, typ, first=None, lse=None, chains=4):
     """Bounds: scores off by (hd + 4 + |s| terms) roundings of 32 bits of sum |q k| / sqrt(hd); probabilities in 21 bits or more
-    and multiples of 2^-32 of the maximum; sums of at most a quarter of the positions in a chain; the result rounded once."""
+    and multiples of 2^-32 of the maximum; sums of at most a quarter (1 / chains) of the positions in a chain; the result rounded once."""
     got, qn = out.double().cpu().numpy(), q.double().cpu().numpy()
     for i, n in enumerate(ctx):
         a = 0 if first is None else first[i]
@@ -241,7 +241,7 @@ def _check_attention(c, q, ctx, out, typ, first=None, lse=None):
         want, wl, mag, pv = oracle.attention(qn[i], k, v)
         ds = (c.hd + 8) * 2.0 ** -24 * mag[:, None]
         vmax = np.abs(v).max() if len(v) else 0.0
-        tol = HALF_STEP[typ] * np.abs(want) + (2 * ds + 2.0 ** -20 + (len(k) / 4 + 32) * 2.0 ** -24) * pv \
+        tol = HALF_STEP[typ] * np.abs(want) + (2 * ds + 2.0 ** -20 + (len(k) / chains + 32) * 2.0 ** -24) * pv \
             + max(1, len(k)) * 2.0 ** -32 * vmax + 2.0 ** -25
         ok = bool((np.abs(got[i] - want) <= tol).all())
         assert ok, (i, n, np.max(np.abs(got[i] - want) - tol))
@@ -250,7 +250,7 @@ def _check_attention(c, q, ctx, out, typ, first=None, lse=None):
             if n <= a:
                 assert (l == -np.inf).all()
             else:
-                assert (np.abs(l - wl) <= ds[:, 0] + (len(k) / 4 + 32) * 2.0 ** -24 + 2.0 ** -22 * (1 + np.abs(wl))).all()
+                assert (np.abs(l - wl) <= ds[:, 0] + (len(k) / chains + 32) * 2.0 ** -24 + 2.0 ** -22 * (1 + np.abs(wl))).all()
 
 
 def _q(rng, n, H, hd, typ, std=1.0):
@@ -304,6 +304,83 @@ def test_attention_lengths_and_rows(pkg, ctxs):
     for _ in range(3):  # the same bits again, from the same workspace
         import torch
         assert torch.equal(out, pkg.attention_decode_kv8(q, c.codes, c.scales, c.tab, _i32(ctxs), workspace=ws))
+
+
+def _shared_pages(c, rng, n, blocks):
+    """Another table for the cache: n rows of `blocks` of its pages, shared at random."""
+    c.table = rng.integers(0, c.codes.shape[0], (n, blocks)).astype(np.int32)
+    c.tab = _i32(c.table)
+
+
+# many rows, of all lengths, seen from 0 or from some position on: shares of a warp from 1,600 (row, KV head) pairs on, those of a CTA
+# below; rows counted by every warp for itself (up to 32) or in parts of 32 or 64
+@pytest.mark.parametrize("fmt,typ", [("e4m3", "bf16"), ("int8", "fp16")])
+@pytest.mark.parametrize("n,H,kvh,hd", [(1700, 6, 1, 128), (820, 16, 2, 64), (410, 12, 4, 32), (211, 64, 8, 128), (1600, 1, 1, 32), (1599, 1, 1, 32),
+                                        (2100, 3, 1, 64), (33, 4, 2, 64), (1025, 2, 1, 128)])
+def test_attention_many_rows(pkg, n, H, kvh, hd, fmt, typ):
+    import torch
+    rng = np.random.default_rng(n + hd)
+    c = Cache(pkg, rng, 20, 3, kvh, hd, fmt)
+    _shared_pages(c, rng, n, 6)
+    ctx = rng.choice(EDGES, n)
+    first = np.where(rng.random(n) < 0.5, 0, rng.integers(0, 300, n))
+    q, lse, status = _q(rng, n, H, hd, typ), torch.empty((n, H), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    ws = pkg.attention_kv8_workspace(n, H, kvh, hd)
+    for f in (None, first):
+        call = lambda: pkg.attention_decode_kv8(q, c.codes, c.scales, c.tab, _i32(ctx), first=None if f is None else _i32(f),  # noqa: E731
+                                                workspace=ws, lse=lse, status=status)
+        out = call()
+        assert int(status) == 0
+        _check_attention(c, q, ctx, out, typ, f, lse=lse, chains=1)
+        assert torch.equal(out, call())
+
+
+# one row that most of the shares hold, among many of one position: joins over three levels; the workspace then serves a batch of few rows
+@pytest.mark.parametrize("hd,long", [(128, 20000), (64, 60000), (32, 300)])
+def test_attention_one_long_row_among_many(pkg, hd, long):
+    import torch
+    rng = np.random.default_rng(hd)
+    n = 1700
+    c = Cache(pkg, rng, 1, 40, 1, hd, "e4m3")
+    _shared_pages(c, rng, n, -(-long // 128))
+    q, ws = _q(rng, n, 5, hd, "fp16"), pkg.attention_kv8_workspace(n, 5, 1, hd)
+    few, ctx = None, np.ones(n, dtype=np.int64)
+    for at in (900, 0, n - 1):
+        ctx[:] = 1
+        ctx[at] = long
+        out = pkg.attention_decode_kv8(q, c.codes, c.scales, c.tab, _i32(ctx), workspace=ws)
+        _check_attention(c, q, ctx, out, "fp16", chains=1)
+        assert torch.equal(out, pkg.attention_decode_kv8(q, c.codes, c.scales, c.tab, _i32(ctx), workspace=ws))
+        out = pkg.attention_decode_kv8(q[:3], c.codes, c.scales, c.tab[:3], _i32([long, 5, long]), workspace=ws)
+        if few is None:
+            _check_attention(c, q[:3], [long, 5, long], out, "fp16")
+            few = out
+        assert torch.equal(out, few)
+
+
+def test_attention_many_rows_some_of_them_wrong(pkg):
+    import torch
+    rng = np.random.default_rng(23)
+    n, H, kvh, hd = 900, 4, 2, 64
+    c = Cache(pkg, rng, 10, 4, kvh, hd, "int8")
+    _shared_pages(c, rng, n, 4)
+    q, ctx = _q(rng, n, H, hd, "bf16"), rng.integers(1, 513, n)
+    first = np.zeros(n)
+    table = c.table.copy()
+    ctx[[3, 500]] = [513, -1]
+    first[[77, 899]] = [-1, -2 ** 31]
+    ctx[[200, 640]] = 300
+    table[200, 2], table[640, 0] = -1, c.codes.shape[0]
+    table[300, 3], ctx[300] = 2 ** 31 - 1, 384  # (a page that is not read)
+    status, lse = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros((n, H), device="cuda")
+    out = pkg.attention_decode_kv8(q, c.codes, c.scales, _i32(table), _i32(ctx), first=_i32(first), lse=lse, status=status)
+    assert int(status) == pkg.SARA_EINVAL
+    right = np.ones(n, dtype=bool)
+    right[[3, 500, 77, 899, 200, 640]] = False
+    keep = torch.from_numpy(right).cuda()
+    assert torch.isnan(out[~keep]).all() and torch.isnan(lse[~keep]).all()
+    c.table = c.table[right]
+    _check_attention(c, q[keep], ctx[right], out[keep], "bf16", lse=lse[keep], chains=1)
 
 
 # scores that rise along the row (a maximum that moves), fall, or are large and far apart; values whose scales differ by 2^60
@@ -474,7 +551,7 @@ def test_rollouts_share_their_prompts_pages(pkg):
     _check_attention(c, q, [259] * n, pkg.attention_decode_kv8(q, c.codes, c.scales, c.tab, _i32([259] * n)), "bf16")
 
 
-@pytest.mark.parametrize("n", [1, 5, 700])
+@pytest.mark.parametrize("n", [1, 5, 700, 2000])
 def test_batches_without_a_position(pkg, n):
     import torch
     codes, scales = pkg.kv8_cache(4, 2, 64)
