@@ -12,6 +12,7 @@ from dataclasses import dataclass
 from .sara import SARA_EINVAL, SaraError, _check, load
 
 KV8_PAGE, KV8_SCALE = 128, 32   # positions of a cache block, and of a scale
+_MOST = 2 ** 31 - 1             # of anything that is counted (the C calls' int32)
 
 torch = None   # imported by the first call, as the rest of the package does
 _lib = None
@@ -78,6 +79,8 @@ def _kv8(codes, scales, table):
     stride, step = table.stride()
     if (step != 1 and blocks != 1) or (n > 1 and stride < blocks):
         _refuse("table must have rows of consecutive elements")
+    if n > _MOST or blocks > _MOST:
+        _refuse("table must have at most 2^31 - 1 rows and columns")
     if stride < blocks:
         stride = blocks
     return _pack_cache(codes.data_ptr(), scales.data_ptr(), table.data_ptr(), stride, nb, blocks, kvh, hd, fmt), n, kvh, hd, dev
@@ -112,6 +115,8 @@ def kv8_write(codes, scales, table, k, v, pos0, seq_start, status=None):
     total, typ = k.shape[0], _types.get(k.dtype, 2)
     if typ == 2 or v.dtype is not k.dtype:
         _refuse("k and v must both be bf16 or fp16")
+    if total > _MOST:
+        _refuse("k and v must have at most 2^31 - 1 rows")
     ks, vs = _tokens(k, total, kvh, hd, dev, "k"), _tokens(v, total, kvh, hd, dev, "v")
     at_pos, at_start = _vector(pos0, _int32, n, dev, "pos0"), _vector(seq_start, _int32, n + 1, dev, "seq_start")
     at_status = None if status is None else _vector(status, _int32, 1, dev, "status")
@@ -127,6 +132,8 @@ def kv8_read(codes, scales, table, pos0, seq_start, total: int, dtype=None, stat
     fp32), row seq_start[i] + j holding position pos0[i] + j of sequence i.  `out`: (k, v) to write into instead; rows
     of no sequence are left as they are there, and are not defined otherwise."""
     cache, n, kvh, hd, dev = _kv8(codes, scales, table)
+    if not 0 <= total <= _MOST:
+        _refuse("total must be 0 .. 2^31 - 1")
     at_pos, at_start = _vector(pos0, _int32, n, dev, "pos0"), _vector(seq_start, _int32, n + 1, dev, "seq_start")
     at_status = None if status is None else _vector(status, _int32, 1, dev, "status")
     if dev < 0 or dev != _device():
@@ -208,6 +215,8 @@ def _logits(z, what="logits"):
     row, step = z.stride()
     if step != 1 and V != 1:
         _refuse(f"{what} must have rows of consecutive elements")
+    if R > _MOST or V > _MOST:
+        _refuse(f"{what} must have at most 2^31 - 1 rows and columns")
     return typ, R, V, row, z.get_device()
 
 

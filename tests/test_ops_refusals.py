@@ -158,3 +158,20 @@ def test_binding_refuses_tensors_that_do_not_fit(pkg):
     _refused(pkg, pkg.logprobs_backward, z, i32(4), st, h, h[:1].expand(4), h)  # (not broadcast)
     _refused(pkg, pkg.logprobs_backward, z, i32(4), st, h, h, h, out=z.half())
     _refused(pkg, pkg.logprobs_backward, z, i32(4), st, h, h, h, out=z[:3])
+
+
+# counts that int32 does not hold are refused before a call could cut them short (tensors without memory)
+def test_binding_refuses_more_rows_than_the_calls_count(pkg):
+    many = 2 ** 32 + 5
+    codes, scales = pkg.kv8_cache(4, 2, 64, device="meta")
+    i32 = lambda *a: torch.empty(*a, dtype=torch.int32, device="meta")  # noqa: E731
+    assert "2^31" in _refused(pkg, pkg.kv8_read, codes, scales, i32(many, 1), i32(many), i32(many + 1), 5)
+    assert "2^31" in _refused(pkg, pkg.kv8_read, codes, scales, i32(3, 2), i32(3), i32(4), many)
+    assert "total" in _refused(pkg, pkg.kv8_read, codes, scales, i32(3, 2), i32(3), i32(4), -1)
+    k = torch.empty((many, 2, 64), dtype=torch.bfloat16, device="meta")
+    assert "2^31" in _refused(pkg, pkg.kv8_write, codes, scales, i32(3, 2), k, k, i32(3), i32(4))
+    for shape in ((1, many), (many, 1)):
+        z = torch.empty(shape, dtype=torch.bfloat16, device="meta")
+        assert "2^31" in _refused(pkg, pkg.logprobs, z, i32(shape[0]))
+        v = torch.empty(shape[0], device="meta")
+        assert "2^31" in _refused(pkg, pkg.logprobs_backward, z, i32(shape[0]), torch.empty((shape[0], 2), device="meta"), v, v)
