@@ -1,10 +1,10 @@
 // Decode attention over the 8-bit paged KV cache: one query row per sequence,
 //     out[i, h] = softmax(q[i, h] . K[first_i .. ctx_i)^T / sqrt(hd)) V[first_i .. ctx_i)
-// Bound by reading the codes once (2 hd bytes a position and KV head), so every byte goes from memory to registers in
-// the order in which the warp-level MMAs want it, 16 bytes a lane, and becomes fp16 there, which both
-// formats fit exactly; a warp takes 16 positions at a time (32 below 128 dims).
-//   - Scores: A = K (rows: positions), B = q^T (columns: the group's query heads, at most 8).  Lane (g, t) loads
-//     16 consecutive dims of positions g and g + 8; which dims meet in a k-step does not matter as long as q is laid out
+// Bound by reading the codes once (2 hd bytes a position and KV head).  They come by asynchronous copies into a ring in shared
+// memory, a warp's own, and become fp16 in registers, which both formats fit exactly; a warp takes 16 positions at a time (32 below
+// 128 dims).
+//   - Scores: A = K (rows: positions), B = q^T (columns: the group's query heads, at most 8).  Lane (g, t) takes
+//     16-byte pieces of positions g and g + 8; which dims meet in a k-step does not matter as long as q is laid out
 //     alike.  bf16 queries enter as fp16 after a power of two has brought the row's largest to 2^14.
 //   - Output: A = V^T (rows: dims, lane (g, t) holds hd / 8 dims of 4 positions, byte permutes pair the positions),
 //     B = P^T, the scores' own registers transposed by movmatrix.  P enters as an fp16 pair, hi + lo: 22 bits, and
@@ -12,17 +12,17 @@
 //   - A scale covers all of a warp's positions: K's is a factor of the scores, V's of P, relative to the largest so far
 //     (vref), so that neither costs a multiplication per code.
 // Online softmax in fp32 per warp; the maximum is re-based only when a probability would pass 2^8, so most steps
-// skip the column maximum and the rescale.  A step's values are asked for before its scores are taken, the next step's keys
-// over the used ones right after: 64 KB an SM are on their way (both ahead of a whole step: 179 us for 174 below).
-// Work: the (row, KV head, positions) triples in one list, cut into equal shares, one per CTA of 4 warps (4 an SM:
-// 8-warp CTAs on whole pages took 212 us for 174, since fewer units overlap where one ends), or per warp where there are many
-// rows (kAttnKv8Units); a unit's first loads are under way while the one before is put together.  A (row, KV head) that several
-// shares hold is joined by the last of them to finish, in the list's order (so results repeat bit for bit), by levels where there
-// are many.
-// Measured (kernel in a graph): 64 rows x 8,192 positions, 32 / 8 heads of 128: 171 us, 6.3 TB/s; 2 x 200,000, 16 / 2 heads: 48 us
-// (the steps end after 33 to 37, the two levels of joins take 10); 26 ragged rows of mean 758, 12 / 2 heads: 12 us and one row 7.6,
-// chains of latencies: share 0.7 us, first keys 1.1, step 0.5, state 0.9, arrival 0.7, join 2.5.  700 ragged rows of mean 200,
-// 32 / 8 heads: 71 us (44 at the copy's rate: the units are 13 steps of a warp, each begins with two exposed latencies).
+// skip the column maximum and the rescale.
+// The next step's copies are under way while a step is computed, across the ends of units: 64 KB an SM, which is enough, and more
+// is worse (64 x 8,192 positions: 166 us, with two steps ahead 177; a step in registers instead, its values asked for with its scores,
+// the next one's keys after them: 174, in int8 188 for 168).  Five CTAs an SM, whose 96 registers spill: 182.
+// Work: the (row, KV head, positions) triples in one list, cut into equal shares, one per CTA of 4 warps (4 an SM), or per warp
+// where there are many rows (kAttnKv8Units).  A (row, KV head) that several shares hold is joined by the last of them to finish,
+// in the list's order (so results repeat bit for bit), by levels where there are many.
+// Measured (kernel in a graph): 64 rows x 8,192 positions, 32 / 8 heads of 128: 166 us, 6.5 TB/s (350 x 4,000: 6.7); 2 x 200,000, 16 / 2
+// heads: 45 (the joins take 10); 26 ragged rows of mean 758, 12 / 2 heads: 12 us and one row 7.7, chains of latencies: share 0.7
+// us, first keys 1.1, step 0.5, state 0.9, arrival 0.7, join 2.5.  700 ragged rows of mean 200, 32 / 8 heads: 65 us (44 at the copy's
+// rate: 8 us until the first step and 5 of joins).
 #pragma once
 #include "kv8.cuh"
 
@@ -37,17 +37,25 @@ constexpr int kAttnKv8SmCtas = 16 / kAttnKv8Warps;
 constexpr int kAttnKv8MaxCtas = 160 * kAttnKv8SmCtas;
 constexpr int kAttnKv8MaxShares = kAttnKv8MaxCtas * kAttnKv8Warps;
 // (row, KV head) pairs from which each warp has a share of its own: nothing is put together between warps, but there are
-// four times the states to join.  8 KV heads of 128, us with a CTA's shares and a warp's: 600 pairs of 200 positions 16.3, 23.0;
-// 1,400: 28.2, 26.8 (of 4,000: 235, 239); 2,800: 49.5, 40.9 (464, 465); 5,600: 88.4, 70.7 (903, 918); of 64 and 32 dims from 1,400 on
-// 6 to 50 % in favour of the warps'
+// four times the states to join.  8 KV heads of 128, us with a CTA's shares and a warp's: 1,040 pairs of 200 positions 23.7, 28.7 (of
+// 4,000: 170, 172); 1,400: 29.4, 28.1 (223, 225); 2,000: 37.0, 33.4 (313, 313); 5,600: 87.6, 64.8 (847, 842); 64 and 32 dims alike
 constexpr int kAttnKv8Units = 1600;
 constexpr int kAttnKv8Levels = 3;                               // of joins
-constexpr int kAttnKv8Group = 16;                               // states joined at a time (2 x 200,000: 48.0 us; 8 49.0, 32 49.5, 64 53.2)
+constexpr int kAttnKv8Group = 16;                               // states joined at a time (2 x 200,000: 48.0 us at the time; 8 49.0, 32 49.5, 64 53.2)
 constexpr int kAttnKv8Batch = 4;                                // of them to a copy, two copies in shared memory
+// Stages of a warp's ring (32 dims, whose stages are half as large, 64 rows x 16,384: 98 us, 106 with two)
+__host__ __device__ constexpr int attn_kv8_stages(int hd) { return hd == 32 ? 3 : 2; }
 constexpr float kAttnKv8Shift = 7.f;                            // log2 of the probabilities' scale
 
 // Floats of a state: max and sum of 8 heads, then their outputs
 __host__ __device__ constexpr int attn_kv8_state(int hd) { return 8 * (hd + 2); }
+
+// Bytes of a warp's ring of keys and values, which is also its part of the joins' room, and of a CTA's with their scales
+__host__ __device__ constexpr int attn_kv8_ring(int hd) {
+    const int ring = attn_kv8_stages(hd) * 2 * attn_kv8_positions(hd) * hd, room = 2 * kAttnKv8Batch / kAttnKv8Warps * attn_kv8_state(hd) * 4;
+    return ring > room ? ring : room;
+}
+__host__ __device__ constexpr int attn_kv8_smem(int hd) { return kAttnKv8Warps * (attn_kv8_ring(hd) + attn_kv8_stages(hd) * 16); }
 
 struct AttnKv8Params {
     Kv8Cache c;
@@ -85,13 +93,16 @@ __device__ __forceinline__ void decode4_half(uint32_t w, uint32_t &lo, uint32_t 
     }
 }
 template <int WORDS>
-__device__ __forceinline__ void load_codes(const uint8_t *p, uint32_t *r) {
+__device__ __forceinline__ void load_codes(uint32_t p, uint32_t *r) {  // from shared memory
     if constexpr (WORDS == 4)
-        asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "l"(p));
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(p) : "memory");
     else if constexpr (WORDS == 2)
-        asm("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "r"(p) : "memory");
     else
-        asm("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(r[0]) : "l"(p));
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(r[0]) : "r"(p) : "memory");
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void *src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
 // A row's positions, and the steps of the list that hold them
@@ -248,16 +259,9 @@ template <int HD, int FMT, int W>
 __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kernel(AttnKv8Params p) {
     constexpr int KW = HD / 16, VW = HD / 32, NT = HD / 16;  // words a lane of a key row, of a value row; output tiles
     constexpr int KL = KW < 4 ? KW : 4;                      // words a load
-    // Steps at a time: 32 dims leave registers for two (64 rows x 16,384: 121 -> 105 us, int8 131 -> 115; 512 positions 12.3 -> 12.7)
-    constexpr int SUB = HD == 32 ? 2 : 1;
     constexpr int POS = attn_kv8_positions(HD), NG = POS / 16, STEP = attn_kv8_step(HD, W), PS = kKv8Page / STEP;
-    constexpr int PITCH = HD + 4;                            // (conflict-free 8-byte stores)
     constexpr int STATE = attn_kv8_state(HD);
-    __shared__ __align__(16) union {
-        float o[kAttnKv8Warps][8][PITCH];     // the warps' outputs
-        float room[2 * kAttnKv8Batch * STATE];  // states that are joined
-    } sm;
-    auto &s_o = sm.o;
+    __shared__ int s_free[kAttnKv8Warps];
     __shared__ float s_m[kAttnKv8Warps][8], s_l[kAttnKv8Warps][8];
     constexpr int SHARES = kAttnKv8Warps / W;                // of a CTA
     __shared__ AttnKv8Join s_joins[SHARES][2];
@@ -343,89 +347,97 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
         return x < big ? x / (share + 1) : more + (x - big) / share;
     };
 
-    AttnKv8Row r = attn_kv8_row<STEP>(p, row);
-    int h = 0, a = 0, b = 0, unit = 0, xa = 0, xb = 0;  // entries unit + a .. unit + b: of the row, for KV head h
-    const int32_t *tab = nullptr;
-    int ids = 0, idbase = 0;  // this lane's entry of the 32 table entries from idbase on
+    // This warp's ring, and what its loads, which run ahead of the sums, are about
+    constexpr int S = attn_kv8_stages(HD), TILE = POS * HD, CHUNKS = HD / 16, LC = TILE / 16 / 32, RING = attn_kv8_ring(HD);
+    extern __shared__ __align__(128) uint8_t s_ring[];
+    static_assert(2 * TILE >= 8 * HD * 4, "a stage holds a warp's sums");
+    static_assert(RING % 128 == 0, "lines");
+    const uint32_t ring = smem_u32(s_ring) + (tid >> 5) * RING;
+    const uint32_t ring_s = smem_u32(s_ring) + kAttnKv8Warps * RING + (tid >> 5) * (S * 16);
+    AttnKv8Row r = attn_kv8_row<STEP>(p, row), lr = r;
+    int h = (lo - base) / r.steps, unit = base + h * r.steps;  // KV head; the first entry of the (row, KV head)
+    int l_row = row, l_h = h - 1, l_unit = unit - r.steps, l_x = 0, l_end = 0, fill = 0;
+    // this warp's steps of a unit in this share, x .. end: of a step x it has positions STEP x + POS warp .. + POS - 1, the row's
+    // first and last step may have none of them
+    auto range = [&](const AttnKv8Row &r, int unit, int &x, int &end) {
+        x = r.step0 + max(lo - unit, 0);
+        end = r.step0 + min(r.steps, hi - unit);
+        if (r.first - x * STEP >= POS * (warp + 1)) ++x;
+        if ((end - 1) * STEP + POS * warp >= r.ctx) --end;
+    };
+    int ids = 0, idbase = -32;  // this lane's entry of the 32 table entries from idbase on
     bool wrong = false;
-    auto block_of = [&](int x, bool begin) {
-        const int page = x / PS;
-        if (begin || page - idbase >= 32) {
-            idbase = page;
-            ids = (page + lane) * PS < xb ? __ldg(tab + page + lane) : 0;
-            const bool out = ids < 0 || ids >= p.c.n_blocks;
-            wrong = wrong || out;
-            ids = out ? -1 : ids;
+    // Where 16 bytes of a tile stand: rows fill lines of 128 bytes, whose eight pieces are exchanged so that the lanes that read at a time
+    // meet all banks
+    auto place = [&](int pos, int chunk, bool value) {
+        const int line = pos * CHUNKS / 8, piece = pos * CHUNKS % 8 + chunk;
+        const int x = HD == 128 ? (value ? line & 6 : (line & 1) * 4) : HD == 64 ? (line & 3) * 2 : (line & 1) * 2;
+        return line * 128 + (piece ^ x) * 16;
+    };
+    // this lane's 16 bytes, and those 512 bytes further on, of keys and values (whose places change sides from row 4 to row 4 at 128 dims)
+    const uint32_t put = place(lane / CHUNKS, lane % CHUNKS, false), put_v = TILE + place(lane / CHUNKS, lane % CHUNKS, true);
+    const int64_t v_behind = (int64_t)KVH * (kKv8Page * HD);
+    auto load = [&]() {
+        while (l_x >= l_end && l_unit + lr.steps < hi) {  // the next unit that has something for this warp
+            l_unit += lr.steps;
+            if (++l_h == KVH) {
+                l_h = 0;
+                do lr = attn_kv8_row<STEP>(p, ++l_row);
+                while (lr.steps == 0);
+                idbase = -32;
+            }
+            range(lr, l_unit, l_x, l_end);
         }
-        return __shfl_sync(0xffffffffu, ids, page - idbase);
-    };
-    const int lane_k = (KW == 8 ? 16 : HD / 4) * t, lane_v = HD / 8 * g;
-    auto step_of = [&](int x, int u) { return u == 0 ? x : min(x + u, xb - 1); };  // (behind the last step that step again, masked)
-    auto edge = [&](int x) {  // whether some of its positions are masked
-        const int p0 = x * STEP + POS * warp;
-        return p0 < r.first || p0 > r.ctx - POS;
-    };
-    auto slot_of = [&](int x, int e) {  // (masked positions stand for the nearest that is not: their probability is 0)
-        return min(max(x * STEP + POS * warp + e, r.first), r.ctx - 1) & (kKv8Page - 1);
-    };
-    auto block_in_page = [&](int x) { return (x % PS * STEP + POS * warp) / kKv8Block; };
-    uint32_t kr[SUB][2 * NG][KW], vr[SUB][4 * NG][VW];  // positions g + 8 e; 2 t + (e & 1) + 8 (e >> 1)
-    float ks[SUB], vs[SUB];
-    int blk[SUB] = {};
-    auto load_k = [&](int x, int u) {
-        const int64_t tile = kv8_tile(p.c, max(blk[u], 0), 0, h);
-        ks[u] = blk[u] < 0 ? nan : __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
-        const uint8_t *k = p.c.codes + tile * (kKv8Page * HD) + lane_k;
-        if (!edge(x)) {
-            k += (x % PS * STEP + POS * warp + g) * HD;
+        if (l_x < l_end) {
+            const int page = l_x / PS;
+            if ((unsigned)(page - idbase) >= 32u) {  // (a row's next head finds them here where there are not many)
+                idbase = page;
+                ids = (page + lane) * PS < lr.step0 + lr.steps ? __ldg(p.c.table + l_row * p.c.table_stride + page + lane) : 0;
+                const bool out = ids < 0 || ids >= p.c.n_blocks;
+                wrong = wrong || out;
+                ids = out ? -1 : ids;
+            }
+            const int block = __shfl_sync(0xffffffffu, ids, page - idbase), p0 = l_x * STEP + POS * warp;
+            const uint32_t to = ring + put + fill * (2 * TILE), to_v = ring + put_v + fill * (2 * TILE), to_s = ring_s + fill * 16;
+            const uint32_t to_v1 = HD == 128 ? to_v ^ 64 : to_v;
+            if (block >= 0) {
+                const int64_t tile = kv8_tile(p.c, block, 0, l_h);
+                const uint8_t *src = p.c.codes + (tile * kKv8Page + (p0 & (kKv8Page - 1))) * HD + 16 * lane, *src_v = src + v_behind;
+                if (p0 >= lr.first && p0 <= lr.ctx - POS) {
 #pragma unroll
-            for (int e = 0; e < 2 * NG; ++e)
-#pragma unroll
-                for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + 8 * e * HD + 64 * i, &kr[u][e][4 * i]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 2 * NG; ++e)
-#pragma unroll
-                for (int i = 0; i < KW / KL; ++i) load_codes<KL>(k + slot_of(x, g + 8 * e) * HD + 64 * i, &kr[u][e][4 * i]);
+                    for (int i = 0; i < LC; ++i) {
+                        cp_async16(to + 512 * i, src + 512 * i);
+                        cp_async16(i & 1 ? to_v1 + 512 * i : to_v + 512 * i, src_v + 512 * i);
+                    }
+                } else {  // masked positions stand for the nearest that is not: their probability is 0
+#pragma unroll 1
+                    for (int i = 0; i < LC; ++i) {
+                        const int at = lane / CHUNKS + i * (32 / CHUNKS), off = (min(max(p0 + at, lr.first), lr.ctx - 1) - p0 - lane / CHUNKS) * HD;
+                        cp_async16(to + 512 * i, src + off);
+                        cp_async16(i & 1 ? to_v1 + 512 * i : to_v + 512 * i, src_v + off);
+                    }
+                }
+                if (lane < 2) cp_async4(to_s + 4 * lane, p.c.scales + (tile + lane * KVH) * kKv8PageBlocks + (p0 & (kKv8Page - 1)) / kKv8Block);
+            } else if (lane < 2) {
+                asm volatile("st.shared.f32 [%0], %1;" ::"r"(to_s + 4 * lane), "f"(nan) : "memory");
+            }
+            ++l_x;
         }
+        cp_async_commit();
+        fill = fill == S - 1 ? 0 : fill + 1;
     };
-    auto load_v = [&](int x, int u) {
-        const int64_t tile = kv8_tile(p.c, max(blk[u], 0), 1, h);
-        vs[u] = __ldg(p.c.scales + tile * kKv8PageBlocks + block_in_page(x));
-        const uint8_t *v = p.c.codes + tile * (kKv8Page * HD) + lane_v;
-        if (!edge(x)) {
-            v += (x % PS * STEP + POS * warp + 2 * t) * HD;
-#pragma unroll
-            for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(v + ((e & 1) + 8 * (e >> 1)) * HD, vr[u][e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(v + slot_of(x, 2 * t + (e & 1) + 8 * (e >> 1)) * HD, vr[u][e]);
-        }
-    };
+    int xa = 0, xb = 0, take = 0;
+#pragma unroll 1
+    for (int i = 0; i < S - 1; ++i) load();
+    uint32_t at_k[2], at_v[2];  // this lane's places in a tile
+    at_k[0] = place(g, KW == 2 ? t / 2 : t, false) + (KW == 2 ? t % 2 * 8 : 0);
+    at_k[1] = at_k[0] ^ 64;  // (128 dims: the dims from 64 on)
+    at_v[0] = place(2 * t, HD == 128 ? g : HD == 64 ? g / 2 : g / 4, true) + (HD == 128 ? 0 : HD == 64 ? g % 2 * 8 : g % 4 * 4);
+    at_v[1] = HD == 128 ? at_v[0] + 128 : HD == 64 ? at_v[0] ^ 64 : at_v[0] ^ 32;
     // queries: head g of the group, the dims of this lane's key words
     uint32_t qb[KW][2];
-    auto begin = [&](int at) {  // the unit of entry `at`; its first keys and its queries are on their way
-        h = (at - base) / r.steps;
-        unit = base + h * r.steps;
-        a = at - unit;
-        b = min(r.steps, hi - unit);
-        // this warp's positions of step x: STEP x + POS warp .. + POS - 1; the row's first and last step may have none
-        xa = r.step0 + a;
-        xb = r.step0 + b;
-        if (xa * STEP + POS * (warp + 1) <= r.first) ++xa;
-        if ((xb - 1) * STEP + POS * warp >= r.ctx) --xb;
-        tab = p.c.table + row * p.c.table_stride;
-        if (xa < xb) {
-#pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                blk[u] = block_of(step_of(xa, u), u == 0);
-                load_k(step_of(xa, u), u);
-            }
-            if constexpr (W == 1) {
-#pragma unroll
-                for (int u = 0; u < SUB; ++u) load_v(step_of(xa, u), u);
-            }
-        }
+    auto begin = [&]() {
+        range(r, unit, xa, xb);
         const uint16_t *qp = p.q + row * p.q_stride + (int64_t)(h * G + min(g, G - 1)) * HD;
 #pragma unroll
         for (int s = 0; s < KW; ++s) {
@@ -436,8 +448,8 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
         }
     };
 
-    begin(lo);
-    for (int at = lo;;) {
+    begin();
+    for (;;) {
         float mul0, mul1;  // from MMA sums to base-2 exponents, heads 2 t and 2 t + 1
         {
 #pragma unroll
@@ -473,65 +485,54 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[j][e] = 0.f;
 #pragma unroll 1
-        for (int x = xa; x < xb; x += SUB) {
-            // these steps' values come while their scores are taken, the next ones' keys after that (a warp's share has the first
-            // values come with the first keys, 700 rows: 78 -> 71 us with the parts above; a CTA's loses 2 % of a long row by it)
-            if constexpr (W > 1) {
+        for (int x = xa; x < xb; ++x) {
+            cp_async_wait<S - 2>();
+            __syncwarp();  // (every lane's copies have come, and every lane has left the stage that is filled next)
+            load();
+            const uint32_t from = ring + take * (2 * TILE), from_s = ring_s + take * 16;
+            take = take == S - 1 ? 0 : take + 1;
+            float ks, vsc;
+            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(ks), "=f"(vsc) : "r"(from_s) : "memory");
+            uint32_t kr[2 * NG][KW];  // positions g + 8 e
 #pragma unroll
-                for (int u = 0; u < SUB; ++u) load_v(step_of(x, u), u);
-            }
-            float s[SUB][NG][4];
+            for (int e = 0; e < 2 * NG; ++e)
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                const float f0 = ks[u] * mul0, f1 = ks[u] * mul1;
+                for (int i = 0; i < KW / KL; ++i) load_codes<KL>(from + at_k[i] + 8 * e * HD, &kr[e][4 * i]);
+            uint32_t vr[4 * NG][VW];  // positions 2 t + (e & 1) + 8 (e >> 1)
 #pragma unroll
-                for (int n = 0; n < NG; ++n) {
-                    float s2[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int e = 0; e < 4 * NG; ++e) load_codes<VW>(from + TILE + at_v[e & 1] + 8 * (e >> 1) * HD, vr[e]);
+            float s[NG][4];
+            const float f0 = ks * mul0, f1 = ks * mul1;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[u][n][e] = 0.f;
+            for (int n = 0; n < NG; ++n) {
+                float s2[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int i = 0; i < KW; ++i) {
-                        uint32_t f[4];
-                        decode4_half<FMT>(kr[u][2 * n][i], f[0], f[2]);
-                        decode4_half<FMT>(kr[u][2 * n + 1][i], f[1], f[3]);
-                        mma_f16_16816(i & 1 ? s2 : s[u][n], f, qb[i][0], qb[i][1]);
-                    }
-                    // s[u][n][0], [1]: position 16 n + g, heads 2 t and 2 t + 1; [2], [3]: position 16 n + g + 8
+                for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[u][n][e] = (s[u][n][e] + s2[e]) * (e & 1 ? f1 : f0);
+                for (int i = 0; i < KW; ++i) {
+                    uint32_t f[4];
+                    decode4_half<FMT>(kr[2 * n][i], f[0], f[2]);
+                    decode4_half<FMT>(kr[2 * n + 1][i], f[1], f[3]);
+                    mma_f16_16816(i & 1 ? s2 : s[n], f, qb[i][0], qb[i][1]);
                 }
-            }
-            float vsc[SUB];
-            bool cut[SUB];
+                // s[n][0], s[n][1]: position 16 n + g, heads 2 t and 2 t + 1; s[n][2], s[n][3]: position 16 n + g + 8
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                vsc[u] = vs[u];
-                cut[u] = edge(x + u);
-            }
-            if (x + SUB < xb) {
-#pragma unroll
-                for (int u = 0; u < SUB; ++u) {
-                    blk[u] = block_of(step_of(x + SUB, u), false);
-                    load_k(step_of(x + SUB, u), u);
-                }
+                for (int e = 0; e < 4; ++e) s[n][e] = (s[n][e] + s2[e]) * (e & 1 ? f1 : f0);
             }
             float t0 = -INFINITY, t1 = -INFINITY;
-#pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                const bool none = u > 0 && x + u >= xb;
-                if (none || cut[u]) {
-#pragma unroll
-                    for (int n = 0; n < NG; ++n) {
-                        const int p0 = (x + u) * STEP + POS * warp + 16 * n + g;
-                        if (none || p0 < r.first || p0 >= r.ctx) s[u][n][0] = s[u][n][1] = -INFINITY;
-                        if (none || p0 + 8 < r.first || p0 + 8 >= r.ctx) s[u][n][2] = s[u][n][3] = -INFINITY;
-                    }
-                }
+            const int p0 = x * STEP + POS * warp;
+            if (p0 < r.first || p0 > r.ctx - POS) {  // some are masked
 #pragma unroll
                 for (int n = 0; n < NG; ++n) {
-                    t0 = fmaxf(t0, fmaxf(s[u][n][0], s[u][n][2]));
-                    t1 = fmaxf(t1, fmaxf(s[u][n][1], s[u][n][3]));
+                    const int at = p0 + 16 * n + g;
+                    if (at < r.first || at >= r.ctx) s[n][0] = s[n][1] = -INFINITY;
+                    if (at + 8 < r.first || at + 8 >= r.ctx) s[n][2] = s[n][3] = -INFINITY;
                 }
+            }
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+                t0 = fmaxf(t0, fmaxf(s[n][0], s[n][2]));
+                t1 = fmaxf(t1, fmaxf(s[n][1], s[n][3]));
             }
             if (__any_sync(0xffffffffu, t0 > m0 + 8.f || t1 > m1 + 8.f)) {
                 float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
@@ -554,52 +555,45 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                 }
             }
             const float c0 = m0 - kAttnKv8Shift, c1 = m1 - kAttnKv8Shift;
+            if (!(vsc <= vref)) {  // the largest scale so far (or NaN)
+                const float inv = 1.f / vsc, f = vref * inv;
+                vref = vsc;
+                vinv = inv;
 #pragma unroll
-            for (int u = 0; u < SUB; ++u) {
-                if (!(vsc[u] <= vref)) {  // the largest scale so far (or NaN)
-                    const float inv = 1.f / vsc[u], f = vref * inv;
-                    vref = vsc[u];
-                    vinv = inv;
+                for (int j = 0; j < NT; ++j)
 #pragma unroll
-                    for (int j = 0; j < NT; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[j][e] *= f;
-                }
-                const float vf = vsc[u] * vinv;
-#pragma unroll
-                for (int n = 0; n < NG; ++n) {
-                    float w0 = ex2(s[u][n][0] - c0), w1 = ex2(s[u][n][1] - c1), w2 = ex2(s[u][n][2] - c0), w3 = ex2(s[u][n][3] - c1);
-                    l0 += w0 + w2;
-                    l1 += w1 + w3;
-                    w0 *= vf;
-                    w1 *= vf;
-                    w2 *= vf;
-                    w3 *= vf;
-                    uint32_t ph[2] = {pack_half2(w0, w1), pack_half2(w2, w3)}, pl[2];
-                    const float2 h0 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[0]));
-                    const float2 h1 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[1]));
-                    pl[0] = movmatrix_trans(pack_half2(w0 - h0.x, w1 - h0.y));
-                    pl[1] = movmatrix_trans(pack_half2(w2 - h1.x, w3 - h1.y));
-                    ph[0] = movmatrix_trans(ph[0]);
-                    ph[1] = movmatrix_trans(ph[1]);
-#pragma unroll
-                    for (int i = 0; i < VW; ++i) {
-                        uint32_t v0[4], v1[4];  // dims 4 i, 4 i + 1 and 4 i + 2, 4 i + 3 of the lane's
-                        const uint32_t a = vr[u][4 * n][i], b = vr[u][4 * n + 1][i], c = vr[u][4 * n + 2][i], d = vr[u][4 * n + 3][i];
-                        decode4_half<FMT>(__byte_perm(a, b, 0x5140), v0[0], v0[1]);
-                        decode4_half<FMT>(__byte_perm(c, d, 0x5140), v0[2], v0[3]);
-                        decode4_half<FMT>(__byte_perm(a, b, 0x7362), v1[0], v1[1]);
-                        decode4_half<FMT>(__byte_perm(c, d, 0x7362), v1[2], v1[3]);
-                        mma_f16_16816(o[2 * i], v0, ph[0], ph[1]);
-                        mma_f16_16816(o[2 * i + 1], v1, ph[0], ph[1]);
-                        mma_f16_16816(o[2 * i], v0, pl[0], pl[1]);
-                        mma_f16_16816(o[2 * i + 1], v1, pl[0], pl[1]);
-                    }
-                }
+                    for (int e = 0; e < 4; ++e) o[j][e] *= f;
             }
-            if (W == 1 && x + SUB < xb) {
+            const float vf = vsc * vinv;
 #pragma unroll
-                for (int u = 0; u < SUB; ++u) load_v(step_of(x + SUB, u), u);
+            for (int n = 0; n < NG; ++n) {
+                float w0 = ex2(s[n][0] - c0), w1 = ex2(s[n][1] - c1), w2 = ex2(s[n][2] - c0), w3 = ex2(s[n][3] - c1);
+                l0 += w0 + w2;
+                l1 += w1 + w3;
+                w0 *= vf;
+                w1 *= vf;
+                w2 *= vf;
+                w3 *= vf;
+                uint32_t ph[2] = {pack_half2(w0, w1), pack_half2(w2, w3)}, pl[2];
+                const float2 h0 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[0]));
+                const float2 h1 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[1]));
+                pl[0] = movmatrix_trans(pack_half2(w0 - h0.x, w1 - h0.y));
+                pl[1] = movmatrix_trans(pack_half2(w2 - h1.x, w3 - h1.y));
+                ph[0] = movmatrix_trans(ph[0]);
+                ph[1] = movmatrix_trans(ph[1]);
+#pragma unroll
+                for (int i = 0; i < VW; ++i) {
+                    uint32_t v0[4], v1[4];  // dims 4 i, 4 i + 1 and 4 i + 2, 4 i + 3 of the lane's
+                    const uint32_t a = vr[4 * n][i], b = vr[4 * n + 1][i], c = vr[4 * n + 2][i], d = vr[4 * n + 3][i];
+                    decode4_half<FMT>(__byte_perm(a, b, 0x5140), v0[0], v0[1]);
+                    decode4_half<FMT>(__byte_perm(c, d, 0x5140), v0[2], v0[3]);
+                    decode4_half<FMT>(__byte_perm(a, b, 0x7362), v1[0], v1[1]);
+                    decode4_half<FMT>(__byte_perm(c, d, 0x7362), v1[2], v1[3]);
+                    mma_f16_16816(o[2 * i], v0, ph[0], ph[1]);
+                    mma_f16_16816(o[2 * i + 1], v1, ph[0], ph[1]);
+                    mma_f16_16816(o[2 * i], v0, pl[0], pl[1]);
+                    mma_f16_16816(o[2 * i + 1], v1, pl[0], pl[1]);
+                }
             }
         }
 
@@ -609,29 +603,23 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             l0 += __shfl_xor_sync(0xffffffffu, l0, d);
             l1 += __shfl_xor_sync(0xffffffffu, l1, d);
         }
-        if constexpr (W > 1) {
-            if (g == 0) {
-                s_m[warp][2 * t] = m0;
-                s_m[warp][2 * t + 1] = m1;
-                s_l[warp][2 * t] = l0;
-                s_l[warp][2 * t + 1] = l1;
-            }
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                *reinterpret_cast<float2 *>(&s_o[warp][2 * t][16 * j + 2 * g]) = make_float2(o[j][0] * vref, o[j][2] * vref);
-                *reinterpret_cast<float2 *>(&s_o[warp][2 * t + 1][16 * j + 2 * g]) = make_float2(o[j][1] * vref, o[j][3] * vref);
-            }
+        if (W > 1 && g == 0) {
+            s_m[warp][2 * t] = m0;
+            s_m[warp][2 * t + 1] = m1;
+            s_l[warp][2 * t] = l0;
+            s_l[warp][2 * t + 1] = l1;
+            if (t == 0) s_free[warp] = fill;
         }
         const AttnKv8Join me = {row, h, unit, unit + r.steps - 1};
-        const bool begins = a == 0, whole = begins && b == r.steps;
-        at = unit + b;
-        if (at < hi) {  // the next unit's loads, while this one is put together
-            if (h == KVH - 1) {
-                base += KVH * r.steps;
+        const bool begins = unit >= lo, last = unit + r.steps >= hi, whole = begins && unit + r.steps <= hi;
+        if (!last) {  // the next unit's queries come while this one is put together
+            unit += r.steps;
+            if (++h == KVH) {
+                h = 0;
                 do r = attn_kv8_row<STEP>(p, ++row);
                 while (r.steps == 0);
             }
-            begin(at);
+            begin();
         }
         float *state = p.part + (c * 2 + begins) * STATE;  // (a share begins in at most one unit that it does not begin)
         if constexpr (W == 1) {
@@ -661,7 +649,20 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                 }
             }
         } else {
+            // put together by way of the warps' free stages, [8 heads][hd places]: conflict-free with places exchanged by eights
+            auto at_of = [&](int w, int stage, int hh, int i) {
+                return reinterpret_cast<float2 *>(s_ring + w * RING + stage * (2 * TILE)) + (hh * HD + (i ^ (hh / 2 * 8))) / 2;
+            };
+            __syncwarp();  // (every lane has left the stage)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                *at_of(warp, fill, 2 * t, 16 * j + 2 * g) = make_float2(o[j][0] * vref, o[j][2] * vref);
+                *at_of(warp, fill, 2 * t + 1, 16 * j + 2 * g) = make_float2(o[j][1] * vref, o[j][3] * vref);
+            }
             __syncthreads();
+            int stage[kAttnKv8Warps];
+#pragma unroll
+            for (int w = 0; w < kAttnKv8Warps; ++w) stage[w] = s_free[w];
             for (int e = tid; e < G * HD / 2; e += kAttnKv8Threads) {
                 const int hh = e / (HD / 2), i = e % (HD / 2) * 2;
                 float M = s_m[0][hh], L = 0.f, y0 = 0.f, y1 = 0.f;
@@ -669,7 +670,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                 for (int w = 1; w < kAttnKv8Warps; ++w) M = fmaxf(M, s_m[w][hh]);
 #pragma unroll
                 for (int w = 0; w < kAttnKv8Warps; ++w) {
-                    const float2 y = *reinterpret_cast<const float2 *>(&s_o[w][hh][i]);
+                    const float2 y = *at_of(w, stage[w], hh, i);
                     const float f = ex2(s_m[w][hh] - M);
                     L += f * s_l[w][hh];
                     y0 += f * y.x;
@@ -690,7 +691,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
         }
         if (!whole && lane == 0 && warp == 0) s_join[begins] = {me.row, me.h, share_of(me.c0), share_of(me.c1)};
         attn_kv8_sync<W>();  // (shared memory is the next unit's)
-        if (at >= hi) break;
+        if (last) break;
     }
     if (wrong) kv8_report(p.status);
 
@@ -701,7 +702,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
 #pragma unroll 1
     for (int i = 0; i < 2; ++i)
         if (s_join[i].row >= 0 && s_last[i])
-            attn_kv8_join<HD, W>({p, s_join[i], c}, sm.room + mine * (2 * kAttnKv8Batch * STATE / SHARES), &s_last[i], 32 * warp + lane);
+            attn_kv8_join<HD, W>({p, s_join[i], c}, reinterpret_cast<float *>(s_ring + mine * RING), &s_last[i], 32 * warp + lane);
 }
 
 inline int64_t attn_kv8_entries(int n, int kvh, int max_blocks, int step) { return (int64_t)n * kvh * max_blocks * (kKv8Page / step); }

@@ -136,8 +136,9 @@ int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
         if (entries > INT32_MAX) throw SaraError(SARA_EINVAL, "too many blocks");
         const unsigned ctas = (unsigned)std::min<int64_t>(std::min(kAttnKv8SmCtas * sm_count(), kAttnKv8MaxCtas), (entries + kAttnKv8Warps / warps - 1) / (kAttnKv8Warps / warps));
         by_shape(cache, [&](auto hd, auto fmt) {
-            if (warps == 1) attn_kv8_kernel<hd.value, fmt.value, 1><<<ctas, kAttnKv8Threads, 0, s>>>(p);
-            else attn_kv8_kernel<hd.value, fmt.value, kAttnKv8Warps><<<ctas, kAttnKv8Threads, 0, s>>>(p);
+            const auto kern = warps == 1 ? attn_kv8_kernel<hd.value, fmt.value, 1> : attn_kv8_kernel<hd.value, fmt.value, kAttnKv8Warps>;
+            static_assert(attn_kv8_smem(hd.value) <= 48 * 1024, "more would have to be asked for");
+            kern<<<ctas, kAttnKv8Threads, attn_kv8_smem(hd.value), s>>>(p);
         });
         CK(cudaGetLastError());
     });
