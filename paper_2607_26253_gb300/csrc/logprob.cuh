@@ -7,7 +7,7 @@
 // logits come so fast that the instructions per logit count, so they are taken two at a time and in base 2:
 //   e^(z - m) = 2^(z log2(e) - r) 2^-c,  r = m log2(e) as rounded, c what the rounding took: one fused operation a logit,
 // and c, the same for all, is put right once, in log S.  Sums in fp32 against the thread's own running maximum.
-// Scores of 2,048 x 151,936 in bf16: 92 us, 6.1 TB/s (rows end in waves: three and a tail); with 8 alternatives 115; 26 rows with
+// Scores of 2,048 x 151,936 in bf16: 89 us, 6.3 TB/s (rows end in waves); with 8 alternatives 115; 26 rows with
 // 8 alternatives 9.9, 5.4 without: the bound on them, their ranks and the cluster's join are latencies.
 #pragma once
 #include "device_common.cuh"
@@ -140,6 +140,7 @@ struct ScoreParams {
     int32_t *top_token;
     float *top_logprob;
     int ctas;  // a row
+    int turn;  // 1: the grid of the last rows may start when this one's CTAs all have; 2: the grid of the last rows; 0: alone
 };
 
 // ------------------------------------------------------------------------------- alternatives
@@ -316,6 +317,7 @@ __global__ void __launch_bounds__(WARPS > 1 ? 32 * WARPS : 256, score_sm_ctas(TY
     __shared__ __align__(8) uint32_t c_sums[3][kScoreMaxCtas], c_key[TOP ? kScoreMaxCtas * 32 : 1][2];  // (rank 0) the cluster's
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = threadIdx.x % STEP;
     const bool cluster = WARPS > 1 && p.ctas > 1;
+    if (p.turn == 1) pdl_allow_dependents();
     if (cluster) cluster_arrive();  // (waited for before the stores into rank 0's shared memory)
     const int64_t r64 = WARPS > 1 ? (int64_t)(blockIdx.x / (unsigned)p.ctas) : (int64_t)blockIdx.x * 8 + warp;
     const int rank = WARPS > 1 ? (int)(blockIdx.x % (unsigned)p.ctas) : 0;
@@ -476,6 +478,7 @@ __global__ void __launch_bounds__(WARPS > 1 ? 32 * WARPS : 256, score_sm_ctas(TY
         }
         if (warp != 0) return;
     }
+    if (p.turn == 2) pdl_wait_prior_grids();  // (so that who waits for these rows waits for the others too)
     const bool none = a.s == 0.f;  // every logit is -inf
     const float m = pad ? 0.f : none ? -INFINITY : a.m, ls = none ? 0.f : fmaf(-kLn2, ScoreSums<TYPE>::carry(a.m), logf(a.s));
     if (lane == 0) {
@@ -496,6 +499,9 @@ __global__ void __launch_bounds__(WARPS > 1 ? 32 * WARPS : 256, score_sm_ctas(TY
 // that fill the SMs lose by it: 2,048 x 151,936 96 us in one CTA each, 102 in two, 163 in eight).  Many rows take a warp each up to
 // 512 vectors, 4 warps up to 8,192 (8,192 x 8,192: 31 us, 43 with 8 warps; 4,096 x 50,304: 66, 72), 8 warps beyond
 // (3,000 x 151,936: 131 us, 140 with 4).  The alternatives' bound wants the 256 threads.
+// Where the last of the waves in which long rows end would leave more than half of the SMs' room empty, its rows are split over 2 or 4
+// CTAs and start as the others end (2,048 x 151,936: 93 -> 89 us, 700 42 -> 36, 900 52 -> 44; 1,300, whose rows of padding leave
+// no third wave, 57 -> 60; with 8 CTAs 95; with alternatives, whose bound costs each CTA its own, 114 -> 116, so not there).
 template <int TYPE, bool TOP>
 inline void launch_score(cudaStream_t s, int sms, ScoreParams p) {
     const int vectors = p.V / (TYPE == SARA_FP32 ? 4 : 8);
@@ -510,6 +516,25 @@ inline void launch_score(cudaStream_t s, int sms, ScoreParams p) {
         if (p.ctas == 1 && vectors <= 8192) {
             score_kernel<TYPE, false, 4><<<(unsigned)p.R, 128, 0, s>>>(p);
             CK(cudaGetLastError());
+            return;
+        }
+    }
+    if constexpr (!TOP) {
+        const int wave = score_sm_ctas(TYPE, false, 8) * sms, last = p.R % wave;
+        if (p.ctas == 1 && vectors > 8192 && p.R > wave && last > 0 && 2 * last <= wave) {
+            p.turn = 1;
+            p.R -= last;
+            launch_cluster(s, false, dim3((unsigned)p.R), dim3(256), 0, 1, score_kernel<TYPE, false, 8>, p);
+            const int64_t r = p.R;
+            p.z = static_cast<const uint8_t *>(p.z) + r * p.stride * RowVectors<TYPE>::kSize;
+            p.tokens += p.tokens ? r : 0;
+            p.logprob += p.logprob ? r : 0;
+            p.entropy += p.entropy ? r : 0;
+            p.stats += p.stats ? 2 * r : 0;
+            p.turn = 2;
+            p.R = last;
+            p.ctas = last * 4 <= wave ? 4 : 2;
+            launch_cluster(s, true, dim3((unsigned)p.R * p.ctas), dim3(256), 0, (unsigned)p.ctas, score_kernel<TYPE, false, 8>, p);
             return;
         }
     }

@@ -28,7 +28,7 @@ int sara_logprobs(const void *logits, int64_t row_stride, int32_t type, int32_t 
     if ((logprob && !tokens) || (top > 0 && (!top_token || !top_logprob))) return SARA_EINVAL;
     if (!logits_ok(logits, row_stride, type, R, V)) return SARA_EINVAL;
     return op_guard([&] {
-        const ScoreParams p{logits, row_stride, R, V, top, tokens, logprob, entropy, stats, top_token, top_logprob, 1};
+        const ScoreParams p{logits, row_stride, R, V, top, tokens, logprob, entropy, stats, top_token, top_logprob, 1, 0};
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         const int sms = sm_count();
         auto launch = [&](auto t) {

@@ -109,6 +109,36 @@ def test_kernels_by_size(pkg, R, V, typ, top):
     _check(pkg.LogProbs(*[pick(x) for x in (o.logprob, o.entropy, o.stats, o.top_token, o.top_logprob)]), pick(z), tok[keep], top)
 
 
+# long rows that fill the SMs and some more: the last ones are taken by 2 or 4 CTAs each, in a grid that starts while the others end
+@pytest.mark.parametrize("R,V,typ", [(700, 70001, "bf16"), (860, 33001, "fp32"), (912, 65552, "fp16"), (913, 65552, "fp16")])
+def test_last_rows_of_many_long_ones(pkg, R, V, typ):
+    import torch
+    rng = np.random.default_rng(R)
+    gen = torch.Generator("cuda").manual_seed(R)
+    z = torch.empty((R, V), device="cuda").normal_(0.0, 3.0, generator=gen).to(_dtype(typ))
+    tok = rng.integers(0, V, R)
+    tok[::11] = -1
+    tok[R - 1], tok[R - 3] = 5, V
+    keep = np.concatenate([rng.permutation(608)[:20], np.arange(606, 612), np.arange(R - 20, R)])
+    o = pkg.logprobs(z, _i32(tok))
+    pick = lambda x: x[_i32(keep).long()] if x is not None else None  # noqa: E731
+    _check(pkg.LogProbs(*[pick(x) for x in (o.logprob, o.entropy, o.stats, None, None)]), pick(z), tok[keep], 0)
+    p = pkg.logprobs(z, None)
+    live = _i32(tok).ge(0)
+    assert p.logprob is None and torch.equal(p.entropy[live], o.entropy[live]) and torch.equal(p.stats[live], o.stats[live])
+    # captured, with a kernel behind it that reads what both grids wrote
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    dtok = _i32(tok)
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=s):
+        c = pkg.logprobs(z, dtok)
+        both = c.logprob + c.entropy
+    for _ in range(5):
+        both.zero_()
+        graph.replay()
+        assert torch.equal(both.nan_to_num(7.0), (o.logprob + o.entropy).nan_to_num(7.0))
+
+
 def test_no_rows(pkg):
     import torch
     z, none = torch.empty((0, 50), device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda")
