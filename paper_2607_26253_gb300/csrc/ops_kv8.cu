@@ -113,6 +113,8 @@ int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
     if (q_stride % 8 || (n_seq > 1 && q_stride < (int64_t)n_heads * cache->head_dim)) return SARA_EINVAL;
     if ((int64_t)n_seq * n_heads > INT32_MAX) return SARA_EINVAL;
     return op_guard([&] {
+        // (counts of entries, at most two a block and CTA, in 32 bits)
+        if ((int64_t)n_seq * cache->n_kv_heads > (((int64_t)1 << 30) - 1) / cache->max_blocks) throw SaraError(SARA_EINVAL, "too many blocks");
         const int hd = cache->head_dim, warps = attn_kv8_warps(n_seq, cache->n_kv_heads, hd, cache->max_blocks);
         if (workspace_bytes < attn_kv8_workspace(hd, warps)) throw SaraError(SARA_EINVAL, "workspace too small");
         AttnKv8Params p{};
@@ -133,7 +135,6 @@ int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
         cudaStream_t s = static_cast<cudaStream_t>(stream);
         // as many CTAs as fit, fewer where there are not as many entries
         const int64_t entries = attn_kv8_entries(n_seq, cache->n_kv_heads, cache->max_blocks, attn_kv8_step(hd, warps));
-        if (entries > INT32_MAX) throw SaraError(SARA_EINVAL, "too many blocks");
         const unsigned ctas = (unsigned)std::min<int64_t>(std::min(kAttnKv8SmCtas * sm_count(), kAttnKv8MaxCtas), (entries + kAttnKv8Warps / warps - 1) / (kAttnKv8Warps / warps));
         by_shape(cache, [&](auto hd, auto fmt) {
             const auto kern = warps == 1 ? attn_kv8_kernel<hd.value, fmt.value, 1> : attn_kv8_kernel<hd.value, fmt.value, kAttnKv8Warps>;

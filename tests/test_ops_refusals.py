@@ -63,6 +63,8 @@ def test_attention_refusals(lib):
                 dict(out=None), dict(out=A + 8), dict(typ=2), dict(typ=-1), dict(ws=None), dict(ws=A + 8), dict(nbytes=0), dict(n=1 << 28, H=16)):
         assert call(**bad) == -1, bad
     assert call(n=0) == 0 and call(n=0, cache=_cache(table=0)) == 0
+    for n, blocks in ((64, 1 << 23), (1 << 29, 1), (1 << 27, 4)):  # 2^30 blocks and heads of them
+        assert call(n=n, H=2, cache=_cache(max_blocks=blocks, table_stride=blocks)) == -1
     # a workspace that was laid out for fewer rows is enough only where the larger batch wants no more
     size = [lib.sara_attention_kv8_workspace_bytes(n, 8, 2, 64) for n in (1, 50, 799, 800, 5000)]
     assert size == sorted(size) and size[0] == size[2] < size[3] == size[4]
