@@ -518,8 +518,6 @@ inline void launch_score(cudaStream_t s, int sms, ScoreParams p) {
             CK(cudaGetLastError());
             return;
         }
-    }
-    if constexpr (!TOP) {
         const int wave = score_sm_ctas(TYPE, false, 8) * sms, last = p.R % wave;
         if (p.ctas == 1 && vectors > 8192 && p.R > wave && last > 0 && 2 * last <= wave) {
             p.turn = 1;
