@@ -6,7 +6,8 @@
 // bf16 174, 6.8).  The scores read them once, 16 bytes a lane, a step's loads in flight during the one before; 16-bit
 // logits come so fast that the instructions per logit count, so they are taken two at a time and in base 2:
 //   e^(z - m) = 2^(z log2(e) - r) 2^-c,  r = m log2(e) as rounded, c what the rounding took: one fused operation a logit,
-// and c, the same for all, is put right once, in log S.  Sums in fp32 against the thread's own running maximum.
+// and c, the same for all, is put right once, in log S.  Sums in fp32 against the thread's own running maximum.  c is half a step of r
+// at most: 1/16 up to |m| = 10^6, but 440 at 10^10 (a mask's usual values), where 2^c has no room.  Larger maxima take z - m first, logit by logit.
 // Scores of 2,048 x 151,936 in bf16: 89 us, 6.3 TB/s (rows end in waves); with 8 alternatives 115; 26 rows with
 // 8 alternatives 9.9, 5.4 without: the bound on them, their ranks and the cluster's join are latencies.
 #pragma once
@@ -206,13 +207,13 @@ __device__ __forceinline__ float warp_nth_largest(float v, int top) {
 }
 
 // ------------------------------------------------------------------------------- sums
-// Maximum m, s = sum 2^(z log2(e) - r), t = sum 2^y y with y that exponent.  Where m log2(e) has no room in fp32 (or logits below m
-// none in their type), r is exact and logits are taken one by one.
+// Maximum m, s = sum 2^(z log2(e) - r), t = sum 2^y y with y that exponent.  Where m is so large that c would count (or logits below m
+// have no room in their type), r is exact (c = 0) and logits are taken one by one.
 template <int TYPE>
 struct ScoreSums {
     static constexpr uint32_t kLeast = TYPE == SARA_FP32 ? 0xfe967699u : TYPE == SARA_BF16 ? 0xfe96fe96u : 0xfbfffbffu;  // -1e38; fp16: its lowest
     float m = -3.4028235e38f, s = 0.f, t = 0.f;
-    static __device__ __forceinline__ bool plain(float m) { return fabsf(m) < 1e37f && (TYPE != SARA_FP16 || m > -6e4f); }
+    static __device__ __forceinline__ bool plain(float m) { return fabsf(m) < 1e6f && (TYPE != SARA_FP16 || m > -6e4f); }
     static __device__ __forceinline__ float carry(float m) { return plain(m) ? fmaf(m, kLog2e, -(m * kLog2e)) : 0.f; }  // c
     // to a maximum n >= m.  (The bound keeps 0 times infinity out where the maxima are that far apart.)
     __device__ __forceinline__ void rebase(float n) {

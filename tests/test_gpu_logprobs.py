@@ -236,6 +236,56 @@ def test_large_and_peaked_logits(pkg, mean, std):
     _check_grad(pkg.logprobs_backward(z, _i32(tok), o.stats, o.entropy, g, gh), z, tok, g, gh)
 
 
+# Masks of finite values, from ones that rounding just reaches to the type's far end, and logits as large: all but three tokens, most of the
+# row in one piece (so that threads begin with nothing else), all of it, at random, or two fills in one row.  The sizes take each kernel: a warp,
+# 4 warps, a cluster, 8 warps a row, with and without alternatives, the last rows split over CTAs.
+FILLS = [-1e6, -3e6, -1e9, -1e10, -1e15, -1e20, -1e30, -1e36, 1e10, 1e20, 1e30]
+FILLS_FP16 = [-1e3, -1e4, -3e4, -59904.0, -60032.0, -6.2e4, -65504.0, 1e4, 3e4, 6e4, 65504.0]
+
+
+def _filled(rng, R, V, typ, r0=0):
+    """Rows r0 .. r0 + R of logits N(0, 3), each with its fill and its pattern."""
+    z = 3.0 * rng.standard_normal((R, V))
+    fills = FILLS_FP16 if typ == "fp16" else FILLS
+    for r in range(R):
+        fill, pattern = fills[(r0 + r) % len(fills)], (r0 + r) // len(fills) % 5
+        keep = np.zeros(V, bool)
+        if pattern == 0:
+            keep[rng.permutation(V)[:3]] = True
+        elif pattern == 1:
+            keep[V - V // 10:] = True
+        elif pattern == 3:
+            keep = rng.random(V) < 0.1
+        elif pattern == 4:
+            keep[:V // 20] = True
+        z[r, ~keep] = fill
+        if pattern == 4:
+            z[r, V // 2:] = fills[(r0 + r + 3) % len(fills)]
+    import torch
+    return torch.from_numpy(z).to(_dtype(typ)).cuda()
+
+
+@pytest.mark.parametrize("typ", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("R,V,top", [(55, 300, 0), (55, 2001, 0), (55, 2001, 5), (55, 8191, 0), (55, 8191, 8), (55, 40007, 0), (55, 40007, 32), (1, 151936, 0),
+                                     (640, 5003, 0), (640, 9001, 7), (609, 70001, 0)])
+def test_finite_masks(pkg, R, V, top, typ):
+    import torch
+    rng = np.random.default_rng(R + V)
+    live = min(R, 55)  # (the rest: other rows' company, rows of padding)
+    z = torch.zeros((R, V), dtype=_dtype(typ), device="cuda")
+    at = np.sort(rng.permutation(R)[:live])
+    at[-1] = R - 1
+    z[_i32(at).long()] = _filled(rng, live, V, typ, 3 if R == 1 else 0)
+    tok = np.full(R, -1)
+    tok[at] = rng.integers(0, V, live)
+    o = pkg.logprobs(z, _i32(tok), top=top)
+    pick = lambda x: x[_i32(at).long()].contiguous() if x is not None else None  # noqa: E731
+    _check(pkg.LogProbs(*[pick(x) for x in (o.logprob, o.entropy, o.stats, o.top_token, o.top_logprob)]), pick(z), tok[at], top)
+    g, gh = (torch.from_numpy(rng.standard_normal(R)).float().cuda() for _ in range(2))
+    y = pkg.logprobs_backward(z, _i32(tok), o.stats, o.entropy, g, gh)
+    _check_grad(pick(y), pick(z), tok[at], pick(g), pick(gh))
+
+
 def test_padding_wrong_tokens_and_no_tokens(pkg):
     import torch
     rng = np.random.default_rng(6)
