@@ -7,12 +7,13 @@
 //     16-byte pieces of positions g and g + 8; which dims meet in a k-step does not matter as long as q is laid out
 //     alike.  bf16 queries enter as fp16 after a power of two has brought the row's largest to 2^14.
 //   - Output: A = V^T (rows: dims, lane (g, t) holds hd / 8 dims of 4 positions, byte permutes pair the positions),
-//     B = P^T, the scores' own registers transposed by movmatrix.  P enters as an fp16 pair, hi + lo: 22 bits, and
-//     multiples of 2^-31 of the maximum (probabilities are scaled by 2^7).
-//   - A scale covers all of a warp's positions: K's is a factor of the scores, V's of P, relative to the largest so far
-//     (vref), so that neither costs a multiplication per code.
-// Online softmax in fp32 per warp; the maximum is re-based only when a probability would pass 2^8, so most steps
-// skip the column maximum and the rescale.
+//     B = P^T, the scores' own registers transposed by movmatrix.
+//   - A scale covers all of a warp's positions: K's is a factor of the scores, V's of P, so that neither costs a multiplication
+//     per code.  P times V's scale enters as an fp16 pair, hi + lo: 22 bits, or within 2^-31 of the largest such product of the head
+//     so far.  A power of two of the head's own, r, brings that one to 2^6 .. 2^7, so that a block of large values without weight does not
+//     push out the small values that have it.
+// Online softmax in fp32 per warp; the maximum and r are re-based only when a probability or a product would pass 2^8 of them, so most
+// steps skip the column maximum and the rescale.
 // The next step's copies are under way while a step is computed, across the ends of units: 64 KB an SM, which is enough, and more
 // is worse (64 x 8,192 positions: 166 us, with two steps ahead 177; a step in registers instead, its values asked for with its scores,
 // the next one's keys after them: 174, in int8 188 for 168).  Five CTAs an SM, whose 96 registers spill: 182.
@@ -74,6 +75,11 @@ struct AttnKv8Params {
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float min_nan(float a, float b) {  // the smaller; a NaN stays
+    float y;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
     return y;
 }
 // Four codes as two fp16 pairs
@@ -479,7 +485,8 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             mul1 = __shfl_sync(0xffffffffu, mul, 8 * t + 4);
         }
 
-        float m0 = -3.4028235e38f, m1 = m0, l0 = 0.f, l1 = 0.f, vref = 0.f, vinv = 0.f, o[NT][4];
+        // o: sums of probability times scale times r times code
+        float m0 = -3.4028235e38f, m1 = m0, l0 = 0.f, l1 = 0.f, r0 = 1.f, r1 = 1.f, o[NT][4];
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
@@ -519,7 +526,6 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[n][e] = (s[n][e] + s2[e]) * (e & 1 ? f1 : f0);
             }
-            float t0 = -INFINITY, t1 = -INFINITY;
             const int p0 = x * STEP + POS * warp;
             if (p0 < r.first || p0 > r.ctx - POS) {  // some are masked
 #pragma unroll
@@ -529,23 +535,44 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                     if (at + 8 < r.first || at + 8 >= r.ctx) s[n][2] = s[n][3] = -INFINITY;
                 }
             }
+            float w[NG][4], t0 = 0.f, t1 = 0.f;
+            auto probabilities = [&]() {
+#pragma unroll
+                for (int n = 0; n < NG; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[n][e] = ex2(s[n][e] - ((e & 1 ? m1 : m0) - kAttnKv8Shift));
+            };
+            probabilities();
 #pragma unroll
             for (int n = 0; n < NG; ++n) {
-                t0 = fmaxf(t0, fmaxf(s[n][0], s[n][2]));
-                t1 = fmaxf(t1, fmaxf(s[n][1], s[n][3]));
+                t0 = fmaxf(t0, fmaxf(w[n][0], w[n][2]));
+                t1 = fmaxf(t1, fmaxf(w[n][1], w[n][3]));
             }
-            if (__any_sync(0xffffffffu, t0 > m0 + 8.f || t1 > m1 + 8.f)) {
-                float n0 = fmaxf(m0, t0), n1 = fmaxf(m1, t1);
+            float g0 = vsc * r0, g1 = vsc * r1;
+            constexpr float kMost = (float)(1 << (int)(kAttnKv8Shift + 8.f));
+            if (__any_sync(0xffffffffu, t0 * fmaxf(fabsf(g0), 1.f) > kMost || t1 * fmaxf(fabsf(g1), 1.f) > kMost)) {
+                float n0 = s[0][0], n1 = s[0][1];
+#pragma unroll
+                for (int n = 0; n < NG; ++n) {
+                    n0 = fmaxf(n0, fmaxf(s[n][0], s[n][2]));
+                    n1 = fmaxf(n1, fmaxf(s[n][1], s[n][3]));
+                }
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) {
                     n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, d));
                     n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, d));
                 }
-                const float a0 = ex2(m0 - n0), a1 = ex2(m1 - n1);
-                m0 = n0;
-                m1 = n1;
-                l0 *= a0;
-                l1 *= a1;
+                // to the larger maximum, and to the larger of the step's products and those so far, whose logarithm -log2(r) is
+                const float v = (float)scale_exp(vsc);
+                auto rebase = [&](float n, float &m, float &r, float &l) {
+                    const float up = fmaxf(m, n), down = m - up, was = (float)-scale_exp(r) + down;
+                    const float k = fminf(fmaxf(ceilf(fmaxf(was, n - up + v)), -126.f), 126.f);
+                    m = up;
+                    r = pow2f(-(int)k);
+                    l *= ex2(down);
+                    return ex2(was - k);
+                };
+                const float a0 = rebase(n0, m0, r0, l0), a1 = rebase(n1, m1, r1, l1);
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
                     o[j][0] *= a0;
@@ -553,27 +580,18 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                     o[j][2] *= a0;
                     o[j][3] *= a1;
                 }
+                probabilities();
+                g0 = vsc * r0;
+                g1 = vsc * r1;
             }
-            const float c0 = m0 - kAttnKv8Shift, c1 = m1 - kAttnKv8Shift;
-            if (!(vsc <= vref)) {  // the largest scale so far (or NaN)
-                const float inv = 1.f / vsc, f = vref * inv;
-                vref = vsc;
-                vinv = inv;
-#pragma unroll
-                for (int j = 0; j < NT; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[j][e] *= f;
-            }
-            const float vf = vsc * vinv;
+            // (an infinite factor, which only probabilities of 0 have left here, is to leave them 0; a NaN stays)
+            g0 = min_nan(g0, 3.4028235e38f);
+            g1 = min_nan(g1, 3.4028235e38f);
 #pragma unroll
             for (int n = 0; n < NG; ++n) {
-                float w0 = ex2(s[n][0] - c0), w1 = ex2(s[n][1] - c1), w2 = ex2(s[n][2] - c0), w3 = ex2(s[n][3] - c1);
-                l0 += w0 + w2;
-                l1 += w1 + w3;
-                w0 *= vf;
-                w1 *= vf;
-                w2 *= vf;
-                w3 *= vf;
+                l0 += w[n][0] + w[n][2];
+                l1 += w[n][1] + w[n][3];
+                const float w0 = w[n][0] * g0, w1 = w[n][1] * g1, w2 = w[n][2] * g0, w3 = w[n][3] * g1;
                 uint32_t ph[2] = {pack_half2(w0, w1), pack_half2(w2, w3)}, pl[2];
                 const float2 h0 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[0]));
                 const float2 h1 = __half22float2(*reinterpret_cast<const __half2 *>(&ph[1]));
@@ -621,19 +639,20 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             }
             begin();
         }
+        const float u0 = pow2f(-scale_exp(r0)), u1 = pow2f(-scale_exp(r1));  // 1 / r
         float *state = p.part + (c * 2 + begins) * STATE;  // (a share begins in at most one unit that it does not begin)
         if constexpr (W == 1) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int hh = 2 * t + e;
-                const float M = e ? m1 : m0, L = e ? l1 : l0, inv = 1.f / L;
+                const float M = e ? m1 : m0, L = e ? l1 : l0, u = e ? u1 : u0, inv = 1.f / L;
                 if (hh >= G) continue;
                 if (whole) {
                     uint32_t y[NT];
 #pragma unroll
                     for (int j = 0; j < NT; ++j)
-                        y[j] = p.type == SARA_BF16 ? pack2<SARA_BF16>(o[j][e] * vref * inv, o[j][2 + e] * vref * inv)
-                                                   : pack2<SARA_FP16>(o[j][e] * vref * inv, o[j][2 + e] * vref * inv);
+                        y[j] = p.type == SARA_BF16 ? pack2<SARA_BF16>(o[j][e] * u * inv, o[j][2 + e] * u * inv)
+                                                   : pack2<SARA_FP16>(o[j][e] * u * inv, o[j][2 + e] * u * inv);
                     uint32_t *out = reinterpret_cast<uint32_t *>(p.out + ((int64_t)me.row * p.H + me.h * G + hh) * HD + HD / 8 * g);
 #pragma unroll
                     for (int j = 0; j < NT; j += 2) *reinterpret_cast<uint2 *>(out + j) = make_uint2(y[j], y[j + 1]);
@@ -641,7 +660,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                 } else {
 #pragma unroll
                     for (int j = 0; j < NT; ++j)
-                        *reinterpret_cast<float2 *>(state + 16 + hh * HD + 16 * j + 2 * g) = make_float2(o[j][e] * vref, o[j][2 + e] * vref);
+                        *reinterpret_cast<float2 *>(state + 16 + hh * HD + 16 * j + 2 * g) = make_float2(o[j][e] * u, o[j][2 + e] * u);
                     if (g == 0) {
                         state[hh] = M;
                         state[8 + hh] = L;
@@ -656,8 +675,8 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             __syncwarp();  // (every lane has left the stage)
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                *at_of(warp, fill, 2 * t, 16 * j + 2 * g) = make_float2(o[j][0] * vref, o[j][2] * vref);
-                *at_of(warp, fill, 2 * t + 1, 16 * j + 2 * g) = make_float2(o[j][1] * vref, o[j][3] * vref);
+                *at_of(warp, fill, 2 * t, 16 * j + 2 * g) = make_float2(o[j][0] * u0, o[j][2] * u0);
+                *at_of(warp, fill, 2 * t + 1, 16 * j + 2 * g) = make_float2(o[j][1] * u1, o[j][3] * u1);
             }
             __syncthreads();
             int stage[kAttnKv8Warps];

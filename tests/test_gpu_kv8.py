@@ -407,6 +407,45 @@ def test_attention_moving_maximum_and_scales(pkg, kind, fmt):
     _check_attention(c, q, [1000, 1024], out, "bf16")
 
 
+# Blocks of values with a large scale and next to no weight, first or in the middle of what a warp sees, among blocks that hold the weight
+# with scales 2^24 to 2^100 smaller (or 2^200, where the others' weight of 2^-392 is nothing beside it); shares of a CTA and of a warp.
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("n,blocks", [(160, 8), (1700, 4), (3, 30)])
+@pytest.mark.parametrize("part", [0, 2])
+@pytest.mark.parametrize("apart", [24, 40, 60, 100, 200])
+def test_attention_values_of_large_scales_without_weight(pkg, apart, part, n, blocks, fmt):
+    import torch
+    rng = np.random.default_rng(apart + part)
+    H, hd = 4, 128
+    c = Cache(pkg, rng, 24, 1, 1, hd, fmt, spare=0)
+    _shared_pages(c, rng, n, blocks)
+    q = _q(rng, n, H, hd, "bf16", 0.1) + 1.0
+    c.scales[:, 0] = 2.0 ** -5                                    # keys: scores of a few units
+    c.codes[:, 0, :, 32 * part:32 * part + 32] = torch.tensor(-96.0, device="cuda").to(c.codes.dtype)
+    far = apart == 200
+    c.scales[:, 0, :, part] = 2.0 ** (-2 if far else -4)          # ... and of -96 2^-4 sqrt(128) = -68, or -272
+    c.scales[:, 1] = 2.0 ** (-100 if far else -apart)
+    c.scales[:, 1, :, part] = 2.0 ** 100 if far else 1.0
+    c.want_codes, c.want_scales = c.values(), c.scales.double().cpu().numpy()
+    ctx = rng.integers(1, 128 * blocks + 1, n)
+    ctx[: n // 2] = 128 * blocks
+    out = pkg.attention_decode_kv8(q, c.codes, c.scales, c.tab, _i32(ctx))
+    got, qn = out.double().cpu().numpy(), q.double().cpu().numpy()
+    for i in rng.permutation(n)[:40]:
+        k, v = oracle.read(c.want_codes, c.want_scales, c.table[i], 0, ctx[i])
+        want, _, mag, pv = oracle.attention(qn[i], k, v)
+        # probabilities: 21 bits or more, or multiples of 2^-31 of the largest probability times its scale, for which pv has at least
+        # p scale / 2^9 of each value that is not 0; below 2^-126 of the largest nothing
+        p = np.exp((k[:, 0] @ qn[i].T) / np.sqrt(hd))
+        p /= p.sum(0)
+        scale = c.want_scales[c.table[i][np.arange(ctx[i]) // 128], 1, 0, np.arange(ctx[i]) % 128 // 32]
+        top = (p * scale[:, None]).max(0)
+        ds = (hd + 8) * 2.0 ** -24 * mag[:, None]
+        tol = HALF_STEP["bf16"] * np.abs(want) + (2 * ds + 2.0 ** -20 + (ctx[i] + 32) * 2.0 ** -24) * pv \
+            + 2.0 ** -31 * top[:, None] * np.abs(v[:, 0] / scale[:, None]).sum(0) + (not far) * 2.0 ** -126 * np.abs(v[:, 0]).sum(0)
+        assert (np.abs(got[i] - want) <= tol).all(), (i, ctx[i], np.max(np.abs(got[i] - want) - tol))
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 def test_attention_reads_nothing_behind_or_before(pkg, fmt):
     # NaN codes and scales outside [first, ctx): in pages of nobody, behind the row's end, before its window
