@@ -562,7 +562,7 @@ __device__ __forceinline__ uint32_t pack_grad(float a, float b) {  // both to th
     return r;
 }
 
-// What a row's gradients share: with R = (max + log S) log2(e) as rounded and c what the rounding added,
+// What a row's gradients share: with R = (max + log S) log2(e) as rounded and c what the roundings added,
 //   y = z log2(e) - R,  p = 2^y 2^c,  dz = -2^y (a y + b) with a = 2^c g' ln 2 and b = 2^c (g + g' (entropy + c ln 2))
 // A subnormal p may meet a factor that makes a normal product.  fp32 takes the full exponential for it; bf16, whose 8 bits can spare
 // the last of y's, has y 32 higher and the factor 2^-32 lower; fp16 has no room for such products.
@@ -574,15 +574,16 @@ struct GradRow {
     bool plain;      // else the logits are taken one by one
     __device__ __forceinline__ GradRow(float m, float ls, float g, float gh, float H) {
         plain = fabsf(m) < 1e6f && (TYPE != SARA_FP16 || m > -6e4f);
-        const float p1 = m * kLog2e, p2 = ls * kLog2e;
-        r = p1 + p2;
-        const float v = r - p1;  // (the sum's own rounding, and the products')
-        const float c = -(((p1 - (r - v)) + (p2 - v)) + (fmaf(m, kLog2e, -p1) + fmaf(ls, kLog2e, -p2)));
+        const float p1 = m * kLog2e, p2 = ls * kLog2e, sum = p1 + p2;
+        const float v = sum - p1;  // (the sum's own rounding, and the products')
+        float c = -(((p1 - (sum - v)) + (p2 - v)) + (fmaf(m, kLog2e, -p1) + fmaf(ls, kLog2e, -p2)));
+        r = sum - kLift;
+        const float w = r - sum;  // (and the lift's)
+        c -= (sum - (r - w)) + (-kLift - w);
         const float k = exp2_approx(c);
         a = k * gh * kLn2;
         b = k * fmaf(gh, fmaf(c, kLn2, H), g);
         if constexpr (kLift > 0.f) {
-            r -= kLift;
             b = fmaf(-kLift, a, b) * 2.3283064e-10f;  // 2^-32
             a *= 2.3283064e-10f;
         }

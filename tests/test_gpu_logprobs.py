@@ -355,6 +355,29 @@ def test_gradient(pkg, R, V, typ):
     assert same is z and torch.equal(same, want)
 
 
+@pytest.mark.parametrize("top", [-8.5, -8.875, -9.25, -10.875])
+def test_gradient_in_bf16_is_not_off_all_one_way(pkg, top):
+    """A row's probabilities share one constant, whose error is all its values'.  Against the correctly rounded gradients, a value that rounds
+    the other way is off by one step, 2^-7 of it or less, and values that are off by e do so with probability e 2^7 at most.
+    The exponents' own rounding is at most 2^-20 (below 32), ln 2 of it in a value, and as good as independent over the row's
+    different logits; the exponential may be off by 2^-22 and what the rows share by four roundings of fp32, all one way."""
+    import torch
+    R = V = 4096
+    grid = np.arange(-255, round(top * 16) + 1) / 16  # (bf16 has them all)
+    row = np.resize(grid, V)
+    z = torch.from_numpy(row).to(_dtype("bf16")).cuda().repeat(R, 1)
+    g = np.exp2(np.random.default_rng(12).random(R)).astype(np.float32)
+    ls = np.float32(np.log(np.exp(row - top).sum()))
+    stats = torch.tensor([top, ls], dtype=torch.float32, device="cuda").repeat(R, 1)
+    y = pkg.logprobs_backward(z, _i32(np.zeros(R)), stats, None, torch.from_numpy(g).cuda())[:, 1:].double()
+    p = torch.from_numpy(np.exp(row[1:] - top - np.float64(ls))).cuda()
+    want = -torch.from_numpy(g).cuda().double()[:, None] * p
+    off = float(((y - want.to(torch.bfloat16).double()) / want).mean())
+    e = 2.0 ** -20 * np.log(2)
+    tol = 6 * np.sqrt((e + 2.0 ** -22) * 2.0 ** -7 / y.numel()) + 6 * e / np.sqrt(3 * len(grid)) + 2.0 ** -22 + 4 * U
+    assert abs(off) <= tol, (off, tol)
+
+
 def test_gradient_against_differences_of_the_forward(pkg):
     # central differences of the kernel's own outputs: h = 1/4 leaves (h^2 / 6) |third derivative| and rounding / h
     import torch
