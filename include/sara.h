@@ -378,7 +378,8 @@ typedef struct {
  * pos0[i], pos0[i] + 1, ...  One token each is a decode step's append, whole prompts a prefill.  Positions
  * before pos0[i] keep their values (their codes are rescaled where a new token raises the block's scale); a block written from its
  * first position on takes a new scale; codes at positions behind the new tokens are left as they are and no longer mean
- * anything in a block that was written to.  A scale only rises until its block is written from its first position on.
+ * anything in a block that was written to.  A scale only rises until its block is written from its first position on: a block that
+ * holds nothing and is first written behind that position wants the lowest scale, 2^-100, before.
  * k, v: [total] rows of [n_kv_heads][head_dim] (type SARA_BF16 or SARA_FP16), k_stride and v_stride elements apart (multiples of 8),
  * 16-byte aligned.  The blocks that a call writes to belong to one sequence each (shared blocks are for reading).
  * A sequence with a wrong range (seq_start, pos0, past max_blocks) is not written, nor is a block whose id is not in

@@ -98,11 +98,13 @@ def _tokens(x, total, kvh, hd, dev, what):
 
 def kv8_cache(n_blocks: int, n_kv_heads: int, head_dim: int, dtype=None, device="cuda"):
     """An empty 8-bit paged KV cache: codes [n_blocks, 2, n_kv_heads, 128, head_dim] (torch.float8_e4m3fn, the default, or
-    torch.int8) and scales [n_blocks, 2, n_kv_heads, 4]."""
+    torch.int8) and scales [n_blocks, 2, n_kv_heads, 4].  Blocks that go from one sequence to another which does not write them from their
+    first position on want their scales set to 2^-100 again, as they are here."""
     if torch is None:
         _start()
     codes = torch.zeros((n_blocks, 2, n_kv_heads, KV8_PAGE, head_dim), dtype=torch.uint8, device=device)
-    scales = torch.ones((n_blocks, 2, n_kv_heads, KV8_PAGE // KV8_SCALE), dtype=torch.float32, device=device)
+    # (the lowest scale: a block's first tokens set their own, wherever in it they stand)
+    scales = torch.full((n_blocks, 2, n_kv_heads, KV8_PAGE // KV8_SCALE), 2.0 ** -100, dtype=torch.float32, device=device)
     return codes.view(dtype or torch.float8_e4m3fn), scales
 
 

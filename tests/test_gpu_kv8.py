@@ -143,6 +143,24 @@ def test_write_extreme_values(pkg, fmt):
     assert np.isfinite(c.scales[c.table[:, 0], 0, 0, 0].cpu().numpy()).all()
 
 
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+def test_first_tokens_of_an_empty_cache_anywhere_in_a_block(pkg, fmt):
+    # a sequence that begins at position 5: the block has held nothing, so its scale is the tokens' own
+    rng = np.random.default_rng(24)
+    codes, scales = pkg.kv8_cache(2, 2, 64, dtype=_dtype(fmt))
+    k, v = _tokens(rng, 40, 2, 64, "bf16", 1e-3)
+    pkg.kv8_write(codes, scales, _i32([[1]]), k, v, _i32([5]), _i32([0, 40]))
+    got = pkg.kv8_read(codes, scales, _i32([[1]]), _i32([5]), _i32([0, 40]), 40, dtype=_dtype("fp32"))
+    for x, y in zip((k, v), got):
+        x, y = x.double().cpu().numpy(), y.double().cpu().numpy()
+        parts = ((0, 27), (27, 40))  # rows of a scale block
+        for a, b in parts:
+            amax = np.abs(x[a:b]).max((0, 2), keepdims=True)
+            # half a step of the value, or of the smallest code at a scale of at most 2 amax / top
+            tol = np.abs(x[a:b]) * 2.0 ** -4 + amax / 448 * 2.0 ** -9 if fmt == "e4m3" else amax / 127
+            assert (np.abs(y[a:b] - x[a:b]) <= tol).all()
+
+
 def test_write_again_from_an_earlier_position(pkg):
     # tokens taken back (a rejected draft): the positions are written again, the scale only rises
     rng = np.random.default_rng(6)
