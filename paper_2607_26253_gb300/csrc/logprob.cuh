@@ -496,18 +496,20 @@ __global__ void __launch_bounds__(WARPS > 1 ? 32 * WARPS : 256, score_sm_ctas(TY
     }
 }
 
-// Few rows are split over a cluster while a CTA would still hold more than 512 vectors and the CTAs fit the SMs at once (8 an SM; rows
-// that fill the SMs lose by it: 2,048 x 151,936 96 us in one CTA each, 102 in two, 163 in eight).  Many rows take a warp each up to
-// 512 vectors, 4 warps up to 8,192 (8,192 x 8,192: 31 us, 43 with 8 warps; 4,096 x 50,304: 66, 72), 8 warps beyond
-// (3,000 x 151,936: 131 us, 140 with 4).  The alternatives' bound wants the 256 threads.
+// Few rows are split over a cluster while a CTA would still hold more than 512 vectors and the CTAs fit the SMs at once (rows that
+// fill the SMs lose by it: 2,048 x 151,936 96 us in one CTA each, 102 in two, 163 in eight).  With twice the CTAs that fit, in bf16: 152 x 151,936
+// 15.7 us for 12.1, 304 21.3 for 18.8, 608 33.8 for 29.4, with 8 alternatives 29.5, 37.7 and 52.7 for 17.5, 24.1 and 43.1, 300 x 9,001 9.5 for
+// 5.4; better there only just behind the line (160 x 151,936 12.5 for 13.5, 305 18.4 for 19.9, 305 x 60,001 9.8 for 13.5).  Many rows take a
+// warp each up to 512 vectors, 4 warps up to 8,192 (8,192 x 8,192: 31 us, 43 with 8 warps; 4,096 x 50,304: 66, 72), 8 warps
+// beyond (3,000 x 151,936: 131 us, 140 with 4).  The alternatives' bound wants the 256 threads.
 // Where the last of the waves in which long rows end would leave more than half of the SMs' room empty, its rows are split over 2 or 4
 // CTAs and start as the others end (2,048 x 151,936: 93 -> 89 us, 700 42 -> 36, 900 52 -> 44; 1,300, whose rows of padding leave
 // no third wave, 57 -> 60; with 8 CTAs 95; with alternatives, whose bound costs each CTA its own, 114 -> 116, so not there).
 template <int TYPE, bool TOP>
 inline void launch_score(cudaStream_t s, int sms, ScoreParams p) {
-    const int vectors = p.V / (TYPE == SARA_FP32 ? 4 : 8);
+    const int vectors = p.V / (TYPE == SARA_FP32 ? 4 : 8), wave = score_sm_ctas(TYPE, TOP, 8) * sms;
     p.ctas = 1;
-    while (p.ctas < kScoreMaxCtas && vectors > 512 * p.ctas && (int64_t)p.R * 2 * p.ctas <= (int64_t)8 * sms) p.ctas *= 2;
+    while (p.ctas < kScoreMaxCtas && vectors > 512 * p.ctas && (int64_t)p.R * 2 * p.ctas <= wave) p.ctas *= 2;
     if (p.ctas == 1 && vectors <= (TOP ? kScoreTopWarpVectors : kScoreWarpVectors)) {
         score_kernel<TYPE, TOP, 1><<<(unsigned)((p.R + 7) / 8), 256, 0, s>>>(p);
         CK(cudaGetLastError());
@@ -519,7 +521,7 @@ inline void launch_score(cudaStream_t s, int sms, ScoreParams p) {
             CK(cudaGetLastError());
             return;
         }
-        const int wave = score_sm_ctas(TYPE, false, 8) * sms, last = p.R % wave;
+        const int last = p.R % wave;
         if (p.ctas == 1 && vectors > 8192 && p.R > wave && last > 0 && 2 * last <= wave) {
             p.turn = 1;
             p.R -= last;

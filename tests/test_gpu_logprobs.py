@@ -109,6 +109,24 @@ def test_kernels_by_size(pkg, R, V, typ, top):
     _check(pkg.LogProbs(*[pick(x) for x in (o.logprob, o.entropy, o.stats, o.top_token, o.top_logprob)]), pick(z), tok[keep], top)
 
 
+# rows that just fill the SMs in clusters of two, four and eight, and one more
+@pytest.mark.parametrize("typ", ["bf16", "fp32"])
+@pytest.mark.parametrize("V,top", [(33001, 0), (33001, 8), (70001, 0)])
+@pytest.mark.parametrize("per_sm", [4, 3])
+@pytest.mark.parametrize("ctas", [2, 4, 8])
+def test_rows_that_fill_the_gpu_in_clusters(pkg, ctas, per_sm, V, top, typ):
+    import torch
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    for R in (per_sm * sms // ctas, per_sm * sms // ctas + 1):
+        rng = np.random.default_rng(R)
+        z = torch.empty((R, V), device="cuda").normal_(0.0, 3.0, generator=torch.Generator("cuda").manual_seed(R)).to(_dtype(typ))
+        tok = rng.integers(0, V, R)
+        keep = np.concatenate([rng.permutation(R - 2)[:6], [R - 2, R - 1]])
+        o = pkg.logprobs(z, _i32(tok), top=top)
+        pick = lambda x: x[_i32(keep).long()] if x is not None else None  # noqa: E731
+        _check(pkg.LogProbs(*[pick(x) for x in (o.logprob, o.entropy, o.stats, o.top_token, o.top_logprob)]), pick(z), tok[keep], top)
+
+
 # long rows that fill the SMs and some more: the last ones are taken by 2 or 4 CTAs each, in a grid that starts while the others end
 @pytest.mark.parametrize("R,V,typ", [(700, 70001, "bf16"), (860, 33001, "fp32"), (912, 65552, "fp16"), (913, 65552, "fp16")])
 def test_last_rows_of_many_long_ones(pkg, R, V, typ):
