@@ -374,8 +374,8 @@ typedef struct {
 
 /*
  * Quantise new tokens into the cache.  Sequence i's tokens are rows seq_start[i] .. seq_start[i + 1] of k and v
- * (seq_start [n_seq + 1], non-decreasing, at most total; rows behind the last sequence are not read) and take its positions
- * pos0[i], pos0[i] + 1, ...  One token each is a decode step's append, whole prompts a prefill.  Positions
+ * (n_seq at most 2^30; seq_start [n_seq + 1], non-decreasing, at most total; rows behind the last sequence are not read) and take its
+ * positions pos0[i], pos0[i] + 1, ...  One token each is a decode step's append, whole prompts a prefill.  Positions
  * before pos0[i] keep their values (their codes are rescaled where a new token raises the block's scale); a block written from its
  * first position on takes a new scale; codes at positions behind the new tokens are left as they are and no longer mean
  * anything in a block that was written to.  A scale only rises until its block is written from its first position on: a block that
@@ -383,7 +383,7 @@ typedef struct {
  * k, v: [total] rows of [n_kv_heads][head_dim] (type SARA_BF16 or SARA_FP16), k_stride and v_stride elements apart (multiples of 8),
  * 16-byte aligned.  The blocks that a call writes to belong to one sequence each (shared blocks are for reading).
  * A sequence with a wrong range (seq_start, pos0, past max_blocks) is not written, nor is a block whose id is not in
- * [0, n_blocks); both set *status.
+ * [0, n_blocks); both set *status.  Where seq_start falls, right sequences beside the wrong one may be left out too.
  */
 SARA_API int sara_kv8_write(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *pos0, const int32_t *seq_start,
                             int32_t total, const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t type,
@@ -391,7 +391,7 @@ SARA_API int sara_kv8_write(const sara_kv8_cache *cache, int32_t n_seq, const in
 
 /*
  * Read tokens back: row seq_start[i] + j of k and v receives position pos0[i] + j of sequence i, rounded once to `type`
- * (any SARA_* type).  Layout as sara_kv8_write.  Rows that belong to no sequence are left as they are.
+ * (any SARA_* type).  Layout and limits as sara_kv8_write.  Rows that belong to no sequence are left as they are.
  * Positions outside the table or in a block whose id is wrong read as NaN and set *status; a wrong seq_start sets it too, and its rows
  * are left as they are.
  */

@@ -15,6 +15,7 @@ constexpr int kKv8Page = SARA_KV8_PAGE;
 constexpr int kKv8Block = SARA_KV8_SCALE;
 constexpr int kKv8PageBlocks = kKv8Page / kKv8Block;
 constexpr int kKv8LowestExp = -100;
+constexpr int kKv8MaxSeqs = 1 << 30;  // of a call: the search for a unit's sequence counts in 32 bits
 
 struct Kv8Cache {
     uint8_t *codes;

@@ -59,7 +59,7 @@ extern "C" {
 int sara_kv8_write(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *pos0, const int32_t *seq_start, int32_t total,
                    const void *k, int64_t k_stride, const void *v, int64_t v_stride, int32_t type, int32_t *status,
                    void *stream) {
-    if (!cache_ok(cache, n_seq) || n_seq < 0 || total < 0 || (type != SARA_BF16 && type != SARA_FP16)) return SARA_EINVAL;
+    if (!cache_ok(cache, n_seq) || n_seq < 0 || n_seq > kKv8MaxSeqs || total < 0 || (type != SARA_BF16 && type != SARA_FP16)) return SARA_EINVAL;
     if (n_seq == 0 || total == 0) return SARA_OK;
     if (!pos0 || !seq_start || !rows_ok(cache, k, k_stride, total) || !rows_ok(cache, v, v_stride, total)) return SARA_EINVAL;
     return op_guard([&] {
@@ -79,7 +79,7 @@ int sara_kv8_write(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *po
 
 int sara_kv8_read(const sara_kv8_cache *cache, int32_t n_seq, const int32_t *pos0, const int32_t *seq_start, int32_t total,
                   void *k, int64_t k_stride, void *v, int64_t v_stride, int32_t type, int32_t *status, void *stream) {
-    if (!cache_ok(cache, n_seq) || n_seq < 0 || total < 0 || type < SARA_BF16 || type > SARA_FP32) return SARA_EINVAL;
+    if (!cache_ok(cache, n_seq) || n_seq < 0 || n_seq > kKv8MaxSeqs || total < 0 || type < SARA_BF16 || type > SARA_FP32) return SARA_EINVAL;
     if (n_seq == 0 || total == 0) return SARA_OK;
     if (!pos0 || !seq_start || !rows_ok(cache, k, k_stride, total) || !rows_ok(cache, v, v_stride, total)) return SARA_EINVAL;
     return op_guard([&] {

@@ -50,6 +50,13 @@ def test_write_and_read_refusals(lib):
             assert call(fn, cache=_cache(table=0), n=0, typ=t, pos0=None, start=None) == 0
 
 
+def test_write_and_read_refuse_more_sequences_than_their_search_counts(lib):
+    # 32-bit sums of its steps would pass 2^31 shortly before the last int32, and its loads leave the starts
+    for fn in (lib.sara_kv8_write, lib.sara_kv8_read):
+        for n in ((1 << 30) + 1, 2 ** 31 - 31, 2 ** 31 - 1):
+            assert fn(_cache(n_kv_heads=1), n, A, A, 1, A, 64, A, 64, 0, None, None) == -1
+
+
 def test_attention_refusals(lib):
     assert lib.sara_attention_kv8_workspace_bytes(0, 8, 2, 64) == 0
     assert lib.sara_attention_kv8_workspace_bytes(4, 8, 0, 64) == 0
