@@ -511,7 +511,7 @@ inline void launch_score(cudaStream_t s, int sms, ScoreParams p) {
     p.ctas = 1;
     while (p.ctas < kScoreMaxCtas && vectors > 512 * p.ctas && (int64_t)p.R * 2 * p.ctas <= wave) p.ctas *= 2;
     if (p.ctas == 1 && vectors <= (TOP ? kScoreTopWarpVectors : kScoreWarpVectors)) {
-        score_kernel<TYPE, TOP, 1><<<(unsigned)((p.R + 7) / 8), 256, 0, s>>>(p);
+        score_kernel<TYPE, TOP, 1><<<((unsigned)p.R + 7) / 8, 256, 0, s>>>(p);
         CK(cudaGetLastError());
         return;
     }

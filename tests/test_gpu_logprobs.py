@@ -489,6 +489,21 @@ def test_rows_past_32_bits(pkg):
     assert float(y[:-2].abs().max()) == 0
 
 
+def test_most_rows(pkg):
+    # 2^31 - 1 rows, of one token each: the last group of eight is not whole
+    import torch
+    R = 2 ** 31 - 1
+    z = torch.zeros((R, 1), dtype=torch.bfloat16, device="cuda")
+    z[R - 1] = 3.0
+    o = pkg.logprobs(z, None)
+    # (the last row: 3 log2(e) is rounded, so its sum is an exponential of the rounding, good to 2^-21 as any: the bound of sums here.  Zeros
+    # round nothing: 2^0 is 1, its logarithm 0.)
+    assert o.logprob is None and float(o.stats[-1, 0]) == 3.0 and abs(float(o.stats[-1, 1])) <= _sum_bound(1) >= abs(float(o.entropy[-1]))
+    for x in (o.entropy[:-1], o.stats[:-1].view(-1)):
+        for a in range(0, x.numel(), 1 << 29):
+            assert not bool(x[a:a + (1 << 29)].any())
+
+
 def test_largest_vocabulary(pkg):
     # token ids up to 2^31 - 2
     import torch
