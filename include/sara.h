@@ -406,8 +406,9 @@ SARA_API int sara_kv8_read(const sara_kv8_cache *cache, int32_t n_seq, const int
  * q, out: [n_seq][n_heads][head_dim] of `type` (SARA_BF16 or SARA_FP16), rows of q q_stride elements apart (a multiple of 8),
  * both 16-byte aligned.  lse: [n_seq][n_heads] fp32 or NULL, the natural logarithm of the sum of the exponentiated scores
  * (-inf for a row without a position).  Masked positions and positions behind ctx are not read.
- * Sums, maxima and scores are held in fp32.  Probabilities times their values' scale are held in 22 bits, or within 2^-31 of the head's largest
- * such product; probabilities below 2^-126 of the head's largest count as 0.
+ * Sums, maxima and scores are held in fp32, and have to be finite there (sums of up to 2^15 |value| a position).  Probabilities times their
+ * values' scale are held in 22 bits, or within 2^-31 of the head's largest such product; probabilities below 2^-126 of the head's largest
+ * count as 0.  bf16 queries: elements 2^31 below their head's largest lose bits, those 2^39 below count as 0 (fp16 ones are exact).
  * A row with ctx outside [0, 128 * max_blocks], first < 0 or a block id outside [0, n_blocks) gives NaN and sets *status.
  * workspace: sara_attention_kv8_workspace_bytes(...) bytes of device scratch, 16-byte aligned, all zero on first use and left
  * zero where it has to be; calls that share one must not overlap.

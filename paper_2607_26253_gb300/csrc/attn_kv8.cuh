@@ -5,7 +5,8 @@
 // 128 dims).
 //   - Scores: A = K (rows: positions), B = q^T (columns: the group's query heads, at most 8).  Lane (g, t) takes
 //     16-byte pieces of positions g and g + 8; which dims meet in a k-step does not matter as long as q is laid out
-//     alike.  bf16 queries enter as fp16 after a power of two has brought the row's largest to 2^14.
+//     alike.  bf16 queries enter as fp16 after a power of two has brought the head's largest to 2^14: exact down to 2^-31 of it,
+//     within 2^-39 of it below, so scores are off by 2^-39 max |q| sum |k| at most (a second, low half would cost as many MMAs again).
 //   - Output: A = V^T (rows: dims, lane (g, t) holds hd / 8 dims of 4 positions, byte permutes pair the positions),
 //     B = P^T, the scores' own registers transposed by movmatrix.
 //   - A scale covers all of a warp's positions: K's is a factor of the scores, V's of P, so that neither costs a multiplication
@@ -16,11 +17,12 @@
 // steps skip the column maximum and the rescale.
 // The next step's copies are under way while a step is computed, across the ends of units: 64 KB an SM, which is enough, and more
 // is worse (64 x 8,192 positions: 166 us, with two steps ahead 177; a step in registers instead, its values asked for with its scores,
-// the next one's keys after them: 174, in int8 188 for 168).  Five CTAs an SM, whose 96 registers spill: 182.
+// the next one's keys after them: 174, in int8 188 for 168).  Five CTAs an SM, whose 96 registers spill: 182; four's 128 spill
+// 28 bytes at most, at 128 dims in e4m3 (<128, e4m3, 1>: 16 stored, 28 loaded), others none.
 // Work: the (row, KV head, positions) triples in one list, cut into equal shares, one per CTA of 4 warps (4 an SM), or per warp
 // where there are many rows (kAttnKv8Units).  A (row, KV head) that several shares hold is joined by the last of them to finish,
 // in the list's order (so results repeat bit for bit), by levels where there are many.
-// Measured (kernel in a graph): 64 rows x 8,192 positions, 32 / 8 heads of 128: 166 us, 6.5 TB/s (350 x 4,000: 6.7); 2 x 200,000, 16 / 2
+// Measured (kernel in a graph): 64 rows x 8,192 positions, 32 / 8 heads of 128: 167 us, 6.4 TB/s (350 x 4,000: 6.7); 2 x 200,000, 16 / 2
 // heads: 45 (the joins take 10); 26 ragged rows of mean 758, 12 / 2 heads: 12 us and one row 7.7, chains of latencies: share 0.7
 // us, first keys 1.1, step 0.5, state 0.9, arrival 0.7, join 2.5.  700 ragged rows of mean 200, 32 / 8 heads: 65 us (44 at the copy's
 // rate: 8 us until the first step and 5 of joins).

@@ -8,8 +8,8 @@
 //   e^(z - m) = 2^(z log2(e) - r) 2^-c,  r = m log2(e) as rounded, c what the rounding took: one fused operation a logit,
 // and c, the same for all, is put right once, in log S.  Sums in fp32 against the thread's own running maximum.  c is half a step of r
 // at most: 1/16 up to |m| = 10^6, but 440 at 10^10 (a mask's usual values), where 2^c has no room.  Larger maxima take z - m first, logit by logit.
-// Scores of 2,048 x 151,936 in bf16: 89 us, 6.3 TB/s (rows end in waves); with 8 alternatives 115; 26 rows with
-// 8 alternatives 9.9, 5.4 without: the bound on them, their ranks and the cluster's join are latencies.
+// Scores of 2,048 x 151,936 in bf16: 88 us, 6.4 TB/s (rows end in waves); with 8 alternatives 115; 26 rows with
+// 8 alternatives 9.6, 5.4 without: the bound on them, their ranks and the cluster's join are latencies.
 #pragma once
 #include "device_common.cuh"
 #include "host_util.h"
@@ -300,7 +300,7 @@ __device__ __forceinline__ float from_ordered(int i) { return __int_as_float(i <
 // One row per group of WARPS warps (1: eight rows to a CTA; else a CTA), or, where p.ctas > 1, per cluster of that many
 // CTAs, each a contiguous share of its vectors.
 // CTAs an SM that the registers have to leave room for.  (The alternatives of 16-bit logits would spill at four: 2,048 x 151,936, top 8:
-// 132 us, 148 with four.)
+// 132 us, 148 with four.  A warp a row in fp32 spills 12 bytes at six.)
 constexpr int score_sm_ctas(int type, bool top, int warps) {
     return warps == 4 ? 8 : warps == 1 && !top ? 6 : warps == 8 && top && type != SARA_FP32 ? 3 : 4;
 }
