@@ -451,6 +451,44 @@ SARA_API int sara_logprobs_backward(const void *logits, int64_t row_stride, int3
                                     const int32_t *tokens, const float *stats, const float *entropy, const float *grad_logprob,
                                     const float *grad_entropy, void *grad_logits, int64_t grad_stride, void *stream);
 
+/* ---------------------------------------------------------------------------------------
+ * The same scores from the last hidden states, for which no logits are stored: z = scale H W^T, H [R][d] the rows' hidden states,
+ * W [V][d] the vocabulary's weights (an lm_head as it lies in memory).  `type` SARA_BF16 or SARA_FP16, of H, W and their gradients; d a
+ * multiple of 8 up to 65,536, R and V at most 2^24; rows of H, W and the gradients stride elements apart (multiples of 8, at least d), all
+ * of them 16-byte aligned; scale > 0 and finite (1 / temperature).  Device pointers, not waited for, nothing allocated; the calls may be
+ * captured.  Products are exact and summed in fp32.
+ * workspace: sara_linear_logprobs_workspace_bytes(R, d, V, backward) bytes of device scratch, 256-byte aligned, whose first 256 bytes are
+ * zero on first use and left zero where they have to be; calls that share one must not overlap.  (12 bytes a row and 256 tokens for the
+ * scores; for the gradient the rows, pieces of at most 16,384 tokens' gradients, some 192 MB of them, and fp32 sums of grad_hidden.)
+ * ------------------------------------------------------------------------------------- */
+SARA_API size_t sara_linear_logprobs_workspace_bytes(int32_t R, int32_t d, int32_t V, int32_t backward);
+
+/*
+ * logprob, entropy, stats [R], [R], [R][2] fp32: as sara_logprobs gives them for the logits z.  tokens [R] int32; a negative one marks
+ * a row of padding, whose hidden state does not matter (logprob 0, entropy 0, stats {0, 0}); one >= V gives the logprob NaN.  A NaN or +inf
+ * among a row's logits makes its logprob, entropy and log S NaN.  Each output may be NULL, and tokens too where logprob is.
+ */
+SARA_API int sara_linear_logprobs(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride, int32_t type,
+                                  int32_t R, int32_t d, int32_t V, const int32_t *tokens, float scale, float *logprob, float *entropy,
+                                  float *stats, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The gradients with respect to the hidden states and the weights: with p = softmax(z) of the row and
+ *   dz[r][v] = grad_logprob[r] (1[v = token[r]] - p_v) - grad_entropy[r] p_v (log p_v + entropy[r]),
+ *   grad_hidden = scale dz W,   grad_weight = scale dz^T H,
+ * the logits made again, piece by piece of the vocabulary, summed in fp32 and rounded once to `type`.  dz enters the products
+ * in `type` (in fp16 times a power of two of the row, so that tokens down to p = 2^-27 keep all its bits).  stats and entropy as
+ * sara_linear_logprobs gave them.  grad_logprob and grad_entropy [R] fp32, each may be NULL (0); entropy is wanted with grad_entropy,
+ * tokens with grad_logprob.  grad_hidden or grad_weight may be NULL (not computed); they overlap neither each other nor hidden and weight.
+ * Rows of padding get 0 and add nothing to grad_weight, whatever their hidden states hold; a token >= V, a NaN or +inf among the logits makes
+ * the row NaN, and with it grad_weight.  Sums are in a fixed order: results repeat bit for bit.
+ */
+SARA_API int sara_linear_logprobs_backward(const void *hidden, int64_t hidden_stride, const void *weight, int64_t weight_stride,
+                                           int32_t type, int32_t R, int32_t d, int32_t V, const int32_t *tokens, float scale,
+                                           const float *stats, const float *entropy, const float *grad_logprob,
+                                           const float *grad_entropy, void *grad_hidden, int64_t grad_hidden_stride, void *grad_weight,
+                                           int64_t grad_weight_stride, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,4 +1,5 @@
-"""Operators on torch CUDA tensors over an 8-bit paged KV cache and over the logits of sampled tokens (include/sara.h).
+"""Operators on torch CUDA tensors over an 8-bit paged KV cache, and over the logits or last hidden states of sampled tokens
+(include/sara.h).
 
 Results are not recorded by autograd: logprobs has its gradient as a call of its own.  These are a decode step's calls, and
 most of them cost more on the host than on the GPU: checks are written out where they are made, messages put together only for a
@@ -269,3 +270,98 @@ def logprobs_backward(logits, tokens, stats, entropy, grad_logprob=None, grad_en
     if rc:
         _check(rc)
     return out
+
+
+def _rows16(x, what, shape=None):
+    """Type, rows, elements of a row, row stride and GPU of a matrix of bf16 or fp16 rows."""
+    if torch is None:
+        _start()
+    typ = _types.get(x.dtype, 2)
+    if typ == 2 or x.dim() != 2 or (shape is not None and x.shape != shape):
+        _refuse(f"{what} must be bf16 or fp16, {'[rows, dim]' if shape is None else tuple(shape)}")
+    rows, d = x.shape
+    row, step = x.stride()
+    if step != 1 and d != 1:
+        _refuse(f"{what} must have rows of consecutive elements")
+    if rows > _MOST or d > _MOST:
+        _refuse(f"{what} must have at most 2^31 - 1 rows and columns")
+    return typ, rows, d, max(row, d) if rows <= 1 else row, x.get_device()
+
+
+def _linear(hidden, weight):
+    """Hidden states and a vocabulary's weights, checked: type, rows, dim, vocabulary, both row strides, GPU."""
+    typ, R, d, hs, dev = _rows16(hidden, "hidden")
+    wtyp, V, wd, ws, wdev = _rows16(weight, "weight")
+    if wtyp != typ or wd != d or wdev != dev:
+        _refuse("weight must be [vocabulary, dim] of hidden's type and dim, on its device")
+    return typ, R, d, V, hs, ws, dev
+
+
+def _linear_scratch(workspace, dev):
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        _refuse("workspace must be contiguous, on the operands' device")
+    return workspace.data_ptr(), workspace.nbytes
+
+
+def linear_logprobs_workspace(rows: int, dim: int, vocab: int, backward: bool = False, device="cuda"):
+    """The scratch of linear_logprobs, or of linear_logprobs_backward, for these sizes, to be kept from call to call
+    (its start zeroed; calls that share it must not overlap)."""
+    if torch is None:
+        _start()
+    if min(rows, dim, vocab) < 0 or max(rows, dim, vocab) > _MOST:
+        _refuse("sizes must be 0 .. 2^31 - 1")
+    ws = torch.empty(max(_lib.sara_linear_logprobs_workspace_bytes(rows, dim, vocab, backward), 256), dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+def linear_logprobs(hidden, weight, tokens, scale: float = 1.0, workspace=None) -> LogProbs:
+    """logprobs of the logits scale * hidden @ weight.T, which are never stored (see sara_linear_logprobs): hidden [R, dim] and
+    weight [vocabulary, dim] bf16 or fp16, dim a multiple of 8, rows may be strided.  tokens [R] int32, negative for rows of padding;
+    None: entropy alone.  No alternatives."""
+    typ, R, d, V, hs, ws, dev = _linear(hidden, weight)
+    tok = None if tokens is None else _vector(tokens, _int32, R, dev, "tokens")
+    if dev < 0 or dev != _device():
+        return _elsewhere(dev, linear_logprobs, hidden, weight, tokens, scale, workspace)
+    if workspace is None:
+        workspace = linear_logprobs_workspace(R, d, V, device=hidden.device)
+    scratch, size = _linear_scratch(workspace, dev)
+    new = hidden.new_empty
+    ent, stats, lp = new(R, dtype=_fp32), new((R, 2), dtype=_fp32), None if tokens is None else new(R, dtype=_fp32)
+    rc = _lib.sara_linear_logprobs(hidden.data_ptr(), hs, weight.data_ptr(), ws, typ, R, d, V, tok, scale, None if lp is None else lp.data_ptr(),
+                                   ent.data_ptr(), stats.data_ptr(), scratch, size, _stream(dev))
+    if rc:
+        _check(rc)
+    return LogProbs(lp, ent, stats)
+
+
+def linear_logprobs_backward(hidden, weight, tokens, stats, entropy, grad_logprob=None, grad_entropy=None, scale: float = 1.0,
+                             workspace=None, grad_hidden=True, grad_weight=True):
+    """Gradients of linear_logprobs with respect to hidden and weight (see sara_linear_logprobs_backward), in their type: grad_logprob and
+    grad_entropy [R] fp32 weigh the rows' log-probabilities and entropies.  grad_hidden, grad_weight: True for a new tensor, False for
+    none (None is returned in its place), or the tensor to write."""
+    typ, R, d, V, hs, ws, dev = _linear(hidden, weight)
+    at_tok, at_stats = _vector(tokens, _int32, R, dev, "tokens"), _matrix(stats, _fp32, (R, 2), dev, "stats")
+    at_ent, at_g = _vector(entropy, _fp32, R, dev, "entropy"), _vector(grad_logprob, _fp32, R, dev, "grad_logprob")
+    at_gh = _vector(grad_entropy, _fp32, R, dev, "grad_entropy")
+    outs = []
+    for x, like, what in ((grad_hidden, hidden, "grad_hidden"), (grad_weight, weight, "grad_weight")):
+        if x is not True and x is not False:
+            otyp, _, _, _, odev = _rows16(x, what, like.shape)
+            if otyp != typ or odev != dev:
+                _refuse(f"{what} must be of its operand's type, on its device")
+        outs.append(x)
+    if dev < 0 or dev != _device():
+        return _elsewhere(dev, linear_logprobs_backward, hidden, weight, tokens, stats, entropy, grad_logprob, grad_entropy, scale,
+                          workspace, grad_hidden, grad_weight)
+    gh, gw = (like.new_empty(like.shape) if x is True else None if x is False else x for x, like in zip(outs, (hidden, weight)))
+    if workspace is None:
+        workspace = linear_logprobs_workspace(R, d, V, True, hidden.device)
+    scratch, size = _linear_scratch(workspace, dev)
+    rc = _lib.sara_linear_logprobs_backward(hidden.data_ptr(), hs, weight.data_ptr(), ws, typ, R, d, V, at_tok, scale, at_stats, at_ent,
+                                            at_g, at_gh, None if gh is None else gh.data_ptr(), d if gh is None or R <= 1 else gh.stride(0),
+                                            None if gw is None else gw.data_ptr(), d if gw is None or V <= 1 else gw.stride(0), scratch, size,
+                                            _stream(dev))
+    if rc:
+        _check(rc)
+    return gh, gw

@@ -22,7 +22,8 @@ EXPORTED = ("sara_create", "sara_collect_step", "sara_teacher_force", "sara_last
             "sara_gemm_workspace_bytes", "sara_gemm_bf16", "sara_attention_workspace_bytes",
             "sara_attention_decode", "sara_sample", "sara_profile", "sara_gemm_bf16_static", "sara_set_limits",
             "sara_abi_version", "sara_kv8_write", "sara_kv8_read", "sara_attention_kv8_workspace_bytes",
-            "sara_attention_decode_kv8", "sara_logprobs", "sara_logprobs_backward")
+            "sara_attention_decode_kv8", "sara_logprobs", "sara_logprobs_backward",
+            "sara_linear_logprobs_workspace_bytes", "sara_linear_logprobs", "sara_linear_logprobs_backward")
 ABI_VERSION = 3
 
 c_p = ctypes.c_void_p
@@ -139,6 +140,14 @@ def load(path: str = LIB_PATH):
     lib.sara_logprobs.restype = ctypes.c_int
     lib.sara_logprobs_backward.argtypes = [c_p, i64, i32, i32, i32] + [c_p] * 6 + [i64, c_p]
     lib.sara_logprobs_backward.restype = ctypes.c_int
+    f32, size = ctypes.c_float, ctypes.c_size_t
+    lib.sara_linear_logprobs_workspace_bytes.argtypes = [i32] * 4
+    lib.sara_linear_logprobs_workspace_bytes.restype = size
+    lib.sara_linear_logprobs.argtypes = [c_p, i64, c_p, i64, i32, i32, i32, i32, c_p, f32, c_p, c_p, c_p, c_p, size, c_p]
+    lib.sara_linear_logprobs.restype = ctypes.c_int
+    lib.sara_linear_logprobs_backward.argtypes = [c_p, i64, c_p, i64, i32, i32, i32, i32, c_p, f32, c_p, c_p, c_p, c_p, c_p, i64, c_p,
+                                                  i64, c_p, size, c_p]
+    lib.sara_linear_logprobs_backward.restype = ctypes.c_int
     lib.sara_abi_version.argtypes = []
     lib.sara_abi_version.restype = ctypes.c_int
     if lib.sara_abi_version() != ABI_VERSION:
