@@ -45,3 +45,21 @@ def grad(z, token, g, gh):
     if token is not None:
         y[token] += g
     return y
+
+
+def linear(h, w, tokens, scale=1.0):
+    """score() of the logits scale h w^T, a row of hidden states each; the logits too."""
+    z = scale * (np.asarray(h, np.float64) @ np.asarray(w, np.float64).T)
+    return [score(z[r], None if tokens is None else int(tokens[r])) for r in range(len(z))], z
+
+
+def linear_grad(h, w, tokens, g, gh, scale=1.0):
+    """Gradients of sum g logprob + gh entropy with respect to h and w, and those with respect to the logits: rows of padding count as
+    hidden states of 0 (their logits' gradients are 0, whatever they hold)."""
+    h = np.asarray(h, np.float64).copy()
+    if tokens is not None:
+        h[np.asarray(tokens) < 0] = 0
+    w = np.asarray(w, np.float64)
+    z = scale * (h @ w.T)
+    dz = np.stack([grad(z[r], None if tokens is None else int(tokens[r]), g[r], gh[r]) for r in range(len(z))])
+    return scale * (dz @ w), scale * (dz.T @ h), dz

@@ -1,0 +1,405 @@
+"""Log-probabilities and entropies from hidden states, and their gradients, on the GPU against the 64-bit oracle, within bounds that
+follow from the arithmetic: exact products summed in fp32, dz rounded to the operands' type, one rounding of the results."""
+import numpy as np
+import pytest
+
+import synth
+from oracle import scoring as oracle
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF = {"bf16": 2.0 ** -8, "fp16": 2.0 ** -11}
+LEAST = {"bf16": 2.0 ** -126, "fp16": 2.0 ** -25}
+
+
+@pytest.fixture(scope="module")
+def pkg():
+    import __graft_entry__
+    __graft_entry__.build()
+    import paper_2607_26253_gb300 as p
+    p.load()
+    return p
+
+
+def _dtype(name):
+    import torch
+    return {"bf16": torch.bfloat16, "fp16": torch.float16}[name]
+
+
+def _i32(a):
+    import torch
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")
+
+
+def _f32(a):
+    import torch
+    return torch.tensor(np.asarray(a), dtype=torch.float32, device="cuda")
+
+
+def _inputs(rng, R, d, V, typ, std=2.0):
+    """Hidden states N(0, 1) and weights that make logits of spread `std`, on the GPU."""
+    import torch
+    h = torch.from_numpy(rng.standard_normal((R, d))).cuda().to(_dtype(typ))
+    w = torch.from_numpy(rng.standard_normal((V, d)) * (std / np.sqrt(d))).cuda().to(_dtype(typ))
+    return h, w
+
+
+def _np(x):
+    return x.double().cpu().numpy()
+
+
+def _chain(n):
+    # relative to the sum of magnitudes: the tensor core adds 16 products at a time and cuts, a step of fp32 each, and a few more inside
+    return (n / 16 + 8) * 2 * U
+
+
+def _logit_error(h, w, scale):
+    """Bound on a row's logits' errors, the largest over the vocabulary."""
+    a = scale * (np.abs(h) @ np.abs(w).T).max(1)
+    return a * (_chain(h.shape[1]) + 2 * U)
+
+
+def _sum_error(V):
+    return (V / 256 + 300) * U  # tiles of 256 in a chain, tiles joined by fewer steps than there are; terms good to 2^-21
+
+
+def _check(o, h, w, tokens, scale):
+    hn, wn = _np(h), _np(w)
+    live = np.ones(len(hn), bool) if tokens is None else np.asarray(tokens) >= 0
+    want, z = oracle.linear(np.where(live[:, None], hn, 0), wn, tokens, scale)
+    e = _logit_error(np.where(live[:, None], hn, 0), wn, scale)
+    lp, H, st = None if o.logprob is None else _np(o.logprob), _np(o.entropy), _np(o.stats)
+    for r, s in enumerate(want):
+        if not live[r]:
+            assert (lp is None or lp[r] == 0) and H[r] == 0 and (st[r] == 0).all(), r
+            continue
+        b = _sum_error(len(wn)) + 2 * e[r]
+        if lp is not None:
+            if np.isnan(s["logprob"]):
+                assert np.isnan(lp[r]), r
+            else:
+                assert abs(lp[r] - s["logprob"]) <= b + 4 * U * (abs(s["logprob"]) + s["logsum"] + 1), (r, lp[r], s)
+        if np.isnan(s["entropy"]):
+            assert np.isnan(H[r]) and np.isnan(st[r, 1]), r
+            continue
+        dist = s["max"] - z[r]
+        mean = float((np.exp(-dist) * dist).sum() / np.exp(-dist).sum())
+        assert abs(H[r] - s["entropy"]) <= (b + 4 * U) * (2 + 2 * mean + s["logsum"]), (r, H[r], s)
+        assert abs(st[r, 0] - s["max"]) <= e[r] + 2 * U * abs(s["max"]) and abs(st[r, 1] - s["logsum"]) <= b + 2 * U * s["logsum"], (r, st[r], s)
+
+
+def _check_grad(got, h, w, tokens, g, gh, scale, typ, spread=True):
+    """spread: inputs as of _inputs, whose errors add up as independent ones do; bounds by magnitudes hold for any."""
+    hn, wn, gn, ghn = _np(h), _np(w), _np(g), _np(gh)
+    live = np.ones(len(hn), bool) if tokens is None else np.asarray(tokens) >= 0
+    dh, dw, dz = oracle.linear_grad(hn, wn, tokens, gn, ghn, scale)
+    h0 = np.where(live[:, None], hn, 0)
+    wrong = np.isnan(dz).any(1)
+    e = 2 * _logit_error(h0, wn, scale) + _sum_error(len(wn))
+    ok = ~wrong
+    # dz's error: p's (2 e and the exponential's), that of log p + H where it counts, one rounding to the type
+    z = scale * (h0 @ wn.T)
+    lp = z - z.max(1, keepdims=True)
+    lp -= np.log(np.exp(lp).sum(1, keepdims=True))
+    H = -(np.exp(lp) * lp).sum(1, keepdims=True)
+    near = (e[:, None] + 8 * U * (np.abs(lp) + 1)) * np.exp(lp) * (np.abs(gn)[:, None] + np.abs(ghn)[:, None] * (np.abs(lp + H) + 2 + H))
+    near = near + 4 * U * np.abs(dz) + 4 * U * np.abs(gn)[:, None] * (np.arange(len(wn)) == (np.asarray(tokens) if tokens is not None else np.full(len(hn), -1))[:, None])
+    err = np.where(live[:, None], near + HALF[typ] * np.abs(dz), 0)
+    if typ == "fp16":  # a row's dz below 2^-27 of its largest possible: half a step of fp16 there
+        err += np.where(live, 2.0 ** -25 * 2.0 ** -12 * (np.abs(gn) + 16 * np.abs(ghn)), 0)[:, None]
+    if got[0] is not None:
+        y = _np(got[0])
+        assert (y[~live] == 0).all() and np.isnan(y[wrong]).all()
+        mag = scale * (np.abs(dz) @ np.abs(wn))
+        tol = scale * (err @ np.abs(wn)) + (_chain(len(wn)) + 40 * U) * mag + HALF[typ] * (1 + 1e-3) * np.abs(dh) + LEAST[typ]
+        if len(wn) > 0:
+            bad = np.abs(y - dh)[ok] > tol[ok]
+            assert not bad.any(), (np.argwhere(bad)[:5], y[ok][bad][:5], dh[ok][bad][:5], tol[ok][bad][:5])
+        if spread and typ == "bf16" and dh[ok].size > 1000 and np.linalg.norm(dh[ok]):
+            assert np.linalg.norm(y[ok] - dh[ok]) <= 1.5 * HALF[typ] * np.linalg.norm(dh[ok])
+    if got[1] is not None:
+        y = _np(got[1])
+        if wrong.any():
+            assert np.isnan(y).all()
+            return
+        low = 0.0
+        if typ == "fp16":  # rows lowered by more than 14 powers of two lose bits: half a step of fp16 times what their dz was raised to
+            b = np.abs(gn) + 16 * np.abs(ghn)
+            low = scale * 2.0 ** -25 * len(hn) * b[live].max() if live.any() else 0.0
+        mag = scale * (np.abs(dz).T @ np.abs(h0))
+        tol = scale * (err.T @ np.abs(h0)) + (_chain(len(hn)) + 40 * U) * mag + HALF[typ] * (1 + 1e-3) * np.abs(dw) + LEAST[typ] + low
+        bad = np.abs(y - dw) > tol
+        assert not bad.any(), (np.argwhere(bad)[:5], y[bad][:5], dw[bad][:5], tol[bad][:5])
+        if spread and typ == "bf16" and dw.size > 1000 and np.linalg.norm(dw):
+            assert np.linalg.norm(y - dw) <= 1.5 * HALF[typ] * np.linalg.norm(dw)
+
+
+def _both(pkg, h, w, tok, scale, g, gh, typ, spread=True):
+    t = None if tok is None else _i32(tok)
+    o = pkg.linear_logprobs(h, w, t, scale=scale)
+    _check(o, h, w, tok, scale)
+    y = pkg.linear_logprobs_backward(h, w, t, o.stats, o.entropy, g if tok is not None else None, gh, scale=scale)
+    _check_grad(y, h, w, tok, g if tok is not None else 0 * g, gh, scale, typ, spread)
+    return o, y
+
+
+# rows and tokens around tiles, dims around chunks of 64 and tiles of 256, from the smallest on
+@pytest.mark.parametrize("typ", ["bf16", "fp16"])
+@pytest.mark.parametrize("R,d,V", [(1, 8, 1), (1, 64, 256), (2, 72, 3), (5, 16, 255), (31, 128, 512), (32, 200, 257), (127, 256, 700), (128, 264, 1024),
+                                   (129, 64, 300), (130, 320, 2001), (255, 520, 513), (256, 1536, 400), (257, 8, 3000), (640, 136, 1111)])
+def test_sizes(pkg, R, d, V, typ):
+    rng = np.random.default_rng(R + d + V)
+    h, w = _inputs(rng, R, d, V, typ)
+    tok = rng.integers(0, V, R)
+    if R > 3:
+        tok[1::7] = -1
+    _both(pkg, h, w, tok, [1.0, 1.25, 0.3][R % 3], _f32(rng.standard_normal(R)), _f32(0.1 * rng.standard_normal(R)), typ)
+
+
+# several pieces of the vocabulary, dH in several parts; the last piece and its parts are shorter
+@pytest.mark.parametrize("typ", ["bf16", "fp16"])
+@pytest.mark.parametrize("R,d,V", [(3, 64, 16384), (40, 72, 33000), (200, 128, 40001), (300, 264, 16385)])
+def test_pieces(pkg, R, d, V, typ):
+    rng = np.random.default_rng(V)
+    h, w = _inputs(rng, R, d, V, typ, 3.0)
+    tok = rng.integers(0, V, R)
+    tok[0] = V - 1
+    _both(pkg, h, w, tok, 1.0, _f32(rng.standard_normal(R)), _f32(0.1 * rng.standard_normal(R)), typ)
+
+
+@pytest.mark.parametrize("typ", ["bf16", "fp16"])
+@pytest.mark.parametrize("R", [9, 400])
+def test_rows_of_padding(pkg, R, typ):
+    import torch
+    rng = np.random.default_rng(R)
+    h, w = _inputs(rng, R, 96, 1500, typ)
+    g, gh = _f32(rng.standard_normal(R)), _f32(rng.standard_normal(R))
+    tok = rng.integers(0, 1500, R)
+    tok[rng.random(R) < 0.5] = -1
+    tok[0] = -7
+    dead = _i32(tok) < 0
+    h[dead] = torch.tensor([np.nan, np.inf, -np.inf] * 32, device="cuda").to(h.dtype)  # (what they hold does not matter)
+    g[dead], gh[dead] = np.nan, np.inf
+    o = pkg.linear_logprobs(h, w, _i32(tok))
+    _check(o, h, w, tok, 1.0)
+    y = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, g, gh)
+    _check_grad(y, h, w, tok, g.nan_to_num(0, 0, 0), gh.nan_to_num(0, 0, 0), 1.0, typ)
+    tok[:] = -1  # nothing but padding
+    o = pkg.linear_logprobs(h, w, _i32(tok))
+    _check(o, h, w, tok, 1.0)
+    a, b = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, g, gh)
+    assert not a.any() and not b.any()
+
+
+def test_no_rows(pkg):
+    import torch
+    w = torch.ones((50, 16), dtype=torch.bfloat16, device="cuda")
+    h, none = w[:0], _i32([])
+    o = pkg.linear_logprobs(h, w, none)
+    assert o.logprob.shape == (0,) and o.stats.shape == (0, 2)
+    a, b = pkg.linear_logprobs_backward(h, w, none, o.stats, o.entropy, o.logprob)
+    assert a.shape == (0, 16) and b.shape == (50, 16) and not b.any()
+
+
+@pytest.mark.parametrize("typ", ["bf16", "fp16"])
+@pytest.mark.parametrize("R", [6, 300])
+def test_wrong_tokens_no_tokens_and_infinite_logits(pkg, R, typ):
+    import torch
+    rng = np.random.default_rng(4)
+    h, w = _inputs(rng, R, 64, 900, typ)
+    g, gh = _f32(rng.standard_normal(R)), _f32(rng.standard_normal(R))
+    tok = rng.integers(0, 900, R)
+    _both(pkg, h, w, None, 1.0, g, gh, typ)
+    tok[1], tok[3] = 900, 2 ** 31 - 1
+    _both(pkg, h, w, tok, 1.0, g, gh, typ)
+    tok[1], tok[3] = -1, 5
+    h[4, 7] = np.nan
+    _both(pkg, h, w, tok, 1.0, g, gh, typ)
+    h[4, 7] = np.inf  # logits of either sign
+    o = pkg.linear_logprobs(h, w, _i32(tok))
+    assert o.logprob.isnan().tolist() == o.entropy.isnan().tolist() == [r == 4 for r in range(R)]
+    a, b = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, g, gh)
+    assert a.isnan().any(1).tolist() == [r == 4 for r in range(R)] and bool(b.isnan().all())
+    # a token that is nobody's: its weights at -inf for hidden states above 0
+    h = h.abs().nan_to_num(1, 1, 1)
+    w[100] = -np.inf
+    tok[4] = 100
+    o = pkg.linear_logprobs(h, w, _i32(tok))
+    keep = torch.tensor([v for v in range(900) if v != 100], device="cuda")
+    without = pkg.linear_logprobs(h, w[keep].contiguous(), None)
+    live = _i32(tok) >= 0
+    assert float(o.logprob[4]) == -np.inf and torch.allclose(o.entropy[live], without.entropy[live], rtol=0, atol=1e-4)
+
+
+def test_large_and_peaked_logits(pkg):
+    # logits of thousands, one token far above the others, all alike
+    import torch
+    rng = np.random.default_rng(5)
+    for std in (3000.0, 40.0, 1e-4):
+        h, w = _inputs(rng, 140, 64, 1300, "bf16", std)
+        _both(pkg, h, w, rng.integers(0, 1300, 140), 1.0, _f32(rng.standard_normal(140)), _f32(0.1 * rng.standard_normal(140)), "bf16", spread=False)
+    h, w = _inputs(rng, 10, 64, 1300, "bf16", 0.0)
+    o = pkg.linear_logprobs(h, w, _i32(rng.integers(0, 1300, 10)))
+    assert torch.allclose(o.entropy, torch.full_like(o.entropy, np.log(1300)), rtol=4e-6)
+
+
+def test_gradients_of_very_different_rows_in_fp16(pkg):
+    # a row's gradient keeps its bits however small its weight beside other rows'
+    rng = np.random.default_rng(6)
+    R = 150
+    h, w = _inputs(rng, R, 64, 2000, "fp16")
+    tok = rng.integers(0, 2000, R)
+    g = rng.standard_normal(R) * 2.0 ** rng.integers(-30, 30, R)
+    g[3], g[5] = 0, 1e-35
+    gh = np.where(rng.random(R) < 0.5, 0, g * 0.1)
+    o = pkg.linear_logprobs(h, w, _i32(tok))
+    dh, _ = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, _f32(g), _f32(gh), scale=1.0, grad_weight=False)
+    k = np.abs(g) < 2.0 ** 14  # (the others' results pass fp16)
+    want = oracle.linear_grad(_np(h), _np(w), tok, g.astype(np.float32).astype(np.float64), gh.astype(np.float32).astype(np.float64))[0]
+    y = _np(dh)
+    for r in np.flatnonzero(k):
+        assert np.linalg.norm(y[r] - want[r]) <= 2 * HALF["fp16"] * np.linalg.norm(want[r]) + 8 * LEAST["fp16"] * 2, r
+
+
+@pytest.mark.parametrize("typ", ["bf16", "fp16"])
+@pytest.mark.parametrize("R", [50, 200])
+def test_strided_rows_and_given_outputs(pkg, R, typ):
+    import torch
+    rng = np.random.default_rng(7)
+    big_h, big_w = _inputs(rng, R, 160, 777, typ)
+    h, w = big_h[:, 8:136], big_w[:, 16:144]
+    tok, g, gh = rng.integers(0, 777, R), _f32(rng.standard_normal(R)), _f32(rng.standard_normal(R))
+    o = pkg.linear_logprobs(h, w, _i32(tok))
+    _check(o, h, w, tok, 1.0)
+    oh, ow = (torch.full_like(x, 7.0) for x in (big_h, big_w))
+    same = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, g, gh, grad_hidden=oh[:, 24:152], grad_weight=ow[:, 32:])
+    _check_grad(same, h, w, tok, g, gh, 1.0, typ)
+    assert (oh[:, :24] == 7).all() and (oh[:, 152:] == 7).all() and (ow[:, :32] == 7).all()
+    for wanted in ((True, False), (False, True)):
+        y = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, g, gh, grad_hidden=wanted[0], grad_weight=wanted[1])
+        assert [x is not None for x in y] == list(wanted)
+        for a, b in zip(y, same):
+            assert a is None or torch.equal(a, b)
+
+
+def test_each_weight_alone(pkg):
+    import torch
+    rng = np.random.default_rng(8)
+    h, w = _inputs(rng, 20, 64, 400, "bf16")
+    tok, g = rng.integers(0, 400, 20), _f32(rng.standard_normal(20))
+    o = pkg.linear_logprobs(h, w, _i32(tok))
+    zero = torch.zeros_like(g)
+    _check_grad(pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, None, g), h, w, tok, g, zero, 1.0, "bf16")
+    _check_grad(pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, None, g), h, w, tok, zero, g, 1.0, "bf16")
+    a, b = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, None)
+    assert not a.any() and not b.any()
+
+
+def test_gradient_against_differences_of_the_forward(pkg):
+    # steps of the weights and hidden states that bf16 holds exactly: h = 2^-4 leaves (h^2 / 6) |third derivative| and rounding / h
+    import torch
+    rng = np.random.default_rng(9)
+    h = torch.from_numpy(rng.integers(-8, 9, (2, 8)) / 8).cuda().bfloat16()
+    w = torch.from_numpy(rng.integers(-8, 9, (5, 8)) / 8).cuda().bfloat16()
+    tok, g, gh, step = _i32([1, 4]), _f32([0.75, -0.5]), _f32([0.25, 0.5]), 2.0 ** -4
+
+    def f(h, w):
+        o = pkg.linear_logprobs(h, w, tok)
+        return float((g.double() * o.logprob.double() + gh.double() * o.entropy.double()).sum())
+
+    o = pkg.linear_logprobs(h, w, tok)
+    dh, dw = pkg.linear_logprobs_backward(h, w, tok, o.stats, o.entropy, g, gh)
+    for x, dx, at in ((h, dh, (1, 3)), (h, dh, (0, 0)), (w, dw, (4, 2)), (w, dw, (0, 7))):
+        was = x[at].clone()
+        x[at] = was + step
+        up = f(h, w)
+        x[at] = was - step
+        down = f(h, w)
+        x[at] = was
+        # third derivatives along one weight: at most the rows' number times |h|^3 <= 1 times polynomials of p of size 1/2 and 1 + |log p|
+        bound = step * step / 6 * (1.25 * 0.5 + 0.75 * (1 + 20)) + 200 * U / step + 3 * HALF["bf16"] * 2
+        assert abs((up - down) / (2 * step) - float(dx[at])) <= bound
+
+
+def test_same_bits_again_on_another_stream_and_captured(pkg):
+    import torch
+    rng = np.random.default_rng(10)
+    R, d, V = 300, 128, 20001
+    h, w = _inputs(rng, R, d, V, "bf16")
+    tok, g = _i32(rng.integers(-1, V, R)), _f32(rng.standard_normal(R))
+    ws, wsb = pkg.linear_logprobs_workspace(R, d, V), pkg.linear_logprobs_workspace(R, d, V, backward=True)
+    s, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    pkg.linear_logprobs(h, w, tok, workspace=ws)
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=s):
+        o = pkg.linear_logprobs(h, w, tok, workspace=ws)
+        y = pkg.linear_logprobs_backward(h, w, tok, o.stats, o.entropy, g, g, workspace=wsb)
+    for _ in range(3):
+        h.copy_(_inputs(rng, R, d, 1, "bf16")[0])
+        tok.copy_(_i32(rng.integers(-1, V, R)))
+        graph.replay()
+        with torch.cuda.stream(s):
+            o2 = pkg.linear_logprobs(h, w, tok)
+            y2 = pkg.linear_logprobs_backward(h, w, tok, o2.stats, o2.entropy, g, g)
+        torch.cuda.synchronize()
+        for a in ("logprob", "entropy", "stats"):
+            assert torch.equal(getattr(o, a), getattr(o2, a))
+        assert torch.equal(y[0], y2[0]) and torch.equal(y[1], y2[1])
+    _check(o, h, w, tok.cpu().numpy(), 1.0)
+
+
+def test_workspace_too_small_or_elsewhere(pkg):
+    import torch
+    h, w = _inputs(np.random.default_rng(11), 200, 64, 600, "bf16")
+    tok = _i32(np.zeros(200))
+    ws = pkg.linear_logprobs_workspace(200, 64, 600)
+    for bad in (ws[:-256], ws[1:], ws.cpu()):
+        with pytest.raises(pkg.SaraError):
+            pkg.linear_logprobs(h, w, tok, workspace=bad)
+    o = pkg.linear_logprobs(h, w, tok, workspace=ws)
+    with pytest.raises(pkg.SaraError):  # (in the operand's place)
+        pkg.linear_logprobs_backward(h, w, tok, o.stats, o.entropy, o.logprob, grad_hidden=h)
+    with pytest.raises(pkg.SaraError):
+        pkg.linear_logprobs_backward(h, w, tok, o.stats, o.entropy, o.logprob, grad_weight=w)
+    assert not torch.isnan(o.logprob).any()
+
+
+def test_alike_with_scores_of_stored_logits(pkg):
+    """The policy loss of a tiny model's rollouts, by way of the logits and without them."""
+    import torch
+    m = synth.WORKLOADS["tiny"].model
+    rng = np.random.default_rng(12)
+    R = 48
+    h, w = _inputs(rng, R, m.d_model, m.vocab, "bf16", 3.0)
+    z = h.float() @ w.float().t()  # exact products, sums of 128 of them in fp32
+    tok = _i32(rng.integers(-1, m.vocab, R))
+    a, b = pkg.logprobs(z, tok), pkg.linear_logprobs(h, w, tok)
+    e = 2 * float(_logit_error(_np(h), _np(w), 1.0).max()) * 2 + 2 * _sum_error(m.vocab)
+    assert float((a.logprob - b.logprob).abs().max()) <= e and float((a.entropy - b.entropy).abs().max()) <= 20 * e
+    adv = _f32(rng.standard_normal(R))
+    dz = pkg.logprobs_backward(z, tok, a.stats, a.entropy, adv, adv).double()
+    dh, dw = pkg.linear_logprobs_backward(h, w, tok, b.stats, b.entropy, adv, adv)
+    assert float((dh.double() - dz @ w.double()).norm()) <= 1.5 * HALF["bf16"] * float((dz @ w.double()).norm())
+    assert float((dw.double() - dz.t() @ h.double()).norm()) <= 1.5 * HALF["bf16"] * float((dz.t() @ h.double()).norm())
+
+
+def test_weights_past_32_bits(pkg):
+    # the last tokens' weights, and their gradients, begin beyond 2^32 bytes
+    import torch
+    V, d = 2 ** 19 + 300, 4352
+    h = torch.full((2, d), 2.0 ** -6, dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros((V, d), dtype=torch.bfloat16, device="cuda")
+    w[V - 1] = 0.25   # logit 17
+    w[5] = 0.125      # 8.5
+    tok = _i32([V - 1, 5])
+    o = pkg.linear_logprobs(h, w, tok)
+    S = 1 + np.exp(-8.5) + (V - 2) * np.exp(-17.0)
+    assert abs(float(o.logprob[0]) + np.log(S)) < 1e-4 and abs(float(o.logprob[1]) + 8.5 + np.log(S)) < 1e-4
+    g = _f32([1.0, 0.0])
+    dh, dw = pkg.linear_logprobs_backward(h, w, tok, o.stats, o.entropy, g)
+    p = 1 / S
+    assert abs(float(dw[V - 1, d - 1]) - (1 - p) * 2.0 ** -6) <= 2.0 ** -6 * 2.0 ** -7 * (1 - p) + 1e-9
+    assert abs(float(dw[V - 2, 0]) + p * np.exp(-17.0) * 2.0 ** -6) <= 2.0 ** -7 * p * np.exp(-17.0) * 2.0 ** -6
+    want = (1 - p) * 0.25 - p * np.exp(-8.5) * 0.125
+    assert abs(float(dh[0, 0]) - want) <= 2.0 ** -6 * abs(want) and float(dh[1].abs().max()) == 0
