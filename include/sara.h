@@ -418,6 +418,25 @@ SARA_API int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_se
                                        int64_t q_stride, const int32_t *ctx, const int32_t *first, void *out, float *lse,
                                        int32_t type, int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * The same for groups of sequences whose first positions are the same (the rollouts of a prompt): group g is the sequences
+ * group_start[g] .. group_start[g + 1] - 1 (group_start [n_groups + 1], non-decreasing, 0 .. n_seq; n_groups at most n_seq; sequences of no group attend by
+ * themselves), and its positions p < prefix[g] are read once for all of its queries, through the table row of its first sequence (whose own
+ * length does not matter for that); positions from prefix[g] on are each sequence's own.  A prefix may end anywhere in a block, and a sequence in
+ * its prefix (ctx[i] <= prefix[g], or 0).  Everything else as sara_attention_decode_kv8, but: probabilities of shared positions times their
+ * values' scale are held in fp16, 11 bits, or within 2^-31 of the query's largest such product.
+ * group_start that falls or leaves 0 .. n_seq makes every row NaN, prefix[g] outside [0, 128 * max_blocks] the rows of its group, a block id outside
+ * [0, n_blocks) the rows that attend to the block; each sets *status.
+ * workspace: sara_attention_shared_kv8_workspace_bytes(...) bytes (for up to these sizes), 256-byte aligned, all zero on first use and
+ * left zero where it has to be; calls that share one must not overlap.
+ */
+SARA_API size_t sara_attention_shared_kv8_workspace_bytes(int32_t n_seq, int32_t n_groups, int32_t n_heads, int32_t n_kv_heads,
+                                                          int32_t head_dim);
+SARA_API int sara_attention_shared_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_t n_heads, const void *q, int64_t q_stride,
+                                       const int32_t *ctx, const int32_t *first, int32_t n_groups, const int32_t *group_start,
+                                       const int32_t *prefix, void *out, float *lse, int32_t type, int32_t *status, void *workspace,
+                                       size_t workspace_bytes, void *stream);
+
 /* ---------------------------------------------------------------------------------------
  * Scoring of sampled tokens, next to sara_sample: log-probabilities of given tokens under softmax(logits), with each row's
  * entropy and top alternatives, and the gradient of both.  Device pointers, not waited for, nothing allocated.

@@ -15,7 +15,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT_DIR, "libsara.so")
-SOURCES = ["engine.cu", "ops.cu", "ops_kv8.cu", "ops_logprob.cu", "ops_linear.cu"]
+SOURCES = ["engine.cu", "ops.cu", "ops_kv8.cu", "ops_logprob.cu", "ops_linear.cu", "ops_shared.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",

@@ -66,6 +66,7 @@ struct AttnKv8Params {
     int64_t q_stride;
     const int32_t *ctx, *first;
     uint16_t *out;
+    float *out32;  // written instead of out where it is not null
     float *lse;
     int32_t *status;
     int *count;   // [share][2][levels] arrivals at a join, kept at its first state; left zero
@@ -133,6 +134,10 @@ __device__ __forceinline__ AttnKv8Row attn_kv8_row(const AttnKv8Params &p, int i
 template <int HD>
 __device__ __forceinline__ void attn_kv8_put(const AttnKv8Params &p, int row, int head, int i, float y0, float y1) {
     const int dim = HD / 8 * (i % 16 / 2) + i / 16 * 2;
+    if (p.out32) {
+        *reinterpret_cast<float2 *>(p.out32 + ((int64_t)row * p.H + head) * HD + dim) = make_float2(y0, y1);
+        return;
+    }
     *reinterpret_cast<uint32_t *>(p.out + ((int64_t)row * p.H + head) * HD + dim) =
         p.type == SARA_BF16 ? pack2<SARA_BF16>(y0, y1) : pack2<SARA_FP16>(y0, y1);
 }
@@ -318,7 +323,10 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             const float y = r.bad ? nan : 0.f;
             const uint32_t y2 = p.type == SARA_BF16 ? pack2<SARA_BF16>(y, y) : pack2<SARA_FP16>(y, y);
             uint32_t *o = reinterpret_cast<uint32_t *>(p.out + (int64_t)i * p.H * HD);
-            for (int e = tid; e < p.H * HD / 2; e += kAttnKv8Threads) o[e] = y2;
+            for (int e = tid; e < p.H * HD / 2; e += kAttnKv8Threads) {
+                if (p.out32) *reinterpret_cast<float2 *>(p.out32 + (int64_t)i * p.H * HD + 2 * e) = make_float2(y, y);
+                else o[e] = y2;
+            }
             if (p.lse)
                 for (int e = tid; e < p.H; e += kAttnKv8Threads) p.lse[(int64_t)i * p.H + e] = r.bad ? nan : -INFINITY;
             if (r.bad && tid == 0) kv8_report(p.status);
@@ -649,7 +657,11 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                 const int hh = 2 * t + e;
                 const float M = e ? m1 : m0, L = e ? l1 : l0, u = e ? u1 : u0, inv = 1.f / L;
                 if (hh >= G) continue;
-                if (whole) {
+                if (whole && p.out32) {
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) attn_kv8_put<HD>(p, me.row, me.h * G + hh, 16 * j + 2 * g, o[j][e] * u * inv, o[j][2 + e] * u * inv);
+                    if (p.lse && g == 0) p.lse[(int64_t)me.row * p.H + me.h * G + hh] = (M - kAttnKv8Shift + log2f(L)) * 0.69314718f;
+                } else if (whole) {
                     uint32_t y[NT];
 #pragma unroll
                     for (int j = 0; j < NT; ++j)
@@ -731,6 +743,8 @@ inline int attn_kv8_warps(int n, int kvh, int hd, int max_blocks) {
     return (int64_t)n * kvh >= kAttnKv8Units && attn_kv8_entries(n, kvh, max_blocks, attn_kv8_step(hd, 1)) <= INT32_MAX ? 1 : kAttnKv8Warps;
 }
 inline size_t attn_kv8_count_bytes() { return kAttnKv8MaxShares * 2 * kAttnKv8Levels * sizeof(int); }
+// The kernel for p's operands, shared with the attention behind a common prefix
+void attn_kv8_launch(const sara_kv8_cache *cache, const AttnKv8Params &p, int warps, cudaStream_t s);
 inline size_t attn_kv8_workspace(int hd, int warps) {
     return attn_kv8_count_bytes() + (size_t)kAttnKv8MaxShares / warps * 2 * attn_kv8_state(hd) * sizeof(float);
 }

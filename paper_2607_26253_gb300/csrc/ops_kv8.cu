@@ -10,36 +10,11 @@
 #include "attn_kv8.cuh"
 #include "host_util.h"
 #include "kv8.cuh"
+#include "kv8_host.h"
 
 using namespace sara;
 
 namespace {
-
-bool misaligned(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) != 0; }
-
-// (a batch of no sequences has no table)
-bool cache_ok(const sara_kv8_cache *c, int n_seq) {
-    return c && c->codes && c->scales && (c->table || n_seq == 0) && c->n_blocks >= 1 && c->max_blocks >= 1 &&
-           c->max_blocks <= INT32_MAX / SARA_KV8_PAGE && c->table_stride >= c->max_blocks && c->n_kv_heads >= 1 &&
-           c->n_kv_heads <= 65536 && (c->head_dim == 32 || c->head_dim == 64 || c->head_dim == 128) &&
-           (c->format == SARA_KV8_E4M3 || c->format == SARA_KV8_INT8) && !misaligned(c->codes, 16) && !misaligned(c->scales, 4);
-}
-
-Kv8Cache device_cache(const sara_kv8_cache *c) {
-    return {c->codes, c->scales, c->table, c->table_stride, c->n_blocks, c->max_blocks, c->n_kv_heads};
-}
-
-// f.template operator()<head_dim, format>()
-template <typename F>
-void by_shape(const sara_kv8_cache *c, F f) {
-    auto with = [&](auto hd) {
-        if (c->format == SARA_KV8_E4M3) f(hd, std::integral_constant<int, SARA_KV8_E4M3>());
-        else f(hd, std::integral_constant<int, SARA_KV8_INT8>());
-    };
-    if (c->head_dim == 32) with(std::integral_constant<int, 32>());
-    else if (c->head_dim == 64) with(std::integral_constant<int, 64>());
-    else with(std::integral_constant<int, 128>());
-}
 
 // Rows of n_kv_heads * head_dim elements of `size` bytes, `stride` elements apart
 bool rows_ok(const sara_kv8_cache *c, const void *p, int64_t stride, int total) {
@@ -53,6 +28,19 @@ unsigned warp_ctas(int64_t warps) {
 }
 
 }  // namespace
+
+// (declared in attn_kv8.cuh)
+void sara::attn_kv8_launch(const sara_kv8_cache *cache, const AttnKv8Params &p, int warps, cudaStream_t s) {
+    // as many CTAs as fit, fewer where there are not as many entries
+    const int64_t entries = attn_kv8_entries(p.n, cache->n_kv_heads, cache->max_blocks, attn_kv8_step(cache->head_dim, warps));
+    const unsigned ctas = (unsigned)std::min<int64_t>(std::min(kAttnKv8SmCtas * sm_count(), kAttnKv8MaxCtas), (entries + kAttnKv8Warps / warps - 1) / (kAttnKv8Warps / warps));
+    by_shape(cache, [&](auto hd, auto fmt) {
+        const auto kern = warps == 1 ? attn_kv8_kernel<hd.value, fmt.value, 1> : attn_kv8_kernel<hd.value, fmt.value, kAttnKv8Warps>;
+        static_assert(attn_kv8_smem(hd.value) <= 48 * 1024, "more would have to be asked for");
+        kern<<<ctas, kAttnKv8Threads, attn_kv8_smem(hd.value), s>>>(p);
+    });
+    CK(cudaGetLastError());
+}
 
 extern "C" {
 
@@ -132,16 +120,7 @@ int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
         p.count = static_cast<int *>(workspace);
         p.part = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + attn_kv8_count_bytes());
         p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)cache->head_dim));
-        cudaStream_t s = static_cast<cudaStream_t>(stream);
-        // as many CTAs as fit, fewer where there are not as many entries
-        const int64_t entries = attn_kv8_entries(n_seq, cache->n_kv_heads, cache->max_blocks, attn_kv8_step(hd, warps));
-        const unsigned ctas = (unsigned)std::min<int64_t>(std::min(kAttnKv8SmCtas * sm_count(), kAttnKv8MaxCtas), (entries + kAttnKv8Warps / warps - 1) / (kAttnKv8Warps / warps));
-        by_shape(cache, [&](auto hd, auto fmt) {
-            const auto kern = warps == 1 ? attn_kv8_kernel<hd.value, fmt.value, 1> : attn_kv8_kernel<hd.value, fmt.value, kAttnKv8Warps>;
-            static_assert(attn_kv8_smem(hd.value) <= 48 * 1024, "more would have to be asked for");
-            kern<<<ctas, kAttnKv8Threads, attn_kv8_smem(hd.value), s>>>(p);
-        });
-        CK(cudaGetLastError());
+        attn_kv8_launch(cache, p, warps, static_cast<cudaStream_t>(stream));
     });
 }
 

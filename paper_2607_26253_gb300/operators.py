@@ -198,6 +198,52 @@ def attention_decode_kv8(q, codes, scales, table, ctx, first=None, workspace=Non
     return out
 
 
+def attention_shared_kv8_workspace(n_seq: int, n_groups: int, n_heads: int, n_kv_heads: int, head_dim: int, device="cuda"):
+    """The scratch of attention_shared_kv8 for up to these sizes, to be kept from call to call (zeroed; calls that
+    share it must not overlap)."""
+    if torch is None:
+        _start()
+    size = _lib.sara_attention_shared_kv8_workspace_bytes(n_seq, n_groups, n_heads, n_kv_heads, head_dim)
+    return torch.zeros(max(size, 256), dtype=torch.uint8, device=device)
+
+
+def attention_shared_kv8(q, codes, scales, table, ctx, group_start, prefix, first=None, workspace=None, out=None, lse=None, status=None):
+    """attention_decode_kv8 for groups of sequences whose first positions are the same (see sara_attention_shared_kv8): sequences
+    group_start[g] .. group_start[g + 1] - 1 share positions p < prefix[g], which are read once, through the table row of the first of
+    them.  group_start [n_groups + 1] and prefix [n_groups] int32; the rest as there."""
+    cache, n, kvh, hd, dev = _kv8(codes, scales, table)
+    typ, shape = _types.get(q.dtype, 2), q.shape
+    if typ == 2 or len(shape) != 3 or shape[0] != n or shape[2] != hd or q.get_device() != dev:
+        _refuse(f"q must be bf16 or fp16, [{n}, heads, {hd}] on the cache's device")
+    H = shape[1]
+    row, head, step = q.stride()
+    if step != 1 or (head != hd and H != 1):
+        _refuse("q must have each row's heads side by side")
+    at_ctx = _vector(ctx, _int32, n, dev, "ctx")
+    if prefix.dim() != 1 or prefix.numel() > n:
+        _refuse("prefix must be int32 [n_groups], of at most as many groups as sequences")
+    groups = prefix.numel()
+    at_start, at_prefix = _vector(group_start, _int32, groups + 1, dev, "group_start"), _vector(prefix, _int32, groups, dev, "prefix")
+    at_first = None if first is None else _vector(first, _int32, n, dev, "first")
+    at_lse = None if lse is None else _matrix(lse, _fp32, (n, H), dev, "lse")
+    at_status = None if status is None else _vector(status, _int32, 1, dev, "status")
+    at_out = None if out is None else _matrix(out, q.dtype, shape, dev, "out")
+    if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
+        _refuse("workspace must be contiguous, on the cache's device")
+    if dev < 0 or dev != _device():
+        return _elsewhere(dev, attention_shared_kv8, q, codes, scales, table, ctx, group_start, prefix, first, workspace, out, lse, status)
+    if out is None:
+        out = q.new_empty(shape)
+        at_out = out.data_ptr()
+    if workspace is None:
+        workspace = attention_shared_kv8_workspace(n, groups, H, kvh, hd, q.device)
+    rc = _lib.sara_attention_shared_kv8(cache, n, H, q.data_ptr(), row, at_ctx, at_first, groups, at_start, at_prefix, at_out, at_lse, typ,
+                                        at_status, workspace.data_ptr(), workspace.nbytes, _stream(dev))
+    if rc:
+        _check(rc)
+    return out
+
+
 @dataclass
 class LogProbs:
     logprob: object            # [R] fp32, of the given tokens (None without tokens)

@@ -23,7 +23,8 @@ EXPORTED = ("sara_create", "sara_collect_step", "sara_teacher_force", "sara_last
             "sara_attention_decode", "sara_sample", "sara_profile", "sara_gemm_bf16_static", "sara_set_limits",
             "sara_abi_version", "sara_kv8_write", "sara_kv8_read", "sara_attention_kv8_workspace_bytes",
             "sara_attention_decode_kv8", "sara_logprobs", "sara_logprobs_backward",
-            "sara_linear_logprobs_workspace_bytes", "sara_linear_logprobs", "sara_linear_logprobs_backward")
+            "sara_linear_logprobs_workspace_bytes", "sara_linear_logprobs", "sara_linear_logprobs_backward",
+            "sara_attention_shared_kv8_workspace_bytes", "sara_attention_shared_kv8")
 ABI_VERSION = 3
 
 c_p = ctypes.c_void_p
@@ -148,6 +149,10 @@ def load(path: str = LIB_PATH):
     lib.sara_linear_logprobs_backward.argtypes = [c_p, i64, c_p, i64, i32, i32, i32, i32, c_p, f32, c_p, c_p, c_p, c_p, c_p, i64, c_p,
                                                   i64, c_p, size, c_p]
     lib.sara_linear_logprobs_backward.restype = ctypes.c_int
+    lib.sara_attention_shared_kv8_workspace_bytes.argtypes = [i32] * 5
+    lib.sara_attention_shared_kv8_workspace_bytes.restype = size
+    lib.sara_attention_shared_kv8.argtypes = [cache_p, i32, i32, c_p, i64, c_p, c_p, i32, c_p, c_p, c_p, c_p, i32, c_p, c_p, size, c_p]
+    lib.sara_attention_shared_kv8.restype = ctypes.c_int
     lib.sara_abi_version.argtypes = []
     lib.sara_abi_version.restype = ctypes.c_int
     if lib.sara_abi_version() != ABI_VERSION:
