@@ -206,7 +206,7 @@ struct SharedWalk {
 
 // ------------------------------------------------------------------------------- prefix
 struct SharedSmem {
-    uint64_t full[kSharedSlots], empty[kSharedSlots], scales[4], q_full[2], s_full[2], p_full[2], pv_done[2];
+    uint64_t full[kSharedSlots], empty[kSharedSlots], scales[4], q_full[2], s_full[2], p_full[2], pv_done[2], o_full[2];
     float scale[4][8];       // of a page: K's four, V's four
     uint32_t nan[4][kSharedConv];  // blocks of a page in which a warp met a NaN among V's codes
     uint32_t tmem_base;
@@ -220,6 +220,29 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, ui
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
         "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
         : "memory");
+}
+// 32 or 16 columns of a lane; the wait is part of the instruction, so that nothing uses the values before it
+__device__ __forceinline__ void tmem_load32(uint32_t taddr, float (&v)[32]) {
+    uint32_t r[32];
+    __syncwarp();
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_load16(uint32_t taddr, float (&v)[16]) {
+    uint32_t r[16];
+    __syncwarp();
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];\n\ttcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[16]) {
     __syncwarp();
@@ -260,6 +283,7 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
             mbar_init(&S.s_full[s], 1);
             mbar_init(&S.p_full[s], 4);
             mbar_init(&S.pv_done[s], 1);
+            mbar_init(&S.o_full[s], 1);
         }
         S.abort = 0;
         fence_mbar_init();
@@ -435,6 +459,7 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
                         tc_mma_ts(tmem + 256 + q * 128, tmem + buf * 128 + k * 8, sdesc_128(b + k * 2048, kSharedQ * 128), idesc_o, x > 0 || k > 0);
                     if (q == nq - 1) tc_commit(&S.empty[sv]);
                     tc_commit(&S.pv_done[q]);
+                    if (x + 1 == (uint32_t)s.count) tc_commit(&S.o_full[q]);
                 }
                 __syncwarp();
                 ++done[q];
@@ -463,7 +488,7 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
         const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), o_at = lanes + 256 + qt * 128;
         SharedWalk w(p, from, to);
         SharedSegment s;
-        uint32_t j0 = 0, tile = 0;  // pages before; pages of this tile of queries
+        uint32_t j0 = 0, tile = 0, unit = 0;  // pages before; pages and units of this tile of queries
         bool ok = true;
         auto wait = [&](uint64_t *bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity & 1, err) && !*ab); };
         while (ok && w.next<TQ>(s)) {
@@ -522,8 +547,8 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
             for (int x = 0; x < s.count && ok; ++x, ++tile) {
                 const uint32_t j = j0 + x, buf = QT == 1 ? j & 1 : (uint32_t)qt;
                 const uint32_t s_at = lanes + buf * 128;
-                wait(&S.scales[j & 3], j >> 2);
                 wait(&S.s_full[buf], QT == 1 ? j >> 1 : tile);
+                wait(&S.scales[j & 3], j >> 2);
                 if (!ok) break;
                 tc_fence_after();
                 if (any) {
@@ -545,7 +570,7 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
                         float v[32];
-                        tmem_ld_32x32b_x32(s_at + 32 * b, v);
+                        tmem_load32(s_at + 32 * b, v);
                         if (masked) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e) v[e] = p0 + 32 * b + e >= lo && p0 + 32 * b + e < hi ? v[e] : -INFINITY;
@@ -570,14 +595,11 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
                             tc_fence_after();
 #pragma unroll 1
                             for (int d = 0; d < HD; d += 16) {
-                                uint64_t o2[8];
-                                tmem_ld_32x32b_x16(o_at + d, o2);
+                                float o[16];
+                                tmem_load16(o_at + d, o);
                                 uint32_t y[16];
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    y[2 * e] = __float_as_uint(__uint_as_float((uint32_t)o2[e]) * f);
-                                    y[2 * e + 1] = __float_as_uint(__uint_as_float((uint32_t)(o2[e] >> 32)) * f);
-                                }
+                                for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(o[e] * f);
                                 tmem_st_x16(o_at + d, y);
                             }
                             tmem_wait_st();
@@ -587,7 +609,7 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
                         float v[32];
-                        tmem_ld_32x32b_x32(s_at + 32 * b, v);
+                        tmem_load32(s_at + 32 * b, v);
                         const float F = ex2(fminf(m - R + ev[b] + kSharedShift, 126.f)) * (vs[b] * pow2f(-(int)ev[b]));
                         uint32_t h[16];
 #pragma unroll
@@ -615,8 +637,8 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&S.p_full[buf]);
             }
-            if (!ok) break;
-            wait(&S.pv_done[qt], tile - 1);
+            // (not pv_done, which may be two pages behind a warp that has just left the last: its parity would not tell)
+            wait(&S.o_full[qt], unit++);
             if (!ok) break;
             tc_fence_after();
             if (any) {
@@ -625,13 +647,11 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
                 const float f = ex2(fminf(fmaxf(R - m - kSharedShift, -1e4f), 126.f));
 #pragma unroll 1
                 for (int d = 0; d < HD; d += 16) {
-                    uint64_t o2[8];
-                    tmem_ld_32x32b_x16(o_at + d, o2);
+                    float y[16];
+                    tmem_load16(o_at + d, y);
                     if (live) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e)
-                            *reinterpret_cast<float2 *>(o + 2 + d + 2 * e) =
-                                make_float2(__uint_as_float((uint32_t)o2[e]) * f, __uint_as_float((uint32_t)(o2[e] >> 32)) * f);
+                        for (int e = 0; e < 16; e += 2) *reinterpret_cast<float2 *>(o + 2 + d + e) = make_float2(y[e] * f, y[e + 1] * f);
                     }
                 }
                 if (live) *reinterpret_cast<float2 *>(o) = make_float2(m, l);

@@ -81,7 +81,8 @@ def test_edges(pkg, H, kvh, hd, fmt, typ):
 # few and many queries of a group: one tile, two, several; long prefixes split over CTAs, short ones many to a CTA
 @pytest.mark.parametrize("fmt,typ", [("e4m3", "bf16"), ("int8", "fp16")])
 @pytest.mark.parametrize("sizes,H,kvh,hd,blocks", [([64], 8, 1, 128, 3), ([16, 17], 8, 1, 128, 2), ([33], 16, 2, 64, 40), ([90, 2], 6, 1, 128, 5), ([3] * 40, 4, 2, 64, 3),
-                                                   ([130], 4, 1, 32, 9), ([2, 200, 2], 2, 1, 128, 4), ([8] * 12, 12, 2, 128, 12), ([40] * 5, 28, 4, 128, 6)])
+                                                   ([130], 4, 1, 32, 9), ([2, 200, 2], 2, 1, 128, 4), ([8] * 12, 12, 2, 128, 12), ([40] * 5, 28, 4, 128, 6),
+                                                   ([42] * 6, 16, 8, 128, 40), ([20] * 5, 24, 4, 128, 60), ([69, 30, 128], 2, 2, 32, 170), ([40] * 9, 32, 8, 64, 30)])
 def test_group_sizes(pkg, sizes, H, kvh, hd, blocks, fmt, typ):
     import torch
     rng = np.random.default_rng(sum(sizes) + hd)
