@@ -1,7 +1,7 @@
 // Log-probabilities of given tokens under softmax(scale H W^T), H [R][d] hidden states, W [V][d] the vocabulary's weights, with the
 // entropy, and the gradient of both with respect to H and W.  No logits are kept:
-//   forward:  the logits of a tile of rows and tokens are the accumulator of one chain of tensor-core products; its epilogue leaves
-//             a row's maximum a, s = sum 2^y and t = sum 2^y y with y = (acc - a) scale log2(e), which a second kernel joins over the tiles
+//   forward:  the logits of a tile of rows and tokens are the accumulator of tensor-core products; its epilogue leaves a row's maximum
+//             a, sum 2^y and sum 2^y y with y = (acc - a) scale log2(e), which a second kernel joins over the tiles
 //   gradient: the vocabulary goes by in pieces.  A piece's logits are made again, its dZ = g (1[v = token] - p) - g' p (log p + H),
 //             [R][piece], is stored in the operands' type, and feeds both products, dH += dZ W and dW = dZ^T H.
 // Bound by the tensor cores from some 300 rows on, by reading W below.
@@ -13,9 +13,17 @@
 // Rows of padding (token < 0) are left out: the live rows are gathered first, so that they cost nothing and their contents,
 // whatever they are, reach nothing.
 //
-// Warp roles (320 threads): warp 0 producer, warp 1 MMA issuer and tensor-memory owner, warps 2..5 and 6..9 the epilogues of
-// alternate tiles (each of one of the two accumulators; a thread has a row).
+// The tensor core cuts its sums off: about half a step of fp32 each 16 products, all towards zero.  A logit's products are therefore
+// summed in parts, which the epilogue adds.
+// dZ enters the products in 16 bits.  Its largest element by far is mostly the token's own: what that one's rounding left off is
+// kept (delta) and added to both gradients in fp32.
+//
+// Warp roles (320 threads): warp 0 producer, warp 1 MMA issuer and tensor-memory owner, warps 2..9 epilogue (warp w: the rows of
+// tensor-memory lanes 32 (w % 4) ..): of the scores every tile, 128 columns a thread, which are in registers before the accumulator is given
+// back; of the others warps 2..5 and 6..9 alternate tiles, one of the two accumulators each.
 #pragma once
+#include <type_traits>
+
 #include "device_common.cuh"
 #include "host_util.h"
 #include "kv8.cuh"
@@ -61,7 +69,10 @@ struct LinParams {
     const float *stats, *entropy, *glp, *gent;
     uint16_t *dz;      // [rows_cap][piece]
     int piece, v0, cols;  // columns of dZ; the piece's first token and tokens
+    float *delta;      // [rows_cap]: what rounding took from dZ at the row's token
     // LIN_GRAD
+    const int *tokc;   // [rows_cap]: the compact rows' tokens
+    const uint16_t *low;  // [rows_cap][d]: the rows that dW's product has
     float *acc;        // [split][rows_cap][d]
     int splits, first; // first: the first piece
     uint16_t *dw;      // or null
@@ -69,10 +80,21 @@ struct LinParams {
     bool dh;
 };
 
+// Chunks of a part of a logit's sum: with two CTAs a tile's epilogue has no time for more parts
+__host__ __device__ constexpr int lin_part(int ctas) { return ctas == 2 ? 8 : 1; }
+constexpr int kLinHits = 256;  // rows of a quarter whose tokens are in a tile of dW and whose delta is added there (the first ones)
+
 struct LinSmem {
     uint64_t full[6], empty[6], acc_full[2], acc_empty[2], drain;
     uint32_t tmem_base;
-    int abort;
+    int abort, stop[2];                  // stop: the epilogue's, for two tiles in turn
+};
+struct LinScoreSmem {
+    float sums[2][3][kLinRows];          // of the second half's columns, for two tiles in turn
+};
+struct LinGradSmem {
+    int found[2][4];                     // of each epilogue warp's quarter of the rows
+    int2 hit[2][4][kLinHits];            // place in the tile, row
 };
 
 // ------------------------------------------------------------------------------- PTX for a pair of CTAs
@@ -230,24 +252,43 @@ struct LinWork {
 };
 
 // ------------------------------------------------------------------------------- epilogues
-// A row's maximum and sums over the tile's logits (see above)
+// A row's maximum a and sums over some of its logits, s and t without one maximum's own terms (1 and 0), so that the logarithm of
+// 1 + s keeps what is small beside the 1 of a row with one likely token
 struct LinSums {
-    float a = -3.4028235e38f, s = 0.f, t = 0.f;
+    float a = -3.4028235e38f, s = -1.f, t = 0.f;  // of none
     // (the bound keeps 0 times infinity out where the maxima are far apart)
-    __device__ __forceinline__ void rebase(float n, float c) {
-        const float y = fmaxf((a - n) * c, -1e4f), f = exp2_approx(y);
-        t = (t + s * y) * f;
-        s *= f;
-        a = n;
-    }
     __device__ __forceinline__ void join(float b, float sb, float tb, float c) {
-        if (b > a) rebase(b, c);
-        const float y = fmaxf((b - a) * c, -1e4f), f = exp2_approx(y);
-        s = fmaf(sb, f, s);
-        t = fmaf(fmaf(sb, y, tb), f, t);
+        const bool up = b > a;
+        const float hi = up ? b : a, lo = up ? a : b, s0 = up ? sb : s, s1 = 1.f + (up ? s : sb), t0 = up ? tb : t, t1 = up ? t : tb;
+        const float y = fmaxf((lo - hi) * c, -1e4f), f = exp2_approx(y);
+        a = hi;
+        s = fmaf(s1, f, s0);
+        t = fmaf(fmaf(s1, y, t1), f, t0);
     }
 };
 
+// 32 columns of a lane, or their sum with v; the wait is part of the instruction, so that nothing uses the values before it
+template <bool ADD>
+__device__ __forceinline__ void lin_tmem_load(uint32_t taddr, float *v) {
+    uint32_t r[32];
+    __syncwarp();
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+          "=r"(r[31])
+        : "r"(taddr)
+        : "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = ADD ? v[i] + __uint_as_float(r[i]) : __uint_as_float(r[i]);
+}
+
+template <int TYPE>
+__device__ __forceinline__ float lin_float(uint16_t x) {
+    return TYPE == SARA_BF16 ? bf16_to_f32(x) : f16_to_f32(x);
+}
 template <int TYPE>
 __device__ __forceinline__ uint16_t lin_round(float x) {
     return TYPE == SARA_BF16 ? f32_to_bf16(x) : __half_as_ushort(__float2half_rn(x));
@@ -258,9 +299,10 @@ __global__ void __launch_bounds__(kLinThreads, 1)
 lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmA2,
            const __grid_constant__ CUtensorMap tmB2, LinParams p) {
     constexpr int STAGES = lin_stages(CTAS), STAGE = lin_stage_bytes(CTAS), A_BYTES = kLinRows * kLinK * 2;
-    constexpr int BN = kLinCols / CTAS;  // a CTA's share of B's rows
+    constexpr int BN = kLinCols / CTAS, PART = lin_part(CTAS);  // a CTA's share of B's rows
     extern __shared__ uint8_t smem_raw[];
     __shared__ LinSmem S;
+    __shared__ std::conditional_t<MODE == LIN_GRAD, LinGradSmem, LinScoreSmem> E;
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CTAS == 2 ? (int)cluster_rank() : 0;
@@ -272,10 +314,10 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         }
         for (int a = 0; a < 2; ++a) {
             mbar_init(&S.acc_full[a], 1);
-            mbar_init(&S.acc_empty[a], 4 * CTAS);
+            mbar_init(&S.acc_empty[a], (MODE == LIN_SCORE ? 8 : 4) * CTAS);
         }
         mbar_init(&S.drain, 1);
-        S.abort = 0;
+        S.abort = S.stop[0] = S.stop[1] = 0;
         fence_mbar_init();
     }
     if (warp == 1) lin_tmem_alloc<CTAS>(&S.tmem_base, 512);
@@ -347,20 +389,26 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         uint32_t ph = 0;
         bool ok = true;
         const uint32_t formats = 1u << 4 | (TYPE == SARA_BF16 ? 1u << 7 | 1u << 10 : 0u) | (uint32_t)(kLinRows * CTAS >> 4) << 24;
+        int it = 0;  // parts
 #pragma unroll 1
         for (int i = 0; rank == 0 && i < work.count && ok; ++i) {
             LinJob j;
             if (!work.job(p, i, j)) break;
-            const int a = i & 1;
-            if (i >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_empty[a], (uint32_t)(((i >> 1) - 1) & 1), err) && !*ab);
-            if (!ok) break;
-            tc_fence_after();
             const bool mn_a = MODE == LIN_GRAD && j.kind == 1, mn_b = MODE == LIN_GRAD;
-            const uint32_t dacc = tmem + (uint32_t)(a * kLinCols);
             const uint32_t idesc = formats | (uint32_t)mn_a << 15 | (uint32_t)mn_b << 16 | (uint32_t)(j.n >> 3) << 17;
             const uint32_t step_a = mn_a ? 2048 : 32, step_b = mn_b ? 2048 : 32;
+            uint32_t dacc = 0;
+            int a = 0;
 #pragma unroll 1
             for (int k = j.k0; k < j.k1; ++k) {
+                const bool begins = MODE == LIN_SCORE ? k % PART == 0 : k == j.k0, ends = k + 1 == j.k1 || (MODE == LIN_SCORE && (k + 1) % PART == 0);
+                if (begins) {
+                    a = it & 1;
+                    dacc = tmem + (uint32_t)(a * kLinCols);
+                    if (it >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_empty[a], (uint32_t)(((it >> 1) - 1) & 1), err) && !*ab);
+                    if (!ok) break;
+                    ++it;
+                }
                 ok = __all_sync(0xffffffffu, mbar_wait(&S.full[s], ph, err) && !*ab);
                 if (!ok) break;
                 tc_fence_after();
@@ -369,9 +417,9 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
                         lin_mma<CTAS>(dacc, sdesc_sw128(at + kk * step_a, kLinK * 128, 1024), sdesc_sw128(at + A_BYTES + kk * step_b, kLinK * 128, 1024),
-                                      idesc, k > j.k0 || kk > 0);
+                                      idesc, !begins || kk > 0);
                     lin_commit<CTAS>(&S.empty[s]);
-                    if (k + 1 == j.k1) lin_commit<CTAS>(&S.acc_full[a]);
+                    if (ends) lin_commit<CTAS>(&S.acc_full[a]);
                 }
                 __syncwarp();
                 if (++s == STAGES) {
@@ -388,23 +436,111 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
     } else {
         // ------------------------------------------------------------ epilogues
         const int quarter = warp & 3, mine = (warp - 2) >> 2, lrow = quarter * 32 + lane;
-        const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(mine * kLinCols);
-        const uint32_t empty = CTAS == 2 ? cluster_addr(&S.acc_empty[mine], 0) : smem_u32(&S.acc_empty[mine]);
-        const float c = p.scale * kLog2e;
+        const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16);
         bool ok = true;
+        auto give = [&](int a) {  // the accumulator back
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (CTAS == 2) mbar_arrive_cluster(cluster_addr(&S.acc_empty[a], 0));
+                else mbar_arrive(&S.acc_empty[a]);
+            }
+        };
+        auto wait = [&](int a, int use) {
+            ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_full[a], (uint32_t)(use & 1), err) && !*ab);
+            tc_fence_after();
+        };
+        if constexpr (MODE == LIN_SCORE) {
+            const float c = p.scale * kLog2e;
+            const int c0 = mine * 128;
+            int it = 0;
 #pragma unroll 1
-        for (int i = mine; i < work.count && ok; i += 2) {
-            LinJob j;
-            if (!work.job(p, i, j)) break;
-            const int m = j.m0 + rank * kLinRows + lrow;  // row of A
-            // what the row wants, read while the MMAs run
-            int tok = -1;
-            float mx = 0.f, ls = 0.f, g = 0.f, gh = 0.f, H = 0.f, raise = 1.f;
-            bool zero = true, wrong = false;
-            if (MODE != LIN_GRAD && m < live) {
-                const int r = p.src ? p.src[m] : m;
-                tok = p.tokens ? p.tokens[r] : 0;
-                if (MODE == LIN_DZ) {
+            for (int i = 0; i < work.count; ++i) {
+                LinJob j;
+                if (!work.job(p, i, j)) break;
+                const int m = j.m0 + rank * kLinRows + lrow;  // row of A
+                const int tok = m < live && p.tokens ? p.tokens[p.src ? p.src[m] : m] : -1;
+                float v[128];
+                const int parts = (j.k1 + PART - 1) / PART;
+#pragma unroll 1
+                for (int q = 0; q < parts && ok; ++q, ++it) {
+                    wait(it & 1, it >> 1);
+                    if (!ok) break;
+                    const uint32_t at = from + (uint32_t)((it & 1) * kLinCols + c0);
+                    if (q == 0) {
+#pragma unroll
+                        for (int cc = 0; cc < 4; ++cc) lin_tmem_load<false>(at + 32 * cc, v + 32 * cc);
+                    } else {
+#pragma unroll
+                        for (int cc = 0; cc < 4; ++cc) lin_tmem_load<true>(at + 32 * cc, v + 32 * cc);
+                    }
+                    give(it & 1);
+                }
+                LinSums x;
+                const int left = p.V - j.n0 - c0, at = tok - j.n0 - c0;  // columns that are tokens; the row's token
+                if ((unsigned)at < 128u) {
+                    float z = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 128; ++e) z = e == at ? v[e] : z;
+                    p.ztok[m] = z;
+                }
+                if (left < 128) {
+#pragma unroll
+                    for (int e = 0; e < 128; ++e) v[e] = e < left ? v[e] : -INFINITY;
+                }
+                float n = v[0];
+#pragma unroll
+                for (int e = 1; e < 128; ++e) n = fmaxf(n, v[e]);
+                x.a = fmaxf(x.a, n);
+                float s0 = 0.f, s1 = 0.f, t1 = 0.f, tops = -1.f;
+#pragma unroll
+                for (int e = 0; e < 128; e += 2) {
+                    const float y0 = (v[e] - x.a) * c, y1 = (v[e + 1] - x.a) * c;
+                    float w0 = exp2_approx(y0), w1 = exp2_approx(y1);
+                    x.t = fmaf(w0, fmaxf(y0, -1000.f), x.t);  // (a logit of -inf adds nothing)
+                    t1 = fmaf(w1, fmaxf(y1, -1000.f), t1);
+                    if constexpr (CTAS == 1) {  // (with more rows the epilogue has no time for it, and no row's small terms weigh as much)
+                        const float o0 = y0 == 0.f ? 1.f : 0.f, o1 = y1 == 0.f ? 1.f : 0.f;
+                        w0 -= o0;
+                        w1 -= o1;
+                        tops += o0 + o1;
+                    }
+                    s0 += w0;
+                    s1 += w1;
+                }
+                x.s = s0 + s1 + tops;
+                x.t += t1;
+                if (mine) {
+                    E.sums[i & 1][0][lrow] = x.a;
+                    E.sums[i & 1][1][lrow] = x.s;
+                    E.sums[i & 1][2][lrow] = x.t;
+                }
+                // one decision for all eight warps, so that none is left in a barrier (a warp that is a tile ahead has the other place and flag)
+                if (!ok) S.stop[i & 1] = 1;
+                named_bar_sync(1, 256);
+                if (*(volatile int *)&S.stop[i & 1]) break;
+                if (!mine && m < live) {
+                    x.join(E.sums[i & 1][0][lrow], E.sums[i & 1][1][lrow], E.sums[i & 1][2][lrow], c);
+                    float *o = p.part + (int64_t)(j.n0 / kLinCols) * p.rows_cap + m;
+                    const int64_t plane = (int64_t)p.token_tiles * p.rows_cap;
+                    o[0] = x.a;
+                    o[plane] = x.s;
+                    o[2 * plane] = x.t;
+                }
+            }
+        } else if constexpr (MODE == LIN_DZ) {
+#pragma unroll 1
+            for (int i = mine; i < work.count && ok; i += 2) {
+                LinJob j;
+                if (!work.job(p, i, j)) break;
+                const int m = j.m0 + rank * kLinRows + lrow;
+                // what the row wants, read while the MMAs run
+                int tok = -1;
+                float mx = 0.f, ls = 0.f, g = 0.f, gh = 0.f, H = 0.f, raise = 1.f;
+                bool zero = true, wrong = false;
+                if (m < live) {
+                    const int r = p.src[m];
+                    tok = p.tokens ? p.tokens[r] : -1;
                     mx = p.stats[2 * (int64_t)r];
                     ls = p.stats[2 * (int64_t)r + 1];
                     if (p.glp) g = p.glp[r];
@@ -415,90 +551,110 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     raise = pow2f(p.kexp[r]);
                     wrong = tok >= p.V;
                     zero = mx == -INFINITY && ls == 0.f && !wrong;
-                    if (!p.tokens) tok = -1;
                 }
-            }
-            ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_full[mine], (uint32_t)((i >> 1) & 1), err) && !*ab);
-            if (!ok) break;
-            tc_fence_after();
-            if constexpr (MODE == LIN_SCORE) {
-                LinSums x;
-                const int left = p.V - j.n0;  // columns that are tokens
-#pragma unroll 1
-                for (int cc = 0; cc < kLinCols; cc += 32) {
-                    float v[32];
-                    tmem_ld_32x32b_x32(from + cc, v);
-                    const int at = tok - j.n0 - cc;
-                    if ((unsigned)at < 32u && m < live) {
-                        float z = 0.f;
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) z = e == at ? v[e] : z;
-                        p.ztok[m] = z;
-                    }
-                    if (left - cc < 32) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] = cc + e < left ? v[e] : -INFINITY;
-                    }
-                    float n = v[0];
-#pragma unroll
-                    for (int e = 1; e < 32; ++e) n = fmaxf(n, v[e]);
-                    if (n > x.a) x.rebase(n, c);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const float y = (v[e] - x.a) * c, w = exp2_approx(y);
-                        x.s += w;
-                        x.t = fmaf(w, fmaxf(y, -1000.f), x.t);  // (a logit of -inf adds nothing)
-                    }
-                }
-                if (m < live) {
-                    float *o = p.part + (int64_t)(j.n0 / kLinCols) * p.rows_cap + m;
-                    const int64_t plane = (int64_t)p.token_tiles * p.rows_cap;
-                    o[0] = x.a;
-                    o[plane] = x.s;
-                    o[2 * plane] = x.t;
-                }
-            } else if constexpr (MODE == LIN_DZ) {
+                wait(mine, i >> 1);
+                if (!ok) break;
                 const int left = p.cols - j.n0;
                 uint16_t *o = p.dz + (int64_t)m * p.piece + j.n0;
 #pragma unroll 1
                 for (int cc = 0; cc < kLinCols; cc += 32) {
                     float v[32];
-                    tmem_ld_32x32b_x32(from + cc, v);
+                    lin_tmem_load<false>(from + (uint32_t)(mine * kLinCols + cc), v);
                     const int at = tok - p.v0 - j.n0 - cc;
+                    uint16_t h[32];
 #pragma unroll
                     for (int e = 0; e < 32; ++e) {
-                        const float lp = fmaf(v[e], p.scale, -mx) - ls, q = exp2_approx(lp * kLog2e);
-                        float y = -q * fmaf(gh, fmaxf(lp, -1000.f) + H, g);
+                        const float lp = fmaf(v[e], p.scale, -mx) - ls, x = exp2_approx(lp * kLog2e);
+                        float y = -x * fmaf(gh, fmaxf(lp, -1000.f) + H, g);
                         if (e == at) y += g;
                         y = wrong ? __int_as_float(0x7fc00000) : y * raise;
                         v[e] = zero || cc + e >= left ? 0.f : y;
+                        h[e] = lin_round<TYPE>(v[e]);
                     }
-                    if (m >= live) {
+                    if ((unsigned)at < 32u && m < live) {
+                        float off = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) v[e] = 0.f;
+                        for (int e = 0; e < 32; ++e) off = e == at ? v[e] - lin_float<TYPE>(h[e]) : off;
+                        p.delta[m] = off;
                     }
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        uint16_t h[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) h[e] = lin_round<TYPE>(v[8 * q + e]);
-                        *reinterpret_cast<uint4 *>(o + cc + 8 * q) = pack8(h);
+                        const uint16_t(&g8)[8] = *reinterpret_cast<const uint16_t(*)[8]>(h + 8 * q);
+                        *reinterpret_cast<uint4 *>(o + cc + 8 * q) = m < live ? pack8(g8) : make_uint4(0, 0, 0, 0);
                     }
                 }
-            } else {
-                const float k = p.scale * pow2f(-p.head->exp);
-                const bool write = j.kind == 0 ? m < live : m < p.cols;
+                give(mine);
+            }
+        } else {
+            const float k = p.scale * pow2f(-p.head->exp);
+#pragma unroll 1
+            for (int i = mine; i < work.count; i += 2) {
+                LinJob j;
+                if (!work.job(p, i, j)) break;
+                const int m = j.m0 + rank * kLinRows + lrow, left = min(p.d - j.n0, j.n);
+                // one decision for the four warps, so that none is left in a barrier (the flag is read by all before the next one)
+                if (!ok) S.stop[mine] = 1;
+                named_bar_sync(1 + mine, 128);
+                if (*(volatile int *)&S.stop[mine]) break;
+                if (j.kind) {
+                    // rows whose token is one of the tile's: each warp looks through a quarter, so that their order is the rows'
+                    const int base = p.v0 + j.m0 + rank * kLinRows, each = ((live + 3) / 4 + 31) / 32 * 32;
+                    int n = 0;
+#pragma unroll 4
+                    for (int x = 0; x < each; x += 32) {
+                        const int r = quarter * each + x + lane;
+                        const int at = r < live ? p.tokc[r] - base : -1;
+                        const bool hit = (unsigned)at < (unsigned)kLinRows;
+                        const uint32_t mask = __ballot_sync(0xffffffffu, hit);
+                        const int to = n + __popc(mask & ((1u << lane) - 1));
+                        if (hit && to < kLinHits) E.hit[mine][quarter][to] = make_int2(at, r);
+                        n += __popc(mask);
+                    }
+                    if (lane == 0) E.found[mine][quarter] = min(n, kLinHits);
+                }
+                named_bar_sync(1 + mine, 128);
+                wait(mine, i >> 1);
+                if (!ok) continue;  // (to the barrier)
+                const bool write = j.kind ? m < p.cols : m < live;
+                int hits = 0;  // of the row
+                if (j.kind) {
+#pragma unroll 1
+                    for (int w = 0; w < 4; ++w)
+                        for (int x = 0; x < E.found[mine][w]; ++x) hits += E.hit[mine][w][x].x == lrow;
+                }
                 float *acc = p.acc + ((int64_t)j.split * p.rows_cap + m) * p.d + j.n0;
                 uint16_t *o = j.kind ? p.dw + (int64_t)(p.v0 + m) * p.dw_stride + j.n0 : nullptr;
-                const int left = p.d - j.n0;
 #pragma unroll 1
-                for (int cc = 0; cc < j.n && cc < left; cc += 32) {
+                for (int cc = 0; cc < left; cc += 32) {
                     float v[32];
-                    tmem_ld_32x32b_x32(from + cc, v);
+                    lin_tmem_load<false>(from + (uint32_t)(mine * kLinCols + cc), v);
                     if (!write) continue;
+                    if (hits) {
+#pragma unroll 1
+                        for (int w = 0; w < 4; ++w)
+#pragma unroll 1
+                            for (int x = 0; x < E.found[mine][w]; ++x) {
+                                const int2 hit = E.hit[mine][w][x];
+                                if (hit.x != lrow) continue;
+                                const float f = p.delta[hit.y];
+                                const uint16_t *h = p.low + (int64_t)hit.y * p.d + j.n0 + cc;
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) {
+                                    if (cc + 8 * q >= left) continue;
+                                    const uint4 y = *reinterpret_cast<const uint4 *>(h + 8 * q);
+                                    const uint32_t u[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        const float2 z = unpack2<TYPE>(u[e]);
+                                        v[8 * q + 2 * e] = fmaf(f, z.x, v[8 * q + 2 * e]);
+                                        v[8 * q + 2 * e + 1] = fmaf(f, z.y, v[8 * q + 2 * e + 1]);
+                                    }
+                                }
+                            }
+                    }
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        if (cc + 8 * q >= left) break;
+                        if (cc + 8 * q >= left) continue;
                         if (j.kind) {
                             uint16_t h[8];
 #pragma unroll
@@ -518,12 +674,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                         }
                     }
                 }
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if (CTAS == 2) mbar_arrive_cluster(empty);
-                else mbar_arrive(&S.acc_empty[mine]);
+                give(mine);
             }
         }
         if (!ok) *ab = 1;
@@ -597,6 +748,8 @@ struct LinGatherParams {
     int64_t stride;
     int d, tile;
     const int *src, *kexp;
+    const int32_t *tokens;  // may be null
+    int *tokc;              // [rows_cap]: the compact rows' tokens, or null
     uint16_t *out, *low;    // [rows_cap][d]; low null: not wanted
 };
 __global__ void __launch_bounds__(256) lin_gather_kernel(LinGatherParams p) {
@@ -604,6 +757,7 @@ __global__ void __launch_bounds__(256) lin_gather_kernel(LinGatherParams p) {
     if (row >= max((live + p.tile - 1) / p.tile, 1) * p.tile) return;
     uint16_t *o = p.out + (int64_t)row * p.d, *o2 = p.low ? p.low + (int64_t)row * p.d : nullptr;
     const int r = row < live ? p.src[row] : 0, down = o2 && row < live ? min(p.head->exp - p.kexp[r], 0) : 0;
+    if (p.tokc && lane == 0) p.tokc[row] = row < live && p.tokens ? p.tokens[r] : -1;
     const uint16_t *h = p.h + r * p.stride;
     const float f = pow2f(max(down, -126));
     for (int x = 8 * lane; x < p.d; x += 256) {
@@ -661,25 +815,30 @@ __global__ void __launch_bounds__(256) lin_join_kernel(LinJoinParams p) {
     if (group || !in) return;
     const float a = x.a, s = x.s, t = x.t;
     const float nan = __int_as_float(0x7fc00000);
-    const bool pad = tok < 0, none = s == 0.f, failed = p.head->err != 0;
-    const float ls = none ? 0.f : logf(s);
+    const bool pad = tok < 0, none = s == -1.f, failed = p.head->err != 0;
+    const float ls = none ? 0.f : log1pf(s);
     float lp = 0.f;
     if (at >= 0 && tok < p.V) lp = none ? -INFINITY : fmaf(p.ztok[at] - a, p.scale, -ls);
     else if (!pad) lp = nan;
     if (p.logprob) p.logprob[r] = failed ? nan : pad ? 0.f : lp;
-    if (p.entropy) p.entropy[r] = failed ? nan : pad || none ? 0.f : fmaf(-kLn2, t / s, ls);
+    if (p.entropy) p.entropy[r] = failed ? nan : pad || none ? 0.f : fmaf(-kLn2, t / (1.f + s), ls);
     if (p.stats) {
         p.stats[2 * (int64_t)r] = failed ? nan : pad ? 0.f : none ? -INFINITY : a * p.scale;
         p.stats[2 * (int64_t)r + 1] = failed ? nan : pad ? 0.f : ls;
     }
 }
 
-// dH: the splits' sums in their order, times scale and what dZ was raised by, to the rows' places; 0 for rows of padding
+// dH: the splits' sums in their order and what rounding took at the row's token, times scale and what dZ was raised by, to the rows' places; 0
+// for rows of padding
 struct LinOutParams {
     const LinHeader *head;
     int R, d, splits, rows_cap;
     const int *pos, *kexp;
-    const float *acc;
+    const float *acc, *delta;
+    const int32_t *tokens;
+    int V;
+    const uint16_t *w;
+    int64_t w_stride;
     float scale;
     uint16_t *out;
     int64_t stride;
@@ -691,8 +850,21 @@ __global__ void __launch_bounds__(256) lin_out_kernel(LinOutParams p) {
     const int at = p.pos[r];
     const float k = p.head->err ? __int_as_float(0x7fc00000) : p.scale * pow2f(-p.kexp[r]);
     uint16_t *o = p.out + r * p.stride;
+    const int tok = p.tokens && at >= 0 ? p.tokens[r] : -1;
+    const bool fix = tok >= 0 && tok < p.V;
+    const float f = fix ? p.delta[at] : 0.f;
     for (int x = 8 * lane; x < p.d; x += 256) {
         float v[8] = {};
+        if (fix) {
+            const uint4 y = *reinterpret_cast<const uint4 *>(p.w + tok * p.w_stride + x);
+            const uint32_t u[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 z = unpack2<TYPE>(u[e]);
+                v[2 * e] = f * z.x;
+                v[2 * e + 1] = f * z.y;
+            }
+        }
         if (at >= 0) {
             for (int s = 0; s < p.splits; ++s) {
                 const float4 *q = reinterpret_cast<const float4 *>(p.acc + ((int64_t)s * p.rows_cap + at) * p.d + x);
@@ -716,7 +888,7 @@ struct LinPlan {
     int ctas, rows_cap, tiles;        // CTAs of a tile; rows up to whole tiles; tiles of tokens
     bool gather;                      // the live rows are gathered
     int piece, splits;                // gradient: tokens of a piece, parts of its dH
-    size_t src, pos, kexp, rows, low, part, ztok, dz, acc, bytes;
+    size_t src, pos, kexp, tokc, delta, rows, low, part, ztok, dz, acc, bytes;
 };
 inline LinPlan lin_plan(int R, int d, int V, bool backward) {
     LinPlan q{};
@@ -741,6 +913,8 @@ inline LinPlan lin_plan(int R, int d, int V, bool backward) {
         q.ztok = take((size_t)q.rows_cap * 4);
     } else {
         q.kexp = take((size_t)R * 4);
+        q.tokc = take((size_t)q.rows_cap * 4);
+        q.delta = take((size_t)q.rows_cap * 4);
         q.low = take((size_t)q.rows_cap * d * 2);
         const int workers = kLinWorkers / q.ctas, mt = q.rows_cap / tm, nt = (int)lin_up(d, kLinCols) / kLinCols;
         int64_t piece = ((int64_t)192 << 20) / 2 / q.rows_cap;

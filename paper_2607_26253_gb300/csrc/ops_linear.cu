@@ -61,7 +61,8 @@ void gather(cudaStream_t s, void *ws, const LinPlan &q, int R, int d, const void
                                         TYPE == SARA_FP16});
     CK(cudaGetLastError());
     lin_gather_kernel<<<(unsigned)q.rows_cap / 8, 256, 0, s>>>({at<LinHeader>(ws, 0), static_cast<const uint16_t *>(hidden), stride, d,
-                                                                     kLinRows * q.ctas, at<int>(ws, q.src), kexp,
+                                                                     kLinRows * q.ctas, at<int>(ws, q.src), kexp, tokens,
+                                                               backward ? at<int>(ws, q.tokc) : nullptr,
                                                                at<uint16_t>(ws, q.rows), backward && TYPE == SARA_FP16 ? at<uint16_t>(ws, q.low) : nullptr});
     CK(cudaGetLastError());
 }
@@ -118,6 +119,9 @@ void gradient(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand
     p.gent = gent;
     p.dz = at<uint16_t>(ws, q.dz);
     p.piece = q.piece;
+    p.tokc = at<int>(ws, q.tokc);
+    p.delta = at<float>(ws, q.delta);
+    p.low = at<uint16_t>(ws, TYPE == SARA_FP16 ? q.low : q.rows);
     p.acc = at<float>(ws, q.acc);
     p.splits = q.splits;
     p.dw = static_cast<uint16_t *>(const_cast<void *>(dw.p));
@@ -134,7 +138,8 @@ void gradient(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand
         launch<LIN_GRAD, CTAS, TYPE>(s, sms, dzk, wn, dzm, xn, p);
     }
     if (!dh.p) return;
-    lin_out_kernel<TYPE><<<(unsigned)(R + 7) / 8, 256, 0, s>>>({p.head, R, d, q.splits, q.rows_cap, at<int>(ws, q.pos), p.kexp, p.acc, scale,
+    lin_out_kernel<TYPE><<<(unsigned)(R + 7) / 8, 256, 0, s>>>({p.head, R, d, q.splits, q.rows_cap, at<int>(ws, q.pos), p.kexp, p.acc, p.delta,
+                                                               tokens, V, static_cast<const uint16_t *>(w.p), w.stride, scale,
                                                                static_cast<uint16_t *>(const_cast<void *>(dh.p)), dh.stride});
     CK(cudaGetLastError());
 }
