@@ -473,12 +473,12 @@ SARA_API int sara_logprobs_backward(const void *logits, int64_t row_stride, int3
 /* ---------------------------------------------------------------------------------------
  * The same scores from the last hidden states, for which no logits are stored: z = scale H W^T, H [R][d] the rows' hidden states,
  * W [V][d] the vocabulary's weights (an lm_head as it lies in memory).  `type` SARA_BF16 or SARA_FP16, of H, W and their gradients; d a
- * multiple of 8 up to 65,536, R and V at most 2^24; rows of H, W and the gradients stride elements apart (multiples of 8, at least d), all
+ * multiple of 8 up to 65,536, R at most 2^22, V at most 2^24; rows of H, W and the gradients stride elements apart (multiples of 8, at least d), all
  * of them 16-byte aligned; scale > 0 and finite (1 / temperature).  Device pointers, not waited for, nothing allocated; the calls may be
  * captured.  Products are exact and summed in fp32.
  * workspace: sara_linear_logprobs_workspace_bytes(R, d, V, backward) bytes of device scratch, 256-byte aligned, whose first 256 bytes are
  * zero on first use and left zero where they have to be; calls that share one must not overlap.  (12 bytes a row and 256 tokens for the
- * scores; for the gradient the rows, pieces of at most 16,384 tokens' gradients, some 192 MB of them, and fp32 sums of grad_hidden.)
+ * scores; for the gradient the rows, up to 192 MB of the gradients of a piece of the vocabulary, and fp32 sums of grad_hidden.)
  * ------------------------------------------------------------------------------------- */
 SARA_API size_t sara_linear_logprobs_workspace_bytes(int32_t R, int32_t d, int32_t V, int32_t backward);
 

@@ -32,8 +32,11 @@
 namespace sara {
 
 constexpr int kLinThreads = 320;
-constexpr int kLinRows = 128, kLinCols = 256, kLinK = 64;  // of a CTA's tile; of a chunk
+constexpr int kLinRows = 128, kLinK = 64;  // rows of a CTA's tile; elements of a chunk
+// Columns of a tile: with one CTA the work is bound by memory, and smaller tiles share it out more evenly
+__host__ __device__ constexpr int lin_cols(int ctas) { return ctas == 2 ? 256 : 128; }
 constexpr int kLinMaxSplits = 32;
+constexpr int kLinSort = 65536, kLinGatherCols = 1024;  // rows that are sorted together; columns of a warp that gathers
 constexpr int kLinWorkers = 152;  // SMs that a plan counts on (on a GPU with others it is as right, if less even)
 
 // What the kernels of a call share, at the start of the workspace
@@ -44,15 +47,19 @@ struct LinHeader {
     int pad[61];
 };
 
-__host__ __device__ constexpr int lin_stage_bytes(int ctas) { return (kLinRows + kLinCols / ctas) * kLinK * 2; }
-__host__ __device__ constexpr int lin_stages(int ctas) { return ctas == 2 ? 6 : 4; }
-__host__ __device__ constexpr size_t lin_smem(int ctas) { return 1024 + (size_t)lin_stages(ctas) * lin_stage_bytes(ctas); }
-
+constexpr int kLinHalf = kLinRows * kLinK * 2;                     // 16 KB: of a stage A's half, B's (128 rows of either), of a block on its way out
 enum LinMode : int {
     LIN_SCORE = 0,  // tiles of logits -> partial sums
     LIN_DZ = 1,     // tiles of logits -> dZ of a piece
     LIN_GRAD = 2,   // dZ of a piece -> dH's sums, dW
 };
+// One CTA stores dZ and dW by way of shared memory, two blocks of 64 columns for each half of its epilogue: whole lines, where each thread's own row
+// would cost the memory pipe an access a lane.  Two CTAs store from registers: their operands leave shared memory no time.  (DZ of 4,096 rows:
+// 135 us a piece, 156 by way of it.)
+__host__ __device__ constexpr bool lin_staged(int mode, int ctas) { return mode != LIN_SCORE && ctas == 1; }
+__host__ __device__ constexpr int lin_stages(int mode, int ctas) { return lin_staged(mode, ctas) ? 4 : 6; }
+__host__ __device__ constexpr size_t lin_smem(int mode, int ctas) { return 1024 + (size_t)(2 * lin_stages(mode, ctas) + (lin_staged(mode, ctas) ? 4 : 0)) * kLinHalf; }
+constexpr int kLinHits = 8;  // rows of a tile of tokens that wait in shared memory for dW's epilogue
 
 struct LinParams {
     LinHeader *head;
@@ -67,35 +74,36 @@ struct LinParams {
     int rows_cap, token_tiles;
     // LIN_DZ
     const float *stats, *entropy, *glp, *gent;
-    uint16_t *dz;      // [rows_cap][piece]
-    int piece, v0, cols;  // columns of dZ; the piece's first token and tokens
+    int v0, cols;      // the piece's first token, and tokens
     float *delta;      // [rows_cap]: what rounding took from dZ at the row's token
     // LIN_GRAD
-    const int *tokc;   // [rows_cap]: the compact rows' tokens
+    const int *start;  // see lin_gather_kernel
+    const int2 *sorted;
+    int buckets;
     const uint16_t *low;  // [rows_cap][d]: the rows that dW's product has
     float *acc;        // [split][rows_cap][d]
     int splits, first; // first: the first piece
-    uint16_t *dw;      // or null
-    int64_t dw_stride;
-    bool dh;
+    bool dh, dw;
+    uint16_t *out;     // DZ: dZ's blocks, [piece / 64][rows_cap][64]; GRAD: dW
+    int64_t out_stride;
+    bool wide;         // its rows' blocks are 32-byte aligned
 };
 
 // Chunks of a part of a logit's sum: with two CTAs a tile's epilogue has no time for more parts
-__host__ __device__ constexpr int lin_part(int ctas) { return ctas == 2 ? 8 : 1; }
-constexpr int kLinHits = 256;  // rows of a quarter whose tokens are in a tile of dW and whose delta is added there (the first ones)
-
+__host__ __device__ constexpr int lin_part(int ctas) { return ctas == 2 ? 8 : 2; }
 struct LinSmem {
-    uint64_t full[6], empty[6], acc_full[2], acc_empty[2], drain;
+    uint64_t full[6], empty[6], acc_full[4], acc_empty[4], drain;
     uint32_t tmem_base;
     int abort, stop[2];                  // stop: the epilogue's, for two tiles in turn
 };
 struct LinScoreSmem {
     float sums[2][3][kLinRows];          // of the second half's columns, for two tiles in turn
 };
+template <int COLS>
 struct LinGradSmem {
-    int found[2][4];                     // of each epilogue warp's quarter of the rows
-    int2 hit[2][4][kLinHits];            // place in the tile, row
+    uint16_t row[2][2][kLinHits][COLS];  // for each half of the epilogue, two tiles in turn
 };
+struct LinNoSmem {};
 
 // ------------------------------------------------------------------------------- PTX for a pair of CTAs
 template <int CTAS>
@@ -161,6 +169,16 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
+__device__ __forceinline__ void lin_store(const CUtensorMap *tm, uint32_t src, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<uint64_t>(tm)), "r"(x),
+                 "r"(y), "r"(src)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+// This thread's stores have been read from shared memory
+__device__ __forceinline__ void lin_stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void lin_stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
 // Shared-memory matrix descriptor, 128-byte swizzle.  K-major: 8 rows of 64 elements after sbo bytes.  M/N-major: lines of 64 rows or
 // columns at one k, 8 k after sbo bytes, the next 64 rows after lbo bytes.
 __device__ __forceinline__ uint64_t sdesc_sw128(uint32_t addr, uint32_t lbo, uint32_t sbo) {
@@ -179,7 +197,7 @@ struct LinJob {
 // LIN_GRAD: dH's jobs are long, so the workers that have one more of them get fewer of dW's.
 template <int MODE, int CTAS>
 struct LinWork {
-    static constexpr int TM = kLinRows * CTAS;
+    static constexpr int TM = kLinRows * CTAS, COLS = lin_cols(CTAS);
     int w, W, mt, nt, count;
     int64_t tiles;
     // LIN_GRAD
@@ -188,11 +206,11 @@ struct LinWork {
     __device__ __forceinline__ LinWork(const LinParams &p, int live, int w_, int W_) : w(w_), W(W_) {
         mt = max((live + TM - 1) / TM, 1);
         if constexpr (MODE != LIN_GRAD) {
-            nt = (p.cols + kLinCols - 1) / kLinCols;
+            nt = (p.cols + COLS - 1) / COLS;
             tiles = (int64_t)mt * nt;
             count = (int)(tiles > w ? (tiles - 1 - w) / W + 1 : 0);
         } else {
-            nt = (p.d + kLinCols - 1) / kLinCols;
+            nt = (p.d + COLS - 1) / COLS;
             kc = (p.cols + kLinK - 1) / kLinK;
             kr = max((live + kLinK - 1) / kLinK, 1);
             splits = min(p.splits, kc);
@@ -219,7 +237,7 @@ struct LinWork {
             const int64_t t = (int64_t)i * W + w;
             if (t >= tiles) return false;
             const int n = (int)(t / mt), m = (int)(t - (int64_t)n * mt);
-            j = {m * TM, n * kLinCols, kLinCols, 0, (p.d + kLinK - 1) / kLinK, 0, 0};
+            j = {m * TM, n * COLS, COLS, 0, (p.d + kLinK - 1) / kLinK, 0, 0};
             return true;
         } else {
             int n, m;
@@ -244,8 +262,8 @@ struct LinWork {
                 j.k1 = kr;
             }
             j.m0 = m * TM;
-            j.n0 = n * kLinCols;
-            j.n = min(kLinCols, (p.d - j.n0 + 64 * CTAS - 1) / (64 * CTAS) * (64 * CTAS));
+            j.n0 = n * COLS;
+            j.n = min(COLS, (p.d - j.n0 + 64 * CTAS - 1) / (64 * CTAS) * (64 * CTAS));
             return true;
         }
     }
@@ -297,12 +315,13 @@ __device__ __forceinline__ uint16_t lin_round(float x) {
 template <int MODE, int CTAS, int TYPE>
 __global__ void __launch_bounds__(kLinThreads, 1)
 lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmA2,
-           const __grid_constant__ CUtensorMap tmB2, LinParams p) {
-    constexpr int STAGES = lin_stages(CTAS), STAGE = lin_stage_bytes(CTAS), A_BYTES = kLinRows * kLinK * 2;
-    constexpr int BN = kLinCols / CTAS, PART = lin_part(CTAS);  // a CTA's share of B's rows
+           const __grid_constant__ CUtensorMap tmB2, const __grid_constant__ CUtensorMap tmOut, LinParams p) {
+    constexpr int STAGES = lin_stages(MODE, CTAS), STAGE = 2 * kLinHalf, COLS = lin_cols(CTAS), BN = COLS / CTAS, PART = lin_part(CTAS);
+    constexpr int ACCS = 512 / COLS;  // accumulators
+    static_assert(BN == kLinRows, "B's share of a stage is as large as A's");
     extern __shared__ uint8_t smem_raw[];
     __shared__ LinSmem S;
-    __shared__ std::conditional_t<MODE == LIN_GRAD, LinGradSmem, LinScoreSmem> E;
+    __shared__ __align__(16) std::conditional_t<MODE == LIN_SCORE, LinScoreSmem, std::conditional_t<MODE == LIN_GRAD, LinGradSmem<COLS>, LinNoSmem>> E;
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CTAS == 2 ? (int)cluster_rank() : 0;
@@ -312,7 +331,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             mbar_init(&S.full[s], 1);
             mbar_init(&S.empty[s], 1);
         }
-        for (int a = 0; a < 2; ++a) {
+        for (int a = 0; a < ACCS; ++a) {
             mbar_init(&S.acc_full[a], 1);
             mbar_init(&S.acc_empty[a], (MODE == LIN_SCORE ? 8 : 4) * CTAS);
         }
@@ -326,6 +345,8 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
     else __syncthreads();
     tc_fence_after();
     const uint32_t tmem = S.tmem_base;
+    pdl_allow_dependents();
+    pdl_wait_prior_grids();
     volatile int *ab = &S.abort;
     const int live = p.src ? p.head->live : p.R;
     const LinWork<MODE, CTAS> work(p, live, (int)blockIdx.x / CTAS, (int)gridDim.x / CTAS);
@@ -344,20 +365,22 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             if (!work.job(p, i, j)) break;
             const bool mn_a = MODE == LIN_GRAD && j.kind == 1, mn_b = MODE == LIN_GRAD;
             const int m = j.m0 + rank * kLinRows, bn = j.n / CTAS, n = j.n0 + rank * bn;
-            const uint32_t bytes = (uint32_t)(A_BYTES + (mn_b ? bn : BN) * kLinK * 2) * CTAS;
+            const uint32_t bytes = (uint32_t)(kLinHalf + bn * kLinK * 2) * CTAS;
 #pragma unroll 1
             for (int k = j.k0; k < j.k1; ++k) {
                 if (loads >= (uint32_t)STAGES) ok = __all_sync(0xffffffffu, mbar_wait(&S.empty[s], ph, err) && !*ab);
                 if (!ok) break;
                 if (elect_one()) {
-                    uint8_t *a = ring + s * STAGE, *b = a + A_BYTES;
+                    uint8_t *a = ring + s * STAGE, *b = a + kLinHalf;
                     const uint32_t bar = CTAS == 2 ? cluster_addr(&S.full[s], 0) : smem_u32(&S.full[s]);
                     if (rank == 0) mbar_arrive_expect_tx(&S.full[s], bytes);
-                    if (!mn_a) {
-                        lin_load<CTAS>(a, &tmA, bar, k * kLinK, m, MODE == LIN_GRAD ? pass : keep);
+                    if (mn_a) {  // (dZ: blocks of 64 columns one after the other)
+                        lin_load<CTAS>(a, &tmA2, bar, 0, m / 64 * p.rows_cap + k * kLinK, pass);
+                        lin_load<CTAS>(a + kLinHalf / 2, &tmA2, bar, 0, (m / 64 + 1) * p.rows_cap + k * kLinK, pass);
+                    } else if (MODE == LIN_GRAD) {
+                        lin_load<CTAS>(a, &tmA, bar, 0, k * p.rows_cap + m, pass);
                     } else {
-                        lin_load<CTAS>(a, &tmA2, bar, m, k * kLinK, pass);
-                        lin_load<CTAS>(a + A_BYTES / 2, &tmA2, bar, m + 64, k * kLinK, pass);
+                        lin_load<CTAS>(a, &tmA, bar, k * kLinK, m, keep);
                     }
                     if (!mn_b) {
                         lin_load<CTAS>(b, &tmB, bar, k * kLinK, p.v0 + n, pass);
@@ -403,9 +426,9 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             for (int k = j.k0; k < j.k1; ++k) {
                 const bool begins = MODE == LIN_SCORE ? k % PART == 0 : k == j.k0, ends = k + 1 == j.k1 || (MODE == LIN_SCORE && (k + 1) % PART == 0);
                 if (begins) {
-                    a = it & 1;
-                    dacc = tmem + (uint32_t)(a * kLinCols);
-                    if (it >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_empty[a], (uint32_t)(((it >> 1) - 1) & 1), err) && !*ab);
+                    a = it % ACCS;
+                    dacc = tmem + (uint32_t)(a * COLS);
+                    if (it >= ACCS) ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_empty[a], (uint32_t)((it / ACCS - 1) & 1), err) && !*ab);
                     if (!ok) break;
                     ++it;
                 }
@@ -416,7 +439,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     const uint32_t at = smem_u32(ring) + (uint32_t)(s * STAGE);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
-                        lin_mma<CTAS>(dacc, sdesc_sw128(at + kk * step_a, kLinK * 128, 1024), sdesc_sw128(at + A_BYTES + kk * step_b, kLinK * 128, 1024),
+                        lin_mma<CTAS>(dacc, sdesc_sw128(at + kk * step_a, kLinK * 128, 1024), sdesc_sw128(at + kLinHalf + kk * step_b, kLinK * 128, 1024),
                                       idesc, !begins || kk > 0);
                     lin_commit<CTAS>(&S.empty[s]);
                     if (ends) lin_commit<CTAS>(&S.acc_full[a]);
@@ -446,13 +469,14 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 else mbar_arrive(&S.acc_empty[a]);
             }
         };
-        auto wait = [&](int a, int use) {
-            ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_full[a], (uint32_t)(use & 1), err) && !*ab);
+        auto wait = [&](int it) {  // for the it-th accumulator
+            ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_full[it % ACCS], (uint32_t)(it / ACCS & 1), err) && !*ab);
             tc_fence_after();
         };
         if constexpr (MODE == LIN_SCORE) {
             const float c = p.scale * kLog2e;
-            const int c0 = mine * 128;
+            constexpr int HALF = COLS / 2;  // columns a thread
+            const int c0 = mine * HALF;
             int it = 0;
 #pragma unroll 1
             for (int i = 0; i < work.count; ++i) {
@@ -460,41 +484,41 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 if (!work.job(p, i, j)) break;
                 const int m = j.m0 + rank * kLinRows + lrow;  // row of A
                 const int tok = m < live && p.tokens ? p.tokens[p.src ? p.src[m] : m] : -1;
-                float v[128];
+                float v[HALF];
                 const int parts = (j.k1 + PART - 1) / PART;
 #pragma unroll 1
                 for (int q = 0; q < parts && ok; ++q, ++it) {
-                    wait(it & 1, it >> 1);
+                    wait(it);
                     if (!ok) break;
-                    const uint32_t at = from + (uint32_t)((it & 1) * kLinCols + c0);
+                    const uint32_t at = from + (uint32_t)(it % ACCS * COLS + c0);
                     if (q == 0) {
 #pragma unroll
-                        for (int cc = 0; cc < 4; ++cc) lin_tmem_load<false>(at + 32 * cc, v + 32 * cc);
+                        for (int cc = 0; cc < HALF / 32; ++cc) lin_tmem_load<false>(at + 32 * cc, v + 32 * cc);
                     } else {
 #pragma unroll
-                        for (int cc = 0; cc < 4; ++cc) lin_tmem_load<true>(at + 32 * cc, v + 32 * cc);
+                        for (int cc = 0; cc < HALF / 32; ++cc) lin_tmem_load<true>(at + 32 * cc, v + 32 * cc);
                     }
-                    give(it & 1);
+                    give(it % ACCS);
                 }
                 LinSums x;
                 const int left = p.V - j.n0 - c0, at = tok - j.n0 - c0;  // columns that are tokens; the row's token
-                if ((unsigned)at < 128u) {
+                if ((unsigned)at < (unsigned)HALF) {
                     float z = 0.f;
 #pragma unroll
-                    for (int e = 0; e < 128; ++e) z = e == at ? v[e] : z;
+                    for (int e = 0; e < HALF; ++e) z = e == at ? v[e] : z;
                     p.ztok[m] = z;
                 }
-                if (left < 128) {
+                if (left < HALF) {
 #pragma unroll
-                    for (int e = 0; e < 128; ++e) v[e] = e < left ? v[e] : -INFINITY;
+                    for (int e = 0; e < HALF; ++e) v[e] = e < left ? v[e] : -INFINITY;
                 }
                 float n = v[0];
 #pragma unroll
-                for (int e = 1; e < 128; ++e) n = fmaxf(n, v[e]);
+                for (int e = 1; e < HALF; ++e) n = fmaxf(n, v[e]);
                 x.a = fmaxf(x.a, n);
                 float s0 = 0.f, s1 = 0.f, t1 = 0.f, tops = -1.f;
 #pragma unroll
-                for (int e = 0; e < 128; e += 2) {
+                for (int e = 0; e < HALF; e += 2) {
                     const float y0 = (v[e] - x.a) * c, y1 = (v[e + 1] - x.a) * c;
                     float w0 = exp2_approx(y0), w1 = exp2_approx(y1);
                     x.t = fmaf(w0, fmaxf(y0, -1000.f), x.t);  // (a logit of -inf adds nothing)
@@ -521,126 +545,190 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 if (*(volatile int *)&S.stop[i & 1]) break;
                 if (!mine && m < live) {
                     x.join(E.sums[i & 1][0][lrow], E.sums[i & 1][1][lrow], E.sums[i & 1][2][lrow], c);
-                    float *o = p.part + (int64_t)(j.n0 / kLinCols) * p.rows_cap + m;
+                    float *o = p.part + (int64_t)(j.n0 / COLS) * p.rows_cap + m;
                     const int64_t plane = (int64_t)p.token_tiles * p.rows_cap;
                     o[0] = x.a;
                     o[plane] = x.s;
                     o[2 * plane] = x.t;
                 }
             }
-        } else if constexpr (MODE == LIN_DZ) {
-#pragma unroll 1
-            for (int i = mine; i < work.count && ok; i += 2) {
-                LinJob j;
-                if (!work.job(p, i, j)) break;
-                const int m = j.m0 + rank * kLinRows + lrow;
-                // what the row wants, read while the MMAs run
-                int tok = -1;
-                float mx = 0.f, ls = 0.f, g = 0.f, gh = 0.f, H = 0.f, raise = 1.f;
-                bool zero = true, wrong = false;
-                if (m < live) {
-                    const int r = p.src[m];
-                    tok = p.tokens ? p.tokens[r] : -1;
-                    mx = p.stats[2 * (int64_t)r];
-                    ls = p.stats[2 * (int64_t)r + 1];
-                    if (p.glp) g = p.glp[r];
-                    if (p.gent) {
-                        gh = p.gent[r];
-                        H = p.entropy[r];
-                    }
-                    raise = pow2f(p.kexp[r]);
-                    wrong = tok >= p.V;
-                    zero = mx == -INFINITY && ls == 0.f && !wrong;
-                }
-                wait(mine, i >> 1);
-                if (!ok) break;
-                const int left = p.cols - j.n0;
-                uint16_t *o = p.dz + (int64_t)m * p.piece + j.n0;
-#pragma unroll 1
-                for (int cc = 0; cc < kLinCols; cc += 32) {
-                    float v[32];
-                    lin_tmem_load<false>(from + (uint32_t)(mine * kLinCols + cc), v);
-                    const int at = tok - p.v0 - j.n0 - cc;
-                    uint16_t h[32];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const float lp = fmaf(v[e], p.scale, -mx) - ls, x = exp2_approx(lp * kLog2e);
-                        float y = -x * fmaf(gh, fmaxf(lp, -1000.f) + H, g);
-                        if (e == at) y += g;
-                        y = wrong ? __int_as_float(0x7fc00000) : y * raise;
-                        v[e] = zero || cc + e >= left ? 0.f : y;
-                        h[e] = lin_round<TYPE>(v[e]);
-                    }
-                    if ((unsigned)at < 32u && m < live) {
-                        float off = 0.f;
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) off = e == at ? v[e] - lin_float<TYPE>(h[e]) : off;
-                        p.delta[m] = off;
-                    }
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const uint16_t(&g8)[8] = *reinterpret_cast<const uint16_t(*)[8]>(h + 8 * q);
-                        *reinterpret_cast<uint4 *>(o + cc + 8 * q) = m < live ? pack8(g8) : make_uint4(0, 0, 0, 0);
-                    }
-                }
-                give(mine);
-            }
         } else {
-            const float k = p.scale * pow2f(-p.head->exp);
+            // 64 columns of the tile's rows to `x`, `y` of the result.  One CTA: by way of one of this half's two places in shared memory, which the
+            // block before the last one has left (after a failed wait the barriers go on and nothing is stored).  Two: each thread its row's.
+            constexpr bool STAGED = lin_staged(MODE, CTAS);
+            const uint32_t out = smem_u32(ring) + (uint32_t)(STAGES * STAGE + mine * 2 * kLinHalf);
+            const bool first = quarter == 0 && lane == 0;
+            int place = 0;
+            auto emit = [&](const uint32_t (&w)[32], int x, int y) {
+                if constexpr (STAGED) {
+                    const uint32_t to = out + place * kLinHalf + lrow * 128;
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((q ^ (lrow & 7)) << 4)), "r"(w[4 * q]), "r"(w[4 * q + 1]),
+                                     "r"(w[4 * q + 2]), "r"(w[4 * q + 3])
+                                     : "memory");
+                    fence_proxy_async_smem();
+                    if (first) lin_stores_read();  // (the other place is free)
+                    __syncwarp();
+                    named_bar_sync(1 + mine, 128);
+                    if (first && ok && (MODE == LIN_DZ || y < p.V)) lin_store(&tmOut, out + place * kLinHalf, x, y);  // (rows behind the last are cut off)
+                    place ^= 1;
+                } else if (ok && (MODE == LIN_DZ || y + lrow < p.V)) {
+                    uint16_t *o = p.out + (int64_t)(y + lrow) * p.out_stride + x;
+                    const int left = MODE == LIN_DZ ? 64 : p.d - x;
+                    if (p.wide && left >= 64) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            float f[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) f[e] = __uint_as_float(w[8 * q + e]);
+                            st_global_v8(reinterpret_cast<float *>(o + 16 * q), f);
+                        }
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            if (8 * q < left) *reinterpret_cast<uint4 *>(o + 8 * q) = make_uint4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
+                    }
+                }
+            };
+            // GRAD: the rows whose token is one of the tile's (`sorted` from `start` on), brought for the tile after the next one's step by step:
+            // where they stand, which they are, then the first of them themselves, so that none of these loads is waited for
+            struct Hits {
+                int x0, n, row, tok;  // (row, tok: lane e's entry e)
+                float delta;
+            };
+            const int blocks = (live + kLinSort - 1) / kLinSort;
+            auto where = [&](int i) {
+                Hits h = {0, 0, 0, -1, 0.f};
+                LinJob j;
+                if (MODE == LIN_GRAD && i < work.count && work.job(p, i, j) && j.kind) {
+                    const int bucket = (p.v0 + j.m0 + rank * kLinRows) / kLinRows;
+                    if (bucket < p.buckets) {
+                        h.x0 = p.start[bucket];
+                        h.n = p.start[bucket + 1];
+                    }
+                }
+                return h;
+            };
+            auto which = [&](Hits &h) {
+                h.n -= h.x0;
+                if (lane < min(h.n, kLinHits)) {
+                    const int2 x = p.sorted[h.x0 + lane];
+                    h.row = x.x;
+                    h.tok = x.y;
+                }
+            };
+            auto fetch = [&](Hits &h, int i, int buf) {
+                LinJob j;
+                if (lane < min(h.n, kLinHits)) h.delta = p.delta[h.row];
+                if (MODE == LIN_GRAD && h.n > 0 && work.job(p, i, j)) {
+                    if constexpr (MODE == LIN_GRAD) {
+                        const int n = min(h.n, kLinHits), left = min(p.d - j.n0, j.n);
+#pragma unroll 1
+                        for (int x = 0; x < n; ++x) {  // (a warp each fourth)
+                            const int row = __shfl_sync(0xffffffffu, h.row, x);
+                            if (x % 4 == quarter && 8 * lane < left)
+                                cp_async16(smem_u32(&E.row[mine][buf][x][8 * lane]), p.low + (int64_t)row * p.d + j.n0 + 8 * lane);
+                        }
+                    }
+                }
+                cp_async_commit();
+            };
+            Hits now = {0, 0, 0, -1, 0.f}, next = now, later = now;
+            int buf = 0;
+            if (MODE == LIN_GRAD && p.dw) {
+                next = where(mine);
+                later = where(mine + 2);
+                which(next);
+                fetch(next, mine, 0);
+            }
+            const float k = MODE == LIN_GRAD ? p.scale * pow2f(-p.head->exp) : 0.f;
 #pragma unroll 1
             for (int i = mine; i < work.count; i += 2) {
                 LinJob j;
                 if (!work.job(p, i, j)) break;
-                const int m = j.m0 + rank * kLinRows + lrow, left = min(p.d - j.n0, j.n);
-                // one decision for the four warps, so that none is left in a barrier (the flag is read by all before the next one)
-                if (!ok) S.stop[mine] = 1;
-                named_bar_sync(1 + mine, 128);
-                if (*(volatile int *)&S.stop[mine]) break;
-                if (j.kind) {
-                    // rows whose token is one of the tile's: each warp looks through a quarter, so that their order is the rows'
-                    const int base = p.v0 + j.m0 + rank * kLinRows, each = ((live + 3) / 4 + 31) / 32 * 32;
-                    int n = 0;
-#pragma unroll 4
-                    for (int x = 0; x < each; x += 32) {
-                        const int r = quarter * each + x + lane;
-                        const int at = r < live ? p.tokc[r] - base : -1;
-                        const bool hit = (unsigned)at < (unsigned)kLinRows;
-                        const uint32_t mask = __ballot_sync(0xffffffffu, hit);
-                        const int to = n + __popc(mask & ((1u << lane) - 1));
-                        if (hit && to < kLinHits) E.hit[mine][quarter][to] = make_int2(at, r);
-                        n += __popc(mask);
+                const int m = j.m0 + rank * kLinRows + lrow;
+                const uint32_t acc_at = from + (uint32_t)(i % ACCS * COLS);
+                if constexpr (MODE == LIN_DZ) {
+                    // what the row wants, read while the MMAs run
+                    int tok = -1;
+                    float mx = 0.f, ls = 0.f, g = 0.f, gh = 0.f, H = 0.f, raise = 1.f;
+                    bool zero = true, wrong = false;
+                    if (m < live) {
+                        const int r = p.src[m];
+                        tok = p.tokens ? p.tokens[r] : -1;
+                        mx = p.stats[2 * (int64_t)r];
+                        ls = p.stats[2 * (int64_t)r + 1];
+                        if (p.glp) g = p.glp[r];
+                        if (p.gent) {
+                            gh = p.gent[r];
+                            H = p.entropy[r];
+                        }
+                        raise = pow2f(p.kexp[r]);
+                        wrong = tok >= p.V;
+                        zero = mx == -INFINITY && ls == 0.f && !wrong;
                     }
-                    if (lane == 0) E.found[mine][quarter] = min(n, kLinHits);
-                }
-                named_bar_sync(1 + mine, 128);
-                wait(mine, i >> 1);
-                if (!ok) continue;  // (to the barrier)
-                const bool write = j.kind ? m < p.cols : m < live;
-                int hits = 0;  // of the row
-                if (j.kind) {
+                    if (ok) wait(i);
+                    const int left = p.cols - j.n0;
 #pragma unroll 1
-                    for (int w = 0; w < 4; ++w)
-                        for (int x = 0; x < E.found[mine][w]; ++x) hits += E.hit[mine][w][x].x == lrow;
-                }
-                float *acc = p.acc + ((int64_t)j.split * p.rows_cap + m) * p.d + j.n0;
-                uint16_t *o = j.kind ? p.dw + (int64_t)(p.v0 + m) * p.dw_stride + j.n0 : nullptr;
+                    for (int cc = 0; cc < COLS; cc += 64) {
+                        uint32_t w[32];
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            float v[32];
+                            lin_tmem_load<false>(acc_at + cc + 32 * half, v);
+                            const int c0 = cc + 32 * half, at = tok - p.v0 - j.n0 - c0;
+                            float off = 0.f;
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) {
+                                const float lp = fmaf(v[e], p.scale, -mx) - ls, x = exp2_approx(lp * kLog2e);
+                                float y = -x * fmaf(gh, fmaxf(lp, -1000.f) + H, g);
+                                if (e == at) y += g;
+                                y = wrong ? __int_as_float(0x7fc00000) : y * raise;
+                                v[e] = zero || c0 + e >= left ? 0.f : y;
+                            }
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) {
+                                const uint32_t x = pack_grad<TYPE>(v[2 * e], v[2 * e + 1]);
+                                const float2 z = unpack2<TYPE>(x);
+                                w[16 * half + e] = x;
+                                off = 2 * e == at ? v[2 * e] - z.x : 2 * e + 1 == at ? v[2 * e + 1] - z.y : off;
+                            }
+                            if ((unsigned)at < 32u && m < live) p.delta[m] = off;
+                        }
+                        if (m >= live) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) w[e] = 0;
+                        }
+                        emit(w, 0, (j.n0 + cc) / 64 * p.rows_cap + j.m0 + rank * kLinRows);
+                    }
+                } else if (j.kind) {
+                    const int token = p.v0 + m;
+                    cp_async_wait<0>();
+                    __syncwarp();
+                    named_bar_sync(1 + mine, 128);  // (its rows have come; the tile before has left the other place)
+                    now = next;
+                    next = later;
+                    which(next);
+                    fetch(next, i + 2, buf ^ 1);
+                    later = where(i + 4);
+                    uint32_t match = 0;  // which of them are the row's
+#pragma unroll
+                    for (int x = 0; x < kLinHits; ++x) match |= (uint32_t)(__shfl_sync(0xffffffffu, now.tok, x) == token) << x;
+                    if (ok) wait(i);
+                    const int left = min(p.d - j.n0, j.n);
 #pragma unroll 1
-                for (int cc = 0; cc < left; cc += 32) {
-                    float v[32];
-                    lin_tmem_load<false>(from + (uint32_t)(mine * kLinCols + cc), v);
-                    if (!write) continue;
-                    if (hits) {
-#pragma unroll 1
-                        for (int w = 0; w < 4; ++w)
-#pragma unroll 1
-                            for (int x = 0; x < E.found[mine][w]; ++x) {
-                                const int2 hit = E.hit[mine][w][x];
-                                if (hit.x != lrow) continue;
-                                const float f = p.delta[hit.y];
-                                const uint16_t *h = p.low + (int64_t)hit.y * p.d + j.n0 + cc;
+                    for (int cc = 0; cc < left; cc += 64) {
+                        uint32_t w[32];
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            float v[32];
+                            const int c0 = cc + 32 * half;
+                            lin_tmem_load<false>(acc_at + c0, v);
+                            auto add = [&](float f, const uint16_t *h) {
 #pragma unroll
                                 for (int q = 0; q < 4; ++q) {
-                                    if (cc + 8 * q >= left) continue;
+                                    if (c0 + 8 * q >= left) continue;
                                     const uint4 y = *reinterpret_cast<const uint4 *>(h + 8 * q);
                                     const uint32_t u[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -650,32 +738,65 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                                         v[8 * q + 2 * e + 1] = fmaf(f, z.y, v[8 * q + 2 * e + 1]);
                                     }
                                 }
+                            };
+                            if (__any_sync(0xffffffffu, match != 0)) {
+#pragma unroll 1
+                                for (int x = 0; x < kLinHits; ++x) {
+                                    const float f = __shfl_sync(0xffffffffu, now.delta, x);
+                                    if (match >> x & 1) add(f, &E.row[mine][buf][x][c0]);
+                                }
                             }
+                            if (now.n > kLinHits || blocks > 1) {  // the others, in their order
+#pragma unroll 1
+                                for (int b = 0; b < blocks; ++b) {
+                                    const int *start = p.start + (int64_t)b * (p.buckets + 1) + (p.v0 + j.m0 + rank * kLinRows) / kLinRows;
+                                    if (token >= p.V) break;
+#pragma unroll 1
+                                    for (int x = start[0] + (b == 0 ? kLinHits : 0); x < start[1]; ++x) {
+                                        const int2 r = p.sorted[b * kLinSort + x];
+                                        if (r.y == token) add(p.delta[r.x], p.low + (int64_t)r.x * p.d + j.n0 + c0);
+                                    }
+                                }
+                            }
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) w[16 * half + e] = pack_grad<TYPE>(v[2 * e] * k, v[2 * e + 1] * k);
+                        }
+                        emit(w, j.n0 + cc, p.v0 + j.m0 + rank * kLinRows);
                     }
+                    buf ^= 1;
+                } else {
+                    if (p.dw) {  // (the next tile may be one of dW's)
+                        now = next;
+                        next = later;
+                        which(next);
+                        fetch(next, i + 2, buf ^ 1);
+                        later = where(i + 4);
+                        buf ^= 1;
+                    }
+                    if (ok) wait(i);
+                    const int left = min(p.d - j.n0, j.n);
+                    float *acc = p.acc + ((int64_t)j.split * p.rows_cap + m) * p.d + j.n0;
+#pragma unroll 1
+                    for (int cc = 0; cc < left; cc += 32) {
+                        float v[32];
+                        lin_tmem_load<false>(acc_at + cc, v);
+                        if (m >= live) continue;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        if (cc + 8 * q >= left) continue;
-                        if (j.kind) {
-                            uint16_t h[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) h[e] = lin_round<TYPE>(v[8 * q + e] * k);
-                            *reinterpret_cast<uint4 *>(o + cc + 8 * q) = pack8(h);
-                        } else {
-                            float4 *to = reinterpret_cast<float4 *>(acc + cc + 8 * q);
-                            float4 x0 = make_float4(v[8 * q], v[8 * q + 1], v[8 * q + 2], v[8 * q + 3]);
-                            float4 x1 = make_float4(v[8 * q + 4], v[8 * q + 5], v[8 * q + 6], v[8 * q + 7]);
+                        for (int q = 0; q < 8; ++q) {
+                            if (cc + 4 * q >= left) continue;
+                            float4 *to = reinterpret_cast<float4 *>(acc + cc + 4 * q);
+                            float4 x = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
                             if (!p.first) {
-                                const float4 y0 = to[0], y1 = to[1];
-                                x0 = make_float4(x0.x + y0.x, x0.y + y0.y, x0.z + y0.z, x0.w + y0.w);
-                                x1 = make_float4(x1.x + y1.x, x1.y + y1.y, x1.z + y1.z, x1.w + y1.w);
+                                const float4 y = *to;
+                                x = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
                             }
-                            to[0] = x0;
-                            to[1] = x1;
+                            *to = x;
                         }
                     }
                 }
-                give(mine);
+                if (ok) give(i % ACCS);
             }
+            if (STAGED && first) lin_stores_done();
         }
         if (!ok) *ab = 1;
     }
@@ -697,10 +818,12 @@ struct LinRowParams {
     const int32_t *tokens;
     const float *glp, *gent;  // null in the forward pass
     int *src, *pos, *kexp;    // [R]; kexp null in the forward pass
+    int *tokc;                // the compact rows' tokens, or null
     bool raise;
 };
 __global__ void __launch_bounds__(1024) lin_rows_kernel(LinRowParams p) {
     __shared__ int s_warp[32], s_exp;
+    pdl_allow_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int base = 0, least = 1 << 20;
     if (threadIdx.x == 0) s_exp = 1 << 20;
@@ -717,7 +840,10 @@ __global__ void __launch_bounds__(1024) lin_rows_kernel(LinRowParams p) {
         const int at = base + before + __popc(mask & ((1u << lane) - 1));
         base += all;
         if (r < p.R) p.pos[r] = on ? at : -1;
-        if (on) p.src[at] = r;
+        if (on) {
+            p.src[at] = r;
+            if (p.tokc) p.tokc[at] = p.tokens ? p.tokens[r] : -1;
+        }
         if (p.kexp && r < p.R) {
             int k = 0;
             if (on && p.raise) {
@@ -742,25 +868,72 @@ __global__ void __launch_bounds__(1024) lin_rows_kernel(LinRowParams p) {
 
 // The live rows side by side, zeros behind them up to a whole tile; in fp16, for dW, once more, each lowered by what its dZ is raised more
 // than the least: rows whose gradients are far below the largest's lose bits that would not reach dW's either.
+// The CTAs behind those put the rows in the order of their tokens' tiles of 128 (and of the rows within one), `kLinSort` rows at a time, so that
+// dW's epilogue finds a tile's: sorted[start[b] .. start[b + 1]) are those of tile b.  A row's place is the number of rows before it, counted
+// by 8 lanes.
 struct LinGatherParams {
     const LinHeader *head;
     const uint16_t *h;
     int64_t stride;
     int d, tile;
     const int *src, *kexp;
-    const int32_t *tokens;  // may be null
-    int *tokc;              // [rows_cap]: the compact rows' tokens, or null
     uint16_t *out, *low;    // [rows_cap][d]; low null: not wanted
+    int row_ctas;           // along x; the others sort
+    const int *tokc;
+    int2 *sorted;           // [rows_cap]: row, token
+    int *start;             // [rows_cap / kLinSort up][buckets + 1]
+    int buckets;
 };
 __global__ void __launch_bounds__(256) lin_gather_kernel(LinGatherParams p) {
-    const int live = p.head->live, row = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    pdl_allow_dependents();
+    pdl_wait_prior_grids();
+    const int live = p.head->live, lane = threadIdx.x & 31;
+    if ((int)blockIdx.x >= p.row_ctas) {
+        if (blockIdx.y) return;
+        const int blocks = max((live + kLinSort - 1) / kLinSort, 1), part = threadIdx.x & 7;
+        const int64_t asks = (int64_t)blocks * (p.buckets + 1) + live, stride = (int64_t)(gridDim.x - p.row_ctas) * 32;
+        __shared__ __align__(16) int s_bucket[2048];
+        for (int64_t q0 = (int64_t)(blockIdx.x - p.row_ctas) * 32; q0 < asks; q0 += stride) {  // (whole CTAs)
+            const int64_t q = q0 + threadIdx.x / 8;
+            const bool row = q < live;
+            const int64_t y = q - live;
+            const int me = row ? (int)q : 0, block = row ? me / kLinSort : (int)min(y / (p.buckets + 1), (int64_t)(blocks - 1));
+            const int token = row ? p.tokc[me] : 0, bucket = row ? token >> 7 : (int)(y - (int64_t)block * (p.buckets + 1));
+            int before = 0;
+            // (a CTA's asks may be of different blocks: all of the rows go by, those of others count as behind)
+            const int first = (int)(q0 < live ? q0 / kLinSort : min((q0 - live) / (p.buckets + 1), (int64_t)(blocks - 1)));
+            const int64_t q1 = min(q0 + 31, asks - 1);
+            const int last = q1 < live ? (int)(q1 / kLinSort) : q0 < live ? blocks - 1 : (int)min((q1 - live) / (p.buckets + 1), (int64_t)(blocks - 1));
+            const int r_first = q0 < live && q1 >= live ? 0 : first * kLinSort;
+            for (int r0 = r_first; r0 < min(live, (last + 1) * kLinSort); r0 += 2048) {
+                __syncthreads();
+                for (int x = threadIdx.x; x < 2048; x += 256) s_bucket[x] = r0 + x < live ? p.tokc[r0 + x] >> 7 : INT32_MAX;
+                __syncthreads();
+                if (r0 / kLinSort != block) continue;
+#pragma unroll 8
+                for (int x = 4 * part; x < 2048; x += 32) {
+                    const int4 b = *reinterpret_cast<const int4 *>(s_bucket + x);
+                    const int d = row ? me - r0 - x : 0;  // (of equal ones those before this row count)
+                    before += (b.x < bucket + (d > 0)) + (b.y < bucket + (d > 1)) + (b.z < bucket + (d > 2)) + (b.w < bucket + (d > 3));
+                }
+            }
+#pragma unroll
+            for (int d = 1; d < 8; d <<= 1) before += __shfl_xor_sync(0xffffffffu, before, d);
+            if (part == 0 && q < asks) {
+                if (row) p.sorted[block * kLinSort + before] = make_int2(me, token);
+                else p.start[y] = before;
+            }
+        }
+        return;
+    }
+    const int row = blockIdx.x * 8 + (threadIdx.x >> 5), x0 = blockIdx.y * kLinGatherCols, x1 = min(p.d, x0 + kLinGatherCols);
     if (row >= max((live + p.tile - 1) / p.tile, 1) * p.tile) return;
     uint16_t *o = p.out + (int64_t)row * p.d, *o2 = p.low ? p.low + (int64_t)row * p.d : nullptr;
     const int r = row < live ? p.src[row] : 0, down = o2 && row < live ? min(p.head->exp - p.kexp[r], 0) : 0;
-    if (p.tokc && lane == 0) p.tokc[row] = row < live && p.tokens ? p.tokens[r] : -1;
     const uint16_t *h = p.h + r * p.stride;
     const float f = pow2f(max(down, -126));
-    for (int x = 8 * lane; x < p.d; x += 256) {
+#pragma unroll 4
+    for (int x = x0 + 8 * lane; x < x1; x += 256) {
         const uint4 v = row < live ? *reinterpret_cast<const uint4 *>(h + x) : make_uint4(0, 0, 0, 0);
         *reinterpret_cast<uint4 *>(o + x) = v;
         if (!o2) continue;
@@ -788,6 +961,7 @@ struct LinJoinParams {
 template <int ROWS>
 __global__ void __launch_bounds__(256) lin_join_kernel(LinJoinParams p) {
     constexpr int G = 256 / ROWS;
+    pdl_wait_prior_grids();
     __shared__ float s_sums[3][G][ROWS];
     const int group = threadIdx.x / ROWS, lane = threadIdx.x % ROWS, r = blockIdx.x * ROWS + lane;
     const bool in = r < p.R;
@@ -840,20 +1014,29 @@ struct LinOutParams {
     const uint16_t *w;
     int64_t w_stride;
     float scale;
-    uint16_t *out;
+    uint16_t *out;      // or null
     int64_t stride;
+    uint16_t *dw;       // or null: made NaN after a failed wait, as out is
+    int64_t dw_stride;
 };
+constexpr int kLinOutCols = 512;  // of a warp
 template <int TYPE>
 __global__ void __launch_bounds__(256) lin_out_kernel(LinOutParams p) {
-    const int r = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-    if (r >= p.R) return;
+    pdl_wait_prior_grids();
+    const bool failed = p.head->err != 0;
+    const int lane = threadIdx.x & 31, r = blockIdx.x * 8 + (threadIdx.x >> 5), x0 = blockIdx.y * kLinOutCols, x1 = min(p.d, x0 + kLinOutCols);
+    if (failed && p.dw)
+        for (int64_t v = r; v < p.V; v += 8 * (int64_t)gridDim.x)
+            for (int x = x0 + lane; x < x1; x += 32) p.dw[v * p.dw_stride + x] = 0x7fff;
+    if (r >= p.R || !p.out) return;
     const int at = p.pos[r];
-    const float k = p.head->err ? __int_as_float(0x7fc00000) : p.scale * pow2f(-p.kexp[r]);
+    const float k = failed ? __int_as_float(0x7fc00000) : p.scale * pow2f(-p.kexp[r]);
     uint16_t *o = p.out + r * p.stride;
     const int tok = p.tokens && at >= 0 ? p.tokens[r] : -1;
     const bool fix = tok >= 0 && tok < p.V;
     const float f = fix ? p.delta[at] : 0.f;
-    for (int x = 8 * lane; x < p.d; x += 256) {
+#pragma unroll 2
+    for (int x = x0 + 8 * lane; x < x1; x += 256) {
         float v[8] = {};
         if (fix) {
             const uint4 y = *reinterpret_cast<const uint4 *>(p.w + tok * p.w_stride + x);
@@ -866,6 +1049,7 @@ __global__ void __launch_bounds__(256) lin_out_kernel(LinOutParams p) {
             }
         }
         if (at >= 0) {
+#pragma unroll 4
             for (int s = 0; s < p.splits; ++s) {
                 const float4 *q = reinterpret_cast<const float4 *>(p.acc + ((int64_t)s * p.rows_cap + at) * p.d + x);
                 const float4 a = q[0], b = q[1];
@@ -873,10 +1057,10 @@ __global__ void __launch_bounds__(256) lin_out_kernel(LinOutParams p) {
                 v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
             }
         }
-        uint16_t h[8];
+        uint32_t h[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = at >= 0 ? lin_round<TYPE>(v[e] * k) : (uint16_t)0;
-        *reinterpret_cast<uint4 *>(o + x) = pack8(h);
+        for (int e = 0; e < 4; ++e) h[e] = at >= 0 ? pack_grad<TYPE>(v[2 * e] * k, v[2 * e + 1] * k) : 0u;
+        *reinterpret_cast<uint4 *>(o + x) = make_uint4(h[0], h[1], h[2], h[3]);
     }
 }
 
@@ -887,15 +1071,25 @@ inline int64_t lin_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 struct LinPlan {
     int ctas, rows_cap, tiles;        // CTAs of a tile; rows up to whole tiles; tiles of tokens
     bool gather;                      // the live rows are gathered
-    int piece, splits;                // gradient: tokens of a piece, parts of its dH
-    size_t src, pos, kexp, tokc, delta, rows, low, part, ztok, dz, acc, bytes;
+    int piece, splits, buckets;       // gradient: tokens of a piece, parts of its dH, tiles of 128 tokens
+    size_t src, pos, kexp, tokc, sorted, start, delta, rows, low, part, ztok, dz, acc, bytes;
 };
+// Tokens of a piece.  76 tiles of 256 (152 of 128) are as many as there are pairs of CTAs (CTAs), so that whatever the rows' tiles the logits' come
+// out even; dZ is kept to 192 MB.  Up to 128 rows the piece's weights, which are read twice, have to stay in L2 besides.
+inline int64_t lin_piece(int rows_cap, int d, int V, int ctas) {
+    constexpr int64_t kEven = 76 * 256;
+    const int64_t most = ((int64_t)192 << 20) / 2 / rows_cap;
+    int64_t piece = ctas == 1 ? (d <= 2304 ? kEven : kEven / 2) : most >= kEven ? most / kEven * kEven : most / 256 * 256;
+    if (piece < 1024) piece = 1024;
+    const int64_t all = lin_up(V, 256);
+    return piece < all ? piece : all;
+}
 inline LinPlan lin_plan(int R, int d, int V, bool backward) {
     LinPlan q{};
     q.ctas = R > kLinRows ? 2 : 1;
-    const int tm = kLinRows * q.ctas;
+    const int tm = kLinRows * q.ctas, cols = lin_cols(q.ctas);
     q.rows_cap = (int)lin_up(R, tm);
-    q.tiles = (int)lin_up(V, kLinCols) / kLinCols;
+    q.tiles = (int)lin_up(V, cols) / cols;
     q.gather = backward || R > kLinRows;
     size_t at = sizeof(LinHeader);
     auto take = [&](size_t bytes) {
@@ -912,20 +1106,18 @@ inline LinPlan lin_plan(int R, int d, int V, bool backward) {
         q.part = take((size_t)3 * q.tiles * q.rows_cap * 4);
         q.ztok = take((size_t)q.rows_cap * 4);
     } else {
+        q.buckets = (int)lin_up(V, kLinRows) / kLinRows;
         q.kexp = take((size_t)R * 4);
         q.tokc = take((size_t)q.rows_cap * 4);
+        q.sorted = take((size_t)q.rows_cap * 8);
+        q.start = take((size_t)(lin_up(R, kLinSort) / kLinSort) * (q.buckets + 1) * 4);
         q.delta = take((size_t)q.rows_cap * 4);
         q.low = take((size_t)q.rows_cap * d * 2);
-        const int workers = kLinWorkers / q.ctas, mt = q.rows_cap / tm, nt = (int)lin_up(d, kLinCols) / kLinCols;
-        int64_t piece = ((int64_t)192 << 20) / 2 / q.rows_cap;
-        piece = piece / kLinCols * kLinCols;
-        if (piece < 4 * kLinCols) piece = 4 * kLinCols;
-        if (piece > 16384) piece = 16384;
-        if (piece > lin_up(V, kLinCols)) piece = lin_up(V, kLinCols);
-        q.piece = (int)piece;
-        const int64_t kc = lin_up(piece < V ? piece : V, kLinK) / kLinK, kr = lin_up(R, kLinK) / kLinK, jw = lin_up(piece, tm) / tm * nt;
-        const int64_t load = (jw * kr + (int64_t)mt * nt * kc) / workers + 1;
-        int64_t s = workers / ((int64_t)mt * nt);
+        const int64_t workers = kLinWorkers / q.ctas, mt = q.rows_cap / tm, nt = lin_up(d, cols) / cols;
+        q.piece = (int)lin_piece(q.rows_cap, d, V, q.ctas);
+        const int64_t kc = lin_up(q.piece < V ? q.piece : V, kLinK) / kLinK, kr = lin_up(R, kLinK) / kLinK, jw = lin_up(q.piece, tm) / tm * nt;
+        const int64_t load = (jw * kr + mt * nt * kc) / workers + 1;
+        int64_t s = workers / (mt * nt);
         if (s < (kc + load - 1) / load) s = (kc + load - 1) / load;
         if (s < 1) s = 1;
         if (s > kc) s = kc;

@@ -2,6 +2,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -36,15 +37,16 @@ CUtensorMap rows_map(const Operand &x, int box) {
 }
 
 bool sizes_ok(int type, int R, int d, int V, float scale) {
-    return (type == SARA_BF16 || type == SARA_FP16) && R >= 0 && R <= (1 << 24) && d >= 8 && d <= 65536 && d % 8 == 0 && V >= 1 &&
+    return (type == SARA_BF16 || type == SARA_FP16) && R >= 0 && R <= (1 << 22) && d >= 8 && d <= 65536 && d % 8 == 0 && V >= 1 &&
            V <= (1 << 24) && scale > 0.f && std::isfinite(scale);
 }
 
 template <int MODE, int CTAS, int TYPE>
-void launch(cudaStream_t s, int sms, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &a2, const CUtensorMap &b2, const LinParams &p) {
+void launch(cudaStream_t s, int sms, bool after, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &a2, const CUtensorMap &b2,
+            const CUtensorMap &out, const LinParams &p) {
     const auto kern = lin_kernel<MODE, CTAS, TYPE>;
-    CK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lin_smem(CTAS)));
-    launch_cluster(s, false, dim3((unsigned)(sms / CTAS * CTAS)), dim3(kLinThreads), lin_smem(CTAS), CTAS, kern, a, b, a2, b2, p);
+    CK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lin_smem(MODE, CTAS)));
+    launch_cluster(s, after, dim3((unsigned)(sms / CTAS * CTAS)), dim3(kLinThreads), lin_smem(MODE, CTAS), CTAS, kern, a, b, a2, b2, out, p);
 }
 
 template <typename T>
@@ -52,19 +54,19 @@ T *at(void *ws, size_t off) {
     return reinterpret_cast<T *>(static_cast<uint8_t *>(ws) + off);
 }
 
-// The live rows gathered, with what the gradient's rows are raised by
+// The live rows gathered, with what the gradient's rows are raised by, and (where dW is wanted) the order of their tokens
 template <int TYPE>
-void gather(cudaStream_t s, void *ws, const LinPlan &q, int R, int d, const void *hidden, int64_t stride, const int32_t *tokens, const float *glp,
-            const float *gent, bool backward) {
-    int *kexp = backward ? at<int>(ws, q.kexp) : nullptr;
-    lin_rows_kernel<<<1, 1024, 0, s>>>({at<LinHeader>(ws, 0), R, tokens, glp, gent, at<int>(ws, q.src), at<int>(ws, q.pos), kexp,
-                                        TYPE == SARA_FP16});
+void gather(cudaStream_t s, void *ws, const LinPlan &q, const Operand &h, const int32_t *tokens, const float *glp, const float *gent, bool backward,
+            bool sort) {
+    const int R = (int)h.rows, d = (int)h.d;
+    int *kexp = backward ? at<int>(ws, q.kexp) : nullptr, *tokc = backward ? at<int>(ws, q.tokc) : nullptr;
+    lin_rows_kernel<<<1, 1024, 0, s>>>({at<LinHeader>(ws, 0), R, tokens, glp, gent, at<int>(ws, q.src), at<int>(ws, q.pos), kexp, tokc, TYPE == SARA_FP16});
     CK(cudaGetLastError());
-    lin_gather_kernel<<<(unsigned)q.rows_cap / 8, 256, 0, s>>>({at<LinHeader>(ws, 0), static_cast<const uint16_t *>(hidden), stride, d,
-                                                                     kLinRows * q.ctas, at<int>(ws, q.src), kexp, tokens,
-                                                               backward ? at<int>(ws, q.tokc) : nullptr,
-                                                               at<uint16_t>(ws, q.rows), backward && TYPE == SARA_FP16 ? at<uint16_t>(ws, q.low) : nullptr});
-    CK(cudaGetLastError());
+    const int row_ctas = q.rows_cap / 8, sort_ctas = sort ? (int)std::min<int64_t>(((int64_t)R + q.buckets + 32) / 32, 2048) : 0;
+    const LinGatherParams p{at<LinHeader>(ws, 0), static_cast<const uint16_t *>(h.p), h.stride, d, kLinRows * q.ctas, at<int>(ws, q.src), kexp,
+                            at<uint16_t>(ws, q.rows), backward && TYPE == SARA_FP16 ? at<uint16_t>(ws, q.low) : nullptr, row_ctas, tokc,
+                            backward ? at<int2>(ws, q.sorted) : nullptr, backward ? at<int>(ws, q.start) : nullptr, q.buckets};
+    launch_cluster(s, true, dim3((unsigned)(row_ctas + sort_ctas), (unsigned)((d + kLinGatherCols - 1) / kLinGatherCols)), dim3(256), 0, 1, lin_gather_kernel, p);
 }
 
 template <int CTAS, int TYPE>
@@ -73,7 +75,7 @@ void score(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand &h
     const int R = (int)h.rows, d = (int)h.d, V = (int)w.rows;
     Operand x = h;
     if (q.gather) {
-        gather<TYPE>(s, ws, q, R, d, h.p, h.stride, tokens, nullptr, nullptr, false);
+        gather<TYPE>(s, ws, q, h, tokens, nullptr, nullptr, false, false);
         x = {at<void>(ws, q.rows), q.rows_cap, d, d};
     }
     LinParams p{};
@@ -89,20 +91,20 @@ void score(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand &h
     p.ztok = at<float>(ws, q.ztok);
     p.rows_cap = q.rows_cap;
     p.token_tiles = q.tiles;
-    const CUtensorMap a = rows_map(x, kLinRows), b = rows_map(w, kLinCols / CTAS);
-    launch<LIN_SCORE, CTAS, TYPE>(s, sms, a, b, a, b, p);
+    const CUtensorMap a = rows_map(x, kLinRows), b = rows_map(w, kLinRows);
+    launch<LIN_SCORE, CTAS, TYPE>(s, sms, q.gather, a, b, a, b, a, p);
     const LinJoinParams j{p.head, R, V, q.tiles, q.rows_cap, tokens, q.gather ? at<int>(ws, q.pos) : nullptr, p.part, p.ztok, scale, logprob, entropy, stats};
-    if (R <= 64) lin_join_kernel<1><<<(unsigned)R, 256, 0, s>>>(j);
-    else lin_join_kernel<8><<<(unsigned)(R + 7) / 8, 256, 0, s>>>(j);
-    CK(cudaGetLastError());
+    if (R <= 64) launch_cluster(s, true, dim3((unsigned)R), dim3(256), 0, 1, lin_join_kernel<1>, j);
+    else launch_cluster(s, true, dim3((unsigned)(R + 7) / 8), dim3(256), 0, 1, lin_join_kernel<8>, j);
 }
 
 template <int CTAS, int TYPE>
 void gradient(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand &h, const Operand &w, const int32_t *tokens, const float *stats,
               const float *entropy, const float *glp, const float *gent, float scale, const Operand &dh, const Operand &dw) {
     const int R = (int)h.rows, d = (int)h.d, V = (int)w.rows;
-    gather<TYPE>(s, ws, q, R, d, h.p, h.stride, tokens, glp, gent, true);
-    const Operand x{at<void>(ws, q.rows), q.rows_cap, d, d}, dz{at<void>(ws, q.dz), q.rows_cap, q.piece, q.piece};
+    gather<TYPE>(s, ws, q, h, tokens, glp, gent, true, dw.p != nullptr);
+    const Operand x{at<void>(ws, q.rows), q.rows_cap, d, d}, low{TYPE == SARA_FP16 ? at<void>(ws, q.low) : x.p, q.rows_cap, d, d};
+    const Operand dz{at<void>(ws, q.dz), (int64_t)q.rows_cap * (q.piece / 64), 64, 64};  // blocks of 64 columns
     LinParams p{};
     p.head = at<LinHeader>(ws, 0);
     p.R = R;
@@ -117,31 +119,33 @@ void gradient(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand
     p.entropy = entropy;
     p.glp = glp;
     p.gent = gent;
-    p.dz = at<uint16_t>(ws, q.dz);
-    p.piece = q.piece;
-    p.tokc = at<int>(ws, q.tokc);
+    p.sorted = at<int2>(ws, q.sorted);
+    p.start = at<int>(ws, q.start);
+    p.buckets = q.buckets;
     p.delta = at<float>(ws, q.delta);
-    p.low = at<uint16_t>(ws, TYPE == SARA_FP16 ? q.low : q.rows);
+    p.low = static_cast<const uint16_t *>(low.p);
     p.acc = at<float>(ws, q.acc);
     p.splits = q.splits;
-    p.dw = static_cast<uint16_t *>(const_cast<void *>(dw.p));
-    p.dw_stride = dw.stride;
     p.dh = dh.p != nullptr;
-    const CUtensorMap xk = rows_map(x, kLinRows), wk = rows_map(w, kLinCols / CTAS), dzk = rows_map(dz, kLinRows);
-    const CUtensorMap dzm = rows_map(dz, kLinK), wn = rows_map(w, kLinK);
-    const CUtensorMap xn = rows_map({TYPE == SARA_FP16 ? at<void>(ws, q.low) : x.p, x.rows, x.stride, x.d}, kLinK);
+    p.dw = dw.p != nullptr;
+    const CUtensorMap xk = rows_map(x, kLinRows), wk = rows_map(w, kLinRows), dzk = rows_map(dz, kLinRows);
+    const CUtensorMap dzm = rows_map(dz, kLinK), wn = rows_map(w, kLinK), xn = rows_map(low, kLinK), out = dw.p ? rows_map(dw, kLinRows) : dzk;
     for (int v = 0; v < V; v += q.piece) {
         p.v0 = v;
         p.cols = V - v < q.piece ? V - v : q.piece;
         p.first = v == 0;
-        launch<LIN_DZ, CTAS, TYPE>(s, sms, xk, wk, xk, wk, p);
-        launch<LIN_GRAD, CTAS, TYPE>(s, sms, dzk, wn, dzm, xn, p);
+        p.out = at<uint16_t>(ws, q.dz);
+        p.out_stride = 64;
+        p.wide = true;
+        launch<LIN_DZ, CTAS, TYPE>(s, sms, true, xk, wk, xk, wk, dzk, p);
+        p.out = static_cast<uint16_t *>(const_cast<void *>(dw.p));
+        p.out_stride = dw.stride;
+        p.wide = (reinterpret_cast<uintptr_t>(dw.p) & 31) == 0 && dw.stride % 16 == 0;
+        launch<LIN_GRAD, CTAS, TYPE>(s, sms, true, dzk, wn, dzm, xn, out, p);
     }
-    if (!dh.p) return;
-    lin_out_kernel<TYPE><<<(unsigned)(R + 7) / 8, 256, 0, s>>>({p.head, R, d, q.splits, q.rows_cap, at<int>(ws, q.pos), p.kexp, p.acc, p.delta,
-                                                               tokens, V, static_cast<const uint16_t *>(w.p), w.stride, scale,
-                                                               static_cast<uint16_t *>(const_cast<void *>(dh.p)), dh.stride});
-    CK(cudaGetLastError());
+    const LinOutParams o{p.head, R, d, q.splits, q.rows_cap, at<int>(ws, q.pos), p.kexp, p.acc, p.delta, tokens, V, static_cast<const uint16_t *>(w.p), w.stride,
+                         scale, static_cast<uint16_t *>(const_cast<void *>(dh.p)), dh.stride, static_cast<uint16_t *>(const_cast<void *>(dw.p)), dw.stride};
+    launch_cluster(s, true, dim3((unsigned)(R + 7) / 8, (unsigned)((d + kLinOutCols - 1) / kLinOutCols)), dim3(256), 0, 1, lin_out_kernel<TYPE>, o);
 }
 
 template <typename F>
