@@ -19,8 +19,9 @@
 // kept (delta) and added to both gradients in fp32.
 //
 // Warp roles (320 threads): warp 0 producer, warp 1 MMA issuer and tensor-memory owner, warps 2..9 epilogue (warp w: the rows of
-// tensor-memory lanes 32 (w % 4) ..): of the scores every tile, 128 columns a thread, which are in registers before the accumulator is given
-// back; of the others warps 2..5 and 6..9 alternate tiles, one of the two accumulators each.
+// tensor-memory lanes 32 (w % 4) .., columns 128 ((w - 2) / 4) ..).  A tile's 128 columns are in a thread's registers before its accumulator,
+// one of two, is given back: the epilogue has a tile's time, not what is left of it (dZ of 4,096 rows: 161 us a piece with
+// warps 2..5 and 6..9 on alternate tiles, reading their accumulator as they go).
 #pragma once
 #include <type_traits>
 
@@ -32,9 +33,7 @@
 namespace sara {
 
 constexpr int kLinThreads = 320;
-constexpr int kLinRows = 128, kLinK = 64;  // rows of a CTA's tile; elements of a chunk
-// Columns of a tile: with one CTA the work is bound by memory, and smaller tiles share it out more evenly
-__host__ __device__ constexpr int lin_cols(int ctas) { return ctas == 2 ? 256 : 128; }
+constexpr int kLinRows = 128, kLinCols = 256, kLinK = 64;  // of a CTA's tile; elements of a chunk
 constexpr int kLinMaxSplits = 32;
 constexpr int kLinSort = 65536, kLinGatherCols = 1024;  // rows that are sorted together; columns of a warp that gathers
 constexpr int kLinWorkers = 152;  // SMs that a plan counts on (on a GPU with others it is as right, if less even)
@@ -47,23 +46,26 @@ struct LinHeader {
     int pad[61];
 };
 
-constexpr int kLinHalf = kLinRows * kLinK * 2;                     // 16 KB: of a stage A's half, B's (128 rows of either), of a block on its way out
+constexpr int kLinBlock = kLinRows * kLinK * 2;  // 16 KB: 128 rows of a chunk
 enum LinMode : int {
     LIN_SCORE = 0,  // tiles of logits -> partial sums
     LIN_DZ = 1,     // tiles of logits -> dZ of a piece
     LIN_GRAD = 2,   // dZ of a piece -> dH's sums, dW
 };
 // One CTA stores dZ and dW by way of shared memory, two blocks of 64 columns for each half of its epilogue: whole lines, where each thread's own row
-// would cost the memory pipe an access a lane.  Two CTAs store from registers: their operands leave shared memory no time.  (DZ of 4,096 rows:
-// 135 us a piece, 156 by way of it.)
+// costs the memory pipe an access a lane.  Two CTAs store from registers: their operands leave shared memory no time.
 __host__ __device__ constexpr bool lin_staged(int mode, int ctas) { return mode != LIN_SCORE && ctas == 1; }
-__host__ __device__ constexpr int lin_stages(int mode, int ctas) { return lin_staged(mode, ctas) ? 4 : 6; }
-__host__ __device__ constexpr size_t lin_smem(int mode, int ctas) { return 1024 + (size_t)(2 * lin_stages(mode, ctas) + (lin_staged(mode, ctas) ? 4 : 0)) * kLinHalf; }
+__host__ __device__ constexpr int lin_stage_bytes(int ctas) { return kLinBlock * (1 + 2 / ctas); }
+__host__ __device__ constexpr int lin_stages(int mode, int ctas) { return ctas == 2 ? 6 : lin_staged(mode, ctas) ? 3 : 4; }
+__host__ __device__ constexpr size_t lin_smem(int mode, int ctas) {
+    return 1024 + (size_t)lin_stages(mode, ctas) * lin_stage_bytes(ctas) + (lin_staged(mode, ctas) ? 4 : 0) * kLinBlock;
+}
 constexpr int kLinHits = 8;  // rows of a tile of tokens that wait in shared memory for dW's epilogue
 
 struct LinParams {
     LinHeader *head;
     int R, d, V;
+    int a_rows;        // of a box of A (up to 128 rows in all: no more than there are; what the others hold does not matter)
     const int32_t *tokens;
     const int *src;    // compact row -> row, or null: the same
     const int *kexp;   // [row] power of two that dZ's row is raised by
@@ -92,16 +94,15 @@ struct LinParams {
 // Chunks of a part of a logit's sum: with two CTAs a tile's epilogue has no time for more parts
 __host__ __device__ constexpr int lin_part(int ctas) { return ctas == 2 ? 8 : 2; }
 struct LinSmem {
-    uint64_t full[6], empty[6], acc_full[4], acc_empty[4], drain;
+    uint64_t full[6], empty[6], acc_full[2], acc_empty[2], drain;
     uint32_t tmem_base;
     int abort, stop[2];                  // stop: the epilogue's, for two tiles in turn
 };
 struct LinScoreSmem {
     float sums[2][3][kLinRows];          // of the second half's columns, for two tiles in turn
 };
-template <int COLS>
 struct LinGradSmem {
-    uint16_t row[2][2][kLinHits][COLS];  // for each half of the epilogue, two tiles in turn
+    uint16_t row[2][2][kLinHits][kLinCols / 2];  // for each half of the columns, two tiles in turn
 };
 struct LinNoSmem {};
 
@@ -197,7 +198,7 @@ struct LinJob {
 // LIN_GRAD: dH's jobs are long, so the workers that have one more of them get fewer of dW's.
 template <int MODE, int CTAS>
 struct LinWork {
-    static constexpr int TM = kLinRows * CTAS, COLS = lin_cols(CTAS);
+    static constexpr int TM = kLinRows * CTAS, COLS = kLinCols;
     int w, W, mt, nt, count;
     int64_t tiles;
     // LIN_GRAD
@@ -285,9 +286,8 @@ struct LinSums {
     }
 };
 
-// 32 columns of a lane, or their sum with v; the wait is part of the instruction, so that nothing uses the values before it
-template <bool ADD>
-__device__ __forceinline__ void lin_tmem_load(uint32_t taddr, float *v) {
+// 32 columns of a lane are added to v; the wait is part of the instruction, so that nothing uses the values before it
+__device__ __forceinline__ void lin_tmem_add(uint32_t taddr, float *v) {
     uint32_t r[32];
     __syncwarp();
     asm volatile(
@@ -300,28 +300,41 @@ __device__ __forceinline__ void lin_tmem_load(uint32_t taddr, float *v) {
         : "r"(taddr)
         : "memory");
 #pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = ADD ? v[i] + __uint_as_float(r[i]) : __uint_as_float(r[i]);
+    for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(r[i]);
 }
 
-template <int TYPE>
-__device__ __forceinline__ float lin_float(uint16_t x) {
-    return TYPE == SARA_BF16 ? bf16_to_f32(x) : f16_to_f32(x);
-}
-template <int TYPE>
-__device__ __forceinline__ uint16_t lin_round(float x) {
-    return TYPE == SARA_BF16 ? f32_to_bf16(x) : __half_as_ushort(__float2half_rn(x));
+// 128 columns of a lane
+__device__ __forceinline__ void lin_tmem_load128(uint32_t taddr, float (&v)[128]) {
+    __syncwarp();
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x128.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32,%33,%34,%35,%36,%3"
+        "7,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63,%64,%65,%66,%67,%68,%69,%70,%71,%7"
+        "2,%73,%74,%75,%76,%77,%78,%79,%80,%81,%82,%83,%84,%85,%86,%87,%88,%89,%90,%91,%92,%93,%94,%95,%96,%97,%98,%99,%100,%101,%102,%103,%104,%105,"
+        "%106,%107,%108,%109,%110,%111,%112,%113,%114,%115,%116,%117,%118,%119,%120,%121,%122,%123,%124,%125,%126,%127}, [%128];\n\ttcgen05.wait::ld.sync.aligned;"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), 
+          "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), 
+          "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]), "=f"(v[32]), "=f"(v[33]), 
+          "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]), "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), 
+          "=f"(v[45]), "=f"(v[46]), "=f"(v[47]), "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]), 
+          "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63]), "=f"(v[64]), "=f"(v[65]), "=f"(v[66]), 
+          "=f"(v[67]), "=f"(v[68]), "=f"(v[69]), "=f"(v[70]), "=f"(v[71]), "=f"(v[72]), "=f"(v[73]), "=f"(v[74]), "=f"(v[75]), "=f"(v[76]), "=f"(v[77]), 
+          "=f"(v[78]), "=f"(v[79]), "=f"(v[80]), "=f"(v[81]), "=f"(v[82]), "=f"(v[83]), "=f"(v[84]), "=f"(v[85]), "=f"(v[86]), "=f"(v[87]), "=f"(v[88]), 
+          "=f"(v[89]), "=f"(v[90]), "=f"(v[91]), "=f"(v[92]), "=f"(v[93]), "=f"(v[94]), "=f"(v[95]), "=f"(v[96]), "=f"(v[97]), "=f"(v[98]), "=f"(v[99]), 
+          "=f"(v[100]), "=f"(v[101]), "=f"(v[102]), "=f"(v[103]), "=f"(v[104]), "=f"(v[105]), "=f"(v[106]), "=f"(v[107]), "=f"(v[108]), "=f"(v[109]), 
+          "=f"(v[110]), "=f"(v[111]), "=f"(v[112]), "=f"(v[113]), "=f"(v[114]), "=f"(v[115]), "=f"(v[116]), "=f"(v[117]), "=f"(v[118]), "=f"(v[119]), 
+          "=f"(v[120]), "=f"(v[121]), "=f"(v[122]), "=f"(v[123]), "=f"(v[124]), "=f"(v[125]), "=f"(v[126]), "=f"(v[127])
+        : "r"(taddr)
+        : "memory");
 }
 
 template <int MODE, int CTAS, int TYPE>
 __global__ void __launch_bounds__(kLinThreads, 1)
 lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmA2,
            const __grid_constant__ CUtensorMap tmB2, const __grid_constant__ CUtensorMap tmOut, LinParams p) {
-    constexpr int STAGES = lin_stages(MODE, CTAS), STAGE = 2 * kLinHalf, COLS = lin_cols(CTAS), BN = COLS / CTAS, PART = lin_part(CTAS);
-    constexpr int ACCS = 512 / COLS;  // accumulators
-    static_assert(BN == kLinRows, "B's share of a stage is as large as A's");
+    constexpr int STAGES = lin_stages(MODE, CTAS), STAGE = lin_stage_bytes(CTAS), COLS = kLinCols, PART = lin_part(CTAS);
     extern __shared__ uint8_t smem_raw[];
     __shared__ LinSmem S;
-    __shared__ __align__(16) std::conditional_t<MODE == LIN_SCORE, LinScoreSmem, std::conditional_t<MODE == LIN_GRAD, LinGradSmem<COLS>, LinNoSmem>> E;
+    __shared__ __align__(16) std::conditional_t<MODE == LIN_SCORE, LinScoreSmem, std::conditional_t<MODE == LIN_GRAD, LinGradSmem, LinNoSmem>> E;
     uint8_t *ring = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CTAS == 2 ? (int)cluster_rank() : 0;
@@ -331,9 +344,9 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             mbar_init(&S.full[s], 1);
             mbar_init(&S.empty[s], 1);
         }
-        for (int a = 0; a < ACCS; ++a) {
+        for (int a = 0; a < 2; ++a) {
             mbar_init(&S.acc_full[a], 1);
-            mbar_init(&S.acc_empty[a], (MODE == LIN_SCORE ? 8 : 4) * CTAS);
+            mbar_init(&S.acc_empty[a], 8 * CTAS);
         }
         mbar_init(&S.drain, 1);
         S.abort = S.stop[0] = S.stop[1] = 0;
@@ -365,18 +378,18 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             if (!work.job(p, i, j)) break;
             const bool mn_a = MODE == LIN_GRAD && j.kind == 1, mn_b = MODE == LIN_GRAD;
             const int m = j.m0 + rank * kLinRows, bn = j.n / CTAS, n = j.n0 + rank * bn;
-            const uint32_t bytes = (uint32_t)(kLinHalf + bn * kLinK * 2) * CTAS;
+            const uint32_t bytes = (uint32_t)((mn_a ? kLinBlock : p.a_rows * kLinK * 2) + bn * kLinK * 2) * CTAS;
 #pragma unroll 1
             for (int k = j.k0; k < j.k1; ++k) {
                 if (loads >= (uint32_t)STAGES) ok = __all_sync(0xffffffffu, mbar_wait(&S.empty[s], ph, err) && !*ab);
                 if (!ok) break;
                 if (elect_one()) {
-                    uint8_t *a = ring + s * STAGE, *b = a + kLinHalf;
+                    uint8_t *a = ring + s * STAGE, *b = a + kLinBlock;
                     const uint32_t bar = CTAS == 2 ? cluster_addr(&S.full[s], 0) : smem_u32(&S.full[s]);
                     if (rank == 0) mbar_arrive_expect_tx(&S.full[s], bytes);
                     if (mn_a) {  // (dZ: blocks of 64 columns one after the other)
                         lin_load<CTAS>(a, &tmA2, bar, 0, m / 64 * p.rows_cap + k * kLinK, pass);
-                        lin_load<CTAS>(a + kLinHalf / 2, &tmA2, bar, 0, (m / 64 + 1) * p.rows_cap + k * kLinK, pass);
+                        lin_load<CTAS>(a + kLinBlock / 2, &tmA2, bar, 0, (m / 64 + 1) * p.rows_cap + k * kLinK, pass);
                     } else if (MODE == LIN_GRAD) {
                         lin_load<CTAS>(a, &tmA, bar, 0, k * p.rows_cap + m, pass);
                     } else {
@@ -426,9 +439,9 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             for (int k = j.k0; k < j.k1; ++k) {
                 const bool begins = MODE == LIN_SCORE ? k % PART == 0 : k == j.k0, ends = k + 1 == j.k1 || (MODE == LIN_SCORE && (k + 1) % PART == 0);
                 if (begins) {
-                    a = it % ACCS;
+                    a = it & 1;
                     dacc = tmem + (uint32_t)(a * COLS);
-                    if (it >= ACCS) ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_empty[a], (uint32_t)((it / ACCS - 1) & 1), err) && !*ab);
+                    if (it >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_empty[a], (uint32_t)((it / 2 - 1) & 1), err) && !*ab);
                     if (!ok) break;
                     ++it;
                 }
@@ -439,7 +452,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     const uint32_t at = smem_u32(ring) + (uint32_t)(s * STAGE);
 #pragma unroll
                     for (int kk = 0; kk < 4; ++kk)
-                        lin_mma<CTAS>(dacc, sdesc_sw128(at + kk * step_a, kLinK * 128, 1024), sdesc_sw128(at + kLinHalf + kk * step_b, kLinK * 128, 1024),
+                        lin_mma<CTAS>(dacc, sdesc_sw128(at + kk * step_a, kLinK * 128, 1024), sdesc_sw128(at + kLinBlock + kk * step_b, kLinK * 128, 1024),
                                       idesc, !begins || kk > 0);
                     lin_commit<CTAS>(&S.empty[s]);
                     if (ends) lin_commit<CTAS>(&S.acc_full[a]);
@@ -458,8 +471,8 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         }
     } else {
         // ------------------------------------------------------------ epilogues
-        const int quarter = warp & 3, mine = (warp - 2) >> 2, lrow = quarter * 32 + lane;
-        const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16);
+        const int quarter = warp & 3, mine = (warp - 2) >> 2, lrow = quarter * 32 + lane, c0 = mine * 128;  // mine: which half of the columns
+        const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c0;
         bool ok = true;
         auto give = [&](int a) {  // the accumulator back
             tc_fence_before();
@@ -470,13 +483,11 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             }
         };
         auto wait = [&](int it) {  // for the it-th accumulator
-            ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_full[it % ACCS], (uint32_t)(it / ACCS & 1), err) && !*ab);
+            ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_full[it & 1], (uint32_t)(it / 2 & 1), err) && !*ab);
             tc_fence_after();
         };
         if constexpr (MODE == LIN_SCORE) {
             const float c = p.scale * kLog2e;
-            constexpr int HALF = COLS / 2;  // columns a thread
-            const int c0 = mine * HALF;
             int it = 0;
 #pragma unroll 1
             for (int i = 0; i < work.count; ++i) {
@@ -484,41 +495,40 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 if (!work.job(p, i, j)) break;
                 const int m = j.m0 + rank * kLinRows + lrow;  // row of A
                 const int tok = m < live && p.tokens ? p.tokens[p.src ? p.src[m] : m] : -1;
-                float v[HALF];
+                float v[128];
                 const int parts = (j.k1 + PART - 1) / PART;
 #pragma unroll 1
                 for (int q = 0; q < parts && ok; ++q, ++it) {
                     wait(it);
                     if (!ok) break;
-                    const uint32_t at = from + (uint32_t)(it % ACCS * COLS + c0);
+                    const uint32_t at = from + (uint32_t)((it & 1) * COLS);
                     if (q == 0) {
-#pragma unroll
-                        for (int cc = 0; cc < HALF / 32; ++cc) lin_tmem_load<false>(at + 32 * cc, v + 32 * cc);
+                        lin_tmem_load128(at, v);
                     } else {
 #pragma unroll
-                        for (int cc = 0; cc < HALF / 32; ++cc) lin_tmem_load<true>(at + 32 * cc, v + 32 * cc);
+                        for (int cc = 0; cc < 128 / 32; ++cc) lin_tmem_add(at + 32 * cc, v + 32 * cc);
                     }
-                    give(it % ACCS);
+                    give(it & 1);
                 }
                 LinSums x;
                 const int left = p.V - j.n0 - c0, at = tok - j.n0 - c0;  // columns that are tokens; the row's token
-                if ((unsigned)at < (unsigned)HALF) {
+                if ((unsigned)at < 128u) {
                     float z = 0.f;
 #pragma unroll
-                    for (int e = 0; e < HALF; ++e) z = e == at ? v[e] : z;
+                    for (int e = 0; e < 128; ++e) z = e == at ? v[e] : z;
                     p.ztok[m] = z;
                 }
-                if (left < HALF) {
+                if (left < 128) {
 #pragma unroll
-                    for (int e = 0; e < HALF; ++e) v[e] = e < left ? v[e] : -INFINITY;
+                    for (int e = 0; e < 128; ++e) v[e] = e < left ? v[e] : -INFINITY;
                 }
                 float n = v[0];
 #pragma unroll
-                for (int e = 1; e < HALF; ++e) n = fmaxf(n, v[e]);
+                for (int e = 1; e < 128; ++e) n = fmaxf(n, v[e]);
                 x.a = fmaxf(x.a, n);
                 float s0 = 0.f, s1 = 0.f, t1 = 0.f, tops = -1.f;
 #pragma unroll
-                for (int e = 0; e < HALF; e += 2) {
+                for (int e = 0; e < 128; e += 2) {
                     const float y0 = (v[e] - x.a) * c, y1 = (v[e + 1] - x.a) * c;
                     float w0 = exp2_approx(y0), w1 = exp2_approx(y1);
                     x.t = fmaf(w0, fmaxf(y0, -1000.f), x.t);  // (a logit of -inf adds nothing)
@@ -556,12 +566,12 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             // 64 columns of the tile's rows to `x`, `y` of the result.  One CTA: by way of one of this half's two places in shared memory, which the
             // block before the last one has left (after a failed wait the barriers go on and nothing is stored).  Two: each thread its row's.
             constexpr bool STAGED = lin_staged(MODE, CTAS);
-            const uint32_t out = smem_u32(ring) + (uint32_t)(STAGES * STAGE + mine * 2 * kLinHalf);
+            const uint32_t out = smem_u32(ring) + (uint32_t)(STAGES * STAGE + mine * 2 * kLinBlock);
             const bool first = quarter == 0 && lane == 0;
             int place = 0;
             auto emit = [&](const uint32_t (&w)[32], int x, int y) {
                 if constexpr (STAGED) {
-                    const uint32_t to = out + place * kLinHalf + lrow * 128;
+                    const uint32_t to = out + place * kLinBlock + lrow * 128;
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((q ^ (lrow & 7)) << 4)), "r"(w[4 * q]), "r"(w[4 * q + 1]),
@@ -571,7 +581,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     if (first) lin_stores_read();  // (the other place is free)
                     __syncwarp();
                     named_bar_sync(1 + mine, 128);
-                    if (first && ok && (MODE == LIN_DZ || y < p.V)) lin_store(&tmOut, out + place * kLinHalf, x, y);  // (rows behind the last are cut off)
+                    if (first && ok && (MODE == LIN_DZ || y < p.V)) lin_store(&tmOut, out + place * kLinBlock, x, y);  // (rows behind the last are cut off)
                     place ^= 1;
                 } else if (ok && (MODE == LIN_DZ || y + lrow < p.V)) {
                     uint16_t *o = p.out + (int64_t)(y + lrow) * p.out_stride + x;
@@ -591,10 +601,10 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     }
                 }
             };
-            // GRAD: the rows whose token is one of the tile's (`sorted` from `start` on), brought for the tile after the next one's step by step:
-            // where they stand, which they are, then the first of them themselves, so that none of these loads is waited for
+            // GRAD: the rows whose token is one of the tile's (`sorted` from `start` on), brought for the tiles behind this one step by step: where
+            // they stand, which they are, then the first of them themselves, so that none of these loads is waited for
             struct Hits {
-                int x0, n, row, tok;  // (row, tok: lane e's entry e)
+                int x0, n, row, tok;  // (row, tok, delta: lane e's entry e)
                 float delta;
             };
             const int blocks = (live + kLinSort - 1) / kLinSort;
@@ -619,17 +629,13 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 }
             };
             auto fetch = [&](Hits &h, int i, int buf) {
-                LinJob j;
                 if (lane < min(h.n, kLinHits)) h.delta = p.delta[h.row];
-                if (MODE == LIN_GRAD && h.n > 0 && work.job(p, i, j)) {
-                    if constexpr (MODE == LIN_GRAD) {
-                        const int n = min(h.n, kLinHits), left = min(p.d - j.n0, j.n);
-#pragma unroll 1
-                        for (int x = 0; x < n; ++x) {  // (a warp each fourth)
-                            const int row = __shfl_sync(0xffffffffu, h.row, x);
-                            if (x % 4 == quarter && 8 * lane < left)
-                                cp_async16(smem_u32(&E.row[mine][buf][x][8 * lane]), p.low + (int64_t)row * p.d + j.n0 + 8 * lane);
-                        }
+                if constexpr (MODE == LIN_GRAD) {
+                    LinJob j;
+                    if (h.n > 0 && work.job(p, i, j)) {
+                        const int n = min(h.n, kLinHits), left = min(p.d - j.n0, j.n) - c0, x = 2 * quarter + lane / 16, at = lane % 16 * 8;
+                        const int row = __shfl_sync(0xffffffffu, h.row, x);  // (a half warp a row)
+                        if (x < n && at < left) cp_async16(smem_u32(&E.row[mine][buf][x][at]), p.low + (int64_t)row * p.d + j.n0 + c0 + at);
                     }
                 }
                 cp_async_commit();
@@ -637,18 +643,23 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             Hits now = {0, 0, 0, -1, 0.f}, next = now, later = now;
             int buf = 0;
             if (MODE == LIN_GRAD && p.dw) {
-                next = where(mine);
-                later = where(mine + 2);
+                next = where(0);
+                later = where(1);
                 which(next);
-                fetch(next, mine, 0);
+                fetch(next, 0, 0);
             }
             const float k = MODE == LIN_GRAD ? p.scale * pow2f(-p.head->exp) : 0.f;
 #pragma unroll 1
-            for (int i = mine; i < work.count; i += 2) {
+            for (int i = 0; i < work.count; ++i) {
                 LinJob j;
                 if (!work.job(p, i, j)) break;
                 const int m = j.m0 + rank * kLinRows + lrow;
-                const uint32_t acc_at = from + (uint32_t)(i % ACCS * COLS);
+                float v[128];
+                auto read = [&]() {
+                    if (ok) wait(i);
+                    lin_tmem_load128(from + (uint32_t)((i & 1) * COLS), v);
+                    if (ok) give(i & 1);
+                };
                 if constexpr (MODE == LIN_DZ) {
                     // what the row wants, read while the MMAs run
                     int tok = -1;
@@ -668,123 +679,113 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                         wrong = tok >= p.V;
                         zero = mx == -INFINITY && ls == 0.f && !wrong;
                     }
-                    if (ok) wait(i);
-                    const int left = p.cols - j.n0;
-#pragma unroll 1
-                    for (int cc = 0; cc < COLS; cc += 64) {
-                        uint32_t w[32];
+                    read();
+                    const int left = p.cols - j.n0 - c0, at = tok - p.v0 - j.n0 - c0;
+                    const float nan = __int_as_float(0x7fc00000);
+                    // what all of the row's have as a factor: 0 where nothing counts, NaN where the token is wrong
+                    raise = wrong ? nan : raise;
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            float v[32];
-                            lin_tmem_load<false>(acc_at + cc + 32 * half, v);
-                            const int c0 = cc + 32 * half, at = tok - p.v0 - j.n0 - c0;
-                            float off = 0.f;
+                    for (int cc = 0; cc < 128; cc += 64) {
+                        uint32_t w[32];
+                        float off = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 64; e += 2) {
+                            float y[2];
+#pragma unroll
+                            for (int x = 0; x < 2; ++x) {
+                                const float lp = fmaf(v[cc + e + x], p.scale, -mx) - ls, q = exp2_approx(lp * kLog2e);
+                                y[x] = -q * fmaf(gh, fmaxf(lp, -1000.f) + H, g);
+                                if (cc + e + x == at) y[x] += g;
+                                y[x] *= raise;
+                            }
+                            w[e / 2] = pack_grad<TYPE>(y[0], y[1]);
+                            if (cc + e == (at & ~1)) {
+                                const float2 z = unpack2<TYPE>(w[e / 2]);
+                                off = at & 1 ? y[1] - z.y : y[0] - z.x;
+                            }
+                        }
+                        if (zero || left < cc + 64) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e) {
-                                const float lp = fmaf(v[e], p.scale, -mx) - ls, x = exp2_approx(lp * kLog2e);
-                                float y = -x * fmaf(gh, fmaxf(lp, -1000.f) + H, g);
-                                if (e == at) y += g;
-                                y = wrong ? __int_as_float(0x7fc00000) : y * raise;
-                                v[e] = zero || c0 + e >= left ? 0.f : y;
+                                if (zero || cc + 2 * e >= left) w[e] = 0;
+                                else if (cc + 2 * e + 1 >= left) w[e] &= 0xffffu;
                             }
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) {
-                                const uint32_t x = pack_grad<TYPE>(v[2 * e], v[2 * e + 1]);
-                                const float2 z = unpack2<TYPE>(x);
-                                w[16 * half + e] = x;
-                                off = 2 * e == at ? v[2 * e] - z.x : 2 * e + 1 == at ? v[2 * e + 1] - z.y : off;
-                            }
-                            if ((unsigned)at < 32u && m < live) p.delta[m] = off;
                         }
-                        if (m >= live) {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) w[e] = 0;
-                        }
-                        emit(w, 0, (j.n0 + cc) / 64 * p.rows_cap + j.m0 + rank * kLinRows);
+                        if (at >= cc && at < cc + 64 && m < live) p.delta[m] = zero ? 0.f : off;
+                        emit(w, 0, (j.n0 + c0 + cc) / 64 * p.rows_cap + j.m0 + rank * kLinRows);
                     }
                 } else if (j.kind) {
-                    const int token = p.v0 + m;
+                    const int token = p.v0 + m, left = min(p.d - j.n0, j.n) - c0;
                     cp_async_wait<0>();
                     __syncwarp();
                     named_bar_sync(1 + mine, 128);  // (its rows have come; the tile before has left the other place)
                     now = next;
                     next = later;
                     which(next);
-                    fetch(next, i + 2, buf ^ 1);
-                    later = where(i + 4);
+                    fetch(next, i + 1, buf ^ 1);
+                    later = where(i + 2);
                     uint32_t match = 0;  // which of them are the row's
 #pragma unroll
                     for (int x = 0; x < kLinHits; ++x) match |= (uint32_t)(__shfl_sync(0xffffffffu, now.tok, x) == token) << x;
-                    if (ok) wait(i);
-                    const int left = min(p.d - j.n0, j.n);
+                    read();
+                    auto add = [&](float f, const uint16_t *h) {
+#pragma unroll
+                        for (int q = 0; q < 16; ++q) {
+                            if (8 * q >= left) continue;
+                            const uint4 y = *reinterpret_cast<const uint4 *>(h + 8 * q);
+                            const uint32_t u[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float2 z = unpack2<TYPE>(u[e]);
+                                v[8 * q + 2 * e] = fmaf(f, z.x, v[8 * q + 2 * e]);
+                                v[8 * q + 2 * e + 1] = fmaf(f, z.y, v[8 * q + 2 * e + 1]);
+                            }
+                        }
+                    };
+                    if (__any_sync(0xffffffffu, match != 0)) {
 #pragma unroll 1
-                    for (int cc = 0; cc < left; cc += 64) {
+                        for (int x = 0; x < min(now.n, kLinHits); ++x) {
+                            const float f = __shfl_sync(0xffffffffu, now.delta, x);
+                            if (match >> x & 1) add(f, E.row[mine][buf][x]);
+                        }
+                    }
+                    if (now.n > kLinHits || blocks > 1) {  // the others, in their order
+#pragma unroll 1
+                        for (int b = 0; b < blocks; ++b) {
+                            const int *start = p.start + (int64_t)b * (p.buckets + 1) + (p.v0 + j.m0 + rank * kLinRows) / kLinRows;
+                            if (token >= p.V) break;
+#pragma unroll 1
+                            for (int x = start[0] + (b == 0 ? kLinHits : 0); x < start[1]; ++x) {
+                                const int2 r = p.sorted[b * kLinSort + x];
+                                if (r.y == token) add(p.delta[r.x], p.low + (int64_t)r.x * p.d + j.n0 + c0);
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int cc = 0; cc < 128; cc += 64) {
+                        if (cc >= left) continue;
                         uint32_t w[32];
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            float v[32];
-                            const int c0 = cc + 32 * half;
-                            lin_tmem_load<false>(acc_at + c0, v);
-                            auto add = [&](float f, const uint16_t *h) {
-#pragma unroll
-                                for (int q = 0; q < 4; ++q) {
-                                    if (c0 + 8 * q >= left) continue;
-                                    const uint4 y = *reinterpret_cast<const uint4 *>(h + 8 * q);
-                                    const uint32_t u[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                                    for (int e = 0; e < 4; ++e) {
-                                        const float2 z = unpack2<TYPE>(u[e]);
-                                        v[8 * q + 2 * e] = fmaf(f, z.x, v[8 * q + 2 * e]);
-                                        v[8 * q + 2 * e + 1] = fmaf(f, z.y, v[8 * q + 2 * e + 1]);
-                                    }
-                                }
-                            };
-                            if (__any_sync(0xffffffffu, match != 0)) {
-#pragma unroll 1
-                                for (int x = 0; x < kLinHits; ++x) {
-                                    const float f = __shfl_sync(0xffffffffu, now.delta, x);
-                                    if (match >> x & 1) add(f, &E.row[mine][buf][x][c0]);
-                                }
-                            }
-                            if (now.n > kLinHits || blocks > 1) {  // the others, in their order
-#pragma unroll 1
-                                for (int b = 0; b < blocks; ++b) {
-                                    const int *start = p.start + (int64_t)b * (p.buckets + 1) + (p.v0 + j.m0 + rank * kLinRows) / kLinRows;
-                                    if (token >= p.V) break;
-#pragma unroll 1
-                                    for (int x = start[0] + (b == 0 ? kLinHits : 0); x < start[1]; ++x) {
-                                        const int2 r = p.sorted[b * kLinSort + x];
-                                        if (r.y == token) add(p.delta[r.x], p.low + (int64_t)r.x * p.d + j.n0 + c0);
-                                    }
-                                }
-                            }
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) w[16 * half + e] = pack_grad<TYPE>(v[2 * e] * k, v[2 * e + 1] * k);
-                        }
-                        emit(w, j.n0 + cc, p.v0 + j.m0 + rank * kLinRows);
+                        for (int e = 0; e < 32; ++e) w[e] = pack_grad<TYPE>(v[cc + 2 * e] * k, v[cc + 2 * e + 1] * k);
+                        emit(w, j.n0 + c0 + cc, p.v0 + j.m0 + rank * kLinRows);
                     }
                     buf ^= 1;
                 } else {
                     if (p.dw) {  // (the next tile may be one of dW's)
-                        now = next;
                         next = later;
                         which(next);
-                        fetch(next, i + 2, buf ^ 1);
-                        later = where(i + 4);
+                        fetch(next, i + 1, buf ^ 1);
+                        later = where(i + 2);
                         buf ^= 1;
                     }
-                    if (ok) wait(i);
-                    const int left = min(p.d - j.n0, j.n);
-                    float *acc = p.acc + ((int64_t)j.split * p.rows_cap + m) * p.d + j.n0;
-#pragma unroll 1
-                    for (int cc = 0; cc < left; cc += 32) {
-                        float v[32];
-                        lin_tmem_load<false>(acc_at + cc, v);
-                        if (m >= live) continue;
+                    read();
+                    const int left = min(p.d - j.n0, j.n) - c0;
+                    float *acc = p.acc + ((int64_t)j.split * p.rows_cap + m) * p.d + j.n0 + c0;
+                    if (m < live) {
 #pragma unroll
-                        for (int q = 0; q < 8; ++q) {
-                            if (cc + 4 * q >= left) continue;
-                            float4 *to = reinterpret_cast<float4 *>(acc + cc + 4 * q);
+                        for (int q = 0; q < 32; ++q) {
+                            if (4 * q >= left) continue;
+                            float4 *to = reinterpret_cast<float4 *>(acc + 4 * q);
                             float4 x = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
                             if (!p.first) {
                                 const float4 y = *to;
@@ -794,7 +795,6 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                         }
                     }
                 }
-                if (ok) give(i % ACCS);
             }
             if (STAGED && first) lin_stores_done();
         }
@@ -1074,12 +1074,11 @@ struct LinPlan {
     int piece, splits, buckets;       // gradient: tokens of a piece, parts of its dH, tiles of 128 tokens
     size_t src, pos, kexp, tokc, sorted, start, delta, rows, low, part, ztok, dz, acc, bytes;
 };
-// Tokens of a piece.  76 tiles of 256 (152 of 128) are as many as there are pairs of CTAs (CTAs), so that whatever the rows' tiles the logits' come
-// out even; dZ is kept to 192 MB.  Up to 128 rows the piece's weights, which are read twice, have to stay in L2 besides.
+// Tokens of a piece.  76 tiles of 256 are as many as there are pairs of CTAs, so that whatever the rows' tiles the logits' come out even; dZ is kept to 192 MB.  Up to 128 rows the piece's weights, which are read twice, have to stay in L2 besides.
 inline int64_t lin_piece(int rows_cap, int d, int V, int ctas) {
     constexpr int64_t kEven = 76 * 256;
     const int64_t most = ((int64_t)192 << 20) / 2 / rows_cap;
-    int64_t piece = ctas == 1 ? (d <= 2304 ? kEven : kEven / 2) : most >= kEven ? most / kEven * kEven : most / 256 * 256;
+    int64_t piece = ctas == 1 ? (d <= 1152 ? 2 * kEven : d <= 2304 ? kEven : kEven / 2) : most >= kEven ? most / kEven * kEven : most / 256 * 256;
     if (piece < 1024) piece = 1024;
     const int64_t all = lin_up(V, 256);
     return piece < all ? piece : all;
@@ -1087,7 +1086,7 @@ inline int64_t lin_piece(int rows_cap, int d, int V, int ctas) {
 inline LinPlan lin_plan(int R, int d, int V, bool backward) {
     LinPlan q{};
     q.ctas = R > kLinRows ? 2 : 1;
-    const int tm = kLinRows * q.ctas, cols = lin_cols(q.ctas);
+    const int tm = kLinRows * q.ctas, cols = kLinCols;
     q.rows_cap = (int)lin_up(R, tm);
     q.tiles = (int)lin_up(V, cols) / cols;
     q.gather = backward || R > kLinRows;

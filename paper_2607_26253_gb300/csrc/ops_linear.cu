@@ -91,7 +91,8 @@ void score(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand &h
     p.ztok = at<float>(ws, q.ztok);
     p.rows_cap = q.rows_cap;
     p.token_tiles = q.tiles;
-    const CUtensorMap a = rows_map(x, kLinRows), b = rows_map(w, kLinRows);
+    p.a_rows = CTAS == 1 ? (int)lin_up(R, 8) : kLinRows;
+    const CUtensorMap a = rows_map(x, p.a_rows), b = rows_map(w, kLinCols / CTAS);
     launch<LIN_SCORE, CTAS, TYPE>(s, sms, q.gather, a, b, a, b, a, p);
     const LinJoinParams j{p.head, R, V, q.tiles, q.rows_cap, tokens, q.gather ? at<int>(ws, q.pos) : nullptr, p.part, p.ztok, scale, logprob, entropy, stats};
     if (R <= 64) launch_cluster(s, true, dim3((unsigned)R), dim3(256), 0, 1, lin_join_kernel<1>, j);
@@ -128,8 +129,9 @@ void gradient(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand
     p.splits = q.splits;
     p.dh = dh.p != nullptr;
     p.dw = dw.p != nullptr;
-    const CUtensorMap xk = rows_map(x, kLinRows), wk = rows_map(w, kLinRows), dzk = rows_map(dz, kLinRows);
-    const CUtensorMap dzm = rows_map(dz, kLinK), wn = rows_map(w, kLinK), xn = rows_map(low, kLinK), out = dw.p ? rows_map(dw, kLinRows) : dzk;
+    p.a_rows = CTAS == 1 ? (int)lin_up(R, 8) : kLinRows;
+    const CUtensorMap xk = rows_map(x, p.a_rows), wk = rows_map(w, kLinCols / CTAS), dzk = rows_map(dz, p.a_rows), dzs = rows_map(dz, kLinRows);
+    const CUtensorMap dzm = rows_map(dz, kLinK), wn = rows_map(w, kLinK), xn = rows_map(low, kLinK), out = dw.p ? rows_map(dw, kLinRows) : dzs;
     for (int v = 0; v < V; v += q.piece) {
         p.v0 = v;
         p.cols = V - v < q.piece ? V - v : q.piece;
@@ -137,7 +139,7 @@ void gradient(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand
         p.out = at<uint16_t>(ws, q.dz);
         p.out_stride = 64;
         p.wide = true;
-        launch<LIN_DZ, CTAS, TYPE>(s, sms, true, xk, wk, xk, wk, dzk, p);
+        launch<LIN_DZ, CTAS, TYPE>(s, sms, true, xk, wk, xk, wk, dzs, p);
         p.out = static_cast<uint16_t *>(const_cast<void *>(dw.p));
         p.out_stride = dw.stride;
         p.wide = (reinterpret_cast<uintptr_t>(dw.p) & 31) == 0 && dw.stride % 16 == 0;
