@@ -52,14 +52,16 @@ enum LinMode : int {
     LIN_DZ = 1,     // tiles of logits -> dZ of a piece
     LIN_GRAD = 2,   // dZ of a piece -> dH's sums, dW
 };
-// One CTA stores dZ and dW by way of shared memory, two blocks of 64 columns for each half of its epilogue: whole lines, where each thread's own row
-// costs the memory pipe an access a lane.  Two CTAs store from registers: their operands leave shared memory no time.
-__host__ __device__ constexpr bool lin_staged(int mode, int ctas) { return mode != LIN_SCORE && ctas == 1; }
+// How results leave: from registers, each thread its row's, which costs the memory pipe an access a lane; or STAGED, by way of shared memory, two blocks of
+// 64 columns for each half of the epilogue, in whole lines, which costs stages of operands.  dW of 301 rows, 5 chunks a tile: 147 us / 118 staged; of
+// 4,096, 58 chunks: 287 / 297; dZ of 4,096 rows: 136 / 140.
+constexpr int kLinStagedRows = 1024;  // up to which dW is staged
 __host__ __device__ constexpr int lin_stage_bytes(int ctas) { return kLinBlock * (1 + 2 / ctas); }
-__host__ __device__ constexpr int lin_stages(int mode, int ctas) { return ctas == 2 ? 6 : lin_staged(mode, ctas) ? 3 : 4; }
-__host__ __device__ constexpr size_t lin_smem(int mode, int ctas) {
-    return 1024 + (size_t)lin_stages(mode, ctas) * lin_stage_bytes(ctas) + (lin_staged(mode, ctas) ? 4 : 0) * kLinBlock;
+__host__ __device__ constexpr int lin_stages(int ctas, bool staged) { return ctas == 2 ? (staged ? 4 : 6) : staged ? 3 : 4; }
+__host__ __device__ constexpr size_t lin_smem(int ctas, bool staged) {
+    return 1024 + (size_t)lin_stages(ctas, staged) * lin_stage_bytes(ctas) + (staged ? 4 : 0) * kLinBlock;
 }
+constexpr int kLinDwCost = 9;
 constexpr int kLinHits = 8;  // rows of a tile of tokens that wait in shared memory for dW's epilogue
 
 struct LinParams {
@@ -194,6 +196,9 @@ struct LinJob {
     int split;  // dH
 };
 
+// A job of dW's in chunks: its products, or its epilogue where those are few
+__host__ __device__ __forceinline__ int lin_dw_cost(int kr) { return kr + 1 > kLinDwCost ? kr + 1 : kLinDwCost; }
+
 // The jobs of a CTA (or pair) `w` of `W`, by number.  Logits: rows fastest, so that the CTAs at work share tokens.
 // LIN_GRAD: dH's jobs are long, so the workers that have one more of them get fewer of dW's.
 template <int MODE, int CTAS>
@@ -220,7 +225,7 @@ struct LinWork {
             const int rem = jh % W;
             wide = W - rem;
             own_h = jh / W + (w < rem);
-            const int ratio = rem ? (kc / splits + kr - 1) / kr : 0;  // dW's jobs in the time of one of dH's
+            const int cost = lin_dw_cost(kr), ratio = rem ? (kc / splits + cost - 1) / cost : 0;  // dW's jobs in the time of one of dH's
             int b = (int)(((int64_t)jw + (int64_t)rem * ratio + W - 1) / W), a = b - ratio;
             if (a < 0) {
                 a = 0;
@@ -303,6 +308,11 @@ __device__ __forceinline__ void lin_tmem_add(uint32_t taddr, float *v) {
     for (int i = 0; i < 32; ++i) v[i] += __uint_as_float(r[i]);
 }
 
+__device__ __forceinline__ float max_nan(float a, float b) {  // the larger; a NaN stays
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
 // 128 columns of a lane
 __device__ __forceinline__ void lin_tmem_load128(uint32_t taddr, float (&v)[128]) {
     __syncwarp();
@@ -327,11 +337,11 @@ __device__ __forceinline__ void lin_tmem_load128(uint32_t taddr, float (&v)[128]
         : "memory");
 }
 
-template <int MODE, int CTAS, int TYPE>
+template <int MODE, int CTAS, int TYPE, bool STAGED>
 __global__ void __launch_bounds__(kLinThreads, 1)
 lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmA2,
            const __grid_constant__ CUtensorMap tmB2, const __grid_constant__ CUtensorMap tmOut, LinParams p) {
-    constexpr int STAGES = lin_stages(MODE, CTAS), STAGE = lin_stage_bytes(CTAS), COLS = kLinCols, PART = lin_part(CTAS);
+    constexpr int STAGES = lin_stages(CTAS, STAGED), STAGE = lin_stage_bytes(CTAS), COLS = kLinCols, PART = lin_part(CTAS);
     extern __shared__ uint8_t smem_raw[];
     __shared__ LinSmem S;
     __shared__ __align__(16) std::conditional_t<MODE == LIN_SCORE, LinScoreSmem, std::conditional_t<MODE == LIN_GRAD, LinGradSmem, LinNoSmem>> E;
@@ -563,9 +573,8 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 }
             }
         } else {
-            // 64 columns of the tile's rows to `x`, `y` of the result.  One CTA: by way of one of this half's two places in shared memory, which the
-            // block before the last one has left (after a failed wait the barriers go on and nothing is stored).  Two: each thread its row's.
-            constexpr bool STAGED = lin_staged(MODE, CTAS);
+            // 64 columns of the tile's rows to `x`, `y` of the result.  STAGED: by way of one of this half's two places in shared memory, which the
+            // block before the last one has left.  (After a failed wait the barriers go on and nothing is stored.)
             const uint32_t out = smem_u32(ring) + (uint32_t)(STAGES * STAGE + mine * 2 * kLinBlock);
             const bool first = quarter == 0 && lane == 0;
             int place = 0;
@@ -661,57 +670,68 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     if (ok) give(i & 1);
                 };
                 if constexpr (MODE == LIN_DZ) {
-                    // what the row wants, read while the MMAs run
+                    // What the row wants, read while the MMAs run.  In base 2: with r = (max + log S) log2(e) as rounded and f what the rounding
+                    // took, y = acc scale log2(e) - r, p = 2^y 2^f, dz = 2^y (a y + b) with a = -2^f g' ln 2, b = -2^f (g + g' (entropy + f ln 2)).
                     int tok = -1;
-                    float mx = 0.f, ls = 0.f, g = 0.f, gh = 0.f, H = 0.f, raise = 1.f;
+                    float r = 0.f, ga = 0.f, gb = 0.f, g = 0.f, mx = 0.f, ls = 0.f;
                     bool zero = true, wrong = false;
+                    const float c = p.scale * kLog2e;
                     if (m < live) {
-                        const int r = p.src[m];
-                        tok = p.tokens ? p.tokens[r] : -1;
-                        mx = p.stats[2 * (int64_t)r];
-                        ls = p.stats[2 * (int64_t)r + 1];
-                        if (p.glp) g = p.glp[r];
+                        const int row = p.src[m];
+                        tok = p.tokens ? p.tokens[row] : -1;
+                        mx = p.stats[2 * (int64_t)row];
+                        ls = p.stats[2 * (int64_t)row + 1];
+                        float gh = 0.f, H = 0.f;
+                        if (p.glp) g = p.glp[row];
                         if (p.gent) {
-                            gh = p.gent[r];
-                            H = p.entropy[r];
+                            gh = p.gent[row];
+                            H = p.entropy[row];
                         }
-                        raise = pow2f(p.kexp[r]);
                         wrong = tok >= p.V;
                         zero = mx == -INFINITY && ls == 0.f && !wrong;
+                        const float raise = wrong ? __int_as_float(0x7fc00000) : pow2f(p.kexp[row]);
+                        const float p1 = mx * kLog2e, p2 = ls * kLog2e;
+                        r = p1 + p2;
+                        const float x = r - p1, f = ((p1 - (r - x)) + (p2 - x)) + (fmaf(mx, kLog2e, -p1) + fmaf(ls, kLog2e, -p2));  // exactly r + f
+                        const float k = exp2_approx(fminf(fmaxf(-f, -100.f), 100.f)) * raise;
+                        ga = -k * gh * kLn2;
+                        gb = -k * fmaf(gh, fmaf(-f, kLn2, H), g);
+                        g *= raise;
                     }
                     read();
                     const int left = p.cols - j.n0 - c0, at = tok - p.v0 - j.n0 - c0;
-                    const float nan = __int_as_float(0x7fc00000);
-                    // what all of the row's have as a factor: 0 where nothing counts, NaN where the token is wrong
-                    raise = wrong ? nan : raise;
+                    const uint64_t c2 = pack_f32x2(c, c), r2 = pack_f32x2(-r, -r), a2 = pack_f32x2(ga, ga), b2 = pack_f32x2(gb, gb);
 #pragma unroll
                     for (int cc = 0; cc < 128; cc += 64) {
                         uint32_t w[32];
-                        float off = 0.f;
 #pragma unroll
                         for (int e = 0; e < 64; e += 2) {
-                            float y[2];
+                            // (2^-1000 is 0; its factor is to stay finite)
+                            const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(v[cc + e], v[cc + e + 1]), c2, r2));
+                            const float y0 = max_nan(y.x, -1000.f), y1 = max_nan(y.y, -1000.f);
+                            const float2 f = unpack_f32x2(fma_f32x2(pack_f32x2(y0, y1), a2, b2));
+                            w[e / 2] = pack_grad<TYPE>(exp2_approx(y0) * f.x, exp2_approx(y1) * f.y);
+                        }
+                        if (__any_sync(0xffffffffu, at >= cc && at < cc + 64)) {  // (seldom) the token's own
+                            if (at >= cc && at < cc + 64 && m < live) {
+                                float z = 0.f;
 #pragma unroll
-                            for (int x = 0; x < 2; ++x) {
-                                const float lp = fmaf(v[cc + e + x], p.scale, -mx) - ls, q = exp2_approx(lp * kLog2e);
-                                y[x] = -q * fmaf(gh, fmaxf(lp, -1000.f) + H, g);
-                                if (cc + e + x == at) y[x] += g;
-                                y[x] *= raise;
-                            }
-                            w[e / 2] = pack_grad<TYPE>(y[0], y[1]);
-                            if (cc + e == (at & ~1)) {
-                                const float2 z = unpack2<TYPE>(w[e / 2]);
-                                off = at & 1 ? y[1] - z.y : y[0] - z.x;
+                                for (int e = 0; e < 64; ++e) z = cc + e == at ? v[cc + e] : z;
+                                const float y = max_nan(fmaf(z, c, -r), -1000.f), x = fmaf(exp2_approx(y), fmaf(y, ga, gb), g);
+                                const uint32_t h = pack_grad<TYPE>(x, x);
+                                p.delta[m] = zero ? 0.f : x - unpack2<TYPE>(h).x;
+#pragma unroll
+                                for (int e = 0; e < 32; ++e)
+                                    if (cc + 2 * e == (at & ~1)) w[e] = at & 1 ? (w[e] & 0xffffu) | (h & 0xffff0000u) : (w[e] & 0xffff0000u) | (h & 0xffffu);
                             }
                         }
-                        if (zero || left < cc + 64) {
+                        if (__any_sync(0xffffffffu, zero) || left < cc + 64) {
 #pragma unroll
                             for (int e = 0; e < 32; ++e) {
                                 if (zero || cc + 2 * e >= left) w[e] = 0;
                                 else if (cc + 2 * e + 1 >= left) w[e] &= 0xffffu;
                             }
                         }
-                        if (at >= cc && at < cc + 64 && m < live) p.delta[m] = zero ? 0.f : off;
                         emit(w, 0, (j.n0 + c0 + cc) / 64 * p.rows_cap + j.m0 + rank * kLinRows);
                     }
                 } else if (j.kind) {
@@ -1115,7 +1135,7 @@ inline LinPlan lin_plan(int R, int d, int V, bool backward) {
         const int64_t workers = kLinWorkers / q.ctas, mt = q.rows_cap / tm, nt = lin_up(d, cols) / cols;
         q.piece = (int)lin_piece(q.rows_cap, d, V, q.ctas);
         const int64_t kc = lin_up(q.piece < V ? q.piece : V, kLinK) / kLinK, kr = lin_up(R, kLinK) / kLinK, jw = lin_up(q.piece, tm) / tm * nt;
-        const int64_t load = (jw * kr + mt * nt * kc) / workers + 1;
+        const int64_t load = (jw * lin_dw_cost((int)kr) + mt * nt * kc) / workers + 1;
         int64_t s = workers / (mt * nt);
         if (s < (kc + load - 1) / load) s = (kc + load - 1) / load;
         if (s < 1) s = 1;

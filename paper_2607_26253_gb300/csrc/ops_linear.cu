@@ -41,12 +41,12 @@ bool sizes_ok(int type, int R, int d, int V, float scale) {
            V <= (1 << 24) && scale > 0.f && std::isfinite(scale);
 }
 
-template <int MODE, int CTAS, int TYPE>
+template <int MODE, int CTAS, int TYPE, bool STAGED>
 void launch(cudaStream_t s, int sms, bool after, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &a2, const CUtensorMap &b2,
             const CUtensorMap &out, const LinParams &p) {
-    const auto kern = lin_kernel<MODE, CTAS, TYPE>;
-    CK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lin_smem(MODE, CTAS)));
-    launch_cluster(s, after, dim3((unsigned)(sms / CTAS * CTAS)), dim3(kLinThreads), lin_smem(MODE, CTAS), CTAS, kern, a, b, a2, b2, out, p);
+    const auto kern = lin_kernel<MODE, CTAS, TYPE, STAGED>;
+    CK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lin_smem(CTAS, STAGED)));
+    launch_cluster(s, after, dim3((unsigned)(sms / CTAS * CTAS)), dim3(kLinThreads), lin_smem(CTAS, STAGED), CTAS, kern, a, b, a2, b2, out, p);
 }
 
 template <typename T>
@@ -93,7 +93,7 @@ void score(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand &h
     p.token_tiles = q.tiles;
     p.a_rows = CTAS == 1 ? (int)lin_up(R, 8) : kLinRows;
     const CUtensorMap a = rows_map(x, p.a_rows), b = rows_map(w, kLinCols / CTAS);
-    launch<LIN_SCORE, CTAS, TYPE>(s, sms, q.gather, a, b, a, b, a, p);
+    launch<LIN_SCORE, CTAS, TYPE, false>(s, sms, q.gather, a, b, a, b, a, p);
     const LinJoinParams j{p.head, R, V, q.tiles, q.rows_cap, tokens, q.gather ? at<int>(ws, q.pos) : nullptr, p.part, p.ztok, scale, logprob, entropy, stats};
     if (R <= 64) launch_cluster(s, true, dim3((unsigned)R), dim3(256), 0, 1, lin_join_kernel<1>, j);
     else launch_cluster(s, true, dim3((unsigned)(R + 7) / 8), dim3(256), 0, 1, lin_join_kernel<8>, j);
@@ -139,11 +139,12 @@ void gradient(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand
         p.out = at<uint16_t>(ws, q.dz);
         p.out_stride = 64;
         p.wide = true;
-        launch<LIN_DZ, CTAS, TYPE>(s, sms, true, xk, wk, xk, wk, dzs, p);
+        launch<LIN_DZ, CTAS, TYPE, CTAS == 1>(s, sms, true, xk, wk, xk, wk, dzs, p);
         p.out = static_cast<uint16_t *>(const_cast<void *>(dw.p));
         p.out_stride = dw.stride;
         p.wide = (reinterpret_cast<uintptr_t>(dw.p) & 31) == 0 && dw.stride % 16 == 0;
-        launch<LIN_GRAD, CTAS, TYPE>(s, sms, true, dzk, wn, dzm, xn, out, p);
+        if (CTAS == 1 || R <= kLinStagedRows) launch<LIN_GRAD, CTAS, TYPE, true>(s, sms, true, dzk, wn, dzm, xn, out, p);
+        else launch<LIN_GRAD, CTAS, TYPE, CTAS == 1>(s, sms, true, dzk, wn, dzm, xn, out, p);
     }
     const LinOutParams o{p.head, R, d, q.splits, q.rows_cap, at<int>(ws, q.pos), p.kexp, p.acc, p.delta, tokens, V, static_cast<const uint16_t *>(w.p), w.stride,
                          scale, static_cast<uint16_t *>(const_cast<void *>(dh.p)), dh.stride, static_cast<uint16_t *>(const_cast<void *>(dw.p)), dw.stride};
