@@ -649,14 +649,24 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 }
                 cp_async_commit();
             };
-            Hits now = {0, 0, 0, -1, 0.f}, next = now, later = now;
+            Hits now = {0, 0, 0, -1, 0.f}, next = now, later = now, last = now;
             int buf = 0;
             if (MODE == LIN_GRAD && p.dw) {
                 next = where(0);
                 later = where(1);
+                last = where(2);
                 which(next);
+                which(later);
                 fetch(next, 0, 0);
             }
+            auto move_on = [&](int i) {
+                now = next;
+                next = later;
+                later = last;
+                fetch(next, i + 1, buf ^ 1);
+                which(later);
+                last = where(i + 3);
+            };
             const float k = MODE == LIN_GRAD ? p.scale * pow2f(-p.head->exp) : 0.f;
 #pragma unroll 1
             for (int i = 0; i < work.count; ++i) {
@@ -739,11 +749,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     cp_async_wait<0>();
                     __syncwarp();
                     named_bar_sync(1 + mine, 128);  // (its rows have come; the tile before has left the other place)
-                    now = next;
-                    next = later;
-                    which(next);
-                    fetch(next, i + 1, buf ^ 1);
-                    later = where(i + 2);
+                    move_on(i);
                     uint32_t match = 0;  // which of them are the row's
 #pragma unroll
                     for (int x = 0; x < kLinHits; ++x) match |= (uint32_t)(__shfl_sync(0xffffffffu, now.tok, x) == token) << x;
@@ -792,10 +798,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     buf ^= 1;
                 } else {
                     if (p.dw) {  // (the next tile may be one of dW's)
-                        next = later;
-                        which(next);
-                        fetch(next, i + 1, buf ^ 1);
-                        later = where(i + 2);
+                        move_on(i);
                         buf ^= 1;
                     }
                     read();
@@ -1094,10 +1097,11 @@ struct LinPlan {
     int piece, splits, buckets;       // gradient: tokens of a piece, parts of its dH, tiles of 128 tokens
     size_t src, pos, kexp, tokc, sorted, start, delta, rows, low, part, ztok, dz, acc, bytes;
 };
-// Tokens of a piece.  76 tiles of 256 are as many as there are pairs of CTAs, so that whatever the rows' tiles the logits' come out even; dZ is kept to 192 MB.  Up to 128 rows the piece's weights, which are read twice, have to stay in L2 besides.
+// Tokens of a piece.  76 tiles of 256 are as many as there are pairs of CTAs, so that whatever the rows' tiles the logits' come out even; dZ is kept to 384 MB
+// (a piece costs some 36 us besides its products, while the last tiles end: 4,096 rows in 16 pieces 3.85 ms, in 8 3.56).  Up to 128 rows the piece's weights, which are read twice, have to stay in L2 besides.
 inline int64_t lin_piece(int rows_cap, int d, int V, int ctas) {
     constexpr int64_t kEven = 76 * 256;
-    const int64_t most = ((int64_t)192 << 20) / 2 / rows_cap;
+    const int64_t most = ((int64_t)384 << 20) / 2 / rows_cap;
     int64_t piece = ctas == 1 ? (d <= 1152 ? 2 * kEven : d <= 2304 ? kEven : kEven / 2) : most >= kEven ? most / kEven * kEven : most / 256 * 256;
     if (piece < 1024) piece = 1024;
     const int64_t all = lin_up(V, 256);
