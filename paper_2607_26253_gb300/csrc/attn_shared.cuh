@@ -3,29 +3,35 @@
 //     out = (2^(m1 - m) o1 + 2^(m2 - m) o2) / (2^(m1 - m) l1 + 2^(m2 - m) l2),   m = max(m1, m2).
 // Bound by reading the shared positions once (2 hd bytes each) up to some 128 queries a KV head, by the tensor cores beyond.
 //
-// Prefix kernel: a unit is (group, KV head, 128 QT queries: rows times heads); its positions go by in pages of 128, and the pages of
-// all units are cut into equal shares, one a CTA.  Three kinds of warps in a row:
-//   - 8 warps bring codes, by plain loads a page or two ahead, and leave them in shared memory as fp16 (which holds both formats exactly), swizzled
-//     as the tensor core reads them: the same image is K-major for the scores and N-major for the values;
-//   - one issues S = Q K^T (128 queries x 128 positions) and O += P V, P from tensor memory, both tcgen05;
-//   - 4 warps per 128 queries, a query a thread: maximum, exponentials, P back to tensor memory in the place of S.
+// Prefix kernel: a unit is (group, KV head, 128 queries: rows times heads); its positions go by in pages of 128, and the pages of all
+// units are cut into equal shares, one a CTA.  Four kinds of warps in a row:
+//   - one brings a page's codes by bulk copies, two pages ahead;
+//   - 4 turn them into fp16 (which holds both formats exactly) in shared memory, swizzled as the tensor core reads them: the same image
+//     is K-major for the scores and N-major for the values;
+//   - one issues S = Q K^T (128 queries x 128 positions) and O += P V, both tcgen05, Q and P from tensor memory; the next page's scores are
+//     made while this one's softmax goes on;
+//   - 8 have the softmax, two threads a query with 64 positions each: maximum, exponentials, P back to tensor memory in the place of S.
 // Scales: K's is a factor of the scores; V's of P, so P times V's scale, relative to the query's largest such product so far (2^R),
 // is what enters the product, in fp16: 11 bits, or within 2^-31 of the largest.  m and R are raised only when a score or a product
 // passes them by 2^8: most pages then need no rescaling of O.
 #pragma once
+#include <cstddef>
+
 #include "attn_kv8.cuh"
 
 namespace sara {
 
-constexpr int kSharedQ = 128, kSharedConv = 8;      // queries of a tile; warps that bring codes
+constexpr int kSharedQ = 128;                       // queries of a unit
+constexpr int kSharedSoft = 8, kSharedConv = 4;     // warps of the softmax; that make fp16
+constexpr int kSharedThreads = 32 * (kSharedSoft + kSharedConv + 2);
 constexpr int kSharedSlots = 4;                     // K and V of two pages
+__host__ __device__ constexpr int shared_tile(int hd) { return kSharedQ * 128 * ((hd + 63) / 64); }  // bytes of 128 rows in blocks of 64 dims
+__host__ __device__ constexpr int shared_raw(int hd) { return 2 * kKv8Page * hd; }                   // of a page's codes
+__host__ __device__ constexpr int shared_raws(int hd) { return hd == 128 ? 2 : 4; }                  // pages of codes
+__host__ __device__ constexpr int shared_smem(int hd) { return 1024 + kSharedSlots * shared_tile(hd) + shared_raws(hd) * shared_raw(hd); }
 constexpr float kSharedShift = 6.f;                 // log2 of the products' scale
 constexpr int kSharedMaxShares = 160;               // CTAs, one an SM
 constexpr int kSharedWideJoin = 1216;               // queries up to which 8 warps join a query
-__host__ __device__ constexpr int shared_warps(int qt) { return 4 * qt + kSharedConv + 1; }
-__host__ __device__ constexpr int shared_threads(int qt) { return 32 * shared_warps(qt); }
-__host__ __device__ constexpr int shared_tile(int hd) { return kSharedQ * 128 * ((hd + 63) / 64); }  // bytes of 128 rows in blocks of 64 dims
-__host__ __device__ constexpr int shared_smem(int hd, int qt) { return 1024 + (qt + kSharedSlots) * shared_tile(hd); }
 
 struct SharedGroup {
     int row0, rows;      // its sequences
@@ -50,7 +56,7 @@ struct SharedParams {
     SharedGroup *group;
     int *row_group, *row_first, *row_prefix;  // [n]: group (-1: none), first own position, shared ones
     float *whole;      // [n][H][hd + 2]: sums of a unit that one share holds: maximum, sum, outputs
-    float *part;       // [share][2][128 QT][hd + 2]: of a unit that begins before the share, or in it
+    float *part;       // [share][2][128][hd + 2]: of a unit that begins before the share, or in it
     int max_shares;
     // join
     const float *own, *own_lse;  // [n][H][hd], [n][H]
@@ -60,10 +66,10 @@ struct SharedParams {
 
 // ------------------------------------------------------------------------------- plan
 // One CTA.  Groups with one sequence, and sequences of no group, are left to the decode attention alone.
-template <int TQ>
 __global__ void __launch_bounds__(1024) shared_plan_kernel(SharedParams p) {
     __shared__ int s_warp[32];
     __shared__ int s_bad;
+    pdl_allow_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t most = (int64_t)p.c.max_blocks * kKv8Page;
     if (threadIdx.x == 0) s_bad = 0;
@@ -112,7 +118,7 @@ __global__ void __launch_bounds__(1024) shared_plan_kernel(SharedParams p) {
             if (bad || x.hi <= x.lo) x.lo = x.hi = 0;
             x.page0 = x.lo / kKv8Page;
             x.pages = x.hi > x.lo ? (x.hi - 1) / kKv8Page - x.page0 + 1 : 0;
-            x.tiles = (int)(((int64_t)x.rows * (p.H / p.c.KVH) + TQ - 1) / TQ);
+            x.tiles = (int)(((int64_t)x.rows * (p.H / p.c.KVH) + kSharedQ - 1) / kSharedQ);
             entries = x.pages * x.tiles * p.c.KVH;
         }
         int end = entries;
@@ -180,7 +186,6 @@ struct SharedWalk {
         x = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         entry1 = x.entry0 + x.pages * x.tiles * p.c.KVH;
     }
-    template <int TQ>
     __device__ __forceinline__ bool next(SharedSegment &s) {
         if (e >= end) return false;
         while (e >= entry1 && g + 1 < p.groups) {
@@ -192,8 +197,8 @@ struct SharedWalk {
         s.count = min(x.pages - at, end - e);
         s.row0 = x.row0;
         s.h = unit / x.tiles;
-        s.q0 = t * TQ;
-        s.queries = min(TQ, x.rows * (p.H / p.c.KVH) - s.q0);
+        s.q0 = t * kSharedQ;
+        s.queries = min(kSharedQ, x.rows * (p.H / p.c.KVH) - s.q0);
         s.lo = x.lo;
         s.hi = x.hi;
         s.page = x.page0 + at;
@@ -206,9 +211,12 @@ struct SharedWalk {
 
 // ------------------------------------------------------------------------------- prefix
 struct SharedSmem {
-    uint64_t full[kSharedSlots], empty[kSharedSlots], scales[4], q_full[2], s_full[2], p_full[2], pv_done[2], o_full[2];
-    float scale[4][8];       // of a page: K's four, V's four
-    uint32_t nan[4][kSharedConv];  // blocks of a page in which a warp met a NaN among V's codes
+    uint64_t raw_full[4], raw_empty[4], full[kSharedSlots], empty[kSharedSlots], scales[4], q_full, s_full[2], p_full[2], pv_done, o_full;
+    float scale[4][8];             // of a page: K's four, V's four
+    alignas(16) uint32_t nan[4][kSharedConv];  // blocks of a page in which a warp met a NaN among V's codes (read 16 bytes at a time)
+    float2 top[2][2][kSharedQ];    // a query's largest score and product, of either half of a page, two pages in turn
+    float sum[kSharedQ];           // of the second half's probabilities
+    int block[4];                  // of a page of codes
     uint32_t tmem_base;
     int abort;
 };
@@ -221,17 +229,20 @@ __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, ui
         "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
         : "memory");
 }
-// 32 or 16 columns of a lane; the wait is part of the instruction, so that nothing uses the values before it
-__device__ __forceinline__ void tmem_load32(uint32_t taddr, float (&v)[32]) {
-    uint32_t r[32];
+// 64 or 16 columns of a lane; the wait is part of the instruction, so that nothing uses the values before it
+__device__ __forceinline__ void tmem_load64(uint32_t taddr, float (&v)[64]) {
     __syncwarp();
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\ttcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,"
+        "%30,%31,%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%64];\n\ttcgen05.wait::ld.sync.aligned;"
+        : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), 
+          "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), 
+          "=f"(v[23]), "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31]), "=f"(v[32]), "=f"(v[33]), 
+          "=f"(v[34]), "=f"(v[35]), "=f"(v[36]), "=f"(v[37]), "=f"(v[38]), "=f"(v[39]), "=f"(v[40]), "=f"(v[41]), "=f"(v[42]), "=f"(v[43]), "=f"(v[44]), 
+          "=f"(v[45]), "=f"(v[46]), "=f"(v[47]), "=f"(v[48]), "=f"(v[49]), "=f"(v[50]), "=f"(v[51]), "=f"(v[52]), "=f"(v[53]), "=f"(v[54]), "=f"(v[55]), 
+          "=f"(v[56]), "=f"(v[57]), "=f"(v[58]), "=f"(v[59]), "=f"(v[60]), "=f"(v[61]), "=f"(v[62]), "=f"(v[63])
         : "r"(taddr)
         : "memory");
-#pragma unroll
-    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 __device__ __forceinline__ void tmem_load16(uint32_t taddr, float (&v)[16]) {
     uint32_t r[16];
@@ -252,7 +263,28 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[
         "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
+__device__ __forceinline__ void tmem_store4(uint32_t taddr, const uint4 &x) {
+    __syncwarp();
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(taddr), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w) : "memory");
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// 32 columns, waited for with every store before
+__device__ __forceinline__ void tmem_store32(uint32_t taddr, const uint32_t (&r)[32]) {
+    __syncwarp();
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};\n\ttcgen05.wait::st.sync.aligned;" ::"r"(taddr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), 
+          "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), 
+          "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+// (bulk_load to a shared-memory address)
+__device__ __forceinline__ void bulk_load_at(uint32_t dst, const void *src, uint32_t bytes, uint64_t *bar, uint64_t policy) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst), "l"(src),
+        "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
+        : "memory");
+}
 __device__ __forceinline__ uint64_t sdesc_128(uint32_t addr, uint32_t lbo) {  // 128-byte swizzle, 8 rows after 1,024 bytes
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
@@ -260,35 +292,35 @@ __device__ __forceinline__ void st_shared_v4(uint32_t at, uint32_t a, uint32_t b
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// QT: tiles of 128 queries that share a page
-template <int HD, int FMT, int QT>
-__global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(SharedParams p) {
-    constexpr int TILE = shared_tile(HD), TQ = kSharedQ * QT;
+template <int HD, int FMT>
+__global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(SharedParams p) {
+    constexpr int TILE = shared_tile(HD), RAW = shared_raw(HD), RAWS = shared_raws(HD);
     constexpr int CHUNKS = HD / 16, LOADS = kKv8Page * CHUNKS / (32 * kSharedConv);  // 16-byte pieces of a row, of a thread
-    constexpr int AHEAD = QT == 1 ? 2 : 1;  // pages on their way
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(16) SharedSmem S;
-    const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u;  // queries, then the slots
-    const uint32_t ring = base + QT * TILE;
+    const uint32_t ring = (smem_u32(smem_raw) + 1023) & ~1023u, raw = ring + kSharedSlots * TILE;
+    constexpr uint32_t O_AT = 256, Q_AT = 384;  // tensor memory: two pages' scores, outputs, queries
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = p.H / p.c.KVH;
     int *err = &p.plan->err;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kSharedSlots; ++s) {
+        for (int s = 0; s < 4; ++s) {
+            mbar_init(&S.raw_full[s], 1);
+            mbar_init(&S.raw_empty[s], kSharedConv);
             mbar_init(&S.full[s], kSharedConv);
             mbar_init(&S.empty[s], 1);
             mbar_init(&S.scales[s], kSharedConv);
         }
         for (int s = 0; s < 2; ++s) {
-            mbar_init(&S.q_full[s], 4);
             mbar_init(&S.s_full[s], 1);
-            mbar_init(&S.p_full[s], 4);
-            mbar_init(&S.pv_done[s], 1);
-            mbar_init(&S.o_full[s], 1);
+            mbar_init(&S.p_full[s], kSharedSoft);
         }
+        mbar_init(&S.q_full, kSharedSoft);
+        mbar_init(&S.pv_done, 1);
+        mbar_init(&S.o_full, 1);
         S.abort = 0;
         fence_mbar_init();
     }
-    constexpr int MMA_WARP = 4 * QT + kSharedConv;
+    constexpr int MMA_WARP = kSharedSoft + kSharedConv, LOAD_WARP = MMA_WARP + 1;
     if (warp == MMA_WARP) {
         tmem_alloc(&S.tmem_base, 512);
         tmem_relinquish();
@@ -296,211 +328,190 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    pdl_wait_prior_grids();
     const uint32_t tmem = S.tmem_base;
     volatile int *ab = &S.abort;
     const SharedShares shares(p.plan->entries, min((int)gridDim.x, p.max_shares));
     const int c = blockIdx.x, from = c < shares.n ? shares.begin(c) : 0, to = c < shares.n ? shares.begin(c + 1) : 0;
+    bool ok = true;
+    auto wait = [&](uint64_t *bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity & 1, err) && !*ab); };
 
     if (from >= to) {
-    } else if (warp >= 4 * QT && warp < MMA_WARP) {
-        // ------------------------------------------------------------ codes to fp16
-        const int cw = warp - 4 * QT, ct = cw * 32 + lane;
-        // the pages that are loaded run ahead of those that are stored
-        SharedWalk lw(p, from, to), sw(p, from, to);
-        SharedSegment ls, ss;
-        int l_at = 0, s_at = 0, ids = 0, idbase = -64;
-        bool wrong = false, more = lw.next<TQ>(ls);
-        uint4 kr[AHEAD][LOADS], vr[AHEAD][LOADS];
-        int valid[AHEAD];  // whether the page's id is right
-        // pieces ct, ct + 256, ... of the page's 128 CHUNKS
-        auto load = [&](int a) {
-            if (more && l_at == ls.count) {
-                more = lw.next<TQ>(ls);
-                l_at = 0;
-                idbase = -64;
-            }
-            if (!more) return;
-            const int page = ls.page + l_at;
-            if ((unsigned)(page - idbase) >= 32u) {
-                idbase = page;
-                ids = page + lane <= (ls.hi - 1) / kKv8Page ? __ldg(p.c.table + ls.row0 * p.c.table_stride + page + lane) : 0;
-                if (ids < 0 || ids >= p.c.n_blocks) {
-                    wrong = true;
-                    ids = -1;
+    } else if (warp == LOAD_WARP) {
+        // ------------------------------------------------------------ codes
+        SharedWalk w(p, from, to);
+        SharedSegment s;
+        uint32_t j = 0;  // pages
+        bool wrong = false;
+        while (ok && w.next(s)) {
+            int ids = 0, idbase = -64;
+#pragma unroll 1
+            for (int x = 0; x < s.count && ok; ++x, ++j) {
+                const int page = s.page + x;
+                if ((unsigned)(page - idbase) >= 32u) {
+                    idbase = page;
+                    ids = page + lane <= (s.hi - 1) / kKv8Page ? __ldg(p.c.table + s.row0 * p.c.table_stride + page + lane) : 0;
+                    if (ids < 0 || ids >= p.c.n_blocks) {
+                        wrong = true;
+                        ids = -1;
+                    }
                 }
+                const int block = __shfl_sync(0xffffffffu, ids, page - idbase);
+                const uint32_t st = j % RAWS;
+                if (j >= RAWS) wait(&S.raw_empty[st], j / RAWS - 1);
+                if (!ok) break;
+                if (lane == 0) {
+                    S.block[st] = block;
+                    if (block >= 0) {
+                        const uint8_t *k = p.c.codes + kv8_tile(p.c, block, 0, s.h) * (kKv8Page * HD);
+                        const uint64_t policy = l2_policy_evict_first();
+                        mbar_arrive_expect_tx(&S.raw_full[st], RAW);
+                        bulk_load_at(raw + st * RAW, k, RAW / 2, &S.raw_full[st], policy);
+                        bulk_load_at(raw + st * RAW + RAW / 2, k + (int64_t)p.c.KVH * (kKv8Page * HD), RAW / 2, &S.raw_full[st], policy);
+                    } else {
+                        mbar_arrive(&S.raw_full[st]);
+                    }
+                }
+                __syncwarp();
             }
-            const int block = __shfl_sync(0xffffffffu, ids, page - idbase);
-            valid[a] = block;
-            const int p0 = page * kKv8Page;
-            const uint8_t *k = p.c.codes + kv8_tile(p.c, max(block, 0), 0, ls.h) * (kKv8Page * HD) + 16 * ct;
-            const uint8_t *v = k + (int64_t)p.c.KVH * (kKv8Page * HD);
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {  // (positions that nobody attends to are not read)
-                const int at = p0 + (ct + 32 * kSharedConv * i) / CHUNKS;
-                const bool on = block >= 0 && at >= ls.lo && at < ls.hi;
-                kr[a][i] = on ? __ldg(reinterpret_cast<const uint4 *>(k + 16 * 32 * kSharedConv * i)) : make_uint4(0, 0, 0, 0);
-                vr[a][i] = on ? __ldg(reinterpret_cast<const uint4 *>(v + 16 * 32 * kSharedConv * i)) : make_uint4(0, 0, 0, 0);
-            }
-            ++l_at;
-        };
-        auto store = [&](uint32_t slot, const uint4 (&x)[LOADS]) {
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int piece = ct + 32 * kSharedConv * i, row = piece / CHUNKS, d = piece % CHUNKS;  // dims 16 d ..
-                uint32_t h[8];
-                decode4_half<FMT>(x[i].x, h[0], h[1]);
-                decode4_half<FMT>(x[i].y, h[2], h[3]);
-                decode4_half<FMT>(x[i].z, h[4], h[5]);
-                decode4_half<FMT>(x[i].w, h[6], h[7]);
-                const uint32_t at = slot + (d / 4) * (kSharedQ * 128) + row * 128, c0 = d % 4 * 2;
-                // (the second 64 dims' pieces the other way round, so that lanes of a row meet all banks)
-                const bool turn = d >= 4;
-                const uint32_t a0 = at + (((c0 + turn) ^ (row & 7)) << 4), a1 = at + (((c0 + !turn) ^ (row & 7)) << 4);
-                st_shared_v4(a0, turn ? h[4] : h[0], turn ? h[5] : h[1], turn ? h[6] : h[2], turn ? h[7] : h[3]);
-                st_shared_v4(a1, turn ? h[0] : h[4], turn ? h[1] : h[5], turn ? h[2] : h[6], turn ? h[3] : h[7]);
-            }
-        };
+        }
+        if (!ok) *ab = 1;
+        // every copy lands before the CTA ends
+        for (uint32_t q = 0; q < RAWS && q < j; ++q) mbar_wait(&S.raw_full[(j - 1 - q) % RAWS], ((j - 1 - q) / RAWS) & 1, err);
+        if (wrong) kv8_report(p.status);
+    } else if (warp >= kSharedSoft && warp < MMA_WARP) {
+        // ------------------------------------------------------------ codes to fp16
+        const int cw = warp - kSharedSoft, ct = cw * 32 + lane;
+        SharedWalk w(p, from, to);
+        SharedSegment s;
+        uint32_t j = 0;
         auto give = [&](uint64_t *bar) {
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar);
         };
-        bool ok = true;
-        uint32_t j = 0;  // pages stored
+        while (ok && w.next(s)) {
+#pragma unroll 1
+            for (int x = 0; x < s.count && ok; ++x, ++j) {
+                const uint32_t st = j % RAWS, sk = 2 * (j & 1), sv = sk + 1, before = (j >> 1) - 1;
+                wait(&S.raw_full[st], j / RAWS);
+                if (!ok) break;
+                const int block = S.block[st], p0 = (s.page + x) * kKv8Page;
+                const bool cut = block < 0 || p0 < s.lo || p0 + kKv8Page > s.hi;  // positions that nobody attends to are 0: what they hold does not matter
+                float scale = __int_as_float(0x7fc00000);
+                if (cw == 0 && lane < 8 && block >= 0)
+                    scale = __ldg(p.c.scales + (((int64_t)block * 2 + lane / 4) * p.c.KVH + s.h) * kKv8PageBlocks + lane % 4);
+                uint32_t nan = 0;
+                auto store = [&](uint32_t src, uint32_t slot, bool value) {
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) load(a);
-        int a = 0;
-        for (bool live = sw.next<TQ>(ss); live && ok; live = sw.next<TQ>(ss)) {
-            const int64_t tiles = (int64_t)ss.h;
-            for (s_at = 0; s_at < ss.count && ok; ++s_at, ++j) {
-                auto step = [&](auto slot_of) {
-                    constexpr int A = decltype(slot_of)::value;
-                    const uint32_t sk = 2 * (j & 1), sv = sk + 1, ph = ((j >> 1) & 1) ^ 1;
-                    const int block = valid[A];
-                    if (cw == 0 && lane < 8) {  // (slot j & 3: read long ago when page j - 4's went)
-                        float f = __int_as_float(0x7fc00000);
-                        if (block >= 0) f = __ldg(p.c.scales + (((int64_t)block * 2 + lane / 4) * p.c.KVH + tiles) * kKv8PageBlocks + lane % 4);
-                        S.scale[j & 3][lane] = f;
-                    }
-                    if (j >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&S.empty[sk], ph, err) && !*ab);
-                    if (!ok) return;
-                    store(ring + sk * TILE, kr[A]);
-                    give(&S.full[sk]);
-                    uint32_t nan = 0;
-                    if constexpr (FMT == SARA_KV8_E4M3) {  // codes 0x7f and 0xff: their block reads as NaN, and 0 times them must not
-#pragma unroll
-                        for (int i = 0; i < LOADS; ++i) {
-                            const uint32_t w[4] = {vr[A][i].x, vr[A][i].y, vr[A][i].z, vr[A][i].w};
+                    for (int i = 0; i < LOADS; ++i) {
+                        const int piece = ct + 32 * kSharedConv * i, row = piece / CHUNKS, d = piece % CHUNKS;  // dims 16 d ..
+                        uint32_t r[4], h[8];
+                        load_codes<4>(src + 16 * piece, r);
+                        if (cut && (block < 0 || p0 + row < s.lo || p0 + row >= s.hi)) r[0] = r[1] = r[2] = r[3] = 0;
+                        if (FMT == SARA_KV8_E4M3 && value) {  // codes 0x7f and 0xff: their block reads as NaN, and 0 times them must not
                             uint32_t any = 0;
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) any |= ((w[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                            for (int e = 0; e < 4; ++e) any |= ((r[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
                             if (any) {
-                                nan |= 1u << ((ct + 32 * kSharedConv * i) / CHUNKS / kKv8Block);
-                                vr[A][i] = make_uint4(0, 0, 0, 0);
+                                nan |= 1u << (row / kKv8Block);
+                                r[0] = r[1] = r[2] = r[3] = 0;
                             }
                         }
-                        nan = __reduce_or_sync(0xffffffffu, nan);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) decode4_half<FMT>(r[e], h[2 * e], h[2 * e + 1]);
+                        const uint32_t at = slot + (d / 4) * (kSharedQ * 128) + row * 128, c0 = d % 4 * 2;
+                        // (the second 64 dims' pieces the other way round, so that lanes of a row meet all banks)
+                        const bool turn = d >= 4;
+                        const uint32_t a0 = at + (((c0 + turn) ^ (row & 7)) << 4), a1 = at + (((c0 + !turn) ^ (row & 7)) << 4);
+                        st_shared_v4(a0, turn ? h[4] : h[0], turn ? h[5] : h[1], turn ? h[6] : h[2], turn ? h[7] : h[3]);
+                        st_shared_v4(a1, turn ? h[0] : h[4], turn ? h[1] : h[5], turn ? h[2] : h[6], turn ? h[3] : h[7]);
                     }
-                    if (j >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&S.empty[sv], ph, err) && !*ab);
-                    if (!ok) return;
-                    store(ring + sv * TILE, vr[A]);
-                    if (lane == 0) S.nan[j & 3][cw] = nan;
-                    give(&S.full[sv]);
-                    if (lane == 0) mbar_arrive(&S.scales[j & 3]);
-                    load(A);
                 };
-                if (AHEAD == 1 || a == 0) step(std::integral_constant<int, 0>());
-                else step(std::integral_constant<int, AHEAD - 1>());
-                a = a + 1 == AHEAD ? 0 : a + 1;
+                if (j >= 2) wait(&S.empty[sk], before);
+                if (!ok) break;
+                store(raw + st * RAW, ring + sk * TILE, false);
+                give(&S.full[sk]);
+                if (j >= 2) wait(&S.empty[sv], before);
+                if (!ok) break;
+                store(raw + st * RAW + RAW / 2, ring + sv * TILE, true);
+                // (place j & 3: read when page j - 2's product was asked for)
+                if (cw == 0 && lane < 8) S.scale[j & 3][lane] = scale;
+                if constexpr (FMT == SARA_KV8_E4M3) nan = __reduce_or_sync(0xffffffffu, nan);
+                if (lane == 0) S.nan[j & 3][cw] = nan;
+                give(&S.full[sv]);
+                if (lane == 0) {
+                    mbar_arrive(&S.raw_empty[st]);
+                    mbar_arrive(&S.scales[j & 3]);
+                }
             }
         }
         if (!ok) *ab = 1;
-        if (wrong) kv8_report(p.status);
     } else if (warp == MMA_WARP) {
         // ------------------------------------------------------------ MMAs
         constexpr uint32_t idesc_s = 1u << 4 | (128u >> 3) << 17 | (128u >> 4) << 24;
         constexpr uint32_t idesc_o = 1u << 4 | 1u << 16 | ((uint32_t)HD >> 3) << 17 | (128u >> 4) << 24;  // values: N-major
         SharedWalk w(p, from, to);
         SharedSegment s;
-        uint32_t j0 = 0, unit[2] = {}, done[2] = {};  // pages before; per tile of queries: units, products issued
-        bool ok = true;
-        auto wait = [&](uint64_t *bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity & 1, err) && !*ab); };
-        while (ok && w.next<TQ>(s)) {
-            const int nq = QT == 1 ? 1 : (s.queries + kSharedQ - 1) / kSharedQ;
-            auto scores = [&](int q, uint32_t x) {  // of the segment's page x
-                const uint32_t j = j0 + x, sk = 2 * (j & 1);
-                if (q == 0) wait(&S.full[sk], j >> 1);
-                const uint32_t buf = QT == 1 ? j & 1 : (uint32_t)q;
-                // its place holds the probabilities of an earlier page until their product is done
-                if (done[q] > 0) wait(&S.pv_done[q], done[q] - 1);
-                if (!ok) return;
-                tc_fence_after();
-                if (elect_one()) {
-                    const uint32_t a = base + q * TILE, b = ring + sk * TILE;
+        uint32_t j0 = 0, unit = 0, done = 0;  // pages before, units, products issued
+        auto scores = [&](uint32_t j) {
+            const uint32_t sk = 2 * (j & 1);
+            wait(&S.full[sk], j >> 1);
+            // its place holds the probabilities of an earlier page until their product is done
+            if (done > 0) wait(&S.pv_done, done - 1);
+            if (!ok) return;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint32_t b = ring + sk * TILE;
 #pragma unroll
-                    for (int k = 0; k < HD / 16; ++k)
-                        tc_mma_bf16(tmem + buf * 128, sdesc_128(a + k / 4 * (kSharedQ * 128) + k % 4 * 32, 16),
-                                    sdesc_128(b + k / 4 * (kSharedQ * 128) + k % 4 * 32, 16), idesc_s, k > 0);
-                    if (q == nq - 1) tc_commit(&S.empty[sk]);
-                    tc_commit(&S.s_full[buf]);
-                }
-                __syncwarp();
-            };
-            auto values = [&](int q, uint32_t x) {
-                const uint32_t j = j0 + x, sv = 2 * (j & 1) + 1, buf = QT == 1 ? j & 1 : (uint32_t)q;
-                if (q == 0) wait(&S.full[sv], j >> 1);
-                wait(&S.p_full[buf], QT == 1 ? j >> 1 : done[q]);
-                if (!ok) return;
+                for (int k = 0; k < HD / 16; ++k)
+                    tc_mma_ts(tmem + (j & 1) * 128, tmem + Q_AT + k * 8, sdesc_128(b + k / 4 * (kSharedQ * 128) + k % 4 * 32, 16), idesc_s, k > 0);
+                tc_commit(&S.s_full[j & 1]);
+                tc_commit(&S.empty[sk]);
+            }
+            __syncwarp();
+        };
+        while (ok && w.next(s)) {
+            wait(&S.q_full, unit++);
+            if (ok) scores(j0);
+#pragma unroll 1
+            for (uint32_t x = 0; x < (uint32_t)s.count && ok; ++x) {
+                const uint32_t j = j0 + x, sv = 2 * (j & 1) + 1;
+                if (x + 1 < (uint32_t)s.count) scores(j + 1);
+                wait(&S.full[sv], j >> 1);
+                wait(&S.p_full[j & 1], j >> 1);
+                if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
                     const uint32_t b = ring + sv * TILE;
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        tc_mma_ts(tmem + 256 + q * 128, tmem + buf * 128 + k * 8, sdesc_128(b + k * 2048, kSharedQ * 128), idesc_o, x > 0 || k > 0);
-                    if (q == nq - 1) tc_commit(&S.empty[sv]);
-                    tc_commit(&S.pv_done[q]);
-                    if (x + 1 == (uint32_t)s.count) tc_commit(&S.o_full[q]);
+                        tc_mma_ts(tmem + O_AT, tmem + (j & 1) * 128 + k * 8, sdesc_128(b + k * 2048, kSharedQ * 128), idesc_o, x > 0 || k > 0);
+                    tc_commit(&S.pv_done);
+                    tc_commit(&S.empty[sv]);
+                    if (x + 1 == (uint32_t)s.count) tc_commit(&S.o_full);
                 }
                 __syncwarp();
-                ++done[q];
-            };
-            for (int q = 0; q < nq; ++q) wait(&S.q_full[q], unit[q]++);
-            for (int q = 0; q < nq && ok; ++q) scores(q, 0);
-#pragma unroll 1
-            for (uint32_t x = 0; x < (uint32_t)s.count && ok; ++x) {
-                if (QT == 1) {
-                    if (x + 1 < (uint32_t)s.count) scores(0, x + 1);
-                    if (ok) values(0, x);
-                } else {
-                    for (int q = 0; q < nq && ok; ++q) values(q, x);
-                    for (int q = 0; q < nq && ok && x + 1 < (uint32_t)s.count; ++q) scores(q, x + 1);
-                }
+                ++done;
             }
             j0 += s.count;
         }
         if (!ok) *ab = 1;
-        // every MMA has retired before tensor memory is released: the last commits
-        for (int q = 0; q < QT; ++q)
-            if (done[q] > 0) mbar_wait(&S.pv_done[q], (done[q] - 1) & 1, err);
-    } else if (warp < 4 * QT) {
-        // ------------------------------------------------------------ softmax, a query a thread
-        const int qt = warp >> 2, lrow = (warp & 3) * 32 + lane;
-        const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16), o_at = lanes + 256 + qt * 128;
+        if (done > 0) mbar_wait(&S.pv_done, (done - 1) & 1, err);  // every MMA has retired before tensor memory is released
+    } else if (warp < kSharedSoft) {
+        // ------------------------------------------------------------ softmax: a query's first or second 64 positions a thread
+        const int quarter = warp & 3, half = warp >> 2, lrow = quarter * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), o_at = lanes + O_AT + half * (HD / 2);
         SharedWalk w(p, from, to);
         SharedSegment s;
-        uint32_t j0 = 0, tile = 0, unit = 0;  // pages before; pages and units of this tile of queries
-        bool ok = true;
-        auto wait = [&](uint64_t *bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity & 1, err) && !*ab); };
-        while (ok && w.next<TQ>(s)) {
-            if (QT == 2 && qt * kSharedQ >= s.queries) {  // (no query of this tile)
-                j0 += s.count;
-                continue;
-            }
-            const int at = s.q0 + qt * kSharedQ + lrow;  // among the group's queries
-            const bool live = qt * kSharedQ + lrow < s.queries;
+        uint32_t j0 = 0, unit = 0;
+        // (after a failed wait the barriers go on, so that no warp is left in one)
+        while (w.next(s)) {
+            const int at = s.q0 + lrow;  // among the group's queries
+            const bool live = lrow < s.queries;
             const int row = s.row0 + (live ? at / G : 0), head = s.h * G + (live ? at % G : 0);
             const bool any = __any_sync(0xffffffffu, live);
-            // the query, as fp16
+            // the query as fp16, one half of it
             float mul = p.scale_log2;
             int lo = 0, hi = 0;
             {
@@ -518,83 +529,86 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
                     f = pow2f(e);
                     mul *= pow2f(-e);
                 }
-                const uint32_t to = base + qt * TILE + lrow * 128;
 #pragma unroll
-                for (int i = 0; i < HD / 8; ++i) {
-                    uint4 x = live ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+                for (int x = 0; x < HD / 16; ++x) {
+                    const int i = half * (HD / 16) + x;
+                    uint4 y = live ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
                     if (p.type == SARA_BF16) {
-                        uint32_t y[4] = {x.x, x.y, x.z, x.w};
+                        uint32_t u[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float2 z = unpack2<SARA_BF16>(y[e]);
-                            y[e] = pack_half2(z.x * f, z.y * f);
+                            const float2 z = unpack2<SARA_BF16>(u[e]);
+                            u[e] = pack_half2(z.x * f, z.y * f);
                         }
-                        x = make_uint4(y[0], y[1], y[2], y[3]);
+                        y = make_uint4(u[0], u[1], u[2], u[3]);
                     }
-                    st_shared_v4(to + i / 8 * (kSharedQ * 128) + (((i % 8) ^ (lrow & 7)) << 4), x.x, x.y, x.z, x.w);
+                    tmem_store4(lanes + Q_AT + i * 4, y);
                 }
                 if (live && p.row_group[row] >= 0) {
                     lo = p.first ? p.first[row] : 0;
                     hi = min(p.ctx[row], p.row_prefix[row]);
                 }
             }
-            fence_proxy_async_smem();
+            tmem_wait_st();
+            tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&S.q_full[qt]);
+            if (lane == 0) mbar_arrive(&S.q_full);
 
             float m = -3.4028235e38f, R = m, l = 0.f;
 #pragma unroll 1
-            for (int x = 0; x < s.count && ok; ++x, ++tile) {
-                const uint32_t j = j0 + x, buf = QT == 1 ? j & 1 : (uint32_t)qt;
-                const uint32_t s_at = lanes + buf * 128;
-                wait(&S.s_full[buf], QT == 1 ? j >> 1 : tile);
+            for (int x = 0; x < s.count; ++x) {
+                const uint32_t j = j0 + x, s_at = lanes + (j & 1) * 128 + half * 64;
+                wait(&S.s_full[j & 1], j >> 1);
                 wait(&S.scales[j & 3], j >> 2);
-                if (!ok) break;
-                tc_fence_after();
                 if (any) {
-                    float ks[4], vs[4], ev[4];
+                    tc_fence_after();
+                    float v[64], ks[2], vs[2], ev[2];
+                    tmem_load64(s_at, v);
                     uint32_t bad = 0;
                     if constexpr (FMT == SARA_KV8_E4M3) {
-                        const uint4 b0 = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][0]), b1 = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][4]);
-                        bad = b0.x | b0.y | b0.z | b0.w | b1.x | b1.y | b1.z | b1.w;
+                        static_assert(kSharedConv == 4 && offsetof(SharedSmem, nan) % 16 == 0, "a word a warp, read at once");
+                        const uint4 b = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][0]);
+                        bad = (b.x | b.y | b.z | b.w) >> (2 * half);
                     }
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        ks[b] = S.scale[j & 3][b] * mul;
-                        vs[b] = bad >> b & 1 ? __int_as_float(0x7fc00000) : S.scale[j & 3][4 + b];
+                    for (int b = 0; b < 2; ++b) {
+                        ks[b] = S.scale[j & 3][2 * half + b] * mul;
+                        vs[b] = bad >> b & 1 ? __int_as_float(0x7fc00000) : S.scale[j & 3][4 + 2 * half + b];
                         ev[b] = (float)min(max(scale_exp(vs[b]), -126), 126);
                     }
-                    const int p0 = (s.page + x) * kKv8Page;
-                    const bool masked = __any_sync(0xffffffffu, lo > p0 || hi < p0 + kKv8Page);
-                    float most = -INFINITY, product = -INFINITY;
+                    const int p0 = (s.page + x) * kKv8Page + 64 * half;
+                    const bool masked = __any_sync(0xffffffffu, lo > p0 || hi < p0 + 64);
+                    if (masked) {
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        float v[32];
-                        tmem_load32(s_at + 32 * b, v);
-                        if (masked) {
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) v[e] = p0 + 32 * b + e >= lo && p0 + 32 * b + e < hi ? v[e] : -INFINITY;
-                        }
-                        float n = fmaxf(v[0], v[1]);
-#pragma unroll
-                        for (int e = 2; e < 32; ++e) n = fmaxf(n, v[e]);
-                        n *= ks[b];
-                        most = fmaxf(most, n);
-                        product = fmaxf(product, n + ev[b]);
+                        for (int e = 0; e < 64; ++e) v[e] = p0 + e >= lo && p0 + e < hi ? v[e] : -INFINITY;
                     }
-                    const bool raise = most > m + 8.f || product > R + 8.f;
+                    float2 top = make_float2(-INFINITY, -INFINITY);
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        float n = fmaxf(v[32 * b], v[32 * b + 1]);
+#pragma unroll
+                        for (int e = 2; e < 32; ++e) n = fmaxf(n, v[32 * b + e]);
+                        n *= ks[b];
+                        top.x = fmaxf(top.x, n);
+                        top.y = fmaxf(top.y, n + ev[b]);
+                    }
+                    S.top[j & 1][half][lrow] = top;
+                    named_bar_sync(1 + quarter, 64);  // (the next page has the other place)
+                    const float2 other = S.top[j & 1][half ^ 1][lrow];
+                    top.x = fmaxf(top.x, other.x);
+                    top.y = fmaxf(top.y, other.y);
+                    const bool raise = top.x > m + 8.f || top.y > R + 8.f;
                     if (__any_sync(0xffffffffu, raise)) {
-                        const float m1 = raise ? fmaxf(m, most) : m, R1 = raise ? fmaxf(R, product) : R;
+                        const float m1 = raise ? fmaxf(m, top.x) : m, R1 = raise ? fmaxf(R, top.y) : R;
                         l *= ex2(fmaxf(m - m1, -1e4f));
                         const float f = ex2(fmaxf(R - R1, -1e4f));
                         m = m1;
                         R = R1;
                         if (x > 0) {
-                            wait(&S.pv_done[qt], tile - 1);
-                            if (!ok) break;
+                            wait(&S.pv_done, j - 1);
                             tc_fence_after();
 #pragma unroll 1
-                            for (int d = 0; d < HD; d += 16) {
+                            for (int d = 0; d < HD / 2; d += 16) {
                                 float o[16];
                                 tmem_load16(o_at + d, o);
                                 uint32_t y[16];
@@ -602,23 +616,19 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
                                 for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(o[e] * f);
                                 tmem_st_x16(o_at + d, y);
                             }
-                            tmem_wait_st();
                         }
                     }
                     float l0 = 0.f, l1 = 0.f;
+                    uint32_t h[32];
 #pragma unroll
-                    for (int b = 0; b < 4; ++b) {
-                        float v[32];
-                        tmem_load32(s_at + 32 * b, v);
+                    for (int b = 0; b < 2; ++b) {
                         const float F = ex2(fminf(m - R + ev[b] + kSharedShift, 126.f)) * (vs[b] * pow2f(-(int)ev[b]));
-                        uint32_t h[16];
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
-                            float a0 = ex2(fmaf(v[e], ks[b], -m)), a1 = ex2(fmaf(v[e + 1], ks[b], -m));
-                            float w0 = a0 * F, w1 = a1 * F;
-                            if (masked) {
-                                const int at0 = p0 + 32 * b + e;
-                                const bool on0 = at0 >= lo && at0 < hi, on1 = at0 + 1 >= lo && at0 + 1 < hi;
+                            const int i = 32 * b + e;
+                            float a0 = ex2(fmaf(v[i], ks[b], -m)), a1 = ex2(fmaf(v[i + 1], ks[b], -m)), w0 = a0 * F, w1 = a1 * F;
+                            if (masked) {  // (0, whatever the scales are)
+                                const bool on0 = p0 + i >= lo && p0 + i < hi, on1 = p0 + i + 1 >= lo && p0 + i + 1 < hi;
                                 a0 = on0 ? a0 : 0.f;
                                 a1 = on1 ? a1 : 0.f;
                                 w0 = on0 ? w0 : 0.f;
@@ -626,35 +636,37 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
                             }
                             l0 += a0;
                             l1 += a1;
-                            h[e / 2] = pack_half2(w0, w1);
+                            h[i / 2] = pack_half2(w0, w1);
                         }
-                        tmem_st_x16(s_at + 16 * b, h);
                     }
                     l += l0 + l1;
-                    tmem_wait_st();
+                    tmem_store32(lanes + (j & 1) * 128 + half * 32, h);  // (both halves have read their scores: the barrier)
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&S.p_full[buf]);
+                if (lane == 0) mbar_arrive(&S.p_full[j & 1]);
             }
             // (not pv_done, which may be two pages behind a warp that has just left the last: its parity would not tell)
-            wait(&S.o_full[qt], unit++);
-            if (!ok) break;
-            tc_fence_after();
+            wait(&S.o_full, unit++);
             if (any) {
+                if (half) S.sum[lrow] = l;
+                named_bar_sync(1 + quarter, 64);
+                tc_fence_after();
                 float *o = s.whole ? p.whole + ((int64_t)row * p.H + head) * (HD + 2)
-                                   : p.part + (((int64_t)c * 2 + s.begins) * TQ + qt * kSharedQ + lrow) * (HD + 2);
+                                   : p.part + (((int64_t)c * 2 + s.begins) * kSharedQ + lrow) * (HD + 2);
                 const float f = ex2(fminf(fmaxf(R - m - kSharedShift, -1e4f), 126.f));
 #pragma unroll 1
-                for (int d = 0; d < HD; d += 16) {
+                for (int d = 0; d < HD / 2; d += 16) {
                     float y[16];
                     tmem_load16(o_at + d, y);
                     if (live) {
 #pragma unroll
-                        for (int e = 0; e < 16; e += 2) *reinterpret_cast<float2 *>(o + 2 + d + e) = make_float2(y[e] * f, y[e + 1] * f);
+                        for (int e = 0; e < 16; e += 2)
+                            *reinterpret_cast<float2 *>(o + 2 + half * (HD / 2) + d + e) = make_float2(y[e] * f, y[e + 1] * f);
                     }
                 }
-                if (live) *reinterpret_cast<float2 *>(o) = make_float2(m, l);
+                if (live && !half) *reinterpret_cast<float2 *>(o) = make_float2(m, l + S.sum[lrow]);
+                named_bar_sync(1 + quarter, 64);  // (the sums have been read)
             }
             tc_fence_before();
             j0 += s.count;
@@ -670,7 +682,7 @@ __global__ void __launch_bounds__(shared_threads(QT), 1) shared_prefix_kernel(Sh
 
 // ------------------------------------------------------------------------------- join
 // A query's state of its own positions and those of its shared ones, W warps to a query
-template <int HD, int TQ, int W>
+template <int HD, int W>
 __global__ void __launch_bounds__(256) shared_join_kernel(SharedParams p, int shares_most) {
     constexpr int D = HD / 32;
     __shared__ float s_m[8], s_l[8], s_o[8][HD];
@@ -697,7 +709,7 @@ __global__ void __launch_bounds__(256) shared_join_kernel(SharedParams p, int sh
     if (g >= 0) {
         const SharedGroup y = p.group[g];
         const SharedShares shares(p.plan->entries, shares_most);
-        const int at = (row - y.row0) * G + head % G, e0 = y.entry0 + (head / G * y.tiles + at / TQ) * y.pages;
+        const int at = (row - y.row0) * G + head % G, e0 = y.entry0 + (head / G * y.tiles + at / kSharedQ) * y.pages;
         const int c0 = shares.of(e0), c1 = shares.of(e0 + y.pages - 1);
         if (c0 == c1) {
             const float *s = p.whole + x * (HD + 2);
@@ -705,7 +717,7 @@ __global__ void __launch_bounds__(256) shared_join_kernel(SharedParams p, int sh
         } else {
 #pragma unroll 4
             for (int c = c0 + part; c <= c1; c += W) {
-                const float *s = p.part + (((int64_t)c * 2 + (c == c0)) * TQ + at % TQ) * (HD + 2);
+                const float *s = p.part + (((int64_t)c * 2 + (c == c0)) * kSharedQ + at % kSharedQ) * (HD + 2);
                 add(s[0], s[1], s + 2);
             }
         }

@@ -35,7 +35,7 @@ SharedLayout shared_layout(int n, int groups, int H, int kvh, int hd) {
     w.out32 = take(states * hd * 4);
     w.lse = take(states * 4);
     w.whole = take(states * (hd + 2) * 4);
-    w.part = take((size_t)kSharedMaxShares * 2 * (2 * kSharedQ) * (hd + 2) * 4);
+    w.part = take((size_t)kSharedMaxShares * 2 * kSharedQ * (hd + 2) * 4);
     w.bytes = at;
     return w;
 }
@@ -45,18 +45,17 @@ T *at(void *ws, size_t off) {
     return reinterpret_cast<T *>(static_cast<uint8_t *>(ws) + off);
 }
 
-template <int HD, int FMT, int QT>
-void shared_launch(const SharedParams &p, int sms, cudaStream_t s) {
-    const auto kern = shared_prefix_kernel<HD, FMT, QT>;
-    CK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_smem(HD, QT)));
-    kern<<<(unsigned)std::min(sms, kSharedMaxShares), shared_threads(QT), shared_smem(HD, QT), s>>>(p);
-    CK(cudaGetLastError());
+template <int HD, int FMT>
+void shared_launch(const SharedParams &p, int shares, cudaStream_t s) {
+    const auto kern = shared_prefix_kernel<HD, FMT>;
+    CK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_smem(HD)));
+    launch_cluster(s, true, dim3((unsigned)shares), dim3(kSharedThreads), shared_smem(HD), 1, kern, p);
 }
-template <int HD, int QT>
+template <int HD>
 void shared_join(const SharedParams &p, int shares, cudaStream_t s) {
     const int64_t states = (int64_t)p.n * p.H;
-    if (states <= kSharedWideJoin) shared_join_kernel<HD, kSharedQ * QT, 8><<<(unsigned)states, 256, 0, s>>>(p, shares);
-    else shared_join_kernel<HD, kSharedQ * QT, 1><<<(unsigned)((states + 7) / 8), 256, 0, s>>>(p, shares);
+    if (states <= kSharedWideJoin) shared_join_kernel<HD, 8><<<(unsigned)states, 256, 0, s>>>(p, shares);
+    else shared_join_kernel<HD, 1><<<(unsigned)((states + 7) / 8), 256, 0, s>>>(p, shares);
     CK(cudaGetLastError());
 }
 
@@ -113,16 +112,9 @@ int sara_attention_shared_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
         p.own_lse = at<float>(workspace, w.lse);
         p.out = static_cast<uint16_t *>(out);
         p.lse = lse;
-        const bool wide = n_groups > 0 && (int64_t)n_seq * (n_heads / cache->n_kv_heads) > (int64_t)kSharedQ * n_groups;
-        if (wide) shared_plan_kernel<2 * kSharedQ><<<1, 1024, 0, s>>>(p);
-        else shared_plan_kernel<kSharedQ><<<1, 1024, 0, s>>>(p);
+        shared_plan_kernel<<<1, 1024, 0, s>>>(p);
         CK(cudaGetLastError());
-        if (n_groups > 0) {
-            by_shape(cache, [&](auto d, auto fmt) {
-                if (wide) shared_launch<d.value, fmt.value, 2>(p, sms, s);
-                else shared_launch<d.value, fmt.value, 1>(p, sms, s);
-            });
-        }
+        if (n_groups > 0) by_shape(cache, [&](auto d, auto fmt) { shared_launch<d.value, fmt.value>(p, shares, s); });
         AttnKv8Params a{};
         a.c = p.c;
         a.q = p.q;
@@ -139,10 +131,7 @@ int sara_attention_shared_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
         a.part = reinterpret_cast<float *>(at<uint8_t>(workspace, w.own) + attn_kv8_count_bytes());
         a.scale_log2 = p.scale_log2;
         attn_kv8_launch(cache, a, warps, s);
-        by_shape(cache, [&](auto d, auto) {
-            if (wide) shared_join<d.value, 2>(p, shares, s);
-            else shared_join<d.value, 1>(p, shares, s);
-        });
+        by_shape(cache, [&](auto d, auto) { shared_join<d.value>(p, shares, s); });
     });
 }
 
