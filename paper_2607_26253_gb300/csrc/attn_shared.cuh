@@ -288,6 +288,31 @@ __device__ __forceinline__ void bulk_load_at(uint32_t dst, const void *src, uint
 __device__ __forceinline__ uint64_t sdesc_128(uint32_t addr, uint32_t lbo) {  // 128-byte swizzle, 8 rows after 1,024 bytes
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {  // a NaN gives way
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t pack_f32x2(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 unpack_f32x2(uint64_t x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
 __device__ __forceinline__ void st_shared_v4(uint32_t at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
@@ -403,7 +428,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                     scale = __ldg(p.c.scales + (((int64_t)block * 2 + lane / 4) * p.c.KVH + s.h) * kKv8PageBlocks + lane % 4);
                 uint32_t nan = 0;
                 auto store = [&](uint32_t src, uint32_t slot, bool value) {
-#pragma unroll
+#pragma unroll 2
                     for (int i = 0; i < LOADS; ++i) {
                         const int piece = ct + 32 * kSharedConv * i, row = piece / CHUNKS, d = piece % CHUNKS;  // dims 16 d ..
                         uint32_t r[4], h[8];
@@ -562,7 +587,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 wait(&S.scales[j & 3], j >> 2);
                 if (any) {
                     tc_fence_after();
-                    float v[64], ks[2], vs[2], ev[2];
+                    float v[64], ks[2], F[2], ev[2];
                     tmem_load64(s_at, v);
                     uint32_t bad = 0;
                     if constexpr (FMT == SARA_KV8_E4M3) {
@@ -570,15 +595,21 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                         const uint4 b = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][0]);
                         bad = (b.x | b.y | b.z | b.w) >> (2 * half);
                     }
+                    const int p0 = (s.page + x) * kKv8Page + 64 * half;
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         ks[b] = S.scale[j & 3][2 * half + b] * mul;
-                        vs[b] = bad >> b & 1 ? __int_as_float(0x7fc00000) : S.scale[j & 3][4 + 2 * half + b];
-                        ev[b] = (float)min(max(scale_exp(vs[b]), -126), 126);
+                        F[b] = S.scale[j & 3][4 + 2 * half + b];
+                        // a block that reads as NaN makes the sums of those that attend to it NaN, and leaves the others alone
+                        if ((bad >> b & 1) || !(fabsf(ks[b]) < INFINITY && fabsf(F[b]) < INFINITY)) {
+                            if (lo < p0 + 32 * b + 32 && hi > p0 + 32 * b) l = __int_as_float(0x7fc00000);
+                            ks[b] = 1.f;
+                            F[b] = 0.f;
+                        }
+                        ev[b] = (float)min(max(scale_exp(F[b]), -126), 126);
+                        F[b] *= pow2f(-(int)ev[b]);
                     }
-                    const int p0 = (s.page + x) * kKv8Page + 64 * half;
-                    const bool masked = __any_sync(0xffffffffu, lo > p0 || hi < p0 + 64);
-                    if (masked) {
+                    if (__any_sync(0xffffffffu, lo > p0 || hi < p0 + 64)) {  // some are masked
 #pragma unroll
                         for (int e = 0; e < 64; ++e) v[e] = p0 + e >= lo && p0 + e < hi ? v[e] : -INFINITY;
                     }
@@ -587,7 +618,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                     for (int b = 0; b < 2; ++b) {
                         float n = fmaxf(v[32 * b], v[32 * b + 1]);
 #pragma unroll
-                        for (int e = 2; e < 32; ++e) n = fmaxf(n, v[32 * b + e]);
+                        for (int e = 2; e < 32; e += 2) n = max3(n, v[32 * b + e], v[32 * b + e + 1]);
                         n *= ks[b];
                         top.x = fmaxf(top.x, n);
                         top.y = fmaxf(top.y, n + ev[b]);
@@ -618,28 +649,23 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                             }
                         }
                     }
-                    float l0 = 0.f, l1 = 0.f;
+                    uint64_t l2 = 0;  // two sums
                     uint32_t h[32];
+                    const uint64_t m2 = pack_f32x2(-m, -m);
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        const float F = ex2(fminf(m - R + ev[b] + kSharedShift, 126.f)) * (vs[b] * pow2f(-(int)ev[b]));
+                        const float f = F[b] * ex2(fminf(m - R + ev[b] + kSharedShift, 126.f));
+                        const uint64_t k2 = pack_f32x2(ks[b], ks[b]), f2 = pack_f32x2(f, f);
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
-                            const int i = 32 * b + e;
-                            float a0 = ex2(fmaf(v[i], ks[b], -m)), a1 = ex2(fmaf(v[i + 1], ks[b], -m)), w0 = a0 * F, w1 = a1 * F;
-                            if (masked) {  // (0, whatever the scales are)
-                                const bool on0 = p0 + i >= lo && p0 + i < hi, on1 = p0 + i + 1 >= lo && p0 + i + 1 < hi;
-                                a0 = on0 ? a0 : 0.f;
-                                a1 = on1 ? a1 : 0.f;
-                                w0 = on0 ? w0 : 0.f;
-                                w1 = on1 ? w1 : 0.f;
-                            }
-                            l0 += a0;
-                            l1 += a1;
-                            h[i / 2] = pack_half2(w0, w1);
+                            const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(v[32 * b + e], v[32 * b + e + 1]), k2, m2));
+                            const uint64_t a = pack_f32x2(ex2(y.x), ex2(y.y));
+                            l2 = add_f32x2(l2, a);
+                            const float2 w = unpack_f32x2(mul_f32x2(a, f2));
+                            h[16 * b + e / 2] = pack_half2(w.x, w.y);
                         }
                     }
-                    l += l0 + l1;
+                    l += unpack_f32x2(l2).x + unpack_f32x2(l2).y;
                     tmem_store32(lanes + (j & 1) * 128 + half * 32, h);  // (both halves have read their scores: the barrier)
                 }
                 tc_fence_before();
