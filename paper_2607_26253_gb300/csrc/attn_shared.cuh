@@ -211,7 +211,7 @@ struct SharedWalk {
 
 // ------------------------------------------------------------------------------- prefix
 struct SharedSmem {
-    uint64_t raw_full[4], raw_empty[4], full[kSharedSlots], empty[kSharedSlots], scales[4], q_full, s_full[2], p_full[2], pv_done, o_full;
+    uint64_t raw_full[4], raw_empty[4], full[kSharedSlots], empty[kSharedSlots], scales[4], flags[4], q_full, s_full[2], p_full[2], pv_done, o_full;
     float scale[4][8];             // of a page: K's four, V's four
     alignas(16) uint32_t nan[4][kSharedConv];  // blocks of a page in which a warp met a NaN among V's codes (read 16 bytes at a time)
     float2 top[2][2][kSharedQ];    // a query's largest score and product, of either half of a page, two pages in turn
@@ -333,7 +333,8 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
             mbar_init(&S.raw_empty[s], kSharedConv);
             mbar_init(&S.full[s], kSharedConv);
             mbar_init(&S.empty[s], 1);
-            mbar_init(&S.scales[s], kSharedConv);
+            mbar_init(&S.scales[s], 1);
+            mbar_init(&S.flags[s], kSharedConv);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&S.s_full[s], 1);
@@ -428,46 +429,62 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                     scale = __ldg(p.c.scales + (((int64_t)block * 2 + lane / 4) * p.c.KVH + s.h) * kKv8PageBlocks + lane % 4);
                 uint32_t nan = 0;
                 auto store = [&](uint32_t src, uint32_t slot, bool value) {
-#pragma unroll 2
-                    for (int i = 0; i < LOADS; ++i) {
-                        const int piece = ct + 32 * kSharedConv * i, row = piece / CHUNKS, d = piece % CHUNKS;  // dims 16 d ..
-                        uint32_t r[4], h[8];
-                        load_codes<4>(src + 16 * piece, r);
-                        if (cut && (block < 0 || p0 + row < s.lo || p0 + row >= s.hi)) r[0] = r[1] = r[2] = r[3] = 0;
-                        if (FMT == SARA_KV8_E4M3 && value) {  // codes 0x7f and 0xff: their block reads as NaN, and 0 times them must not
-                            uint32_t any = 0;
+                    constexpr int BATCH = LOADS < 4 ? LOADS : 4;
+#pragma unroll 1
+                    for (int i0 = 0; i0 < LOADS; i0 += BATCH) {
+                        uint32_t r[BATCH][4];
+                        int row[BATCH], d[BATCH];  // dims 16 d ..
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) any |= ((r[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-                            if (any) {
-                                nan |= 1u << (row / kKv8Block);
-                                r[0] = r[1] = r[2] = r[3] = 0;
+                        for (int i = 0; i < BATCH; ++i) {
+                            const int piece = ct + 32 * kSharedConv * (i0 + i);
+                            if constexpr (HD == 128) {  // (8 lanes: two rows' pieces of different halves, whose places meet all banks)
+                                row[i] = piece / 16 * 2 + (piece / 4 & 1);
+                                d[i] = (piece & 3) + 4 * ((piece / 4 ^ piece / 8) & 1);
+                            } else {
+                                row[i] = piece / CHUNKS;
+                                d[i] = piece % CHUNKS;
                             }
+                            load_codes<4>(src + row[i] * HD + 16 * d[i], r[i]);
                         }
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) decode4_half<FMT>(r[e], h[2 * e], h[2 * e + 1]);
-                        const uint32_t at = slot + (d / 4) * (kSharedQ * 128) + row * 128, c0 = d % 4 * 2;
-                        // (the second 64 dims' pieces the other way round, so that lanes of a row meet all banks)
-                        const bool turn = d >= 4;
-                        const uint32_t a0 = at + (((c0 + turn) ^ (row & 7)) << 4), a1 = at + (((c0 + !turn) ^ (row & 7)) << 4);
-                        st_shared_v4(a0, turn ? h[4] : h[0], turn ? h[5] : h[1], turn ? h[6] : h[2], turn ? h[7] : h[3]);
-                        st_shared_v4(a1, turn ? h[0] : h[4], turn ? h[1] : h[5], turn ? h[2] : h[6], turn ? h[3] : h[7]);
+                        for (int i = 0; i < BATCH; ++i) {
+                            uint32_t h[8];
+                            if (cut && (block < 0 || p0 + row[i] < s.lo || p0 + row[i] >= s.hi)) r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
+                            if (FMT == SARA_KV8_E4M3 && value) {  // codes 0x7f and 0xff: their block reads as NaN, and 0 times them must not
+                                uint32_t any = 0;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) any |= (r[i][e] & 0x7f7f7f7fu) + 0x01010101u;
+                                if (any & 0x80808080u) {
+                                    nan |= 1u << (row[i] / kKv8Block);
+                                    r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
+                                }
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) decode4_half<FMT>(r[i][e], h[2 * e], h[2 * e + 1]);
+                            const uint32_t at = slot + (d[i] / 4) * (kSharedQ * 128) + row[i] * 128, place = (d[i] % 4 * 2) ^ (row[i] & 7);
+                            st_shared_v4(at + (place << 4), h[0], h[1], h[2], h[3]);
+                            st_shared_v4(at + ((place ^ 1) << 4), h[4], h[5], h[6], h[7]);
+                        }
                     }
                 };
                 if (j >= 2) wait(&S.empty[sk], before);
                 if (!ok) break;
                 store(raw + st * RAW, ring + sk * TILE, false);
+                // (place j & 3: read when page j - 2's product was asked for)
+                if (cw == 0 && lane < 8) S.scale[j & 3][lane] = scale;
                 give(&S.full[sk]);
+                if (cw == 0 && lane == 0) mbar_arrive(&S.scales[j & 3]);
                 if (j >= 2) wait(&S.empty[sv], before);
                 if (!ok) break;
                 store(raw + st * RAW + RAW / 2, ring + sv * TILE, true);
-                // (place j & 3: read when page j - 2's product was asked for)
-                if (cw == 0 && lane < 8) S.scale[j & 3][lane] = scale;
-                if constexpr (FMT == SARA_KV8_E4M3) nan = __reduce_or_sync(0xffffffffu, nan);
-                if (lane == 0) S.nan[j & 3][cw] = nan;
+                if constexpr (FMT == SARA_KV8_E4M3) {
+                    nan = __reduce_or_sync(0xffffffffu, nan);
+                    if (lane == 0) S.nan[j & 3][cw] = nan;
+                }
                 give(&S.full[sv]);
                 if (lane == 0) {
                     mbar_arrive(&S.raw_empty[st]);
-                    mbar_arrive(&S.scales[j & 3]);
+                    if (FMT == SARA_KV8_E4M3) mbar_arrive(&S.flags[j & 3]);
                 }
             }
         }
@@ -583,28 +600,25 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
 #pragma unroll 1
             for (int x = 0; x < s.count; ++x) {
                 const uint32_t j = j0 + x, s_at = lanes + (j & 1) * 128 + half * 64;
-                wait(&S.s_full[j & 1], j >> 1);
                 wait(&S.scales[j & 3], j >> 2);
+                wait(&S.s_full[j & 1], j >> 1);
                 if (any) {
                     tc_fence_after();
                     float v[64], ks[2], F[2], ev[2];
                     tmem_load64(s_at, v);
-                    uint32_t bad = 0;
-                    if constexpr (FMT == SARA_KV8_E4M3) {
-                        static_assert(kSharedConv == 4 && offsetof(SharedSmem, nan) % 16 == 0, "a word a warp, read at once");
-                        const uint4 b = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][0]);
-                        bad = (b.x | b.y | b.z | b.w) >> (2 * half);
-                    }
                     const int p0 = (s.page + x) * kKv8Page + 64 * half;
+                    // a block that reads as NaN makes the sums of those that attend to it NaN, and leaves the others alone
+                    auto poison = [&](int b) {
+                        if (lo < p0 + 32 * b + 32 && hi > p0 + 32 * b) l = __int_as_float(0x7fc00000);
+                        F[b] = 0.f;
+                    };
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         ks[b] = S.scale[j & 3][2 * half + b] * mul;
                         F[b] = S.scale[j & 3][4 + 2 * half + b];
-                        // a block that reads as NaN makes the sums of those that attend to it NaN, and leaves the others alone
-                        if ((bad >> b & 1) || !(fabsf(ks[b]) < INFINITY && fabsf(F[b]) < INFINITY)) {
-                            if (lo < p0 + 32 * b + 32 && hi > p0 + 32 * b) l = __int_as_float(0x7fc00000);
+                        if (!(fabsf(ks[b]) < INFINITY && fabsf(F[b]) < INFINITY)) {
+                            poison(b);
                             ks[b] = 1.f;
-                            F[b] = 0.f;
                         }
                         ev[b] = (float)min(max(scale_exp(F[b]), -126), 126);
                         F[b] *= pow2f(-(int)ev[b]);
@@ -647,6 +661,16 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                                 for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(o[e] * f);
                                 tmem_st_x16(o_at + d, y);
                             }
+                        }
+                    }
+                    if constexpr (FMT == SARA_KV8_E4M3) {
+                        wait(&S.flags[j & 3], j >> 2);
+                        static_assert(kSharedConv == 4 && offsetof(SharedSmem, nan) % 16 == 0, "a word a warp, read at once");
+                        const uint4 b = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][0]);
+                        const uint32_t bad = (b.x | b.y | b.z | b.w) >> (2 * half);
+                        if (bad & 3) {
+                            if (bad & 1) poison(0);
+                            if (bad & 2) poison(1);
                         }
                     }
                     uint64_t l2 = 0;  // two sums
