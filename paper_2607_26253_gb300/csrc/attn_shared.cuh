@@ -6,7 +6,7 @@
 // Prefix kernel: a unit is (group, KV head, 128 queries: rows times heads); its positions go by in pages of 128, and the pages of all
 // units are cut into equal shares, one a CTA.  Four kinds of warps in a row:
 //   - one brings a page's codes by bulk copies, two pages ahead;
-//   - 4 turn them into fp16 (which holds both formats exactly) in shared memory, swizzled as the tensor core reads them: the same image
+//   - 3 and 3 turn keys and values into fp16 (which holds both formats exactly) in shared memory, swizzled as the tensor core reads them: the same image
 //     is K-major for the scores and N-major for the values;
 //   - one issues S = Q K^T (128 queries x 128 positions) and O += P V, both tcgen05, Q and P from tensor memory; the next page's scores are
 //     made while this one's softmax goes on;
@@ -22,8 +22,8 @@
 namespace sara {
 
 constexpr int kSharedQ = 128;                       // queries of a unit
-constexpr int kSharedSoft = 8, kSharedConv = 4;     // warps of the softmax; that make fp16
-constexpr int kSharedThreads = 32 * (kSharedSoft + kSharedConv + 2);
+constexpr int kSharedSoft = 8, kSharedConv = 3;     // warps of the softmax; that make fp16 of keys, and of values
+constexpr int kSharedThreads = 32 * (kSharedSoft + 2 * kSharedConv + 2);
 constexpr int kSharedSlots = 4;                     // K and V of two pages
 __host__ __device__ constexpr int shared_tile(int hd) { return kSharedQ * 128 * ((hd + 63) / 64); }  // bytes of 128 rows in blocks of 64 dims
 __host__ __device__ constexpr int shared_raw(int hd) { return 2 * kKv8Page * hd; }                   // of a page's codes
@@ -213,12 +213,11 @@ struct SharedWalk {
 struct SharedSmem {
     uint64_t raw_full[4], raw_empty[4], full[kSharedSlots], empty[kSharedSlots], scales[4], flags[4], q_full, s_full[2], p_full[2], pv_done, o_full;
     float scale[4][8];             // of a page: K's four, V's four
-    alignas(16) uint32_t nan[4][kSharedConv];  // blocks of a page in which a warp met a NaN among V's codes (read 16 bytes at a time)
+    alignas(16) uint32_t nan[4][4];  // blocks of a page in which a warp met a NaN among V's codes (read 16 bytes at a time)
     float2 top[2][2][kSharedQ];    // a query's largest score and product, of either half of a page, two pages in turn
     float sum[kSharedQ];           // of the second half's probabilities
     int block[4];                  // of a page of codes
     uint32_t tmem_base;
-    int abort;
 };
 
 __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -320,7 +319,8 @@ __device__ __forceinline__ void st_shared_v4(uint32_t at, uint32_t a, uint32_t b
 template <int HD, int FMT>
 __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(SharedParams p) {
     constexpr int TILE = shared_tile(HD), RAW = shared_raw(HD), RAWS = shared_raws(HD);
-    constexpr int CHUNKS = HD / 16, LOADS = kKv8Page * CHUNKS / (32 * kSharedConv);  // 16-byte pieces of a row, of a thread
+    constexpr int CHUNKS = HD / 16, PIECES = kKv8Page * CHUNKS;  // 16-byte pieces of a row, of a tile
+    constexpr int BATCH = HD == 128 ? 4 : 3, LOADS = (PIECES + 32 * kSharedConv * BATCH - 1) / (32 * kSharedConv * BATCH) * BATCH;  // of a thread
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(16) SharedSmem S;
     const uint32_t ring = (smem_u32(smem_raw) + 1023) & ~1023u, raw = ring + kSharedSlots * TILE;
@@ -330,7 +330,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
     if (threadIdx.x == 0) {
         for (int s = 0; s < 4; ++s) {
             mbar_init(&S.raw_full[s], 1);
-            mbar_init(&S.raw_empty[s], kSharedConv);
+            mbar_init(&S.raw_empty[s], 2 * kSharedConv);
             mbar_init(&S.full[s], kSharedConv);
             mbar_init(&S.empty[s], 1);
             mbar_init(&S.scales[s], 1);
@@ -343,10 +343,9 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         mbar_init(&S.q_full, kSharedSoft);
         mbar_init(&S.pv_done, 1);
         mbar_init(&S.o_full, 1);
-        S.abort = 0;
         fence_mbar_init();
     }
-    constexpr int MMA_WARP = kSharedSoft + kSharedConv, LOAD_WARP = MMA_WARP + 1;
+    constexpr int MMA_WARP = kSharedSoft + 2 * kSharedConv, LOAD_WARP = MMA_WARP + 1;
     if (warp == MMA_WARP) {
         tmem_alloc(&S.tmem_base, 512);
         tmem_relinquish();
@@ -356,11 +355,10 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
     tc_fence_after();
     pdl_wait_prior_grids();
     const uint32_t tmem = S.tmem_base;
-    volatile int *ab = &S.abort;
     const SharedShares shares(p.plan->entries, min((int)gridDim.x, p.max_shares));
     const int c = blockIdx.x, from = c < shares.n ? shares.begin(c) : 0, to = c < shares.n ? shares.begin(c + 1) : 0;
     bool ok = true;
-    auto wait = [&](uint64_t *bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity & 1, err) && !*ab); };
+    auto wait = [&](uint64_t *bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity & 1, err)); };
 
     if (from >= to) {
     } else if (warp == LOAD_WARP) {
@@ -401,94 +399,83 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 __syncwarp();
             }
         }
-        if (!ok) *ab = 1;
         // every copy lands before the CTA ends
         for (uint32_t q = 0; q < RAWS && q < j; ++q) mbar_wait(&S.raw_full[(j - 1 - q) % RAWS], ((j - 1 - q) / RAWS) & 1, err);
         if (wrong) kv8_report(p.status);
     } else if (warp >= kSharedSoft && warp < MMA_WARP) {
         // ------------------------------------------------------------ codes to fp16
-        const int cw = warp - kSharedSoft, ct = cw * 32 + lane;
+        const int cw = (warp - kSharedSoft) % kSharedConv, ct = cw * 32 + lane;
+        const bool value = warp >= kSharedSoft + kSharedConv;
         SharedWalk w(p, from, to);
         SharedSegment s;
         uint32_t j = 0;
-        auto give = [&](uint64_t *bar) {
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar);
-        };
         while (ok && w.next(s)) {
 #pragma unroll 1
             for (int x = 0; x < s.count && ok; ++x, ++j) {
-                const uint32_t st = j % RAWS, sk = 2 * (j & 1), sv = sk + 1, before = (j >> 1) - 1;
+                const uint32_t st = j % RAWS, at = 2 * (j & 1) + value;
                 wait(&S.raw_full[st], j / RAWS);
                 if (!ok) break;
                 const int block = S.block[st], p0 = (s.page + x) * kKv8Page;
                 const bool cut = block < 0 || p0 < s.lo || p0 + kKv8Page > s.hi;  // positions that nobody attends to are 0: what they hold does not matter
                 float scale = __int_as_float(0x7fc00000);
-                if (cw == 0 && lane < 8 && block >= 0)
+                if (!value && cw == 0 && lane < 8 && block >= 0)
                     scale = __ldg(p.c.scales + (((int64_t)block * 2 + lane / 4) * p.c.KVH + s.h) * kKv8PageBlocks + lane % 4);
+                if (j >= 2) wait(&S.empty[at], (j >> 1) - 1);
+                if (!ok) break;
+                const uint32_t src = raw + st * RAW + (value ? RAW / 2 : 0), slot = ring + at * TILE;
                 uint32_t nan = 0;
-                auto store = [&](uint32_t src, uint32_t slot, bool value) {
-                    constexpr int BATCH = LOADS < 4 ? LOADS : 4;
 #pragma unroll 1
-                    for (int i0 = 0; i0 < LOADS; i0 += BATCH) {
-                        uint32_t r[BATCH][4];
-                        int row[BATCH], d[BATCH];  // dims 16 d ..
+                for (int i0 = 0; i0 < LOADS; i0 += BATCH) {
+                    uint32_t r[BATCH][4];
+                    int row[BATCH], d[BATCH];  // dims 16 d ..
 #pragma unroll
-                        for (int i = 0; i < BATCH; ++i) {
-                            const int piece = ct + 32 * kSharedConv * (i0 + i);
-                            if constexpr (HD == 128) {  // (8 lanes: two rows' pieces of different halves, whose places meet all banks)
-                                row[i] = piece / 16 * 2 + (piece / 4 & 1);
-                                d[i] = (piece & 3) + 4 * ((piece / 4 ^ piece / 8) & 1);
-                            } else {
-                                row[i] = piece / CHUNKS;
-                                d[i] = piece % CHUNKS;
-                            }
-                            load_codes<4>(src + row[i] * HD + 16 * d[i], r[i]);
+                    for (int i = 0; i < BATCH; ++i) {
+                        const int piece = min(ct + 32 * kSharedConv * (i0 + i), PIECES - 8 + lane % 8);  // (the last ones again: the same values)
+                        if constexpr (HD == 128) {  // (8 lanes: two rows' pieces of different halves, whose places meet all banks)
+                            row[i] = piece / 16 * 2 + (piece / 4 & 1);
+                            d[i] = (piece & 3) + 4 * ((piece / 4 ^ piece / 8) & 1);
+                        } else {
+                            row[i] = piece / CHUNKS;
+                            d[i] = piece % CHUNKS;
                         }
-#pragma unroll
-                        for (int i = 0; i < BATCH; ++i) {
-                            uint32_t h[8];
-                            if (cut && (block < 0 || p0 + row[i] < s.lo || p0 + row[i] >= s.hi)) r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
-                            if (FMT == SARA_KV8_E4M3 && value) {  // codes 0x7f and 0xff: their block reads as NaN, and 0 times them must not
-                                uint32_t any = 0;
-#pragma unroll
-                                for (int e = 0; e < 4; ++e) any |= (r[i][e] & 0x7f7f7f7fu) + 0x01010101u;
-                                if (any & 0x80808080u) {
-                                    nan |= 1u << (row[i] / kKv8Block);
-                                    r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
-                                }
-                            }
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) decode4_half<FMT>(r[i][e], h[2 * e], h[2 * e + 1]);
-                            const uint32_t at = slot + (d[i] / 4) * (kSharedQ * 128) + row[i] * 128, place = (d[i] % 4 * 2) ^ (row[i] & 7);
-                            st_shared_v4(at + (place << 4), h[0], h[1], h[2], h[3]);
-                            st_shared_v4(at + ((place ^ 1) << 4), h[4], h[5], h[6], h[7]);
-                        }
+                        load_codes<4>(src + row[i] * HD + 16 * d[i], r[i]);
                     }
-                };
-                if (j >= 2) wait(&S.empty[sk], before);
-                if (!ok) break;
-                store(raw + st * RAW, ring + sk * TILE, false);
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i) {
+                        uint32_t h[8];
+                        if (cut && (block < 0 || p0 + row[i] < s.lo || p0 + row[i] >= s.hi)) r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
+                        if (FMT == SARA_KV8_E4M3 && value) {  // codes 0x7f and 0xff: their block reads as NaN, and 0 times them must not
+                            uint32_t any = 0;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) any |= (r[i][e] & 0x7f7f7f7fu) + 0x01010101u;
+                            if (any & 0x80808080u) {
+                                nan |= 1u << (row[i] / kKv8Block);
+                                r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
+                            }
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) decode4_half<FMT>(r[i][e], h[2 * e], h[2 * e + 1]);
+                        const uint32_t to = slot + (d[i] / 4) * (kSharedQ * 128) + row[i] * 128, place = (d[i] % 4 * 2) ^ (row[i] & 7);
+                        st_shared_v4(to + (place << 4), h[0], h[1], h[2], h[3]);
+                        st_shared_v4(to + ((place ^ 1) << 4), h[4], h[5], h[6], h[7]);
+                    }
+                }
                 // (place j & 3: read when page j - 2's product was asked for)
-                if (cw == 0 && lane < 8) S.scale[j & 3][lane] = scale;
-                give(&S.full[sk]);
-                if (cw == 0 && lane == 0) mbar_arrive(&S.scales[j & 3]);
-                if (j >= 2) wait(&S.empty[sv], before);
-                if (!ok) break;
-                store(raw + st * RAW + RAW / 2, ring + sv * TILE, true);
-                if constexpr (FMT == SARA_KV8_E4M3) {
+                if (!value && cw == 0 && lane < 8) S.scale[j & 3][lane] = scale;
+                if (FMT == SARA_KV8_E4M3 && value) {
                     nan = __reduce_or_sync(0xffffffffu, nan);
                     if (lane == 0) S.nan[j & 3][cw] = nan;
                 }
-                give(&S.full[sv]);
+                fence_proxy_async_smem();
+                __syncwarp();
                 if (lane == 0) {
+                    mbar_arrive(&S.full[at]);
                     mbar_arrive(&S.raw_empty[st]);
-                    if (FMT == SARA_KV8_E4M3) mbar_arrive(&S.flags[j & 3]);
+                    if (!value && cw == 0) mbar_arrive(&S.scales[j & 3]);
+                    if (FMT == SARA_KV8_E4M3 && value) mbar_arrive(&S.flags[j & 3]);
                 }
             }
         }
-        if (!ok) *ab = 1;
     } else if (warp == MMA_WARP) {
         // ------------------------------------------------------------ MMAs
         constexpr uint32_t idesc_s = 1u << 4 | (128u >> 3) << 17 | (128u >> 4) << 24;
@@ -538,7 +525,6 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
             }
             j0 += s.count;
         }
-        if (!ok) *ab = 1;
         if (done > 0) mbar_wait(&S.pv_done, (done - 1) & 1, err);  // every MMA has retired before tensor memory is released
     } else if (warp < kSharedSoft) {
         // ------------------------------------------------------------ softmax: a query's first or second 64 positions a thread
@@ -665,9 +651,9 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                     }
                     if constexpr (FMT == SARA_KV8_E4M3) {
                         wait(&S.flags[j & 3], j >> 2);
-                        static_assert(kSharedConv == 4 && offsetof(SharedSmem, nan) % 16 == 0, "a word a warp, read at once");
+                        static_assert(kSharedConv == 3 && offsetof(SharedSmem, nan) % 16 == 0, "a word a warp, read at once");
                         const uint4 b = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][0]);
-                        const uint32_t bad = (b.x | b.y | b.z | b.w) >> (2 * half);
+                        const uint32_t bad = (b.x | b.y | b.z) >> (2 * half);
                         if (bad & 3) {
                             if (bad & 1) poison(0);
                             if (bad & 2) poison(1);
@@ -721,7 +707,6 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
             tc_fence_before();
             j0 += s.count;
         }
-        if (!ok) *ab = 1;
     }
     __syncwarp();
     tc_fence_before();
