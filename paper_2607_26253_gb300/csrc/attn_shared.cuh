@@ -5,7 +5,7 @@
 //
 // Prefix kernel: a unit is (group, KV head, 128 queries: rows times heads); its positions go by in pages of 128, and the pages of all
 // units are cut into equal shares, one a CTA.  Four kinds of warps in a row:
-//   - one brings a page's codes by bulk copies, two pages ahead;
+//   - one brings a page's codes by bulk copies, two or three pages ahead;
 //   - 3 and 3 turn keys and values into fp16 (which holds both formats exactly) in shared memory, swizzled as the tensor core reads them: the same image
 //     is K-major for the scores and N-major for the values;
 //   - one issues S = Q K^T (128 queries x 128 positions) and O += P V, both tcgen05, Q and P from tensor memory; the next page's scores are
@@ -26,9 +26,11 @@ constexpr int kSharedSoft = 8, kSharedConv = 3;     // warps of the softmax; tha
 constexpr int kSharedThreads = 32 * (kSharedSoft + 2 * kSharedConv + 2);
 constexpr int kSharedSlots = 4;                     // K and V of two pages
 __host__ __device__ constexpr int shared_tile(int hd) { return kSharedQ * 128 * ((hd + 63) / 64); }  // bytes of 128 rows in blocks of 64 dims
-__host__ __device__ constexpr int shared_raw(int hd) { return 2 * kKv8Page * hd; }                   // of a page's codes
-__host__ __device__ constexpr int shared_raws(int hd) { return hd == 128 ? 2 : 4; }                  // pages of codes
-__host__ __device__ constexpr int shared_smem(int hd) { return 1024 + kSharedSlots * shared_tile(hd) + shared_raws(hd) * shared_raw(hd); }
+__host__ __device__ constexpr int shared_raw(int hd) { return kKv8Page * hd; }                       // of a page's keys or values in codes
+__host__ __device__ constexpr int shared_raws(int hd, int v) { return hd == 128 ? 3 - v : 4; }       // of those: keys, values
+__host__ __device__ constexpr int shared_smem(int hd) {
+    return 1024 + kSharedSlots * shared_tile(hd) + (shared_raws(hd, 0) + shared_raws(hd, 1)) * shared_raw(hd);
+}
 constexpr float kSharedShift = 6.f;                 // log2 of the products' scale
 constexpr int kSharedMaxShares = 160;               // CTAs, one an SM
 constexpr int kSharedWideJoin = 1216;               // queries up to which 8 warps join a query
@@ -211,12 +213,13 @@ struct SharedWalk {
 
 // ------------------------------------------------------------------------------- prefix
 struct SharedSmem {
-    uint64_t raw_full[4], raw_empty[4], full[kSharedSlots], empty[kSharedSlots], scales[4], flags[4], q_full, s_full[2], p_full[2], pv_done, o_full;
+    uint64_t raw_full[2][4], raw_empty[2][4], full[kSharedSlots], empty[kSharedSlots], q_full, s_full[2], p_full[2], pv_done, o_full;
     float scale[4][8];             // of a page: K's four, V's four
+    float raw_scale[4][8];         // the same, as they come with the keys
     alignas(16) uint32_t nan[4][4];  // blocks of a page in which a warp met a NaN among V's codes (read 16 bytes at a time)
-    float2 top[2][2][kSharedQ];    // a query's largest score and product, of either half of a page, two pages in turn
+    float2 top[2][kSharedQ];       // a query's largest score and product, of either half of a page
     float sum[kSharedQ];           // of the second half's probabilities
-    int block[4];                  // of a page of codes
+    int block[2][4];               // of a page of codes
     uint32_t tmem_base;
 };
 
@@ -277,15 +280,31 @@ __device__ __forceinline__ void tmem_store32(uint32_t taddr, const uint32_t (&r)
           "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
         : "memory");
 }
+// Arrive on `bar` when this thread's asynchronous copies so far have come (none: at once)
+__device__ __forceinline__ void cp_async_arrive(uint64_t *bar) {
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
 // (bulk_load to a shared-memory address)
-__device__ __forceinline__ void bulk_load_at(uint32_t dst, const void *src, uint32_t bytes, uint64_t *bar, uint64_t policy) {
-    asm volatile(
-        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst), "l"(src),
-        "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
-        : "memory");
+__device__ __forceinline__ void bulk_load_at(uint32_t dst, const void *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
+                 "r"(smem_u32(bar))
+                 : "memory");
 }
 __device__ __forceinline__ uint64_t sdesc_128(uint32_t addr, uint32_t lbo) {  // 128-byte swizzle, 8 rows after 1,024 bytes
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// Whether any of the barrier's threads says so
+__device__ __forceinline__ bool named_bar_or(int id, int nthreads, bool x) {
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.pred q, %2, %3, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)x), "r"(id), "r"(nthreads)
+        : "memory");
+    return r != 0;
 }
 __device__ __forceinline__ float max3(float a, float b, float c) {  // a NaN gives way
     float y;
@@ -318,9 +337,9 @@ __device__ __forceinline__ void st_shared_v4(uint32_t at, uint32_t a, uint32_t b
 
 template <int HD, int FMT>
 __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(SharedParams p) {
-    constexpr int TILE = shared_tile(HD), RAW = shared_raw(HD), RAWS = shared_raws(HD);
-    constexpr int CHUNKS = HD / 16, PIECES = kKv8Page * CHUNKS;  // 16-byte pieces of a row, of a tile
-    constexpr int BATCH = HD == 128 ? 4 : 3, LOADS = (PIECES + 32 * kSharedConv * BATCH - 1) / (32 * kSharedConv * BATCH) * BATCH;  // of a thread
+    constexpr int TILE = shared_tile(HD), RAW = shared_raw(HD), RAWS[2] = {shared_raws(HD, 0), shared_raws(HD, 1)};
+    constexpr int CHUNKS = HD / 16, STEP = 32 * kSharedConv / CHUNKS;  // 16-byte pieces of a row; rows that the warps of a tile cover at a time
+    constexpr int LOADS = (kKv8Page + STEP - 1) / STEP, BATCH = 4;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(16) SharedSmem S;
     const uint32_t ring = (smem_u32(smem_raw) + 1023) & ~1023u, raw = ring + kSharedSlots * TILE;
@@ -329,12 +348,12 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
     int *err = &p.plan->err;
     if (threadIdx.x == 0) {
         for (int s = 0; s < 4; ++s) {
-            mbar_init(&S.raw_full[s], 1);
-            mbar_init(&S.raw_empty[s], 2 * kSharedConv);
+            for (int v = 0; v < 2; ++v) {
+                mbar_init(&S.raw_full[v][s], v ? 1 : 9);  // (keys come with eight scales)
+                mbar_init(&S.raw_empty[v][s], kSharedConv);
+            }
             mbar_init(&S.full[s], kSharedConv);
             mbar_init(&S.empty[s], 1);
-            mbar_init(&S.scales[s], 1);
-            mbar_init(&S.flags[s], kSharedConv);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(&S.s_full[s], 1);
@@ -365,7 +384,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         // ------------------------------------------------------------ codes
         SharedWalk w(p, from, to);
         SharedSegment s;
-        uint32_t j = 0;  // pages
+        uint32_t j = 0, got[2] = {};  // pages, of which copies are under way
         bool wrong = false;
         while (ok && w.next(s)) {
             int ids = 0, idbase = -64;
@@ -381,87 +400,94 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                     }
                 }
                 const int block = __shfl_sync(0xffffffffu, ids, page - idbase);
-                const uint32_t st = j % RAWS;
-                if (j >= RAWS) wait(&S.raw_empty[st], j / RAWS - 1);
-                if (!ok) break;
-                if (lane == 0) {
-                    S.block[st] = block;
-                    if (block >= 0) {
-                        const uint8_t *k = p.c.codes + kv8_tile(p.c, block, 0, s.h) * (kKv8Page * HD);
-                        const uint64_t policy = l2_policy_evict_first();
-                        mbar_arrive_expect_tx(&S.raw_full[st], RAW);
-                        bulk_load_at(raw + st * RAW, k, RAW / 2, &S.raw_full[st], policy);
-                        bulk_load_at(raw + st * RAW + RAW / 2, k + (int64_t)p.c.KVH * (kKv8Page * HD), RAW / 2, &S.raw_full[st], policy);
-                    } else {
-                        mbar_arrive(&S.raw_full[st]);
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    const uint32_t st = j % RAWS[v];
+                    if (j >= (uint32_t)RAWS[v]) wait(&S.raw_empty[v][st], j / RAWS[v] - 1);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        S.block[v][st] = block;
+                        if (block >= 0) {
+                            mbar_arrive_expect_tx(&S.raw_full[v][st], RAW);
+                            bulk_load_at(raw + (v * RAWS[0] + st) * RAW, p.c.codes + kv8_tile(p.c, block, v, s.h) * (kKv8Page * HD), RAW, &S.raw_full[v][st]);
+                        } else {
+                            mbar_arrive(&S.raw_full[v][st]);
+                        }
                     }
+                    if (v == 0 && lane < 8) {
+                        if (block >= 0)
+                            cp_async4(smem_u32(&S.raw_scale[st][lane]),
+                                      p.c.scales + (((int64_t)block * 2 + lane / 4) * p.c.KVH + s.h) * kKv8PageBlocks + lane % 4);
+                        cp_async_arrive(&S.raw_full[0][st]);
+                    }
+                    __syncwarp();
+                    ++got[v];
                 }
-                __syncwarp();
             }
         }
         // every copy lands before the CTA ends
-        for (uint32_t q = 0; q < RAWS && q < j; ++q) mbar_wait(&S.raw_full[(j - 1 - q) % RAWS], ((j - 1 - q) / RAWS) & 1, err);
+        for (int v = 0; v < 2; ++v)
+            for (uint32_t q = 1; q <= (uint32_t)RAWS[v] && q <= got[v]; ++q) mbar_wait(&S.raw_full[v][(got[v] - q) % RAWS[v]], ((got[v] - q) / RAWS[v]) & 1, err);
         if (wrong) kv8_report(p.status);
     } else if (warp >= kSharedSoft && warp < MMA_WARP) {
         // ------------------------------------------------------------ codes to fp16
         const int cw = (warp - kSharedSoft) % kSharedConv, ct = cw * 32 + lane;
         const bool value = warp >= kSharedSoft + kSharedConv;
+        const uint32_t raws = value ? RAWS[1] : RAWS[0];
+        // this thread's row and 16 dims of the first STEP rows (128 dims: 8 lanes have pieces of different halves of two rows, whose places meet
+        // all banks)
+        const int row = HD == 128 ? ct / 16 * 2 + (ct / 4 & 1) : ct / CHUNKS, d = HD == 128 ? (ct & 3) + 4 * ((ct / 4 ^ ct / 8) & 1) : ct % CHUNKS;
         SharedWalk w(p, from, to);
         SharedSegment s;
         uint32_t j = 0;
         while (ok && w.next(s)) {
 #pragma unroll 1
             for (int x = 0; x < s.count && ok; ++x, ++j) {
-                const uint32_t st = j % RAWS, at = 2 * (j & 1) + value;
-                wait(&S.raw_full[st], j / RAWS);
+                const uint32_t st = j % raws, at = 2 * (j & 1) + value;
+                wait(&S.raw_full[value][st], j / raws);
                 if (!ok) break;
-                const int block = S.block[st], p0 = (s.page + x) * kKv8Page;
+                const int block = S.block[value][st], p0 = (s.page + x) * kKv8Page;
                 const bool cut = block < 0 || p0 < s.lo || p0 + kKv8Page > s.hi;  // positions that nobody attends to are 0: what they hold does not matter
-                float scale = __int_as_float(0x7fc00000);
-                if (!value && cw == 0 && lane < 8 && block >= 0)
-                    scale = __ldg(p.c.scales + (((int64_t)block * 2 + lane / 4) * p.c.KVH + s.h) * kKv8PageBlocks + lane % 4);
                 if (j >= 2) wait(&S.empty[at], (j >> 1) - 1);
                 if (!ok) break;
-                const uint32_t src = raw + st * RAW + (value ? RAW / 2 : 0), slot = ring + at * TILE;
+                const uint32_t src = raw + ((value ? RAWS[0] : 0) + st) * RAW + row * HD + 16 * d, slot = ring + at * TILE;
+                // the places of dims 16 d .. in the row, as the tensor core reads it; STEP rows on they are the same ones or change sides
+                const uint32_t to = slot + (d / 4) * (kSharedQ * 128) + row * 128, place = ((d % 4 * 2) ^ (row & 7)) << 4;
+                const uint32_t even[2] = {to + place, to + (place ^ 16)}, odd[2] = {to + (place ^ (STEP % 8 * 16)), to + (place ^ (STEP % 8 * 16) ^ 16)};
+                static_assert(STEP % 8 == 0 || STEP % 8 == 4, "an exclusive or is then the sum");
                 uint32_t nan = 0;
-#pragma unroll 1
+#pragma unroll
                 for (int i0 = 0; i0 < LOADS; i0 += BATCH) {
                     uint32_t r[BATCH][4];
-                    int row[BATCH], d[BATCH];  // dims 16 d ..
+#pragma unroll
+                    for (int i = 0; i < BATCH; ++i)
+                        if (i0 + i < LOADS && ((i0 + i + 1) * STEP <= kKv8Page || row + (i0 + i) * STEP < kKv8Page)) load_codes<4>(src + (i0 + i) * STEP * HD, r[i]);
 #pragma unroll
                     for (int i = 0; i < BATCH; ++i) {
-                        const int piece = min(ct + 32 * kSharedConv * (i0 + i), PIECES - 8 + lane % 8);  // (the last ones again: the same values)
-                        if constexpr (HD == 128) {  // (8 lanes: two rows' pieces of different halves, whose places meet all banks)
-                            row[i] = piece / 16 * 2 + (piece / 4 & 1);
-                            d[i] = (piece & 3) + 4 * ((piece / 4 ^ piece / 8) & 1);
-                        } else {
-                            row[i] = piece / CHUNKS;
-                            d[i] = piece % CHUNKS;
-                        }
-                        load_codes<4>(src + row[i] * HD + 16 * d[i], r[i]);
-                    }
-#pragma unroll
-                    for (int i = 0; i < BATCH; ++i) {
+                        const int x = i0 + i, at_row = row + x * STEP;
+                        if (x >= LOADS || !((x + 1) * STEP <= kKv8Page || at_row < kKv8Page)) continue;
                         uint32_t h[8];
-                        if (cut && (block < 0 || p0 + row[i] < s.lo || p0 + row[i] >= s.hi)) r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
+                        if (cut) {
+                            if (block < 0 || p0 + at_row < s.lo || p0 + at_row >= s.hi) r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
+                        }
                         if (FMT == SARA_KV8_E4M3 && value) {  // codes 0x7f and 0xff: their block reads as NaN, and 0 times them must not
                             uint32_t any = 0;
 #pragma unroll
                             for (int e = 0; e < 4; ++e) any |= (r[i][e] & 0x7f7f7f7fu) + 0x01010101u;
                             if (any & 0x80808080u) {
-                                nan |= 1u << (row[i] / kKv8Block);
+                                nan |= 1u << (at_row / kKv8Block);
                                 r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
                             }
                         }
 #pragma unroll
                         for (int e = 0; e < 4; ++e) decode4_half<FMT>(r[i][e], h[2 * e], h[2 * e + 1]);
-                        const uint32_t to = slot + (d[i] / 4) * (kSharedQ * 128) + row[i] * 128, place = (d[i] % 4 * 2) ^ (row[i] & 7);
-                        st_shared_v4(to + (place << 4), h[0], h[1], h[2], h[3]);
-                        st_shared_v4(to + ((place ^ 1) << 4), h[4], h[5], h[6], h[7]);
+                        const uint32_t(&o)[2] = x % 2 ? odd : even;
+                        st_shared_v4(o[0] + x * STEP * 128, h[0], h[1], h[2], h[3]);
+                        st_shared_v4(o[1] + x * STEP * 128, h[4], h[5], h[6], h[7]);
                     }
                 }
                 // (place j & 3: read when page j - 2's product was asked for)
-                if (!value && cw == 0 && lane < 8) S.scale[j & 3][lane] = scale;
+                if (!value && cw == 0 && lane < 8) S.scale[j & 3][lane] = block >= 0 ? S.raw_scale[st][lane] : __int_as_float(0x7fc00000);
                 if (FMT == SARA_KV8_E4M3 && value) {
                     nan = __reduce_or_sync(0xffffffffu, nan);
                     if (lane == 0) S.nan[j & 3][cw] = nan;
@@ -470,9 +496,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 __syncwarp();
                 if (lane == 0) {
                     mbar_arrive(&S.full[at]);
-                    mbar_arrive(&S.raw_empty[st]);
-                    if (!value && cw == 0) mbar_arrive(&S.scales[j & 3]);
-                    if (FMT == SARA_KV8_E4M3 && value) mbar_arrive(&S.flags[j & 3]);
+                    mbar_arrive(&S.raw_empty[value][st]);
                 }
             }
         }
@@ -583,28 +607,39 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
             if (lane == 0) mbar_arrive(&S.q_full);
 
             float m = -3.4028235e38f, R = m, l = 0.f;
+            // a block that reads as NaN (bit b: of this half's) makes the sums of those that attend to it NaN, and leaves the others alone
+            auto poison = [&](int page, uint32_t bad) {
+                const int p0 = page * kKv8Page + 64 * half;
+                if ((bad & 1) && lo < p0 + 32 && hi > p0) l = __int_as_float(0x7fc00000);
+                if ((bad & 2) && lo < p0 + 64 && hi > p0 + 32) l = __int_as_float(0x7fc00000);
+            };
+            // the flags of values that have gone into a product: page j's by the scores of page j + 2, the last two's by the end
+            auto flags = [&](uint32_t j, int page) {
+                if constexpr (FMT == SARA_KV8_E4M3) {
+                    static_assert(kSharedConv == 3 && offsetof(SharedSmem, nan) % 16 == 0, "a word a warp, read at once");
+                    const uint4 b = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][0]);
+                    const uint32_t bad = (b.x | b.y | b.z) >> (2 * half) & 3;
+                    if (bad) poison(page, bad);
+                }
+            };
 #pragma unroll 1
             for (int x = 0; x < s.count; ++x) {
                 const uint32_t j = j0 + x, s_at = lanes + (j & 1) * 128 + half * 64;
-                wait(&S.scales[j & 3], j >> 2);
-                wait(&S.s_full[j & 1], j >> 1);
+                wait(&S.s_full[j & 1], j >> 1);  // (the page's scales were there before its keys)
                 if (any) {
                     tc_fence_after();
                     float v[64], ks[2], F[2], ev[2];
                     tmem_load64(s_at, v);
+                    if (x >= 2) flags(j - 2, s.page + x - 2);
                     const int p0 = (s.page + x) * kKv8Page + 64 * half;
-                    // a block that reads as NaN makes the sums of those that attend to it NaN, and leaves the others alone
-                    auto poison = [&](int b) {
-                        if (lo < p0 + 32 * b + 32 && hi > p0 + 32 * b) l = __int_as_float(0x7fc00000);
-                        F[b] = 0.f;
-                    };
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         ks[b] = S.scale[j & 3][2 * half + b] * mul;
                         F[b] = S.scale[j & 3][4 + 2 * half + b];
                         if (!(fabsf(ks[b]) < INFINITY && fabsf(F[b]) < INFINITY)) {
-                            poison(b);
+                            poison(s.page + x, 1 << b);
                             ks[b] = 1.f;
+                            F[b] = 0.f;
                         }
                         ev[b] = (float)min(max(scale_exp(F[b]), -126), 126);
                         F[b] *= pow2f(-(int)ev[b]);
@@ -623,13 +658,13 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                         top.x = fmaxf(top.x, n);
                         top.y = fmaxf(top.y, n + ev[b]);
                     }
-                    S.top[j & 1][half][lrow] = top;
-                    named_bar_sync(1 + quarter, 64);  // (the next page has the other place)
-                    const float2 other = S.top[j & 1][half ^ 1][lrow];
-                    top.x = fmaxf(top.x, other.x);
-                    top.y = fmaxf(top.y, other.y);
-                    const bool raise = top.x > m + 8.f || top.y > R + 8.f;
-                    if (__any_sync(0xffffffffu, raise)) {
+                    if (named_bar_or(1 + quarter, 64, top.x > m + 8.f || top.y > R + 8.f)) {  // of either half: both raise the same
+                        S.top[half][lrow] = top;
+                        named_bar_sync(1 + quarter, 64);
+                        const float2 other = S.top[half ^ 1][lrow];
+                        top.x = fmaxf(top.x, other.x);
+                        top.y = fmaxf(top.y, other.y);
+                        const bool raise = top.x > m + 8.f || top.y > R + 8.f;
                         const float m1 = raise ? fmaxf(m, top.x) : m, R1 = raise ? fmaxf(R, top.y) : R;
                         l *= ex2(fmaxf(m - m1, -1e4f));
                         const float f = ex2(fmaxf(R - R1, -1e4f));
@@ -647,16 +682,6 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                                 for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(o[e] * f);
                                 tmem_st_x16(o_at + d, y);
                             }
-                        }
-                    }
-                    if constexpr (FMT == SARA_KV8_E4M3) {
-                        wait(&S.flags[j & 3], j >> 2);
-                        static_assert(kSharedConv == 3 && offsetof(SharedSmem, nan) % 16 == 0, "a word a warp, read at once");
-                        const uint4 b = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][0]);
-                        const uint32_t bad = (b.x | b.y | b.z) >> (2 * half);
-                        if (bad & 3) {
-                            if (bad & 1) poison(0);
-                            if (bad & 2) poison(1);
                         }
                     }
                     uint64_t l2 = 0;  // two sums
@@ -685,6 +710,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
             // (not pv_done, which may be two pages behind a warp that has just left the last: its parity would not tell)
             wait(&S.o_full, unit++);
             if (any) {
+                for (int x = max(s.count - 2, 0); x < s.count; ++x) flags(j0 + x, s.page + x);
                 if (half) S.sum[lrow] = l;
                 named_bar_sync(1 + quarter, 64);
                 tc_fence_after();
