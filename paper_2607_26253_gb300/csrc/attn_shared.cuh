@@ -339,7 +339,7 @@ template <int HD, int FMT>
 __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(SharedParams p) {
     constexpr int TILE = shared_tile(HD), RAW = shared_raw(HD), RAWS[2] = {shared_raws(HD, 0), shared_raws(HD, 1)};
     constexpr int CHUNKS = HD / 16, STEP = 32 * kSharedConv / CHUNKS;  // 16-byte pieces of a row; rows that the warps of a tile cover at a time
-    constexpr int LOADS = (kKv8Page + STEP - 1) / STEP, BATCH = 4;
+    constexpr int BATCH = 4;  // of them
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(16) SharedSmem S;
     const uint32_t ring = (smem_u32(smem_raw) + 1023) & ~1023u, raw = ring + kSharedSlots * TILE;
@@ -384,12 +384,36 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         // ------------------------------------------------------------ codes
         SharedWalk w(p, from, to);
         SharedSegment s;
-        uint32_t j = 0, got[2] = {};  // pages, of which copies are under way
+        uint32_t got[2] = {};  // pages asked for
         bool wrong = false;
+        // keys, then the values of the page before: keys are wanted earlier, and have more room
+        auto bring = [&](auto value, int block, int h) {
+            constexpr int v = decltype(value)::value;
+            const uint32_t j = got[v], st = j % RAWS[v];
+            if (j >= (uint32_t)RAWS[v]) wait(&S.raw_empty[v][st], j / RAWS[v] - 1);
+            if (!ok) return;
+            if (lane == 0) {
+                S.block[v][st] = block;
+                if (block >= 0) {
+                    mbar_arrive_expect_tx(&S.raw_full[v][st], RAW);
+                    bulk_load_at(raw + (v * RAWS[0] + st) * RAW, p.c.codes + kv8_tile(p.c, block, v, h) * (kKv8Page * HD), RAW, &S.raw_full[v][st]);
+                } else {
+                    mbar_arrive(&S.raw_full[v][st]);
+                }
+            }
+            if (v == 0 && lane < 8) {
+                if (block >= 0)
+                    cp_async4(smem_u32(&S.raw_scale[st][lane]), p.c.scales + (((int64_t)block * 2 + lane / 4) * p.c.KVH + h) * kKv8PageBlocks + lane % 4);
+                cp_async_arrive(&S.raw_full[0][st]);
+            }
+            __syncwarp();
+            ++got[v];
+        };
+        int last = 0, last_h = -1;  // the page before
         while (ok && w.next(s)) {
             int ids = 0, idbase = -64;
 #pragma unroll 1
-            for (int x = 0; x < s.count && ok; ++x, ++j) {
+            for (int x = 0; x < s.count && ok; ++x) {
                 const int page = s.page + x;
                 if ((unsigned)(page - idbase) >= 32u) {
                     idbase = page;
@@ -400,31 +424,13 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                     }
                 }
                 const int block = __shfl_sync(0xffffffffu, ids, page - idbase);
-#pragma unroll
-                for (int v = 0; v < 2; ++v) {
-                    const uint32_t st = j % RAWS[v];
-                    if (j >= (uint32_t)RAWS[v]) wait(&S.raw_empty[v][st], j / RAWS[v] - 1);
-                    if (!ok) break;
-                    if (lane == 0) {
-                        S.block[v][st] = block;
-                        if (block >= 0) {
-                            mbar_arrive_expect_tx(&S.raw_full[v][st], RAW);
-                            bulk_load_at(raw + (v * RAWS[0] + st) * RAW, p.c.codes + kv8_tile(p.c, block, v, s.h) * (kKv8Page * HD), RAW, &S.raw_full[v][st]);
-                        } else {
-                            mbar_arrive(&S.raw_full[v][st]);
-                        }
-                    }
-                    if (v == 0 && lane < 8) {
-                        if (block >= 0)
-                            cp_async4(smem_u32(&S.raw_scale[st][lane]),
-                                      p.c.scales + (((int64_t)block * 2 + lane / 4) * p.c.KVH + s.h) * kKv8PageBlocks + lane % 4);
-                        cp_async_arrive(&S.raw_full[0][st]);
-                    }
-                    __syncwarp();
-                    ++got[v];
-                }
+                bring(std::integral_constant<int, 0>(), block, s.h);
+                if (last_h >= 0 && ok) bring(std::integral_constant<int, 1>(), last, last_h);
+                last = block;
+                last_h = s.h;
             }
         }
+        if (last_h >= 0 && ok) bring(std::integral_constant<int, 1>(), last, last_h);
         // every copy lands before the CTA ends
         for (int v = 0; v < 2; ++v)
             for (uint32_t q = 1; q <= (uint32_t)RAWS[v] && q <= got[v]; ++q) mbar_wait(&S.raw_full[v][(got[v] - q) % RAWS[v]], ((got[v] - q) / RAWS[v]) & 1, err);
@@ -456,34 +462,35 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 const uint32_t even[2] = {to + place, to + (place ^ 16)}, odd[2] = {to + (place ^ (STEP % 8 * 16)), to + (place ^ (STEP % 8 * 16) ^ 16)};
                 static_assert(STEP % 8 == 0 || STEP % 8 == 4, "an exclusive or is then the sum");
                 uint32_t nan = 0;
-#pragma unroll
-                for (int i0 = 0; i0 < LOADS; i0 += BATCH) {
+                // (not unrolled further: the warps' different parts share the instruction cache)
+#pragma unroll 1
+                for (int at_row = row, off = 0; at_row < kKv8Page; at_row += BATCH * STEP, off += BATCH * STEP * 128) {
                     uint32_t r[BATCH][4];
 #pragma unroll
                     for (int i = 0; i < BATCH; ++i)
-                        if (i0 + i < LOADS && ((i0 + i + 1) * STEP <= kKv8Page || row + (i0 + i) * STEP < kKv8Page)) load_codes<4>(src + (i0 + i) * STEP * HD, r[i]);
+                        if (at_row + i * STEP < kKv8Page) load_codes<4>(src + (at_row - row + i * STEP) * HD, r[i]);
 #pragma unroll
                     for (int i = 0; i < BATCH; ++i) {
-                        const int x = i0 + i, at_row = row + x * STEP;
-                        if (x >= LOADS || !((x + 1) * STEP <= kKv8Page || at_row < kKv8Page)) continue;
+                        const int x = at_row + i * STEP;
+                        if (x >= kKv8Page) continue;
                         uint32_t h[8];
                         if (cut) {
-                            if (block < 0 || p0 + at_row < s.lo || p0 + at_row >= s.hi) r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
+                            if (block < 0 || p0 + x < s.lo || p0 + x >= s.hi) r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
                         }
                         if (FMT == SARA_KV8_E4M3 && value) {  // codes 0x7f and 0xff: their block reads as NaN, and 0 times them must not
                             uint32_t any = 0;
 #pragma unroll
                             for (int e = 0; e < 4; ++e) any |= (r[i][e] & 0x7f7f7f7fu) + 0x01010101u;
                             if (any & 0x80808080u) {
-                                nan |= 1u << (at_row / kKv8Block);
+                                nan |= 1u << (x / kKv8Block);
                                 r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
                             }
                         }
 #pragma unroll
                         for (int e = 0; e < 4; ++e) decode4_half<FMT>(r[i][e], h[2 * e], h[2 * e + 1]);
-                        const uint32_t(&o)[2] = x % 2 ? odd : even;
-                        st_shared_v4(o[0] + x * STEP * 128, h[0], h[1], h[2], h[3]);
-                        st_shared_v4(o[1] + x * STEP * 128, h[4], h[5], h[6], h[7]);
+                        const uint32_t(&o)[2] = i % 2 ? odd : even;
+                        st_shared_v4(o[0] + off + i * STEP * 128, h[0], h[1], h[2], h[3]);
+                        st_shared_v4(o[1] + off + i * STEP * 128, h[4], h[5], h[6], h[7]);
                     }
                 }
                 // (place j & 3: read when page j - 2's product was asked for)
