@@ -462,6 +462,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 const uint32_t even[2] = {to + place, to + (place ^ 16)}, odd[2] = {to + (place ^ (STEP % 8 * 16)), to + (place ^ (STEP % 8 * 16) ^ 16)};
                 static_assert(STEP % 8 == 0 || STEP % 8 == 4, "an exclusive or is then the sum");
                 uint32_t nan = 0;
+                __half2 seen = __floats2half2_rn(0.f, 0.f);
                 // (not unrolled further: the warps' different parts share the instruction cache)
 #pragma unroll 1
                 for (int at_row = row, off = 0; at_row < kKv8Page; at_row += BATCH * STEP, off += BATCH * STEP * 128) {
@@ -477,20 +478,30 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                         if (cut) {
                             if (block < 0 || p0 + x < s.lo || p0 + x >= s.hi) r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
                         }
-                        if (FMT == SARA_KV8_E4M3 && value) {  // codes 0x7f and 0xff: their block reads as NaN, and 0 times them must not
-                            uint32_t any = 0;
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) any |= (r[i][e] & 0x7f7f7f7fu) + 0x01010101u;
-                            if (any & 0x80808080u) {
-                                nan |= 1u << (x / kKv8Block);
-                                r[i][0] = r[i][1] = r[i][2] = r[i][3] = 0;
-                            }
-                        }
 #pragma unroll
                         for (int e = 0; e < 4; ++e) decode4_half<FMT>(r[i][e], h[2 * e], h[2 * e + 1]);
+                        if (FMT == SARA_KV8_E4M3) {  // (0, or NaN from a code's on)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) seen = __hfma2(*reinterpret_cast<const __half2 *>(&h[e]), __floats2half2_rn(0.f, 0.f), seen);
+                        }
                         const uint32_t(&o)[2] = i % 2 ? odd : even;
                         st_shared_v4(o[0] + off + i * STEP * 128, h[0], h[1], h[2], h[3]);
                         st_shared_v4(o[1] + off + i * STEP * 128, h[4], h[5], h[6], h[7]);
+                    }
+                }
+                if (FMT == SARA_KV8_E4M3 && value && __any_sync(0xffffffffu, __hisnan(__low2half(seen)) || __hisnan(__high2half(seen)))) {
+                    // codes 0x7f and 0xff (none that kv8_write writes): their block reads as NaN, and probabilities of 0 times them are not to
+#pragma unroll 1
+                    for (int x = row; x < kKv8Page; x += STEP) {
+                        uint32_t r[4], any = 0;
+                        load_codes<4>(src + (x - row) * HD, r);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) any |= (r[e] & 0x7f7f7f7fu) + 0x01010101u;
+                        if (!(any & 0x80808080u) || p0 + x < s.lo || p0 + x >= s.hi) continue;
+                        nan |= 1u << (x / kKv8Block);
+                        const uint32_t(&o)[2] = (x - row) / STEP % 2 ? odd : even;
+                        st_shared_v4(o[0] + (x - row) * 128, 0, 0, 0, 0);
+                        st_shared_v4(o[1] + (x - row) * 128, 0, 0, 0, 0);
                     }
                 }
                 // (place j & 3: read when page j - 2's product was asked for)

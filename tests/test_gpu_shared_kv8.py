@@ -103,3 +103,40 @@ def test_group_sizes(pkg, sizes, H, kvh, hd, blocks, fmt, typ):
     for _ in range(3):  # the same bits again, from the same workspace
         again, lse2, _ = _run(pkg, c, q, ctx, start, prefix, workspace=ws)
         assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_nan_reaches_its_rows_alone(pkg, hd, fmt):
+    """Scales of NaN, and in e4m3 codes of NaN, among keys and values: a row is NaN where it attends to the block of 32, whichever way,
+    and as it would be without them where it does not."""
+    import torch
+    rng = np.random.default_rng(hd)
+    n, prefix = 40, 700
+    ctx = np.array([(37 * i) % 760 for i in range(n)])
+    first = np.where(np.arange(n) % 3 == 0, (53 * np.arange(n)) % 600, 0)
+    c = Cache(pkg, rng, n, 6, 2, hd, fmt)
+    q = _q(rng, n, 12, hd, "bf16")
+    want = _run(pkg, c, q, ctx, [0, n], [prefix], first)[:2]
+    shared = c.table[0]
+    for at, kv, how in ((10, 0, "scale"), (300, 1, "scale"), (420, 0, "code"), (640, 1, "code"), (127, 1, "code"), (128, 0, "scale"), (699, 1, "code")):
+        page, slot = shared[at // 128], at % 128
+        codes, scales = c.codes.view(torch.uint8).clone(), c.scales.clone()
+        if how == "scale":
+            scales[page, kv, :, slot // 32] = float("nan")
+            hit = (first < at // 32 * 32 + 32) & (np.minimum(ctx, prefix) > at // 32 * 32) & (first < ctx)
+        else:
+            if fmt == "int8":
+                continue
+            codes[page, kv, :, slot, hd // 2] = 0xff
+            # (a value's code makes its block NaN, a key's its position)
+            lo, hi = (at // 32 * 32, at // 32 * 32 + 32) if kv else (at, at + 1)
+            hit = (first < hi) & (np.minimum(ctx, prefix) > lo) & (first < ctx)
+        lse, status = torch.empty((n, 12), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+        out = pkg.attention_shared_kv8(q, codes.view(c.codes.dtype), scales, c.tab, _i32(ctx), _i32([0, n]), _i32([prefix]), first=_i32(first), lse=lse, status=status)
+        assert int(status) == 0
+        for i in range(n):
+            if hit[i]:
+                assert bool(out[i].isnan().all()) and bool(lse[i].isnan().all()), (at, kv, how, i)
+            else:
+                assert torch.equal(out[i], want[0][i]) and torch.equal(lse[i], want[1][i]), (at, kv, how, i)
