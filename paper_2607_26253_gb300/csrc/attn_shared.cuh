@@ -9,8 +9,8 @@
 //   - 3 and 3 turn keys and values into fp16 (which holds both formats exactly) in shared memory, swizzled as the tensor core reads them: the same image
 //     is K-major for the scores and N-major for the values;
 //   - one issues S = Q K^T (128 queries x 128 positions) and O += P V, both tcgen05, Q and P from tensor memory; the next page's scores are
-//     made while this one's softmax goes on;
-//   - 8 have the softmax, two threads a query with 64 positions each: maximum, exponentials, P back to tensor memory in the place of S.
+//     made while this one's softmax goes on, two pages of scores in turn;
+//   - 8 have the softmax, two threads a query with 64 positions each: maximum, exponentials, P back to tensor memory.
 // Scales: K's is a factor of the scores; V's of P, so P times V's scale, relative to the query's largest such product so far (2^R),
 // is what enters the product, in fp16: 11 bits, or within 2^-31 of the largest.  m and R are raised only when a score or a product
 // passes them by 2^8: most pages then need no rescaling of O.
@@ -213,7 +213,7 @@ struct SharedWalk {
 
 // ------------------------------------------------------------------------------- prefix
 struct SharedSmem {
-    uint64_t raw_full[2][4], raw_empty[2][4], full[kSharedSlots], empty[kSharedSlots], q_full, s_full[2], p_full[2], pv_done, o_full;
+    uint64_t raw_full[2][4], raw_empty[2][4], full[kSharedSlots], empty[kSharedSlots], q_full, s_full[2], p_full[2], pv_done;
     float scale[4][8];             // of a page: K's four, V's four
     float raw_scale[4][8];         // the same, as they come with the keys
     alignas(16) uint32_t nan[4][4];  // blocks of a page in which a warp met a NaN among V's codes (read 16 bytes at a time)
@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(16) SharedSmem S;
     const uint32_t ring = (smem_u32(smem_raw) + 1023) & ~1023u, raw = ring + kSharedSlots * TILE;
-    constexpr uint32_t O_AT = 256, Q_AT = 384;  // tensor memory: two pages' scores, outputs, queries
+    constexpr uint32_t O_AT = 256, Q_AT = 384, P_AT = 448;  // tensor memory: two pages' scores, outputs, queries, probabilities
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, G = p.H / p.c.KVH;
     int *err = &p.plan->err;
     if (threadIdx.x == 0) {
@@ -361,7 +361,6 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         }
         mbar_init(&S.q_full, kSharedSoft);
         mbar_init(&S.pv_done, 1);
-        mbar_init(&S.o_full, 1);
         fence_mbar_init();
     }
     constexpr int MMA_WARP = kSharedSoft + 2 * kSharedConv, LOAD_WARP = MMA_WARP + 1;
@@ -528,8 +527,6 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         auto scores = [&](uint32_t j) {
             const uint32_t sk = 2 * (j & 1);
             wait(&S.full[sk], j >> 1);
-            // its place holds the probabilities of an earlier page until their product is done
-            if (done > 0) wait(&S.pv_done, done - 1);
             if (!ok) return;
             tc_fence_after();
             if (elect_one()) {
@@ -545,25 +542,24 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         while (ok && w.next(s)) {
             wait(&S.q_full, unit++);
             if (ok) scores(j0);
+            if (ok && s.count > 1) scores(j0 + 1);
 #pragma unroll 1
             for (uint32_t x = 0; x < (uint32_t)s.count && ok; ++x) {
                 const uint32_t j = j0 + x, sv = 2 * (j & 1) + 1;
-                if (x + 1 < (uint32_t)s.count) scores(j + 1);
                 wait(&S.full[sv], j >> 1);
-                wait(&S.p_full[j & 1], j >> 1);
+                wait(&S.p_full[j & 1], j >> 1);  // (and the page's scores have been read)
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
                     const uint32_t b = ring + sv * TILE;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        tc_mma_ts(tmem + O_AT, tmem + (j & 1) * 128 + k * 8, sdesc_128(b + k * 2048, kSharedQ * 128), idesc_o, x > 0 || k > 0);
+                    for (int k = 0; k < 8; ++k) tc_mma_ts(tmem + O_AT, tmem + P_AT + k * 8, sdesc_128(b + k * 2048, kSharedQ * 128), idesc_o, x > 0 || k > 0);
                     tc_commit(&S.pv_done);
                     tc_commit(&S.empty[sv]);
-                    if (x + 1 == (uint32_t)s.count) tc_commit(&S.o_full);
                 }
                 __syncwarp();
                 ++done;
+                if (x + 2 < (uint32_t)s.count) scores(j + 2);
             }
             j0 += s.count;
         }
@@ -574,7 +570,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), o_at = lanes + O_AT + half * (HD / 2);
         SharedWalk w(p, from, to);
         SharedSegment s;
-        uint32_t j0 = 0, unit = 0;
+        uint32_t j0 = 0;
         // (after a failed wait the barriers go on, so that no warp is left in one)
         while (w.next(s)) {
             const int at = s.q0 + lrow;  // among the group's queries
@@ -631,7 +627,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 if ((bad & 1) && lo < p0 + 32 && hi > p0) l = __int_as_float(0x7fc00000);
                 if ((bad & 2) && lo < p0 + 64 && hi > p0 + 32) l = __int_as_float(0x7fc00000);
             };
-            // the flags of values that have gone into a product: page j's by the scores of page j + 2, the last two's by the end
+            // the flags of values that have gone into a product: page j's when page j + 1's is asked for, the last two's by the end
             auto flags = [&](uint32_t j, int page) {
                 if constexpr (FMT == SARA_KV8_E4M3) {
                     static_assert(kSharedConv == 3 && offsetof(SharedSmem, nan) % 16 == 0, "a word a warp, read at once");
@@ -643,12 +639,21 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
 #pragma unroll 1
             for (int x = 0; x < s.count; ++x) {
                 const uint32_t j = j0 + x, s_at = lanes + (j & 1) * 128 + half * 64;
+                // the product before this page's has been taken (every page waits for it once: a phase later its parity would not tell)
+                bool waited = j == 0;
+                auto before = [&]() {
+                    if (!waited) {
+                        wait(&S.pv_done, j - 1);
+                        tc_fence_after();
+                    }
+                    waited = true;
+                };
                 wait(&S.s_full[j & 1], j >> 1);  // (the page's scales were there before its keys)
                 if (any) {
                     tc_fence_after();
                     float v[64], ks[2], F[2], ev[2];
                     tmem_load64(s_at, v);
-                    if (x >= 2) flags(j - 2, s.page + x - 2);
+                    if (x >= 2) flags(j - 2, s.page + x - 2);  // (the page before has waited for it)
                     const int p0 = (s.page + x) * kKv8Page + 64 * half;
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
@@ -689,8 +694,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                         m = m1;
                         R = R1;
                         if (x > 0) {
-                            wait(&S.pv_done, j - 1);
-                            tc_fence_after();
+                            before();
 #pragma unroll 1
                             for (int d = 0; d < HD / 2; d += 16) {
                                 float o[16];
@@ -719,14 +723,15 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                         }
                     }
                     l += unpack_f32x2(l2).x + unpack_f32x2(l2).y;
-                    tmem_store32(lanes + (j & 1) * 128 + half * 32, h);  // (both halves have read their scores: the barrier)
+                    before();
+                    tmem_store32(lanes + P_AT + half * 32, h);
                 }
+                before();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&S.p_full[j & 1]);
             }
-            // (not pv_done, which may be two pages behind a warp that has just left the last: its parity would not tell)
-            wait(&S.o_full, unit++);
+            wait(&S.pv_done, j0 + s.count - 1);
             if (any) {
                 for (int x = max(s.count - 2, 0); x < s.count; ++x) flags(j0 + x, s.page + x);
                 if (half) S.sum[lrow] = l;
