@@ -168,31 +168,34 @@ struct SharedSegment {
     int lo, hi, page;           // the group's positions; the first page
     bool begins, whole;
 };
+// A warp's way through its share: kept in shared memory, since it is wanted between segments only.
 struct SharedWalk {
-    const SharedParams &p;
-    int g, e, end;
+    int g, e, end, entry1;  // group, next entry, the share's end; the next group's first entry
     SharedGroup x;
-    int entry1;  // of the next group
-    __device__ __forceinline__ SharedWalk(const SharedParams &p_, int from, int to) : p(p_), g(0), e(from), end(to) {
-        int hi = p.groups;  // the last group that begins at `from` or before
-        while (g < hi) {
-            const int mid = (g + hi) / 2;
-            if (__ldg(&p.group[mid].entry0) <= from) g = mid + 1;
-            else hi = mid;
-        }
-        g = max(g - 1, 0);
-        load();
-    }
-    __device__ __forceinline__ void load() {
+    SharedSegment s;        // the present segment
+    __device__ __forceinline__ void load(const SharedParams &p) {
         const int4 a = __ldg(reinterpret_cast<const int4 *>(p.group + g)), b = __ldg(reinterpret_cast<const int4 *>(p.group + g) + 1);
         x = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         entry1 = x.entry0 + x.pages * x.tiles * p.c.KVH;
     }
-    __device__ __forceinline__ bool next(SharedSegment &s) {
+    // (one lane)
+    __device__ __forceinline__ void begin(const SharedParams &p, int from, int to) {
+        int lo = 0, hi = p.groups;  // the last group that begins at `from` or before
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (__ldg(&p.group[mid].entry0) <= from) lo = mid + 1;
+            else hi = mid;
+        }
+        g = max(lo - 1, 0);
+        e = from;
+        end = to;
+        load(p);
+    }
+    __device__ __forceinline__ bool advance(const SharedParams &p) {
         if (e >= end) return false;
         while (e >= entry1 && g + 1 < p.groups) {
             ++g;
-            load();
+            load(p);
         }
         const int off = e - x.entry0, unit = off / x.pages, at = off - unit * x.pages, t = unit % x.tiles;
         s.e = e;
@@ -209,6 +212,13 @@ struct SharedWalk {
         e += s.count;
         return true;
     }
+    // The next segment, or false behind the last (a warp)
+    __device__ __forceinline__ bool next(const SharedParams &p) {
+        __syncwarp();
+        bool more = false;
+        if ((threadIdx.x & 31) == 0) more = advance(p);
+        return __shfl_sync(0xffffffffu, more, 0);  // (orders what lane 0 wrote)
+    }
 };
 
 // ------------------------------------------------------------------------------- prefix
@@ -216,11 +226,12 @@ struct SharedSmem {
     uint64_t raw_full[2][4], raw_empty[2][4], full[kSharedSlots], empty[kSharedSlots], q_full, s_full[2], p_full[2], pv_done;
     float scale[4][8];             // of a page: K's four, V's four
     float raw_scale[4][8];         // the same, as they come with the keys
-    alignas(16) uint32_t nan[4][4];  // blocks of a page in which a warp met a NaN among V's codes (read 16 bytes at a time)
+    alignas(16) uint32_t nan[4][2][4];  // blocks of a page in which a warp met a NaN among K's, V's codes (read 16 bytes at a time)
     float2 top[2][kSharedQ];       // a query's largest score and product, of either half of a page
     float sum[kSharedQ];           // of the second half's probabilities
     int block[2][4];               // of a page of codes
     uint32_t tmem_base;
+    SharedWalk walk[kSharedThreads / 32];
 };
 
 __device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
@@ -375,14 +386,15 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
     const uint32_t tmem = S.tmem_base;
     const SharedShares shares(p.plan->entries, min((int)gridDim.x, p.max_shares));
     const int c = blockIdx.x, from = c < shares.n ? shares.begin(c) : 0, to = c < shares.n ? shares.begin(c + 1) : 0;
+    SharedWalk &w = S.walk[warp];
+    const SharedSegment &s = w.s;
+    if (from < to && lane == 0) w.begin(p, from, to);
     bool ok = true;
     auto wait = [&](uint64_t *bar, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity & 1, err)); };
 
     if (from >= to) {
     } else if (warp == LOAD_WARP) {
         // ------------------------------------------------------------ codes
-        SharedWalk w(p, from, to);
-        SharedSegment s;
         uint32_t got[2] = {};  // pages asked for
         bool wrong = false;
         // keys, then the values of the page before: keys are wanted earlier, and have more room
@@ -409,7 +421,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
             ++got[v];
         };
         int last = 0, last_h = -1;  // the page before
-        while (ok && w.next(s)) {
+        while (ok && w.next(p)) {
             int ids = 0, idbase = -64;
 #pragma unroll 1
             for (int x = 0; x < s.count && ok; ++x) {
@@ -442,10 +454,8 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         // this thread's row and 16 dims of the first STEP rows (128 dims: 8 lanes have pieces of different halves of two rows, whose places meet
         // all banks)
         const int row = HD == 128 ? ct / 16 * 2 + (ct / 4 & 1) : ct / CHUNKS, d = HD == 128 ? (ct & 3) + 4 * ((ct / 4 ^ ct / 8) & 1) : ct % CHUNKS;
-        SharedWalk w(p, from, to);
-        SharedSegment s;
         uint32_t j = 0;
-        while (ok && w.next(s)) {
+        while (ok && w.next(p)) {
 #pragma unroll 1
             for (int x = 0; x < s.count && ok; ++x, ++j) {
                 const uint32_t st = j % raws, at = 2 * (j & 1) + value;
@@ -488,8 +498,8 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                         st_shared_v4(o[1] + off + i * STEP * 128, h[4], h[5], h[6], h[7]);
                     }
                 }
-                if (FMT == SARA_KV8_E4M3 && value && __any_sync(0xffffffffu, __hisnan(__low2half(seen)) || __hisnan(__high2half(seen)))) {
-                    // codes 0x7f and 0xff (none that kv8_write writes): their block reads as NaN, and probabilities of 0 times them are not to
+                if (FMT == SARA_KV8_E4M3 && __any_sync(0xffffffffu, __hisnan(__low2half(seen)) || __hisnan(__high2half(seen)))) {
+                    // codes 0x7f and 0xff (none that kv8_write writes): their block reads as NaN, and nothing else is to be
 #pragma unroll 1
                     for (int x = row; x < kKv8Page; x += STEP) {
                         uint32_t r[4], any = 0;
@@ -505,9 +515,9 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 }
                 // (place j & 3: read when page j - 2's product was asked for)
                 if (!value && cw == 0 && lane < 8) S.scale[j & 3][lane] = block >= 0 ? S.raw_scale[st][lane] : __int_as_float(0x7fc00000);
-                if (FMT == SARA_KV8_E4M3 && value) {
+                if (FMT == SARA_KV8_E4M3) {
                     nan = __reduce_or_sync(0xffffffffu, nan);
-                    if (lane == 0) S.nan[j & 3][cw] = nan;
+                    if (lane == 0) S.nan[j & 3][value][cw] = nan;
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -521,8 +531,6 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         // ------------------------------------------------------------ MMAs
         constexpr uint32_t idesc_s = 1u << 4 | (128u >> 3) << 17 | (128u >> 4) << 24;
         constexpr uint32_t idesc_o = 1u << 4 | 1u << 16 | ((uint32_t)HD >> 3) << 17 | (128u >> 4) << 24;  // values: N-major
-        SharedWalk w(p, from, to);
-        SharedSegment s;
         uint32_t j0 = 0, unit = 0, done = 0;  // pages before, units, products issued
         auto scores = [&](uint32_t j) {
             const uint32_t sk = 2 * (j & 1);
@@ -539,7 +547,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
             }
             __syncwarp();
         };
-        while (ok && w.next(s)) {
+        while (ok && w.next(p)) {
             wait(&S.q_full, unit++);
             if (ok) scores(j0);
             if (ok && s.count > 1) scores(j0 + 1);
@@ -568,11 +576,9 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         // ------------------------------------------------------------ softmax: a query's first or second 64 positions a thread
         const int quarter = warp & 3, half = warp >> 2, lrow = quarter * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), o_at = lanes + O_AT + half * (HD / 2);
-        SharedWalk w(p, from, to);
-        SharedSegment s;
         uint32_t j0 = 0;
         // (after a failed wait the barriers go on, so that no warp is left in one)
-        while (w.next(s)) {
+        while (w.next(p)) {
             const int at = s.q0 + lrow;  // among the group's queries
             const bool live = lrow < s.queries;
             const int row = s.row0 + (live ? at / G : 0), head = s.h * G + (live ? at % G : 0);
@@ -627,12 +633,12 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 if ((bad & 1) && lo < p0 + 32 && hi > p0) l = __int_as_float(0x7fc00000);
                 if ((bad & 2) && lo < p0 + 64 && hi > p0 + 32) l = __int_as_float(0x7fc00000);
             };
-            // the flags of values that have gone into a product: page j's when page j + 1's is asked for, the last two's by the end
+            // the flags of codes that have gone into a product: page j's when page j + 1's is asked for, the last two's by the end
             auto flags = [&](uint32_t j, int page) {
                 if constexpr (FMT == SARA_KV8_E4M3) {
                     static_assert(kSharedConv == 3 && offsetof(SharedSmem, nan) % 16 == 0, "a word a warp, read at once");
-                    const uint4 b = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][0]);
-                    const uint32_t bad = (b.x | b.y | b.z) >> (2 * half) & 3;
+                    const uint4 a = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][0][0]), b = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][1][0]);
+                    const uint32_t bad = (a.x | a.y | a.z | b.x | b.y | b.z) >> (2 * half) & 3;
                     if (bad) poison(page, bad);
                 }
             };
@@ -651,10 +657,13 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 wait(&S.s_full[j & 1], j >> 1);  // (the page's scales were there before its keys)
                 if (any) {
                     tc_fence_after();
-                    float v[64], ks[2], F[2], ev[2];
-                    tmem_load64(s_at, v);
                     if (x >= 2) flags(j - 2, s.page + x - 2);  // (the page before has waited for it)
                     const int p0 = (s.page + x) * kKv8Page + 64 * half;
+                    // its positions from `skip` on, `take` of them; a query that attends to none has all of them, and exponents of -1e30
+                    const bool none = lo >= p0 + 64 || hi <= p0;
+                    const int skip = none ? 0 : max(lo - p0, 0), take = none ? 64 : min(hi - p0, 64) - skip;
+                    float v[64], ks[2], F[2], ev[2];
+                    tmem_load64(s_at, v);
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         ks[b] = S.scale[j & 3][2 * half + b] * mul;
@@ -667,9 +676,9 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                         ev[b] = (float)min(max(scale_exp(F[b]), -126), 126);
                         F[b] *= pow2f(-(int)ev[b]);
                     }
-                    if (__any_sync(0xffffffffu, lo > p0 || hi < p0 + 64)) {  // some are masked
+                    if (__any_sync(0xffffffffu, take < 64)) {
 #pragma unroll
-                        for (int e = 0; e < 64; ++e) v[e] = p0 + e >= lo && p0 + e < hi ? v[e] : -INFINITY;
+                        for (int e = 0; e < 64; ++e) v[e] = (unsigned)(e - skip) < (unsigned)take ? v[e] : -INFINITY;
                     }
                     float2 top = make_float2(-INFINITY, -INFINITY);
 #pragma unroll
@@ -681,6 +690,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                         top.x = fmaxf(top.x, n);
                         top.y = fmaxf(top.y, n + ev[b]);
                     }
+                    if (none) top = make_float2(-INFINITY, -INFINITY);
                     if (named_bar_or(1 + quarter, 64, top.x > m + 8.f || top.y > R + 8.f)) {  // of either half: both raise the same
                         S.top[half][lrow] = top;
                         named_bar_sync(1 + quarter, 64);
@@ -708,11 +718,13 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                     }
                     uint64_t l2 = 0;  // two sums
                     uint32_t h[32];
-                    const uint64_t m2 = pack_f32x2(-m, -m);
+                    const float off = none ? -1e30f : -m;
+                    const uint64_t m2 = pack_f32x2(off, off);
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         const float f = F[b] * ex2(fminf(m - R + ev[b] + kSharedShift, 126.f));
-                        const uint64_t k2 = pack_f32x2(ks[b], ks[b]), f2 = pack_f32x2(f, f);
+                        const float k = none ? 0.f : ks[b];
+                        const uint64_t k2 = pack_f32x2(k, k), f2 = pack_f32x2(f, f);
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
                             const float2 y = unpack_f32x2(fma_f32x2(pack_f32x2(v[32 * b + e], v[32 * b + e + 1]), k2, m2));

@@ -129,9 +129,7 @@ def test_nan_reaches_its_rows_alone(pkg, hd, fmt):
             if fmt == "int8":
                 continue
             codes[page, kv, :, slot, hd // 2] = 0xff
-            # (a value's code makes its block NaN, a key's its position)
-            lo, hi = (at // 32 * 32, at // 32 * 32 + 32) if kv else (at, at + 1)
-            hit = (first < hi) & (np.minimum(ctx, prefix) > lo) & (first < ctx)
+            hit = (first < at // 32 * 32 + 32) & (np.minimum(ctx, prefix) > at // 32 * 32) & (first < ctx)
         lse, status = torch.empty((n, 12), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
         out = pkg.attention_shared_kv8(q, codes.view(c.codes.dtype), scales, c.tab, _i32(ctx), _i32([0, n]), _i32([prefix]), first=_i32(first), lse=lse, status=status)
         assert int(status) == 0
