@@ -31,6 +31,8 @@ __host__ __device__ constexpr int shared_raws(int hd, int v) { return hd == 128 
 __host__ __device__ constexpr int shared_smem(int hd) {
     return 1024 + kSharedSlots * shared_tile(hd) + (shared_raws(hd, 0) + shared_raws(hd, 1)) * shared_raw(hd);
 }
+// Floats of a query's state: outputs, maximum, sum, and two to whole 16 bytes
+__host__ __device__ constexpr int shared_state(int hd) { return hd + 4; }
 constexpr float kSharedShift = 6.f;                 // log2 of the products' scale
 constexpr int kSharedMaxShares = 160;               // CTAs, one an SM
 constexpr int kSharedWideJoin = 1216;               // queries up to which 8 warps join a query
@@ -57,8 +59,8 @@ struct SharedParams {
     SharedPlan *plan;
     SharedGroup *group;
     int *row_group, *row_first, *row_prefix;  // [n]: group (-1: none), first own position, shared ones
-    float *whole;      // [n][H][hd + 2]: sums of a unit that one share holds: maximum, sum, outputs
-    float *part;       // [share][2][128][hd + 2]: of a unit that begins before the share, or in it
+    float *whole;      // [n][H] states: sums of a unit that one share holds
+    float *part;       // [share][2][128] states: of a unit that begins before the share, or in it
     int max_shares;
     // join
     const float *own, *own_lse;  // [n][H][hd], [n][H]
@@ -74,7 +76,10 @@ __global__ void __launch_bounds__(1024) shared_plan_kernel(SharedParams p) {
     pdl_allow_dependents();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t most = (int64_t)p.c.max_blocks * kKv8Page;
-    if (threadIdx.x == 0) s_bad = 0;
+    if (threadIdx.x == 0) {
+        s_bad = 0;
+        p.plan->err = 0;
+    }
     __syncthreads();
     for (int g = threadIdx.x; g < p.groups; g += 1024) {
         const int a = p.start[g], b = p.start[g + 1];
@@ -224,9 +229,9 @@ struct SharedWalk {
 // ------------------------------------------------------------------------------- prefix
 struct SharedSmem {
     uint64_t raw_full[2][4], raw_empty[2][4], full[kSharedSlots], empty[kSharedSlots], q_full, s_full[2], p_full[2], pv_done;
-    float scale[4][8];             // of a page: K's four, V's four
+    float scale[8][3][4];          // of a page's blocks: K's scale, V's as 2^e and what is left, e
     float raw_scale[4][8];         // the same, as they come with the keys
-    alignas(16) uint32_t nan[4][2][4];  // blocks of a page in which a warp met a NaN among K's, V's codes (read 16 bytes at a time)
+    alignas(16) uint32_t nan[8][2][4];  // blocks of a page in which a warp met a NaN among K's, V's codes, and ([0][3]) those whose scales are none
     float2 top[2][kSharedQ];       // a query's largest score and product, of either half of a page
     float sum[kSharedQ];           // of the second half's probabilities
     int block[2][4];               // of a page of codes
@@ -372,6 +377,8 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         }
         mbar_init(&S.q_full, kSharedSoft);
         mbar_init(&S.pv_done, 1);
+        for (int s = 0; s < 8; ++s)
+            for (int k = 0; k < 8; ++k) S.nan[s][k / 4][k % 4] = 0;
         fence_mbar_init();
     }
     constexpr int MMA_WARP = kSharedSoft + 2 * kSharedConv, LOAD_WARP = MMA_WARP + 1;
@@ -463,6 +470,24 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 if (!ok) break;
                 const int block = S.block[value][st], p0 = (s.page + x) * kKv8Page;
                 const bool cut = block < 0 || p0 < s.lo || p0 + kKv8Page > s.hi;  // positions that nobody attends to are 0: what they hold does not matter
+                // (eight places: the page three before has its scores, so that the softmax is done with the one five before, and a page's flags are read in the one
+                // behind it, or when the next unit's first scores may have been made)
+                if (!value && cw == kSharedConv - 1) {  // (the warp with the fewest rows.  A block whose scale is NaN or infinite reads as NaN: it goes in as 0, and is flagged)
+                    float k = 1.f, f = 0.f;
+                    if (block >= 0 && lane < 4) {
+                        k = S.raw_scale[st][lane];
+                        f = S.raw_scale[st][4 + lane];
+                    }
+                    const bool bad = block < 0 || !(fabsf(k) < INFINITY && fabsf(f) < INFINITY);
+                    const int e = min(max(scale_exp(bad ? 0.f : f), -126), 126);
+                    const uint32_t flag = __ballot_sync(0xffffffffu, bad) & 15;
+                    if (lane < 4) {
+                        S.scale[j & 7][0][lane] = bad ? 1.f : k;
+                        S.scale[j & 7][1][lane] = bad ? 0.f : f * pow2f(-e);
+                        S.scale[j & 7][2][lane] = (float)e;
+                    }
+                    if (lane == 0) S.nan[j & 7][0][3] = flag;
+                }
                 if (j >= 2) wait(&S.empty[at], (j >> 1) - 1);
                 if (!ok) break;
                 const uint32_t src = raw + ((value ? RAWS[0] : 0) + st) * RAW + row * HD + 16 * d, slot = ring + at * TILE;
@@ -513,11 +538,9 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                         st_shared_v4(o[1] + (x - row) * 128, 0, 0, 0, 0);
                     }
                 }
-                // (place j & 3: read when page j - 2's product was asked for)
-                if (!value && cw == 0 && lane < 8) S.scale[j & 3][lane] = block >= 0 ? S.raw_scale[st][lane] : __int_as_float(0x7fc00000);
                 if (FMT == SARA_KV8_E4M3) {
                     nan = __reduce_or_sync(0xffffffffu, nan);
-                    if (lane == 0) S.nan[j & 3][value][cw] = nan;
+                    if (lane == 0) S.nan[j & 7][value][cw] = nan;
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -577,55 +600,73 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         const int quarter = warp & 3, half = warp >> 2, lrow = quarter * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(quarter * 32) << 16), o_at = lanes + O_AT + half * (HD / 2);
         uint32_t j0 = 0;
-        // (after a failed wait the barriers go on, so that no warp is left in one)
-        while (w.next(p)) {
+        // A unit's query as fp16, one half of it, into tensor memory (the scores of the unit before have been made): its outputs' place, its positions
+        // and the factor that brings scores to base-2 exponents
+        struct Query {
+            float *out;
+            float mul;
+            int lo, hi;
+            bool live, any;
+        };
+        auto begin = [&]() {
+            Query y;
             const int at = s.q0 + lrow;  // among the group's queries
-            const bool live = lrow < s.queries;
-            const int row = s.row0 + (live ? at / G : 0), head = s.h * G + (live ? at % G : 0);
-            const bool any = __any_sync(0xffffffffu, live);
-            // the query as fp16, one half of it
-            float mul = p.scale_log2;
-            int lo = 0, hi = 0;
-            {
+            y.live = lrow < s.queries;
+            y.any = __any_sync(0xffffffffu, y.live);
+            const int row = s.row0 + (y.live ? at / G : 0), head = s.h * G + (y.live ? at % G : 0);
+            y.out = s.whole ? p.whole + ((int64_t)row * p.H + head) * shared_state(HD)
+                            : p.part + (((int64_t)c * 2 + s.begins) * kSharedQ + lrow) * shared_state(HD);
+            y.mul = p.scale_log2;
+            y.lo = y.hi = 0;
+            if (y.any) {
                 const uint4 *src = reinterpret_cast<const uint4 *>(p.q + row * p.q_stride + (int64_t)head * HD);
-                uint32_t top = 0;
-                float f = 1.f;
-                if (live && p.type == SARA_BF16) {
+                const int first = p.first ? p.first[row] : 0, end = min(p.ctx[row], p.row_prefix[row]), group = p.row_group[row];
+                uint4 x[HD / 8];
 #pragma unroll
-                    for (int i = 0; i < HD / 8; ++i) {
-                        const uint4 x = __ldg(src + i);
-                        top = __vmaxu2(top, __vmaxu2(__vmaxu2(x.x & 0x7fff7fffu, x.y & 0x7fff7fffu), __vmaxu2(x.z & 0x7fff7fffu, x.w & 0x7fff7fffu)));
-                    }
+                for (int i = 0; i < HD / 8; ++i) x[i] = __ldg(src + i);
+                float f = 1.f;
+                if (p.type == SARA_BF16) {
+                    uint32_t top = 0;
+#pragma unroll
+                    for (int i = 0; i < HD / 8; ++i)
+                        top = __vmaxu2(top, __vmaxu2(__vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu), __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu)));
                     top = max(top & 0xffff, top >> 16);
                     const int e = max(min(14 - ((int)(top >> 7) - 127), 126), -113);  // brings the largest magnitude's power of two to 2^14
                     f = pow2f(e);
-                    mul *= pow2f(-e);
+                    y.mul *= pow2f(-e);
                 }
 #pragma unroll
-                for (int x = 0; x < HD / 16; ++x) {
-                    const int i = half * (HD / 16) + x;
-                    uint4 y = live ? __ldg(src + i) : make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < HD / 16; ++i) {
+                    const uint4 z = half ? x[HD / 16 + i] : x[i];
+                    uint32_t u[4] = {z.x, z.y, z.z, z.w};
                     if (p.type == SARA_BF16) {
-                        uint32_t u[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float2 z = unpack2<SARA_BF16>(u[e]);
-                            u[e] = pack_half2(z.x * f, z.y * f);
+                            const float2 g = unpack2<SARA_BF16>(u[e]);
+                            u[e] = pack_half2(g.x * f, g.y * f);
                         }
-                        y = make_uint4(u[0], u[1], u[2], u[3]);
                     }
-                    tmem_store4(lanes + Q_AT + i * 4, y);
+                    tmem_store4(lanes + Q_AT + (half * (HD / 16) + i) * 4, make_uint4(u[0], u[1], u[2], u[3]));
                 }
-                if (live && p.row_group[row] >= 0) {
-                    lo = p.first ? p.first[row] : 0;
-                    hi = min(p.ctx[row], p.row_prefix[row]);
+                if (y.live && group >= 0) {
+                    y.lo = first;
+                    y.hi = end;
                 }
+                tmem_wait_st();
             }
-            tmem_wait_st();
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&S.q_full);
-
+            return y;
+        };
+        // (after a failed wait the barriers go on, so that no warp is left in one)
+        bool more = w.next(p);
+        Query next = begin();
+        while (more) {
+            const Query now = next;
+            const bool any = now.any;
+            const int lo = now.lo, hi = now.hi, count = s.count, page0 = s.page;
+            const float mul = now.mul;
             float m = -3.4028235e38f, R = m, l = 0.f;
             // a block that reads as NaN (bit b: of this half's) makes the sums of those that attend to it NaN, and leaves the others alone
             auto poison = [&](int page, uint32_t bad) {
@@ -633,17 +674,18 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 if ((bad & 1) && lo < p0 + 32 && hi > p0) l = __int_as_float(0x7fc00000);
                 if ((bad & 2) && lo < p0 + 64 && hi > p0 + 32) l = __int_as_float(0x7fc00000);
             };
-            // the flags of codes that have gone into a product: page j's when page j + 1's is asked for, the last two's by the end
+            // the flags of codes that have gone into a product: a page's when the next one's is asked for
             auto flags = [&](uint32_t j, int page) {
+                static_assert(kSharedConv == 3 && offsetof(SharedSmem, nan) % 16 == 0, "a word a warp, read at once");
+                uint32_t bad = S.nan[j & 7][0][3];
                 if constexpr (FMT == SARA_KV8_E4M3) {
-                    static_assert(kSharedConv == 3 && offsetof(SharedSmem, nan) % 16 == 0, "a word a warp, read at once");
-                    const uint4 a = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][0][0]), b = *reinterpret_cast<const uint4 *>(&S.nan[j & 3][1][0]);
-                    const uint32_t bad = (a.x | a.y | a.z | b.x | b.y | b.z) >> (2 * half) & 3;
-                    if (bad) poison(page, bad);
+                    const uint4 a = *reinterpret_cast<const uint4 *>(&S.nan[j & 7][0][0]), b = *reinterpret_cast<const uint4 *>(&S.nan[j & 7][1][0]);
+                    bad = a.x | a.y | a.z | a.w | b.x | b.y | b.z;
                 }
+                if (bad >> (2 * half) & 3) poison(page, bad >> (2 * half));
             };
 #pragma unroll 1
-            for (int x = 0; x < s.count; ++x) {
+            for (int x = 0; x < count; ++x) {
                 const uint32_t j = j0 + x, s_at = lanes + (j & 1) * 128 + half * 64;
                 // the product before this page's has been taken (every page waits for it once: a phase later its parity would not tell)
                 bool waited = j == 0;
@@ -657,8 +699,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 wait(&S.s_full[j & 1], j >> 1);  // (the page's scales were there before its keys)
                 if (any) {
                     tc_fence_after();
-                    if (x >= 2) flags(j - 2, s.page + x - 2);  // (the page before has waited for it)
-                    const int p0 = (s.page + x) * kKv8Page + 64 * half;
+                    const int p0 = (page0 + x) * kKv8Page + 64 * half;
                     // its positions from `skip` on, `take` of them; a query that attends to none has all of them, and exponents of -1e30
                     const bool none = lo >= p0 + 64 || hi <= p0;
                     const int skip = none ? 0 : max(lo - p0, 0), take = none ? 64 : min(hi - p0, 64) - skip;
@@ -666,15 +707,9 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                     tmem_load64(s_at, v);
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        ks[b] = S.scale[j & 3][2 * half + b] * mul;
-                        F[b] = S.scale[j & 3][4 + 2 * half + b];
-                        if (!(fabsf(ks[b]) < INFINITY && fabsf(F[b]) < INFINITY)) {
-                            poison(s.page + x, 1 << b);
-                            ks[b] = 1.f;
-                            F[b] = 0.f;
-                        }
-                        ev[b] = (float)min(max(scale_exp(F[b]), -126), 126);
-                        F[b] *= pow2f(-(int)ev[b]);
+                        ks[b] = S.scale[j & 7][0][2 * half + b] * mul;
+                        F[b] = S.scale[j & 7][1][2 * half + b];
+                        ev[b] = S.scale[j & 7][2][2 * half + b];
                     }
                     if (__any_sync(0xffffffffu, take < 64)) {
 #pragma unroll
@@ -683,9 +718,13 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                     float2 top = make_float2(-INFINITY, -INFINITY);
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        float n = fmaxf(v[32 * b], v[32 * b + 1]);
+                        float n = fmaxf(v[32 * b], v[32 * b + 1]), n1 = fmaxf(v[32 * b + 2], v[32 * b + 3]);
 #pragma unroll
-                        for (int e = 2; e < 32; e += 2) n = max3(n, v[32 * b + e], v[32 * b + e + 1]);
+                        for (int e = 4; e < 32; e += 4) {
+                            n = max3(n, v[32 * b + e], v[32 * b + e + 1]);
+                            n1 = max3(n1, v[32 * b + e + 2], v[32 * b + e + 3]);
+                        }
+                        n = fmaxf(n, n1);
                         n *= ks[b];
                         top.x = fmaxf(top.x, n);
                         top.y = fmaxf(top.y, n + ev[b]);
@@ -737,36 +776,38 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                     l += unpack_f32x2(l2).x + unpack_f32x2(l2).y;
                     before();
                     tmem_store32(lanes + P_AT + half * 32, h);
+                    if (x > 0) flags(j - 1, page0 + x - 1);
                 }
                 before();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&S.p_full[j & 1]);
             }
-            wait(&S.pv_done, j0 + s.count - 1);
+            // the next unit's queries go in before this one's outputs come out, so that its scores are made meanwhile
+            more = w.next(p);
+            if (more) next = begin();
+            wait(&S.pv_done, j0 + count - 1);
             if (any) {
-                for (int x = max(s.count - 2, 0); x < s.count; ++x) flags(j0 + x, s.page + x);
+                flags(j0 + count - 1, page0 + count - 1);
                 if (half) S.sum[lrow] = l;
                 named_bar_sync(1 + quarter, 64);
                 tc_fence_after();
-                float *o = s.whole ? p.whole + ((int64_t)row * p.H + head) * (HD + 2)
-                                   : p.part + (((int64_t)c * 2 + s.begins) * kSharedQ + lrow) * (HD + 2);
                 const float f = ex2(fminf(fmaxf(R - m - kSharedShift, -1e4f), 126.f));
 #pragma unroll 1
                 for (int d = 0; d < HD / 2; d += 16) {
                     float y[16];
                     tmem_load16(o_at + d, y);
-                    if (live) {
+                    if (now.live) {
 #pragma unroll
-                        for (int e = 0; e < 16; e += 2)
-                            *reinterpret_cast<float2 *>(o + 2 + half * (HD / 2) + d + e) = make_float2(y[e] * f, y[e + 1] * f);
+                        for (int e = 0; e < 16; e += 4)
+                            *reinterpret_cast<float4 *>(now.out + half * (HD / 2) + d + e) = make_float4(y[e] * f, y[e + 1] * f, y[e + 2] * f, y[e + 3] * f);
                     }
                 }
-                if (live && !half) *reinterpret_cast<float2 *>(o) = make_float2(m, l + S.sum[lrow]);
+                if (now.live && !half) *reinterpret_cast<float2 *>(now.out + HD) = make_float2(m, l + S.sum[lrow]);
                 named_bar_sync(1 + quarter, 64);  // (the sums have been read)
             }
             tc_fence_before();
-            j0 += s.count;
+            j0 += count;
         }
     }
     __syncwarp();
@@ -808,13 +849,13 @@ __global__ void __launch_bounds__(256) shared_join_kernel(SharedParams p, int sh
         const int at = (row - y.row0) * G + head % G, e0 = y.entry0 + (head / G * y.tiles + at / kSharedQ) * y.pages;
         const int c0 = shares.of(e0), c1 = shares.of(e0 + y.pages - 1);
         if (c0 == c1) {
-            const float *s = p.whole + x * (HD + 2);
-            if (part == 0) add(s[0], s[1], s + 2);
+            const float *s = p.whole + x * shared_state(HD);
+            if (part == 0) add(s[HD], s[HD + 1], s);
         } else {
 #pragma unroll 4
             for (int c = c0 + part; c <= c1; c += W) {
-                const float *s = p.part + (((int64_t)c * 2 + (c == c0)) * kSharedQ + at % kSharedQ) * (HD + 2);
-                add(s[0], s[1], s + 2);
+                const float *s = p.part + (((int64_t)c * 2 + (c == c0)) * kSharedQ + at % kSharedQ) * shared_state(HD);
+                add(s[HD], s[HD + 1], s);
             }
         }
     }

@@ -34,8 +34,8 @@ SharedLayout shared_layout(int n, int groups, int H, int kvh, int hd) {
     w.row_prefix = take(rows * 4);
     w.out32 = take(states * hd * 4);
     w.lse = take(states * 4);
-    w.whole = take(states * (hd + 2) * 4);
-    w.part = take((size_t)kSharedMaxShares * 2 * kSharedQ * (hd + 2) * 4);
+    w.whole = take(states * shared_state(hd) * 4);
+    w.part = take((size_t)kSharedMaxShares * 2 * kSharedQ * shared_state(hd) * 4);
     w.bytes = at;
     return w;
 }
