@@ -478,7 +478,9 @@ SARA_API int sara_logprobs_backward(const void *logits, int64_t row_stride, int3
  * captured.  Products are exact and summed in fp32.
  * workspace: sara_linear_logprobs_workspace_bytes(R, d, V, backward) bytes of device scratch, 256-byte aligned, whose first 256 bytes are
  * zero on first use and left zero where they have to be; calls that share one must not overlap.  (12 bytes a row and 256 tokens for the
- * scores; for the gradient the rows, up to 384 MB of the gradients of a piece of the vocabulary, and fp32 sums of grad_hidden.)
+ * scores; for the gradient the rows, the gradients of a piece of the vocabulary, up to 384 MB or
+ * 1,024 tokens, and fp32 sums of grad_hidden, up to 32 where there are few rows.  A call whose wait inside a kernel runs out, which none
+ * should, gives NaN, and so do later ones with its workspace until it is zeroed.)
  * ------------------------------------------------------------------------------------- */
 SARA_API size_t sara_linear_logprobs_workspace_bytes(int32_t R, int32_t d, int32_t V, int32_t backward);
 

@@ -1109,6 +1109,7 @@ inline int64_t lin_piece(int rows_cap, int d, int V, int ctas) {
 }
 inline LinPlan lin_plan(int R, int d, int V, bool backward) {
     LinPlan q{};
+    R = R > 1 ? R : 1;  // (no rows: a call has nothing to cut)
     q.ctas = R > kLinRows ? 2 : 1;
     const int tm = kLinRows * q.ctas, cols = kLinCols;
     q.rows_cap = (int)lin_up(R, tm);
