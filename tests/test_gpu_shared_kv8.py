@@ -138,3 +138,221 @@ def test_nan_reaches_its_rows_alone(pkg, hd, fmt):
                 assert bool(out[i].isnan().all()) and bool(lse[i].isnan().all()), (at, kv, how, i)
             else:
                 assert torch.equal(out[i], want[0][i]) and torch.equal(lse[i], want[1][i]), (at, kv, how, i)
+
+
+def _batch(pkg, rng, fmt="e4m3", typ="bf16", hd=64, H=8, kvh=2, blocks=6):
+    """Rows of no group before, between empty groups' places and behind, a group of one, groups of several."""
+    start = [2, 2, 7, 8, 8, 40, 45]
+    prefix = [100, 300, 200, 128, 513, 64]
+    n = 48
+    c = Cache(pkg, rng, n, blocks, kvh, hd, fmt)
+    ctx = rng.integers(0, 128 * blocks + 1, n)
+    ctx[9], ctx[10], ctx[11], ctx[12] = 0, 513, 512, 514
+    return c, _q(rng, n, H, hd, typ), ctx, start, prefix
+
+
+@pytest.mark.parametrize("typ", ["bf16", "fp16"])
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_windows_strides_and_rows_of_no_group(pkg, hd, fmt, typ):
+    import torch
+    rng = np.random.default_rng(hd + 3)
+    c, q, ctx, start, prefix = _batch(pkg, rng, fmt, typ, hd)
+    n, H = q.shape[:2]
+    # windows from in the prefix, at its end, behind it, at and behind the row's end
+    first = np.maximum(0, rng.choice([0, 1, 31, 33, 127, 128, 200, 300, 512, 513, 520, 700], n))
+    first[14], first[15], first[16], ctx[14], ctx[15], ctx[16] = 513, 512, 700, 600, 600, 650
+    wide = torch.full((n, 3 * H * hd + 8), float("nan"), dtype=q.dtype, device="cuda")
+    strided = wide[:, 8:8 + H * hd].view(n, H, hd)
+    strided.copy_(q)
+    out = torch.full_like(q, 7.0)
+    got, lse, status = _run(pkg, c, strided, ctx, start, prefix, first, out=out)
+    assert got is out and status == 0
+    _check(c, q, ctx, start, prefix, out, typ, first=first, lse=lse)
+    again = pkg.attention_shared_kv8(q, c.codes, c.scales, c.tab, _i32(ctx), _i32(start), _i32(prefix), first=_i32(first))
+    assert torch.equal(again, out)
+    alone, lse, status = _run(pkg, c, q, ctx, [0], [], first)  # no groups
+    assert status == 0
+    _check(c, q, ctx, [0], [], alone, typ, first=first, lse=lse)
+
+
+def test_the_others_tables_do_not_matter_in_the_prefix(pkg):
+    import torch
+    rng = np.random.default_rng(8)
+    n, prefix = 20, 500
+    c = Cache(pkg, rng, n, 6, 2, 128, "e4m3")
+    q = _q(rng, n, 8, 128, "bf16")
+    ctx = rng.integers(prefix, 700, n)
+    want = _run(pkg, c, q, ctx, [0, n], [prefix])
+    c.tab[1:, :3] = 1 << 30  # (pages wholly in the prefix)
+    got = _run(pkg, c, q, ctx, [0, n], [prefix])
+    assert got[2] == 0 and torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+@pytest.mark.parametrize("hd", [32, 128])
+def test_wrong_groups_prefixes_lengths_and_blocks_are_nan_and_reported(pkg, hd):
+    import torch
+    rng = np.random.default_rng(hd + 1)
+    c, q, ctx, start, prefix = _batch(pkg, rng, hd=hd)
+    n = len(ctx)
+    want = _run(pkg, c, q, ctx, start, prefix)
+    assert want[2] == 0
+    lead, shared = _groups(n, start, prefix)
+
+    def check(got, bad):
+        assert got[2] == pkg.SARA_EINVAL
+        for i in range(n):
+            if bad[i]:
+                assert bool(got[0][i].isnan().all()) and bool(got[1][i].isnan().all()), i
+            else:
+                assert torch.equal(got[0][i], want[0][i]) and torch.equal(got[1][i], want[1][i]), i
+
+    for wrong in ([2, 2, 1, 8, 8, 40, 45], [-1, 2, 7, 8, 8, 40, 45], [2, 2, 7, 8, 8, 40, 49], [2, 2, 7, 8, 1 << 30, 40, 45], [2, 2, 7, 8, -(1 << 31), 40, 45]):
+        check(_run(pkg, c, q, ctx, wrong, prefix), np.ones(n, bool))
+    for bad in (-1, 6 * 128 + 1, 2 ** 31 - 1, -2 ** 31):
+        check(_run(pkg, c, q, ctx, start, prefix[:4] + [bad] + prefix[5:]), (np.arange(n) >= 8) & (np.arange(n) < 40))
+    for bad in (-1, 6 * 128 + 1):
+        wrong = ctx.copy()
+        wrong[20] = bad
+        check(_run(pkg, c, q, wrong, start, prefix), np.arange(n) == 20)
+    for bad in (-1, c.codes.shape[0], 2 ** 31 - 1):
+        was = int(c.tab[8, 2])
+        c.tab[8, 2] = bad
+        check(_run(pkg, c, q, ctx, start, prefix), (np.arange(n) >= 8) & (np.arange(n) < 40) & (ctx > 256))
+        c.tab[8, 2] = was
+    assert torch.equal(_run(pkg, c, q, ctx, start, prefix)[0], want[0])
+
+
+@pytest.mark.parametrize("fmt,typ", [("e4m3", "fp16"), ("int8", "bf16")])
+def test_maxima_that_move_and_scales_without_weight(pkg, fmt, typ):
+    """Scores that rise and fall by hundreds from page to page, values' scales over 60 powers of two in either direction: the error is
+    bounded by the largest probability times scale, not by scales that no probability goes with."""
+    import torch
+    rng = np.random.default_rng(4)
+    n, prefix, blocks, hd = 40, 1500, 12, 64
+    c = Cache(pkg, rng, n, blocks, 1, hd, fmt)
+    c.scales[:, 0] *= torch.exp2(_i32(rng.integers(-2, 6, c.scales[:, 0].shape)).float())
+    c.scales[:, 1] = torch.exp2(_i32(rng.integers(-30, 31, c.scales[:, 1].shape)).float())
+    c.want_scales = c.scales.double().cpu().numpy()
+    q = _q(rng, n, 4, hd, typ)
+    ctx = rng.integers(prefix - 100, 1536, n)
+    out, lse, status = _run(pkg, c, q, ctx, [0, n], [prefix])
+    assert status == 0
+    got, qn = out.double().cpu().numpy(), q.double().cpu().numpy()
+    for i in range(n):
+        cut = min(prefix, ctx[i])
+        parts = [oracle.read(c.want_codes, c.want_scales, c.table[0], 0, cut), oracle.read(c.want_codes, c.want_scales, c.table[i], cut, max(ctx[i], cut))]
+        k, v = (np.concatenate([x[j] for x in parts]) for j in (0, 1))
+        want, wl, mag, pv = oracle.attention(qn[i], k, v)
+        z = np.einsum("hd,pd->hp", qn[i], k[:, 0]) / np.sqrt(hd)
+        p = np.exp(z - wl[:, None])
+        s = np.concatenate([c.want_scales[c.table[0]][:, 1, 0].reshape(-1)[:(cut + 31) // 32].repeat(32)[:cut],
+                            c.want_scales[c.table[i]][:, 1, 0].reshape(-1).repeat(32)[cut:max(ctx[i], cut)]])
+        ds = (hd + 24) * 2.0 ** -24 * mag[:, None]
+        tol = HALF_STEP[typ] * np.abs(want) + (2.0 ** -11 + 2 * ds + 2.0 ** -19 + (len(k) / 4 + 64) * 2.0 ** -24) * pv \
+            + len(k) * 2.0 ** -31 * 448 * (p * s).max(1)[:, None] + (2.0 ** -25 if typ == "fp16" else 0)
+        ok = np.abs(want) < 65504 if typ == "fp16" else np.ones(want.shape, bool)  # (fp16 holds no more)
+        assert (np.abs(got[i] - want)[ok] <= tol[ok]).all(), (i, np.max((np.abs(got[i] - want) / tol)[ok]))
+
+
+@pytest.mark.parametrize("typ", ["bf16", "fp16"])
+def test_queries_of_every_size(pkg, typ):
+    import torch
+    rng = np.random.default_rng(6)
+    n, prefix = 24, 400
+    c = Cache(pkg, rng, n, 4, 2, 128, "e4m3")
+    q = _q(rng, n, 8, 128, typ)
+    size = torch.exp2(_i32(np.arange(n) % 12 * 3 - 24).float()) if typ == "fp16" else torch.exp2(_i32((np.arange(n) % 12 - 10) * 12).float())
+    q = (q.float() * size[:, None, None]).to(q.dtype)
+    q[3] = 0
+    ctx = rng.integers(300, 512, n)
+    out, lse, status = _run(pkg, c, q, ctx, [0, n], [prefix])
+    assert status == 0
+    _check(c, q, ctx, [0, n], [prefix], out, typ, lse=lse)
+    broken = q.clone()  # of one sequence, and of one of its heads: the others do not notice
+    broken[5], broken[7, 2, 9], broken[8, 1, 0] = float("nan"), float("inf"), float("nan")
+    got, lse2, _ = _run(pkg, c, broken, ctx, [0, n], [prefix])
+    assert bool(got[5].isnan().all()) and bool(got[8, 1].isnan().all())
+    hit = torch.zeros(n, 8, dtype=torch.bool, device="cuda")
+    hit[5], hit[7, 2], hit[8, 1] = True, True, True
+    assert torch.equal(got[~hit], out[~hit]) and torch.equal(lse2[~hit], lse[~hit])
+
+
+def test_more_groups_than_a_block_plans_at_once(pkg):
+    rng = np.random.default_rng(7)
+    sizes = rng.integers(0, 3, 2300)
+    start = np.concatenate([[0], np.cumsum(sizes)])
+    n = int(start[-1])
+    prefix = rng.integers(0, 257, 2300)
+    prefix = prefix[:n] if len(prefix) > n else prefix
+    start = start[:len(prefix) + 1]
+    ctx = rng.integers(0, 257, n)
+    c = Cache(pkg, rng, 10, 2, 1, 32, "int8")
+    c.table = rng.integers(0, c.codes.shape[0], (n, 2)).astype(np.int32)
+    c.tab = _i32(c.table)
+    q = _q(rng, n, 3, 32, "fp16")
+    out, lse, status = _run(pkg, c, q, ctx, start, prefix)
+    assert status == 0
+    _check(c, q, ctx, start, prefix, out, "fp16", lse=lse, rows=np.unique(rng.integers(0, n, 400)))
+
+
+def test_a_cache_past_32_bits(pkg):
+    import torch
+    rng = np.random.default_rng(9)
+    n, prefix = 12, 300
+    c = Cache(pkg, rng, n, 4, 8, 128, "int8")
+    q = _q(rng, n, 16, 128, "bf16")
+    ctx = rng.integers(250, 512, n)
+    want = _run(pkg, c, q, ctx, [0, n], [prefix])
+    nb, many = c.codes.shape[0], (1 << 32) // (2 * 8 * 128 * 128) + 300
+    codes = torch.zeros((many, *c.codes.shape[1:]), dtype=c.codes.dtype, device="cuda")
+    scales = torch.full((many, *c.scales.shape[1:]), float("nan"), device="cuda")
+    codes[many - nb:], scales[many - nb:] = c.codes, c.scales
+    c.codes, c.scales, c.tab = codes, scales, c.tab + (many - nb)
+    got = _run(pkg, c, q, ctx, [0, n], [prefix])
+    assert got[2] == 0 and torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+def test_captured_on_another_stream_and_two_calls_at_once(pkg):
+    import torch
+    rng = np.random.default_rng(10)
+    c, q, ctx, start, prefix = _batch(pkg, rng, hd=128)
+    n, H = q.shape[:2]
+    args = [_i32(ctx), _i32(start), _i32(prefix)]
+    want, lse, _ = _run(pkg, c, q, ctx, start, prefix)
+    new = lambda: pkg.attention_shared_kv8_workspace(n + 5, len(prefix) + 2, H, 2, 128)  # noqa: E731  (room for more)
+    shared, streams = new(), [torch.cuda.Stream() for _ in range(2)]
+    graphs, outs = [torch.cuda.CUDAGraph() for _ in range(2)], [torch.zeros_like(q) for _ in range(2)]
+    q2 = torch.zeros_like(q)
+    for g, out, x in zip(graphs, outs, (q, q2)):  # two graphs that share a workspace, replayed in turn
+        with torch.cuda.graph(g, stream=streams[0]):
+            pkg.attention_shared_kv8(x, c.codes, c.scales, c.tab, *args, workspace=shared, out=out)
+    for _ in range(3):
+        q2.copy_(q.flip(0) if _ == 1 else q)
+        for g in graphs:
+            g.replay()
+        assert torch.equal(outs[0], want)
+        assert torch.equal(outs[1], want) == (_ != 1)
+    spaces = [new() for _ in range(2)]
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(10):  # two streams, each its own workspace
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):
+                outs[k].append(pkg.attention_shared_kv8(q, c.codes, c.scales, c.tab, *args, workspace=spaces[k]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, want) for k in range(2) for x in outs[k])
+
+
+def test_the_same_sequence_in_every_row(pkg):
+    import torch
+    rng = np.random.default_rng(11)
+    n = 33
+    c = Cache(pkg, rng, 1, 5, 2, 64, "e4m3")
+    c.table = np.repeat(c.table, n, 0)
+    c.tab = _i32(c.table)
+    q = _q(rng, 1, 8, 64, "fp16").expand(n, 8, 64).contiguous()
+    out, lse, status = _run(pkg, c, q, [600] * n, [0, n], [555])
+    assert status == 0 and bool((out == out[0]).all()) and bool((lse == lse[0]).all())
+    _check(c, q, [600] * n, [0, n], [555], out, "fp16", lse=lse, rows=[0])
+    assert pkg.attention_shared_kv8(q[:0], c.codes, c.scales, c.tab[:0], _i32([]), _i32([0]), _i32([])).shape == (0, 8, 64)
