@@ -73,6 +73,9 @@ struct AttnKv8Params {
     float *part;  // [share][2] states
     int n, H, type;
     float scale_log2;  // log2(e) / sqrt(hd)
+    // GROUPS: positions before prefix[g] of rows start[g] .. start[g + 1] - 1 stand in the table row of the first of them
+    const int32_t *start, *prefix;
+    int groups;
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -118,15 +121,45 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void *src) {
 struct AttnKv8Row {
     int first, ctx, step0, steps;
     bool bad;
+    // GROUPS: positions before `cut` are in row `lead` of the table, and have the steps before `turn`; the step that holds some of either is
+    // in the list twice
+    int cut, lead, turn, twice;
 };
-template <int STEP>
-__device__ __forceinline__ AttnKv8Row attn_kv8_row(const AttnKv8Params &p, int i) {
+// wrong: (GROUPS) what says whose rows are whose is
+template <int STEP, bool GROUPS>
+__device__ __forceinline__ AttnKv8Row attn_kv8_row(const AttnKv8Params &p, int i, bool wrong) {
     AttnKv8Row r;
     r.ctx = __ldg(p.ctx + i);
     r.first = p.first ? min(__ldg(p.first + i), r.ctx) : 0;  // (past the end: no position)
     r.bad = r.ctx < 0 || r.first < 0 || r.ctx > (int64_t)p.c.max_blocks * kKv8Page;
     r.step0 = r.first / STEP;
     r.steps = r.bad || r.ctx <= r.first ? 0 : (r.ctx - 1) / STEP - r.step0 + 1;
+    if constexpr (GROUPS) {
+        r.cut = r.first;
+        r.lead = i;
+        r.turn = r.step0;
+        r.twice = 0;
+        int lo = 0, hi = p.groups;  // the last group that begins at i or before
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (__ldg(p.start + mid) <= i) lo = mid + 1;
+            else hi = mid;
+        }
+        if (lo > 0 && !wrong && i < __ldg(p.start + lo)) {
+            const int shared = __ldg(p.prefix + lo - 1);
+            wrong = shared < 0 || shared > (int64_t)p.c.max_blocks * kKv8Page;
+            r.lead = __ldg(p.start + lo - 1);
+            if (r.steps && r.lead != i) r.cut = min(max(shared, r.first), r.ctx);
+        }
+        if (wrong) {
+            r.bad = true;
+            r.steps = 0;
+        } else if (r.cut > r.first) {
+            r.turn = (r.cut - 1) / STEP + 1;
+            r.twice = r.cut < r.ctx && r.cut % STEP != 0;
+            r.steps += r.twice;
+        }
+    }
     return r;
 }
 
@@ -267,8 +300,8 @@ __device__ __forceinline__ void attn_kv8_join(AttnKv8Group<HD, W> u, float *room
     }
 }
 
-// W: warps of a share
-template <int HD, int FMT, int W>
+// W: warps of a share; GROUPS: rows may share their first positions
+template <int HD, int FMT, int W, bool GROUPS = false>
 __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kernel(AttnKv8Params p) {
     constexpr int KW = HD / 16, VW = HD / 32, NT = HD / 16;  // words a lane of a key row, of a value row; output tiles
     constexpr int KL = KW < 4 ? KW : 4;                      // words a load
@@ -284,6 +317,15 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
     auto &s_last = s_lasts[mine];
     const int KVH = p.c.KVH, G = p.H / KVH;
     const float nan = __int_as_float(0x7fc00000);
+    bool no_groups = false;  // (wrong ones)
+    if constexpr (GROUPS) {
+        for (int g = tid; g < p.groups; g += kAttnKv8Threads) {
+            const int a = __ldg(p.start + g), b = __ldg(p.start + g + 1);
+            no_groups = no_groups || a < 0 || b < a || b > p.n;
+        }
+        no_groups = __syncthreads_or(no_groups);
+    }
+    auto row_of = [&](int i) { return attn_kv8_row<STEP, GROUPS>(p, i, no_groups); };
 
     // this share lo .. hi of the list, and the row in which it begins: up to 32 rows by every warp for itself, more in 32 parts,
     // 8 a warp (every warp all by itself took 94 us for 88 at 700 rows)
@@ -293,7 +335,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
     int steps = 0, total = 0;
     bool idle = false;  // a row without a position (or a wrong one) that is this CTA's to write
     auto steps_of = [&](int i) {
-        const int y = i < p.n ? attn_kv8_row<STEP>(p, i).steps : 0;
+        const int y = i < p.n ? row_of(i).steps : 0;
         idle = idle || (i < p.n && y == 0 && (unsigned)i % gridDim.x == blockIdx.x);
         return y;
     };
@@ -318,7 +360,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
     total = __reduce_add_sync(0xffffffffu, total);
     if (idle) {
         for (int i = blockIdx.x; i < p.n; i += gridDim.x) {
-            const AttnKv8Row r = attn_kv8_row<STEP>(p, i);
+            const AttnKv8Row r = row_of(i);
             if (r.steps) continue;
             const float y = r.bad ? nan : 0.f;
             const uint32_t y2 = p.type == SARA_BF16 ? pack2<SARA_BF16>(y, y) : pack2<SARA_FP16>(y, y);
@@ -352,7 +394,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
     };
     if (many) {
         row = find(part) * deep * 32;
-        for (int k = 32; k == 32; row += k) k = find(row + lane < p.n ? attn_kv8_row<STEP>(p, row + lane).steps : 0);
+        for (int k = 32; k == 32; row += k) k = find(row + lane < p.n ? row_of(row + lane).steps : 0);
     } else {
         row = find(steps);
     }
@@ -370,18 +412,27 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
     static_assert(RING % 128 == 0, "lines");
     const uint32_t ring = smem_u32(s_ring) + (tid >> 5) * RING;
     const uint32_t ring_s = smem_u32(s_ring) + kAttnKv8Warps * RING + (tid >> 5) * (S * 16);
-    AttnKv8Row r = attn_kv8_row<STEP>(p, row), lr = r;
+    AttnKv8Row r = row_of(row), lr = r;
     int h = (lo - base) / r.steps, unit = base + h * r.steps;  // KV head; the first entry of the (row, KV head)
     int l_row = row, l_h = h - 1, l_unit = unit - r.steps, l_x = 0, l_end = 0, fill = 0;
     // this warp's steps of a unit in this share, x .. end: of a step x it has positions STEP x + POS warp .. + POS - 1, the row's
     // first and last step may have none of them
+    // (GROUPS: before the turn of those from r.first on, behind it of those up to r.ctx)
+    auto behind_turn = [&](const AttnKv8Row &r, int x) { return GROUPS && x >= r.turn; };
     auto range = [&](const AttnKv8Row &r, int unit, int &x, int &end) {
         x = r.step0 + max(lo - unit, 0);
         end = r.step0 + min(r.steps, hi - unit);
+        if constexpr (GROUPS) {
+            const bool a = behind_turn(r, x), b = behind_turn(r, end - 1);
+            const int from = (a ? r.cut : r.first) - (x - (a ? r.twice : 0)) * STEP, to = (b ? r.ctx : r.cut) - (end - 1 - (b ? r.twice : 0)) * STEP;
+            if (from >= POS * (warp + 1)) ++x;
+            if (POS * warp >= to) --end;
+            return;
+        }
         if (r.first - x * STEP >= POS * (warp + 1)) ++x;
         if ((end - 1) * STEP + POS * warp >= r.ctx) --end;
     };
-    int ids = 0, idbase = -32;  // this lane's entry of the 32 table entries from idbase on
+    int ids = 0, idbase = -32, idrow = -1;  // this lane's entry of the 32 table entries from idbase on (GROUPS: of row idrow)
     bool wrong = false;
     // Where 16 bytes of a tile stand: rows fill lines of 128 bytes, whose eight pieces are exchanged so that the lanes that read at a time
     // meet all banks
@@ -398,28 +449,39 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             l_unit += lr.steps;
             if (++l_h == KVH) {
                 l_h = 0;
-                do lr = attn_kv8_row<STEP>(p, ++l_row);
+                do lr = row_of(++l_row);
                 while (lr.steps == 0);
                 idbase = -32;
             }
             range(lr, l_unit, l_x, l_end);
         }
         if (l_x < l_end) {
-            const int page = l_x / PS;
+            int l_s = l_x, l_first = lr.first, l_ctx = lr.ctx, l_steps = lr.step0 + lr.steps, l_from = l_row;
+            if constexpr (GROUPS) {  // (behind its turn a row has its own positions, in its own row of the table)
+                const bool own = behind_turn(lr, l_x);
+                l_s = own ? l_x - lr.twice : l_x;
+                l_first = own ? lr.cut : lr.first;
+                l_ctx = own ? lr.ctx : lr.cut;
+                l_steps = own ? l_steps - lr.twice : lr.turn;
+                l_from = own ? l_row : lr.lead;
+                if (l_from != idrow) idbase = -32;
+                idrow = l_from;
+            }
+            const int page = l_s / PS;
             if ((unsigned)(page - idbase) >= 32u) {  // (a row's next head finds them here where there are not many)
                 idbase = page;
-                ids = (page + lane) * PS < lr.step0 + lr.steps ? __ldg(p.c.table + l_row * p.c.table_stride + page + lane) : 0;
+                ids = (page + lane) * PS < l_steps ? __ldg(p.c.table + l_from * p.c.table_stride + page + lane) : 0;
                 const bool out = ids < 0 || ids >= p.c.n_blocks;
                 wrong = wrong || out;
                 ids = out ? -1 : ids;
             }
-            const int block = __shfl_sync(0xffffffffu, ids, page - idbase), p0 = l_x * STEP + POS * warp;
+            const int block = __shfl_sync(0xffffffffu, ids, page - idbase), p0 = l_s * STEP + POS * warp;
             const uint32_t to = ring + put + fill * (2 * TILE), to_v = ring + put_v + fill * (2 * TILE), to_s = ring_s + fill * 16;
             const uint32_t to_v1 = HD == 128 ? to_v ^ 64 : to_v;
             if (block >= 0) {
                 const int64_t tile = kv8_tile(p.c, block, 0, l_h);
                 const uint8_t *src = p.c.codes + (tile * kKv8Page + (p0 & (kKv8Page - 1))) * HD + 16 * lane, *src_v = src + v_behind;
-                if (p0 >= lr.first && p0 <= lr.ctx - POS) {
+                if (p0 >= l_first && p0 <= l_ctx - POS) {
 #pragma unroll
                     for (int i = 0; i < LC; ++i) {
                         cp_async16(to + 512 * i, src + 512 * i);
@@ -428,12 +490,14 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
                 } else {  // masked positions stand for the nearest that is not: their probability is 0
 #pragma unroll 1
                     for (int i = 0; i < LC; ++i) {
-                        const int at = lane / CHUNKS + i * (32 / CHUNKS), off = (min(max(p0 + at, lr.first), lr.ctx - 1) - p0 - lane / CHUNKS) * HD;
+                        const int at = lane / CHUNKS + i * (32 / CHUNKS), off = (min(max(p0 + at, l_first), l_ctx - 1) - p0 - lane / CHUNKS) * HD;
                         cp_async16(to + 512 * i, src + off);
                         cp_async16(i & 1 ? to_v1 + 512 * i : to_v + 512 * i, src_v + off);
                     }
                 }
-                if (lane < 2) cp_async4(to_s + 4 * lane, p.c.scales + (tile + lane * KVH) * kKv8PageBlocks + (p0 & (kKv8Page - 1)) / kKv8Block);
+                // (GROUPS: of a position that is not masked, there may be none in the warp's)
+                const int at_s = GROUPS ? min(max(p0, l_first), l_ctx - 1) : p0;
+                if (lane < 2) cp_async4(to_s + 4 * lane, p.c.scales + (tile + lane * KVH) * kKv8PageBlocks + (at_s & (kKv8Page - 1)) / kKv8Block);
             } else if (lane < 2) {
                 asm volatile("st.shared.f32 [%0], %1;" ::"r"(to_s + 4 * lane), "f"(nan) : "memory");
             }
@@ -536,13 +600,19 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[n][e] = (s[n][e] + s2[e]) * (e & 1 ? f1 : f0);
             }
-            const int p0 = x * STEP + POS * warp;
-            if (p0 < r.first || p0 > r.ctx - POS) {  // some are masked
+            int p0 = x * STEP + POS * warp, w_first = r.first, w_ctx = r.ctx;
+            if constexpr (GROUPS) {
+                const bool own = behind_turn(r, x);
+                p0 -= own ? r.twice * STEP : 0;
+                w_first = own ? r.cut : r.first;
+                w_ctx = own ? r.ctx : r.cut;
+            }
+            if (p0 < w_first || p0 > w_ctx - POS) {  // some are masked
 #pragma unroll
                 for (int n = 0; n < NG; ++n) {
                     const int at = p0 + 16 * n + g;
-                    if (at < r.first || at >= r.ctx) s[n][0] = s[n][1] = -INFINITY;
-                    if (at + 8 < r.first || at + 8 >= r.ctx) s[n][2] = s[n][3] = -INFINITY;
+                    if (at < w_first || at >= w_ctx) s[n][0] = s[n][1] = -INFINITY;
+                    if (at + 8 < w_first || at + 8 >= w_ctx) s[n][2] = s[n][3] = -INFINITY;
                 }
             }
             float w[NG][4], t0 = 0.f, t1 = 0.f;
@@ -644,7 +714,7 @@ __global__ void __launch_bounds__(kAttnKv8Threads, kAttnKv8SmCtas) attn_kv8_kern
             unit += r.steps;
             if (++h == KVH) {
                 h = 0;
-                do r = attn_kv8_row<STEP>(p, ++row);
+                do r = row_of(++row);
                 while (r.steps == 0);
             }
             begin();
@@ -743,7 +813,7 @@ inline int attn_kv8_warps(int n, int kvh, int hd, int max_blocks) {
     return (int64_t)n * kvh >= kAttnKv8Units && attn_kv8_entries(n, kvh, max_blocks, attn_kv8_step(hd, 1)) <= INT32_MAX ? 1 : kAttnKv8Warps;
 }
 inline size_t attn_kv8_count_bytes() { return kAttnKv8MaxShares * 2 * kAttnKv8Levels * sizeof(int); }
-// The kernel for p's operands, shared with the attention behind a common prefix
+// The kernel for p's operands, shared with the attention behind a common prefix (which gives groups to shares of CTAs only)
 void attn_kv8_launch(const sara_kv8_cache *cache, const AttnKv8Params &p, int warps, cudaStream_t s);
 inline size_t attn_kv8_workspace(int hd, int warps) {
     return attn_kv8_count_bytes() + (size_t)kAttnKv8MaxShares / warps * 2 * attn_kv8_state(hd) * sizeof(float);

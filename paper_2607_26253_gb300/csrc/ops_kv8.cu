@@ -35,7 +35,8 @@ void sara::attn_kv8_launch(const sara_kv8_cache *cache, const AttnKv8Params &p, 
     const int64_t entries = attn_kv8_entries(p.n, cache->n_kv_heads, cache->max_blocks, attn_kv8_step(cache->head_dim, warps));
     const unsigned ctas = (unsigned)std::min<int64_t>(std::min(kAttnKv8SmCtas * sm_count(), kAttnKv8MaxCtas), (entries + kAttnKv8Warps / warps - 1) / (kAttnKv8Warps / warps));
     by_shape(cache, [&](auto hd, auto fmt) {
-        const auto kern = warps == 1 ? attn_kv8_kernel<hd.value, fmt.value, 1> : attn_kv8_kernel<hd.value, fmt.value, kAttnKv8Warps>;
+        const auto kern = p.groups ? attn_kv8_kernel<hd.value, fmt.value, kAttnKv8Warps, true>
+                          : warps == 1 ? attn_kv8_kernel<hd.value, fmt.value, 1> : attn_kv8_kernel<hd.value, fmt.value, kAttnKv8Warps>;
         static_assert(attn_kv8_smem(hd.value) <= 48 * 1024, "more would have to be asked for");
         kern<<<ctas, kAttnKv8Threads, attn_kv8_smem(hd.value), s>>>(p);
     });

@@ -45,6 +45,11 @@ T *at(void *ws, size_t off) {
     return reinterpret_cast<T *>(static_cast<uint8_t *>(ws) + off);
 }
 
+// Whether each row reads all of its positions by itself: in one launch of the decode attention
+bool shared_alone(int n, int groups, int kvh, int hd, int max_blocks) {
+    return groups == 0 || ((int64_t)n * kvh < kAttnKv8Units && (int64_t)n * kvh * max_blocks * (kKv8Page * 2 * hd) <= kSharedAlone);
+}
+
 template <int HD, int FMT>
 void shared_launch(const SharedParams &p, int shares, cudaStream_t s) {
     const auto kern = shared_prefix_kernel<HD, FMT>;
@@ -85,10 +90,31 @@ int sara_attention_shared_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
         const SharedLayout w = shared_layout(n_seq, n_groups, n_heads, cache->n_kv_heads, hd);
         if (workspace_bytes < w.bytes) throw SaraError(SARA_EINVAL, "workspace too small");
         cudaStream_t s = static_cast<cudaStream_t>(stream);
-        const int sms = sm_count(), shares = std::min(sms, kSharedMaxShares);
+        AttnKv8Params a{};
+        a.c = device_cache(cache);
+        a.q = static_cast<const uint16_t *>(q);
+        a.q_stride = q_stride;
+        a.ctx = ctx;
+        a.status = status;
+        a.n = n_seq;
+        a.H = n_heads;
+        a.type = type;
+        a.count = at<int>(workspace, w.own);
+        a.part = reinterpret_cast<float *>(at<uint8_t>(workspace, w.own) + attn_kv8_count_bytes());
+        a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)hd));
+        if (shared_alone(n_seq, n_groups, cache->n_kv_heads, hd, cache->max_blocks)) {
+            a.first = first;
+            a.out = static_cast<uint16_t *>(out);
+            a.lse = lse;
+            a.start = group_start;
+            a.prefix = prefix;
+            a.groups = n_groups;
+            attn_kv8_launch(cache, a, warps, s);
+            return;
+        }
         SharedParams p{};
-        p.c = device_cache(cache);
-        p.q = static_cast<const uint16_t *>(q);
+        p.c = a.c;
+        p.q = a.q;
         p.q_stride = q_stride;
         p.ctx = ctx;
         p.first = first;
@@ -98,7 +124,7 @@ int sara_attention_shared_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
         p.groups = n_groups;
         p.H = n_heads;
         p.type = type;
-        p.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)hd));
+        p.scale_log2 = a.scale_log2;
         p.status = status;
         p.plan = at<SharedPlan>(workspace, 0);
         p.group = at<SharedGroup>(workspace, w.group);
@@ -107,29 +133,18 @@ int sara_attention_shared_kv8(const sara_kv8_cache *cache, int32_t n_seq, int32_
         p.row_prefix = at<int>(workspace, w.row_prefix);
         p.whole = at<float>(workspace, w.whole);
         p.part = at<float>(workspace, w.part);
-        p.max_shares = shares;
         p.own = at<float>(workspace, w.out32);
         p.own_lse = at<float>(workspace, w.lse);
         p.out = static_cast<uint16_t *>(out);
         p.lse = lse;
+        const int shares = std::min(sm_count(), kSharedMaxShares);
+        p.max_shares = shares;
         shared_plan_kernel<<<1, 1024, 0, s>>>(p);
         CK(cudaGetLastError());
-        if (n_groups > 0) by_shape(cache, [&](auto d, auto fmt) { shared_launch<d.value, fmt.value>(p, shares, s); });
-        AttnKv8Params a{};
-        a.c = p.c;
-        a.q = p.q;
-        a.q_stride = q_stride;
-        a.ctx = ctx;
+        by_shape(cache, [&](auto d, auto fmt) { shared_launch<d.value, fmt.value>(p, shares, s); });
         a.first = p.row_first;
         a.out32 = at<float>(workspace, w.out32);
         a.lse = at<float>(workspace, w.lse);
-        a.status = status;
-        a.n = n_seq;
-        a.H = n_heads;
-        a.type = type;
-        a.count = at<int>(workspace, w.own);
-        a.part = reinterpret_cast<float *>(at<uint8_t>(workspace, w.own) + attn_kv8_count_bytes());
-        a.scale_log2 = p.scale_log2;
         attn_kv8_launch(cache, a, warps, s);
         by_shape(cache, [&](auto d, auto) { shared_join<d.value>(p, shares, s); });
     });

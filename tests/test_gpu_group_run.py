@@ -6,6 +6,7 @@ import pytest
 import test_gpu_linear_logprobs as linear
 import test_gpu_shared_kv8 as shared
 from test_gpu_kv8 import Cache, _i32, _q, _tokens
+from test_gpu_shared_kv8 import route  # noqa: F401  (both)
 
 pytestmark = pytest.mark.gpu
 
@@ -48,11 +49,12 @@ def test_decode_then_score_then_gradient(pkg, sizes, H, kvh, hd, V, fmt, typ):
     tok[::7] = -1
     g, gh = (torch.from_numpy(rng.standard_normal(n)).float().cuda() for _ in range(2))
     args = _i32(ctx), _i32(start), _i32(prompt), _i32(tok)
+    tab = shared._table(c)
     ws = pkg.attention_shared_kv8_workspace(n, len(sizes), H, kvh, hd)
     ws1, ws2 = (pkg.linear_logprobs_workspace(n, H * hd, V, back) for back in (False, True))
 
     def run():
-        out = pkg.attention_shared_kv8(q, c.codes, c.scales, c.tab, *args[:3], workspace=ws)
+        out = pkg.attention_shared_kv8(q, c.codes, c.scales, tab, *args[:3], workspace=ws)
         hidden = out.view(n, H * hd)
         s = pkg.linear_logprobs(hidden, w, args[3], scale=2.0, workspace=ws1)
         return out, s, pkg.linear_logprobs_backward(hidden, w, args[3], s.stats, s.entropy, g, gh, scale=2.0, workspace=ws2)
