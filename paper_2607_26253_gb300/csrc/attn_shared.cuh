@@ -35,7 +35,7 @@ __host__ __device__ constexpr int shared_smem(int hd) {
 __host__ __device__ constexpr int shared_state(int hd) { return hd + 4; }
 constexpr float kSharedShift = 6.f;                 // log2 of the products' scale
 constexpr int kSharedMaxShares = 160;               // CTAs, one an SM
-constexpr int64_t kSharedAlone = 64 << 20;
+constexpr double kSharedAlone = 160 << 20;         // bytes that it does not pay to share
 constexpr int kSharedWideJoin = 1216;               // queries up to which 8 warps join a query
 
 struct SharedGroup {

@@ -45,9 +45,16 @@ T *at(void *ws, size_t off) {
     return reinterpret_cast<T *>(static_cast<uint8_t *>(ws) + off);
 }
 
-// Whether each row reads all of its positions by itself: in one launch of the decode attention
+// Whether each row reads all of its positions by itself, in one launch of the decode attention.  Four launches cost some 15 us more, and the
+// prefix kernel takes a page in twice the time that reading it takes: with k rows to a group, of which a share f is common, it saves
+// f (1 - 2 / k) of the bytes' time, nothing for pairs.  The lengths are on the device: the bytes are those that the table's rows have room
+// for.  us alone and shared, half of all positions common (where two are given: and 9 of 10), 128 dims: k = 2, 512 MB 102, 119 (2 GB: 324,
+// 352); k = 3, 384 MB 72, 86 (79), 768 MB 130, 136 (120); k = 4, 256 MB 57, 66 (56), 512 MB 94, 97 (83); k = 8, 64 MB 24, 35 (34), 128 MB
+// 33, 42 (36); k = 16, 128 MB 32, 37 (34), 256 MB 50, 56 (40); k = 64, 128 MB 32, 41 (33), 256 MB 50, 57 (39); alike in 64 and 32 dims.
 bool shared_alone(int n, int groups, int kvh, int hd, int max_blocks) {
-    return groups == 0 || ((int64_t)n * kvh < kAttnKv8Units && (int64_t)n * kvh * max_blocks * (kKv8Page * 2 * hd) <= kSharedAlone);
+    const int64_t blocks = (int64_t)n * kvh * max_blocks;
+    if (blocks > 1 << 28) return false;  // (steps are counted in 32 bits)
+    return n <= 2 * (int64_t)groups || groups == 0 || (double)blocks * (kKv8Page * 2 * hd) * (1. - 2. * groups / n) <= kSharedAlone;
 }
 
 template <int HD, int FMT>

@@ -49,7 +49,7 @@ def test_decode_then_score_then_gradient(pkg, sizes, H, kvh, hd, V, fmt, typ):
     tok[::7] = -1
     g, gh = (torch.from_numpy(rng.standard_normal(n)).float().cuda() for _ in range(2))
     args = _i32(ctx), _i32(start), _i32(prompt), _i32(tok)
-    tab = shared._table(c)
+    tab = shared._table(c, len(sizes))
     ws = pkg.attention_shared_kv8_workspace(n, len(sizes), H, kvh, hd)
     ws1, ws2 = (pkg.linear_logprobs_workspace(n, H * hd, V, back) for back in (False, True))
 

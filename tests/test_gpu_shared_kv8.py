@@ -18,7 +18,7 @@ def pkg():
     return p
 
 
-ALONE = 1 << 26  # bytes that the table's rows have room for up to which every row attends by itself
+ALONE = 160 << 20  # bytes that the table's rows have room for, less those of two rows a group, up to which every row attends by itself
 
 
 @pytest.fixture(params=["alone", "shared"], autouse=True)
@@ -27,10 +27,10 @@ def route(request, monkeypatch):
     monkeypatch.setattr(Cache, "wide", request.param == "shared", raising=False)
 
 
-def _table(c):
+def _table(c, groups):
     import torch
     n = len(c.tab)
-    more = max(0, ALONE // (n * c.kvh * 256 * c.hd) + 1 - c.tab.shape[1]) if c.wide and n else 0
+    more = max(0, ALONE // ((n - 2 * groups) * c.kvh * 256 * c.hd) + 1 - c.tab.shape[1]) if c.wide and n > 2 * groups else 0
     return torch.cat([c.tab, torch.full((n, more), -7, dtype=torch.int32, device="cuda")], 1)
 
 
@@ -69,7 +69,7 @@ def _check(c, q, ctx, start, prefix, out, typ, first=None, lse=None, rows=None):
 def _run(pkg, c, q, ctx, start, prefix, first=None, **kw):
     import torch
     lse, status = torch.empty(q.shape[:2], device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
-    out = pkg.attention_shared_kv8(q, c.codes, c.scales, _table(c), _i32(ctx), _i32(start), _i32(prefix), first=None if first is None else _i32(first),
+    out = pkg.attention_shared_kv8(q, c.codes, c.scales, _table(c, len(prefix)), _i32(ctx), _i32(start), _i32(prefix), first=None if first is None else _i32(first),
                                    lse=lse, status=status, **kw)
     return out, lse, int(status)
 
@@ -147,7 +147,7 @@ def test_nan_reaches_its_rows_alone(pkg, hd, fmt):
             codes[page, kv, :, slot, hd // 2] = 0xff
             hit = (first < at // 32 * 32 + 32) & (np.minimum(ctx, prefix) > at // 32 * 32) & (first < ctx)
         lse, status = torch.empty((n, 12), device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
-        out = pkg.attention_shared_kv8(q, codes.view(c.codes.dtype), scales, _table(c), _i32(ctx), _i32([0, n]), _i32([prefix]), first=_i32(first), lse=lse, status=status)
+        out = pkg.attention_shared_kv8(q, codes.view(c.codes.dtype), scales, _table(c, 1), _i32(ctx), _i32([0, n]), _i32([prefix]), first=_i32(first), lse=lse, status=status)
         assert int(status) == 0
         for i in range(n):
             if hit[i]:
@@ -186,7 +186,7 @@ def test_windows_strides_and_rows_of_no_group(pkg, hd, fmt, typ):
     got, lse, status = _run(pkg, c, strided, ctx, start, prefix, first, out=out)
     assert got is out and status == 0
     _check(c, q, ctx, start, prefix, out, typ, first=first, lse=lse)
-    again = pkg.attention_shared_kv8(q, c.codes, c.scales, _table(c), _i32(ctx), _i32(start), _i32(prefix), first=_i32(first))
+    again = pkg.attention_shared_kv8(q, c.codes, c.scales, _table(c, len(prefix)), _i32(ctx), _i32(start), _i32(prefix), first=_i32(first))
     assert torch.equal(again, out)
     alone, lse, status = _run(pkg, c, q, ctx, [0], [], first)  # no groups
     assert status == 0
@@ -224,7 +224,7 @@ def test_wrong_groups_prefixes_lengths_and_blocks_are_nan_and_reported(pkg, hd):
 
     for wrong in ([2, 2, 1, 8, 8, 40, 45], [-1, 2, 7, 8, 8, 40, 45], [2, 2, 7, 8, 8, 40, 49], [2, 2, 7, 8, 1 << 30, 40, 45], [2, 2, 7, 8, -(1 << 31), 40, 45]):
         check(_run(pkg, c, q, ctx, wrong, prefix), np.ones(n, bool))
-    most = _table(c).shape[1] * 128
+    most = _table(c, len(prefix)).shape[1] * 128
     for bad in (-1, most + 1, 2 ** 31 - 1, -2 ** 31):
         check(_run(pkg, c, q, ctx, start, prefix[:4] + [bad] + prefix[5:]), (np.arange(n) >= 8) & (np.arange(n) < 40))
     for bad in (-1, most + 1):
@@ -294,9 +294,10 @@ def test_queries_of_every_size(pkg, typ):
     assert torch.equal(got[~hit], out[~hit]) and torch.equal(lse2[~hit], lse[~hit])
 
 
-def test_more_groups_than_a_block_plans_at_once(pkg):
+@pytest.mark.parametrize("most", [2, 7])
+def test_more_groups_than_a_block_plans_at_once(pkg, most):
     rng = np.random.default_rng(7)
-    sizes = rng.integers(0, 3, 2300)
+    sizes = rng.integers(0, most + 1, 2300)
     start = np.concatenate([[0], np.cumsum(sizes)])
     n = int(start[-1])
     prefix = rng.integers(0, 257, 2300)
@@ -334,7 +335,7 @@ def test_captured_on_another_stream_and_two_calls_at_once(pkg):
     rng = np.random.default_rng(10)
     c, q, ctx, start, prefix = _batch(pkg, rng, hd=128)
     n, H = q.shape[:2]
-    args = [_table(c), _i32(ctx), _i32(start), _i32(prefix)]
+    args = [_table(c, len(prefix)), _i32(ctx), _i32(start), _i32(prefix)]
     want, lse, _ = _run(pkg, c, q, ctx, start, prefix)
     new = lambda: pkg.attention_shared_kv8_workspace(n + 5, len(prefix) + 2, H, 2, 128)  # noqa: E731  (room for more)
     shared, streams = new(), [torch.cuda.Stream() for _ in range(2)]
