@@ -62,6 +62,7 @@ __host__ __device__ constexpr size_t lin_smem(int ctas, bool staged) {
     return 1024 + (size_t)lin_stages(ctas, staged) * lin_stage_bytes(ctas) + (staged ? 4 : 0) * kLinBlock;
 }
 constexpr int kLinDwCost = 9;
+constexpr int kLinNoToken = 1 << 30;  // (behind every token)
 constexpr int kLinHits = 8;  // rows of a tile of tokens that wait in shared memory for dW's epilogue
 
 struct LinParams {
@@ -775,15 +776,26 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                             if (match >> x & 1) add(f, E.row[mine][buf][x]);
                         }
                     }
-                    if (now.n > kLinHits || blocks > 1) {  // the others, in their order
+                    // the others, in their order, each thread its token's (5,027 rows of 512 tokens, dW of 96 columns: 86 us, 422 with a look at all of the
+                    // tile's; a warp together for a token's, 4 columns a lane, costs registers: 164, and 301 rows' dW 136 -> 146, while 4,096 rows of one token
+                    // take 4.1 ms instead of 7.4)
+                    if (now.n > kLinHits || blocks > 1) {
 #pragma unroll 1
                         for (int b = 0; b < blocks; ++b) {
                             const int *start = p.start + (int64_t)b * (p.buckets + 1) + (p.v0 + j.m0 + rank * kLinRows) / kLinRows;
                             if (token >= p.V) break;
+                            int x = start[0] + (b == 0 ? kLinHits : 0), end = start[1];
+                            const int2 *sorted = p.sorted + (int64_t)b * kLinSort;
+                            for (int high = end; x < high;) {  // the first of the token's
+                                const int mid = (x + high) / 2;
+                                if (sorted[mid].y < token) x = mid + 1;
+                                else high = mid;
+                            }
 #pragma unroll 1
-                            for (int x = start[0] + (b == 0 ? kLinHits : 0); x < start[1]; ++x) {
-                                const int2 r = p.sorted[b * kLinSort + x];
-                                if (r.y == token) add(p.delta[r.x], p.low + (int64_t)r.x * p.d + j.n0 + c0);
+                            for (; x < end; ++x) {
+                                const int2 r = sorted[x];
+                                if (r.y != token) break;
+                                add(p.delta[r.x], p.low + (int64_t)r.x * p.d + j.n0 + c0);
                             }
                         }
                     }
@@ -891,7 +903,7 @@ __global__ void __launch_bounds__(1024) lin_rows_kernel(LinRowParams p) {
 
 // The live rows side by side, zeros behind them up to a whole tile; in fp16, for dW, once more, each lowered by what its dZ is raised more
 // than the least: rows whose gradients are far below the largest's lose bits that would not reach dW's either.
-// The CTAs behind those put the rows in the order of their tokens' tiles of 128 (and of the rows within one), `kLinSort` rows at a time, so that
+// The CTAs behind those put the rows in the order of their tokens (and of the rows of one), `kLinSort` rows at a time, so that
 // dW's epilogue finds a tile's: sorted[start[b] .. start[b + 1]) are those of tile b.  A row's place is the number of rows before it, counted
 // by 8 lanes.
 struct LinGatherParams {
@@ -915,13 +927,14 @@ __global__ void __launch_bounds__(256) lin_gather_kernel(LinGatherParams p) {
         if (blockIdx.y) return;
         const int blocks = max((live + kLinSort - 1) / kLinSort, 1), part = threadIdx.x & 7;
         const int64_t asks = (int64_t)blocks * (p.buckets + 1) + live, stride = (int64_t)(gridDim.x - p.row_ctas) * 32;
-        __shared__ __align__(16) int s_bucket[2048];
+        __shared__ __align__(16) int s_key[2048];
         for (int64_t q0 = (int64_t)(blockIdx.x - p.row_ctas) * 32; q0 < asks; q0 += stride) {  // (whole CTAs)
             const int64_t q = q0 + threadIdx.x / 8;
             const bool row = q < live;
             const int64_t y = q - live;
             const int me = row ? (int)q : 0, block = row ? me / kLinSort : (int)min(y / (p.buckets + 1), (int64_t)(blocks - 1));
-            const int token = row ? p.tokc[me] : 0, bucket = row ? token >> 7 : (int)(y - (int64_t)block * (p.buckets + 1));
+            const int token = row ? p.tokc[me] : 0;
+            const int key = row ? min(token, kLinNoToken) : (int)(y - (int64_t)block * (p.buckets + 1)) * kLinRows;
             int before = 0;
             // (a CTA's asks may be of different blocks: all of the rows go by, those of others count as behind)
             const int first = (int)(q0 < live ? q0 / kLinSort : min((q0 - live) / (p.buckets + 1), (int64_t)(blocks - 1)));
@@ -930,14 +943,14 @@ __global__ void __launch_bounds__(256) lin_gather_kernel(LinGatherParams p) {
             const int r_first = q0 < live && q1 >= live ? 0 : first * kLinSort;
             for (int r0 = r_first; r0 < min(live, (last + 1) * kLinSort); r0 += 2048) {
                 __syncthreads();
-                for (int x = threadIdx.x; x < 2048; x += 256) s_bucket[x] = r0 + x < live ? p.tokc[r0 + x] >> 7 : INT32_MAX;
+                for (int x = threadIdx.x; x < 2048; x += 256) s_key[x] = r0 + x < live ? min(p.tokc[r0 + x], kLinNoToken) : INT32_MAX;
                 __syncthreads();
                 if (r0 / kLinSort != block) continue;
 #pragma unroll 8
                 for (int x = 4 * part; x < 2048; x += 32) {
-                    const int4 b = *reinterpret_cast<const int4 *>(s_bucket + x);
+                    const int4 b = *reinterpret_cast<const int4 *>(s_key + x);
                     const int d = row ? me - r0 - x : 0;  // (of equal ones those before this row count)
-                    before += (b.x < bucket + (d > 0)) + (b.y < bucket + (d > 1)) + (b.z < bucket + (d > 2)) + (b.w < bucket + (d > 3));
+                    before += (b.x < key + (d > 0)) + (b.y < key + (d > 1)) + (b.z < key + (d > 2)) + (b.w < key + (d > 3));
                 }
             }
 #pragma unroll
