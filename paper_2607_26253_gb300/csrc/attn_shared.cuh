@@ -46,7 +46,7 @@ struct SharedGroup {
     int entry0;          // pages of units before its first
 };
 struct SharedPlan {      // at the start of the workspace
-    int err, entries, bad, pad[61];
+    int err, entries, pad[62];
 };
 
 struct SharedParams {
@@ -169,7 +169,7 @@ struct SharedShares {
 
 // A share's pages of a unit
 struct SharedSegment {
-    int e, count;               // first entry, pages
+    int count;                  // pages
     int row0, h, q0, queries;   // the group's first row; KV head; first query and number of the unit's queries
     int lo, hi, page;           // the group's positions; the first page
     bool begins, whole;
@@ -204,7 +204,6 @@ struct SharedWalk {
             load(p);
         }
         const int off = e - x.entry0, unit = off / x.pages, at = off - unit * x.pages, t = unit % x.tiles;
-        s.e = e;
         s.count = min(x.pages - at, end - e);
         s.row0 = x.row0;
         s.h = unit / x.tiles;
@@ -235,6 +234,7 @@ struct SharedSmem {
     alignas(16) uint32_t nan[8][2][4];  // blocks of a page in which a warp met a NaN among K's, V's codes, and ([0][3]) those whose scales are none
     float2 top[2][kSharedQ];       // a query's largest score and product, of either half of a page
     float sum[kSharedQ];           // of the second half's probabilities
+    uint32_t size[2][kSharedQ];    // of a query's halves, the largest element in bits
     int block[2][4];               // of a page of codes
     uint32_t tmem_base;
     SharedWalk walk[kSharedThreads / 32];
@@ -622,24 +622,25 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
             if (y.any) {
                 const uint4 *src = reinterpret_cast<const uint4 *>(p.q + row * p.q_stride + (int64_t)head * HD);
                 const int first = p.first ? p.first[row] : 0, end = min(p.ctx[row], p.row_prefix[row]), group = p.row_group[row];
-                uint4 x[HD / 8];
+                uint4 x[HD / 16];
 #pragma unroll
-                for (int i = 0; i < HD / 8; ++i) x[i] = __ldg(src + i);
+                for (int i = 0; i < HD / 16; ++i) x[i] = __ldg(src + half * (HD / 16) + i);
                 float f = 1.f;
                 if (p.type == SARA_BF16) {
                     uint32_t top = 0;
 #pragma unroll
-                    for (int i = 0; i < HD / 8; ++i)
+                    for (int i = 0; i < HD / 16; ++i)
                         top = __vmaxu2(top, __vmaxu2(__vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu), __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu)));
-                    top = max(top & 0xffff, top >> 16);
+                    S.size[half][lrow] = max(top & 0xffff, top >> 16);
+                    named_bar_sync(1 + quarter, 64);
+                    top = max(S.size[0][lrow], S.size[1][lrow]);
                     const int e = max(min(14 - ((int)(top >> 7) - 127), 126), -113);  // brings the largest magnitude's power of two to 2^14
                     f = pow2f(e);
                     y.mul *= pow2f(-e);
                 }
 #pragma unroll
                 for (int i = 0; i < HD / 16; ++i) {
-                    const uint4 z = half ? x[HD / 16 + i] : x[i];
-                    uint32_t u[4] = {z.x, z.y, z.z, z.w};
+                    uint32_t u[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
                     if (p.type == SARA_BF16) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {

@@ -94,8 +94,9 @@ struct LinParams {
     bool wide;         // its rows' blocks are 32-byte aligned
 };
 
-// Chunks of a part of a logit's sum: with two CTAs a tile's epilogue has no time for more parts
-__host__ __device__ constexpr int lin_part(int ctas) { return ctas == 2 ? 8 : 2; }
+// Chunks of a part of a logit's sum: with two CTAs a tile's epilogue has no time for more parts; the errors of a few rows, which nothing averages
+// away, get some more (1 x 2,048 x 151,936: 109 us with 2, 113 with 1; entropies of 1 x 944 x 32,990 off by 4.3e-6 and below 1e-6)
+__device__ __forceinline__ int lin_part(int ctas, int rows) { return ctas == 2 ? 8 : rows <= 8 ? 1 : 2; }
 struct LinSmem {
     uint64_t full[6], empty[6], acc_full[2], acc_empty[2], drain;
     uint32_t tmem_base;
@@ -342,7 +343,8 @@ template <int MODE, int CTAS, int TYPE, bool STAGED>
 __global__ void __launch_bounds__(kLinThreads, 1)
 lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmA2,
            const __grid_constant__ CUtensorMap tmB2, const __grid_constant__ CUtensorMap tmOut, LinParams p) {
-    constexpr int STAGES = lin_stages(CTAS, STAGED), STAGE = lin_stage_bytes(CTAS), COLS = kLinCols, PART = lin_part(CTAS);
+    constexpr int STAGES = lin_stages(CTAS, STAGED), STAGE = lin_stage_bytes(CTAS), COLS = kLinCols;
+    const int PART = lin_part(CTAS, p.R);
     extern __shared__ uint8_t smem_raw[];
     __shared__ LinSmem S;
     __shared__ __align__(16) std::conditional_t<MODE == LIN_SCORE, LinScoreSmem, std::conditional_t<MODE == LIN_GRAD, LinGradSmem, LinNoSmem>> E;
