@@ -203,6 +203,8 @@ def attention_shared_kv8_workspace(n_seq: int, n_groups: int, n_heads: int, n_kv
     share it must not overlap)."""
     if torch is None:
         _start()
+    if min(n_seq, n_groups, n_heads, n_kv_heads, head_dim) < 0 or max(n_seq, n_groups, n_heads, n_kv_heads, head_dim) > _MOST:
+        _refuse("sizes must be 0 .. 2^31 - 1")
     size = _lib.sara_attention_shared_kv8_workspace_bytes(n_seq, n_groups, n_heads, n_kv_heads, head_dim)
     return torch.zeros(max(size, 256), dtype=torch.uint8, device=device)
 
@@ -331,7 +333,7 @@ def _rows16(x, what, shape=None):
         _refuse(f"{what} must have rows of consecutive elements")
     if rows > _MOST or d > _MOST:
         _refuse(f"{what} must have at most 2^31 - 1 rows and columns")
-    return typ, rows, d, max(row, d) if rows <= 1 else row, x.get_device()
+    return typ, rows, d, d if rows <= 1 else row, x.get_device()  # (a single row has no stride)
 
 
 def _linear(hidden, weight):

@@ -403,3 +403,13 @@ def test_weights_past_32_bits(pkg):
     assert abs(float(dw[V - 2, 0]) + p * np.exp(-17.0) * 2.0 ** -6) <= 2.0 ** -7 * p * np.exp(-17.0) * 2.0 ** -6
     want = (1 - p) * 0.25 - p * np.exp(-8.5) * 0.125
     assert abs(float(dh[0, 0]) - want) <= 2.0 ** -6 * abs(want) and float(dh[1].abs().max()) == 0
+
+
+def test_a_single_row_has_no_stride(pkg):
+    """One row of a matrix whose rows are no multiple of 8 elements apart, and one token of a vocabulary."""
+    import torch
+    rng = np.random.default_rng(12)
+    h = torch.from_numpy(rng.standard_normal((9, 100))).cuda().bfloat16()[8:9, 32:96]  # (8 x 200 + 64 bytes: aligned)
+    for w in (torch.from_numpy(rng.standard_normal((300, 64))).cuda().bfloat16(), torch.from_numpy(rng.standard_normal((9, 100))).cuda().bfloat16()[8:9, 32:96]):
+        g = torch.ones(1, device="cuda")
+        _both(pkg, h, w, [0], 1.0, g, g, "bf16", spread=False)

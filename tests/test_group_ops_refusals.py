@@ -92,6 +92,8 @@ def test_binding_refuses_tensors_that_do_not_fit_a_shared_prefix(pkg):  # noqa: 
     att(lse=torch.zeros(3, 8).double())
     att(status=i32(2))
     att(workspace=torch.zeros(2048, dtype=torch.uint8)[::2])
+    for bad in ((-1, 1, 8, 2, 64), (2 ** 32 + 5, 1, 8, 2, 64), (4, 2 ** 32 + 1, 8, 2, 64)):
+        assert "0 .. 2^31 - 1" in _refused(pkg, pkg.attention_shared_kv8_workspace, *bad, device="cpu")
 
 
 def test_binding_refuses_tensors_that_do_not_fit_linear_scoring(pkg):  # noqa: F811
