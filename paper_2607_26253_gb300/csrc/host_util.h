@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 
 #include <atomic>
+#include <cstdint>
 #include <stdexcept>
 #include <string>
 
@@ -36,6 +37,20 @@ inline int sm_count() {
     if (dev >= 0 && dev < kMaxDevices) known[dev].store(sms, std::memory_order_relaxed);
     return sms;
 }
+
+// Shared memory beyond 48 KB, asked for once a device (two threads may both do so)
+struct SmemOnce {
+    std::atomic<uint64_t> told{0};
+    template <typename Kern>
+    void ask(Kern kern, size_t bytes) {
+        int dev = 0;
+        CK(cudaGetDevice(&dev));
+        const uint64_t bit = dev >= 0 && dev < 64 ? (uint64_t)1 << dev : 0;
+        if (told.load(std::memory_order_acquire) & bit) return;
+        CK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+        told.fetch_or(bit, std::memory_order_release);
+    }
+};
 
 // Runs an entry point's body: the code it returns, no exception past the C boundary.
 template <typename F>

@@ -45,7 +45,8 @@ template <int MODE, int CTAS, int TYPE, bool STAGED>
 void launch(cudaStream_t s, int sms, bool after, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &a2, const CUtensorMap &b2,
             const CUtensorMap &out, const LinParams &p) {
     const auto kern = lin_kernel<MODE, CTAS, TYPE, STAGED>;
-    CK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lin_smem(CTAS, STAGED)));
+    static SmemOnce smem;
+    smem.ask(kern, lin_smem(CTAS, STAGED));
     launch_cluster(s, after, dim3((unsigned)(sms / CTAS * CTAS)), dim3(kLinThreads), lin_smem(CTAS, STAGED), CTAS, kern, a, b, a2, b2, out, p);
 }
 
@@ -60,13 +61,19 @@ void gather(cudaStream_t s, void *ws, const LinPlan &q, const Operand &h, const 
             bool sort) {
     const int R = (int)h.rows, d = (int)h.d;
     int *kexp = backward ? at<int>(ws, q.kexp) : nullptr, *tokc = backward ? at<int>(ws, q.tokc) : nullptr;
-    lin_rows_kernel<<<1, 1024, 0, s>>>({at<LinHeader>(ws, 0), R, tokens, glp, gent, at<int>(ws, q.src), at<int>(ws, q.pos), kexp, tokc, TYPE == SARA_FP16});
-    CK(cudaGetLastError());
+    const LinRowParams rows{at<LinHeader>(ws, 0), R, tokens, glp, gent, at<int>(ws, q.src), at<int>(ws, q.pos), kexp, tokc, TYPE == SARA_FP16};
     const int row_ctas = q.rows_cap / 8, sort_ctas = sort ? (int)std::min<int64_t>(((int64_t)R + q.buckets + 32) / 32, 2048) : 0;
     const LinGatherParams p{at<LinHeader>(ws, 0), static_cast<const uint16_t *>(h.p), h.stride, d, kLinRows * q.ctas, at<int>(ws, q.src), kexp,
                             at<uint16_t>(ws, q.rows), backward && TYPE == SARA_FP16 ? at<uint16_t>(ws, q.low) : nullptr, row_ctas, tokc,
                             backward ? at<int2>(ws, q.sorted) : nullptr, backward ? at<int>(ws, q.start) : nullptr, q.buckets};
-    launch_cluster(s, true, dim3((unsigned)(row_ctas + sort_ctas), (unsigned)((d + kLinGatherCols - 1) / kLinGatherCols)), dim3(256), 0, 1, lin_gather_kernel, p);
+    const dim3 grid((unsigned)(row_ctas + sort_ctas), (unsigned)((d + kLinGatherCols - 1) / kLinGatherCols));
+    if (R <= kLinFew) {
+        launch_cluster(s, false, grid, dim3(256), 0, 1, lin_gather_kernel<true>, p, rows);
+    } else {
+        lin_rows_kernel<<<1, 1024, 0, s>>>(rows);
+        CK(cudaGetLastError());
+        launch_cluster(s, true, grid, dim3(256), 0, 1, lin_gather_kernel<false>, p, rows);
+    }
 }
 
 template <int CTAS, int TYPE>

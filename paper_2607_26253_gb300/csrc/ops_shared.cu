@@ -60,7 +60,8 @@ bool shared_alone(int n, int groups, int kvh, int hd, int max_blocks) {
 template <int HD, int FMT>
 void shared_launch(const SharedParams &p, int shares, cudaStream_t s) {
     const auto kern = shared_prefix_kernel<HD, FMT>;
-    CK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, shared_smem(HD)));
+    static SmemOnce smem;
+    smem.ask(kern, shared_smem(HD));
     launch_cluster(s, true, dim3((unsigned)shares), dim3(kSharedThreads), shared_smem(HD), 1, kern, p);
 }
 template <int HD>
