@@ -344,6 +344,8 @@ __global__ void __launch_bounds__(kLinThreads, 1)
 lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmA2,
            const __grid_constant__ CUtensorMap tmB2, const __grid_constant__ CUtensorMap tmOut, LinParams p) {
     constexpr int STAGES = lin_stages(CTAS, STAGED), STAGE = lin_stage_bytes(CTAS), COLS = kLinCols;
+    // (bf16's products have few bits to cut off: the gradient's logits are summed in one there.  In fp16 2,048 of them lose 2^-15 of the sum)
+    constexpr bool PARTED = MODE == LIN_SCORE || (MODE == LIN_DZ && TYPE == SARA_FP16);
     const int PART = lin_part(CTAS, p.R);
     extern __shared__ uint8_t smem_raw[];
     __shared__ LinSmem S;
@@ -450,7 +452,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             int a = 0;
 #pragma unroll 1
             for (int k = j.k0; k < j.k1; ++k) {
-                const bool begins = MODE == LIN_SCORE ? k % PART == 0 : k == j.k0, ends = k + 1 == j.k1 || (MODE == LIN_SCORE && (k + 1) % PART == 0);
+                const bool begins = PARTED ? k % PART == 0 : k == j.k0, ends = k + 1 == j.k1 || (PARTED && (k + 1) % PART == 0);
                 if (begins) {
                     a = it & 1;
                     dacc = tmem + (uint32_t)(a * COLS);
@@ -671,6 +673,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 last = where(i + 3);
             };
             const float k = MODE == LIN_GRAD ? p.scale * pow2f(-p.head->exp) : 0.f;
+            int it = 0;  // accumulators
 #pragma unroll 1
             for (int i = 0; i < work.count; ++i) {
                 LinJob j;
@@ -678,9 +681,21 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 const int m = j.m0 + rank * kLinRows + lrow;
                 float v[128];
                 auto read = [&]() {
-                    if (ok) wait(i);
-                    lin_tmem_load128(from + (uint32_t)((i & 1) * COLS), v);
-                    if (ok) give(i & 1);
+                    if (ok) wait(it);
+                    lin_tmem_load128(from + (uint32_t)((it & 1) * COLS), v);
+                    if (ok) give(it & 1);
+                    ++it;
+                    if constexpr (PARTED) {
+#pragma unroll 1
+                        for (int q = 1; q < (j.k1 + PART - 1) / PART && ok; ++q, ++it) {
+                            wait(it);
+                            if (!ok) break;
+                            const uint32_t at = from + (uint32_t)((it & 1) * COLS);
+#pragma unroll
+                            for (int cc = 0; cc < 128 / 32; ++cc) lin_tmem_add(at + 32 * cc, v + 32 * cc);
+                            give(it & 1);
+                        }
+                    }
                 };
                 if constexpr (MODE == LIN_DZ) {
                     // What the row wants, read while the MMAs run.  In base 2: with r = (max + log S) log2(e) as rounded and f what the rounding
@@ -730,7 +745,14 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                                 float z = 0.f;
 #pragma unroll
                                 for (int e = 0; e < 64; ++e) z = cc + e == at ? v[cc + e] : z;
-                                const float y = max_nan(fmaf(z, c, -r), -1000.f), x = fmaf(exp2_approx(y), fmaf(y, ga, gb), g);
+                                // 1 - p from the logarithm.  The logit is made in one sum here: a token within its error of the maximum is the maximum,
+                                // or shares it, where 1 - p does not depend on the difference (1 - p = 1e-5 at a logit of 22: off by 2.6 times itself without)
+                                const int row = p.src[m];
+                                float t = fmaf(z, p.scale, -mx);
+                                if (fabsf(t) <= (p.d / 16 + 8) * 0x1p-24f * fabsf(mx)) t = 0.f;
+                                const float lp = max_nan(t - ls, -700.f), H = p.gent ? p.entropy[row] : 0.f, gh = p.gent ? p.gent[row] : 0.f;
+                                const float x = (wrong ? __int_as_float(0x7fc00000) : pow2f(p.kexp[row])) *
+                                                (-(p.glp ? p.glp[row] : 0.f) * expm1f(lp) - gh * expf(lp) * (lp + H));
                                 const uint32_t h = pack_grad<TYPE>(x, x);
                                 p.delta[m] = zero ? 0.f : x - unpack2<TYPE>(h).x;
 #pragma unroll

@@ -413,3 +413,30 @@ def test_a_single_row_has_no_stride(pkg):
     for w in (torch.from_numpy(rng.standard_normal((300, 64))).cuda().bfloat16(), torch.from_numpy(rng.standard_normal((9, 100))).cuda().bfloat16()[8:9, 32:96]):
         g = torch.ones(1, device="cuda")
         _both(pkg, h, w, [0], 1.0, g, g, "bf16", spread=False)
+
+
+@pytest.mark.parametrize("typ", ["bf16", "fp16"])
+@pytest.mark.parametrize("R,d,V,logit", [(1, 944, 3000, 12), (1, 1464, 32570, 22), (2, 96, 513, 9), (200, 512, 2000, 18), (129, 2048, 700, 30)])
+def test_gradients_of_tokens_that_are_nearly_certain(pkg, R, d, V, logit, typ):
+    """1 - p of 1e-2 to 1e-10: the whole gradient hangs on it.  A row's error: one rounding of each dz but the token's and of the result, the logits'
+    errors (2^-24 of them a step of 16 products, and what the formula adds) in the exponents of the others, and twice the same for 1 - p."""
+    import torch
+    rng = np.random.default_rng(R + d)
+    h = torch.from_numpy(rng.standard_normal((R, d))).cuda().to(_dtype(typ))
+    w = torch.from_numpy(rng.standard_normal((V, d)) / np.sqrt(d)).cuda().to(_dtype(typ))
+    tok = rng.permutation(V)[:R]
+    for r in range(R):
+        w[tok[r]] = (h[r].double() * (logit / float((h[r].double() ** 2).sum()))).to(w.dtype)
+    t = _i32(tok)
+    o = pkg.linear_logprobs(h, w, t)
+    g, gh = torch.from_numpy(rng.standard_normal(R)).float().cuda(), torch.from_numpy(rng.standard_normal(R)).float().cuda() / 64
+    got, _ = pkg.linear_logprobs_backward(h, w, t, o.stats, o.entropy, g, gh)
+    want, _, dz = oracle.linear_grad(_np(h), _np(w), tok, _np(g), _np(gh))
+    size, mag = np.abs(_np(h) @ _np(w).T).max(1, keepdims=True), np.abs(dz) @ np.abs(_np(w))
+    tol = (2 * HALF[typ] + 4 * (d / 16 + 16) * U * (size + 1) + 1e-4) * mag + LEAST[typ]
+    b, wn = np.abs(_np(g)) + 16 * np.abs(_np(gh)), np.abs(_np(w))
+    if typ == "fp16":  # dz below 2^-27 of a row's largest possible: half a step of fp16 there, as _check_grad has it
+        tol += (2.0 ** -25 * 2.0 ** -12 * b)[:, None] * wn.sum(0)
+    if R > 128:  # the sum beside the maximum's 1: 64 terms in a chain that it is one of, 66 roundings of 2^-24, in log S and in the entropy
+        tol += (66 * U * (np.abs(_np(g)) + 2 * np.abs(_np(gh))))[:, None] * wn[tok]
+    assert (np.abs(_np(got) - want) <= tol).all(), np.max(np.abs(_np(got) - want) / tol)
