@@ -828,11 +828,24 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
 }
 
 // ------------------------------------------------------------------------------- join
-// A query's state of its own positions and those of its shared ones, W warps to a query
+template <int N>
+__device__ __forceinline__ void vec_load(const float *p, float (&y)[N]) {
+    if constexpr (N == 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(p);
+        y[0] = x.x, y[1] = x.y, y[2] = x.z, y[3] = x.w;
+    } else if constexpr (N == 2) {
+        const float2 x = *reinterpret_cast<const float2 *>(p);
+        y[0] = x.x, y[1] = x.y;
+    } else {
+        y[0] = *p;
+    }
+}
+// A query's state of its own positions and those of its shared ones, W warps to a query; D neighbouring dims a lane
 template <int HD, int W>
 __global__ void __launch_bounds__(256) shared_join_kernel(SharedParams p, int shares_most) {
     constexpr int D = HD / 32;
-    __shared__ float s_m[8], s_l[8], s_o[8][HD];
+    __shared__ float s_m[8], s_l[8];
+    __shared__ __align__(16) float s_o[8][HD];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = W == 1 ? 0 : warp;
     const int64_t x = W == 1 ? (int64_t)blockIdx.x * 8 + warp : blockIdx.x;
     if (x >= (int64_t)p.n * p.H) return;
@@ -840,8 +853,7 @@ __global__ void __launch_bounds__(256) shared_join_kernel(SharedParams p, int sh
     float m = -3.4028235e38f, l = 0.f, o[D] = {};
     auto add = [&](float m1, float l1, const float *src) {
         float y[D];
-#pragma unroll
-        for (int d = 0; d < D; ++d) y[d] = src[lane + 32 * d];
+        vec_load<D>(src + D * lane, y);
         const float n = fmaxf(m, m1), a = ex2(fmaxf(m - n, -1e4f)), down = m1 - n, b = ex2(down < -1e4f ? -1e4f : down);  // (a NaN stays)
         m = n;
         l = fmaf(l1, b, l * a);
@@ -875,7 +887,7 @@ __global__ void __launch_bounds__(256) shared_join_kernel(SharedParams p, int sh
             s_l[warp] = l;
         }
 #pragma unroll
-        for (int d = 0; d < D; ++d) s_o[warp][lane + 32 * d] = o[d];
+        for (int d = 0; d < D; ++d) s_o[warp][D * lane + d] = o[d];
         __syncthreads();
         if (warp) return;
 #pragma unroll
@@ -884,10 +896,16 @@ __global__ void __launch_bounds__(256) shared_join_kernel(SharedParams p, int sh
     // (nothing anywhere: 0 and -inf.  A failed wait: NaN)
     const bool none = l == 0.f;
     const float inv = p.plan->err ? __int_as_float(0x7fc00000) : none ? 0.f : 1.f / l;
+    uint16_t *out = p.out + x * HD + D * lane;
+    if constexpr (D == 1) {
+        *out = p.type == SARA_BF16 ? f32_to_bf16(o[0] * inv) : __half_as_ushort(__float2half_rn(o[0] * inv));
+    } else {
+        uint32_t y[D / 2];
 #pragma unroll
-    for (int d = 0; d < D; ++d) {
-        const float y = o[d] * inv;
-        p.out[x * HD + lane + 32 * d] = p.type == SARA_BF16 ? f32_to_bf16(y) : __half_as_ushort(__float2half_rn(y));
+        for (int d = 0; d < D; d += 2)
+            y[d / 2] = p.type == SARA_BF16 ? pack2<SARA_BF16>(o[d] * inv, o[d + 1] * inv) : pack2<SARA_FP16>(o[d] * inv, o[d + 1] * inv);
+        if constexpr (D == 4) *reinterpret_cast<uint2 *>(out) = make_uint2(y[0], y[1]);
+        else *reinterpret_cast<uint32_t *>(out) = y[0];
     }
     if (p.lse && lane == 0) p.lse[x] = none ? -INFINITY : (m + log2f(l)) * 0.69314718f;
 }

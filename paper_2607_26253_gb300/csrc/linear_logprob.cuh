@@ -4,7 +4,9 @@
 //             a, sum 2^y and sum 2^y y with y = (acc - a) scale log2(e), which a second kernel joins over the tiles
 //   gradient: the vocabulary goes by in pieces.  A piece's logits are made again, its dZ = g (1[v = token] - p) - g' p (log p + H),
 //             [R][piece], is stored in the operands' type, and feeds both products, dH += dZ W and dW = dZ^T H.
-// Bound by the tensor cores from some 300 rows on, by reading W below.
+// Bound by the tensor cores from some 300 rows on, by reading W below.  us of a call (and of its floor): scores of 1 x 2,048 x 151,936 115 (92), of
+// 26 x 1,536 x 151,936 93 (69), of 4,096 x 1,536 x 151,936 1,010 (910); gradient of 301 x 2,048 x 32,001 in fp16 202 (56: 106 with rows in
+// whole tiles), of 4,096 x 1,536 x 151,936 3,475 (2,730; 3,013 at the rate that the power cap leaves).
 //
 // One persistent kernel does all the products (D = A B^T, fp32 in tensor memory): 256 columns, 128 rows a CTA, K in chunks of 64.
 // With more than 128 rows two CTAs (a cluster) share a tile of 256 x 256, each bringing half of A's rows and half of B's: 64 bytes
@@ -957,7 +959,7 @@ __global__ void __launch_bounds__(1024) lin_rows_kernel(LinRowParams p) {
 // The CTAs behind those put the rows in the order of their tokens (and of the rows of one), `kLinSort` rows at a time, so that
 // dW's epilogue finds a tile's: sorted[start[b] .. start[b + 1]) are those of tile b.  A row's place is the number of rows before it, counted
 // by 8 lanes.
-// FEW: each CTA finds the rows for itself, the first one for the kernels behind it too (a launch less: gradient of 32 x 128 x 512 24.7 -> 21 us).
+// FEW: each CTA finds the rows for itself, the first one for the kernels behind it too (a launch less: gradient of 32 x 128 x 512 through the binding 33 -> 29 us, on the device 24.7 -> 24.2).
 struct LinGatherParams {
     const LinHeader *head;
     const uint16_t *h;
