@@ -440,3 +440,21 @@ def test_gradients_of_tokens_that_are_nearly_certain(pkg, R, d, V, logit, typ):
     if R > 128:  # the sum beside the maximum's 1: 64 terms in a chain that it is one of, 66 roundings of 2^-24, in log S and in the entropy
         tol += (66 * U * (np.abs(_np(g)) + 2 * np.abs(_np(gh))))[:, None] * wn[tok]
     assert (np.abs(_np(got) - want) <= tol).all(), np.max(np.abs(_np(got) - want) / tol)
+
+
+@pytest.mark.parametrize("typ", ["bf16", "fp16"])
+@pytest.mark.parametrize("R,V,how", [(1023, 300, "any"), (1024, 300, "any"), (1025, 300, "any"), (700, 40, "same"), (1500, 600, "few"), (90, 513, "last"), (2000, 512, "wide")])
+def test_rows_found_and_sorted_by_token(pkg, R, V, how, typ):
+    """Row counts around what a CTA finds for itself, and many rows to a token: its corrections come from more rows than wait in shared memory."""
+    import torch
+    rng = np.random.default_rng(R)
+    d = 328 if how == "wide" else 64
+    h = torch.from_numpy(rng.standard_normal((R, d))).cuda().to(_dtype(typ))
+    w = torch.from_numpy(rng.standard_normal((V, d)) / np.sqrt(d)).cuda().to(_dtype(typ))
+    tok = {"any": rng.integers(0, V, R), "same": np.full(R, 7), "few": rng.integers(250, 260, R), "last": np.full(R, V - 1), "wide": rng.integers(0, V, R)}[how]
+    tok[rng.random(R) < 0.2] = -1
+    g, gh = (torch.from_numpy(rng.standard_normal(R)).float().cuda() for _ in range(2))
+    _, y = _both(pkg, h, w, tok, 1.0, g, gh, typ, spread=False)
+    o = pkg.linear_logprobs(h, w, _i32(tok))
+    again = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, g, gh)
+    assert torch.equal(y[0], again[0]) and torch.equal(y[1], again[1])
