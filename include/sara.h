@@ -426,8 +426,8 @@ SARA_API int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_se
  * its prefix (ctx[i] <= prefix[g], or 0).  Groups of up to two sequences on average, and tables whose rows have room for little (160 MB of codes for
  * large groups, more for small ones), are attended to row by row, which is then faster: each reads the shared positions for itself.
  * Everything else as sara_attention_decode_kv8, but: probabilities of shared positions times their values' scale may be held in fp16, 11 bits,
- * or within 2^-31 of the query's largest such product, and a NaN among e4m3 codes, of which sara_kv8_write writes none, may make all of a
- * row NaN that attends to its block of 32.
+ * or within 2^-31 of the query's largest such product, and a NaN among e4m3 codes or a negative scale of keys, of which sara_kv8_write writes
+ * none, may make all of a row NaN that attends to its block of 32.
  * group_start that falls or leaves 0 .. n_seq makes every row NaN, prefix[g] outside [0, 128 * max_blocks] the rows of its group, a block id outside
  * [0, n_blocks) the rows that attend to the block; each sets *status.
  * workspace: sara_attention_shared_kv8_workspace_bytes(...) bytes (for up to these sizes), 256-byte aligned, all zero on first use and

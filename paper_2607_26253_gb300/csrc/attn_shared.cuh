@@ -481,13 +481,15 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 const bool cut = block < 0 || p0 < s.lo || p0 + kKv8Page > s.hi;  // positions that nobody attends to are 0: what they hold does not matter
                 // (eight places: the page three before has its scores, so that the softmax is done with the one five before, and a page's flags are read in the one
                 // behind it, or when the next unit's first scores may have been made)
-                if (!value && cw == kSharedConv - 1) {  // (the warp with the fewest rows.  A block whose scale is NaN or infinite reads as NaN: it goes in as 0, and is flagged)
+                // (the warp with the fewest rows.  A block whose scale is NaN or infinite, or negative among keys, reads as NaN: it goes in as 0 with a scale of 1, and is
+                // flagged, which reaches the rows that attend to it alone.  So whatever the memory of a block holds that nobody has written does not matter)
+                if (!value && cw == kSharedConv - 1) {
                     float k = 1.f, f = 0.f;
                     if (block >= 0 && lane < 4) {
                         k = S.raw_scale[st][lane];
                         f = S.raw_scale[st][4 + lane];
                     }
-                    const bool bad = block < 0 || !(fabsf(k) < INFINITY && fabsf(f) < INFINITY);
+                    const bool bad = block < 0 || max(__float_as_uint(k), __float_as_uint(f) & 0x7fffffffu) >= 0x7f800000u;
                     const int e = min(max(scale_exp(bad ? 0.f : f), -126), 126);
                     const uint32_t flag = __ballot_sync(0xffffffffu, bad) & 15;
                     if (lane < 4) {
@@ -717,7 +719,9 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                     tmem_load64(s_at, v);
 #pragma unroll
                     for (int b = 0; b < 2; ++b) {
-                        ks[b] = S.scale[j & 7][0][2 * half + b] * mul;
+                        // (a masked product is -inf times this, which may not be 0 then.  A factor below 2^-126, of a query or keys of zeros, counts as that: |q k| <= 2^32
+                        // here, so the scores stay 0 beside any that counts)
+                        ks[b] = fmaxf(S.scale[j & 7][0][2 * half + b] * mul, 0x1p-126f);
                         F[b] = S.scale[j & 7][1][2 * half + b];
                         ev[b] = S.scale[j & 7][2][2 * half + b];
                     }

@@ -373,3 +373,77 @@ def test_the_same_sequence_in_every_row(pkg):
     assert status == 0
     _check(c, q, [600] * n, [0, n], [555], out, "fp16", lse=lse)
     assert pkg.attention_shared_kv8(q[:0], c.codes, c.scales, c.tab[:0], _i32([]), _i32([0]), _i32([])).shape == (0, 8, 64)
+
+
+def _unwritten(c, used, scale):
+    """Scales of blocks that hold no position of `used` (pairs of a row of the table and a range), as memory that nobody has written may have them."""
+    import torch
+    keep = torch.zeros(c.scales.shape[0], 4, dtype=torch.bool)
+    for row, a, b in used:
+        for x in range(a // 32, -(-b // 32)):
+            keep[row[x // 4], x % 4] = True
+    c.scales = torch.where(keep.cuda()[:, None, None, :], c.scales, torch.tensor(scale, device="cuda"))
+    c.want_scales = c.scales.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, -1.0, -2.0 ** 100, 2.0 ** -100, 1e-45, 2.0 ** 120, float("inf"), float("nan")])
+@pytest.mark.parametrize("hd,fmt,typ", [(128, "e4m3", "bf16"), (64, "int8", "fp16"), (32, "e4m3", "bf16")])
+def test_scales_of_blocks_that_nobody_attends_to_do_not_matter(pkg, hd, fmt, typ, scale):
+    """Prefixes, rows and windows that end and begin in each block of a page."""
+    rng = np.random.default_rng(hd)
+    n, blocks = 24, 6
+    for prefix, lo in ((400, 0), (390, 0), (416, 33), (449, 70), (500, 97), (16, 0), (33, 32), (512, 64), (530, 300)):
+        c = Cache(pkg, rng, n, blocks, 2, hd, fmt)
+        ctx = np.maximum(prefix - rng.integers(0, 3, n), lo + 1)  # rollouts just begun
+        ctx[::5] = prefix + 1
+        first = np.full(n, lo)
+        _unwritten(c, [(c.table[0], lo, prefix)] + [(c.table[i], prefix, ctx[i]) for i in range(n) if ctx[i] > prefix], scale)
+        q = _q(rng, n, 8, hd, typ)
+        q[2], q[3, 1] = 0, 0
+        out, lse, status = _run(pkg, c, q, ctx, [0, n], [prefix], first)
+        assert status == 0
+        _check(c, q, ctx, [0, n], [prefix], out, typ, first=first, lse=lse)
+
+
+@pytest.mark.parametrize("typ,size", [("bf16", 0.0), ("bf16", 2.0 ** -133), ("bf16", 2.0 ** -126), ("bf16", 2.0 ** -60), ("fp16", 0.0), ("fp16", 2.0 ** -24)])
+@pytest.mark.parametrize("hd", [32, 128])
+def test_queries_and_keys_next_to_nothing(pkg, hd, typ, size):
+    """Heads of zeros and of the least elements over keys of zeros, which have the lowest scale, and over others; rows that end in each block."""
+    import torch
+    rng = np.random.default_rng(hd + 1)
+    n, prefix = 20, 400
+    for k_scale in (2.0 ** -100, 2.0 ** -126, 0.0, 2.0 ** -8):
+        c = Cache(pkg, rng, n, 5, 2, hd, "e4m3")
+        c.scales[:, 0] = k_scale
+        if k_scale == 2.0 ** -100:
+            c.codes.view(torch.uint8)[:, 0] = 0
+        c.want_codes, c.want_scales = c.values(), c.scales.double().cpu().numpy()
+        q = _q(rng, n, 8, hd, typ)
+        small = (q.float().sign() * size).to(q.dtype)
+        q[:, ::2] = small[:, ::2]
+        ctx = rng.integers(300, 430, n)
+        out, lse, status = _run(pkg, c, q, ctx, [0, n], [prefix])
+        assert status == 0
+        _check(c, q, ctx, [0, n], [prefix], out, typ, lse=lse)
+
+
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_keys_of_a_scale_below_zero(pkg, hd):
+    """None that is ever written: rows that attend to its block are NaN, or have it as a factor where they go by themselves; the others do not notice."""
+    rng = np.random.default_rng(3)
+    n, prefix = 40, 450
+    c = Cache(pkg, rng, n, 4, 2, hd, "int8")
+    q = _q(rng, n, 8, hd, "bf16")
+    ctx, first = rng.integers(200, 500, n), rng.choice([0, 100, 300], n)
+    first = np.minimum(first, ctx)
+    want = _run(pkg, c, q, ctx, [0, n], [prefix], first)
+    c.scales[c.table[0, 1], 0, :, 2] *= -1  # positions 192 .. 223
+    c.want_scales = c.scales.double().cpu().numpy()
+    out, lse, status = _run(pkg, c, q, ctx, [0, n], [prefix], first)
+    assert status == 0
+    hit = (first < 224) & (ctx > 192) & (first < ctx)
+    if c.wide:
+        assert bool(out[hit].isnan().all()) and bool(lse[hit].isnan().all())
+    else:
+        _check(c, q, ctx, [0, n], [prefix], out, "bf16", first=first, lse=lse)
+    assert (out[~hit] == want[0][~hit]).all() and (lse[~hit] == want[1][~hit]).all()
