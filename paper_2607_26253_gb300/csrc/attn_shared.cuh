@@ -239,7 +239,7 @@ struct SharedSmem {
     uint64_t raw_full[2][4], raw_empty[2][4], full[kSharedSlots], empty[kSharedSlots], q_full, s_full[2], p_full[2], pv_done;
     float scale[8][3][4];          // of a page's blocks: K's scale, V's as 2^e and what is left, e
     float raw_scale[4][8];         // the same, as they come with the keys
-    alignas(16) uint32_t nan[8][2][4];  // blocks of a page in which a warp met a NaN among K's, V's codes, and ([0][3]) those whose scales are none
+    alignas(16) uint32_t nan[8][2][4];  // blocks of a page in which a warp met a NaN among K's, V's codes, and ([0][3]) those whose scales are none (16: the page itself is none)
     float2 top[2][kSharedQ];       // a query's largest score and product, of either half of a page
     float sum[kSharedQ];           // of the second half's probabilities
     uint32_t size[2][kSharedQ];    // of a query's halves, the largest element in bits
@@ -412,7 +412,6 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
     } else if (warp == LOAD_WARP) {
         // ------------------------------------------------------------ codes
         uint32_t got[2] = {};  // pages asked for
-        bool wrong = false;
         // keys, then the values of the page before: keys are wanted earlier, and have more room
         auto bring = [&](auto value, int block, int h) {
             constexpr int v = decltype(value)::value;
@@ -445,10 +444,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                 if ((unsigned)(page - idbase) >= 32u) {
                     idbase = page;
                     ids = page + lane <= (s.hi - 1) / kKv8Page ? __ldg(p.c.table + s.row0 * p.c.table_stride + page + lane) : 0;
-                    if (ids < 0 || ids >= p.c.n_blocks) {
-                        wrong = true;
-                        ids = -1;
-                    }
+                    if (ids >= p.c.n_blocks) ids = -1;  // (any negative one: none.  Rows that attend to it report it)
                 }
                 const int block = __shfl_sync(0xffffffffu, ids, page - idbase);
                 bring(std::integral_constant<int, 0>(), block, s.h);
@@ -461,7 +457,6 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
         // every copy lands before the CTA ends
         for (int v = 0; v < 2; ++v)
             for (uint32_t q = 1; q <= (uint32_t)RAWS[v] && q <= got[v]; ++q) mbar_wait(&S.raw_full[v][(got[v] - q) % RAWS[v]], ((got[v] - q) / RAWS[v]) & 1, err);
-        if (wrong) kv8_report(p.status);
     } else if (warp >= kSharedSoft && warp < MMA_WARP) {
         // ------------------------------------------------------------ codes to fp16
         const int cw = (warp - kSharedSoft) % kSharedConv, ct = cw * 32 + lane;
@@ -497,7 +492,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
                         S.scale[j & 7][1][lane] = bad ? 0.f : f * pow2f(-e);
                         S.scale[j & 7][2][lane] = (float)e;
                     }
-                    if (lane == 0) S.nan[j & 7][0][3] = flag;
+                    if (lane == 0) S.nan[j & 7][0][3] = flag | (block < 0 ? 16u : 0u);
                 }
                 if (j >= 2) wait(&S.empty[at], (j >> 1) - 1);
                 if (!ok) break;
@@ -683,6 +678,7 @@ __global__ void __launch_bounds__(kSharedThreads, 1) shared_prefix_kernel(Shared
             // a block that reads as NaN (bit b: of this half's) makes the sums of those that attend to it NaN, and leaves the others alone
             auto poison = [&](int page, uint32_t bad) {
                 const int p0 = page * kKv8Page + 64 * half;
+                if ((bad << (2 * half) & 16) && lo < p0 + 64 && hi > p0) kv8_report(p.status);
                 if ((bad & 1) && lo < p0 + 32 && hi > p0) l = __int_as_float(0x7fc00000);
                 if ((bad & 2) && lo < p0 + 64 && hi > p0 + 32) l = __int_as_float(0x7fc00000);
             };

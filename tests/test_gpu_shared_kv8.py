@@ -447,3 +447,27 @@ def test_keys_of_a_scale_below_zero(pkg, hd):
     else:
         _check(c, q, ctx, [0, n], [prefix], out, "bf16", first=first, lse=lse)
     assert (out[~hit] == want[0][~hit]).all() and (lse[~hit] == want[1][~hit]).all()
+
+
+@pytest.mark.parametrize("fmt,typ", [("e4m3", "bf16"), ("int8", "fp16")])
+def test_wrong_blocks_that_no_row_attends_to_are_not_reported(pkg, fmt, typ):
+    """Windows that leave a gap among a group's shared positions, its pages none of the cache's; then one row that attends to one of them."""
+    rng = np.random.default_rng(12)
+    n, prefix = 24, 900
+    c = Cache(pkg, rng, n, 8, 2, 64, fmt)
+    early = np.arange(n) % 2 == 0
+    first = np.where(early, 0, 650)
+    ctx = np.where(early, 200, 950)
+    ctx[4] = 250
+    c.tab[0, 2:5] = _i32([-1, 1 << 30, c.codes.shape[0]])  # positions 256 .. 639
+    q = _q(rng, n, 8, 64, typ)
+    out, lse, status = _run(pkg, c, q, ctx, [0, n], [prefix], first)
+    assert status == 0
+    _check(c, q, ctx, [0, n], [prefix], out, typ, first=first, lse=lse)
+    for row, a, b in ((4, 0, 257), (7, 639, 950), (9, 639, 640)):
+        first2, ctx2 = first.copy(), ctx.copy()
+        first2[row], ctx2[row] = a, b
+        out, lse, status = _run(pkg, c, q, ctx2, [0, n], [prefix], first2)
+        assert status == pkg.SARA_EINVAL
+        assert bool(out[row].isnan().all()) and bool(lse[row].isnan().all())
+        _check(c, q, ctx2, [0, n], [prefix], out, typ, first=first2, lse=lse, rows=[i for i in range(n) if i != row])
