@@ -501,8 +501,9 @@ SARA_API int sara_linear_logprobs(const void *hidden, int64_t hidden_stride, con
  *   dz[r][v] = grad_logprob[r] (1[v = token[r]] - p_v) - grad_entropy[r] p_v (log p_v + entropy[r]),
  *   grad_hidden = scale dz W,   grad_weight = scale dz^T H,
  * the logits made again, piece by piece of the vocabulary, summed in fp32 and rounded once to `type`.  dz enters the products
- * in `type` (in fp16 times a power of two of the row, so that tokens down to p = 2^-27 keep all its bits).  stats and entropy as
- * sara_linear_logprobs gave them.  grad_logprob and grad_entropy [R] fp32, each may be NULL (0); entropy is wanted with grad_entropy,
+ * in `type` (in fp16 times a power of two of the row, so that tokens down to p = 2^-27 keep all its bits; hidden
+ * states enter grad_weight with all theirs down to (|grad_logprob| + 16 |grad_entropy|) |hidden| = 2^-27 of the largest such product, and are off by
+ * 2^-38 of it at most below that).  stats and entropy as sara_linear_logprobs gave them.  grad_logprob and grad_entropy [R] fp32, each may be NULL (0); entropy is wanted with grad_entropy,
  * tokens with grad_logprob.  grad_hidden or grad_weight may be NULL (not computed); they overlap neither each other nor hidden and weight.
  * Rows of padding get 0 and add nothing to grad_weight, whatever their hidden states hold; a token >= V, a NaN or +inf among the logits makes
  * the row NaN, and with it grad_weight.  Sums are in a fixed order: results repeat bit for bit.

@@ -44,8 +44,9 @@ constexpr int kLinWorkers = 152;  // SMs that a plan counts on (on a GPU with ot
 struct LinHeader {
     int err;   // bits of device_common.cuh; left zero
     int live;  // rows that are not padding
-    int exp;   // the least power of two of a row's dZ (0 in bf16)
-    int pad[61];
+    int exp;   // dW's sums are raised by this power of two (0 in bf16)
+    int up;    // kLinUp less the least that a row allows, of those seen so far; left zero
+    int pad[60];
 };
 
 constexpr int kLinBlock = kLinRows * kLinK * 2;  // 16 KB: 128 rows of a chunk
@@ -87,7 +88,7 @@ struct LinParams {
     const int *start;  // see lin_gather_kernel
     const int2 *sorted;
     int buckets;
-    const uint16_t *low;  // [rows_cap][d]: the rows that dW's product has
+    const uint16_t *low;  // [rows_cap][d]: the rows as dW's product has them
     float *acc;        // [split][rows_cap][d]
     int splits, first; // first: the first piece
     bool dh, dw;
@@ -872,7 +873,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
 
 // ------------------------------------------------------------------------------- rows
 // The live rows' places, and in fp16 the power of two that each row's dZ is raised by, so that the largest is of some 2^13
-// and p down to 2^-27 of it is not a subnormal number.  (|dZ| <= |g| + |g'| p |log p + H|, the last factors below 16.)  bf16 has fp32's range.
+// and p down to 2^-27 of it is not a subnormal number.  (|dZ| <= b = |g| + 16 |g'|, for p |log p + H| is below 16.)  bf16 has fp32's range.
 struct LinRowParams {
     LinHeader *head;
     int R;
@@ -885,16 +886,15 @@ struct LinRowParams {
 // What a CTA that finds the rows for itself keeps of them
 constexpr int kLinFew = 1024;
 struct LinFew {
-    int live, exp;
+    int live;
     int src[kLinFew], kexp[kLinFew], tokc[kLinFew];
 };
 // A CTA of THREADS; write: for the kernels behind it; keep: for itself
 template <int THREADS>
 __device__ __forceinline__ void lin_rows(const LinRowParams &p, bool write, LinFew *keep) {
-    __shared__ int s_warp[32], s_exp;
+    __shared__ int s_warp[32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int base = 0, least = 1 << 20;
-    if (threadIdx.x == 0) s_exp = 1 << 20;
+    int base = 0;
     if (threadIdx.x < 32) s_warp[threadIdx.x] = 0;
 #pragma unroll 1
     for (int r0 = 0; r0 < p.R; r0 += THREADS) {
@@ -922,29 +922,19 @@ __device__ __forceinline__ void lin_rows(const LinRowParams &p, bool write, LinF
             int k = 0;
             if (on && p.raise) {
                 const float b = (p.glp ? fabsf(p.glp[r]) : 0.f) + 16.f * (p.gent ? fabsf(p.gent[r]) : 0.f);
-                // 2^e > b >= 2^(e - 1) (a NaN, an infinity or 0: 0)
-                if (b > 0.f && b < INFINITY) {
-                    k = max(min(13 - (ilogbf(b) + 1), 120), -120);
-                    least = min(least, k);
-                }
+                // 2^e > b >= 2^(e - 1) (a NaN or an infinity: 0)
+                if (b < INFINITY) k = b > 0.f ? max(min(13 - (ilogbf(b) + 1), 120), -120) : 120;
             }
             if (write) p.kexp[r] = k;
             if (keep) keep->kexp[r] = k;
         }
     }
-    least = __reduce_min_sync(0xffffffffu, least);
-    if (lane == 0) atomicMin(&s_exp, least);
-    __syncthreads();
     if (threadIdx.x == 0) {
-        const int exp = s_exp == 1 << 20 ? 0 : s_exp;
         if (write) {
             p.head->live = base;
-            p.head->exp = exp;
+            p.head->exp = 0;
         }
-        if (keep) {
-            keep->live = base;
-            keep->exp = exp;
-        }
+        if (keep) keep->live = base;
     }
     __syncthreads();
 }
@@ -954,19 +944,21 @@ __global__ void __launch_bounds__(1024) lin_rows_kernel(LinRowParams p) {
     lin_rows<1024>(p, true, nullptr);
 }
 
-// The live rows side by side, zeros behind them up to a whole tile; in fp16, for dW, once more, each lowered by what its dZ is raised more
-// than the least: rows whose gradients are far below the largest's lose bits that would not reach dW's either.
+// The live rows side by side, zeros behind them up to a whole tile; in fp16, for dW, the power of two 2^E that its sums are raised by is found on the way:
+// dW = 2^-E sum (2^k dZ) (2^(E - k) h), k what the row's dZ is raised by, E the largest for which no 2^(E - k) |h| passes 2^15.
 // The CTAs behind those put the rows in the order of their tokens (and of the rows of one), `kLinSort` rows at a time, so that
 // dW's epilogue finds a tile's: sorted[start[b] .. start[b + 1]) are those of tile b.  A row's place is the number of rows before it, counted
 // by 8 lanes.
 // FEW: each CTA finds the rows for itself, the first one for the kernels behind it too (a launch less: gradient of 32 x 128 x 512 through the binding 33 -> 29 us, on the device 24.7 -> 24.2).
+constexpr int kLinUp = 512;  // (the least is 15 - 16 - 120, the greatest 15 + 23 + 120)
 struct LinGatherParams {
-    const LinHeader *head;
+    LinHeader *head;
     const uint16_t *h;
     int64_t stride;
     int d, tile;
     const int *src, *kexp;
-    uint16_t *out, *low;    // [rows_cap][d]; low null: not wanted
+    uint16_t *out;          // [rows_cap][d]
+    bool raise;             // 2^E is wanted
     int row_ctas;           // along x; the others sort
     const int *tokc;
     int2 *sorted;           // [rows_cap]: row, token
@@ -978,18 +970,16 @@ __global__ void __launch_bounds__(256) lin_gather_kernel(LinGatherParams p, LinR
     __shared__ std::conditional_t<FEW, LinFew, LinNoSmem> s_few;
     pdl_allow_dependents();
     pdl_wait_prior_grids();
-    int live, exp;
+    int live;
     const int *src = p.src, *kexp = p.kexp, *tokc = p.tokc;
     if constexpr (FEW) {
         lin_rows<256>(rows, blockIdx.x == 0 && blockIdx.y == 0, &s_few);
         live = s_few.live;
-        exp = s_few.exp;
         src = s_few.src;
         kexp = s_few.kexp;
         tokc = s_few.tokc;
     } else {
         live = p.head->live;
-        exp = p.head->exp;
     }
     const int lane = threadIdx.x & 31;
     if ((int)blockIdx.x >= p.row_ctas) {
@@ -1033,22 +1023,51 @@ __global__ void __launch_bounds__(256) lin_gather_kernel(LinGatherParams p, LinR
     }
     const int row = blockIdx.x * 8 + (threadIdx.x >> 5), x0 = blockIdx.y * kLinGatherCols, x1 = min(p.d, x0 + kLinGatherCols);
     if (row >= max((live + p.tile - 1) / p.tile, 1) * p.tile) return;
-    uint16_t *o = p.out + (int64_t)row * p.d, *o2 = p.low ? p.low + (int64_t)row * p.d : nullptr;
-    const int r = row < live ? src[row] : 0, down = o2 && row < live ? min(exp - kexp[r], 0) : 0;
+    uint16_t *o = p.out + (int64_t)row * p.d;
+    const int r = row < live ? src[row] : 0;
     const uint16_t *h = p.h + r * p.stride;
-    const float f = pow2f(max(down, -126));
+    uint32_t top = 0;
 #pragma unroll 4
     for (int x = x0 + 8 * lane; x < x1; x += 256) {
         const uint4 v = row < live ? *reinterpret_cast<const uint4 *>(h + x) : make_uint4(0, 0, 0, 0);
         *reinterpret_cast<uint4 *>(o + x) = v;
-        if (!o2) continue;
+        top = __vmaxu2(top, __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu)));
+    }
+    if (!p.raise || row >= live) return;
+    const uint32_t most = __reduce_max_sync(0xffffffffu, max(top & 0xffff, top >> 16));
+    if (lane || !most) return;
+    // |h| < 2^e of these (an infinity or a NaN: as the largest number)
+    const int e = most >= 1024 ? min((int)(most >> 10) - 14, 16) : 8 - __clz(most), up = kLinUp - (15 - e + kexp[r]);
+    if (up > *(volatile int *)&p.head->up) atomicMax(&p.head->up, up);
+}
+
+// fp16: the rows as dW's product has them, 2^(E - k) h.  A row keeps all bits but of elements that come out below 2^-14: with |dZ| 2^k < 2^13 they are off by
+// 2^-25 2^13 2^-E at most, 2^-38 of the largest b |h| of any row.  Where that is within 2^13, it is less than half of fp16's least step.
+struct LinLowParams {
+    LinHeader *head;
+    int d, tile;
+    const int *src, *kexp;
+    const uint16_t *rows;
+    uint16_t *low;
+};
+__global__ void __launch_bounds__(256) lin_low_kernel(LinLowParams p) {
+    pdl_allow_dependents();
+    pdl_wait_prior_grids();
+    const int live = p.head->live, up = p.head->up, exp = up ? min(kLinUp - up, 126) : 0;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) p.head->exp = exp;
+    const int lane = threadIdx.x & 31, row = blockIdx.x * 8 + (threadIdx.x >> 5), x0 = blockIdx.y * kLinGatherCols, x1 = min(p.d, x0 + kLinGatherCols);
+    if (row >= max((live + p.tile - 1) / p.tile, 1) * p.tile) return;
+    const float f = pow2f(row < live ? max(exp - p.kexp[p.src[row]], -126) : 0);  // (of zeros behind the rows: any)
+#pragma unroll 4
+    for (int x = x0 + 8 * lane; x < x1; x += 256) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(p.rows + (int64_t)row * p.d + x);
         uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float2 y = __half22float2(*reinterpret_cast<const __half2 *>(&w[e]));
             w[e] = pack_half2(y.x * f, y.y * f);
         }
-        *reinterpret_cast<uint4 *>(o2 + x) = make_uint4(w[0], w[1], w[2], w[3]);
+        *reinterpret_cast<uint4 *>(p.low + (int64_t)row * p.d + x) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
@@ -1110,7 +1129,7 @@ __global__ void __launch_bounds__(256) lin_join_kernel(LinJoinParams p) {
 // dH: the splits' sums in their order and what rounding took at the row's token, times scale and what dZ was raised by, to the rows' places; 0
 // for rows of padding
 struct LinOutParams {
-    const LinHeader *head;
+    LinHeader *head;
     int R, d, splits, rows_cap;
     const int *pos, *kexp;
     const float *acc, *delta;
@@ -1129,6 +1148,7 @@ template <int TYPE>
 __global__ void __launch_bounds__(256) lin_out_kernel(LinOutParams p) {
     pdl_wait_prior_grids();
     const bool failed = p.head->err != 0;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) p.head->up = 0;
     const int lane = threadIdx.x & 31, r = blockIdx.x * 8 + (threadIdx.x >> 5), x0 = blockIdx.y * kLinOutCols, x1 = min(p.d, x0 + kLinOutCols);
     if (failed && p.dw)
         for (int64_t v = r; v < p.V; v += 8 * (int64_t)gridDim.x)

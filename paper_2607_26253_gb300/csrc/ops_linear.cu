@@ -55,16 +55,16 @@ T *at(void *ws, size_t off) {
     return reinterpret_cast<T *>(static_cast<uint8_t *>(ws) + off);
 }
 
-// The live rows gathered, with what the gradient's rows are raised by, and (where dW is wanted) the order of their tokens
+// The live rows gathered, with what the gradient's rows are raised by, and (where dW is wanted) the order of their tokens and the rows as its product has them
 template <int TYPE>
 void gather(cudaStream_t s, void *ws, const LinPlan &q, const Operand &h, const int32_t *tokens, const float *glp, const float *gent, bool backward,
-            bool sort) {
+            bool weights) {
     const int R = (int)h.rows, d = (int)h.d;
     int *kexp = backward ? at<int>(ws, q.kexp) : nullptr, *tokc = backward ? at<int>(ws, q.tokc) : nullptr;
     const LinRowParams rows{at<LinHeader>(ws, 0), R, tokens, glp, gent, at<int>(ws, q.src), at<int>(ws, q.pos), kexp, tokc, TYPE == SARA_FP16};
-    const int row_ctas = q.rows_cap / 8, sort_ctas = sort ? (int)std::min<int64_t>(((int64_t)R + q.buckets + 32) / 32, 2048) : 0;
+    const int row_ctas = q.rows_cap / 8, sort_ctas = weights ? (int)std::min<int64_t>(((int64_t)R + q.buckets + 32) / 32, 2048) : 0;
     const LinGatherParams p{at<LinHeader>(ws, 0), static_cast<const uint16_t *>(h.p), h.stride, d, kLinRows * q.ctas, at<int>(ws, q.src), kexp,
-                            at<uint16_t>(ws, q.rows), backward && TYPE == SARA_FP16 ? at<uint16_t>(ws, q.low) : nullptr, row_ctas, tokc,
+                            at<uint16_t>(ws, q.rows), weights && TYPE == SARA_FP16, row_ctas, tokc,
                             backward ? at<int2>(ws, q.sorted) : nullptr, backward ? at<int>(ws, q.start) : nullptr, q.buckets};
     const dim3 grid((unsigned)(row_ctas + sort_ctas), (unsigned)((d + kLinGatherCols - 1) / kLinGatherCols));
     if (R <= kLinFew) {
@@ -74,6 +74,9 @@ void gather(cudaStream_t s, void *ws, const LinPlan &q, const Operand &h, const 
         CK(cudaGetLastError());
         launch_cluster(s, true, grid, dim3(256), 0, 1, lin_gather_kernel<false>, p, rows);
     }
+    if (!p.raise) return;
+    const LinLowParams low{p.head, d, p.tile, p.src, kexp, p.out, at<uint16_t>(ws, q.low)};
+    launch_cluster(s, true, dim3((unsigned)row_ctas, grid.y), dim3(256), 0, 1, lin_low_kernel, low);
 }
 
 template <int CTAS, int TYPE>

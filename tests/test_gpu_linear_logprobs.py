@@ -458,3 +458,84 @@ def test_rows_found_and_sorted_by_token(pkg, R, V, how, typ):
     o = pkg.linear_logprobs(h, w, _i32(tok))
     again = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, g, gh)
     assert torch.equal(y[0], again[0]) and torch.equal(y[1], again[1])
+
+
+def _weights_bound(h, w, tok, g, gh, dz, want):
+    """What dW may be off by in fp16 (scale 1): dz by what _check_grad has (its exponents, one rounding but at the row's token, half a step of fp16 below 2^-27 of
+    the row's largest possible b = |g| + 16 |g'|), sums of R products in fp32, one rounding of the result; and rows whose b max|h| is far below the
+    largest's lose bits of h: 2^-38 of the largest b max|h|, times dz / b."""
+    hn, wn, gn, ghn = np.abs(_np(h)), _np(w), np.abs(_np(g))[:, None], np.abs(_np(gh))[:, None]
+    z = _np(h) @ wn.T
+    lp = z - z.max(1, keepdims=True)
+    lp -= np.log(np.exp(lp).sum(1, keepdims=True))
+    H = -(np.exp(lp) * lp).sum(1, keepdims=True)
+    e = (2 * _logit_error(_np(h), wn, 1.0) + _sum_error(len(wn)))[:, None]
+    b, own = gn + 16 * ghn, np.arange(len(wn)) == np.asarray(tok)[:, None]
+    err = (e + 8 * U * (np.abs(lp) + 1)) * np.exp(lp) * (gn + ghn * (np.abs(lp + H) + 2 + H)) + 4 * U * np.abs(dz) + 4 * U * gn * own
+    err += np.where(own, 0, HALF["fp16"] * np.abs(dz)) + 2.0 ** -25 * 2.0 ** -12 * b
+    err += HALF["fp16"] ** 2 * np.abs(dz)
+    low = 2.0 ** -38 * (b[:, 0] * hn.max(1)).max() * (np.abs(dz) / np.maximum(b, 1e-300)).sum(0)
+    return err.T @ hn + (_chain(len(hn)) + 40 * U) * (np.abs(dz).T @ hn) + HALF["fp16"] * (1 + 1e-3) * np.abs(want) + LEAST["fp16"] + low[:, None]
+
+
+@pytest.mark.parametrize("R,up,down,big", [(40, 10, -10, 1.0), (300, 12, -12, 1.0), (40, 3, -3, 2.0 ** -10), (200, 14, -14, 1.0), (60, 0, -9, 2.0 ** 5)])
+def test_weights_gradient_of_rows_of_small_weight_in_fp16(pkg, R, up, down, big):
+    """Rows of small weight beside rows of large weight, whose hidden states have other dims: dW's there is well within fp16, and keeps its bits."""
+    import torch
+    rng = np.random.default_rng(R)
+    d, V = 128, 900
+    large = np.arange(R) % 2 == 0
+    h, w = rng.standard_normal((R, d)) * big, rng.standard_normal((V, d)) * (2 / np.sqrt(d)) / big
+    h[large, d // 2:], h[~large, :d // 2] = 0, 0
+    tok = rng.integers(0, V, R)
+    h, w = torch.from_numpy(h).cuda().half(), torch.from_numpy(w).cuda().half()
+    size = np.where(large, 2.0 ** up, 2.0 ** down)
+    g, gh = _f32(rng.choice([-1, 1], R) * size * (0.5 + rng.random(R))), _f32(rng.standard_normal(R) * size / 64)
+    o = pkg.linear_logprobs(h, w, _i32(tok))
+    _, dw = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, g, gh)
+    _, want, dz = oracle.linear_grad(_np(h), _np(w), tok, _np(g), _np(gh))
+    tol = _weights_bound(h, w, tok, g, gh, dz, want)
+    bad = (np.abs(_np(dw) - want) > tol) & (np.abs(want) < 65504)
+    assert not bad.any(), np.max(np.abs(_np(dw) - want)[bad] / tol[bad])
+
+
+def test_weights_gradient_of_very_different_rows_in_fp16(pkg):
+    """Weights over 2^-30 .. 2^14, some of them 0, hidden states of very different sizes, some of them 0 too."""
+    import torch
+    rng = np.random.default_rng(16)
+    for R in (90, 250):
+        d, V = 64, 700
+        h = rng.standard_normal((R, d)) * 2.0 ** rng.integers(-8, 3, R)[:, None]
+        h[3], h[5], h[R - 2] = 60000.0, 0, 2.0 ** -24  # (the first of no weight)
+        h, w = torch.from_numpy(h).cuda().half(), torch.from_numpy(rng.standard_normal((V, d)) / np.sqrt(d)).cuda().half()
+        tok = rng.integers(0, V, R)
+        tok[4] = -1
+        g = rng.standard_normal(R) * 2.0 ** rng.integers(-30, 15, R)
+        g[3], g[7], g[8] = 0, 1e-35, -1e-40
+        gh = np.where(rng.random(R) < 0.5, 0, g * 0.1)
+        g[4] = 2.0 ** 100  # (padding)
+        o = pkg.linear_logprobs(h, w, _i32(tok))
+        for size in (1.0, 2.0 ** -20):
+            gs, ghs = _f32(g * size), _f32(gh * size)
+            _, dw = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, gs, ghs)
+            h0 = h.clone()
+            h0[4], gs[4], ghs[4] = 0, 0, 0
+            _, want, dz = oracle.linear_grad(_np(h0), _np(w), tok, _np(gs), _np(ghs))
+            tol = _weights_bound(h0, w, tok, gs, ghs, dz, want)
+            bad = (np.abs(_np(dw) - want) > tol) & (np.abs(want) < 60000)
+            assert not bad.any(), np.max(np.abs(_np(dw) - want)[bad] / tol[bad])
+
+
+def test_weights_gradient_does_not_depend_on_calls_before(pkg):
+    """One workspace for rows of large weight and of small, in fp16: what a call finds of its rows is not left for the next."""
+    import torch
+    rng = np.random.default_rng(17)
+    R, d, V = 64, 64, 300
+    h, w = _inputs(rng, R, d, V, "fp16")
+    tok, g = _i32(rng.integers(0, V, R)), _f32(rng.standard_normal(R))
+    o = pkg.linear_logprobs(h, w, tok)
+    fresh = lambda k: pkg.linear_logprobs_backward(h, w, tok, o.stats, o.entropy, g * k, None)  # noqa: E731
+    ws = pkg.linear_logprobs_workspace(R, d, V, backward=True)
+    for k in (1.0, 2.0 ** 12, 2.0 ** -12, 1.0, 0.0, 2.0 ** -6):
+        a, b = fresh(k), pkg.linear_logprobs_backward(h, w, tok, o.stats, o.entropy, g * k, None, workspace=ws)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]), k
