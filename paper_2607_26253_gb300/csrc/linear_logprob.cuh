@@ -748,11 +748,13 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                                 float z = 0.f;
 #pragma unroll
                                 for (int e = 0; e < 64; ++e) z = cc + e == at ? v[cc + e] : z;
-                                // 1 - p from the logarithm.  The logit is made in one sum here: a token within its error of the maximum is the maximum,
-                                // or shares it, where 1 - p does not depend on the difference (1 - p = 1e-5 at a logit of 22: off by 2.6 times itself without)
+                                // 1 - p from the logarithm.  A token within the error of its logit's sums (bf16: one; fp16: parts of 512 products at most, as the
+                                // scores') of the maximum is the maximum, or shares it, where 1 - p depends little on the difference (1 - p = 1e-5 at a logit
+                                // of 22 in bf16: off by 2.6 times itself without.  fp16 with bf16's error, 4,096 dims, a token 1.4e-3 below a maximum of 100: 1 - p off by 1.4e-3)
                                 const int row = p.src[m];
                                 float t = fmaf(z, p.scale, -mx);
-                                if (fabsf(t) <= (p.d / 16 + 8) * 0x1p-24f * fabsf(mx)) t = 0.f;
+                                const int steps = TYPE == SARA_FP16 ? min(p.d / 16, 32) + p.d / 512 : p.d / 16;
+                                if (fabsf(t) <= (steps + 8) * 0x1p-24f * fabsf(mx)) t = 0.f;
                                 const float lp = max_nan(t - ls, -700.f), H = p.gent ? p.entropy[row] : 0.f, gh = p.gent ? p.gent[row] : 0.f;
                                 const float x = (wrong ? __int_as_float(0x7fc00000) : pow2f(p.kexp[row])) *
                                                 (-(p.glp ? p.glp[row] : 0.f) * expm1f(lp) - gh * expf(lp) * (lp + H));

@@ -539,3 +539,23 @@ def test_weights_gradient_does_not_depend_on_calls_before(pkg):
     for k in (1.0, 2.0 ** 12, 2.0 ** -12, 1.0, 0.0, 2.0 ** -6):
         a, b = fresh(k), pkg.linear_logprobs_backward(h, w, tok, o.stats, o.entropy, g * k, None, workspace=ws)
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]), k
+
+
+def test_two_likely_tokens_in_fp16(pkg):
+    """Logits of 100 and 46 steps of 2^-15 less, exact in fp32 whatever the order: 1 - p of either depends on the difference.  The gradient's first half
+    of dims is the first token's, the other half the second's.  Bound: the result's rounding, and 300 steps of fp32 in log S and in exponents."""
+    import torch
+    d, V = 4096, 300
+    for R in (3, 200):
+        h = torch.ones((R, d), dtype=torch.float16, device="cuda")
+        w = torch.zeros((V, d), dtype=torch.float16, device="cuda")
+        w[17, :d // 2], w[250, d // 2:] = 100 / 2048, 100 / 2048
+        w[250, d // 2:d // 2 + 46] -= 2.0 ** -15
+        for t in (17, 250):
+            tok, g = np.full(R, t), _f32(np.ones(R))
+            o = pkg.linear_logprobs(h, w, _i32(tok))
+            dh, _ = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, g, grad_weight=False)
+            want, _, dz = oracle.linear_grad(_np(h), _np(w), tok, np.ones(R), np.zeros(R))
+            own = _np(w)[t][None] != 0  # the other token's dz is rounded to fp16
+            tol = (HALF["fp16"] * np.where(own, 1, 2) + 300 * U) * np.abs(want) + LEAST["fp16"]
+            assert (np.abs(_np(dh) - want) <= tol).all(), (R, t, np.max(np.abs(_np(dh) - want) / tol))
