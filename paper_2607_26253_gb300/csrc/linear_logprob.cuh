@@ -15,7 +15,7 @@
 // Rows of padding (token < 0) are left out: the live rows are gathered first, so that they cost nothing and their contents,
 // whatever they are, reach nothing.
 //
-// The tensor core cuts its sums off: about half a step of fp32 each 16 products, all towards zero.  A logit's products are therefore
+// The tensor core cuts its sums off: one to two steps of fp32 each 16 products, all towards zero.  A logit's products are therefore
 // summed in parts, which the epilogue adds.
 // dZ enters the products in 16 bits.  Its largest element by far is mostly the token's own: what that one's rounding left off is
 // kept (delta) and added to both gradients in fp32.
@@ -97,9 +97,12 @@ struct LinParams {
     bool wide;         // its rows' blocks are 32-byte aligned
 };
 
-// Chunks of a part of a logit's sum: with two CTAs a tile's epilogue has no time for more parts; the errors of a few rows, which nothing averages
+// Chunks of a part of a logit's sum.  Scores and fp16: with two CTAs a tile's epilogue has no time for more parts; the errors of a few rows, which nothing averages
 // away, get some more (1 x 2,048 x 151,936: 109 us with 2, 113 with 1; entropies of 1 x 944 x 32,990 off by 4.3e-6 and below 1e-6)
 __device__ __forceinline__ int lin_part(int ctas, int rows) { return ctas == 2 ? 8 : rows <= 8 ? 1 : 2; }
+// The gradient's in bf16, whose products have fewer bits to cut off and whose results have 8: one sum up to 2,048 dims, LONG sums of parts of as many beyond
+// (65,536 products of one sign in one sum: a logit of 36 was off by 0.012, and p by as much of itself; a loop over one part costs 128 x 1,536 x 151,936 3 %).
+constexpr int kLinLongPart = 32;
 struct LinSmem {
     uint64_t full[6], empty[6], acc_full[2], acc_empty[2], drain;
     uint32_t tmem_base;
@@ -342,14 +345,13 @@ __device__ __forceinline__ void lin_tmem_load128(uint32_t taddr, float (&v)[128]
         : "memory");
 }
 
-template <int MODE, int CTAS, int TYPE, bool STAGED>
+template <int MODE, int CTAS, int TYPE, bool STAGED, bool LONG = false>
 __global__ void __launch_bounds__(kLinThreads, 1)
 lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmA2,
            const __grid_constant__ CUtensorMap tmB2, const __grid_constant__ CUtensorMap tmOut, LinParams p) {
     constexpr int STAGES = lin_stages(CTAS, STAGED), STAGE = lin_stage_bytes(CTAS), COLS = kLinCols;
-    // (bf16's products have few bits to cut off: the gradient's logits are summed in one there.  In fp16 2,048 of them lose 2^-15 of the sum)
-    constexpr bool PARTED = MODE == LIN_SCORE || (MODE == LIN_DZ && TYPE == SARA_FP16);
-    const int PART = lin_part(CTAS, p.R);
+    constexpr bool PARTED = MODE == LIN_SCORE || (MODE == LIN_DZ && (TYPE == SARA_FP16 || LONG));
+    const int PART = LONG ? kLinLongPart : lin_part(CTAS, p.R);
     extern __shared__ uint8_t smem_raw[];
     __shared__ LinSmem S;
     __shared__ __align__(16) std::conditional_t<MODE == LIN_SCORE, LinScoreSmem, std::conditional_t<MODE == LIN_GRAD, LinGradSmem, LinNoSmem>> E;
@@ -748,13 +750,14 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                                 float z = 0.f;
 #pragma unroll
                                 for (int e = 0; e < 64; ++e) z = cc + e == at ? v[cc + e] : z;
-                                // 1 - p from the logarithm.  A token within the error of its logit's sums (bf16: one; fp16: parts of 512 products at most, as the
-                                // scores') of the maximum is the maximum, or shares it, where 1 - p depends little on the difference (1 - p = 1e-5 at a logit
-                                // of 22 in bf16: off by 2.6 times itself without.  fp16 with bf16's error, 4,096 dims, a token 1.4e-3 below a maximum of 100: 1 - p off by 1.4e-3)
+                                // 1 - p from the logarithm.  A token within the error of its logit's sums of the maximum (of either call's, whose parts may be
+                                // others) is the maximum, or shares it, where 1 - p depends little on the difference.  (Each 16 products lose 2 steps of the part's sum at
+                                // most.  1 - p = 1e-5 at a logit of 22 in bf16: off by 2.6 times itself without.  fp16 with the error of one sum over 4,096 dims, a token 1.4e-3
+                                // below a maximum of 100: 1 - p off by 1.4e-3)
                                 const int row = p.src[m];
                                 float t = fmaf(z, p.scale, -mx);
-                                const int steps = TYPE == SARA_FP16 ? min(p.d / 16, 32) + p.d / 512 : p.d / 16;
-                                if (fabsf(t) <= (steps + 8) * 0x1p-24f * fabsf(mx)) t = 0.f;
+                                constexpr int kSteps = TYPE == SARA_FP16 ? 8 * kLinK / 16 : kLinLongPart * kLinK / 16;
+                                if (fabsf(t) <= (2 * min(p.d / 16, kSteps) + p.d / 512 + 8) * 0x1p-24f * fabsf(mx)) t = 0.f;
                                 const float lp = max_nan(t - ls, -700.f), H = p.gent ? p.entropy[row] : 0.f, gh = p.gent ? p.gent[row] : 0.f;
                                 const float x = (wrong ? __int_as_float(0x7fc00000) : pow2f(p.kexp[row])) *
                                                 (-(p.glp ? p.glp[row] : 0.f) * expm1f(lp) - gh * expf(lp) * (lp + H));

@@ -41,10 +41,10 @@ bool sizes_ok(int type, int R, int d, int V, float scale) {
            V <= (1 << 24) && scale > 0.f && std::isfinite(scale);
 }
 
-template <int MODE, int CTAS, int TYPE, bool STAGED>
+template <int MODE, int CTAS, int TYPE, bool STAGED, bool LONG = false>
 void launch(cudaStream_t s, int sms, bool after, const CUtensorMap &a, const CUtensorMap &b, const CUtensorMap &a2, const CUtensorMap &b2,
             const CUtensorMap &out, const LinParams &p) {
-    const auto kern = lin_kernel<MODE, CTAS, TYPE, STAGED>;
+    const auto kern = lin_kernel<MODE, CTAS, TYPE, STAGED, LONG>;
     static SmemOnce smem;
     smem.ask(kern, lin_smem(CTAS, STAGED));
     launch_cluster(s, after, dim3((unsigned)(sms / CTAS * CTAS)), dim3(kLinThreads), lin_smem(CTAS, STAGED), CTAS, kern, a, b, a2, b2, out, p);
@@ -149,7 +149,8 @@ void gradient(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand
         p.out = at<uint16_t>(ws, q.dz);
         p.out_stride = 64;
         p.wide = true;
-        launch<LIN_DZ, CTAS, TYPE, CTAS == 1>(s, sms, true, xk, wk, xk, wk, dzs, p);
+        if (TYPE == SARA_BF16 && d > kLinLongPart * kLinK) launch<LIN_DZ, CTAS, TYPE, CTAS == 1, TYPE == SARA_BF16>(s, sms, true, xk, wk, xk, wk, dzs, p);
+        else launch<LIN_DZ, CTAS, TYPE, CTAS == 1>(s, sms, true, xk, wk, xk, wk, dzs, p);
         p.out = static_cast<uint16_t *>(const_cast<void *>(dw.p));
         p.out_stride = dw.stride;
         p.wide = (reinterpret_cast<uintptr_t>(dw.p) & 31) == 0 && dw.stride % 16 == 0;

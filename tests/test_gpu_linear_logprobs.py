@@ -559,3 +559,56 @@ def test_two_likely_tokens_in_fp16(pkg):
             own = _np(w)[t][None] != 0  # the other token's dz is rounded to fp16
             tol = (HALF["fp16"] * np.where(own, 1, 2) + 300 * U) * np.abs(want) + LEAST["fp16"]
             assert (np.abs(_np(dh) - want) <= tol).all(), (R, t, np.max(np.abs(_np(dh) - want) / tol))
+
+
+@pytest.mark.parametrize("R", [4, 256])
+def test_logits_of_long_hidden_states_in_bf16(pkg, R):
+    """65,536 products of one sign to a logit of 36, which two tokens have: the probability of each is 1/2, and the gradient of a third is minus the weights of
+    either, exactly.  An error of p of 1/512 shows; parts of 2,048 products lose at most 2^-15 of the logit, 1.1e-3."""
+    import torch
+    rng = np.random.default_rng(13)
+    d, V = 65536, 300
+    h = torch.from_numpy(rng.integers(128, 256, d) * 2.0 ** -7).cuda().bfloat16().repeat(R, 1)
+    w = torch.zeros((V, d), dtype=torch.bfloat16, device="cuda")
+    w[3] = torch.from_numpy(rng.integers(128, 256, d) * 2.0 ** -19).cuda().bfloat16()
+    w[7] = w[3]
+    z = float((h[0].double() * w[3].double()).sum())
+    assert 35 < z < 37
+    tok, g = _i32(np.full(R, 100)), _f32(np.ones(R))
+    o = pkg.linear_logprobs(h, w, tok)
+    assert abs(float(o.logprob[0]) + z + np.log(2)) < 1e-3
+    dh, dw = pkg.linear_logprobs_backward(h, w, tok, o.stats, o.entropy, g)
+    assert torch.equal(dh, -w[3].expand(R, d)), float((dh.float() / w[3].float()).mean())
+    assert torch.equal(dw[3], -R / 2 * h[0]) and torch.equal(dw[7], dw[3])
+
+
+@pytest.mark.parametrize("typ", ["bf16", "fp16"])
+@pytest.mark.parametrize("R,d,V,logit", [(3, 4096, 3000, 17), (2, 8192, 2000, 33), (200, 8192, 900, 17), (130, 4096, 700, 34), (1, 2048, 5000, 16.5)])
+def test_gradients_of_nearly_certain_tokens_of_long_hidden_states(pkg, R, d, V, logit, typ):
+    """Logits next to a power of two, of products of one sign: the sums that the gradient makes again lose the most there."""
+    test_gradients_of_tokens_that_are_nearly_certain(pkg, R, d, V, logit, typ)
+
+
+@pytest.mark.parametrize("typ", ["bf16", "fp16"])
+@pytest.mark.parametrize("R,d,V,logit", [(140, 1024, 2000, 17), (200, 4096, 900, 20)])
+def test_scores_in_small_batches_gradients_in_one(pkg, R, d, V, logit, typ):
+    """Few rows' logits are summed in other parts than many rows': 1 - p of nearly certain tokens, from the scores of a few rows at a time.  Bounds as in
+    test_gradients_of_tokens_that_are_nearly_certain for up to 128 rows."""
+    import torch
+    rng = np.random.default_rng(R + d)
+    h = torch.from_numpy(rng.standard_normal((R, d))).cuda().to(_dtype(typ))
+    w = torch.from_numpy(rng.standard_normal((V, d)) / np.sqrt(d)).cuda().to(_dtype(typ))
+    tok = rng.permutation(V)[:R]
+    for r in range(R):
+        w[tok[r]] = (h[r].double() * (logit / float((h[r].double() ** 2).sum()))).to(w.dtype)
+    t, step = _i32(tok), 20
+    o = [pkg.linear_logprobs(h[a:a + step], w, t[a:a + step]) for a in range(0, R, step)]
+    stats, entropy = torch.cat([x.stats for x in o]), torch.cat([x.entropy for x in o])
+    g, gh = torch.from_numpy(rng.standard_normal(R)).float().cuda(), torch.from_numpy(rng.standard_normal(R)).float().cuda() / 64
+    got, _ = pkg.linear_logprobs_backward(h, w, t, stats, entropy, g, gh)
+    want, _, dz = oracle.linear_grad(_np(h), _np(w), tok, _np(g), _np(gh))
+    size, mag = np.abs(_np(h) @ _np(w).T).max(1, keepdims=True), np.abs(dz) @ np.abs(_np(w))
+    tol = (2 * HALF[typ] + 4 * (d / 16 + 16) * U * (size + 1) + 1e-4) * mag + LEAST[typ]
+    if typ == "fp16":
+        tol += (2.0 ** -25 * 2.0 ** -12 * (np.abs(_np(g)) + 16 * np.abs(_np(gh))))[:, None] * np.abs(_np(w)).sum(0)
+    assert (np.abs(_np(got) - want) <= tol).all(), np.max(np.abs(_np(got) - want) / tol)
