@@ -612,3 +612,70 @@ def test_scores_in_small_batches_gradients_in_one(pkg, R, d, V, logit, typ):
     if typ == "fp16":
         tol += (2.0 ** -25 * 2.0 ** -12 * (np.abs(_np(g)) + 16 * np.abs(_np(gh))))[:, None] * np.abs(_np(w)).sum(0)
     assert (np.abs(_np(got) - want) <= tol).all(), np.max(np.abs(_np(got) - want) / tol)
+
+
+@pytest.mark.parametrize("how", ["spread", "few"])
+@pytest.mark.parametrize("live", [70000, 131100])
+def test_more_rows_than_are_sorted_together(pkg, live, how):
+    """Rows are put in their tokens' order 65,536 at a time.  All logits alike, so that p = 1 / V; each token's rows come in groups of 17, 7 of weight 1 and hidden states of
+    1 and 10 of 0.7 and -1, whose gradients add up to nothing: what is left of dW in bf16 are the roundings of the other tokens' dz, which are known, and those of the
+    rows' own, which are put right row by row (0.02 a group: a row left out, or counted twice, is 0.0006 or 0.0016 off).  Bound: sums of R
+    products in steps of 16, each cut off at 2^-23 of a partial sum (of some 1 in a group and what is left of them behind it), and the result's rounding."""
+    import torch
+    rng = np.random.default_rng(live)
+    d, V, n = 64, 300, live // 17
+    assert (n + 1) * 17 > 65536
+    g17 = np.array([1, -.7, -.7, 1, -.7, 1, -.7, -.7, 1, -.7, 1, -.7, -.7, 1, -.7, 1, -.7])  # (partial sums within 1.2)
+    assert abs(g17.sum()) < 1e-9
+    tok = np.repeat(rng.integers(0, V, n) if how == "spread" else rng.integers(250, 253, n), 17)
+    sign, g = np.tile(np.sign(g17), n), np.tile(np.abs(g17), n)
+    R = 17 * n + 3000  # padding among them
+    at = np.sort(rng.permutation(R)[:17 * n])
+    toks, gs, hs = np.full(R, -1), np.full(R, 5.0), np.full(R, 9.0)
+    toks[at], gs[at], hs[at] = tok, g, sign
+    h = torch.from_numpy(hs).cuda().bfloat16()[:, None].repeat(1, d)
+    w = torch.zeros((V, d), dtype=torch.bfloat16, device="cuda")
+    ws, wsb = (pkg.linear_logprobs_workspace(R, d, V, backward=x) for x in (False, True))
+    o = pkg.linear_logprobs(h, w, _i32(toks), workspace=ws)
+    lp = _np(o.logprob)
+    assert (lp[toks < 0] == 0).all() and np.abs(lp[at] + np.log(V)).max() < 1e-5
+    dh, dw = pkg.linear_logprobs_backward(h, w, _i32(toks), o.stats, o.entropy, _f32(gs), workspace=wsb)
+    assert not dh.any()
+    bf16 = lambda x: torch.tensor(x, dtype=torch.float32).bfloat16().double().numpy()  # noqa: E731
+    g32 = g.astype(np.float32).astype(np.float64)
+    own = np.bincount(tok, sign * g32 * (1 - 1 / V), V)
+    other = sign * bf16(-g32 / V)
+    want = own + other.sum() - np.bincount(tok, other, V)
+    got = _np(dw)
+    rows = np.bincount(tok, minlength=V).max()
+    part = max(1.2, 0.02 * rows / 17 + abs(other.sum()))
+    tol = (live / 16 + 8) * 2.0 ** -23 * part + rows * 2.0 ** -24 * part + HALF["bf16"] * np.abs(want) + 1e-6
+    assert (got == got[:, :1]).all()
+    assert (np.abs(got[:, 0] - want) <= tol).all(), (np.max(np.abs(got[:, 0] - want) / tol), got[:4, 0], want[:4])
+
+
+def test_gradients_of_more_rows_than_are_sorted_together(pkg):
+    """Some 70,000 rows with logits of their own: a sample of them, and of the tokens, against 64 bits."""
+    import torch
+    rng = np.random.default_rng(70)
+    R, d, V = 70100, 64, 300
+    h, w = _inputs(rng, R, d, V, "bf16")
+    tok = rng.integers(0, V, R)
+    tok[rng.random(R) < 0.02] = -1
+    g, gh = _f32(rng.standard_normal(R)), _f32(0.1 * rng.standard_normal(R))
+    o = pkg.linear_logprobs(h, w, _i32(tok))
+    dh, dw = pkg.linear_logprobs_backward(h, w, _i32(tok), o.stats, o.entropy, g, gh)
+    some = np.unique(np.concatenate([rng.integers(0, R, 200), [0, 65535, 65536, 65537, R - 1]]))
+    at = torch.from_numpy(some).cuda()
+    _check(type(o)(o.logprob[at], o.entropy[at], o.stats[at]), h[at], w, tok[some], 1.0)
+    _check_grad((dh[at], None), h[at], w, tok[some], g[at], gh[at], 1.0, "bf16")
+    z = h.double() @ w.double().t()
+    lp = torch.log_softmax(z, 1)
+    dz = -g.double()[:, None] * lp.exp() - gh.double()[:, None] * lp.exp() * (lp - (lp.exp() * lp).sum(1, keepdim=True))
+    t = torch.from_numpy(tok).cuda()
+    dz[t >= 0, t[t >= 0]] += g.double()[t >= 0]
+    dz[t < 0] = 0
+    want = dz.t() @ h.double()
+    mag = dz.abs().t() @ h.double().abs()
+    assert bool(((dw.double() - want).abs() <= (_chain(R) + HALF["bf16"]) * mag + HALF["bf16"] * want.abs()).all())
+    assert float((dw.double() - want).norm()) <= 1.5 * HALF["bf16"] * float(want.norm())
