@@ -103,6 +103,9 @@ __device__ __forceinline__ int lin_part(int ctas, int rows) { return ctas == 2 ?
 // The gradient's in bf16, whose products have fewer bits to cut off and whose results have 8: one sum up to 2,048 dims, LONG sums of parts of as many beyond
 // (65,536 products of one sign in one sum: a logit of 36 was off by 0.012, and p by as much of itself; a loop over one part costs 128 x 1,536 x 151,936 3 %).
 constexpr int kLinLongPart = 32;
+// Gradients of more than kLinLong chunks of rows or tokens are LONG too, in parts (fp16: dW of 262,144 rows, of one sign in one sum, was off by 1.7e-3, dH of a
+// vocabulary of 780,000 by 1.1e-2).  Sums of one sign lost 2 to 4 times 2^-24 of themselves each 16 products: 3 to 6e-4 at kLinLong chunks.
+constexpr int kLinLong = 640, kLinGradPart = 64;
 struct LinSmem {
     uint64_t full[6], empty[6], acc_full[2], acc_empty[2], drain;
     uint32_t tmem_base;
@@ -350,8 +353,8 @@ __global__ void __launch_bounds__(kLinThreads, 1)
 lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmA2,
            const __grid_constant__ CUtensorMap tmB2, const __grid_constant__ CUtensorMap tmOut, LinParams p) {
     constexpr int STAGES = lin_stages(CTAS, STAGED), STAGE = lin_stage_bytes(CTAS), COLS = kLinCols;
-    constexpr bool PARTED = MODE == LIN_SCORE || (MODE == LIN_DZ && (TYPE == SARA_FP16 || LONG));
-    const int PART = LONG ? kLinLongPart : lin_part(CTAS, p.R);
+    constexpr bool PARTED = LONG || MODE == LIN_SCORE || (MODE == LIN_DZ && TYPE == SARA_FP16);
+    const int PART = !LONG ? lin_part(CTAS, p.R) : MODE == LIN_GRAD ? kLinGradPart : kLinLongPart;
     extern __shared__ uint8_t smem_raw[];
     __shared__ LinSmem S;
     __shared__ __align__(16) std::conditional_t<MODE == LIN_SCORE, LinScoreSmem, std::conditional_t<MODE == LIN_GRAD, LinGradSmem, LinNoSmem>> E;
@@ -457,7 +460,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             int a = 0;
 #pragma unroll 1
             for (int k = j.k0; k < j.k1; ++k) {
-                const bool begins = PARTED ? k % PART == 0 : k == j.k0, ends = k + 1 == j.k1 || (PARTED && (k + 1) % PART == 0);
+                const bool begins = PARTED ? (k - j.k0) % PART == 0 : k == j.k0, ends = k + 1 == j.k1 || (PARTED && (k + 1 - j.k0) % PART == 0);
                 if (begins) {
                     a = it & 1;
                     dacc = tmem + (uint32_t)(a * COLS);
@@ -692,7 +695,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     ++it;
                     if constexpr (PARTED) {
 #pragma unroll 1
-                        for (int q = 1; q < (j.k1 + PART - 1) / PART && ok; ++q, ++it) {
+                        for (int q = 1; q < (j.k1 - j.k0 + PART - 1) / PART && ok; ++q, ++it) {
                             wait(it);
                             if (!ok) break;
                             const uint32_t at = from + (uint32_t)((it & 1) * COLS);

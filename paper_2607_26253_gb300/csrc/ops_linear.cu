@@ -142,6 +142,8 @@ void gradient(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand
     p.a_rows = CTAS == 1 ? (int)lin_up(R, 8) : kLinRows;
     const CUtensorMap xk = rows_map(x, p.a_rows), wk = rows_map(w, kLinCols / CTAS), dzk = rows_map(dz, p.a_rows), dzs = rows_map(dz, kLinRows);
     const CUtensorMap dzm = rows_map(dz, kLinK), wn = rows_map(w, kLinK), xn = rows_map(low, kLinK), out = dw.p ? rows_map(dw, kLinRows) : dzs;
+    // (up to 128 rows a piece is not that long)
+    const bool many = CTAS == 2 && std::max(lin_up(R, kLinK), lin_up(std::min(q.piece, V), kLinK) / q.splits) > (int64_t)kLinLong * kLinK;
     for (int v = 0; v < V; v += q.piece) {
         p.v0 = v;
         p.cols = V - v < q.piece ? V - v : q.piece;
@@ -154,7 +156,8 @@ void gradient(cudaStream_t s, int sms, void *ws, const LinPlan &q, const Operand
         p.out = static_cast<uint16_t *>(const_cast<void *>(dw.p));
         p.out_stride = dw.stride;
         p.wide = (reinterpret_cast<uintptr_t>(dw.p) & 31) == 0 && dw.stride % 16 == 0;
-        if (CTAS == 1 || R <= kLinStagedRows) launch<LIN_GRAD, CTAS, TYPE, true>(s, sms, true, dzk, wn, dzm, xn, out, p);
+        if (many) launch<LIN_GRAD, 2, TYPE, false, true>(s, sms, true, dzk, wn, dzm, xn, out, p);
+        else if (CTAS == 1 || R <= kLinStagedRows) launch<LIN_GRAD, CTAS, TYPE, true>(s, sms, true, dzk, wn, dzm, xn, out, p);
         else launch<LIN_GRAD, CTAS, TYPE, CTAS == 1>(s, sms, true, dzk, wn, dzm, xn, out, p);
     }
     const LinOutParams o{p.head, R, d, q.splits, q.rows_cap, at<int>(ws, q.pos), p.kexp, p.acc, p.delta, tokens, V, static_cast<const uint16_t *>(w.p), w.stride,

@@ -679,3 +679,50 @@ def test_gradients_of_more_rows_than_are_sorted_together(pkg):
     mag = dz.abs().t() @ h.double().abs()
     assert bool(((dw.double() - want).abs() <= (_chain(R) + HALF["bf16"]) * mag + HALF["bf16"] * want.abs()).all())
     assert float((dw.double() - want).norm()) <= 1.5 * HALF["bf16"] * float(want.norm())
+
+
+@pytest.mark.parametrize("typ,R", [("bf16", 1 << 19), ("fp16", 1 << 18)])
+def test_weights_gradient_of_very_many_rows(pkg, typ, R):
+    """Every row all but certain of the last token, whose dz is -g in each, and sampled from the others: dW of the last token is minus the sum of all g h, which
+    are positive.  Bound: 1 - p below 2^-30, one rounding of the result, 2^-12 of the sum (parts of 4,096 rows lose at most 3 steps of 2^-24 each 16)."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(R)
+    d, V = 64, 300
+    h = (torch.randint(128, 256, (R, d), generator=gen, device="cuda") * 2.0 ** -7).to(_dtype(typ))
+    h *= 2.0 ** -8  # (sums within fp16)
+    w = torch.zeros((V, d), dtype=h.dtype, device="cuda")
+    w[V - 1] = 128.0  # a logit of 48
+    tok = torch.randint(0, V - 1, (R,), generator=gen, device="cuda", dtype=torch.int32)
+    g = torch.randint(128, 256, (R,), generator=gen, device="cuda").float() * 2.0 ** -7
+    o = pkg.linear_logprobs(h, w, tok)
+    assert float(o.entropy.max()) < 1e-6
+    dh, dw = pkg.linear_logprobs_backward(h, w, tok, o.stats, o.entropy, g)
+    want = -(g.double()[:, None] * h.double()).sum(0)
+    assert bool(((dw[V - 1].double() - want).abs() <= (HALF[typ] + 2.0 ** -12) * want.abs()).all()), float((dw[V - 1].double() / want).mean())
+    some = torch.arange(0, R, 4099, device="cuda")
+    assert torch.equal(dh[some], -w[V - 1] * g[some, None].to(h.dtype))
+
+
+def test_gradient_of_a_very_large_vocabulary(pkg):
+    """Half a million tokens alike: dH of a row, whose token is none of the likely ones, is minus the mean of their weights, which are positive."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    R, d, V = 150, 20480, 780000
+    h = torch.zeros((R, d), dtype=torch.float16, device="cuda")
+    h[:, 0] = 1
+    w = (torch.randint(1024, 2048, (V, d), generator=gen, device="cuda", dtype=torch.int16)).to(torch.float16).mul_(2.0 ** -10)
+    w[:, 0] = 0
+    w[5, 0] = -60
+    tok, g = _i32(np.full(R, 5)), _f32(np.full(R, 2.0))
+    o = pkg.linear_logprobs(h, w, tok)
+    dh, _ = pkg.linear_logprobs_backward(h, w, tok, o.stats, o.entropy, g, grad_weight=False)
+    total = torch.zeros(d, dtype=torch.float64, device="cuda")
+    for a in range(0, V, 20000):
+        total += w[a:a + 20000].double().sum(0)
+    want = 2 * (w[5].double() - (total - w[5].double()) / (V - 1))[1:]
+    # dz of a token: 2 / (V - 1) in fp16, whose rounding all of them share
+    dz = torch.tensor(2.0 * 2 ** 20 / (V - 1)).half().double() * 2.0 ** -20
+    off = float(dz * (V - 1) / 2 - 1)
+    mean = (2 * (total - w[5].double()) / (V - 1))[1:]
+    assert bool(((dh[0, 1:].double() - (want - off * mean)).abs() <= HALF["fp16"] * want.abs() + (2.0 ** -12 + 300 * U) * mean).all()), float((dh[0, 1:].double() - (want - off * mean)).mean())
+    assert torch.equal(dh[0], dh[R - 1])
