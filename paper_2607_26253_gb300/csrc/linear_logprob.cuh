@@ -362,6 +362,8 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = CTAS == 2 ? (int)cluster_rank() : 0;
     int *err = &p.head->err;
+    // (a tile of dW's adds its rows' corrections one after the other: some 1 us each, 4 s where 2^22 rows have one token)
+    const uint64_t limit = kWaitLimitNs + (MODE == LIN_GRAD ? (uint64_t)p.R * 4096 : 0);
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(&S.full[s], 1);
@@ -404,7 +406,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             const uint32_t bytes = (uint32_t)((mn_a ? kLinBlock : p.a_rows * kLinK * 2) + bn * kLinK * 2) * CTAS;
 #pragma unroll 1
             for (int k = j.k0; k < j.k1; ++k) {
-                if (loads >= (uint32_t)STAGES) ok = __all_sync(0xffffffffu, mbar_wait(&S.empty[s], ph, err) && !*ab);
+                if (loads >= (uint32_t)STAGES) ok = __all_sync(0xffffffffu, mbar_wait(&S.empty[s], ph, err, limit) && !*ab);
                 if (!ok) break;
                 if (elect_one()) {
                     uint8_t *a = ring + s * STAGE, *b = a + kLinBlock;
@@ -439,7 +441,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             if (rank == 0)
                 for (uint32_t q = 0; q < (uint32_t)STAGES && q < loads; ++q) {
                     const uint32_t last = (loads - 1 - q) / STAGES * STAGES + q;
-                    mbar_wait(&S.full[q], (last / STAGES) & 1, err);
+                    mbar_wait(&S.full[q], (last / STAGES) & 1, err, limit);
                 }
         }
     } else if (warp == 1) {
@@ -464,11 +466,11 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 if (begins) {
                     a = it & 1;
                     dacc = tmem + (uint32_t)(a * COLS);
-                    if (it >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_empty[a], (uint32_t)((it / 2 - 1) & 1), err) && !*ab);
+                    if (it >= 2) ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_empty[a], (uint32_t)((it / 2 - 1) & 1), err, limit) && !*ab);
                     if (!ok) break;
                     ++it;
                 }
-                ok = __all_sync(0xffffffffu, mbar_wait(&S.full[s], ph, err) && !*ab);
+                ok = __all_sync(0xffffffffu, mbar_wait(&S.full[s], ph, err, limit) && !*ab);
                 if (!ok) break;
                 tc_fence_after();
                 if (elect_one()) {
@@ -490,7 +492,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         if (!ok) *ab = 1;
         if (rank == 0) {
             if (elect_one()) lin_commit_here<CTAS>(&S.drain);
-            mbar_wait(&S.drain, 0, err);  // every MMA has retired before tensor memory is released
+            mbar_wait(&S.drain, 0, err, limit);  // every MMA has retired before tensor memory is released
         }
     } else {
         // ------------------------------------------------------------ epilogues
@@ -506,7 +508,7 @@ lin_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             }
         };
         auto wait = [&](int it) {  // for the it-th accumulator
-            ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_full[it & 1], (uint32_t)(it / 2 & 1), err) && !*ab);
+            ok = __all_sync(0xffffffffu, mbar_wait(&S.acc_full[it & 1], (uint32_t)(it / 2 & 1), err, limit) && !*ab);
             tc_fence_after();
         };
         if constexpr (MODE == LIN_SCORE) {

@@ -726,3 +726,22 @@ def test_gradient_of_a_very_large_vocabulary(pkg):
     mean = (2 * (total - w[5].double()) / (V - 1))[1:]
     assert bool(((dh[0, 1:].double() - (want - off * mean)).abs() <= HALF["fp16"] * want.abs() + (2.0 ** -12 + 300 * U) * mean).all()), float((dh[0, 1:].double() - (want - off * mean)).mean())
     assert torch.equal(dh[0], dh[R - 1])
+
+
+def test_millions_of_rows_of_one_token(pkg):
+    """Their roundings are put right one after the other, which takes a CTA seconds while it has another tile to do: no wait of its may run out meanwhile.  Every third row
+    weighs -1, the others 1/2, and all hidden states are 1, so that next to nothing is left.  Bound: parts of 4,096 rows lose at most 4 steps of 2^-24 each 16 of a part's
+    sum of some 1; corrections, of 2^-10 and less, come in threes of no sum; the result's rounding."""
+    import torch
+    R, d, V = 1 << 21, 4872, 1000
+    g = torch.full((R,), 0.5, device="cuda")
+    g[::3] = -1.0
+    h, w = torch.ones((R, d), dtype=torch.bfloat16, device="cuda"), torch.zeros((V, d), dtype=torch.bfloat16, device="cuda")
+    tok = torch.full((R,), 7, dtype=torch.int32, device="cuda")
+    stats, entropy = torch.zeros((R, 2), device="cuda"), torch.zeros(R, device="cuda")
+    stats[:, 1] = float(np.log(V))
+    _, dw = pkg.linear_logprobs_backward(h, w, tok, stats, entropy, g, grad_hidden=False)
+    want = torch.full((V,), -float(g.double().sum()) / V, dtype=torch.float64)
+    want[7] += float(g.double().sum())
+    assert not dw.isnan().any()
+    assert bool(((dw.double().cpu() - want[:, None]).abs() <= HALF["bf16"] * want[:, None].abs() + 0.05).all()), (dw[7], want[7])
