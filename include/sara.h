@@ -477,7 +477,7 @@ SARA_API int sara_logprobs_backward(const void *logits, int64_t row_stride, int3
  * The same scores from the last hidden states, for which no logits are stored: z = scale H W^T, H [R][d] the rows' hidden states,
  * W [V][d] the vocabulary's weights (an lm_head as it lies in memory).  `type` SARA_BF16 or SARA_FP16, of H, W and their gradients; d a
  * multiple of 8 up to 65,536, R at most 2^22, V at most 2^24; rows of H, W and the gradients stride elements apart (multiples of 8, at least d), all
- * of them 16-byte aligned; scale > 0 and finite (1 / temperature).  Device pointers, not waited for, nothing allocated; the calls may be
+ * of them 16-byte aligned; scale > 0 and at most 2^127 (1 / temperature).  Device pointers, not waited for, nothing allocated; the calls may be
  * captured.  Products are exact and summed in fp32.
  * workspace: sara_linear_logprobs_workspace_bytes(R, d, V, backward) bytes of device scratch, 256-byte aligned, whose first 256 bytes are
  * zero on first use and left zero where they have to be; calls that share one must not overlap.  (12 bytes a row and 256 tokens for the

@@ -3,7 +3,6 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
-#include <cmath>
 #include <type_traits>
 
 #include "../../include/sara.h"
@@ -38,7 +37,7 @@ CUtensorMap rows_map(const Operand &x, int box) {
 
 bool sizes_ok(int type, int R, int d, int V, float scale) {
     return (type == SARA_BF16 || type == SARA_FP16) && R >= 0 && R <= (1 << 22) && d >= 8 && d <= 65536 && d % 8 == 0 && V >= 1 &&
-           V <= (1 << 24) && scale > 0.f && std::isfinite(scale);
+           V <= (1 << 24) && scale > 0.f && scale <= 0x1p127f;  // (log2(e) times it is finite)
 }
 
 template <int MODE, int CTAS, int TYPE, bool STAGED, bool LONG = false>

@@ -142,3 +142,9 @@ def test_binding_refuses_more_rows_than_the_calls_count(pkg):  # noqa: F811
         assert "2^31" in _refused(pkg, pkg.linear_logprobs_workspace, R, d, V)
     codes, scales = pkg.kv8_cache(4, 2, 64, device="meta")
     assert "2^31" in _refused(pkg, pkg.attention_shared_kv8, new(many, 8, 64), codes, scales, i32(many, 1), i32(many), i32(2), i32(1))
+
+
+def test_scales_whose_exponents_leave_fp32_are_refused(lib):  # noqa: F811
+    for scale, rc in ((2.0 ** 127, 0), (1.0000002 * 2.0 ** 127, -1), (3.4e38, -1), (1e-45, 0)):
+        assert lib.sara_linear_logprobs(A, 64, A, 64, 0, 0, 64, 100, A, scale, A, A, A, A, 1 << 40, None) == rc, scale
+        assert lib.sara_linear_logprobs_backward(A, 64, 2 * A, 64, 0, 0, 64, 100, A, scale, A, A, A, A, 3 * A, 64, None, 64, A, 1 << 40, None) == rc, scale
