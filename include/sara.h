@@ -425,6 +425,8 @@ SARA_API int sara_attention_decode_kv8(const sara_kv8_cache *cache, int32_t n_se
  * length does not matter for that); positions from prefix[g] on are each sequence's own.  A prefix may end anywhere in a block, and a sequence in
  * its prefix (ctx[i] <= prefix[g], or 0).  Groups of up to two sequences on average, and tables whose rows have room for little (160 MB of codes for
  * large groups, more for small ones), are attended to row by row, which is then faster: each reads the shared positions for itself.
+ * (The room, n_seq * n_kv_heads * max_blocks, stands for the lengths, which the host does not know: max_blocks is best no more than the longest sequence or prefix needs,
+ * in a table whose table_stride may be larger.)
  * Everything else as sara_attention_decode_kv8, but: probabilities of shared positions times their values' scale may be held in fp16, 11 bits,
  * or within 2^-31 of the query's largest such product, and a NaN among e4m3 codes or a negative scale of keys, of which sara_kv8_write writes
  * none, may make all of a row NaN that attends to its block of 32.
@@ -478,7 +480,7 @@ SARA_API int sara_logprobs_backward(const void *logits, int64_t row_stride, int3
  * W [V][d] the vocabulary's weights (an lm_head as it lies in memory).  `type` SARA_BF16 or SARA_FP16, of H, W and their gradients; d a
  * multiple of 8 up to 65,536, R at most 2^22, V at most 2^24; rows of H, W and the gradients stride elements apart (multiples of 8, at least d), all
  * of them 16-byte aligned; scale > 0 and at most 2^127 (1 / temperature).  Device pointers, not waited for, nothing allocated; the calls may be
- * captured.  Products are exact and summed in fp32.
+ * captured.  Products are exact and summed in fp32, up to 40,960 in a row: the tensor core's sums of one sign lose 2 to 4 times 2^-24 of themselves each 16 products.
  * workspace: sara_linear_logprobs_workspace_bytes(R, d, V, backward) bytes of device scratch, 256-byte aligned, whose first 256 bytes are
  * zero on first use and left zero where they have to be; calls that share one must not overlap.  (12 bytes a row and 256 tokens for the
  * scores; for the gradient the rows, the gradients of a piece of the vocabulary, up to 384 MB or
@@ -504,7 +506,8 @@ SARA_API int sara_linear_logprobs(const void *hidden, int64_t hidden_stride, con
  * in `type` (in fp16 times a power of two of the row, so that tokens down to p = 2^-27 keep all its bits; hidden
  * states enter grad_weight with all theirs down to (|grad_logprob| + 16 |grad_entropy|) |hidden| = 2^-27 of the largest such product, and are off by
  * 2^-38 of it at most below that).  stats and entropy as sara_linear_logprobs gave them.  grad_logprob and grad_entropy [R] fp32, each may be NULL (0); entropy is wanted with grad_entropy,
- * tokens with grad_logprob.  grad_hidden or grad_weight may be NULL (not computed); they overlap neither each other nor hidden and weight.
+ * tokens with grad_logprob.  grad_hidden or grad_weight may be NULL (not computed); their memory, from the first row to the end of
+ * the last with what is between, meets neither each other's nor that of hidden and weight.
  * Rows of padding get 0 and add nothing to grad_weight, whatever their hidden states hold; a token >= V, a NaN or +inf among the logits makes
  * the row NaN, and with it grad_weight.  Sums are in a fixed order: results repeat bit for bit.
  */

@@ -2,9 +2,9 @@
 // computed once for all of a group's queries, each sequence's own by the decode attention, and the two are joined,
 //     out = (2^(m1 - m) o1 + 2^(m2 - m) o2) / (2^(m1 - m) l1 + 2^(m2 - m) l2),   m = max(m1, m2).
 // Bound by reading the shared positions once (2 hd bytes each) up to some 128 queries a KV head, by the tensor cores beyond.  What it comes to
-// (us, 32 / 8 heads of 128 dims in e4m3): 8 groups of 64 with 32,768 positions in common and 128 each of their own 411, of which the prefix kernel
+// (us, 32 / 8 heads of 128 dims in e4m3): 8 groups of 64 with 32,768 positions in common and 128 each of their own 412, of which the prefix kernel
 // 355 (a page of 128 queries 3,200 cycles; its products alone would take 1,000, its exponentials 1,024: each page is a chain of scores,
-// maximum, exponentials and product whose parts wait for one another); 64 groups of 8 with 1,024 and 512: 171, of which the prefix kernel 70
+// maximum, exponentials and product whose parts wait for one another); 64 groups of 8 with 1,024 and 512: 172, of which the prefix kernel 70
 // (27 pages of 3 or 4 units a CTA: 2,800 cycles a page, some 9,000 a change of units and 10,000 until the first page) and each
 // sequence's own positions 89.
 // Rows that save little by it attend by themselves (see the entry point).
@@ -18,7 +18,8 @@
 //     made while this one's softmax goes on, two pages of scores in turn;
 //   - 8 have the softmax, two threads a query with 64 positions each: maximum, exponentials, P back to tensor memory.
 // 8 x 64, us, as they were found: codes made fp16 by the softmax's warps 543, by warps of their own 534, no waits for scales and maxima 491, masks only where a
-// query has some 424, scales prepared once a page 414.
+// query has some 424, scales prepared once a page 414, queries read once 410; 412 with what makes any scale behind a mask safe (blocks looked at
+// one by one as they are converted: 423).
 // Scales: K's is a factor of the scores; V's of P, so P times V's scale, relative to the query's largest such product so far (2^R),
 // is what enters the product, in fp16: 11 bits, or within 2^-31 of the largest.  m and R are raised only when a score or a product
 // passes them by 2^8: most pages then need no rescaling of O.

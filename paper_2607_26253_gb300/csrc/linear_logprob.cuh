@@ -4,9 +4,9 @@
 //             a, sum 2^y and sum 2^y y with y = (acc - a) scale log2(e), which a second kernel joins over the tiles
 //   gradient: the vocabulary goes by in pieces.  A piece's logits are made again, its dZ = g (1[v = token] - p) - g' p (log p + H),
 //             [R][piece], is stored in the operands' type, and feeds both products, dH += dZ W and dW = dZ^T H.
-// Bound by the tensor cores from some 300 rows on, by reading W below.  us of a call (and of its floor): scores of 1 x 2,048 x 151,936 115 (92), of
-// 26 x 1,536 x 151,936 93 (69), of 4,096 x 1,536 x 151,936 1,010 (910); gradient of 301 x 2,048 x 32,001 in fp16 202 (56: 106 with rows in
-// whole tiles), of 4,096 x 1,536 x 151,936 3,475 (2,730; 3,013 at the rate that the power cap leaves).
+// Bound by the tensor cores from some 300 rows on, by reading W below.  us of a call in a CUDA graph (and of its floor): scores of 1 x 2,048 x 151,936 115 (92),
+// of 26 x 1,536 x 151,936 93 (69), of 4,096 x 1,536 x 151,936 1,016 (910; 1,120 back to back); gradient of 301 x 2,048 x 32,001 in fp16 205 (56: 106 with rows
+// in whole tiles), of 4,096 x 1,536 x 151,936 3,510 (2,730; 3,013 at the rate that the power cap leaves; 3,570 back to back).
 //
 // One persistent kernel does all the products (D = A B^T, fp32 in tensor memory): 256 columns, 128 rows a CTA, K in chunks of 64.
 // With more than 128 rows two CTAs (a cluster) share a tile of 256 x 256, each bringing half of A's rows and half of B's: 64 bytes
@@ -15,8 +15,8 @@
 // Rows of padding (token < 0) are left out: the live rows are gathered first, so that they cost nothing and their contents,
 // whatever they are, reach nothing.
 //
-// The tensor core cuts its sums off: one to two steps of fp32 each 16 products, all towards zero.  A logit's products are therefore
-// summed in parts, which the epilogue adds.
+// The tensor core cuts its sums off, all towards zero: sums of one sign lost 1.4 to 4 times 2^-24 of themselves each 16 products.  Long sums are therefore
+// made in parts, which the epilogue adds.
 // dZ enters the products in 16 bits.  Its largest element by far is mostly the token's own: what that one's rounding left off is
 // kept (delta) and added to both gradients in fp32.
 //

@@ -212,7 +212,8 @@ def attention_shared_kv8_workspace(n_seq: int, n_groups: int, n_heads: int, n_kv
 def attention_shared_kv8(q, codes, scales, table, ctx, group_start, prefix, first=None, workspace=None, out=None, lse=None, status=None):
     """attention_decode_kv8 for groups of sequences whose first positions are the same (see sara_attention_shared_kv8): sequences
     group_start[g] .. group_start[g + 1] - 1 share positions p < prefix[g], which are read once, through the table row of the first of
-    them.  group_start [n_groups + 1] and prefix [n_groups] int32; the rest as there."""
+    them.  group_start [n_groups + 1] and prefix [n_groups] int32; the rest as there.  A table's columns that no sequence or prefix needs are best
+    left out, table[:, :needed]: rows with room for little are attended to one by one, which is then faster."""
     cache, n, kvh, hd, dev = _kv8(codes, scales, table)
     typ, shape = _types.get(q.dtype, 2), q.shape
     if typ == 2 or len(shape) != 3 or shape[0] != n or shape[2] != hd or q.get_device() != dev:
